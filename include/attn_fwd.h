@@ -75,7 +75,8 @@ typedef enum {
     ATTN_ERR_DEVICE_TIMEOUT = 9,       /* a kernel gave up on a bounded on-chip wait */
     ATTN_ERR_WORKSPACE = 10,           /* workspace missing, misaligned or too small */
     ATTN_ERR_STATIC_CAPACITY = 11,     /* problem does not fit the library's built-in staging buffer */
-    ATTN_ERR_COUNTER_SLOTS = 12        /* no work counter left for this launch (see "Streams and CUDA graphs") */
+    ATTN_ERR_COUNTER_SLOTS = 12,       /* no work counter left for this launch (see "Streams and CUDA graphs") */
+    ATTN_ERR_DEVICE_INDEX = 13         /* a kernel met a page, position or length out of range (attn_last_device_status) */
 } attn_status_t;
 
 /*
@@ -242,6 +243,104 @@ int attn_bwd(const void* q, const void* k, const void* v, const void* o, const f
 size_t attn_bwd_workspace_bytes(int B, int H, int Sq);
 
 /*
+ * attn_qk_norm_rope -- from a projection's output to the tensors that attention reads, in one pass: per-head
+ * normalisation of Q and K, rotation by position, and the change of layout to [B, heads, S, D].
+ *
+ *     n = x / sqrt(mean(x^2) + eps) * weight        (over the D values of one head),
+ *     y: pair i of the first R values of n turned by the angle whose cosine and sine are cos_sin[pos][i] and
+ *        cos_sin[pos][R/2 + i]:  (a, b) -> (a cos - b sin, b cos + a sin);  the pair is (i, i + R/2), or (2i, 2i + 1)
+ *        with interleaved != 0;  values R .. D-1 are not rotated.
+ *
+ * q, k, v  : device, 16-bit `dtype`, 16-byte aligned: token s of sequence b, head h begins at element
+ *            b * batch + s * token + h * head of its tensor (views of one fused projection); the D values of a head are
+ *            contiguous.  v is copied without arithmetic; v and v_out may both be NULL.
+ * in_strides: HOST array of 9: {batch, token, head} of q, of k, of v, in elements, each a multiple of 8.
+ * q_weight, k_weight: device, [D], 16-byte aligned, of `dtype` (weight_f32 == 0) or fp32 (weight_f32 != 0).
+ *            NULL: that tensor is not normalised.
+ * cos_sin  : device, fp32 [table_len][R], 16-byte aligned: R/2 cosines, then R/2 sines per position.  R is a multiple of 16,
+ *            0 <= R <= D; R == 0: no rotation (cos_sin is not read).
+ * positions: device int32 [B][S], or NULL: the token's index s (then S <= table_len).  A position outside
+ *            [0, table_len) gives NaN in that token's q and k rows and ATTN_ERR_DEVICE_INDEX in the device status.
+ * q_out [B,H,S,D]; k_out, v_out [B,Hkv,S,D]: device, contiguous, 16-byte aligned.
+ * D in {64, 128, 256}; H and Hkv are independent.  B * S == 0 is a successful no-op.  Arithmetic in fp32, rounded once.
+ */
+int attn_qk_norm_rope(const void* q, const void* k, const void* v, const long long* in_strides, const void* q_weight,
+                      const void* k_weight, int weight_f32, const float* cos_sin, int table_len, int R, int interleaved,
+                      const int* positions, float eps, void* q_out, void* k_out, void* v_out, int B, int S, int H, int Hkv,
+                      int D, int dtype, void* stream);
+
+/*
+ * attn_qk_norm_rope_bwd -- gradients of attn_qk_norm_rope.
+ * dq [B,H,S,D]; dk, dv [B,Hkv,S,D]: device, contiguous, the gradients of the three outputs (as attn_bwd writes them).
+ * q, k, in_strides (6: q, k), weights, table, positions, eps: as in the forward call.
+ * dq_in, dk_in, dv_in, out_strides (9): gradients of q, k, v in the layout of the projection (written; rows must not
+ *            overlap).  dv and dv_in may both be NULL.  In place of q and k NULL may stand where that weight is NULL.
+ * dq_weight, dk_weight: device, fp32 [D], 4-byte aligned (written; sums over all rows and heads in a fixed order, so results
+ *            repeat); NULL allowed where the weight is NULL, otherwise required.
+ * workspace: device, 256-byte aligned, at least attn_qk_norm_rope_bwd_workspace_bytes(D) bytes, or ATTN_ERR_WORKSPACE.
+ *            Two calls that may run at the same time need one each.
+ * B * S == 0 writes zero weight gradients.  A position out of range gives NaN in its rows and in the weight gradients.
+ */
+int attn_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const void* q, const void* k,
+                          const long long* in_strides, const void* q_weight, const void* k_weight, int weight_f32,
+                          const float* cos_sin, int table_len, int R, int interleaved, const int* positions, float eps,
+                          void* dq_in, void* dk_in, void* dv_in, const long long* out_strides, float* dq_weight,
+                          float* dk_weight, int B, int S, int H, int Hkv, int D, int dtype, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace attn_qk_norm_rope_bwd needs (0 for an unsupported head dim). */
+size_t attn_qk_norm_rope_bwd_workspace_bytes(int D);
+
+/*
+ * Paged key/value cache.  k_cache and v_cache hold num_pages pages of page_size key (value) rows for each of Hkv heads:
+ * the row of slot s, head h in page p begins at element p * page + h * head + s * slot of its cache, cache_strides =
+ * HOST array {page, head, slot} of k_cache, then of v_cache (elements, multiples of 8; any order of the axes).  Key j of
+ * sequence b lies in page block_table[b * table_stride + j / page_size], slot j % page_size.  page_size is a power of
+ * two; max_pages * page_size <= 2^31 - 1, max_pages being the entries of a row of block_table (device int32).
+ * Entries that no key of a sequence needs are not read; pages may be shared by sequences.
+ *
+ * attn_paged_append -- new tokens of n_seqs sequences: q, k normalised and rotated as by attn_qk_norm_rope at the
+ * token's position in its sequence, k and v written into the cache.
+ * q [tokens, H, D], k, v [tokens, Hkv, D]: device; in_strides: HOST array of 6, {token, head} of q, k, v.  q and q_out may
+ *            both be NULL (keys and values only).
+ * seq_lens : device int32 [n_seqs], the sequences' lengths WITH the new tokens.
+ * cu_seqlens: device int32 [n_seqs + 1], first token of each sequence's new ones and their end; NULL: one new token per
+ *            sequence, tokens == n_seqs.  Tokens behind cu_seqlens[n_seqs] and tokens of sequences of length 0 are padding: their
+ *            rows of q_out and the cache stay as they were.
+ * q_out    : device, contiguous [tokens, H, D].
+ * A token whose position falls below 0, beyond the block table or the rotation table, or whose page is not in
+ * [0, num_pages), is skipped in the same way and reported as ATTN_ERR_DEVICE_INDEX in the device status.
+ * The page slots written by one call must be different ones (a page that two sequences append to holds rows of either).
+ */
+int attn_paged_append(const void* q, const void* k, const void* v, const long long* in_strides, const void* q_weight,
+                      const void* k_weight, int weight_f32, const float* cos_sin, int table_len, int R, int interleaved,
+                      float eps, void* q_out, void* k_cache, void* v_cache, const long long* cache_strides, int num_pages,
+                      int page_size, const int* block_table, long long table_stride, int max_pages, const int* seq_lens,
+                      const int* cu_seqlens, int n_seqs, int tokens, int H, int Hkv, int D, int dtype, void* stream);
+
+/*
+ * attn_paged_decode -- attention of one new token per sequence over a paged cache: row b of q sees the keys
+ * j < seq_lens[b] of its sequence; with window > 0 only those with j >= seq_lens[b] - window or j < sinks (the newest
+ * token's view under attn_fwd_window); window == 0: all.
+ * q, o [B,H,D], lse [B,H]: device, contiguous; H % Hkv == 0 (grouped heads as in attn_fwd_gqa); D in {64, 128, 256}.
+ * seq_lens : device int32 [B].  Length 0 (or less) gives O = 0, LSE = -inf.  A length beyond max_pages * page_size is cut to
+ *            that, a visible key whose page is not in [0, num_pages) counts as hidden, and either is reported as
+ *            ATTN_ERR_DEVICE_INDEX in the device status.  Pages and slots of hidden keys are never read.
+ * workspace: device, 256-byte aligned, at least attn_paged_decode_workspace_bytes(H, Hkv, D) bytes (whatever the lengths are), or
+ *            ATTN_ERR_WORKSPACE.  Two calls that may run at the same time need one each.
+ * The lengths and the table are read on the device, so a captured call may be replayed with new ones.  The result does
+ * not depend on timing (no atomics).  The key axis is cut evenly over the GPU whatever the lengths are; the cut depends on
+ * all lengths of the batch, so a sequence's result may differ in its last bits when other sequences' lengths change.
+ */
+int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, const long long* cache_strides, int num_pages,
+                      int page_size, const int* block_table, long long table_stride, int max_pages, const int* seq_lens,
+                      void* o, float* lse, int B, int H, int Hkv, int D, float scale, int window, int sinks, int dtype,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace attn_paged_decode needs (0 for an invalid shape). */
+size_t attn_paged_decode_workspace_bytes(int H, int Hkv, int D);
+
+/*
  * attn_fwd_simt -- same operator, same arguments, same conventions, computed by a plain
  * CUDA-core kernel (one warp per query row, fp32 arithmetic, online softmax).  It is one to
  * two orders of magnitude slower than attn_fwd and exists as an on-device cross-check that
@@ -318,7 +417,9 @@ int attn_query_support(int D, int dtype, int causal);
 
 /* Synchronises `stream`, then returns and clears the device-side status word of the current
  * device: ATTN_OK, or ATTN_ERR_DEVICE_TIMEOUT if any kernel since the last call gave up on a
- * bounded wait (its output is then undefined).  ATTN_ERR_CUDA if the synchronisation fails. */
+ * bounded wait (its output is then undefined), or ATTN_ERR_DEVICE_INDEX if one met an index out of
+ * range in its device-side arguments (what it did instead is said at the entry point).
+ * ATTN_ERR_CUDA if the synchronisation fails. */
 int attn_last_device_status(void* stream);
 
 /* Static, human-readable name of a status code. */

@@ -21,12 +21,14 @@ STATUS_NAMES = {
     3: "ATTN_ERR_UNSUPPORTED_HEAD_DIM", 4: "ATTN_ERR_UNSUPPORTED_DTYPE", 5: "ATTN_ERR_MISALIGNED",
     6: "ATTN_ERR_BAD_SCALE", 7: "ATTN_ERR_UNSUPPORTED_ARCH", 8: "ATTN_ERR_CUDA",
     9: "ATTN_ERR_DEVICE_TIMEOUT", 10: "ATTN_ERR_WORKSPACE", 11: "ATTN_ERR_STATIC_CAPACITY",
-    12: "ATTN_ERR_COUNTER_SLOTS",
+    12: "ATTN_ERR_COUNTER_SLOTS", 13: "ATTN_ERR_DEVICE_INDEX",
 }
 
 # every symbol include/attn_fwd.h declares
 EXPORTS = ["attn_bwd", "attn_bwd_workspace_bytes", "attn_fwd", "attn_fwd_gqa", "attn_fwd_partial", "attn_combine", "attn_combine_gather", "attn_fwd_qkv_dims", "attn_fwd_splitkv", "attn_fwd_splitkv_workspace_bytes", "attn_fwd_fp8", "attn_fwd_simt", "attn_fwd_host", "attn_fwd_host_workspace_bytes",
            "attn_fwd_host_static", "attn_fwd_host_static_capacity",
+           "attn_qk_norm_rope", "attn_qk_norm_rope_bwd", "attn_qk_norm_rope_bwd_workspace_bytes", "attn_paged_append", "attn_paged_decode",
+           "attn_paged_decode_workspace_bytes",
            "attn_query_support", "attn_last_device_status", "attn_status_string"]
 
 _lib = None
@@ -86,6 +88,19 @@ def load() -> ctypes.CDLL:
     lib.attn_fwd_host_static.argtypes = sig
     lib.attn_fwd_host_static_capacity.restype = ctypes.c_size_t
     lib.attn_fwd_host_static_capacity.argtypes = []
+    ll, sz = ctypes.c_longlong, ctypes.c_size_t
+    lib.attn_qk_norm_rope.restype = i
+    lib.attn_qk_norm_rope.argtypes = [vp] * 6 + [i, vp, i, i, i, vp, f, vp, vp, vp] + [i] * 6 + [vp]
+    lib.attn_qk_norm_rope_bwd.restype = i
+    lib.attn_qk_norm_rope_bwd.argtypes = [vp] * 8 + [i, vp, i, i, i, vp, f] + [vp] * 6 + [i] * 6 + [vp, sz, vp]
+    lib.attn_qk_norm_rope_bwd_workspace_bytes.restype = sz
+    lib.attn_qk_norm_rope_bwd_workspace_bytes.argtypes = [i]
+    lib.attn_paged_append.restype = i
+    lib.attn_paged_append.argtypes = [vp] * 6 + [i, vp, i, i, i, f] + [vp] * 4 + [i, i, vp, ll, i, vp, vp] + [i] * 6 + [vp]
+    lib.attn_paged_decode.restype = i
+    lib.attn_paged_decode.argtypes = [vp] * 4 + [i, i, vp, ll, i] + [vp] * 3 + [i] * 4 + [f, i, i, i, vp, sz, vp]
+    lib.attn_paged_decode_workspace_bytes.restype = sz
+    lib.attn_paged_decode_workspace_bytes.argtypes = [i] * 3
     lib.attn_query_support.restype = i
     lib.attn_query_support.argtypes = [i, i, i]
     lib.attn_last_device_status.restype = i
@@ -340,6 +355,260 @@ def attn_bwd(q, k, v, o, lse, dout, scale: float, causal: bool = False, dq=None,
     if rc != 0:
         raise AttnError(rc, "attn_bwd")
     return dq, dk, dv
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _row_strides(tensors, axes):
+    """Element strides of the given axes of each tensor (0 for None) as a host array, last axis contiguous."""
+    vals = []
+    for t in tensors:
+        if t is None:
+            vals += [0] * len(axes)
+            continue
+        st = t.stride()
+        if st[-1] != 1 and t.shape[-1] > 1:
+            raise ValueError("the values of a head must be contiguous")
+        vals += [st[a] for a in axes]
+    return (ctypes.c_longlong * len(vals))(*vals)
+
+
+def _check_on(device, dtype, **tensors):
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if t.device != device:
+            raise ValueError("%s must lie on %s" % (name, device))
+        if dtype is not None and t.dtype != dtype:
+            raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+
+
+def _check_dense(**tensors):
+    for name, t in tensors.items():
+        if t is not None and not t.is_contiguous():
+            raise ValueError("%s must be contiguous" % name)
+
+
+def _check_shape(name, t, shape):
+    if t is not None and tuple(t.shape) != shape:
+        raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
+
+
+def _check_rope(x, D, q_weight, k_weight, cos_sin):
+    """Weights [D] of one type (x's or fp32) and the table fp32 [positions, R]: (weights are fp32, table length, R)."""
+    f32 = None
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is None:
+            continue
+        if tuple(w.shape) != (D,) or not w.is_contiguous() or w.device != x.device:
+            raise ValueError("%s must be a contiguous [%d] tensor on %s" % (name, D, x.device))
+        if w.dtype != x.dtype and w.dtype != torch.float32:
+            raise TypeError("%s must be %s or float32, got %s" % (name, x.dtype, w.dtype))
+        if f32 is not None and f32 != (w.dtype == torch.float32):
+            raise TypeError("q_weight and k_weight must share one dtype")
+        f32 = w.dtype == torch.float32
+    if cos_sin is None:
+        return int(bool(f32)), 0, 0
+    if cos_sin.dim() != 2 or cos_sin.dtype != torch.float32 or not cos_sin.is_contiguous() or cos_sin.device != x.device:
+        raise ValueError("cos_sin must be a contiguous float32 [positions, R] tensor on %s" % x.device)
+    return int(bool(f32)), cos_sin.shape[0], cos_sin.shape[1]
+
+
+def attn_qk_norm_rope(q, k, v, q_weight, k_weight, cos_sin, positions=None, eps: float = 1e-6, interleaved: bool = False,
+                      q_out=None, k_out=None, v_out=None, stream=None):
+    """Per-head normalisation and rotation of q [B,S,H,D] and k [B,S,Hkv,D] (strided views of a projection, each head
+    contiguous) into the layout that the attention calls read: q_out [B,H,S,D], k_out [B,Hkv,S,D], and v (may be None)
+    copied to v_out [B,Hkv,S,D].  q_weight, k_weight: [D] in q's dtype or float32 (None: not normalised); cos_sin: float32
+    [positions, R], R/2 cosines then R/2 sines per position (None: not rotated); positions: int32 [B,S] (None: 0 .. S-1);
+    interleaved: pairs (2i, 2i+1) instead of (i, i + R/2)."""
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q and k must be [B,S,heads,D]")
+    B, S, H, D = q.shape
+    Hkv = k.shape[2]
+    _check_shape("k", k, (B, S, Hkv, D))
+    _check_shape("v", v, (B, S, Hkv, D))
+    dt = _dtype_code(q)
+    if not q.is_cuda:
+        raise ValueError("q must be a CUDA tensor")
+    _check_on(q.device, q.dtype, k=k, v=v, q_out=q_out, k_out=k_out, v_out=v_out)
+    f32, n_pos, R = _check_rope(q, D, q_weight, k_weight, cos_sin)
+    if positions is not None:
+        _check_shape("positions", positions, (B, S))
+        _check_on(q.device, torch.int32, positions=positions)
+        _check_dense(positions=positions)
+    q_out = torch.empty((B, H, S, D), dtype=q.dtype, device=q.device) if q_out is None else q_out
+    k_out = torch.empty((B, Hkv, S, D), dtype=q.dtype, device=q.device) if k_out is None else k_out
+    if v is None:
+        v_out = None
+    elif v_out is None:
+        v_out = torch.empty((B, Hkv, S, D), dtype=q.dtype, device=q.device)
+    _check_shape("q_out", q_out, (B, H, S, D))
+    _check_shape("k_out", k_out, (B, Hkv, S, D))
+    _check_shape("v_out", v_out, (B, Hkv, S, D))
+    _check_dense(q_out=q_out, k_out=k_out, v_out=v_out)
+    with torch.cuda.device(q.device):
+        rc = load().attn_qk_norm_rope(q.data_ptr(), k.data_ptr(), _ptr(v), _row_strides((q, k, v), (0, 1, 2)), _ptr(q_weight),
+                                      _ptr(k_weight), f32, _ptr(cos_sin), n_pos, R, int(bool(interleaved)), _ptr(positions),
+                                      float(eps), q_out.data_ptr(), k_out.data_ptr(), _ptr(v_out), B, S, H, Hkv, D, dt,
+                                      _stream_ptr(stream))
+    if rc != 0:
+        raise AttnError(rc, "attn_qk_norm_rope")
+    return q_out, k_out, v_out
+
+
+def attn_qk_norm_rope_bwd_workspace_bytes(D) -> int:
+    return int(load().attn_qk_norm_rope_bwd_workspace_bytes(D))
+
+
+def attn_qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positions=None, eps: float = 1e-6,
+                          interleaved: bool = False, dq_in=None, dk_in=None, dv_in=None, workspace=None, stream=None):
+    """Gradients of attn_qk_norm_rope: dq [B,H,S,D], dk, dv [B,Hkv,S,D] (contiguous; dv may be None) are the gradients of its
+    outputs, q [B,S,H,D], k [B,S,Hkv,D] its inputs.  Returns (dq_in [B,S,H,D], dk_in, dv_in [B,S,Hkv,D], dq_weight, dk_weight
+    (float32 [D], None without a weight)).  dq_in, dk_in, dv_in may be given as strided views of one buffer.
+    `workspace`: CUDA uint8 tensor of at least attn_qk_norm_rope_bwd_workspace_bytes(D) bytes (allocated here when None)."""
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q and k must be [B,S,heads,D]")
+    B, S, H, D = q.shape
+    Hkv = k.shape[2]
+    _check_shape("k", k, (B, S, Hkv, D))
+    _check_shape("dq", dq, (B, H, S, D))
+    _check_shape("dk", dk, (B, Hkv, S, D))
+    _check_shape("dv", dv, (B, Hkv, S, D))
+    dt = _dtype_code(q)
+    if not q.is_cuda:
+        raise ValueError("q must be a CUDA tensor")
+    _check_on(q.device, q.dtype, k=k, dq=dq, dk=dk, dv=dv, dq_in=dq_in, dk_in=dk_in, dv_in=dv_in)
+    _check_dense(dq=dq, dk=dk, dv=dv)
+    f32, n_pos, R = _check_rope(q, D, q_weight, k_weight, cos_sin)
+    if positions is not None:
+        _check_shape("positions", positions, (B, S))
+        _check_on(q.device, torch.int32, positions=positions)
+        _check_dense(positions=positions)
+    dq_in = torch.empty((B, S, H, D), dtype=q.dtype, device=q.device) if dq_in is None else dq_in
+    dk_in = torch.empty((B, S, Hkv, D), dtype=q.dtype, device=q.device) if dk_in is None else dk_in
+    if dv is None:
+        dv_in = None
+    elif dv_in is None:
+        dv_in = torch.empty((B, S, Hkv, D), dtype=q.dtype, device=q.device)
+    _check_shape("dq_in", dq_in, (B, S, H, D))
+    _check_shape("dk_in", dk_in, (B, S, Hkv, D))
+    _check_shape("dv_in", dv_in, (B, S, Hkv, D))
+    dqw = None if q_weight is None else torch.empty(D, dtype=torch.float32, device=q.device)
+    dkw = None if k_weight is None else torch.empty(D, dtype=torch.float32, device=q.device)
+    if workspace is None:
+        workspace = torch.empty(max(attn_qk_norm_rope_bwd_workspace_bytes(D), 256), dtype=torch.uint8, device=q.device)
+    with torch.cuda.device(q.device):
+        rc = load().attn_qk_norm_rope_bwd(dq.data_ptr(), dk.data_ptr(), _ptr(dv), q.data_ptr(), k.data_ptr(),
+                                          _row_strides((q, k), (0, 1, 2)), _ptr(q_weight), _ptr(k_weight), f32, _ptr(cos_sin),
+                                          n_pos, R, int(bool(interleaved)), _ptr(positions), float(eps), dq_in.data_ptr(),
+                                          dk_in.data_ptr(), _ptr(dv_in), _row_strides((dq_in, dk_in, dv_in), (0, 1, 2)),
+                                          _ptr(dqw), _ptr(dkw), B, S, H, Hkv, D, dt, workspace.data_ptr(), workspace.numel(),
+                                          _stream_ptr(stream))
+    if rc != 0:
+        raise AttnError(rc, "attn_qk_norm_rope_bwd")
+    return dq_in, dk_in, dv_in, dqw, dkw
+
+
+def _check_cache(x, D, k_cache, v_cache, block_table, seq_lens):
+    """Caches [pages, Hkv, page_size, D] (any strides, rows contiguous), block_table int32 [sequences, max_pages], seq_lens
+    int32 [sequences].  Returns (pages, Hkv, page_size)."""
+    if k_cache.dim() != 4 or k_cache.shape[3] != D or v_cache.shape != k_cache.shape:
+        raise ValueError("k_cache and v_cache must be [pages, Hkv, page_size, %d]" % D)
+    _check_on(x.device, x.dtype, k_cache=k_cache, v_cache=v_cache)
+    _check_on(x.device, torch.int32, block_table=block_table, seq_lens=seq_lens)
+    n, Hkv, page_size, _ = k_cache.shape
+    if seq_lens.dim() != 1 or block_table.dim() != 2 or block_table.shape[0] != seq_lens.shape[0]:
+        raise ValueError("block_table must be [sequences, max_pages] and seq_lens [sequences]")
+    if not seq_lens.is_contiguous() or (block_table.stride(1) != 1 and block_table.shape[1] > 1):
+        raise ValueError("seq_lens and the rows of block_table must be contiguous")
+    return n, Hkv, page_size
+
+
+def attn_paged_append(q, k, v, k_cache, v_cache, block_table, seq_lens, q_weight=None, k_weight=None, cos_sin=None, cu_seqlens=None,
+                      eps: float = 1e-6, interleaved: bool = False, q_out=None, stream=None):
+    """Appends new tokens to a paged cache: q [T,H,D] (may be None) and k [T,Hkv,D] normalised and rotated as by
+    attn_qk_norm_rope at each token's position in its sequence, k and v [T,Hkv,D] written into the pages of k_cache, v_cache
+    ([pages, Hkv, page_size, D], any strides).  seq_lens int32 [B]: lengths with the new tokens; block_table int32 [B, max_pages];
+    cu_seqlens int32 [B+1]: first new token of each sequence and the end (None: one token per sequence, T == B).  Tokens
+    behind the end, and of sequences of length 0, are padding: nothing is written for them.  Returns q_out [T,H,D]."""
+    if k.dim() != 3 or (q is not None and q.dim() != 3):
+        raise ValueError("q must be [tokens,H,D]; k and v [tokens,Hkv,D]")
+    T, Hkv, D = k.shape
+    _check_shape("v", v, (T, Hkv, D))
+    H = 0
+    if q is not None:
+        H = q.shape[1]
+        _check_shape("q", q, (T, H, D))
+    dt = _dtype_code(k)
+    if not k.is_cuda:
+        raise ValueError("k must be a CUDA tensor")
+    _check_on(k.device, k.dtype, q=q, v=v, q_out=q_out)
+    f32, n_pos, R = _check_rope(k, D, q_weight, k_weight, cos_sin)
+    pages, heads, page_size = _check_cache(k, D, k_cache, v_cache, block_table, seq_lens)
+    if heads != Hkv:
+        raise ValueError("the caches hold %d heads, k has %d" % (heads, Hkv))
+    n_seqs = seq_lens.shape[0]
+    if cu_seqlens is not None:
+        _check_shape("cu_seqlens", cu_seqlens, (n_seqs + 1,))
+        _check_on(k.device, torch.int32, cu_seqlens=cu_seqlens)
+        _check_dense(cu_seqlens=cu_seqlens)
+    elif T != n_seqs:
+        raise ValueError("without cu_seqlens there is one token per sequence: %d tokens, %d sequences" % (T, n_seqs))
+    if q is None:
+        q_out = None
+    elif q_out is None:
+        q_out = torch.empty((T, H, D), dtype=k.dtype, device=k.device)
+    _check_shape("q_out", q_out, (T, H, D))
+    _check_dense(q_out=q_out)
+    with torch.cuda.device(k.device):
+        rc = load().attn_paged_append(_ptr(q), k.data_ptr(), v.data_ptr(), _row_strides((q, k, v), (0, 1)), _ptr(q_weight),
+                                      _ptr(k_weight), f32, _ptr(cos_sin), n_pos, R, int(bool(interleaved)), float(eps), _ptr(q_out),
+                                      k_cache.data_ptr(), v_cache.data_ptr(), _row_strides((k_cache, v_cache), (0, 1, 2)), pages,
+                                      page_size, block_table.data_ptr(), block_table.stride(0), block_table.shape[1],
+                                      seq_lens.data_ptr(), _ptr(cu_seqlens), n_seqs, T, H, Hkv, D, dt, _stream_ptr(stream))
+    if rc != 0:
+        raise AttnError(rc, "attn_paged_append")
+    return q_out
+
+
+def attn_paged_decode_workspace_bytes(H, Hkv, D) -> int:
+    return int(load().attn_paged_decode_workspace_bytes(H, Hkv, D))
+
+
+def attn_paged_decode(q, k_cache, v_cache, block_table, seq_lens, scale: float, window: int = 0, sinks: int = 0, out=None,
+                      lse=None, workspace=None, stream=None):
+    """Attention of one new token per sequence, q [B,H,D], over a paged cache (see attn_paged_append): keys below seq_lens[b],
+    and with window > 0 only the last `window` of them and the first `sinks`.  Returns o [B,H,D] and lse [B,H] (float32).
+    `workspace`: CUDA uint8 tensor of at least attn_paged_decode_workspace_bytes(H, Hkv, D) bytes (allocated here when None)."""
+    if q.dim() != 3:
+        raise ValueError("q must be [B,H,D]")
+    B, H, D = q.shape
+    dt = _dtype_code(q)
+    if not q.is_cuda or not q.is_contiguous():
+        raise ValueError("q must be a contiguous CUDA tensor")
+    pages, Hkv, page_size = _check_cache(q, D, k_cache, v_cache, block_table, seq_lens)
+    _check_shape("seq_lens", seq_lens, (B,))
+    if out is None:
+        out = torch.empty((B, H, D), dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty((B, H), dtype=torch.float32, device=q.device)
+    _check_shape("out", out, (B, H, D))
+    _check_shape("lse", lse, (B, H))
+    _check_on(q.device, q.dtype, out=out)
+    _check_on(q.device, torch.float32, lse=lse)
+    _check_dense(out=out, lse=lse)
+    if workspace is None:
+        workspace = torch.empty(max(attn_paged_decode_workspace_bytes(H, Hkv, D), 256), dtype=torch.uint8, device=q.device)
+    with torch.cuda.device(q.device):
+        rc = load().attn_paged_decode(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _row_strides((k_cache, v_cache), (0, 1, 2)),
+                                      pages, page_size, block_table.data_ptr(), block_table.stride(0), block_table.shape[1],
+                                      seq_lens.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H, Hkv, D, float(scale), int(window),
+                                      int(sinks), dt, workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
+    if rc != 0:
+        raise AttnError(rc, "attn_paged_decode")
+    return out, lse
 
 
 def attn_fwd_simt(q, k, v, scale: float, causal: bool = False, out=None, lse=None, stream=None):

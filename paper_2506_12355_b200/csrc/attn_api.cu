@@ -17,6 +17,8 @@
 #include "../../include/attn_fwd.h"
 #include "attn_bwd.cuh"
 #include "attn_combine.cuh"
+#include "attn_paged.cuh"
+#include "attn_rope.cuh"
 #include "attn_simt.cuh"
 #include "attn_tc_qtmem.cuh"
 #include "attn_tc_pipe.cuh"
@@ -45,7 +47,8 @@
 
 namespace {
 
-// Device-side status word: 0, or ATTN_ERR_DEVICE_TIMEOUT once a kernel gave up on a wait.
+// Device-side status word: 0, ATTN_ERR_DEVICE_TIMEOUT once a kernel gave up on a wait, or ATTN_ERR_DEVICE_INDEX once one
+// met an index out of range.
 __device__ int g_device_status = 0;
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
@@ -994,7 +997,7 @@ int attn_last_device_status(void* stream) {
         int zero = 0;
         if (cudaMemcpyToSymbol(g_device_status, &zero, sizeof(int)) != cudaSuccess) return ATTN_ERR_CUDA;
     }
-    return h == 0 ? ATTN_OK : ATTN_ERR_DEVICE_TIMEOUT;
+    return h;
 }
 
 const char* attn_status_string(int status) {
@@ -1012,8 +1015,11 @@ const char* attn_status_string(int status) {
         case ATTN_ERR_WORKSPACE: return "ATTN_ERR_WORKSPACE";
         case ATTN_ERR_STATIC_CAPACITY: return "ATTN_ERR_STATIC_CAPACITY";
         case ATTN_ERR_COUNTER_SLOTS: return "ATTN_ERR_COUNTER_SLOTS";
+        case ATTN_ERR_DEVICE_INDEX: return "ATTN_ERR_DEVICE_INDEX";
         default: return "ATTN_ERR_UNKNOWN";
     }
 }
 
 }  // extern "C"
+
+#include "attn_cache_api.cuh"

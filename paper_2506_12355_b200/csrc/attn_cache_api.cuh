@@ -1,0 +1,390 @@
+// C ABI of the operators around the attention kernels (declared in include/attn_fwd.h): normalisation and rotation of queries and
+// keys, the paged cache.  Included at the end of attn_api.cu; host-side validation and launches only.
+
+namespace {
+
+bool misaligned(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
+
+// The status word's address, looked up once per device.
+int* cached_status_ptr() {
+    static std::mutex mu;
+    static int* ptr[kMaxDevices] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return nullptr;
+    std::lock_guard<std::mutex> lock(mu);
+    if (!ptr[dev]) ptr[dev] = device_status_ptr();
+    return ptr[dev];
+}
+
+bool strides_ok(const long long* s, int n) {
+    for (int i = 0; i < n; ++i)
+        if (s[i] % 8 != 0) return false;
+    return true;
+}
+
+bool head_dim_ok(int D) { return D == 64 || D == 128 || D == 256; }
+bool dtype_ok(int dtype) { return dtype == ATTN_DTYPE_FP16 || dtype == ATTN_DTYPE_BF16; }
+
+// What the three entry points of the rotation share.
+int validate_rope(const void* q_weight, const void* k_weight, const float* cos_sin, int table_len, int R, float eps, int D, int dtype) {
+    if (!head_dim_ok(D)) return ATTN_ERR_UNSUPPORTED_HEAD_DIM;
+    if (!dtype_ok(dtype)) return ATTN_ERR_UNSUPPORTED_DTYPE;
+    if (R < 0 || R > D || R % 16 != 0 || (R > 0 && table_len < 1)) return ATTN_ERR_BAD_SHAPE;
+    if (R > 0 && !cos_sin) return ATTN_ERR_NULL_POINTER;
+    if (misaligned(q_weight, 16) || misaligned(k_weight, 16) || (R > 0 && misaligned(cos_sin, 16))) return ATTN_ERR_MISALIGNED;
+    if (!isfinite(eps) || eps < 0.f) return ATTN_ERR_BAD_SCALE;
+    return ATTN_OK;
+}
+
+int validate_cache(const void* k_cache, const void* v_cache, const long long* cache_strides, int num_pages, int page_size,
+                   const int* block_table, int max_pages, const int* seq_lens) {
+    if (num_pages < 0 || max_pages < 0 || page_size < 1 || (page_size & (page_size - 1)) != 0) return ATTN_ERR_BAD_SHAPE;
+    if (static_cast<int64_t>(max_pages) * page_size > 2147483647LL) return ATTN_ERR_BAD_SHAPE;
+    if (!cache_strides || !seq_lens || (max_pages > 0 && !block_table) || (num_pages > 0 && (!k_cache || !v_cache))) return ATTN_ERR_NULL_POINTER;
+    if (misaligned(k_cache, 16) || misaligned(v_cache, 16) || !strides_ok(cache_strides, 6)) return ATTN_ERR_MISALIGNED;
+    if (misaligned(block_table, 4) || misaligned(seq_lens, 4)) return ATTN_ERR_MISALIGNED;
+    return ATTN_OK;
+}
+
+int log2_of(int x) {
+    int s = 0;
+    while ((1 << s) < x) ++s;
+    return s;
+}
+
+void rope_units(attn_rope::RopeParams& p, int D) {
+    const int per = attn_rope::kDeep * (256 / D);
+    int end = 0;
+    for (int i = 0; i < 3; ++i) {
+        end += (p.heads[i] + per - 1) / per;
+        p.unit_end[i] = end;
+    }
+}
+
+template <bool PAGED>
+int launch_rope(attn_rope::RopeParams& p, int D, int dtype, cudaStream_t st) {
+    rope_units(p, D);
+    if (p.tokens == 0 || p.unit_end[2] == 0) return ATTN_OK;
+    const int64_t gx = (p.tokens + attn_rope::kWarps - 1) / attn_rope::kWarps;
+    if (gx > 2147483647LL) return ATTN_ERR_BAD_SHAPE;
+    // few tokens: their heads are spread over blocks until the GPU has eight blocks per SM
+    int64_t gy = (148 * 8 + gx - 1) / gx;
+    if (gy > p.unit_end[2]) gy = p.unit_end[2];
+    if (gy > 65535) gy = 65535;
+    const dim3 grid(static_cast<unsigned>(gx), static_cast<unsigned>(gy));
+#define ATTN_ROPE_CASE(DD, TT) \
+    if (D == DD && dtype == TT) attn_rope::attn_rope_kernel<DD, TT, PAGED><<<grid, attn_rope::kWarps * 32, 0, st>>>(p);
+    ATTN_ROPE_CASE(64, 0)
+    ATTN_ROPE_CASE(64, 1)
+    ATTN_ROPE_CASE(128, 0)
+    ATTN_ROPE_CASE(128, 1)
+    ATTN_ROPE_CASE(256, 0)
+    ATTN_ROPE_CASE(256, 1)
+#undef ATTN_ROPE_CASE
+    return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;
+}
+
+// A launch that may begin while the kernel before it on the stream still runs; the kernel itself waits for that one's
+// results (griddepcontrol.wait).
+template <class... Params, class... Args>
+bool launch_dependent(void (*kern)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, Params(args)...) == cudaSuccess;
+}
+
+// The row strides of [B, heads, S, D], contiguous.
+attn_rope::Strides head_major(int heads, int S, int D) {
+    return attn_rope::Strides{static_cast<int64_t>(heads) * S * D, D, static_cast<int64_t>(S) * D};
+}
+
+constexpr int kRopeBwdBlocks = 148 * 4;   // blocks of the gradient kernel at most (each leaves 2 D partial sums)
+
+}  // namespace
+
+extern "C" {
+
+int attn_qk_norm_rope(const void* q, const void* k, const void* v, const long long* in_strides, const void* q_weight,
+                      const void* k_weight, int weight_f32, const float* cos_sin, int table_len, int R, int interleaved,
+                      const int* positions, float eps, void* q_out, void* k_out, void* v_out, int B, int S, int H, int Hkv,
+                      int D, int dtype, void* stream) {
+    if (B < 0 || S < 0 || H < 0 || Hkv < 0 || S > kMaxSeq) return ATTN_ERR_BAD_SHAPE;
+    int rc = validate_rope(q_weight, k_weight, cos_sin, table_len, R, eps, D, dtype);
+    if (rc != ATTN_OK) return rc;
+    if (R > 0 && !positions && S > table_len) return ATTN_ERR_BAD_SHAPE;
+    const int64_t tokens = static_cast<int64_t>(B) * S;
+    if (tokens == 0 || (H == 0 && Hkv == 0)) return ATTN_OK;
+    if (!in_strides || (H > 0 && (!q || !q_out)) || (Hkv > 0 && (!k || !k_out || !v != !v_out))) return ATTN_ERR_NULL_POINTER;
+    if (misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(q_out, 16) || misaligned(k_out, 16) ||
+        misaligned(v_out, 16) || misaligned(positions, 4) || !strides_ok(in_strides, 9))
+        return ATTN_ERR_MISALIGNED;
+    rc = check_arch();
+    if (rc != ATTN_OK) return rc;
+    attn_rope::RopeParams p = {};
+    const void* in[3] = {q, k, v};
+    void* out[3] = {q_out, k_out, v_out};
+    const int heads[3] = {H, Hkv, v ? Hkv : 0};
+    for (int i = 0; i < 3; ++i) {
+        p.in[i] = in[i];
+        p.out[i] = out[i];
+        p.heads[i] = heads[i];
+        p.is[i] = attn_rope::Strides{in_strides[3 * i], in_strides[3 * i + 1], in_strides[3 * i + 2]};
+        p.os[i] = head_major(heads[i], S, D);
+    }
+    p.weight[0] = q_weight;
+    p.weight[1] = k_weight;
+    p.weight_f32 = weight_f32;
+    p.table = cos_sin;
+    p.table_len = table_len;
+    p.R = R;
+    p.interleaved = interleaved;
+    p.positions = positions;
+    p.eps = eps;
+    p.tokens = tokens;
+    p.S = S;
+    p.status = cached_status_ptr();
+    if (!p.status) return ATTN_ERR_CUDA;
+    return launch_rope<false>(p, D, dtype, static_cast<cudaStream_t>(stream));
+}
+
+size_t attn_qk_norm_rope_bwd_workspace_bytes(int D) {
+    return head_dim_ok(D) ? static_cast<size_t>(kRopeBwdBlocks) * 2 * D * sizeof(float) : 0;
+}
+
+int attn_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const void* q, const void* k,
+                          const long long* in_strides, const void* q_weight, const void* k_weight, int weight_f32,
+                          const float* cos_sin, int table_len, int R, int interleaved, const int* positions, float eps,
+                          void* dq_in, void* dk_in, void* dv_in, const long long* out_strides, float* dq_weight,
+                          float* dk_weight, int B, int S, int H, int Hkv, int D, int dtype, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+    if (B < 0 || S < 0 || H < 0 || Hkv < 0 || S > kMaxSeq) return ATTN_ERR_BAD_SHAPE;
+    int rc = validate_rope(q_weight, k_weight, cos_sin, table_len, R, eps, D, dtype);
+    if (rc != ATTN_OK) return rc;
+    if (R > 0 && !positions && S > table_len) return ATTN_ERR_BAD_SHAPE;
+    const int64_t tokens = static_cast<int64_t>(B) * S;
+    if ((q_weight && !dq_weight) || (k_weight && !dk_weight)) return ATTN_ERR_NULL_POINTER;
+    if (misaligned(dq_weight, 4) || misaligned(dk_weight, 4)) return ATTN_ERR_MISALIGNED;
+    if (tokens > 0) {
+        if (!in_strides || !out_strides) return ATTN_ERR_NULL_POINTER;
+        if (H > 0 && (!dq || !dq_in || (q_weight && !q))) return ATTN_ERR_NULL_POINTER;
+        if (Hkv > 0 && (!dk || !dk_in || (k_weight && !k) || !dv != !dv_in)) return ATTN_ERR_NULL_POINTER;
+        if (misaligned(dq, 16) || misaligned(dk, 16) || misaligned(dv, 16) || misaligned(q, 16) || misaligned(k, 16) ||
+            misaligned(dq_in, 16) || misaligned(dk_in, 16) || misaligned(dv_in, 16) || misaligned(positions, 4) ||
+            !strides_ok(in_strides, 6) || !strides_ok(out_strides, 9))
+            return ATTN_ERR_MISALIGNED;
+        const int heads[3] = {H, Hkv, dv ? Hkv : 0};
+        for (int i = 0; i < 3; ++i) {   // an output whose rows lie on top of each other
+            const long long* s = out_strides + 3 * i;
+            if (heads[i] > 0 && ((B > 1 && s[0] == 0) || (S > 1 && s[1] == 0) || (heads[i] > 1 && s[2] == 0))) return ATTN_ERR_BAD_SHAPE;
+        }
+    }
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < attn_qk_norm_rope_bwd_workspace_bytes(D)) return ATTN_ERR_WORKSPACE;
+    rc = check_arch();
+    if (rc != ATTN_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (tokens == 0 || (H == 0 && Hkv == 0)) {
+        if (dq_weight && cudaMemsetAsync(dq_weight, 0, D * sizeof(float), st) != cudaSuccess) return ATTN_ERR_CUDA;
+        if (dk_weight && cudaMemsetAsync(dk_weight, 0, D * sizeof(float), st) != cudaSuccess) return ATTN_ERR_CUDA;
+        return ATTN_OK;
+    }
+    attn_rope::RopeParams p = {};
+    const void* in[3] = {q, k, nullptr};
+    const void* dy[3] = {dq, dk, dv};
+    void* out[3] = {dq_in, dk_in, dv_in};
+    const int heads[3] = {H, Hkv, dv ? Hkv : 0};
+    for (int i = 0; i < 3; ++i) {
+        p.in[i] = in[i];
+        p.dy[i] = dy[i];
+        p.out[i] = out[i];
+        p.heads[i] = heads[i];
+        if (i < 2) p.is[i] = attn_rope::Strides{in_strides[3 * i], in_strides[3 * i + 1], in_strides[3 * i + 2]};
+        p.os[i] = attn_rope::Strides{out_strides[3 * i], out_strides[3 * i + 1], out_strides[3 * i + 2]};
+        p.ds[i] = head_major(heads[i], S, D);
+    }
+    p.weight[0] = q_weight;
+    p.weight[1] = k_weight;
+    p.weight_f32 = weight_f32;
+    p.table = cos_sin;
+    p.table_len = table_len;
+    p.R = R;
+    p.interleaved = interleaved;
+    p.positions = positions;
+    p.eps = eps;
+    p.tokens = tokens;
+    p.S = S;
+    p.partial = static_cast<float*>(workspace);
+    p.status = cached_status_ptr();
+    if (!p.status) return ATTN_ERR_CUDA;
+    int64_t blocks = (tokens + attn_rope::kWarps - 1) / attn_rope::kWarps;
+    if (blocks > kRopeBwdBlocks) blocks = kRopeBwdBlocks;
+#define ATTN_ROPE_CASE(DD, TT) \
+    if (D == DD && dtype == TT) attn_rope::attn_rope_bwd_kernel<DD, TT><<<static_cast<unsigned>(blocks), attn_rope::kWarps * 32, 0, st>>>(p);
+    ATTN_ROPE_CASE(64, 0)
+    ATTN_ROPE_CASE(64, 1)
+    ATTN_ROPE_CASE(128, 0)
+    ATTN_ROPE_CASE(128, 1)
+    ATTN_ROPE_CASE(256, 0)
+    ATTN_ROPE_CASE(256, 1)
+#undef ATTN_ROPE_CASE
+    if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
+    if (!dq_weight && !dk_weight) return ATTN_OK;
+    return launch_dependent(attn_rope::attn_rope_weight_grad_kernel, dim3(2 * D / 32), dim3(1024), 0, st, p.partial,
+                            static_cast<int>(blocks), D, dq_weight, dk_weight)
+               ? ATTN_OK
+               : ATTN_ERR_CUDA;
+}
+
+int attn_paged_append(const void* q, const void* k, const void* v, const long long* in_strides, const void* q_weight,
+                      const void* k_weight, int weight_f32, const float* cos_sin, int table_len, int R, int interleaved,
+                      float eps, void* q_out, void* k_cache, void* v_cache, const long long* cache_strides, int num_pages,
+                      int page_size, const int* block_table, long long table_stride, int max_pages, const int* seq_lens,
+                      const int* cu_seqlens, int n_seqs, int tokens, int H, int Hkv, int D, int dtype, void* stream) {
+    if (n_seqs < 0 || tokens < 0 || H < 0 || Hkv < 0 || (!cu_seqlens && tokens != n_seqs)) return ATTN_ERR_BAD_SHAPE;
+    int rc = validate_rope(q_weight, k_weight, cos_sin, table_len, R, eps, D, dtype);
+    if (rc != ATTN_OK) return rc;
+    if (tokens == 0 || n_seqs == 0 || (H == 0 && Hkv == 0)) return ATTN_OK;
+    if (!in_strides || !q != !q_out || (Hkv > 0 && (!k || !v)) || (H > 0 && !q && Hkv == 0)) return ATTN_ERR_NULL_POINTER;
+    rc = validate_cache(k_cache, v_cache, cache_strides, num_pages, page_size, block_table, max_pages, seq_lens);
+    if (rc != ATTN_OK) return rc;
+    if (misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(q_out, 16) || misaligned(cu_seqlens, 4) ||
+        !strides_ok(in_strides, 6))
+        return ATTN_ERR_MISALIGNED;
+    for (int i = 0; i < 2; ++i) {   // cache rows that lie on top of each other
+        const long long* s = cache_strides + 3 * i;
+        if (Hkv > 0 && ((num_pages > 1 && s[0] == 0) || (Hkv > 1 && s[1] == 0) || (page_size > 1 && s[2] == 0))) return ATTN_ERR_BAD_SHAPE;
+    }
+    rc = check_arch();
+    if (rc != ATTN_OK) return rc;
+    attn_rope::RopeParams p = {};
+    const void* in[3] = {q, k, v};
+    void* out[3] = {q_out, k_cache, v_cache};
+    const int heads[3] = {q ? H : 0, Hkv, Hkv};
+    for (int i = 0; i < 3; ++i) {
+        p.in[i] = in[i];
+        p.out[i] = out[i];
+        p.heads[i] = heads[i];
+        p.is[i] = attn_rope::Strides{0, in_strides[2 * i], in_strides[2 * i + 1]};
+    }
+    p.os[0] = attn_rope::Strides{0, static_cast<int64_t>(H) * D, D};
+    for (int i = 0; i < 2; ++i) p.os[1 + i] = attn_rope::Strides{cache_strides[3 * i], cache_strides[3 * i + 2], cache_strides[3 * i + 1]};
+    p.weight[0] = q_weight;
+    p.weight[1] = k_weight;
+    p.weight_f32 = weight_f32;
+    p.table = cos_sin;
+    p.table_len = table_len;
+    p.R = R;
+    p.interleaved = interleaved;
+    p.eps = eps;
+    p.tokens = tokens;
+    p.S = tokens;
+    p.cu_seqlens = cu_seqlens;
+    p.seq_lens = seq_lens;
+    p.block_table = block_table;
+    p.table_stride = table_stride;
+    p.n_seqs = n_seqs;
+    p.max_len = max_pages * page_size;
+    p.num_pages = num_pages;
+    p.page_shift = log2_of(page_size);
+    p.status = cached_status_ptr();
+    if (!p.status) return ATTN_ERR_CUDA;
+    return launch_rope<true>(p, D, dtype, static_cast<cudaStream_t>(stream));
+}
+
+size_t attn_paged_decode_workspace_bytes(int H, int Hkv, int D) {
+    if (H < 0 || Hkv < 1 || H % Hkv != 0 || !head_dim_ok(D)) return 0;
+    const int rows = H / Hkv <= 8 ? 8 : 16;
+    return align256(static_cast<size_t>(2) * attn_paged::kMaxCtas * rows * (D + 2) * sizeof(float));
+}
+
+int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, const long long* cache_strides, int num_pages,
+                      int page_size, const int* block_table, long long table_stride, int max_pages, const int* seq_lens,
+                      void* o, float* lse, int B, int H, int Hkv, int D, float scale, int window, int sinks, int dtype,
+                      void* workspace, size_t workspace_bytes, void* stream) {
+    if (B < 0 || H < 0 || Hkv < 0 || window < 0 || sinks < 0) return ATTN_ERR_BAD_SHAPE;
+    if (H > 0 && (Hkv == 0 || H % Hkv != 0)) return ATTN_ERR_BAD_SHAPE;
+    if (!head_dim_ok(D)) return ATTN_ERR_UNSUPPORTED_HEAD_DIM;
+    if (!dtype_ok(dtype)) return ATTN_ERR_UNSUPPORTED_DTYPE;
+    if (static_cast<int64_t>(B) * H > 2147483647LL) return ATTN_ERR_BAD_SHAPE;
+    if (!isfinite(scale) || scale < 0.f) return ATTN_ERR_BAD_SCALE;
+    if (B == 0 || H == 0) return ATTN_OK;
+    if (!q || !o || !lse) return ATTN_ERR_NULL_POINTER;
+    int rc = validate_cache(k_cache, v_cache, cache_strides, num_pages, page_size, block_table, max_pages, seq_lens);
+    if (rc != ATTN_OK) return rc;
+    if (misaligned(q, 16) || misaligned(o, 16) || misaligned(lse, 4)) return ATTN_ERR_MISALIGNED;
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < attn_paged_decode_workspace_bytes(H, Hkv, D)) return ATTN_ERR_WORKSPACE;
+    rc = check_arch();
+    if (rc != ATTN_OK) return rc;
+    DeviceInfo di;
+    if (device_info(&di) != ATTN_OK) return ATTN_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    attn_paged::DecodeParams p = {};
+    p.q = q;
+    p.k_cache = static_cast<const uint8_t*>(k_cache);
+    p.v_cache = static_cast<const uint8_t*>(v_cache);
+    p.o = o;
+    p.lse = lse;
+    p.block_table = block_table;
+    p.seq_lens = seq_lens;
+    p.parts = static_cast<float*>(workspace);
+    p.k_page = cache_strides[0] * 2;
+    p.k_head = cache_strides[1] * 2;
+    p.k_slot = cache_strides[2] * 2;
+    p.v_page = cache_strides[3] * 2;
+    p.v_head = cache_strides[4] * 2;
+    p.v_slot = cache_strides[5] * 2;
+    p.table_stride = table_stride;
+    p.B = B;
+    p.H = H;
+    p.Hkv = Hkv;
+    p.group = H / Hkv;
+    p.sub = (p.group + 15) / 16;
+    p.max_len = max_pages * page_size;
+    p.num_pages = num_pages;
+    p.page_shift = log2_of(page_size);
+    p.window = window;
+    p.sinks = sinks;
+    p.scale_log2 = scale * 1.4426950408889634f;
+    p.status = cached_status_ptr();
+    if (!p.status) return ATTN_ERR_CUDA;
+    const int64_t pairs = static_cast<int64_t>(B) * Hkv * p.sub;
+    // one CTA per SM, and no more than there can be tiles (64 keys are the smallest tile)
+    const int64_t most = pairs * ((static_cast<int64_t>(p.max_len) + 63) / 64 + 1);
+    int grid = di.sm_count < attn_paged::kMaxCtas ? di.sm_count : attn_paged::kMaxCtas;
+    if (most < grid) grid = static_cast<int>(most);
+    p.grid = grid;
+#define ATTN_DECODE_CASE(DD, TT, GG)                                                                                     \
+    if (D == DD && dtype == TT && (p.group <= 8) == (GG == 8)) {                                                         \
+        using C = attn_paged::DecodeCfg<DD, GG>;                                                                         \
+        auto kern = attn_paged::attn_paged_decode_kernel<DD, TT, GG>;                                                    \
+        if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), C::SMEM_BYTES)) return ATTN_ERR_CUDA;               \
+        kern<<<grid, C::THREADS, C::SMEM_BYTES, st>>>(p);                                                                \
+        if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;                                                     \
+        return launch_dependent(attn_paged::attn_paged_join_kernel<DD, TT, GG>, dim3(static_cast<unsigned>(pairs)), dim3(256), 0, st, p) \
+                   ? ATTN_OK                                                                                             \
+                   : ATTN_ERR_CUDA;                                                                                      \
+    }
+    ATTN_DECODE_CASE(64, 0, 8)
+    ATTN_DECODE_CASE(64, 1, 8)
+    ATTN_DECODE_CASE(128, 0, 8)
+    ATTN_DECODE_CASE(128, 1, 8)
+    ATTN_DECODE_CASE(256, 0, 8)
+    ATTN_DECODE_CASE(256, 1, 8)
+    ATTN_DECODE_CASE(64, 0, 16)
+    ATTN_DECODE_CASE(64, 1, 16)
+    ATTN_DECODE_CASE(128, 0, 16)
+    ATTN_DECODE_CASE(128, 1, 16)
+    ATTN_DECODE_CASE(256, 0, 16)
+    ATTN_DECODE_CASE(256, 1, 16)
+#undef ATTN_DECODE_CASE
+    return ATTN_ERR_UNSUPPORTED_DTYPE;
+}
+
+}  // extern "C"

@@ -243,6 +243,34 @@ int attn_bwd(const void* q, const void* k, const void* v, const void* o, const f
 size_t attn_bwd_workspace_bytes(int B, int H, int Sq);
 
 /*
+ * attn_fwd_window -- causal attention under a sliding window, with first tokens that stay visible: query i stands at position
+ * p = i + q_offset, and key j is visible to it iff
+ *
+ *     j <= p   and   (j > p - window   or   j < sinks).
+ *
+ * q [B,H,Sq,D], k, v [B,Hkv,Sk,D], o, lse: as for attn_fwd_gqa; D in {64, 128} (otherwise ATTN_ERR_UNSUPPORTED_HEAD_DIM).
+ * window >= 1 counts the query's own key; 0: no lower end (causal attention at an offset).  sinks >= 0.  q_offset >= 0 is the
+ * position of query 0: a chunk of queries behind keys that are already there has q_offset = Sk - Sq; q_offset + Sq <=
+ * 2^31 - 1 - 256.  K/V tiles that no row of a Q tile sees are neither read nor computed, so the time goes with
+ * Sq * min(window + sinks, Sk).  A query without a visible key gives O = 0, LSE = -inf.
+ * K and V must be finite also where they are hidden (tiles are computed whole: a NaN or infinity in a hidden V row
+ * would reach rows of the same tile).  Everything else -- layouts, scale, errors, asynchrony -- as for attn_fwd_gqa.
+ */
+int attn_fwd_window(const void* q, const void* k, const void* v, void* o, float* lse, int B, int H, int Hkv, int Sq, int Sk,
+                    int D, float scale, int window, int sinks, int q_offset, int dtype, void* stream);
+
+/*
+ * attn_bwd_window -- backward pass of attn_fwd_window: arguments as attn_bwd, with the window of the forward call.
+ * workspace: at least attn_bwd_window_workspace_bytes(...) bytes.  Deterministic (no atomics).
+ */
+int attn_bwd_window(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* dout, void* dq,
+                    void* dk, void* dv, int B, int H, int Hkv, int Sq, int Sk, int D, float scale, int window, int sinks,
+                    int q_offset, int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace attn_bwd_window needs (0 for an invalid shape). */
+size_t attn_bwd_window_workspace_bytes(int B, int H, int Hkv, int Sq, int Sk, int D, int window, int sinks, int q_offset);
+
+/*
  * attn_qk_norm_rope -- from a projection's output to the tensors that attention reads, in one pass: per-head
  * normalisation of Q and K, rotation by position, and the change of layout to [B, heads, S, D].
  *

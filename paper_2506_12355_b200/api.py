@@ -27,6 +27,7 @@ STATUS_NAMES = {
 # every symbol include/attn_fwd.h declares
 EXPORTS = ["attn_bwd", "attn_bwd_workspace_bytes", "attn_fwd", "attn_fwd_gqa", "attn_fwd_partial", "attn_combine", "attn_combine_gather", "attn_fwd_qkv_dims", "attn_fwd_splitkv", "attn_fwd_splitkv_workspace_bytes", "attn_fwd_fp8", "attn_fwd_simt", "attn_fwd_host", "attn_fwd_host_workspace_bytes",
            "attn_fwd_host_static", "attn_fwd_host_static_capacity",
+           "attn_fwd_window", "attn_bwd_window", "attn_bwd_window_workspace_bytes",
            "attn_qk_norm_rope", "attn_qk_norm_rope_bwd", "attn_qk_norm_rope_bwd_workspace_bytes", "attn_paged_append", "attn_paged_decode",
            "attn_paged_decode_workspace_bytes",
            "attn_query_support", "attn_last_device_status", "attn_status_string"]
@@ -89,6 +90,12 @@ def load() -> ctypes.CDLL:
     lib.attn_fwd_host_static_capacity.restype = ctypes.c_size_t
     lib.attn_fwd_host_static_capacity.argtypes = []
     ll, sz = ctypes.c_longlong, ctypes.c_size_t
+    lib.attn_fwd_window.restype = i
+    lib.attn_fwd_window.argtypes = [vp] * 5 + [i] * 6 + [f] + [i] * 4 + [vp]
+    lib.attn_bwd_window.restype = i
+    lib.attn_bwd_window.argtypes = [vp] * 9 + [i] * 6 + [f] + [i] * 4 + [vp, sz, vp]
+    lib.attn_bwd_window_workspace_bytes.restype = sz
+    lib.attn_bwd_window_workspace_bytes.argtypes = [i] * 9
     lib.attn_qk_norm_rope.restype = i
     lib.attn_qk_norm_rope.argtypes = [vp] * 6 + [i, vp, i, i, i, vp, f, vp, vp, vp] + [i] * 6 + [vp]
     lib.attn_qk_norm_rope_bwd.restype = i
@@ -354,6 +361,54 @@ def attn_bwd(q, k, v, o, lse, dout, scale: float, causal: bool = False, dq=None,
                              int(bool(causal)), dt, workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
     if rc != 0:
         raise AttnError(rc, "attn_bwd")
+    return dq, dk, dv
+
+
+def attn_fwd_window(q, k, v, scale: float, window: int, sinks: int = 0, q_offset: int = 0, out=None, lse=None, stream=None):
+    """Attention under a sliding window: q [B,H,Sq,D] at positions q_offset, q_offset + 1, .., k, v [B,Hkv,Sk,D] (D in {64, 128});
+    key j is visible at position p iff j <= p and (j > p - window or j < sinks); window 0: no lower end."""
+    B, H, Hkv, Sq, Sk, D, _ = _check_grouped(q, k, v)
+    dt = _dtype_code(q)
+    out, lse = _outputs(q, B, H, Sq, D, out, lse)
+    with torch.cuda.device(q.device):
+        rc = load().attn_fwd_window(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H, Hkv, Sq, Sk, D,
+                                    float(scale), int(window), int(sinks), int(q_offset), dt, _stream_ptr(stream))
+    if rc != 0:
+        raise AttnError(rc, "attn_fwd_window")
+    return out, lse
+
+
+def attn_bwd_window_workspace_bytes(B, H, Hkv, Sq, Sk, D, window, sinks=0, q_offset=0) -> int:
+    return int(load().attn_bwd_window_workspace_bytes(B, H, Hkv, Sq, Sk, D, window, sinks, q_offset))
+
+
+def attn_bwd_window(q, k, v, o, lse, dout, scale: float, window: int, sinks: int = 0, q_offset: int = 0, dq=None, dk=None, dv=None,
+                    workspace=None, stream=None):
+    """Gradients (dq, dk, dv) of attn_fwd_window's output for the upstream gradient dout; o and lse from the forward call.
+    `workspace`: CUDA uint8 tensor of at least attn_bwd_window_workspace_bytes(...) bytes (allocated here when None)."""
+    B, H, Hkv, Sq, Sk, D, _ = _check_grouped(q, k, v)
+    _check_shape("o", o, (B, H, Sq, D))
+    _check_shape("dout", dout, (B, H, Sq, D))
+    _check_shape("lse", lse, (B, H, Sq))
+    dt = _dtype_code(q)
+    dq = torch.empty_like(q) if dq is None else dq
+    dk = torch.empty_like(k) if dk is None else dk
+    dv = torch.empty_like(v) if dv is None else dv
+    _check_shape("dq", dq, (B, H, Sq, D))
+    _check_shape("dk", dk, (B, Hkv, Sk, D))
+    _check_shape("dv", dv, (B, Hkv, Sk, D))
+    _check_on(q.device, q.dtype, o=o, dout=dout, dq=dq, dk=dk, dv=dv)
+    _check_on(q.device, torch.float32, lse=lse)
+    _check_dense(o=o, lse=lse, dout=dout, dq=dq, dk=dk, dv=dv)
+    if workspace is None:
+        n = attn_bwd_window_workspace_bytes(B, H, Hkv, Sq, Sk, D, window, sinks, q_offset)
+        workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=q.device)
+    with torch.cuda.device(q.device):
+        rc = load().attn_bwd_window(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), dout.data_ptr(),
+                                    dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, H, Hkv, Sq, Sk, D, float(scale), int(window),
+                                    int(sinks), int(q_offset), dt, workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
+    if rc != 0:
+        raise AttnError(rc, "attn_bwd_window")
     return dq, dk, dv
 
 

@@ -272,10 +272,10 @@ int g_test_skip_ring_item = -1;   // test build only: consumed by the next launc
 #endif
 
 // Pipelined, warp-specialised kernel (head dims 64 and 128): one CTA per pair of 128-row Q tiles.
-template <int D, int DTYPE>
+template <int D, int DTYPE, bool WINDOW = false>
 int launch_tc_pipe(const void* q, const void* k, const void* v, void* o, float* lse, int B, int H, int Hkv, int Sq, int Sk,
                    float scale, int causal, int k_offset, cudaStream_t st, float o_scale = 1.f, int64_t kv_stride_rows = -1,
-                   int n_splits = 1) {
+                   int n_splits = 1, int window = 0, int sinks = 0) {
     // n_splits > 1: the keys are cut into n_splits ranges of whole tiles; range s of a head is a work item of its own
     // and writes its partial result as head s * (B * H) + bh of o and lse, which then hold n_splits partial results
     constexpr int ES = DTYPE == ATTN_DTYPE_FP8_E4M3 ? 1 : 2;                 // bytes per Q/K/V element
@@ -285,7 +285,7 @@ int launch_tc_pipe(const void* q, const void* k, const void* v, void* o, float* 
     // head dim 64, where the tensor core leaves more issue slots to the softmax warps
     constexpr int PN = DTYPE == ATTN_DTYPE_FP8_E4M3 ? ATTN_FP8_POLY_NUM : (D == 64 ? ATTN_POLY64_NUM : ATTN_POLY_NUM);
     constexpr int PD = DTYPE == ATTN_DTYPE_FP8_E4M3 ? ATTN_FP8_POLY_DEN : (D == 64 ? ATTN_POLY64_DEN : ATTN_POLY_DEN);
-    auto kern = n_splits > 1 ? attn_tc::attn_fwd_tc_pipe_kernel<D, DTYPE, PN, PD, true> : attn_tc::attn_fwd_tc_pipe_kernel<D, DTYPE, PN, PD, false>;
+    auto kern = n_splits > 1 ? attn_tc::attn_fwd_tc_pipe_kernel<D, DTYPE, PN, PD, !WINDOW> : attn_tc::attn_fwd_tc_pipe_kernel<D, DTYPE, PN, PD, false, WINDOW>;
     if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), C::SMEM_BYTES)) return ATTN_ERR_CUDA;
     const int64_t BH = static_cast<int64_t>(B) * H;
     const int64_t n_pairs = (static_cast<int64_t>(Sq) + 2 * C::BM - 1) / (2 * C::BM);
@@ -327,6 +327,8 @@ int launch_tc_pipe(const void* q, const void* k, const void* v, void* o, float* 
         const int merge = causal ? ATTN_MERGE_LAST : 1;
         prm.last_group = static_cast<int>(n_groups >= merge ? n_groups - merge : 0);
     }
+    prm.window = window;
+    prm.sinks = sinks;
     prm.n_items = static_cast<int>(n_pairs * BH * n_splits);
     prm.halves_from = 2147483647;
     prm.n_splits = n_splits;
@@ -586,6 +588,123 @@ int host_pipelined(const void* q_host, const void* k_host, const void* v_host, v
 
 }  // namespace
 
+namespace {
+
+// attn_bwd's workspace: two fp32 row vectors [B*H][Sq_pad], Sq_pad = Sq rounded up to a multiple of 64
+size_t bwd_sq_pad(int Sq) { return (static_cast<size_t>(Sq) + 63) / 64 * 64; }
+
+// The backward pass of attn_bwd and, with WINDOW, of attn_bwd_window (whose own arguments are the last three).
+template <bool WINDOW>
+int bwd(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* dout, void* dq, void* dk, void* dv,
+        int B, int H, int Hkv, int Sq, int Sk, int D, float scale, int causal, int dtype, void* workspace, size_t workspace_bytes,
+        void* stream, int window, int sinks, int q_offset) {
+    if (D != 64 && D != 128) {
+        if (B < 0 || H < 0 || Hkv < 0 || Sq < 0 || Sk < 0 || D < 0) return ATTN_ERR_BAD_SHAPE;
+        return ATTN_ERR_UNSUPPORTED_HEAD_DIM;
+    }
+    // the shared checks on q, k, v (dq stands in for o, the caller's lse is checked as a float pointer)
+    int rc = validate(q, k, v, dq, lse, B, H, Hkv, Sq, Sk, D, scale, dtype, true);
+    if (rc != ATTN_OK) return rc;
+    const size_t n_q = static_cast<size_t>(B) * H * Sq, n_kv = static_cast<size_t>(B) * Hkv * Sk;
+    if (n_q > 0 && (!o || !dout)) return ATTN_ERR_NULL_POINTER;
+    if (n_kv > 0 && (!dk || !dv)) return ATTN_ERR_NULL_POINTER;
+    if ((reinterpret_cast<uintptr_t>(o) | reinterpret_cast<uintptr_t>(dout) | reinterpret_cast<uintptr_t>(dk) |
+         reinterpret_cast<uintptr_t>(dv)) & 15u)
+        return ATTN_ERR_MISALIGNED;
+    if (n_q == 0 && n_kv == 0) return ATTN_OK;
+    if (n_q > 0 && n_kv > 0 &&
+        (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < attn_bwd_workspace_bytes(B, H, Sq)))
+        return ATTN_ERR_WORKSPACE;
+    rc = check_arch();
+    if (rc != ATTN_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    // no queries: nothing reaches K and V; no keys: nothing reaches Q
+    if (n_q == 0 || n_kv == 0) {
+        if (n_kv > 0 && (cudaMemsetAsync(dk, 0, n_kv * D * 2, st) != cudaSuccess || cudaMemsetAsync(dv, 0, n_kv * D * 2, st) != cudaSuccess))
+            return ATTN_ERR_CUDA;
+        if (n_q > 0 && cudaMemsetAsync(dq, 0, n_q * D * 2, st) != cudaSuccess) return ATTN_ERR_CUDA;
+        return ATTN_OK;
+    }
+    const int64_t BH = static_cast<int64_t>(B) * H, BHkv = static_cast<int64_t>(B) * Hkv;
+    const int64_t n_qtiles = (static_cast<int64_t>(Sq) + 127) / 128, n_ktiles = (static_cast<int64_t>(Sk) + 127) / 128;
+    if (n_qtiles * BH > 2147483647LL || n_ktiles * BHkv > 2147483647LL) return ATTN_ERR_BAD_SHAPE;
+    const int64_t sq_pad = static_cast<int64_t>(bwd_sq_pad(Sq));
+    float* nl2 = static_cast<float*>(workspace);
+    float* ndelta = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + align256(static_cast<size_t>(BH) * sq_pad * sizeof(float)));
+    attn_grad::BwdParams prm;
+    prm.nl2 = nl2;
+    prm.ndelta = ndelta;
+    prm.Sq_pad = static_cast<int>(sq_pad);
+    prm.Sq = Sq;
+    prm.Sk = Sk;
+    prm.scale = scale;
+    prm.scale_log2 = scale * 1.4426950408889634f;
+    prm.causal = causal ? 1 : 0;
+    prm.window = window;
+    prm.sinks = sinks;
+    prm.q_offset = q_offset;
+    prm.H = H;
+    prm.Hkv = Hkv;
+    prm.n_qtiles = static_cast<int>(n_qtiles);
+    prm.n_ktiles = static_cast<int>(n_ktiles);
+    prm.status = device_status_ptr();
+    if (!prm.status) return ATTN_ERR_CUDA;
+    // resident tiles and outputs move in boxes of 128 rows, streamed tiles in boxes of 64 rows
+    DeviceInfo di;
+    int dev = 0;
+    if (device_info(&di, &dev) != ATTN_OK) return ATTN_ERR_CUDA;
+    const int sms = di.sm_count;   // persistent grids: one CTA per SM, later tiles from the stream's work counter
+    unsigned int* counter = nullptr;
+    if (n_qtiles * BH > sms || n_ktiles * BHkv > sms) {
+        rc = work_counter(di, dev, st, &counter);
+        if (rc != ATTN_OK) return rc;
+    }
+    CUtensorMap mq, mk, mv, mdo, mq64, mk64, mv64, mdo64, mdq, mdk, mdv;
+    if (!make_map(&mq, q, dtype, BH, Sq, D, 128) || !make_map(&mdo, dout, dtype, BH, Sq, D, 128) ||
+        !make_map(&mq64, q, dtype, BH, Sq, D, 64) || !make_map(&mdo64, dout, dtype, BH, Sq, D, 64) ||
+        !make_map(&mdq, dq, dtype, BH, Sq, D, 128) || !make_map(&mk, k, dtype, BHkv, Sk, D, 128) ||
+        !make_map(&mv, v, dtype, BHkv, Sk, D, 128) || !make_map(&mk64, k, dtype, BHkv, Sk, D, 64) ||
+        !make_map(&mv64, v, dtype, BHkv, Sk, D, 64) || !make_map(&mdk, dk, dtype, BHkv, Sk, D, 128) ||
+        !make_map(&mdv, dv, dtype, BHkv, Sk, D, 128))
+        return ATTN_ERR_CUDA;
+#define ATTN_BWD_CASE(DD, TT)                                                                                              \
+    if (D == DD && dtype == TT) {                                                                                          \
+        using CQ = attn_grad::BwdCfg<DD, 0>;                                                                                \
+        using CKV = attn_grad::BwdCfg<DD, 1>;                                                                               \
+        auto kq = attn_grad::attn_bwd_kernel<DD, TT, 0, WINDOW>;                                                                    \
+        auto kkv = attn_grad::attn_bwd_kernel<DD, TT, 1, WINDOW>;                                                                   \
+        if (!allow_dynamic_smem(reinterpret_cast<const void*>(kq), CQ::SMEM_BYTES) ||                                      \
+            !allow_dynamic_smem(reinterpret_cast<const void*>(kkv), CKV::SMEM_BYTES))                                      \
+            return ATTN_ERR_CUDA;                                                                                          \
+        const int64_t rows = BH * sq_pad;                                                                                  \
+        int64_t blocks = (rows + 7) / 8;                                                                                   \
+        if (blocks > 148 * 16) blocks = 148 * 16;                                                                          \
+        attn_grad::attn_bwd_rows_kernel<DD, TT><<<static_cast<unsigned>(blocks), 256, 0, st>>>(o, dout, lse, nl2, ndelta, Sq, \
+                                                                                              prm.Sq_pad, rows);          \
+        prm.out0 = dq;                                                                                                     \
+        prm.out1 = nullptr;                                                                                                \
+        prm.n_tiles_total = static_cast<int>(n_qtiles * BH);                                                               \
+        prm.counter = prm.n_tiles_total > sms ? counter : nullptr;                                                         \
+        kq<<<static_cast<unsigned>(prm.n_tiles_total < sms ? prm.n_tiles_total : sms), CQ::THREADS, CQ::SMEM_BYTES, st>>>(  \
+            mq, mdo, mk64, mv64, mdq, mdq, prm);                                                                           \
+        prm.out0 = dv;                                                                                                     \
+        prm.out1 = dk;                                                                                                     \
+        prm.n_tiles_total = static_cast<int>(n_ktiles * BHkv);                                                             \
+        prm.counter = prm.n_tiles_total > sms ? counter : nullptr;                                                         \
+        kkv<<<static_cast<unsigned>(prm.n_tiles_total < sms ? prm.n_tiles_total : sms), CKV::THREADS, CKV::SMEM_BYTES, st>>>( \
+            mk, mv, mq64, mdo64, mdv, mdk, prm);                                                                           \
+        return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;                                                \
+    }
+    ATTN_BWD_CASE(64, 0)
+    ATTN_BWD_CASE(64, 1)
+    ATTN_BWD_CASE(128, 0)
+    ATTN_BWD_CASE(128, 1)
+#undef ATTN_BWD_CASE
+    return ATTN_ERR_UNSUPPORTED_DTYPE;
+}
+
+}  // namespace
+
 extern "C" {
 
 #ifdef ATTN_TEST_HOOKS
@@ -806,9 +925,6 @@ int attn_fwd_fp8(const void* q, const void* k, const void* v, void* o, float* ls
     return launch_tc_pipe<128, ATTN_DTYPE_FP8_E4M3>(q, k, v, o, lse, B, H, Hkv, Sq, Sk, s_eff, causal, 0, st, v_factor);
 }
 
-// attn_bwd's workspace: two fp32 row vectors [B*H][Sq_pad], Sq_pad = Sq rounded up to a multiple of 64
-size_t bwd_sq_pad(int Sq) { return (static_cast<size_t>(Sq) + 63) / 64 * 64; }
-
 size_t attn_bwd_workspace_bytes(int B, int H, int Sq) {
     if (B < 0 || H < 0 || Sq < 0) return 0;
     return 2 * align256(static_cast<size_t>(B) * H * bwd_sq_pad(Sq) * sizeof(float));
@@ -817,106 +933,8 @@ size_t attn_bwd_workspace_bytes(int B, int H, int Sq) {
 int attn_bwd(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* dout, void* dq,
              void* dk, void* dv, int B, int H, int Hkv, int Sq, int Sk, int D, float scale, int causal, int dtype,
              void* workspace, size_t workspace_bytes, void* stream) {
-    if (D != 64 && D != 128) {
-        if (B < 0 || H < 0 || Hkv < 0 || Sq < 0 || Sk < 0 || D < 0) return ATTN_ERR_BAD_SHAPE;
-        return ATTN_ERR_UNSUPPORTED_HEAD_DIM;
-    }
-    // the shared checks on q, k, v (dq stands in for o, the caller's lse is checked as a float pointer)
-    int rc = validate(q, k, v, dq, lse, B, H, Hkv, Sq, Sk, D, scale, dtype, true);
-    if (rc != ATTN_OK) return rc;
-    const size_t n_q = static_cast<size_t>(B) * H * Sq, n_kv = static_cast<size_t>(B) * Hkv * Sk;
-    if (n_q > 0 && (!o || !dout)) return ATTN_ERR_NULL_POINTER;
-    if (n_kv > 0 && (!dk || !dv)) return ATTN_ERR_NULL_POINTER;
-    if ((reinterpret_cast<uintptr_t>(o) | reinterpret_cast<uintptr_t>(dout) | reinterpret_cast<uintptr_t>(dk) |
-         reinterpret_cast<uintptr_t>(dv)) & 15u)
-        return ATTN_ERR_MISALIGNED;
-    if (n_q == 0 && n_kv == 0) return ATTN_OK;
-    if (n_q > 0 && n_kv > 0 &&
-        (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < attn_bwd_workspace_bytes(B, H, Sq)))
-        return ATTN_ERR_WORKSPACE;
-    rc = check_arch();
-    if (rc != ATTN_OK) return rc;
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    // no queries: nothing reaches K and V; no keys: nothing reaches Q
-    if (n_q == 0 || n_kv == 0) {
-        if (n_kv > 0 && (cudaMemsetAsync(dk, 0, n_kv * D * 2, st) != cudaSuccess || cudaMemsetAsync(dv, 0, n_kv * D * 2, st) != cudaSuccess))
-            return ATTN_ERR_CUDA;
-        if (n_q > 0 && cudaMemsetAsync(dq, 0, n_q * D * 2, st) != cudaSuccess) return ATTN_ERR_CUDA;
-        return ATTN_OK;
-    }
-    const int64_t BH = static_cast<int64_t>(B) * H, BHkv = static_cast<int64_t>(B) * Hkv;
-    const int64_t n_qtiles = (static_cast<int64_t>(Sq) + 127) / 128, n_ktiles = (static_cast<int64_t>(Sk) + 127) / 128;
-    if (n_qtiles * BH > 2147483647LL || n_ktiles * BHkv > 2147483647LL) return ATTN_ERR_BAD_SHAPE;
-    const int64_t sq_pad = static_cast<int64_t>(bwd_sq_pad(Sq));
-    float* nl2 = static_cast<float*>(workspace);
-    float* ndelta = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + align256(static_cast<size_t>(BH) * sq_pad * sizeof(float)));
-    attn_grad::BwdParams prm;
-    prm.nl2 = nl2;
-    prm.ndelta = ndelta;
-    prm.Sq_pad = static_cast<int>(sq_pad);
-    prm.Sq = Sq;
-    prm.Sk = Sk;
-    prm.scale = scale;
-    prm.scale_log2 = scale * 1.4426950408889634f;
-    prm.causal = causal ? 1 : 0;
-    prm.H = H;
-    prm.Hkv = Hkv;
-    prm.n_qtiles = static_cast<int>(n_qtiles);
-    prm.n_ktiles = static_cast<int>(n_ktiles);
-    prm.status = device_status_ptr();
-    if (!prm.status) return ATTN_ERR_CUDA;
-    // resident tiles and outputs move in boxes of 128 rows, streamed tiles in boxes of 64 rows
-    DeviceInfo di;
-    int dev = 0;
-    if (device_info(&di, &dev) != ATTN_OK) return ATTN_ERR_CUDA;
-    const int sms = di.sm_count;   // persistent grids: one CTA per SM, later tiles from the stream's work counter
-    unsigned int* counter = nullptr;
-    if (n_qtiles * BH > sms || n_ktiles * BHkv > sms) {
-        rc = work_counter(di, dev, st, &counter);
-        if (rc != ATTN_OK) return rc;
-    }
-    CUtensorMap mq, mk, mv, mdo, mq64, mk64, mv64, mdo64, mdq, mdk, mdv;
-    if (!make_map(&mq, q, dtype, BH, Sq, D, 128) || !make_map(&mdo, dout, dtype, BH, Sq, D, 128) ||
-        !make_map(&mq64, q, dtype, BH, Sq, D, 64) || !make_map(&mdo64, dout, dtype, BH, Sq, D, 64) ||
-        !make_map(&mdq, dq, dtype, BH, Sq, D, 128) || !make_map(&mk, k, dtype, BHkv, Sk, D, 128) ||
-        !make_map(&mv, v, dtype, BHkv, Sk, D, 128) || !make_map(&mk64, k, dtype, BHkv, Sk, D, 64) ||
-        !make_map(&mv64, v, dtype, BHkv, Sk, D, 64) || !make_map(&mdk, dk, dtype, BHkv, Sk, D, 128) ||
-        !make_map(&mdv, dv, dtype, BHkv, Sk, D, 128))
-        return ATTN_ERR_CUDA;
-#define ATTN_BWD_CASE(DD, TT)                                                                                              \
-    if (D == DD && dtype == TT) {                                                                                          \
-        using CQ = attn_grad::BwdCfg<DD, 0>;                                                                                \
-        using CKV = attn_grad::BwdCfg<DD, 1>;                                                                               \
-        auto kq = attn_grad::attn_bwd_kernel<DD, TT, 0>;                                                                    \
-        auto kkv = attn_grad::attn_bwd_kernel<DD, TT, 1>;                                                                   \
-        if (!allow_dynamic_smem(reinterpret_cast<const void*>(kq), CQ::SMEM_BYTES) ||                                      \
-            !allow_dynamic_smem(reinterpret_cast<const void*>(kkv), CKV::SMEM_BYTES))                                      \
-            return ATTN_ERR_CUDA;                                                                                          \
-        const int64_t rows = BH * sq_pad;                                                                                  \
-        int64_t blocks = (rows + 7) / 8;                                                                                   \
-        if (blocks > 148 * 16) blocks = 148 * 16;                                                                          \
-        attn_grad::attn_bwd_rows_kernel<DD, TT><<<static_cast<unsigned>(blocks), 256, 0, st>>>(o, dout, lse, nl2, ndelta, Sq, \
-                                                                                              prm.Sq_pad, rows);          \
-        prm.out0 = dq;                                                                                                     \
-        prm.out1 = nullptr;                                                                                                \
-        prm.n_tiles_total = static_cast<int>(n_qtiles * BH);                                                               \
-        prm.counter = prm.n_tiles_total > sms ? counter : nullptr;                                                         \
-        kq<<<static_cast<unsigned>(prm.n_tiles_total < sms ? prm.n_tiles_total : sms), CQ::THREADS, CQ::SMEM_BYTES, st>>>(  \
-            mq, mdo, mk64, mv64, mdq, mdq, prm);                                                                           \
-        prm.out0 = dv;                                                                                                     \
-        prm.out1 = dk;                                                                                                     \
-        prm.n_tiles_total = static_cast<int>(n_ktiles * BHkv);                                                             \
-        prm.counter = prm.n_tiles_total > sms ? counter : nullptr;                                                         \
-        kkv<<<static_cast<unsigned>(prm.n_tiles_total < sms ? prm.n_tiles_total : sms), CKV::THREADS, CKV::SMEM_BYTES, st>>>( \
-            mk, mv, mq64, mdo64, mdv, mdk, prm);                                                                           \
-        return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;                                                \
-    }
-    ATTN_BWD_CASE(64, 0)
-    ATTN_BWD_CASE(64, 1)
-    ATTN_BWD_CASE(128, 0)
-    ATTN_BWD_CASE(128, 1)
-#undef ATTN_BWD_CASE
-    return ATTN_ERR_UNSUPPORTED_DTYPE;
+    return bwd<false>(q, k, v, o, lse, dout, dq, dk, dv, B, H, Hkv, Sq, Sk, D, scale, causal, dtype, workspace, workspace_bytes,
+                      stream, 0, 0, 0);
 }
 
 int attn_fwd_simt(const void* q, const void* k, const void* v, void* o, float* lse, int B, int H, int Sq, int Sk,

@@ -112,6 +112,7 @@ struct BwdParams {
     int H, Hkv;
     int n_qtiles, n_ktiles; // 128-row tiles of the query and of the key axis
     int n_tiles_total;      // tiles of this pass over all heads
+    int window, sinks, q_offset;   // WINDOW: key j is visible to query i iff j <= p and (j > p - window or j < sinks), p = i + q_offset
     unsigned int* counter;  // work counter {next tile, CTAs done}, zero at launch and again at exit:
                             // tile = gridDim.x + atomicAdd(counter, 1); NULL when the grid covers every tile
     int* status;
@@ -190,12 +191,20 @@ struct BwdTile {
     int sub_lo, sub_hi;     // range of 64-row tiles of the streamed axis
     int n_steps;            // 0: nothing reaches this tile (its gradients are zero)
     int kv_bh_of_q;         // MODE 0: K/V head of this query head
+    int n_sink;             // WINDOW, MODE 0: steps before the window's own, over the tiles of the first keys
 };
+
+// WINDOW: may key `key` be hidden from query row `row`?
+__device__ __forceinline__ bool window_hides(const BwdParams& prm, int key, int row) {
+    const int p = row + prm.q_offset;
+    return key >= prm.Sk || key > p || (key < p - prm.window + 1 && key >= prm.sinks);
+}
 
 // tmR0 / tmR1: maps of the resident tiles, boxes of 128 rows (MODE 0: Q, dO; MODE 1: K, V); tmT0 / tmT1: maps of
 // the streamed tiles, boxes of 64 rows (MODE 0: K, V; MODE 1: Q, dO); tmOut0 / tmOut1: MODE 0: dQ, unused;
 // MODE 1: dV, dK (boxes of 128 rows).
-template <int D, int DTYPE, int MODE>
+// WINDOW: the instance for sliding windows: other step lists and another mask.
+template <int D, int DTYPE, int MODE, bool WINDOW = false>
 __global__ void __launch_bounds__(384, 1)
 attn_bwd_kernel(const __grid_constant__ CUtensorMap tmR0, const __grid_constant__ CUtensorMap tmR1,
                 const __grid_constant__ CUtensorMap tmT0, const __grid_constant__ CUtensorMap tmT1,
@@ -257,7 +266,29 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tmR0, const __grid_constant_
         BwdTile t;
         const int bid_tile = lin % tiles_per_head;
         t.bh_res = lin / tiles_per_head;
-        if constexpr (MODE == 0) {
+        t.n_sink = 0;
+        if constexpr (WINDOW && MODE == 0) {
+            // keys from the first row's lowest to the last row's own, behind the tiles of the first keys
+            t.tile = prm.n_qtiles - 1 - bid_tile;
+            const int r0 = t.tile * BT, r1 = r0 + BT - 1 < prm.Sq ? r0 + BT - 1 : prm.Sq - 1;
+            const int k0 = r0 + prm.q_offset - prm.window + 1, k1 = r1 + prm.q_offset;
+            const int sink_subs = ((prm.sinks < prm.Sk ? prm.sinks : prm.Sk) + BS - 1) / BS;
+            t.sub_lo = (k0 > 0 ? k0 : 0) / BS;
+            t.sub_hi = k0 < prm.Sk ? (k1 < prm.Sk ? k1 : prm.Sk - 1) / BS + 1 : t.sub_lo;
+            t.n_sink = t.sub_hi > t.sub_lo && t.sub_lo < sink_subs ? t.sub_lo : sink_subs;
+            t.n_steps = t.n_sink + t.sub_hi - t.sub_lo;
+        } else if constexpr (WINDOW) {
+            // query rows from the first that stands at or behind the tile's first key to the last whose window reaches its last
+            // key, or (tiles with first keys, visible to all later rows) to the end
+            t.tile = bid_tile;
+            const int c0 = t.tile * BT, c1 = c0 + BT - 1 < prm.Sk ? c0 + BT - 1 : prm.Sk - 1;
+            int64_t last = static_cast<int64_t>(c1) + prm.window - 1 - prm.q_offset;
+            if (c0 < prm.sinks || last > prm.Sq - 1) last = prm.Sq - 1;
+            t.sub_lo = (c0 > prm.q_offset ? c0 - prm.q_offset : 0) / BS;
+            t.sub_hi = last < 0 ? 0 : static_cast<int>(last) / BS + 1;
+            if (t.sub_lo > t.sub_hi) t.sub_lo = t.sub_hi;
+            t.n_steps = (t.sub_hi - t.sub_lo) * group;
+        } else if constexpr (MODE == 0) {
             t.tile = prm.causal ? prm.n_qtiles - 1 - bid_tile : bid_tile;
             const int last_key = attn_tc::last_visible_key(t.tile * BT + BT - 1, prm.Sk, prm.causal, 0);
             t.sub_lo = 0;
@@ -279,7 +310,8 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tmR0, const __grid_constant_
         else return (t.bh_res / prm.Hkv) * prm.H + (t.bh_res % prm.Hkv) * group + u / (t.sub_hi - t.sub_lo);
     };
     auto step_sub = [&](const BwdTile& t, int u) {
-        if constexpr (MODE == 0) return u;
+        if constexpr (WINDOW && MODE == 0) return u < t.n_sink ? u : t.sub_lo + u - t.n_sink;
+        else if constexpr (MODE == 0) return u;
         else return t.sub_lo + u % (t.sub_hi - t.sub_lo);
     };
     // Consumers of the scheduler: the tile index at position p of this CTA's walk (-1: no more); the slot is handed
@@ -586,7 +618,11 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tmR0, const __grid_constant_
                 //   MODE 0: rows tile*128 .. +127, keys ts*64 .. +63;  MODE 1: keys tile*128 .. +127, rows ts*64 .. +63
                 const int key0 = MODE == 0 ? ts * BS : t.tile * BT, nkeys = MODE == 0 ? BS : BT;
                 const int row0 = MODE == 0 ? t.tile * BT : ts * BS;
-                const bool partial = (key0 + nkeys > prm.Sk) || (prm.causal && key0 + nkeys - 1 > row0);
+                bool partial = (key0 + nkeys > prm.Sk) || (prm.causal && key0 + nkeys - 1 > row0);
+                if constexpr (WINDOW) {
+                    const int p0 = row0 + prm.q_offset, p1 = p0 + (MODE == 0 ? BT : BS) - 1;
+                    partial = key0 + nkeys > prm.Sk || key0 + nkeys - 1 > p0 || (key0 < p1 - prm.window + 1 && key0 + nkeys > prm.sinks);
+                }
                 // the whole S and dP row of this step into registers, then tensor memory is free for the next step
                 uint32_t sr[BS], dpr[BS];
 #pragma unroll
@@ -624,7 +660,13 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tmR0, const __grid_constant_
                         float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
                         if constexpr (MASKED) {
                             bool v0, v1;
-                            if constexpr (MODE == 0) {
+                            if constexpr (WINDOW && MODE == 0) {
+                                v0 = !window_hides(prm, key0 + col, my_row);
+                                v1 = !window_hides(prm, key0 + col + 1, my_row);
+                            } else if constexpr (WINDOW) {
+                                v0 = !window_hides(prm, my_row, row0 + col);
+                                v1 = !window_hides(prm, my_row, row0 + col + 1);
+                            } else if constexpr (MODE == 0) {
                                 v0 = key0 + col < prm.Sk && (!prm.causal || key0 + col <= my_row);
                                 v1 = key0 + col + 1 < prm.Sk && (!prm.causal || key0 + col + 1 <= my_row);
                             } else {

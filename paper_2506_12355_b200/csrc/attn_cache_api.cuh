@@ -1,5 +1,5 @@
-// C ABI of the operators around the attention kernels (declared in include/attn_fwd.h): normalisation and rotation of queries and
-// keys, the paged cache.  Included at the end of attn_api.cu; host-side validation and launches only.
+// C ABI of the operators around the attention kernels (declared in include/attn_fwd.h): sliding windows, normalisation and
+// rotation of queries and keys, the paged cache.  Included at the end of attn_api.cu; host-side validation and launches only.
 
 namespace {
 
@@ -106,11 +106,57 @@ attn_rope::Strides head_major(int heads, int S, int D) {
     return attn_rope::Strides{static_cast<int64_t>(heads) * S * D, D, static_cast<int64_t>(S) * D};
 }
 
+// The window arguments: window 0 stands for one without an end.
+int validate_window(int Sq, int* window, int sinks, int q_offset) {
+    if (*window < 0 || sinks < 0 || q_offset < 0 || static_cast<int64_t>(q_offset) + (Sq > 0 ? Sq : 0) > kMaxSeq) return ATTN_ERR_BAD_SHAPE;
+    if (*window == 0) *window = 2147483647;
+    return ATTN_OK;
+}
+
 constexpr int kRopeBwdBlocks = 148 * 4;   // blocks of the gradient kernel at most (each leaves 2 D partial sums)
 
 }  // namespace
 
 extern "C" {
+
+int attn_fwd_window(const void* q, const void* k, const void* v, void* o, float* lse, int B, int H, int Hkv, int Sq, int Sk,
+                    int D, float scale, int window, int sinks, int q_offset, int dtype, void* stream) {
+    if (D != 64 && D != 128) {
+        if (B < 0 || H < 0 || Hkv < 0 || Sq < 0 || Sk < 0 || D < 0) return ATTN_ERR_BAD_SHAPE;
+        return ATTN_ERR_UNSUPPORTED_HEAD_DIM;
+    }
+    int rc = validate(q, k, v, o, lse, B, H, Hkv, Sq, Sk, D, scale, dtype, true);
+    if (rc == ATTN_OK) rc = validate_window(Sq, &window, sinks, q_offset);
+    if (rc != ATTN_OK) return rc;
+    if (static_cast<int64_t>(B) * H * Sq == 0) return ATTN_OK;
+    rc = check_arch();
+    if (rc != ATTN_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (Sk == 0) return fill_empty(o, lse, static_cast<int64_t>(B) * H * Sq * D, static_cast<int64_t>(B) * H * Sq, st);
+#define ATTN_WINDOW_CASE(DD, TT) \
+    if (D == DD && dtype == TT)  \
+        return launch_tc_pipe<DD, TT, true>(q, k, v, o, lse, B, H, Hkv, Sq, Sk, scale, 1, -q_offset, st, 1.f, -1, 1, window, sinks);
+    ATTN_WINDOW_CASE(64, 0)
+    ATTN_WINDOW_CASE(64, 1)
+    ATTN_WINDOW_CASE(128, 0)
+    ATTN_WINDOW_CASE(128, 1)
+#undef ATTN_WINDOW_CASE
+    return ATTN_ERR_UNSUPPORTED_DTYPE;
+}
+
+size_t attn_bwd_window_workspace_bytes(int B, int H, int Hkv, int Sq, int Sk, int D, int window, int sinks, int q_offset) {
+    (void)Hkv; (void)Sk; (void)D; (void)window; (void)sinks; (void)q_offset;
+    return attn_bwd_workspace_bytes(B, H, Sq);
+}
+
+int attn_bwd_window(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* dout, void* dq,
+                    void* dk, void* dv, int B, int H, int Hkv, int Sq, int Sk, int D, float scale, int window, int sinks,
+                    int q_offset, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    const int rc = validate_window(Sq, &window, sinks, q_offset);
+    if (rc != ATTN_OK) return rc;
+    return bwd<true>(q, k, v, o, lse, dout, dq, dk, dv, B, H, Hkv, Sq, Sk, D, scale, 1, dtype, workspace, workspace_bytes, stream,
+                     window, sinks, q_offset);
+}
 
 int attn_qk_norm_rope(const void* q, const void* k, const void* v, const long long* in_strides, const void* q_weight,
                       const void* k_weight, int weight_f32, const float* cos_sin, int table_len, int R, int interleaved,

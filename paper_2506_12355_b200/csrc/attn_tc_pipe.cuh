@@ -27,6 +27,10 @@
 // grown by more than 2^8; otherwise the stale m is kept (P values up to 256, exact after the final
 // division by l), so the O accumulator rarely needs rescaling.
 //
+// Sliding window (WINDOW = true): query i at position p = i + q_offset sees key j iff j <= p and (j > p - window or
+// j < sinks).  The steps of an item are then the tiles of the first tokens and a run of tiles from the window's lower
+// edge; the rest of the loop is the same.  What changes inside it is noted at the places.
+//
 // 8-bit inputs (the FP8 case study of Section 4.4): the same kernel with E4M3 tiles of half the size,
 // kind::f8f6f4 MMAs and P written back as E4M3, four values per tensor-memory column; see the
 // constants at the top of the kernel.
@@ -68,7 +72,9 @@ struct PipeParams {
     int heads_per_group;    // heads whose K/V are walked together (L2 residency)
     int last_group;         // index of the final group, which takes all remaining heads
     int H, Hkv;             // query heads and key/value heads per batch element (H % Hkv == 0)
-    int k_offset;           // global index of key 0 of this K/V shard (0 for whole problems); enters the causal mask
+    int k_offset;           // global index of key 0 of this K/V shard (0 for whole problems); enters the causal mask.
+                            // Negative: minus the position of query 0
+    int window, sinks;      // WINDOW: keys that a query sees up to its own, and first keys that stay visible
     int n_items;            // work items: n_pairs * BH * n_splits, plus one for every item at or beyond halves_from
     int halves_from;        // items from this index on are cut into their two Q tiles (each half a work item of its own,
                             // consecutive indices); INT_MAX: none.  Used when the last wave of a launch of equally long
@@ -98,8 +104,43 @@ struct PipeItem {
                         // and the MMA warp then reads its loop bounds from there on every step.
     __device__ __forceinline__ int nkv(int t) const { return t ? n_kv1 : n_kv0; }
     int n_max;
+    // WINDOW: steps below n_sink are the tiles 0, 1, ..; step i >= n_sink is tile i + shift.  The first of those may lie
+    // below Q tile 1's window, which then leaves that step (the hole) out: hole is its number, or -1.
+    int n_sink, shift, hole;
+    __device__ __forceinline__ int tile_of(int i) const { return i < n_sink ? i : i + shift; }
+    __device__ __forceinline__ bool takes(int t, int i) const { return i < nkv(t) && !(t == 1 && i == hole); }
+    // steps that Q tile t takes before step i
+    __device__ __forceinline__ int before(int t, int i) const { return i - ((t == 1 && hole >= 0 && i > hole) ? 1 : 0); }
 };
 
+// The steps of the item's two Q tiles under a window (q0, bh, kv_bh are set).  Each 128-row tile needs the tiles that hold
+// its first row's lowest and its last row's highest key; the pair walks the union.
+__device__ __forceinline__ void pipe_window_steps(const PipeParams& prm, PipeItem& it, int only_tile, int BM, int BN) {
+    const int off = -prm.k_offset;
+    const int sinks = prm.sinks < prm.Sk ? prm.sinks : prm.Sk;
+    int lo[2], hi[2];     // window tiles of each Q tile; hi < lo: none
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int r0 = it.q0 + t * BM, r1 = r0 + BM - 1 < prm.Sq ? r0 + BM - 1 : prm.Sq - 1;
+        const int k0 = r0 + off - prm.window + 1, k1 = r1 + off;
+        lo[t] = (k0 > 0 ? k0 : 0) / BN;
+        hi[t] = (r0 < prm.Sq && k0 < prm.Sk) ? (k1 < prm.Sk ? k1 : prm.Sk - 1) / BN : -1;
+    }
+    const int sink_tiles = (sinks + BN - 1) / BN;
+    const bool any = hi[0] >= lo[0];                       // Q tile 1 has window tiles only if Q tile 0 has
+    it.n_sink = any && lo[0] < sink_tiles ? lo[0] : sink_tiles;
+    it.shift = lo[0] - it.n_sink;
+    it.n_kv0 = it.n_sink + (any ? hi[0] - lo[0] + 1 : 0);
+    // Q tile 1 without window tiles of its own (it stands behind all keys) still takes those first tiles that the pair walks
+    // as Q tile 0's window
+    const int own = hi[1] >= lo[1] ? hi[1] - lo[0] + 1 : (any && sink_tiles > lo[0] ? sink_tiles - lo[0] : 0);
+    it.n_kv1 = it.q0 + BM >= prm.Sq ? 0 : it.n_sink + own;
+    it.hole = (hi[1] >= lo[1] && lo[1] > lo[0] && lo[0] >= sink_tiles) ? it.n_sink : -1;
+    if (only_tile == 1) it.n_kv0 = -1;
+    if (only_tile == 0) it.n_kv1 = -1;
+}
+
+template <bool WINDOW>
 __device__ __forceinline__ PipeItem pipe_decode_item(const PipeParams& prm, int lin_all, int BM, int BN) {
     PipeItem it;
     // the tail of the item order may consist of half items: two consecutive indices per (head, Q tile pair)
@@ -123,20 +164,24 @@ __device__ __forceinline__ PipeItem pipe_decode_item(const PipeParams& prm, int 
     it.q0 = pair * 2 * BM;
     // grouped-query attention: H / Hkv consecutive query heads read the same K/V head
     it.kv_bh = (it.bh / prm.H) * prm.Hkv + (it.bh % prm.H) / (prm.H / prm.Hkv);
+    if constexpr (WINDOW) {
+        pipe_window_steps(prm, it, only_tile, BM, BN);
+    } else {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const int qs = it.q0 + t * BM;
-        int n = 0;
-        if (qs < prm.Sq) {
-            const int last_key = last_visible_key(qs + BM - 1, prm.Sk, prm.causal, prm.k_offset);
-            n = last_key < 0 ? 0 : last_key / BN + 1;   // 0: no row of the tile sees a key of this shard
+        for (int t = 0; t < 2; ++t) {
+            const int qs = it.q0 + t * BM;
+            int n = 0;
+            if (qs < prm.Sq) {
+                const int last_key = last_visible_key(qs + BM - 1, prm.Sk, prm.causal, prm.k_offset);
+                n = last_key < 0 ? 0 : last_key / BN + 1;   // 0: no row of the tile sees a key of this shard
+            }
+            // the part of those tiles that lies in this item's key range
+            int in_range = n - split * prm.split_tiles;
+            if (in_range > prm.split_tiles) in_range = prm.split_tiles;
+            n = in_range < 0 ? 0 : in_range;
+            if (only_tile >= 0 && only_tile != t) n = -1;
+            if (t == 0) it.n_kv0 = n; else it.n_kv1 = n;
         }
-        // the part of those tiles that lies in this item's key range
-        int in_range = n - split * prm.split_tiles;
-        if (in_range > prm.split_tiles) in_range = prm.split_tiles;
-        n = in_range < 0 ? 0 : in_range;
-        if (only_tile >= 0 && only_tile != t) n = -1;
-        if (t == 0) it.n_kv0 = n; else it.n_kv1 = n;
     }
     it.k_tile0 = split * prm.split_tiles;
     it.o_bh = split * prm.BH + it.bh;
@@ -145,8 +190,8 @@ __device__ __forceinline__ PipeItem pipe_decode_item(const PipeParams& prm, int 
 }
 
 // SPLITS: the instance for problems whose keys are cut into ranges (split-KV decoding); the plain instance does not
-// carry the range's tile offset and output head through its loops.
-template <int D, int DTYPE, int POLY_NUM, int POLY_DEN, bool SPLITS = false>
+// carry the range's tile offset and output head through its loops.  WINDOW: the instance for sliding windows (not with SPLITS).
+template <int D, int DTYPE, int POLY_NUM, int POLY_DEN, bool SPLITS = false, bool WINDOW = false>
 __global__ void __launch_bounds__(384, 1)
 attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                         const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmO,
@@ -192,7 +237,8 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         B_COUNT = 22 + 2 * NSLOT
     };
     auto bar = [&](int i) { return bars_u32 + i * 8; };
-    // scheduler slots [4][8]: item index (-1: no more work), bh, kv_bh, q0, n_kv0, n_kv1
+    // scheduler slots [4][8]: item index (-1: no more work), bh, kv_bh, q0, n_kv0, n_kv1, and two words of the instance:
+    // SPLITS: first tile, output head;  WINDOW: shift, n_sink and whether there is a hole
     volatile int* sched_item = reinterpret_cast<volatile int*>(bars + B_COUNT);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + B_COUNT) + 32;
     volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + B_COUNT) + 33;
@@ -250,6 +296,12 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         it.n_kv1 = e[5];
         it.k_tile0 = SPLITS ? e[6] : 0;
         it.o_bh = SPLITS ? e[7] : it.bh;
+        it.hole = -1;
+        if constexpr (WINDOW) {
+            it.shift = e[6];
+            it.n_sink = e[7] >> 1;
+            if (e[7] & 1) it.hole = it.n_sink;
+        }
         it.n_max = it.n_kv0 > it.n_kv1 ? it.n_kv0 : it.n_kv1;
         if (hand_back) mbar_arrive(bar(B_SCHEDEMPTY + slot));
         return item;
@@ -277,14 +329,14 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                     if (next < 0 || next >= prm.n_items) next = -1;
                     volatile int* e = sched_item + slot * 8;
                     if (next >= 0) {
-                        const PipeItem d = pipe_decode_item(prm, next, BM, BN);
+                        const PipeItem d = pipe_decode_item<WINDOW>(prm, next, BM, BN);
                         e[1] = d.bh;
                         e[2] = d.kv_bh;
                         e[3] = d.q0;
                         e[4] = d.n_kv0;
                         e[5] = d.n_kv1;
-                        e[6] = d.k_tile0;
-                        e[7] = d.o_bh;
+                        e[6] = WINDOW ? d.shift : d.k_tile0;
+                        e[7] = WINDOW ? 2 * d.n_sink + (d.hole >= 0 ? 1 : 0) : d.o_bh;
                     }
                     e[0] = next;
                     mbar_arrive(bar(B_SCHEDFULL + slot));
@@ -325,12 +377,12 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                         if (has_v) {
 #pragma unroll
                             for (int bx = 0; bx < NBOX; ++bx)
-                                tma_load_3d(sKV(2 * g) + bx * BN * 128, &tmV, bar(B_KVFULL + g), bx * C::BOX_COLS, (it.k_tile0 + i - 1) * BN, it.kv_bh);
+                                tma_load_3d(sKV(2 * g) + bx * BN * 128, &tmV, bar(B_KVFULL + g), bx * C::BOX_COLS, (WINDOW ? it.tile_of(i - 1) : it.k_tile0 + i - 1) * BN, it.kv_bh);
                         }
                         if (has_k) {
 #pragma unroll
                             for (int bx = 0; bx < NBOX; ++bx)
-                                tma_load_3d(sKV(2 * g + 1) + bx * BN * 128, &tmK, bar(B_KVFULL + g), bx * C::BOX_COLS, (it.k_tile0 + i) * BN, it.kv_bh);
+                                tma_load_3d(sKV(2 * g + 1) + bx * BN * 128, &tmK, bar(B_KVFULL + g), bx * C::BOX_COLS, (WINDOW ? it.tile_of(i) : it.k_tile0 + i) * BN, it.kv_bh);
                         }
                     }
                     return true;
@@ -400,7 +452,8 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                 if (it.n_max > 0) ok = kv_full_wait(kv_base);
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    if (ok && it.nkv(t) > 0) {
+                    // (a Q tile that leaves step 0 out gets its first S in the loop below)
+                    if (ok && (WINDOW ? it.takes(t, 0) : it.nkv(t) > 0)) {
                         ok = mbar_wait(bar(B_QFULL + t), uses[t] & 1, abort_flag);
                         if (ok) {
                             tc_fence_after_sync();
@@ -418,19 +471,21 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                     if (!(ok = kv_full_wait(kv_base + j + 1))) break;
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
-                        if (j < it.nkv(t)) {
-                            const uint32_t par = (it_base[t] + j) & 1;
+                        const int jt = WINDOW ? it.before(t, j) : j;      // steps of this tile before step j
+                        if (WINDOW ? it.takes(t, j) : j < it.nkv(t)) {
+                            const uint32_t par = (it_base[t] + jt) & 1;
                             if (!(ok = mbar_wait(bar(B_PFULL + t), par, abort_flag))) break;
                             // the epilogue of the previous item must have read O_t before it is overwritten
-                            if (j == 0 && uses[t] > 0 && !(ok = mbar_wait(bar(B_OFREE + t), (uses[t] - 1) & 1, abort_flag))) break;
+                            if (jt == 0 && uses[t] > 0 && !(ok = mbar_wait(bar(B_OFREE + t), (uses[t] - 1) & 1, abort_flag))) break;
                             tc_fence_after_sync();
-                            issue_pv(t, vslot, j > 0, 0, 3 * (BN / KSTEP) / 4);
+                            issue_pv(t, vslot, jt > 0, 0, 3 * (BN / KSTEP) / 4);
                             if (!(ok = mbar_wait(bar(B_PFULL2 + t), par, abort_flag))) break;
                             tc_fence_after_sync();
                             issue_pv(t, vslot, true, 3 * (BN / KSTEP) / 4, BN / KSTEP);
                             if (j + 1 == it.nkv(t)) commit(B_OFINAL + t);
                         }
-                        if (j + 1 < it.nkv(t)) {
+                        if (WINDOW ? it.takes(t, j + 1) : j + 1 < it.nkv(t)) {
+                            if (WINDOW && it.before(t, j + 1) == 0 && !(ok = mbar_wait(bar(B_QFULL + t), uses[t] & 1, abort_flag))) break;
                             tc_fence_after_sync();
                             issue_s(t, kslot);
                             commit(B_SFULL + t);
@@ -442,7 +497,7 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                 if (it.n_max > 0) kv_base += it.n_max + 1;
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    it_base[t] += it.nkv(t) > 0 ? it.nkv(t) : 0;
+                    it_base[t] += it.nkv(t) > 0 ? (WINDOW ? it.before(t, it.nkv(t)) : it.nkv(t)) : 0;
                     uses[t] += it.nkv(t) > 0 ? 1 : 0;
                 }
             }
@@ -469,7 +524,7 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             PipeItem it;
             const int item = next_item(k, lane == 0, it);
             if (item < 0) break;
-            const int n = it.nkv(t);
+            const int n = WINDOW && it.nkv(t) > 0 ? it.before(t, it.nkv(t)) : it.nkv(t);
             const int q0 = it.q0;
             const int row = q0 + t * BM + r;
             if (n <= 0) {
@@ -486,19 +541,33 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             }
             const int row_w0 = q0 + t * BM + (warp & 3) * 32;   // first row of this warp
             float m = -INFINITY, l = 0.f;
+            // WINDOW: a row's first tiles may be hidden from it altogether, so its reference maximum is taken from the first
+            // tile that shows it a key (without a window that is always the first tile).
+            bool unset = true, any_unset = true;
 
             for (int j = 0; j < n; ++j) {
                 if (!(ok = mbar_wait(bar(B_SFULL + t), (it_base + j) & 1, abort_flag))) break;
                 tc_fence_after_sync();
                 // Visibility of this K/V tile, per warp (rows 32 w .. 32 w + 31 of the Q tile): a chunk of
                 // 32 keys is FULL (every row sees all of it), EMPTY (no row sees any of it) or PARTIAL.
-                const int kv0 = (it.k_tile0 + j) * BN;
+                const int step = WINDOW && t == 1 && it.hole >= 0 && j >= it.hole ? j + 1 : j;
+                const int kv0 = (WINDOW ? it.tile_of(step) : it.k_tile0 + j) * BN;
                 const int lim = last_visible_key(row, prm.Sk, prm.causal, prm.k_offset);   // of this row
                 const int lim_lo = last_visible_key(row_w0, prm.Sk, prm.causal, prm.k_offset);
                 const int lim_hi = last_visible_key(row_w0 + 31, prm.Sk, prm.causal, prm.k_offset);
-                auto chunk_full = [&](int ch) { return kv0 + 32 * ch + 31 <= lim_lo; };
-                auto chunk_empty = [&](int ch) { return kv0 + 32 * ch > lim_hi; };
-                const bool all_full = chunk_full(BN / 32 - 1);
+                // WINDOW: this row's lowest key of the window, and those of the warp's first and last row
+                const int low = row - prm.k_offset - prm.window + 1;
+                const int low_lo = row_w0 - prm.k_offset - prm.window + 1, low_hi = low_lo + 31;
+                auto chunk_full = [&](int ch) {
+                    const int a = kv0 + 32 * ch;
+                    return a + 31 <= lim_lo && (!WINDOW || a >= low_hi || a + 31 < prm.sinks);
+                };
+                auto chunk_empty = [&](int ch) {
+                    const int a = kv0 + 32 * ch;
+                    return a > lim_hi || (WINDOW && a + 31 < low_lo && a >= prm.sinks);
+                };
+                auto hidden = [&](int key) { return key > lim || (WINDOW && key < low && key >= prm.sinks); };
+                const bool all_full = chunk_full(BN / 32 - 1) && (!WINDOW || kv0 >= low_hi || kv0 + BN - 1 < prm.sinks);
 
                 // Masked (diagonal / ragged) tiles are brought into the form the fast path expects, so that
                 // they run the same (instruction-cache resident) code as every other tile: hidden scores are
@@ -517,7 +586,7 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                             tmem_ld_wait();
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
-                                if (kv0 + ch * 32 + e > lim) tmp[e] = 0xff800000u;
+                                if (hidden(kv0 + ch * 32 + e)) tmp[e] = 0xff800000u;
                         }
                         tmem_st_32x32b_x32(tS + ch * 32, tmp);
                     }
@@ -532,9 +601,9 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                 bool done = false;
                 // With a positive scale every tile takes the fast path: masked tiles were pre-masked above,
                 // and the first tile takes its exact row maximum as the reference first.
-                bool use_fast = j > 0 && all_full;
+                bool use_fast = (WINDOW ? !any_unset : j > 0) && all_full;
                 if (c > 0.f && !use_fast) {
-                    if (j == 0) {
+                    if (WINDOW ? any_unset : j == 0) {
                         float mx0[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) mx0[i] = fmaxf(__uint_as_float(sr[2 * i]), __uint_as_float(sr[2 * i + 1]));
@@ -545,7 +614,15 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                                 mx0[i] = max3(mx0[i], __uint_as_float(sr[e + 2 * i]), __uint_as_float(sr[e + 2 * i + 1]));
                         const float mxf = fmaxf(fmaxf(fmaxf(mx0[0], mx0[1]), fmaxf(mx0[2], mx0[3])),
                                                 fmaxf(fmaxf(mx0[4], mx0[5]), fmaxf(mx0[6], mx0[7])));
-                        m = (mxf == -INFINITY) ? 0.f : mxf;
+                        if constexpr (WINDOW) {
+                            if (unset) {
+                                m = (mxf == -INFINITY) ? 0.f : mxf;
+                                unset = mxf == -INFINITY;
+                            }
+                            any_unset = __any_sync(0xffffffffu, unset);
+                        } else {
+                            m = (mxf == -INFINITY) ? 0.f : mxf;
+                        }
                     }
                     use_fast = true;
                 }
@@ -639,7 +716,7 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                             } else if (!chunk_empty(ch)) {
 #pragma unroll
                                 for (int e = 0; e < 32; ++e)
-                                    mxs[e & 7] = fmaxf(mxs[e & 7], (kv0 + ch * 32 + e <= lim) ? __uint_as_float(sr[ch * 32 + e]) : -INFINITY);
+                                    mxs[e & 7] = fmaxf(mxs[e & 7], !hidden(kv0 + ch * 32 + e) ? __uint_as_float(sr[ch * 32 + e]) : -INFINITY);
                             }
                         }
                         const float mx = fmaxf(fmaxf(fmaxf(mxs[0], mxs[1]), fmaxf(mxs[2], mxs[3])),
@@ -686,7 +763,7 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
 #pragma unroll
                             for (int e = 0; e < 32; ++e) {
                                 const int key = kv0 + ch * 32 + e;
-                                pv[e] = (key <= lim) ? ex2_approx(fmaf(__uint_as_float(sr[ch * 32 + e]), c, nmc)) : 0.f;
+                                pv[e] = !hidden(key) ? ex2_approx(fmaf(__uint_as_float(sr[ch * 32 + e]), c, nmc)) : 0.f;
                                 rs += pv[e];
                             }
                         } else {

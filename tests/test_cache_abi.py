@@ -62,6 +62,31 @@ def test_norm_rope_bwd_validation(lib):
         assert f() in (7, 8) and f(qw=None, q=None, dqw=None) in (7, 8) and f(dv=None, dvi=None) in (7, 8)
 
 
+def test_window_validation(lib):
+    def f(q=0x1000, k=0x2000, v=0x3000, o=0x4000, lse=0x5000, B=1, H=4, Hkv=2, Sq=128, Sk=256, D=128, scale=0.1, W=16, sinks=2, off=0, dtype=1):
+        return lib.attn_fwd_window(q, k, v, o, lse, B, H, Hkv, Sq, Sk, D, scale, W, sinks, off, dtype, None)
+
+    def b(q=0x1000, k=0x2000, v=0x3000, o=0x4000, lse=0x5000, B=1, H=4, Hkv=2, Sq=128, Sk=256, D=128, scale=0.1, W=16, sinks=2, off=0, dtype=1,
+          dout=0x6000, dq=0x7000, dk=0x8000, dv=0x9000, ws=0x10000, ws_n=1 << 28):
+        return lib.attn_bwd_window(q, k, v, o, lse, dout, dq, dk, dv, B, H, Hkv, Sq, Sk, D, scale, W, sinks, off, dtype, ws, ws_n, None)
+    for call in (f, b):
+        for name in ("q", "k", "v", "o", "lse"):
+            assert call(**{name: None}) == 1, name
+        assert call(W=-1) == 2 and call(sinks=-1) == 2 and call(off=-1) == 2 and call(off=2 ** 31 - 300) == 2
+        assert call(B=-1) == 2 and call(Hkv=3) == 2
+        for D in (256, 96, 0):
+            assert call(D=D) == 3
+        assert call(dtype=2) == 4 and call(q=0x1008) == 5 and call(scale=float("nan")) == 6
+        if no_device():
+            assert call() in (7, 8) and call(W=0) in (7, 8) and call(W=2 ** 31 - 1, sinks=2 ** 31 - 1) in (7, 8)
+    assert f(Sq=0) == 0 and b(Sq=0, Sk=0) == 0
+    for name in ("dout", "dq", "dk", "dv"):
+        assert b(**{name: None}) == 1
+    assert b(ws=None) == 10 and b(ws_n=64) == 10
+    assert lib.attn_bwd_window_workspace_bytes(1, 2, 2, 100, 100, 64, 10, 0, 0) >= lib.attn_bwd_workspace_bytes(1, 2, 100)
+    assert lib.attn_bwd_window_workspace_bytes(-1, 2, 2, 100, 100, 64, 10, 0, 0) == 0
+
+
 def test_append_validation(lib):
     def f(q=0x1000, k=0x2000, v=0x3000, st=None, tab=None, n=0, R=0, eps=1e-6, qo=0x4000, kc=0x5000, vc=0x6000, cs=None, pages=4, page=16,
           bt=0x700, ts=4, mp=4, lens=0x800, cu=None, seqs=3, tokens=3, H=4, Hkv=2, D=64, dtype=0):

@@ -261,7 +261,8 @@ int attn_fwd_window(const void* q, const void* k, const void* v, void* o, float*
 
 /*
  * attn_bwd_window -- backward pass of attn_fwd_window: arguments as attn_bwd, with the window of the forward call.
- * workspace: at least attn_bwd_window_workspace_bytes(...) bytes.  Deterministic (no atomics).
+ * workspace: at least attn_bwd_window_workspace_bytes(...) bytes (with sinks it also holds
+ * partial sums for the first keys, whose gradients collect from every later query).  Deterministic (no atomics).
  */
 int attn_bwd_window(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* dout, void* dq,
                     void* dk, void* dv, int B, int H, int Hkv, int Sq, int Sk, int D, float scale, int window, int sinks,

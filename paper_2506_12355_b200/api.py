@@ -126,10 +126,28 @@ def _dtype_code(t: torch.Tensor) -> int:
     raise TypeError("q/k/v must be float16 or bfloat16, got %s" % t.dtype)
 
 
+# torch's current stream of a device as a plain handle, without building a Stream object (3 us of a call's host time)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream_ptr(stream) -> int:
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         stream = torch.cuda.current_stream()
     return int(stream.cuda_stream)
+
+
+def _call(name, device, stream, *args):
+    """The C entry point `name` with `args` and the stream, on `device`; raises AttnError for a status other than ATTN_OK."""
+    fn = getattr(_lib or load(), name)
+    if device.index == torch.cuda.current_device():
+        rc = fn(*args, _stream_ptr(stream))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, _stream_ptr(stream))
+    if rc != 0:
+        raise AttnError(rc, name)
 
 
 def _check_qkv(q, k, v):
@@ -368,13 +386,17 @@ def attn_fwd_window(q, k, v, scale: float, window: int, sinks: int = 0, q_offset
     """Attention under a sliding window: q [B,H,Sq,D] at positions q_offset, q_offset + 1, .., k, v [B,Hkv,Sk,D] (D in {64, 128});
     key j is visible at position p iff j <= p and (j > p - window or j < sinks); window 0: no lower end."""
     B, H, Hkv, Sq, Sk, D, _ = _check_grouped(q, k, v)
-    dt = _dtype_code(q)
-    out, lse = _outputs(q, B, H, Sq, D, out, lse)
-    with torch.cuda.device(q.device):
-        rc = load().attn_fwd_window(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H, Hkv, Sq, Sk, D,
-                                    float(scale), int(window), int(sinks), int(q_offset), dt, _stream_ptr(stream))
-    if rc != 0:
-        raise AttnError(rc, "attn_fwd_window")
+    dt, dtype, device = _dtype_code(q), q.dtype, q.device
+    if out is None:
+        out = torch.empty(q.shape, dtype=dtype, device=device)
+    else:
+        _require(out, "out", (B, H, Sq, D), dtype, device)
+    if lse is None:
+        lse = torch.empty((B, H, Sq), dtype=torch.float32, device=device)
+    else:
+        _require(lse, "lse", (B, H, Sq), torch.float32, device)
+    _call("attn_fwd_window", device, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H, Hkv, Sq, Sk, D,
+          float(scale), int(window), int(sinks), int(q_offset), dt)
     return out, lse
 
 
@@ -387,28 +409,23 @@ def attn_bwd_window(q, k, v, o, lse, dout, scale: float, window: int, sinks: int
     """Gradients (dq, dk, dv) of attn_fwd_window's output for the upstream gradient dout; o and lse from the forward call.
     `workspace`: CUDA uint8 tensor of at least attn_bwd_window_workspace_bytes(...) bytes (allocated here when None)."""
     B, H, Hkv, Sq, Sk, D, _ = _check_grouped(q, k, v)
-    _check_shape("o", o, (B, H, Sq, D))
-    _check_shape("dout", dout, (B, H, Sq, D))
-    _check_shape("lse", lse, (B, H, Sq))
-    dt = _dtype_code(q)
+    dt, dtype, device = _dtype_code(q), q.dtype, q.device
+    q_shape, k_shape = (B, H, Sq, D), (B, Hkv, Sk, D)
+    _require(o, "o", q_shape, dtype, device)
+    _require(dout, "dout", q_shape, dtype, device)
+    _require(lse, "lse", (B, H, Sq), torch.float32, device)
     dq = torch.empty_like(q) if dq is None else dq
     dk = torch.empty_like(k) if dk is None else dk
     dv = torch.empty_like(v) if dv is None else dv
-    _check_shape("dq", dq, (B, H, Sq, D))
-    _check_shape("dk", dk, (B, Hkv, Sk, D))
-    _check_shape("dv", dv, (B, Hkv, Sk, D))
-    _check_on(q.device, q.dtype, o=o, dout=dout, dq=dq, dk=dk, dv=dv)
-    _check_on(q.device, torch.float32, lse=lse)
-    _check_dense(o=o, lse=lse, dout=dout, dq=dq, dk=dk, dv=dv)
+    _require(dq, "dq", q_shape, dtype, device)
+    _require(dk, "dk", k_shape, dtype, device)
+    _require(dv, "dv", k_shape, dtype, device)
     if workspace is None:
         n = attn_bwd_window_workspace_bytes(B, H, Hkv, Sq, Sk, D, window, sinks, q_offset)
-        workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=q.device)
-    with torch.cuda.device(q.device):
-        rc = load().attn_bwd_window(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), dout.data_ptr(),
-                                    dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, H, Hkv, Sq, Sk, D, float(scale), int(window),
-                                    int(sinks), int(q_offset), dt, workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
-    if rc != 0:
-        raise AttnError(rc, "attn_bwd_window")
+        workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+    _call("attn_bwd_window", device, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), dout.data_ptr(),
+          dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, H, Hkv, Sq, Sk, D, float(scale), int(window), int(sinks), int(q_offset), dt, workspace.data_ptr(),
+          _bytes(workspace))
     return dq, dk, dv
 
 
@@ -416,59 +433,48 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _row_strides(tensors, axes):
-    """Element strides of the given axes of each tensor (0 for None) as a host array, last axis contiguous."""
-    vals = []
-    for t in tensors:
-        if t is None:
-            vals += [0] * len(axes)
-            continue
-        st = t.stride()
-        if st[-1] != 1 and t.shape[-1] > 1:
-            raise ValueError("the values of a head must be contiguous")
-        vals += [st[a] for a in axes]
-    return (ctypes.c_longlong * len(vals))(*vals)
+_Strides = {n: ctypes.c_longlong * n for n in (6, 9)}
 
 
-def _check_on(device, dtype, **tensors):
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if t.device != device:
-            raise ValueError("%s must lie on %s" % (name, device))
-        if dtype is not None and t.dtype != dtype:
-            raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+def _rows3(a, b, c=None):
+    """Element strides of axes 0, 1, 2 of two or three tensors (zeros for None) as a host array."""
+    if c is None:
+        return _Strides[9](*a.stride()[:3], *b.stride()[:3], 0, 0, 0)
+    return _Strides[9](*a.stride()[:3], *b.stride()[:3], *c.stride()[:3])
 
 
-def _check_dense(**tensors):
-    for name, t in tensors.items():
-        if t is not None and not t.is_contiguous():
-            raise ValueError("%s must be contiguous" % name)
-
-
-def _check_shape(name, t, shape):
-    if t is not None and tuple(t.shape) != shape:
+def _require(t, name, shape, dtype, device, dense=True):
+    """t has this shape, type and device; its last axis (dense: all of it) is contiguous."""
+    if t.shape != shape:
         raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.device != device:
+        raise ValueError("%s must lie on %s, got %s" % (name, device, t.device))
+    if dense:
+        if not t.is_contiguous():
+            raise ValueError("%s must be contiguous" % name)
+    elif shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError("the values of a head of %s must be contiguous" % name)
 
 
 def _check_rope(x, D, q_weight, k_weight, cos_sin):
     """Weights [D] of one type (x's or fp32) and the table fp32 [positions, R]: (weights are fp32, table length, R)."""
     f32 = None
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+    for w in (q_weight, k_weight):
         if w is None:
             continue
-        if tuple(w.shape) != (D,) or not w.is_contiguous() or w.device != x.device:
-            raise ValueError("%s must be a contiguous [%d] tensor on %s" % (name, D, x.device))
-        if w.dtype != x.dtype and w.dtype != torch.float32:
-            raise TypeError("%s must be %s or float32, got %s" % (name, x.dtype, w.dtype))
+        _require(w, "q_weight, k_weight", (D,), x.dtype if w.dtype != torch.float32 else torch.float32, x.device)
         if f32 is not None and f32 != (w.dtype == torch.float32):
             raise TypeError("q_weight and k_weight must share one dtype")
         f32 = w.dtype == torch.float32
     if cos_sin is None:
         return int(bool(f32)), 0, 0
-    if cos_sin.dim() != 2 or cos_sin.dtype != torch.float32 or not cos_sin.is_contiguous() or cos_sin.device != x.device:
-        raise ValueError("cos_sin must be a contiguous float32 [positions, R] tensor on %s" % x.device)
-    return int(bool(f32)), cos_sin.shape[0], cos_sin.shape[1]
+    if cos_sin.dim() != 2:
+        raise ValueError("cos_sin must be [positions, R]")
+    shape = cos_sin.shape
+    _require(cos_sin, "cos_sin", shape, torch.float32, x.device)
+    return int(bool(f32)), shape[0], shape[1]
 
 
 def attn_qk_norm_rope(q, k, v, q_weight, k_weight, cos_sin, positions=None, eps: float = 1e-6, interleaved: bool = False,
@@ -482,34 +488,34 @@ def attn_qk_norm_rope(q, k, v, q_weight, k_weight, cos_sin, positions=None, eps:
         raise ValueError("q and k must be [B,S,heads,D]")
     B, S, H, D = q.shape
     Hkv = k.shape[2]
-    _check_shape("k", k, (B, S, Hkv, D))
-    _check_shape("v", v, (B, S, Hkv, D))
-    dt = _dtype_code(q)
+    dt, dtype, device = _dtype_code(q), q.dtype, q.device
     if not q.is_cuda:
         raise ValueError("q must be a CUDA tensor")
-    _check_on(q.device, q.dtype, k=k, v=v, q_out=q_out, k_out=k_out, v_out=v_out)
+    _require(q, "q", (B, S, H, D), dtype, device, False)
+    _require(k, "k", (B, S, Hkv, D), dtype, device, False)
     f32, n_pos, R = _check_rope(q, D, q_weight, k_weight, cos_sin)
     if positions is not None:
-        _check_shape("positions", positions, (B, S))
-        _check_on(q.device, torch.int32, positions=positions)
-        _check_dense(positions=positions)
-    q_out = torch.empty((B, H, S, D), dtype=q.dtype, device=q.device) if q_out is None else q_out
-    k_out = torch.empty((B, Hkv, S, D), dtype=q.dtype, device=q.device) if k_out is None else k_out
+        _require(positions, "positions", (B, S), torch.int32, device)
+    if q_out is None:
+        q_out = torch.empty((B, H, S, D), dtype=dtype, device=device)
+    else:
+        _require(q_out, "q_out", (B, H, S, D), dtype, device)
+    kv_shape = (B, Hkv, S, D)
+    if k_out is None:
+        k_out = torch.empty(kv_shape, dtype=dtype, device=device)
+    else:
+        _require(k_out, "k_out", kv_shape, dtype, device)
     if v is None:
         v_out = None
-    elif v_out is None:
-        v_out = torch.empty((B, Hkv, S, D), dtype=q.dtype, device=q.device)
-    _check_shape("q_out", q_out, (B, H, S, D))
-    _check_shape("k_out", k_out, (B, Hkv, S, D))
-    _check_shape("v_out", v_out, (B, Hkv, S, D))
-    _check_dense(q_out=q_out, k_out=k_out, v_out=v_out)
-    with torch.cuda.device(q.device):
-        rc = load().attn_qk_norm_rope(q.data_ptr(), k.data_ptr(), _ptr(v), _row_strides((q, k, v), (0, 1, 2)), _ptr(q_weight),
-                                      _ptr(k_weight), f32, _ptr(cos_sin), n_pos, R, int(bool(interleaved)), _ptr(positions),
-                                      float(eps), q_out.data_ptr(), k_out.data_ptr(), _ptr(v_out), B, S, H, Hkv, D, dt,
-                                      _stream_ptr(stream))
-    if rc != 0:
-        raise AttnError(rc, "attn_qk_norm_rope")
+    else:
+        _require(v, "v", (B, S, Hkv, D), dtype, device, False)
+        if v_out is None:
+            v_out = torch.empty(kv_shape, dtype=dtype, device=device)
+        else:
+            _require(v_out, "v_out", kv_shape, dtype, device)
+    _call("attn_qk_norm_rope", device, stream, q.data_ptr(), k.data_ptr(), _ptr(v), _rows3(q, k, v), _ptr(q_weight), _ptr(k_weight), f32,
+          _ptr(cos_sin), n_pos, R, bool(interleaved), _ptr(positions), float(eps), q_out.data_ptr(), k_out.data_ptr(), _ptr(v_out), B, S, H,
+          Hkv, D, dt)
     return q_out, k_out, v_out
 
 
@@ -527,58 +533,63 @@ def attn_qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positio
         raise ValueError("q and k must be [B,S,heads,D]")
     B, S, H, D = q.shape
     Hkv = k.shape[2]
-    _check_shape("k", k, (B, S, Hkv, D))
-    _check_shape("dq", dq, (B, H, S, D))
-    _check_shape("dk", dk, (B, Hkv, S, D))
-    _check_shape("dv", dv, (B, Hkv, S, D))
-    dt = _dtype_code(q)
+    dt, dtype, device = _dtype_code(q), q.dtype, q.device
     if not q.is_cuda:
         raise ValueError("q must be a CUDA tensor")
-    _check_on(q.device, q.dtype, k=k, dq=dq, dk=dk, dv=dv, dq_in=dq_in, dk_in=dk_in, dv_in=dv_in)
-    _check_dense(dq=dq, dk=dk, dv=dv)
+    q_shape, k_shape = (B, S, H, D), (B, S, Hkv, D)
+    _require(q, "q", q_shape, dtype, device, False)
+    _require(k, "k", k_shape, dtype, device, False)
+    _require(dq, "dq", (B, H, S, D), dtype, device)
+    _require(dk, "dk", (B, Hkv, S, D), dtype, device)
     f32, n_pos, R = _check_rope(q, D, q_weight, k_weight, cos_sin)
     if positions is not None:
-        _check_shape("positions", positions, (B, S))
-        _check_on(q.device, torch.int32, positions=positions)
-        _check_dense(positions=positions)
-    dq_in = torch.empty((B, S, H, D), dtype=q.dtype, device=q.device) if dq_in is None else dq_in
-    dk_in = torch.empty((B, S, Hkv, D), dtype=q.dtype, device=q.device) if dk_in is None else dk_in
+        _require(positions, "positions", (B, S), torch.int32, device)
+    if dq_in is None:
+        dq_in = torch.empty(q_shape, dtype=dtype, device=device)
+    else:
+        _require(dq_in, "dq_in", q_shape, dtype, device, False)
+    if dk_in is None:
+        dk_in = torch.empty(k_shape, dtype=dtype, device=device)
+    else:
+        _require(dk_in, "dk_in", k_shape, dtype, device, False)
     if dv is None:
         dv_in = None
-    elif dv_in is None:
-        dv_in = torch.empty((B, S, Hkv, D), dtype=q.dtype, device=q.device)
-    _check_shape("dq_in", dq_in, (B, S, H, D))
-    _check_shape("dk_in", dk_in, (B, S, Hkv, D))
-    _check_shape("dv_in", dv_in, (B, S, Hkv, D))
-    dqw = None if q_weight is None else torch.empty(D, dtype=torch.float32, device=q.device)
-    dkw = None if k_weight is None else torch.empty(D, dtype=torch.float32, device=q.device)
+    else:
+        _require(dv, "dv", (B, Hkv, S, D), dtype, device)
+        if dv_in is None:
+            dv_in = torch.empty(k_shape, dtype=dtype, device=device)
+        else:
+            _require(dv_in, "dv_in", k_shape, dtype, device, False)
+    dqw = None if q_weight is None else torch.empty(D, dtype=torch.float32, device=device)
+    dkw = None if k_weight is None else torch.empty(D, dtype=torch.float32, device=device)
     if workspace is None:
-        workspace = torch.empty(max(attn_qk_norm_rope_bwd_workspace_bytes(D), 256), dtype=torch.uint8, device=q.device)
-    with torch.cuda.device(q.device):
-        rc = load().attn_qk_norm_rope_bwd(dq.data_ptr(), dk.data_ptr(), _ptr(dv), q.data_ptr(), k.data_ptr(),
-                                          _row_strides((q, k), (0, 1, 2)), _ptr(q_weight), _ptr(k_weight), f32, _ptr(cos_sin),
-                                          n_pos, R, int(bool(interleaved)), _ptr(positions), float(eps), dq_in.data_ptr(),
-                                          dk_in.data_ptr(), _ptr(dv_in), _row_strides((dq_in, dk_in, dv_in), (0, 1, 2)),
-                                          _ptr(dqw), _ptr(dkw), B, S, H, Hkv, D, dt, workspace.data_ptr(), workspace.numel(),
-                                          _stream_ptr(stream))
-    if rc != 0:
-        raise AttnError(rc, "attn_qk_norm_rope_bwd")
+        workspace = torch.empty(max(attn_qk_norm_rope_bwd_workspace_bytes(D), 256), dtype=torch.uint8, device=device)
+    _call("attn_qk_norm_rope_bwd", device, stream, dq.data_ptr(), dk.data_ptr(), _ptr(dv), q.data_ptr(), k.data_ptr(), _rows3(q, k),
+          _ptr(q_weight), _ptr(k_weight), f32, _ptr(cos_sin), n_pos, R, bool(interleaved), _ptr(positions), float(eps), dq_in.data_ptr(),
+          dk_in.data_ptr(), _ptr(dv_in), _rows3(dq_in, dk_in, dv_in), _ptr(dqw), _ptr(dkw), B, S, H, Hkv, D, dt, workspace.data_ptr(),
+          _bytes(workspace))
     return dq_in, dk_in, dv_in, dqw, dkw
 
 
-def _check_cache(x, D, k_cache, v_cache, block_table, seq_lens):
+def _bytes(workspace):
+    return workspace.numel() * workspace.element_size()
+
+
+def _check_cache(D, dtype, device, k_cache, v_cache, block_table, seq_lens):
     """Caches [pages, Hkv, page_size, D] (any strides, rows contiguous), block_table int32 [sequences, max_pages], seq_lens
-    int32 [sequences].  Returns (pages, Hkv, page_size)."""
-    if k_cache.dim() != 4 or k_cache.shape[3] != D or v_cache.shape != k_cache.shape:
-        raise ValueError("k_cache and v_cache must be [pages, Hkv, page_size, %d]" % D)
-    _check_on(x.device, x.dtype, k_cache=k_cache, v_cache=v_cache)
-    _check_on(x.device, torch.int32, block_table=block_table, seq_lens=seq_lens)
-    n, Hkv, page_size, _ = k_cache.shape
-    if seq_lens.dim() != 1 or block_table.dim() != 2 or block_table.shape[0] != seq_lens.shape[0]:
+    int32 [sequences].  Returns (pages, Hkv, page_size, the caches' strides)."""
+    shape = k_cache.shape
+    if len(shape) != 4 or shape[3] != D:
+        raise ValueError("k_cache and v_cache must be [pages, Hkv, page_size, %d], got %s" % (D, list(shape)))
+    _require(k_cache, "k_cache", shape, dtype, device, False)
+    _require(v_cache, "v_cache", shape, dtype, device, False)
+    if seq_lens.dim() != 1 or block_table.dim() != 2:
         raise ValueError("block_table must be [sequences, max_pages] and seq_lens [sequences]")
-    if not seq_lens.is_contiguous() or (block_table.stride(1) != 1 and block_table.shape[1] > 1):
-        raise ValueError("seq_lens and the rows of block_table must be contiguous")
-    return n, Hkv, page_size
+    n = seq_lens.shape[0]
+    _require(seq_lens, "seq_lens", (n,), torch.int32, device)
+    _require(block_table, "block_table", (n, block_table.shape[1]), torch.int32, device, False)
+    k, v = k_cache.stride(), v_cache.stride()
+    return shape[0], shape[1], shape[2], _Strides[6](k[0], k[1], k[2], v[0], v[1], v[2])
 
 
 def attn_paged_append(q, k, v, k_cache, v_cache, block_table, seq_lens, q_weight=None, k_weight=None, cos_sin=None, cu_seqlens=None,
@@ -590,46 +601,42 @@ def attn_paged_append(q, k, v, k_cache, v_cache, block_table, seq_lens, q_weight
     behind the end, and of sequences of length 0, are padding: nothing is written for them.  Returns q_out [T,H,D]."""
     if k.dim() != 3 or (q is not None and q.dim() != 3):
         raise ValueError("q must be [tokens,H,D]; k and v [tokens,Hkv,D]")
-    T, Hkv, D = k.shape
-    _check_shape("v", v, (T, Hkv, D))
-    H = 0
-    if q is not None:
-        H = q.shape[1]
-        _check_shape("q", q, (T, H, D))
-    dt = _dtype_code(k)
+    T, Hkv, D = kv_shape = k.shape
+    dt, dtype, device = _dtype_code(k), k.dtype, k.device
     if not k.is_cuda:
         raise ValueError("k must be a CUDA tensor")
-    _check_on(k.device, k.dtype, q=q, v=v, q_out=q_out)
+    _require(k, "k", kv_shape, dtype, device, False)
+    _require(v, "v", kv_shape, dtype, device, False)
+    H, qs = 0, (0, 0)
+    if q is not None:
+        H = q.shape[1]
+        _require(q, "q", (T, H, D), dtype, device, False)
+        qs = q.stride()
+        if q_out is None:
+            q_out = torch.empty((T, H, D), dtype=dtype, device=device)
+        else:
+            _require(q_out, "q_out", (T, H, D), dtype, device)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
     f32, n_pos, R = _check_rope(k, D, q_weight, k_weight, cos_sin)
-    pages, heads, page_size = _check_cache(k, D, k_cache, v_cache, block_table, seq_lens)
+    pages, heads, page_size, cache_strides = _check_cache(D, dtype, device, k_cache, v_cache, block_table, seq_lens)
     if heads != Hkv:
         raise ValueError("the caches hold %d heads, k has %d" % (heads, Hkv))
     n_seqs = seq_lens.shape[0]
     if cu_seqlens is not None:
-        _check_shape("cu_seqlens", cu_seqlens, (n_seqs + 1,))
-        _check_on(k.device, torch.int32, cu_seqlens=cu_seqlens)
-        _check_dense(cu_seqlens=cu_seqlens)
+        _require(cu_seqlens, "cu_seqlens", (n_seqs + 1,), torch.int32, device)
     elif T != n_seqs:
         raise ValueError("without cu_seqlens there is one token per sequence: %d tokens, %d sequences" % (T, n_seqs))
-    if q is None:
-        q_out = None
-    elif q_out is None:
-        q_out = torch.empty((T, H, D), dtype=k.dtype, device=k.device)
-    _check_shape("q_out", q_out, (T, H, D))
-    _check_dense(q_out=q_out)
-    with torch.cuda.device(k.device):
-        rc = load().attn_paged_append(_ptr(q), k.data_ptr(), v.data_ptr(), _row_strides((q, k, v), (0, 1)), _ptr(q_weight),
-                                      _ptr(k_weight), f32, _ptr(cos_sin), n_pos, R, int(bool(interleaved)), float(eps), _ptr(q_out),
-                                      k_cache.data_ptr(), v_cache.data_ptr(), _row_strides((k_cache, v_cache), (0, 1, 2)), pages,
-                                      page_size, block_table.data_ptr(), block_table.stride(0), block_table.shape[1],
-                                      seq_lens.data_ptr(), _ptr(cu_seqlens), n_seqs, T, H, Hkv, D, dt, _stream_ptr(stream))
-    if rc != 0:
-        raise AttnError(rc, "attn_paged_append")
+    ks, vs = k.stride(), v.stride()
+    _call("attn_paged_append", device, stream, _ptr(q), k.data_ptr(), v.data_ptr(), _Strides[6](qs[0], qs[1], ks[0], ks[1], vs[0], vs[1]),
+          _ptr(q_weight), _ptr(k_weight), f32, _ptr(cos_sin), n_pos, R, bool(interleaved), float(eps), _ptr(q_out), k_cache.data_ptr(),
+          v_cache.data_ptr(), cache_strides, pages, page_size, block_table.data_ptr(), block_table.stride(0), block_table.shape[1],
+          seq_lens.data_ptr(), _ptr(cu_seqlens), n_seqs, T, H, Hkv, D, dt)
     return q_out
 
 
 def attn_paged_decode_workspace_bytes(H, Hkv, D) -> int:
-    return int(load().attn_paged_decode_workspace_bytes(H, Hkv, D))
+    return int((_lib or load()).attn_paged_decode_workspace_bytes(H, Hkv, D))
 
 
 def attn_paged_decode(q, k_cache, v_cache, block_table, seq_lens, scale: float, window: int = 0, sinks: int = 0, out=None,
@@ -639,30 +646,27 @@ def attn_paged_decode(q, k_cache, v_cache, block_table, seq_lens, scale: float, 
     `workspace`: CUDA uint8 tensor of at least attn_paged_decode_workspace_bytes(H, Hkv, D) bytes (allocated here when None)."""
     if q.dim() != 3:
         raise ValueError("q must be [B,H,D]")
-    B, H, D = q.shape
-    dt = _dtype_code(q)
-    if not q.is_cuda or not q.is_contiguous():
-        raise ValueError("q must be a contiguous CUDA tensor")
-    pages, Hkv, page_size = _check_cache(q, D, k_cache, v_cache, block_table, seq_lens)
-    _check_shape("seq_lens", seq_lens, (B,))
+    B, H, D = q_shape = q.shape
+    dt, dtype, device = _dtype_code(q), q.dtype, q.device
+    if not q.is_cuda:
+        raise ValueError("q must be a CUDA tensor")
+    _require(q, "q", q_shape, dtype, device)
+    pages, Hkv, page_size, cache_strides = _check_cache(D, dtype, device, k_cache, v_cache, block_table, seq_lens)
+    if seq_lens.shape[0] != B:
+        raise ValueError("q has %d rows, seq_lens %d" % (B, seq_lens.shape[0]))
     if out is None:
-        out = torch.empty((B, H, D), dtype=q.dtype, device=q.device)
+        out = torch.empty(q_shape, dtype=dtype, device=device)
+    else:
+        _require(out, "out", q_shape, dtype, device)
     if lse is None:
-        lse = torch.empty((B, H), dtype=torch.float32, device=q.device)
-    _check_shape("out", out, (B, H, D))
-    _check_shape("lse", lse, (B, H))
-    _check_on(q.device, q.dtype, out=out)
-    _check_on(q.device, torch.float32, lse=lse)
-    _check_dense(out=out, lse=lse)
+        lse = torch.empty((B, H), dtype=torch.float32, device=device)
+    else:
+        _require(lse, "lse", (B, H), torch.float32, device)
     if workspace is None:
-        workspace = torch.empty(max(attn_paged_decode_workspace_bytes(H, Hkv, D), 256), dtype=torch.uint8, device=q.device)
-    with torch.cuda.device(q.device):
-        rc = load().attn_paged_decode(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _row_strides((k_cache, v_cache), (0, 1, 2)),
-                                      pages, page_size, block_table.data_ptr(), block_table.stride(0), block_table.shape[1],
-                                      seq_lens.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H, Hkv, D, float(scale), int(window),
-                                      int(sinks), dt, workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
-    if rc != 0:
-        raise AttnError(rc, "attn_paged_decode")
+        workspace = torch.empty(max(attn_paged_decode_workspace_bytes(H, Hkv, D), 256), dtype=torch.uint8, device=device)
+    _call("attn_paged_decode", device, stream, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), cache_strides, pages, page_size,
+          block_table.data_ptr(), block_table.stride(0), block_table.shape[1], seq_lens.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H,
+          Hkv, D, float(scale), int(window), int(sinks), dt, workspace.data_ptr(), _bytes(workspace))
     return out, lse
 
 

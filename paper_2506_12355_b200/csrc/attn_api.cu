@@ -593,6 +593,53 @@ namespace {
 // attn_bwd's workspace: two fp32 row vectors [B*H][Sq_pad], Sq_pad = Sq rounded up to a multiple of 64
 size_t bwd_sq_pad(int Sq) { return (static_cast<size_t>(Sq) + 63) / 64 * 64; }
 
+// A launch that may begin while the kernel before it on the stream still runs; the kernel itself waits for that one's
+// results (griddepcontrol.wait).
+template <class... Params, class... Args>
+bool launch_dependent(void (*kern)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, Params(args)...) == cudaSuccess;
+}
+
+// How attn_bwd_window cuts the work on the first keys' tiles (BwdParams::n_chunks; a function of the shape alone, because
+// the workspace size follows from it).  Such a tile has the steps of its own window and, for every query behind that, one per
+// 64 rows and query head.  Those are cut so that an item is no longer than a usual tile or than a third of an SM's share
+// of the whole pass, whichever is more; where they are fewer than a usual tile's steps they stay with the tile.
+struct SinkPlan {
+    int n_tiles = 0, n_chunks = 0;
+    size_t part_floats = 0;
+};
+
+SinkPlan sink_plan(int B, int H, int Hkv, int Sq, int Sk, int D, int window, int sinks, int q_offset) {
+    SinkPlan s;
+    if (B <= 0 || H <= 0 || Hkv <= 0 || Sq <= 0 || Sk <= 0 || sinks <= 0) return s;
+    const int64_t group = H / Hkv, subs = (static_cast<int64_t>(Sq) + 63) / 64, tiles = (static_cast<int64_t>(Sk) + 127) / 128;
+    const int64_t n_tiles = ((sinks < Sk ? sinks : Sk) + 127) / 128;
+    int64_t window_rows = static_cast<int64_t>(window) + 127;                        // of one tile
+    if (window_rows > Sq) window_rows = Sq;
+    const int64_t usual = group * ((window_rows + 63) / 64 + 1);
+    int64_t last = (Sk < 128 ? Sk : 128) - 1 + static_cast<int64_t>(window) - 1 - q_offset;   // last query of tile 0's window
+    int64_t behind = last < 0 ? subs : subs - (last / 64 + 1);
+    if (behind * group <= usual) return s;
+    const int64_t all = static_cast<int64_t>(B) * Hkv * (tiles * usual + n_tiles * behind * group);
+    const int64_t share = all / (148 * 3), steps = usual > share ? usual : share;
+    int64_t n = (behind * group + steps - 1) / steps;
+    if (n > 64) n = 64;
+    s.n_tiles = static_cast<int>(n_tiles);
+    s.n_chunks = static_cast<int>(n);
+    s.part_floats = static_cast<size_t>(B) * Hkv * n_tiles * (n + 1) * 2 * 128 * D;
+    return s;
+}
+
 // The backward pass of attn_bwd and, with WINDOW, of attn_bwd_window (whose own arguments are the last three).
 template <bool WINDOW>
 int bwd(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* dout, void* dq, void* dk, void* dv,
@@ -612,8 +659,10 @@ int bwd(const void* q, const void* k, const void* v, const void* o, const float*
          reinterpret_cast<uintptr_t>(dv)) & 15u)
         return ATTN_ERR_MISALIGNED;
     if (n_q == 0 && n_kv == 0) return ATTN_OK;
+    const SinkPlan sinks_cut = WINDOW ? sink_plan(B, H, Hkv, Sq, Sk, D, window, sinks, q_offset) : SinkPlan();
     if (n_q > 0 && n_kv > 0 &&
-        (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < attn_bwd_workspace_bytes(B, H, Sq)))
+        (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) ||
+         workspace_bytes < attn_bwd_workspace_bytes(B, H, Sq) + sinks_cut.part_floats * sizeof(float)))
         return ATTN_ERR_WORKSPACE;
     rc = check_arch();
     if (rc != ATTN_OK) return rc;
@@ -627,7 +676,8 @@ int bwd(const void* q, const void* k, const void* v, const void* o, const float*
     }
     const int64_t BH = static_cast<int64_t>(B) * H, BHkv = static_cast<int64_t>(B) * Hkv;
     const int64_t n_qtiles = (static_cast<int64_t>(Sq) + 127) / 128, n_ktiles = (static_cast<int64_t>(Sk) + 127) / 128;
-    if (n_qtiles * BH > 2147483647LL || n_ktiles * BHkv > 2147483647LL) return ATTN_ERR_BAD_SHAPE;
+    const int64_t n_kv_items = BHkv * (n_ktiles + static_cast<int64_t>(sinks_cut.n_tiles) * sinks_cut.n_chunks);
+    if (n_qtiles * BH > 2147483647LL || n_kv_items > 2147483647LL) return ATTN_ERR_BAD_SHAPE;
     const int64_t sq_pad = static_cast<int64_t>(bwd_sq_pad(Sq));
     float* nl2 = static_cast<float*>(workspace);
     float* ndelta = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + align256(static_cast<size_t>(BH) * sq_pad * sizeof(float)));
@@ -643,6 +693,10 @@ int bwd(const void* q, const void* k, const void* v, const void* o, const float*
     prm.window = window;
     prm.sinks = sinks;
     prm.q_offset = q_offset;
+    prm.n_sink_tiles = sinks_cut.n_tiles;
+    prm.n_chunks = sinks_cut.n_chunks;
+    prm.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + attn_bwd_workspace_bytes(B, H, Sq));
+    prm.n_tiles_total_kv = static_cast<int>(n_ktiles * BHkv);
     prm.H = H;
     prm.Hkv = Hkv;
     prm.n_qtiles = static_cast<int>(n_qtiles);
@@ -655,7 +709,7 @@ int bwd(const void* q, const void* k, const void* v, const void* o, const float*
     if (device_info(&di, &dev) != ATTN_OK) return ATTN_ERR_CUDA;
     const int sms = di.sm_count;   // persistent grids: one CTA per SM, later tiles from the stream's work counter
     unsigned int* counter = nullptr;
-    if (n_qtiles * BH > sms || n_ktiles * BHkv > sms) {
+    if (n_qtiles * BH > sms || n_kv_items > sms) {
         rc = work_counter(di, dev, st, &counter);
         if (rc != ATTN_OK) return rc;
     }
@@ -689,11 +743,17 @@ int bwd(const void* q, const void* k, const void* v, const void* o, const float*
             mq, mdo, mk64, mv64, mdq, mdq, prm);                                                                           \
         prm.out0 = dv;                                                                                                     \
         prm.out1 = dk;                                                                                                     \
-        prm.n_tiles_total = static_cast<int>(n_ktiles * BHkv);                                                             \
+        prm.n_tiles_total = static_cast<int>(n_kv_items);                                                                  \
         prm.counter = prm.n_tiles_total > sms ? counter : nullptr;                                                         \
         kkv<<<static_cast<unsigned>(prm.n_tiles_total < sms ? prm.n_tiles_total : sms), CKV::THREADS, CKV::SMEM_BYTES, st>>>( \
             mk, mv, mq64, mdo64, mdv, mdk, prm);                                                                           \
-        return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;                                                \
+        if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;                                                       \
+        if (!WINDOW || sinks_cut.n_chunks == 0) return ATTN_OK;                                                            \
+        const int64_t total = BHkv * sinks_cut.n_tiles * 2 * 128 * (DD / 4);                                               \
+        return launch_dependent(attn_grad::attn_bwd_sink_join_kernel<DD, TT>, dim3(static_cast<unsigned>((total + 255) / 256)), \
+                                dim3(256), 0, st, prm.parts, dk, dv, sinks_cut.n_tiles, sinks_cut.n_chunks + 1, Sk, scale, total) \
+                   ? ATTN_OK                                                                                               \
+                   : ATTN_ERR_CUDA;                                                                                        \
     }
     ATTN_BWD_CASE(64, 0)
     ATTN_BWD_CASE(64, 1)

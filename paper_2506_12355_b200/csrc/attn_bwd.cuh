@@ -111,8 +111,15 @@ struct BwdParams {
     int causal;
     int H, Hkv;
     int n_qtiles, n_ktiles; // 128-row tiles of the query and of the key axis
-    int n_tiles_total;      // tiles of this pass over all heads
+    int n_tiles_total;      // items of this pass over all heads
+    int n_tiles_total_kv;   // 128-row tiles of the key axis over all heads
     int window, sinks, q_offset;   // WINDOW: key j is visible to query i iff j <= p and (j > p - window or j < sinks), p = i + q_offset
+    // WINDOW, MODE 1: all later queries see the first keys, so their tiles would take many times the steps of any other and
+    // the launch would wait for them.  With n_chunks > 0 the steps behind such a tile's window are cut into n_chunks items
+    // of their own (first in the order); those and the tile's window part leave fp32 partial sums, parts[K/V head][tile]
+    // [n_chunks + 1][dV, dK][128][D], and attn_bwd_sink_join_kernel adds them.
+    int n_sink_tiles, n_chunks;
+    float* parts;
     unsigned int* counter;  // work counter {next tile, CTAs done}, zero at launch and again at exit:
                             // tile = gridDim.x + atomicAdd(counter, 1); NULL when the grid covers every tile
     int* status;
@@ -192,13 +199,9 @@ struct BwdTile {
     int n_steps;            // 0: nothing reaches this tile (its gradients are zero)
     int kv_bh_of_q;         // MODE 0: K/V head of this query head
     int n_sink;             // WINDOW, MODE 0: steps before the window's own, over the tiles of the first keys
+    int part;               // WINDOW, MODE 1: index of the partial result this item leaves, or -1
+    int first_step;         // WINDOW, MODE 1: this item's steps begin here in the tile's list
 };
-
-// WINDOW: may key `key` be hidden from query row `row`?
-__device__ __forceinline__ bool window_hides(const BwdParams& prm, int key, int row) {
-    const int p = row + prm.q_offset;
-    return key >= prm.Sk || key > p || (key < p - prm.window + 1 && key >= prm.sinks);
-}
 
 // tmR0 / tmR1: maps of the resident tiles, boxes of 128 rows (MODE 0: Q, dO; MODE 1: K, V); tmT0 / tmT1: maps of
 // the streamed tiles, boxes of 64 rows (MODE 0: K, V; MODE 1: Q, dO); tmOut0 / tmOut1: MODE 0: dQ, unused;
@@ -264,9 +267,22 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tmR0, const __grid_constant_
     const int tiles_per_head = MODE == 0 ? prm.n_qtiles : prm.n_ktiles;
     auto decode = [&](int lin) {
         BwdTile t;
+        t.n_sink = 0;
+        t.part = -1;
+        t.first_step = 0;
+        int chunk = -1;
+        if constexpr (WINDOW && MODE == 1) {
+            const int extra = prm.n_chunks * prm.n_sink_tiles * (prm.n_tiles_total_kv / prm.n_ktiles);   // chunk items
+            if (lin < extra) {
+                chunk = lin % prm.n_chunks;
+                const int x = lin / prm.n_chunks;
+                lin = (x / prm.n_sink_tiles) * prm.n_ktiles + x % prm.n_sink_tiles;
+            } else {
+                lin -= extra;
+            }
+        }
         const int bid_tile = lin % tiles_per_head;
         t.bh_res = lin / tiles_per_head;
-        t.n_sink = 0;
         if constexpr (WINDOW && MODE == 0) {
             // keys from the first row's lowest to the last row's own, behind the tiles of the first keys
             t.tile = prm.n_qtiles - 1 - bid_tile;
@@ -283,11 +299,23 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tmR0, const __grid_constant_
             t.tile = bid_tile;
             const int c0 = t.tile * BT, c1 = c0 + BT - 1 < prm.Sk ? c0 + BT - 1 : prm.Sk - 1;
             int64_t last = static_cast<int64_t>(c1) + prm.window - 1 - prm.q_offset;
-            if (c0 < prm.sinks || last > prm.Sq - 1) last = prm.Sq - 1;
+            if ((c0 < prm.sinks && prm.n_chunks == 0) || last > prm.Sq - 1) last = prm.Sq - 1;
             t.sub_lo = (c0 > prm.q_offset ? c0 - prm.q_offset : 0) / BS;
             t.sub_hi = last < 0 ? 0 : static_cast<int>(last) / BS + 1;
+            if (prm.n_chunks > 0 && t.tile < prm.n_sink_tiles) {
+                t.part = (t.bh_res * prm.n_sink_tiles + t.tile) * (prm.n_chunks + 1) + (chunk < 0 ? prm.n_chunks : chunk);
+                if (chunk >= 0) {    // the queries behind the window
+                    if (t.sub_hi > t.sub_lo) t.sub_lo = t.sub_hi;
+                    t.sub_hi = (prm.Sq + BS - 1) / BS;
+                }
+            }
             if (t.sub_lo > t.sub_hi) t.sub_lo = t.sub_hi;
             t.n_steps = (t.sub_hi - t.sub_lo) * group;
+            if (chunk >= 0) {
+                const int64_t n = t.n_steps;
+                t.first_step = static_cast<int>(n * chunk / prm.n_chunks);
+                t.n_steps = static_cast<int>(n * (chunk + 1) / prm.n_chunks) - t.first_step;
+            }
         } else if constexpr (MODE == 0) {
             t.tile = prm.causal ? prm.n_qtiles - 1 - bid_tile : bid_tile;
             const int last_key = attn_tc::last_visible_key(t.tile * BT + BT - 1, prm.Sk, prm.causal, 0);
@@ -307,12 +335,12 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tmR0, const __grid_constant_
     // streamed tile of step u of tile t: (head index in its tensor, index of the 64-row tile)
     auto step_head = [&](const BwdTile& t, int u) {
         if constexpr (MODE == 0) return t.kv_bh_of_q;
-        else return (t.bh_res / prm.Hkv) * prm.H + (t.bh_res % prm.Hkv) * group + u / (t.sub_hi - t.sub_lo);
+        else return (t.bh_res / prm.Hkv) * prm.H + (t.bh_res % prm.Hkv) * group + (WINDOW ? t.first_step + u : u) / (t.sub_hi - t.sub_lo);
     };
     auto step_sub = [&](const BwdTile& t, int u) {
         if constexpr (WINDOW && MODE == 0) return u < t.n_sink ? u : t.sub_lo + u - t.n_sink;
         else if constexpr (MODE == 0) return u;
-        else return t.sub_lo + u % (t.sub_hi - t.sub_lo);
+        else return t.sub_lo + (WINDOW ? t.first_step + u : u) % (t.sub_hi - t.sub_lo);
     };
     // Consumers of the scheduler: the tile index at position p of this CTA's walk (-1: no more); the slot is handed
     // back at once (the caller keeps what it needs in registers).
@@ -581,6 +609,10 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tmR0, const __grid_constant_
                 if (lin < 0) return -1;
                 t = decode(lin);
                 if (t.n_steps > 0) return p;
+                if (WINDOW && MODE == 1 && t.part >= 0) {
+                    zero_rows(prm.parts, static_cast<int64_t>(t.part) * 2 * BT * 2, 2 * BT * 2, D, tid, 256);   // fp32: two 16-bit rows each
+                    continue;
+                }
                 const int rows_total = MODE == 0 ? prm.Sq : prm.Sk;
                 const int rows = rows_total - t.tile * BT < BT ? rows_total - t.tile * BT : BT;
                 if (rows > 0) {
@@ -642,6 +674,10 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tmR0, const __grid_constant_
 #pragma unroll
                 for (int ch = 0; ch < BS / 32; ++ch) {
                     uint32_t pk_p[16], pk_ds[16];
+                    uint32_t seen = 0;      // WINDOW: bit e: element 32 ch + e is visible
+                    if constexpr (WINDOW && MASKED)
+                        seen = MODE == 0 ? attn_tc::window_keys(key0 + 32 * ch, my_row + prm.q_offset, prm.Sk, prm.window, prm.sinks)
+                                         : attn_tc::window_queries(row0 + 32 * ch + prm.q_offset, my_row, prm.Sk, prm.window, prm.sinks);
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
                         const int col = 32 * ch + e;
@@ -660,12 +696,9 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tmR0, const __grid_constant_
                         float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
                         if constexpr (MASKED) {
                             bool v0, v1;
-                            if constexpr (WINDOW && MODE == 0) {
-                                v0 = !window_hides(prm, key0 + col, my_row);
-                                v1 = !window_hides(prm, key0 + col + 1, my_row);
-                            } else if constexpr (WINDOW) {
-                                v0 = !window_hides(prm, my_row, row0 + col);
-                                v1 = !window_hides(prm, my_row, row0 + col + 1);
+                            if constexpr (WINDOW) {
+                                v0 = seen & (1u << e);
+                                v1 = seen & (2u << e);
                             } else if constexpr (MODE == 0) {
                                 v0 = key0 + col < prm.Sk && (!prm.causal || key0 + col <= my_row);
                                 v1 = key0 + col + 1 < prm.Sk && (!prm.causal || key0 + col + 1 <= my_row);
@@ -717,6 +750,29 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tmR0, const __grid_constant_
             // every 64-column piece of the output has a staging tile of its own: one barrier, then all stores at once ----
             if (!(ok = mbar_wait(bar(B_ACCFINAL), kk & 1, abort_flag))) break;
             tc_fence_after_sync();
+            if (WINDOW && MODE == 1 && t.part >= 0) {
+                // a partial result: fp32, straight to global memory (a row per thread, 128 contiguous bytes at a time)
+                float* part = prm.parts + static_cast<int64_t>(t.part) * 2 * BT * D;
+#pragma unroll
+                for (int a = 0; a < NACC; ++a)
+#pragma unroll
+                    for (int h = 0; h < D / 64; ++h) {
+                        uint32_t acc[32];
+                        tmem_ld_32x32b_x32(tmem + (a == 0 ? C::ACC0_COL : C::ACC1_COL) + lane_off + h * 64 + 32 * half, acc);
+                        tmem_ld_wait();
+                        if (a == NACC - 1 && h == D / 64 - 1) {
+                            tc_fence_before_sync();
+                            mbar_arrive(bar(B_ACCFREE));
+                        }
+                        uint4* dst = reinterpret_cast<uint4*>(part + (a * BT + r) * D + h * 64 + 32 * half);
+#pragma unroll
+                        for (int g = 0; g < 8; ++g) dst[g] = make_uint4(acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]);
+                    }
+                gs0 += t.n_steps;
+                k = kn;
+                t = tn;
+                continue;
+            }
             if (tid == 0) tma_store_wait_read<0>();              // the previous tile's stores have read the staging tiles
             if (!(ok = all_sync())) break;
 #pragma unroll
@@ -769,6 +825,35 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tmR0, const __grid_constant_
     __syncthreads();
     if (tid == 0) finish_cta(prm.status, *abort_flag != 0, prm.counter);
     if (warp == 8) tmem_dealloc(tmem, C::TMEM_COLS);
+}
+
+// dK, dV of the tiles with first keys: the sum of their n_chunks + 1 partial results, in order.  One thread per 4 columns.
+template <int D, int DTYPE>
+__global__ void __launch_bounds__(256)
+attn_bwd_sink_join_kernel(const float* __restrict__ parts, void* __restrict__ dk, void* __restrict__ dv, int n_sink_tiles, int n_parts,
+                          int Sk, float scale, int64_t total) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= total) return;
+    constexpr int SEG = D / 4;
+    const int seg = static_cast<int>(i % SEG);
+    const int row = static_cast<int>(i / SEG % 128);
+    const int a = static_cast<int>(i / (SEG * 128) % 2);
+    const int64_t x = i / (SEG * 128 * 2);                    // (K/V head, tile)
+    const int64_t key = x % n_sink_tiles * 128 + row;
+    if (key >= Sk) return;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float4* src = reinterpret_cast<const float4*>(parts) + ((x * n_parts * 2 + a) * 128 + row) * SEG + seg;
+#pragma unroll 4
+    for (int p = 0; p < n_parts; ++p) {
+        const float4 v = __ldcg(src + static_cast<int64_t>(p) * 2 * 128 * SEG);
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    const float f = a == 1 ? scale : 1.f;
+    uint2 w;
+    w.x = pack2<DTYPE>(s.x * f, s.y * f);
+    w.y = pack2<DTYPE>(s.z * f, s.w * f);
+    reinterpret_cast<uint2*>(a == 1 ? dk : dv)[(x / n_sink_tiles * Sk + key) * SEG + seg] = w;
 }
 
 }  // namespace attn_grad

@@ -84,23 +84,6 @@ int launch_rope(attn_rope::RopeParams& p, int D, int dtype, cudaStream_t st) {
     return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;
 }
 
-// A launch that may begin while the kernel before it on the stream still runs; the kernel itself waits for that one's
-// results (griddepcontrol.wait).
-template <class... Params, class... Args>
-bool launch_dependent(void (*kern)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = block;
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, Params(args)...) == cudaSuccess;
-}
-
 // The row strides of [B, heads, S, D], contiguous.
 attn_rope::Strides head_major(int heads, int S, int D) {
     return attn_rope::Strides{static_cast<int64_t>(heads) * S * D, D, static_cast<int64_t>(S) * D};
@@ -145,8 +128,9 @@ int attn_fwd_window(const void* q, const void* k, const void* v, void* o, float*
 }
 
 size_t attn_bwd_window_workspace_bytes(int B, int H, int Hkv, int Sq, int Sk, int D, int window, int sinks, int q_offset) {
-    (void)Hkv; (void)Sk; (void)D; (void)window; (void)sinks; (void)q_offset;
-    return attn_bwd_workspace_bytes(B, H, Sq);
+    if (B < 0 || H < 0 || Hkv < 0 || Sq < 0 || Sk < 0 || D < 0 || (H > 0 && (Hkv == 0 || H % Hkv != 0))) return 0;
+    if (validate_window(Sq, &window, sinks, q_offset) != ATTN_OK) return 0;
+    return attn_bwd_workspace_bytes(B, H, Sq) + sink_plan(B, H, Hkv, Sq, Sk, D, window, sinks, q_offset).part_floats * sizeof(float);
 }
 
 int attn_bwd_window(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* dout, void* dq,

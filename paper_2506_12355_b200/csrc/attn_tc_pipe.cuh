@@ -207,7 +207,11 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
     constexpr int KSTEP = 32 / ES;               // contraction elements per MMA instruction (32 bytes)
     constexpr int PCOLS = 32 * ES / 4;           // tensor-memory columns of 32 P values
     constexpr float P_OFF = FP8 ? 5.f : 0.f;
-    constexpr float LAG = FP8 ? 3.f : 8.f;
+    // WINDOW: rows often take their first reference from a tile that shows them one key or a few (the first tokens, the
+    // window's lower edge), and the true maximum then runs further ahead.  P may grow as far as its type goes: up to 2^14 in
+    // fp16; bf16 and the fp32 sums have the exponents for 2^64.  (With 2^8 nearly every item took the rescaling path once:
+    // 45 instead of ~25 us at 32 heads x 1000 queries, window 255, one first token.)
+    constexpr float LAG = FP8 ? 3.f : (WINDOW ? (DTYPE == 0 ? 14.f : 64.f) : 8.f);
     using C = PipeCfg<D, ES>;
     constexpr int BM = C::BM, BN = C::BN, NBOX = C::NBOX, NSLOT = C::NSLOT;
     constexpr int NGRP = NSLOT / 2;   // ring groups in flight (two tile slots each)
@@ -555,8 +559,7 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                 const int lim = last_visible_key(row, prm.Sk, prm.causal, prm.k_offset);   // of this row
                 const int lim_lo = last_visible_key(row_w0, prm.Sk, prm.causal, prm.k_offset);
                 const int lim_hi = last_visible_key(row_w0 + 31, prm.Sk, prm.causal, prm.k_offset);
-                // WINDOW: this row's lowest key of the window, and those of the warp's first and last row
-                const int low = row - prm.k_offset - prm.window + 1;
+                // WINDOW: the lowest keys of the window of the warp's first and last row
                 const int low_lo = row_w0 - prm.k_offset - prm.window + 1, low_hi = low_lo + 31;
                 auto chunk_full = [&](int ch) {
                     const int a = kv0 + 32 * ch;
@@ -566,7 +569,10 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                     const int a = kv0 + 32 * ch;
                     return a > lim_hi || (WINDOW && a + 31 < low_lo && a >= prm.sinks);
                 };
-                auto hidden = [&](int key) { return key > lim || (WINDOW && key < low && key >= prm.sinks); };
+                const int pos = row - prm.k_offset;
+                // element e of chunk ch is hidden from this row; `seen`: WINDOW: the chunk's visible keys as bits
+                auto seen_keys = [&](int ch) { return WINDOW ? window_keys(kv0 + 32 * ch, pos, prm.Sk, prm.window, prm.sinks) : 0u; };
+                auto hidden = [&](uint32_t seen, int ch, int e) { return WINDOW ? !(seen & (1u << e)) : kv0 + ch * 32 + e > lim; };
                 const bool all_full = chunk_full(BN / 32 - 1) && (!WINDOW || kv0 >= low_hi || kv0 + BN - 1 < prm.sinks);
 
                 // Masked (diagonal / ragged) tiles are brought into the form the fast path expects, so that
@@ -584,9 +590,10 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                         } else {
                             tmem_ld_32x32b_x32(tS + ch * 32, tmp);
                             tmem_ld_wait();
+                            const uint32_t seen = seen_keys(ch);
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
-                                if (hidden(kv0 + ch * 32 + e)) tmp[e] = 0xff800000u;
+                                if (hidden(seen, ch, e)) tmp[e] = 0xff800000u;
                         }
                         tmem_st_32x32b_x32(tS + ch * 32, tmp);
                     }
@@ -714,9 +721,10 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                                         mxs[i] = max3(mxs[i], __uint_as_float(sr[ch * 32 + e + 2 * i]),
                                                       __uint_as_float(sr[ch * 32 + e + 2 * i + 1]));
                             } else if (!chunk_empty(ch)) {
+                                const uint32_t seen = seen_keys(ch);
 #pragma unroll
                                 for (int e = 0; e < 32; ++e)
-                                    mxs[e & 7] = fmaxf(mxs[e & 7], !hidden(kv0 + ch * 32 + e) ? __uint_as_float(sr[ch * 32 + e]) : -INFINITY);
+                                    mxs[e & 7] = fmaxf(mxs[e & 7], !hidden(seen, ch, e) ? __uint_as_float(sr[ch * 32 + e]) : -INFINITY);
                             }
                         }
                         const float mx = fmaxf(fmaxf(fmaxf(mxs[0], mxs[1]), fmaxf(mxs[2], mxs[3])),
@@ -760,10 +768,10 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                                 acc[(e / 2) & 3] = add_f32x2(acc[(e / 2) & 3], pack_f32x2(pv[e], pv[e + 1]));
                             }
                         } else if (!chunk_empty(ch)) {
+                            const uint32_t seen = seen_keys(ch);
 #pragma unroll
                             for (int e = 0; e < 32; ++e) {
-                                const int key = kv0 + ch * 32 + e;
-                                pv[e] = !hidden(key) ? ex2_approx(fmaf(__uint_as_float(sr[ch * 32 + e]), c, nmc)) : 0.f;
+                                pv[e] = !hidden(seen, ch, e) ? ex2_approx(fmaf(__uint_as_float(sr[ch * 32 + e]), c, nmc)) : 0.f;
                                 rs += pv[e];
                             }
                         } else {

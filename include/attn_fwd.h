@@ -354,7 +354,8 @@ int attn_paged_append(const void* q, const void* k, const void* v, const long lo
  * q, o [B,H,D], lse [B,H]: device, contiguous; H % Hkv == 0 (grouped heads as in attn_fwd_gqa); D in {64, 128, 256}.
  * seq_lens : device int32 [B].  Length 0 (or less) gives O = 0, LSE = -inf.  A length beyond max_pages * page_size is cut to
  *            that, a visible key whose page is not in [0, num_pages) counts as hidden, and either is reported as
- *            ATTN_ERR_DEVICE_INDEX in the device status.  Pages and slots of hidden keys are never read.
+ *            ATTN_ERR_DEVICE_INDEX in the device status.  Pages of which no key is visible are not read; what lies in hidden slots
+ *            does not matter (it may be NaN).  num_pages == 0: every key is hidden.
  * workspace: device, 256-byte aligned, at least attn_paged_decode_workspace_bytes(H, Hkv, D) bytes (whatever the lengths are), or
  *            ATTN_ERR_WORKSPACE.  Two calls that may run at the same time need one each.
  * The lengths and the table are read on the device, so a captured call may be replayed with new ones.  The result does

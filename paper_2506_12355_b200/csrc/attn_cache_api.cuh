@@ -46,6 +46,64 @@ int validate_cache(const void* k_cache, const void* v_cache, const long long* ca
     return ATTN_OK;
 }
 
+// Tensor map over one cache: columns, then the slot, head and page axes by ascending stride; box = 64 columns x `rows` slots,
+// 128-byte swizzle.  `axes` receives the coordinate number of the slot, head and page axis (2 bits each).  A map is a pure
+// function of these arguments; the last ones are kept per thread, as a serving loop passes the same caches in every step.
+struct CacheMapKey {
+    const void* base;
+    long long stride[3];
+    int dtype, D, n[3], rows;
+    bool operator==(const CacheMapKey& o) const {
+        return base == o.base && stride[0] == o.stride[0] && stride[1] == o.stride[1] && stride[2] == o.stride[2] && dtype == o.dtype &&
+               D == o.D && n[0] == o.n[0] && n[1] == o.n[1] && n[2] == o.n[2] && rows == o.rows;
+    }
+};
+
+bool make_cache_map(CUtensorMap* map, int* axes, const void* base, const long long* cache_strides, int dtype, int D, int num_pages, int Hkv,
+                    int page_size, int rows) {
+    struct Entry {
+        bool valid = false;
+        CacheMapKey key;
+        CUtensorMap map;
+        int axes;
+    };
+    constexpr int kEntries = 128;     // the caches of 64 layers
+    thread_local Entry cache[kEntries];
+    const CacheMapKey key{base, {cache_strides[2], cache_strides[1], cache_strides[0]}, dtype, D, {page_size, Hkv, num_pages}, rows};
+    Entry& e = cache[((reinterpret_cast<uintptr_t>(base) >> 9) * 0x9E3779B97F4A7C15ull >> 40) % kEntries];
+    if (!e.valid || !(e.key == key)) {
+        EncodeTiledFn enc = get_encode_fn();
+        if (!enc) return false;
+        int order[3] = {0, 1, 2};     // slot, head, page
+        for (int i = 0; i < 2; ++i)
+            for (int j = 0; j < 2 - i; ++j)
+                if (key.stride[order[j]] > key.stride[order[j + 1]]) {
+                    const int x = order[j];
+                    order[j] = order[j + 1];
+                    order[j + 1] = x;
+                }
+        cuuint64_t dims[4] = {static_cast<cuuint64_t>(D)}, strides[3];
+        cuuint32_t box[4] = {64}, estr[4] = {1, 1, 1, 1};
+        e.axes = 0;
+        for (int i = 0; i < 3; ++i) {
+            const int a = order[i];
+            dims[1 + i] = static_cast<cuuint64_t>(key.n[a]);
+            // (an axis of one element may come with any stride, 0 among them: give it one that the encoder accepts)
+            strides[i] = static_cast<cuuint64_t>(key.n[a] > 1 ? key.stride[a] : D) * 2;
+            box[1 + i] = a == 0 ? static_cast<cuuint32_t>(rows) : 1;
+            e.axes |= (i + 1) << (2 * a);
+        }
+        const CUtensorMapDataType type = dtype == ATTN_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+        e.valid = enc(&e.map, type, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+        if (!e.valid) return false;
+        e.key = key;
+    }
+    *map = e.map;
+    *axes = e.axes;
+    return true;
+}
+
 int log2_of(int x) {
     int s = 0;
     while ((1 << s) < x) ++s;
@@ -355,21 +413,16 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
     DeviceInfo di;
     if (device_info(&di) != ATTN_OK) return ATTN_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (num_pages == 0) return fill_empty(o, lse, static_cast<int64_t>(B) * H * D, static_cast<int64_t>(B) * H, st);
+    for (int i = 0; i < 6; ++i)
+        if (cache_strides[i] < 0 || cache_strides[i] >= (1LL << 39)) return ATTN_ERR_BAD_SHAPE;
     attn_paged::DecodeParams p = {};
     p.q = q;
-    p.k_cache = static_cast<const uint8_t*>(k_cache);
-    p.v_cache = static_cast<const uint8_t*>(v_cache);
     p.o = o;
     p.lse = lse;
     p.block_table = block_table;
     p.seq_lens = seq_lens;
     p.parts = static_cast<float*>(workspace);
-    p.k_page = cache_strides[0] * 2;
-    p.k_head = cache_strides[1] * 2;
-    p.k_slot = cache_strides[2] * 2;
-    p.v_page = cache_strides[3] * 2;
-    p.v_head = cache_strides[4] * 2;
-    p.v_slot = cache_strides[5] * 2;
     p.table_stride = table_stride;
     p.B = B;
     p.H = H;
@@ -395,7 +448,13 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
         using C = attn_paged::DecodeCfg<DD, GG>;                                                                         \
         auto kern = attn_paged::attn_paged_decode_kernel<DD, TT, GG>;                                                    \
         if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), C::SMEM_BYTES)) return ATTN_ERR_CUDA;               \
-        kern<<<grid, C::THREADS, C::SMEM_BYTES, st>>>(p);                                                                \
+        const int rows = page_size < C::CK ? page_size : C::CK;                                                          \
+        p.box_shift = log2_of(rows);                                                                                     \
+        CUtensorMap mk, mv;                                                                                              \
+        if (!make_cache_map(&mk, &p.k_axes, k_cache, cache_strides, TT, DD, num_pages, Hkv, page_size, rows) ||          \
+            !make_cache_map(&mv, &p.v_axes, v_cache, cache_strides + 3, TT, DD, num_pages, Hkv, page_size, rows))        \
+            return ATTN_ERR_CUDA;                                                                                        \
+        kern<<<grid, C::THREADS, C::SMEM_BYTES, st>>>(mk, mv, p);                                                        \
         if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;                                                     \
         return launch_dependent(attn_paged::attn_paged_join_kernel<DD, TT, GG>, dim3(static_cast<unsigned>(pairs)), dim3(256), 0, st, p) \
                    ? ATTN_OK                                                                                             \

@@ -7,27 +7,27 @@
 // Every visible key's K and V row is read once: 4 D bytes per key and K/V head, 2 multiply-adds per value and query head.
 // That is HBM-bound for every group size up to 16 query heads per K/V head, so all of the design serves the loads:
 //
-//   * Key axis cut into tiles of 16 keys per warp; the tiles of all (sequence, K/V head) pairs form one list, of which
-//     every CTA of a one-wave persistent grid takes an equal, contiguous part, whatever the lengths are.  The list is
-//     laid out from the device-side lengths by each CTA for itself (no host copy of the lengths, no plan to keep).
-//     A (sequence, head) pair inside one CTA's part is finished there; one that is cut by a border leaves one fp32
-//     partial result per CTA (at most two per CTA), and a second small kernel joins those.
-//   * A thread copies exactly the 16-byte pieces that it will feed to the tensor core itself (cp.async into its own slots of
-//     a ring in shared memory), so there is no synchronisation between copy and use, pages of any power-of-two size and
-//     any strides cost the same, and 128 KB and more per SM are in flight.
-//   * The products run on mma.sync m16n8k16.  With 16 query rows they need a few percent of its rate; a tcgen05
-//     instruction takes 128 rows, 112 of which would be padding, and K/V tiles staged for it by one thread.
-//     First product: A = Q (rows: query heads), B = K (columns: keys).  The contraction order over D is free, so that a
-//     thread's 16 contiguous bytes serve two instructions.  The accumulator layout of S is the A layout of the second
-//     product (B = V, columns: value dims, again in the order in which 16-byte pieces deliver them).
-//   * P is fed as two 16-bit parts (hi + lo), so its rounding does not show in O.  With up to 8 query heads per K/V head
-//     the low parts take rows 8 .. 15 of the same instructions.
+//   * The keys are cut into chunks of CK per warp, 8 (or 4) chunks to a tile; the tiles of all (sequence, K/V head) pairs form
+//     one list, of which every CTA of a one-wave persistent grid takes an equal, contiguous part, whatever the lengths
+//     are.  Each CTA lays the list out for itself from the device-side lengths (no host copy of them, no plan to keep).
+//     A pair inside one CTA's part is finished there; one that is cut by a border leaves one fp32 partial result per
+//     CTA (at most two per CTA), and a second small kernel joins those.
+//   * Each warp keeps a ring of its own in shared memory, filled by TMA boxes of up to CK rows x 128 bytes (a box lies in one
+//     page), one mbarrier per stage, and no other synchronisation: 128 to 192 KB per SM are in flight.  Measured at
+//     4 x 65536 keys of 8 heads x 128: per-thread 16-byte copies (cp.async) stop at 4.9 TB/s however deep the ring is, the TMA
+//     reaches 6.4 TB/s, which is the card's copy rate.
+//   * The products run on mma.sync m16n8k16, transposed: S^T = K Q^T (rows: 16 keys, columns: 8 query heads) and
+//     O^T = V^T P^T (rows: 16 value dims).  With 8 to 16 query heads they need a few percent of its rate; a tcgen05
+//     instruction takes 128 rows.  The contraction order over D, the order of the value dims and that of the keys are free:
+//     a thread's 16 contiguous bytes serve two instructions, and the key order (see krow) makes the reads of the
+//     128-byte-swizzled boxes free of bank conflicts for both operands.
+//   * P is fed as two 16-bit parts (hi + lo), so its rounding does not show in O.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <stdint.h>
 
-#include "sm100_ptx.cuh"
+#include "attn_tc_common.cuh"
 
 namespace attn_paged {
 
@@ -41,13 +41,16 @@ template <int D, int GH>
 struct DecodeCfg {
     static constexpr int NW = D == 256 ? 4 : 8;             // warps
     static constexpr int THREADS = NW * 32;
-    static constexpr int NCH = D / 8;                       // 16-byte pieces of a thread's share of 16 keys (K and V)
-    static constexpr int STAGE_BYTES = NW * NCH * 512;
-    // ring stages: as many as fit beside the merge buffer
-    static constexpr int NSTAGE = D == 64 ? (GH == 8 ? 6 : 5) : (D == 128 ? (GH == 8 ? 3 : 2) : 2);
+    static constexpr int CK = D == 64 ? 32 : 16;            // keys of a warp's chunk
+    static constexpr int NPL = D / 64;                      // planes of 64 columns (128 bytes a row)
+    static constexpr int PLANE = CK * 128;
+    static constexpr int CHUNK_BYTES = 2 * NPL * PLANE;     // K, then V
+    static constexpr int STAGE_BYTES = NW * CHUNK_BYTES;
     static constexpr int ROW = D + 4;                       // floats of a row in the merge buffer (16-byte rows, banks shifted)
     static constexpr int MERGE_BYTES = NW * GH * ROW * 4 + NW * GH * 8;
-    static constexpr int SMEM_BYTES = NSTAGE * STAGE_BYTES + MERGE_BYTES + 64;
+    // ring stages: three where they fit beside the merge buffer
+    static constexpr int NSTAGE = 3 * STAGE_BYTES + MERGE_BYTES + 1024 + 512 <= 232448 ? 3 : 2;
+    static constexpr int SMEM_BYTES = 1024 + NSTAGE * STAGE_BYTES + MERGE_BYTES + 8 * NW * NSTAGE + 16;
     static_assert(SMEM_BYTES <= 232448, "shared memory budget");
     // a partial result: O [GH][D] (not normalised), then reference exponent and sum [GH][2], fp32
     static constexpr int PART_FLOATS = GH * (D + 2);
@@ -55,45 +58,57 @@ struct DecodeCfg {
 
 struct DecodeParams {
     const void* q;              // [B, H, D]
-    const uint8_t* k_cache;     // [pages, Hkv, slots, D] through byte strides
-    const uint8_t* v_cache;
     void* o;
     float* lse;
     const int* block_table;
     const int* seq_lens;
     float* parts;
     int* status;
-    int64_t k_page, k_head, k_slot, v_page, v_head, v_slot;   // byte strides
     int64_t table_stride;       // entries between the rows of block_table
     int B, H, Hkv, group, sub;  // query heads per K/V head; parts of at most 16 of them
     int max_len;                // slots that a row of block_table covers
     int num_pages, page_shift;
+    int box_shift;              // log2 of the rows of a TMA box: min(CK, page_size)
+    int k_axes, v_axes;         // coordinate (1, 2 or 3) of the maps' slot, head and page axis: 2 bits each
     int window, sinks;
     float scale_log2;
     int grid;                   // CTAs of the first kernel
 };
 
-// Visible chunks of 16 keys of one sequence: n_sink of them from key 0, then those from chunk `lo`.
+// Visible chunks of CK keys of one sequence: n_sink of them from key 0, then those from chunk `lo`.
 struct SeqRange {
     int len, win_lo;   // keys >= win_lo are visible, and those < sinks
     int n_sink, lo, n_chunks;
 };
 
+template <int CK>
 __device__ __forceinline__ SeqRange seq_range(const DecodeParams& p, int b) {
     SeqRange r;
     int len = p.seq_lens[b];
     len = len < 0 ? 0 : (len > p.max_len ? p.max_len : len);
     r.len = len;
     r.win_lo = (p.window > 0 && p.window < len) ? len - p.window : 0;
-    r.lo = r.win_lo >> 4;
-    const int sink_chunks = (p.sinks >> 4) + ((p.sinks & 15) != 0);
+    r.lo = r.win_lo / CK;
+    const int sink_chunks = p.sinks / CK + (p.sinks % CK != 0);
     r.n_sink = sink_chunks < r.lo ? sink_chunks : r.lo;
-    r.n_chunks = r.n_sink + ((len + 15) >> 4) - r.lo;
+    r.n_chunks = r.n_sink + len / CK + (len % CK != 0) - r.lo;
     return r;
 }
 
 template <int NW>
 __device__ __forceinline__ int seq_tiles(const SeqRange& r) { return (r.n_chunks + NW - 1) / NW; }
+
+// One box of the cache: columns 64 * plane .., rows from `slot` of a page's head.
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int axes, int plane, int slot, int head, int page) {
+    const int s = axes & 3, h = (axes >> 2) & 3;
+    const int c1 = s == 1 ? slot : (h == 1 ? head : page);
+    const int c2 = s == 2 ? slot : (h == 2 ? head : page);
+    const int c3 = s == 3 ? slot : (h == 3 ? head : page);
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(64 * plane), "r"(c1), "r"(c2), "r"(c3)
+        : "memory");
+}
 
 // CTA c of `ctas` takes the tiles [total * c / ctas, total * (c + 1) / ctas).  No more CTAs than tiles: none is empty, so
 // that a cut pair has a partial result from every CTA between its first and its last one.
@@ -108,13 +123,6 @@ __device__ __forceinline__ int64_t warp_sum(int64_t x) {
     for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
     return x;
 }
-
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool live) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 __device__ __forceinline__ uint4 lds128(uint32_t a) {
     uint4 v;
@@ -149,39 +157,74 @@ __device__ __forceinline__ void split2(float x0, float x1, uint32_t& hi, uint32_
 }
 
 // Position in the tile list, advanced tile by tile.  Every warp of a CTA walks the same tiles.
-template <int NW>
+template <int NW, int CK>
 struct TileWalk {
     int b, h, t, t_end;   // sequence, K/V head (times head part), tile inside the pair, tiles of the pair
+    int kvh, r0;          // K/V head, first query head of the part inside its group
     SeqRange r;
-    __device__ __forceinline__ void next(const DecodeParams& p, int heads) {
-        if (++t < t_end) return;
+    __device__ __forceinline__ void at(const DecodeParams& p, int b_, int h_, int t_) {
+        b = b_;
+        h = h_;
+        t = t_;
+        r = seq_range<CK>(p, b);
+        t_end = seq_tiles<NW>(r);
+        split_head(p);
+    }
+    __device__ __forceinline__ void split_head(const DecodeParams& p) {
+        kvh = p.sub == 1 ? h : h / p.sub;
+        r0 = (h - kvh * p.sub) * 16;
+    }
+    // true: the next tile belongs to another pair
+    __device__ __forceinline__ bool next(const DecodeParams& p, int heads) {
+        if (++t < t_end) return false;
         t = 0;
-        if (++h < heads) return;
-        h = 0;
-        do {
-            if (++b >= p.B) return;      // the end of the list: not used again
-            r = seq_range(p, b);
-            t_end = seq_tiles<NW>(r);
-        } while (t_end == 0);
+        if (++h == heads) {
+            h = 0;
+            do {
+                if (++b >= p.B) return true;      // the end of the list: not used again
+                r = seq_range<CK>(p, b);
+                t_end = seq_tiles<NW>(r);
+            } while (t_end == 0);
+        }
+        split_head(p);
+        return true;
     }
 };
+
+// The transpose of an 8 x 8 matrix of 16-bit values, a row of which lies on four lanes.
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
 
 // P carries a factor 2^P_OFF where 16-bit floats run out of small numbers (fp16); the reference maximum may lag by 2^LAG.
 template <int DTYPE> struct ExpRange { static constexpr float P_OFF = DTYPE == 0 ? 6.f : 0.f, LAG = 8.f; };
 
-// GH: query rows of an item, 8 (up to 8 query heads per K/V head) or 16.
+// GH: query heads of an item, 8 (up to 8 query heads per K/V head) or 16.
 template <int D, int DTYPE, int GH>
 __global__ void __launch_bounds__(DecodeCfg<D, GH>::THREADS, 1)
-attn_paged_decode_kernel(const DecodeParams p) {
+attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const DecodeParams p) {
     using C = DecodeCfg<D, GH>;
-    constexpr int NW = C::NW, NSTAGE = C::NSTAGE, NCH = C::NCH;
+    constexpr int NW = C::NW, NSTAGE = C::NSTAGE, CK = C::CK, NPL = C::NPL;
+    constexpr int NSUB = CK / 16;                   // groups of 16 keys: rows of one product
     constexpr int KI = D / 32, VI = D / 64;         // 16-byte pieces of a thread: per key row of K, per key row of V
     constexpr float P_OFF = ExpRange<DTYPE>::P_OFF, LAG = ExpRange<DTYPE>::LAG;
-    extern __shared__ __align__(128) uint8_t smem[];
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (sm100::smem_u32(smem_raw) & 1023u)) & 1023u);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
     float* merge = reinterpret_cast<float*>(smem + NSTAGE * C::STAGE_BYTES);
     float2* merge_ml = reinterpret_cast<float2*>(merge + NW * GH * C::ROW);
-    int64_t* scan = reinterpret_cast<int64_t*>(smem);        // before the ring is used: [0..31] warp sums, then the start
+    int64_t* scan = reinterpret_cast<int64_t*>(merge);       // at the beginning: [0..31] warp sums, then the start
+    const uint32_t bars = sm100::smem_u32(smem) + NSTAGE * C::STAGE_BYTES + C::MERGE_BYTES;     // [warp][stage]: a chunk has arrived
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + NSTAGE * C::STAGE_BYTES + C::MERGE_BYTES + 8 * NW * NSTAGE);
+    if (tid < NW * NSTAGE) sm100::mbar_init(bars + 8 * tid, 1);
+    if (tid == 0) {
+        *abort_flag = 0;
+        sm100::prefetch_tensormap(&tmK);
+        sm100::prefetch_tensormap(&tmV);
+        sm100::fence_barrier_init();
+    }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // ---- lay out the tile list: total tiles, and the pair and tile at which this CTA's part begins ----
@@ -190,7 +233,7 @@ attn_paged_decode_kernel(const DecodeParams p) {
     const int b0 = tid * per, b1 = b0 + per < p.B ? b0 + per : p.B;
     int64_t mine = 0;
     for (int b = b0; b < b1; ++b) {
-        mine += seq_tiles<NW>(seq_range(p, b));
+        mine += seq_tiles<NW>(seq_range<CK>(p, b));
         if (p.seq_lens[b] > p.max_len && blockIdx.x == 0) report_bad_index(p.status);
     }
     int64_t incl = mine;
@@ -210,12 +253,13 @@ attn_paged_decode_kernel(const DecodeParams p) {
     total *= heads;
     const int ctas = cta_count(total, p.grid);
     if (static_cast<int>(blockIdx.x) >= ctas) return;
-    const int64_t first = cta_begin(total, blockIdx.x, ctas), steps = cta_begin(total, blockIdx.x + 1, ctas) - first;
+    const int64_t first = cta_begin(total, blockIdx.x, ctas);
+    const int steps = static_cast<int>(cta_begin(total, blockIdx.x + 1, ctas) - first);
     // the thread whose sequences hold tile `first` finds it
     if (first >= before * heads && first < (before + mine) * heads) {
         int64_t rem = first - before * heads;
         for (int b = b0; b < b1; ++b) {
-            const int n = seq_tiles<NW>(seq_range(p, b));
+            const int n = seq_tiles<NW>(seq_range<CK>(p, b));
             if (rem < static_cast<int64_t>(n) * heads) {
                 scan[32] = b;
                 scan[33] = rem / n;
@@ -226,248 +270,263 @@ attn_paged_decode_kernel(const DecodeParams p) {
         }
     }
     __syncthreads();
-    TileWalk<NW> ld, cu;      // the copies run NSTAGE - 1 tiles ahead of the arithmetic
-    ld.b = static_cast<int>(scan[32]);
-    ld.h = static_cast<int>(scan[33]);
-    ld.t = static_cast<int>(scan[34]);
-    ld.r = seq_range(p, ld.b);
-    ld.t_end = seq_tiles<NW>(ld.r);
+    TileWalk<NW, CK> ld, cu;      // the copies run NSTAGE - 1 tiles ahead of the arithmetic
+    ld.at(p, static_cast<int>(scan[32]), static_cast<int>(scan[33]), static_cast<int>(scan[34]));
     cu = ld;
-    __syncthreads();          // the ring takes over the scan's shared memory
+    __syncthreads();          // the merge buffer takes over the scan's shared memory
 
-    const uint32_t ring = sm100::smem_u32(smem) + warp * NCH * 512 + lane * 16;
-    // key 16 of this warp's chunk of tile t, first key index; negative: no chunk
-    auto chunk_key = [&](const TileWalk<NW>& w) {
+    const uint32_t ring = sm100::smem_u32(smem) + warp * C::CHUNK_BYTES, my_bars = bars + 8 * warp * NSTAGE;
+    // first key of this warp's chunk in the walk's tile; negative: no chunk
+    auto chunk_key = [&](const TileWalk<NW, CK>& w) {
         const int ch = w.t * NW + warp;
         if (ch >= w.r.n_chunks) return -1;
-        return (ch < w.r.n_sink ? ch : w.r.lo + ch - w.r.n_sink) << 4;
+        return (ch < w.r.n_sink ? ch : w.r.lo + ch - w.r.n_sink) * CK;
     };
-    auto visible = [&](const SeqRange& r, int key) { return key < r.len && (key >= r.win_lo || key < p.sinks); };
-    // page of key chunk + lane % 16 of the walk's tile (-1: hidden or not a page)
-    auto fetch_page = [&](const TileWalk<NW>& w) {
-        const int k0 = chunk_key(w);
+    // page of key (chunk + lane % CK) of the copies' tile, where any key of its box is visible: -1: hidden, -2: not a page
+    const int box = 1 << p.box_shift, slot_mask = (1 << p.page_shift) - 1;
+    auto fetch_page = [&](int k0) {
+        const int first_key = (k0 + (lane & (CK - 1))) & ~(box - 1);
         int page = -1;
-        if (k0 >= 0) {
-            const int key = k0 + (lane & 15);
-            if (visible(w.r, key)) {
-                page = __ldg(p.block_table + static_cast<int64_t>(w.b) * p.table_stride + (key >> p.page_shift));
-                if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages)) page = -2;
-            }
+        if (k0 >= 0 && first_key < ld.r.len && (first_key > ld.r.win_lo - box || first_key < p.sinks)) {
+            page = __ldg(p.block_table + static_cast<int64_t>(ld.b) * p.table_stride + (first_key >> p.page_shift));
+            if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages)) page = -2;
         }
         return page;
     };
-    int64_t loaded = 0;
-    int page_next = fetch_page(ld);
-    // live keys of the chunks in flight, one bit per key, NSTAGE deep
-    uint32_t live_q[NSTAGE];
+    int loaded = 0;
+    int key_next = chunk_key(ld), page_next = fetch_page(key_next);
+    // visible keys of the chunks in flight, one bit per key
+    uint32_t live_q[NSTAGE], phases = 0;
 #pragma unroll
     for (int s = 0; s < NSTAGE; ++s) live_q[s] = 0;
-    const int slot_mask = (1 << p.page_shift) - 1;
     auto issue = [&](int stage, uint32_t& live_out) {
         live_out = 0;
         if (loaded < steps) {
-            const int k0 = chunk_key(ld);
-            int page = page_next;
-            if (page == -2) report_bad_index(p.status);
-            const uint32_t live = __ballot_sync(0xffffffffu, page >= 0) & 0xffffu;
+            const int k0 = key_next, page = page_next, key = k0 + (lane & (CK - 1));
+            const bool seen = page >= 0 && key < ld.r.len && (key >= ld.r.win_lo || key < p.sinks);
+            const uint32_t live = __ballot_sync(0xffffffffu, seen) & (CK == 32 ? 0xffffffffu : 0xffffu);
             live_out = live;
             if (live) {
-                const int kvh = ld.h / p.sub;
-                const uint32_t dst = ring + stage * C::STAGE_BYTES;
-                const uint8_t* kb = p.k_cache + kvh * p.k_head + c * 16;
-                const uint8_t* vb = p.v_cache + kvh * p.v_head + g * 16;
-#pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    const int row = 8 * n + g;
-                    const int pg = __shfl_sync(0xffffffffu, page, row);
-                    const uint8_t* src = pg >= 0 ? kb + pg * p.k_page + ((k0 + row) & slot_mask) * p.k_slot : p.k_cache;
-#pragma unroll
-                    for (int i = 0; i < KI; ++i) cp_async16(dst + (n * KI + i) * 512, pg >= 0 ? src + i * 64 : src, pg >= 0);
-                }
-#pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    const int row = 8 * (n >> 1) + 2 * c + (n & 1);
-                    const int pg = __shfl_sync(0xffffffffu, page, row);
-                    const uint8_t* src = pg >= 0 ? vb + pg * p.v_page + ((k0 + row) & slot_mask) * p.v_slot : p.v_cache;
-#pragma unroll
-                    for (int i = 0; i < VI; ++i) cp_async16(dst + (2 * KI + n * VI + i) * 512, pg >= 0 ? src + i * 128 : src, pg >= 0);
+                const uint32_t dst = ring + stage * C::STAGE_BYTES, bar = my_bars + 8 * stage;
+                // pages that are loaded: the first lane of each box counts
+                const uint32_t boxes = __ballot_sync(0xffffffffu, lane < CK && (lane & (box - 1)) == 0 && page >= 0);
+                if (lane == 0) sm100::mbar_arrive_expect_tx(bar, __popc(boxes) * 2 * NPL * box * 128);
+                __syncwarp();     // armed before the first copy; and every lane has read what this stage held
+                for (int o0 = 0; o0 < 2 * NPL * (CK >> p.box_shift); o0 += 32) {
+                    const int o = o0 + lane, row = (o / (2 * NPL)) << p.box_shift, pl = o % (2 * NPL);
+                    const int pg = __shfl_sync(0xffffffffu, page, row & 31);
+                    if (row < CK && pg >= 0) {
+                        const bool is_v = pl >= NPL;
+                        load_box(dst + pl * C::PLANE + row * 128, is_v ? &tmV : &tmK, bar, is_v ? p.v_axes : p.k_axes, is_v ? pl - NPL : pl,
+                                 (k0 + row) & slot_mask, ld.kvh, pg);
+                    }
                 }
             }
+            if (page == -2) report_bad_index(p.status);
             ld.next(p, heads);
-            if (++loaded < steps) page_next = fetch_page(ld);
+            if (++loaded < steps) {
+                key_next = chunk_key(ld);
+                page_next = fetch_page(key_next);
+            }
         }
-        cp_async_commit();
     };
 #pragma unroll
     for (int s = 0; s < NSTAGE - 1; ++s) issue(s, live_q[s]);
 
-    uint32_t qa[KI][4], qb[KI][4];        // Q fragments: rows g and (GH == 16) g + 8
-    float acc[VI][8][4];
-    float m[2], l[2];                     // reference maximum of the raw scores and this thread's part of the sum, rows g, g + 8
+    // This lane's rows and pieces inside a 16-key group of a swizzled box (16-byte piece x of row r lies at piece x ^ (r % 8)).
+    // Row g (+ 8) of a product is key krow (+ 8); with this order the eight lanes of a shared-memory phase read eight different
+    // pieces for K (rows krow(2j), krow(2j+1), four pieces each) and for V (four rows, two pieces each).
+    const int krow = g ^ ((g & 1) << 2), vrow0 = 2 * c, vrow1 = (2 * c + 1) ^ 4;
+    const uint32_t k_off = krow * 128 + ((c ^ krow) << 4);                       // pieces c + 4: the same with bit 6 flipped
+    const uint32_t v_off0 = NPL * C::PLANE + vrow0 * 128 + ((g ^ vrow0) << 4), v_off1 = NPL * C::PLANE + vrow1 * 128 + ((g ^ vrow1) << 4);
+
+    constexpr int NT = GH / 8;            // groups of 8 query heads
+    uint32_t qf[NT][KI][4];               // Q^T: this lane's 16-byte pieces of head 8 nt + g
+    float acc[NT][VI][4][4];              // O^T: dims 64 i + 8 g + 2 x (+ 1: elements 2, 3) of heads 8 nt + 2 c, + 1
+    float m[NT][2], l[NT][2];             // reference maximum of the raw scores and this lane's part of the sum, same heads
     auto start_pair = [&]() {
-        const int kvh = cu.h / p.sub, r0 = (cu.h - kvh * p.sub) * 16;
 #pragma unroll
-        for (int i = 0; i < KI; ++i) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { qa[i][e] = 0; qb[i][e] = 0; }
+        for (int nt = 0; nt < NT; ++nt) {
+            const int head = cu.r0 + 8 * nt + g;
+            const bool used = head < p.group;
             const uint8_t* qp = static_cast<const uint8_t*>(p.q) +
-                                ((static_cast<int64_t>(cu.b) * p.H + kvh * p.group + r0 + g) * D + 32 * i + 8 * c) * 2;
-            if (r0 + g < p.group) {
-                const uint4 w = __ldg(reinterpret_cast<const uint4*>(qp));
-                qa[i][0] = w.x; qa[i][1] = w.y; qa[i][2] = w.z; qa[i][3] = w.w;
+                                ((static_cast<int64_t>(cu.b) * p.H + cu.kvh * p.group + (used ? head : 0)) * D + 8 * c) * 2;
+#pragma unroll
+            for (int i = 0; i < KI; ++i) {
+                const uint4 w = __ldg(reinterpret_cast<const uint4*>(qp + i * 64));
+                qf[nt][i][0] = used ? w.x : 0u;
+                qf[nt][i][1] = used ? w.y : 0u;
+                qf[nt][i][2] = used ? w.z : 0u;
+                qf[nt][i][3] = used ? w.w : 0u;
             }
-            if (GH == 16 && r0 + g + 8 < p.group) {
-                const uint4 w = __ldg(reinterpret_cast<const uint4*>(qp + 8 * D * 2));
-                qb[i][0] = w.x; qb[i][1] = w.y; qb[i][2] = w.z; qb[i][3] = w.w;
-            }
+#pragma unroll
+            for (int i = 0; i < VI; ++i)
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[nt][i][x][e] = 0.f;
+            m[nt][0] = m[nt][1] = -INFINITY;
+            l[nt][0] = l[nt][1] = 0.f;
         }
-#pragma unroll
-        for (int i = 0; i < VI; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) acc[i][e][x] = 0.f;
-        m[0] = m[1] = -INFINITY;
-        l[0] = l[1] = 0.f;
     };
     const float sc = p.scale_log2;
-    bool fresh = true;
-    int pair_first_t = cu.t;    // first tile of the current pair in this CTA's part
-    int n_pairs = 0;            // pairs finished so far by this CTA (0: a cut pair goes to slot 0)
+    start_pair();
+    bool from_start = cu.t == 0;    // this CTA has the current pair from its first tile
+    int n_pairs = 0;                // pairs that this CTA has left so far (0: a cut pair goes to slot 0)
 
-    for (int64_t s0 = 0; s0 < steps; s0 += NSTAGE) {
+    for (int s0 = 0; s0 < steps; s0 += NSTAGE) {
 #pragma unroll
         for (int st = 0; st < NSTAGE; ++st) {
-            const int64_t s = s0 + st;
+            const int s = s0 + st;
             if (s >= steps) break;
-            if (fresh) {
-                start_pair();
-                fresh = false;
-                pair_first_t = cu.t;
-            }
+            __syncwarp();
             issue((st + NSTAGE - 1) % NSTAGE, live_q[(st + NSTAGE - 1) % NSTAGE]);
-            cp_async_wait<NSTAGE - 1>();
-            const uint32_t live = live_q[st];
-            if (live) {      // uniform over the warp
+            uint32_t live = live_q[st];
+            if (live) {
+                // (a copy that never arrives ends in an error status: the rest of the loop goes on without its keys)
+                if (!sm100::mbar_wait(my_bars + 8 * st, (phases >> st) & 1, abort_flag)) live = 0;
+                phases ^= 1u << st;
+            }
+            if (__any_sync(0xffffffffu, live != 0)) {
                 const uint32_t src = ring + st * C::STAGE_BYTES;
-                float sf[2][4];
+                const bool full = live == (CK == 32 ? 0xffffffffu : 0xffffu);
+                float sf[NSUB][NT][4];               // S^T: keys krow (0, 1) and krow + 8 (2, 3) of each group, heads 2 c, 2 c + 1
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    float even[4] = {0.f, 0.f, 0.f, 0.f}, odd[4] = {0.f, 0.f, 0.f, 0.f};
+                for (int sub = 0; sub < NSUB; ++sub) {
+                    float odd[NT][4];                // a second chain of products
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sf[sub][nt][e] = odd[nt][e] = 0.f;
 #pragma unroll
                     for (int i = 0; i < KI; ++i) {
-                        const uint4 w = lds128(src + (n * KI + i) * 512);
-                        mma16816<DTYPE>(even, qa[i][0], qb[i][0], qa[i][1], qb[i][1], w.x, w.y);
-                        mma16816<DTYPE>(odd, qa[i][2], qb[i][2], qa[i][3], qb[i][3], w.z, w.w);
+                        const uint32_t at = src + (i >> 1) * C::PLANE + sub * 2048 + ((i & 1) ? k_off ^ 64u : k_off);
+                        const uint4 a = lds128(at), b = lds128(at + 1024);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            mma16816<DTYPE>(sf[sub][nt], a.x, b.x, a.y, b.y, qf[nt][i][0], qf[nt][i][1]);
+                            mma16816<DTYPE>(odd[nt], a.z, b.z, a.w, b.w, qf[nt][i][2], qf[nt][i][3]);
+                        }
                     }
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) sf[n][x] = even[x] + odd[x];
-                }
-                if (live != 0xffffu) {
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int n = 0; n < 2; ++n)
-#pragma unroll
-                        for (int x = 0; x < 4; ++x)
-                            if (!((live >> (8 * n + 2 * c + (x & 1))) & 1)) sf[n][x] = -INFINITY;
+                        for (int e = 0; e < 4; ++e) {
+                            sf[sub][nt][e] += odd[nt][e];
+                            if (!full && !((live >> (16 * sub + krow + (e < 2 ? 0 : 8))) & 1)) sf[sub][nt][e] = -INFINITY;
+                        }
                 }
                 // advance the reference maximum only when a score ran ahead of it by more than 2^LAG (or there is none yet)
-                float mx[2];
-                mx[0] = fmaxf(fmaxf(sf[0][0], sf[0][1]), fmaxf(sf[1][0], sf[1][1]));
-                mx[1] = fmaxf(fmaxf(sf[0][2], sf[0][3]), fmaxf(sf[1][2], sf[1][3]));
-                bool ahead = m[0] == -INFINITY || (mx[0] - m[0]) * sc > LAG;
-                if (GH == 16) ahead |= m[1] == -INFINITY || (mx[1] - m[1]) * sc > LAG;
+                auto chunk_max = [&](float (&s)[NSUB][NT][4], int nt, int h) {
+                    float x = fmaxf(s[0][nt][h], s[0][nt][2 + h]);
+#pragma unroll
+                    for (int sub = 1; sub < NSUB; ++sub) x = sm100::max3(x, s[sub][nt][h], s[sub][nt][2 + h]);
+                    return x;
+                };
+                bool ahead = false;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        ahead |= m[nt][h] == -INFINITY || (chunk_max(sf, nt, h) - m[nt][h]) * sc > LAG;
                 if (__any_sync(0xffffffffu, ahead)) {
 #pragma unroll
-                    for (int r = 0; r < GH / 8; ++r) {
-                        float x = mx[r];
-                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));   // finite: the chunk has a live key
-                        const float mn = fmaxf(m[r], x);
-                        const float alpha = m[r] == -INFINITY ? 0.f : sm100::ex2_approx((m[r] - mn) * sc);
-                        m[r] = mn;
-                        l[r] *= alpha;
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int i = 0; i < VI; ++i)
+                        for (int h = 0; h < 2; ++h) {
+                            float x = chunk_max(sf, nt, h);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                if (GH == 8) {
+                            for (int off = 4; off < 32; off <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
+                            const float mn = fmaxf(m[nt][h], x);
+                            const float alpha = m[nt][h] == -INFINITY ? 0.f : sm100::ex2_approx((m[nt][h] - mn) * sc);
+                            m[nt][h] = mn;
+                            l[nt][h] *= alpha;
 #pragma unroll
-                                    for (int x4 = 0; x4 < 4; ++x4) acc[i][e][x4] *= alpha;
-                                } else {
-                                    acc[i][e][2 * r] *= alpha;
-                                    acc[i][e][2 * r + 1] *= alpha;
+                            for (int i = 0; i < VI; ++i)
+#pragma unroll
+                                for (int x4 = 0; x4 < 4; ++x4) {
+                                    acc[nt][i][x4][h] *= alpha;
+                                    acc[nt][i][x4][2 + h] *= alpha;
                                 }
-                            }
-                    }
-                }
-                uint32_t hi[2][2], lo[2][2];   // [key half][row half]
-#pragma unroll
-                for (int r = 0; r < GH / 8; ++r) {
-                    const float off = P_OFF - (m[r] == -INFINITY ? 0.f : m[r] * sc);   // every score so far -inf: P = 0
-#pragma unroll
-                    for (int n = 0; n < 2; ++n) {
-                        float p0 = sm100::ex2_approx(fmaf(sf[n][2 * r], sc, off)), p1 = sm100::ex2_approx(fmaf(sf[n][2 * r + 1], sc, off));
-                        if (live != 0xffffu) {      // explicit zeros: with scale 0 the hidden scores' -inf * 0 is no number
-                            const uint32_t bits = live >> (8 * n + 2 * c);
-                            p0 = (bits & 1) ? p0 : 0.f;
-                            p1 = (bits & 2) ? p1 : 0.f;
                         }
-                        l[r] += p0 + p1;
-                        split2<DTYPE>(p0, p1, hi[n][r], lo[n][r]);
-                    }
                 }
+                float off[NT][2];
 #pragma unroll
-                for (int i = 0; i < VI; ++i) {
-                    uint32_t v[4][4];
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-                        const uint4 w = lds128(src + (2 * KI + n * VI + i) * 512);
-                        v[n][0] = w.x; v[n][1] = w.y; v[n][2] = w.z; v[n][3] = w.w;
+                    for (int h = 0; h < 2; ++h) off[nt][h] = P_OFF - (m[nt][h] == -INFINITY ? 0.f : m[nt][h] * sc);   // every score so far -inf: P = 0
+#pragma unroll
+                for (int sub = 0; sub < NSUB; ++sub) {
+                    uint32_t hi[NT][2], lo[NT][2];   // P^T as B operand: keys vrow0, vrow1 (0) and + 8 (1) of head g
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        float pr[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            pr[e] = sm100::ex2_approx(fmaf(sf[sub][nt][e], sc, off[nt][e & 1]));
+                            // explicit zeros: with scale 0 the hidden scores' -inf * 0 is no number
+                            if (!full) pr[e] = ((live >> (16 * sub + krow + (e < 2 ? 0 : 8))) & 1) ? pr[e] : 0.f;
+                        }
+                        l[nt][0] += pr[0] + pr[2];
+                        l[nt][1] += pr[1] + pr[3];
+#pragma unroll
+                        for (int n = 0; n < 2; ++n) {
+                            uint32_t a, b;
+                            split2<DTYPE>(pr[2 * n], pr[2 * n + 1], a, b);
+                            hi[nt][n] = transpose8x8(a);
+                            lo[nt][n] = transpose8x8(b);
+                        }
                     }
 #pragma unroll
-                    for (int w = 0; w < 4; ++w)
+                    for (int i = 0; i < VI; ++i) {
+                        const uint32_t at = src + i * C::PLANE + sub * 2048;
+                        uint4 v[4] = {lds128(at + v_off0), lds128(at + v_off1), lds128(at + v_off0 + 1024), lds128(at + v_off1 + 1024)};
+                        if (!full) {     // hidden slots may hold anything, infinities and NaN among it
 #pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const uint32_t vb0 = __byte_perm(v[0][w], v[1][w], x ? 0x7632 : 0x5410);
-                            const uint32_t vb1 = __byte_perm(v[2][w], v[3][w], x ? 0x7632 : 0x5410);
-                            float* a = acc[i][2 * w + x];
-                            if (GH == 8) {
-                                mma16816<DTYPE>(a, hi[0][0], lo[0][0], hi[1][0], lo[1][0], vb0, vb1);
-                            } else {
-                                mma16816<DTYPE>(a, hi[0][0], hi[0][1], hi[1][0], hi[1][1], vb0, vb1);
-                                mma16816<DTYPE>(a, lo[0][0], lo[0][1], lo[1][0], lo[1][1], vb0, vb1);
+                            for (int n = 0; n < 4; ++n)
+                                if (!((live >> (16 * sub + ((n & 1) ? vrow1 : vrow0) + 8 * (n >> 1))) & 1)) v[n] = make_uint4(0u, 0u, 0u, 0u);
+                        }
+                        const uint32_t w[4][4] = {{v[0].x, v[0].y, v[0].z, v[0].w}, {v[1].x, v[1].y, v[1].z, v[1].w},
+                                                  {v[2].x, v[2].y, v[2].z, v[2].w}, {v[3].x, v[3].y, v[3].z, v[3].w}};
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            // V^T: dims 2 x and 2 x + 1 of this lane's 8 as rows g and g + 8, key pairs side by side
+                            const uint32_t a0 = __byte_perm(w[0][x], w[1][x], 0x5410), a1 = __byte_perm(w[0][x], w[1][x], 0x7632);
+                            const uint32_t a2 = __byte_perm(w[2][x], w[3][x], 0x5410), a3 = __byte_perm(w[2][x], w[3][x], 0x7632);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                mma16816<DTYPE>(acc[nt][i][x], a0, a1, a2, a3, hi[nt][0], hi[nt][1]);
+                                mma16816<DTYPE>(acc[nt][i][x], a0, a1, a2, a3, lo[nt][0], lo[nt][1]);
                             }
                         }
+                    }
                 }
             }
             // ---- end of the pair, or of this CTA's part: merge the warps ----
             const bool end_pair = cu.t + 1 == cu.t_end;
             if (end_pair || s + 1 == steps) {
 #pragma unroll
-                for (int r = 0; r < GH / 8; ++r) {
-                    float x = l[r];
-                    x += __shfl_xor_sync(0xffffffffu, x, 1);
-                    x += __shfl_xor_sync(0xffffffffu, x, 2);
-                    if (c == 0) merge_ml[warp * GH + 8 * r + g] = make_float2(m[r] * sc, x);   // x = 0: no key, the first value is not used
-                }
+                for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-                for (int i = 0; i < VI; ++i)
+                    for (int h = 0; h < 2; ++h) {
+                        float x = l[nt][h];
 #pragma unroll
-                    for (int r = 0; r < GH / 8; ++r)
+                        for (int off = 4; off < 32; off <<= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+                        const int head = 8 * nt + 2 * c + h;
+                        if (g == 0) merge_ml[warp * GH + head] = make_float2(m[nt][h] * sc, x);   // x = 0: no key, the first value is not used
+                        float* dst = merge + (warp * GH + head) * C::ROW + 8 * g;
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            // value dims 64 i + 16 c + 8 j + (0 .. 7) of row g + 8 r
-                            float* dst = merge + (warp * GH + 8 * r + g) * C::ROW + 64 * i + 16 * c + 8 * j;
-                            float v[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) v[e] = GH == 8 ? acc[i][e][j] + acc[i][e][2 + j] : acc[i][e][2 * r + j];
-                            *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
-                            *reinterpret_cast<float4*>(dst + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                        for (int i = 0; i < VI; ++i) {
+                            *reinterpret_cast<float4*>(dst + 64 * i) =
+                                make_float4(acc[nt][i][0][h], acc[nt][i][0][2 + h], acc[nt][i][1][h], acc[nt][i][1][2 + h]);
+                            *reinterpret_cast<float4*>(dst + 64 * i + 4) =
+                                make_float4(acc[nt][i][2][h], acc[nt][i][2][2 + h], acc[nt][i][3][h], acc[nt][i][3][2 + h]);
                         }
+                    }
+                }
                 __syncthreads();
-                const int kvh = cu.h / p.sub, r0 = (cu.h - kvh * p.sub) * 16;
-                const int rows = p.group - r0 < GH ? p.group - r0 : GH;
-                const bool whole = end_pair && pair_first_t == 0;
+                const int rows = p.group - cu.r0 < GH ? p.group - cu.r0 : GH;
+                const bool whole = end_pair && from_start;
                 float* part = p.parts + (2 * static_cast<int64_t>(blockIdx.x) + (n_pairs > 0 ? 1 : 0)) * C::PART_FLOATS;
                 for (int e = tid; e < rows * (D / 4); e += C::THREADS) {
                     const int row = e / (D / 4), d4 = e % (D / 4);
@@ -492,7 +551,7 @@ attn_paged_decode_kernel(const DecodeParams p) {
                         o.w = fmaf(f, v.w, o.w);
                     }
                     if (whole) {
-                        const int64_t out_row = static_cast<int64_t>(cu.b) * p.H + kvh * p.group + r0 + row;
+                        const int64_t out_row = static_cast<int64_t>(cu.b) * p.H + cu.kvh * p.group + cu.r0 + row;
                         const float inv = sum != 0.f ? 1.f / sum : 0.f;
                         uint2 w;
                         w.x = sm100::pack2<DTYPE>(o.x * inv, o.y * inv);
@@ -506,12 +565,15 @@ attn_paged_decode_kernel(const DecodeParams p) {
                 }
                 __syncthreads();     // the merge buffer may be written again
                 ++n_pairs;
-                fresh = true;
             }
-            cu.next(p, heads);
+            if (cu.next(p, heads) && s + 1 < steps) {
+                start_pair();
+                from_start = true;
+            }
         }
     }
-    cp_async_wait<0>();
+    __syncthreads();
+    if (tid == 0 && *abort_flag != 0) atomicExch(p.status, attn_tc::kStatusTimeout);
 }
 
 // Joins the partial results of the pairs that more than one CTA of the first kernel worked on, and writes the rows of
@@ -530,7 +592,7 @@ attn_paged_join_kernel(const DecodeParams p) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     int64_t before = 0, total = 0;
     for (int x = tid; x < p.B; x += 256) {
-        const int n = seq_tiles<NW>(seq_range(p, x));
+        const int n = seq_tiles<NW>(seq_range<C::CK>(p, x));
         total += n;
         if (x < b) before += n;
     }
@@ -548,7 +610,7 @@ attn_paged_join_kernel(const DecodeParams p) {
         total += red[8 + w];
     }
     total *= heads;
-    const int n = seq_tiles<NW>(seq_range(p, b));
+    const int n = seq_tiles<NW>(seq_range<C::CK>(p, b));
     // Every CTA waits for the first kernel, also one without work: in a graph this kernel's end stands for both.
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int kvh = h / p.sub, r0 = (h - kvh * p.sub) * 16;

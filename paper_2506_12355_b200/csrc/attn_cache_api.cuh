@@ -46,6 +46,15 @@ int validate_cache(const void* k_cache, const void* v_cache, const long long* ca
     return ATTN_OK;
 }
 
+// log2 of the heads that a tile of the decode kernel covers side by side: all warps' worth where the number of heads has that
+// power of two, else as many as it has.
+int tile_heads_shift(int64_t heads, int D) {
+    const int warps = D == 256 ? 4 : 8;
+    int s = 0;
+    while ((2 << s) <= warps && heads % (2 << s) == 0) ++s;
+    return s;
+}
+
 // Tensor map over one cache: columns, then the slot, head and page axes by ascending stride; box = 64 columns x `rows` slots,
 // 128-byte swizzle.  `axes` receives the coordinate number of the slot, head and page axis (2 bits each).  A map is a pure
 // function of these arguments; the last ones are kept per thread, as a serving loop passes the same caches in every step.
@@ -388,8 +397,9 @@ int attn_paged_append(const void* q, const void* k, const void* v, const long lo
 
 size_t attn_paged_decode_workspace_bytes(int H, int Hkv, int D) {
     if (H < 0 || Hkv < 1 || H % Hkv != 0 || !head_dim_ok(D)) return 0;
-    const int rows = H / Hkv <= 8 ? 8 : 16;
-    return align256(static_cast<size_t>(2) * attn_paged::kMaxCtas * rows * (D + 2) * sizeof(float));
+    const int group = H / Hkv, rows = group <= 8 ? 8 : 16;
+    const size_t parts = static_cast<size_t>(2) * attn_paged::kMaxCtas << tile_heads_shift(Hkv * ((group + 15) / 16), D);
+    return align256(parts * rows * (D + 2) * sizeof(float));
 }
 
 int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, const long long* cache_strides, int num_pages,
@@ -429,6 +439,8 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
     p.Hkv = Hkv;
     p.group = H / Hkv;
     p.sub = (p.group + 15) / 16;
+    p.heads = Hkv * p.sub;
+    p.hpt_shift = tile_heads_shift(p.heads, D);
     p.max_len = max_pages * page_size;
     p.num_pages = num_pages;
     p.page_shift = log2_of(page_size);
@@ -437,9 +449,10 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
     p.scale_log2 = scale * 1.4426950408889634f;
     p.status = cached_status_ptr();
     if (!p.status) return ATTN_ERR_CUDA;
-    const int64_t pairs = static_cast<int64_t>(B) * Hkv * p.sub;
-    // one CTA per SM, and no more than there can be tiles (64 keys are the smallest tile)
-    const int64_t most = pairs * ((static_cast<int64_t>(p.max_len) + 63) / 64 + 1);
+    const int64_t pairs = static_cast<int64_t>(B) * p.heads;
+    if (pairs > 2147483647LL) return ATTN_ERR_BAD_SHAPE;
+    // one CTA per SM, and no more than there can be tiles (16 keys are the smallest tile)
+    const int64_t most = pairs * ((static_cast<int64_t>(p.max_len) + 15) / 16 + 2);
     int grid = di.sm_count < attn_paged::kMaxCtas ? di.sm_count : attn_paged::kMaxCtas;
     if (most < grid) grid = static_cast<int>(most);
     p.grid = grid;
@@ -456,7 +469,7 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
             return ATTN_ERR_CUDA;                                                                                        \
         kern<<<grid, C::THREADS, C::SMEM_BYTES, st>>>(mk, mv, p);                                                        \
         if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;                                                     \
-        return launch_dependent(attn_paged::attn_paged_join_kernel<DD, TT, GG>, dim3(static_cast<unsigned>(pairs)), dim3(256), 0, st, p) \
+        return launch_dependent(attn_paged::attn_paged_join_kernel<DD, TT, GG>, dim3(static_cast<unsigned>(pairs)), dim3(512), 0, st, p) \
                    ? ATTN_OK                                                                                             \
                    : ATTN_ERR_CUDA;                                                                                      \
     }

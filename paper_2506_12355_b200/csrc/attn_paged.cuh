@@ -7,11 +7,13 @@
 // Every visible key's K and V row is read once: 4 D bytes per key and K/V head, 2 multiply-adds per value and query head.
 // That is HBM-bound for every group size up to 16 query heads per K/V head, so all of the design serves the loads:
 //
-//   * The keys are cut into chunks of CK per warp, 8 (or 4) chunks to a tile; the tiles of all (sequence, K/V head) pairs form
-//     one list, of which every CTA of a one-wave persistent grid takes an equal, contiguous part, whatever the lengths
-//     are.  Each CTA lays the list out for itself from the device-side lengths (no host copy of them, no plan to keep).
-//     A pair inside one CTA's part is finished there; one that is cut by a border leaves one fp32 partial result per
-//     CTA (at most two per CTA), and a second small kernel joins those.
+//   * A warp works on chunks of CK keys of one head.  The warps of a CTA take different heads of the same keys where there
+//     are enough heads (a page holds its heads side by side, so a step of the CTA reads one contiguous piece of it, and no
+//     warp has to wait for another), and neighbouring chunks where there are not.  Such a step is a tile; the tiles of all
+//     (sequence, group of heads) pairs form one list, of which every CTA of a one-wave persistent grid takes an equal,
+//     contiguous part, whatever the lengths are.  Each CTA lays the list out for itself from the device-side lengths (no
+//     host copy of them, no plan to keep).  A pair inside one CTA's part is finished there; one that is cut by a border
+//     leaves one fp32 partial result per CTA (at most two per CTA), and a second small kernel joins those.
 //   * Each warp keeps a ring of its own in shared memory, filled by TMA boxes of up to CK rows x 128 bytes (a box lies in one
 //     page), one mbarrier per stage, and no other synchronisation: 128 to 192 KB per SM are in flight.  Measured at
 //     4 x 65536 keys of 8 heads x 128: per-thread 16-byte copies (cp.async) stop at 4.9 TB/s however deep the ring is, the TMA
@@ -52,7 +54,7 @@ struct DecodeCfg {
     static constexpr int NSTAGE = 3 * STAGE_BYTES + MERGE_BYTES + 1024 + 512 <= 232448 ? 3 : 2;
     static constexpr int SMEM_BYTES = 1024 + NSTAGE * STAGE_BYTES + MERGE_BYTES + 8 * NW * NSTAGE + 16;
     static_assert(SMEM_BYTES <= 232448, "shared memory budget");
-    // a partial result: O [GH][D] (not normalised), then reference exponent and sum [GH][2], fp32
+    // a partial result of one head: O [GH][D] (not normalised), then reference exponent and sum [GH][2], fp32
     static constexpr int PART_FLOATS = GH * (D + 2);
 };
 
@@ -65,7 +67,9 @@ struct DecodeParams {
     float* parts;
     int* status;
     int64_t table_stride;       // entries between the rows of block_table
-    int B, H, Hkv, group, sub;  // query heads per K/V head; parts of at most 16 of them
+    int B, H, Hkv, group, sub;  // query heads per K/V head; parts of at most 16 of them (each a head of its own from here on)
+    int heads;                  // Hkv * sub
+    int hpt_shift;              // log2 of the heads that a tile covers side by side (long lists); the other warps take further chunks
     int max_len;                // slots that a row of block_table covers
     int num_pages, page_shift;
     int box_shift;              // log2 of the rows of a TMA box: min(CK, page_size)
@@ -95,8 +99,13 @@ __device__ __forceinline__ SeqRange seq_range(const DecodeParams& p, int b) {
     return r;
 }
 
+// Tiles of one sequence and group of heads; a tile has NW >> hpt_shift chunks.
 template <int NW>
-__device__ __forceinline__ int seq_tiles(const SeqRange& r) { return (r.n_chunks + NW - 1) / NW; }
+__device__ __forceinline__ int seq_tiles(const SeqRange& r, int hpt_shift) {
+    constexpr int LOG_NW = NW == 8 ? 3 : 2;
+    const int shift = LOG_NW - hpt_shift;
+    return (r.n_chunks + (1 << shift) - 1) >> shift;
+}
 
 // One box of the cache: columns 64 * plane .., rows from `slot` of a page's head.
 __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int axes, int plane, int slot, int head, int page) {
@@ -113,6 +122,18 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, u
 // CTA c of `ctas` takes the tiles [total * c / ctas, total * (c + 1) / ctas).  No more CTAs than tiles: none is empty, so
 // that a cut pair has a partial result from every CTA between its first and its last one.
 __device__ __forceinline__ int cta_count(int64_t total, int grid) { return total < grid ? static_cast<int>(total) : grid; }
+
+// The list's form follows from its length.  Heads side by side read whole pages and leave nothing to merge inside a CTA
+// (64 sequences of up to 8192 keys, 8 heads of 128: 180 us against 199), but cut each pair into as many parts as there are
+// CTAs on it, and joining those is what a short list waits for (one sequence of 1000 keys: 12.5 us against 9.3 with all
+// warps on one head).  So tiles side by side are taken when every CTA gets at least kLongList of them.
+constexpr int kLongList = 4;
+struct ListForm { int64_t total; int hpt_shift; };
+__device__ __forceinline__ ListForm list_form(const DecodeParams& p, int64_t total_side, int64_t total_one) {
+    total_side *= p.heads >> p.hpt_shift;
+    if (p.hpt_shift == 0 || total_side >= static_cast<int64_t>(kLongList) * p.grid) return {total_side, p.hpt_shift};
+    return {total_one * p.heads, 0};
+}
 __device__ __forceinline__ int64_t cta_begin(int64_t total, int c, int ctas) { return total * c / ctas; }
 __device__ __forceinline__ int cta_of_tile(int64_t total, int64_t t, int ctas) {
     return static_cast<int>(((t + 1) * ctas - 1) / total);
@@ -156,34 +177,37 @@ __device__ __forceinline__ void split2(float x0, float x1, uint32_t& hi, uint32_
     lo = sm100::pack2<DTYPE>(x0 - h0, x1 - h1);
 }
 
-// Position in the tile list, advanced tile by tile.  Every warp of a CTA walks the same tiles.
+// Position in the tile list, advanced tile by tile.  Every warp of a CTA walks the same tiles; kvh and r0 are its own.
 template <int NW, int CK>
 struct TileWalk {
-    int b, h, t, t_end;   // sequence, K/V head (times head part), tile inside the pair, tiles of the pair
+    int b, h, t, t_end;   // sequence, group of heads, tile inside the pair, tiles of the pair
     int kvh, r0;          // K/V head, first query head of the part inside its group
+    int hs;               // log2 of the heads of a tile
     SeqRange r;
-    __device__ __forceinline__ void at(const DecodeParams& p, int b_, int h_, int t_) {
+    __device__ __forceinline__ void at(const DecodeParams& p, int hs_, int b_, int h_, int t_) {
+        hs = hs_;
         b = b_;
         h = h_;
         t = t_;
         r = seq_range<CK>(p, b);
-        t_end = seq_tiles<NW>(r);
+        t_end = seq_tiles<NW>(r, hs);
         split_head(p);
     }
     __device__ __forceinline__ void split_head(const DecodeParams& p) {
-        kvh = p.sub == 1 ? h : h / p.sub;
-        r0 = (h - kvh * p.sub) * 16;
+        const int head = (h << hs) + ((threadIdx.x >> 5) & ((1 << hs) - 1));
+        kvh = p.sub == 1 ? head : head / p.sub;
+        r0 = (head - kvh * p.sub) * 16;
     }
     // true: the next tile belongs to another pair
-    __device__ __forceinline__ bool next(const DecodeParams& p, int heads) {
+    __device__ __forceinline__ bool next(const DecodeParams& p, int groups) {
         if (++t < t_end) return false;
         t = 0;
-        if (++h == heads) {
+        if (++h == groups) {
             h = 0;
             do {
                 if (++b >= p.B) return true;      // the end of the list: not used again
                 r = seq_range<CK>(p, b);
-                t_end = seq_tiles<NW>(r);
+                t_end = seq_tiles<NW>(r, hs);
             } while (t_end == 0);
         }
         split_head(p);
@@ -215,7 +239,7 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
     float* merge = reinterpret_cast<float*>(smem + NSTAGE * C::STAGE_BYTES);
     float2* merge_ml = reinterpret_cast<float2*>(merge + NW * GH * C::ROW);
-    int64_t* scan = reinterpret_cast<int64_t*>(merge);       // at the beginning: [0..31] warp sums, then the start
+    int64_t* scan = reinterpret_cast<int64_t*>(merge);       // at the beginning: [0..31] warp sums, [32..34] the start
     const uint32_t bars = sm100::smem_u32(smem) + NSTAGE * C::STAGE_BYTES + C::MERGE_BYTES;     // [warp][stage]: a chunk has arrived
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + NSTAGE * C::STAGE_BYTES + C::MERGE_BYTES + 8 * NW * NSTAGE);
     if (tid < NW * NSTAGE) sm100::mbar_init(bars + 8 * tid, 1);
@@ -228,57 +252,69 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // ---- lay out the tile list: total tiles, and the pair and tile at which this CTA's part begins ----
-    const int heads = p.Hkv * p.sub;
     const int per = (p.B + C::THREADS - 1) / C::THREADS;     // consecutive sequences of a thread
     const int b0 = tid * per, b1 = b0 + per < p.B ? b0 + per : p.B;
-    int64_t mine = 0;
+    int64_t mine[2] = {0, 0};                                // tiles in either form of the list
     for (int b = b0; b < b1; ++b) {
-        mine += seq_tiles<NW>(seq_range<CK>(p, b));
+        const SeqRange r = seq_range<CK>(p, b);
+        mine[0] += seq_tiles<NW>(r, p.hpt_shift);
+        mine[1] += seq_tiles<NW>(r, 0);
         if (p.seq_lens[b] > p.max_len && blockIdx.x == 0) report_bad_index(p.status);
     }
-    int64_t incl = mine;
+    int64_t incl[2] = {mine[0], mine[1]};
 #pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-        const int64_t up = __shfl_up_sync(0xffffffffu, incl, off);
-        if (lane >= off) incl += up;
+    for (int off = 1; off < 32; off <<= 1)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            const int64_t up = __shfl_up_sync(0xffffffffu, incl[f], off);
+            if (lane >= off) incl[f] += up;
+        }
+    if (lane == 31) {
+        scan[warp] = incl[0];
+        scan[16 + warp] = incl[1];
     }
-    if (lane == 31) scan[warp] = incl;
     __syncthreads();
-    int64_t before = incl - mine, total = 0;
+    int64_t before2[2] = {incl[0] - mine[0], incl[1] - mine[1]}, total2[2] = {0, 0};
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-        if (w < warp) before += scan[w];
-        total += scan[w];
-    }
-    total *= heads;
+    for (int w = 0; w < NW; ++w)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            if (w < warp) before2[f] += scan[16 * f + w];
+            total2[f] += scan[16 * f + w];
+        }
+    const ListForm form = list_form(p, total2[0], total2[1]);
+    const int64_t total = form.total;
+    const int hs = form.hpt_shift, groups = p.heads >> hs;
+    const bool side = hs == p.hpt_shift;
+    const int64_t before = side ? before2[0] : before2[1], my_tiles = side ? mine[0] : mine[1];
     const int ctas = cta_count(total, p.grid);
     if (static_cast<int>(blockIdx.x) >= ctas) return;
     const int64_t first = cta_begin(total, blockIdx.x, ctas);
     const int steps = static_cast<int>(cta_begin(total, blockIdx.x + 1, ctas) - first);
     // the thread whose sequences hold tile `first` finds it
-    if (first >= before * heads && first < (before + mine) * heads) {
-        int64_t rem = first - before * heads;
+    if (first >= before * groups && first < (before + my_tiles) * groups) {
+        int64_t rem = first - before * groups;
         for (int b = b0; b < b1; ++b) {
-            const int n = seq_tiles<NW>(seq_range<CK>(p, b));
-            if (rem < static_cast<int64_t>(n) * heads) {
+            const int n = seq_tiles<NW>(seq_range<CK>(p, b), hs);
+            if (rem < static_cast<int64_t>(n) * groups) {
                 scan[32] = b;
                 scan[33] = rem / n;
                 scan[34] = rem % n;
                 break;
             }
-            rem -= static_cast<int64_t>(n) * heads;
+            rem -= static_cast<int64_t>(n) * groups;
         }
     }
     __syncthreads();
     TileWalk<NW, CK> ld, cu;      // the copies run NSTAGE - 1 tiles ahead of the arithmetic
-    ld.at(p, static_cast<int>(scan[32]), static_cast<int>(scan[33]), static_cast<int>(scan[34]));
+    ld.at(p, hs, static_cast<int>(scan[32]), static_cast<int>(scan[33]), static_cast<int>(scan[34]));
     cu = ld;
     __syncthreads();          // the merge buffer takes over the scan's shared memory
 
     const uint32_t ring = sm100::smem_u32(smem) + warp * C::CHUNK_BYTES, my_bars = bars + 8 * warp * NSTAGE;
     // first key of this warp's chunk in the walk's tile; negative: no chunk
     auto chunk_key = [&](const TileWalk<NW, CK>& w) {
-        const int ch = w.t * NW + warp;
+        const int ch = (w.t * NW + warp) >> hs;
         if (ch >= w.r.n_chunks) return -1;
         return (ch < w.r.n_sink ? ch : w.r.lo + ch - w.r.n_sink) * CK;
     };
@@ -323,7 +359,7 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                 }
             }
             if (page == -2) report_bad_index(p.status);
-            ld.next(p, heads);
+            ld.next(p, groups);
             if (++loaded < steps) {
                 key_next = chunk_key(ld);
                 page_next = fetch_page(key_next);
@@ -502,71 +538,109 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                     }
                 }
             }
-            // ---- end of the pair, or of this CTA's part: merge the warps ----
+            // ---- end of the pair, or of this CTA's part ----
             const bool end_pair = cu.t + 1 == cu.t_end;
             if (end_pair || s + 1 == steps) {
+                const bool whole = end_pair && from_start;
+                const int hpt = 1 << hs;
+                float* part = p.parts + (2 * static_cast<int64_t>(blockIdx.x) + (n_pairs > 0 ? 1 : 0)) * hpt * C::PART_FLOATS;
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float x = l[nt][h];
+                    for (int h = 0; h < 2; ++h)
 #pragma unroll
-                        for (int off = 4; off < 32; off <<= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
-                        const int head = 8 * nt + 2 * c + h;
-                        if (g == 0) merge_ml[warp * GH + head] = make_float2(m[nt][h] * sc, x);   // x = 0: no key, the first value is not used
-                        float* dst = merge + (warp * GH + head) * C::ROW + 8 * g;
+                        for (int o = 4; o < 32; o <<= 1) l[nt][h] += __shfl_xor_sync(0xffffffffu, l[nt][h], o);
+                if (hpt == NW) {
+                    // every warp has a head to itself: straight from the registers, 8 contiguous dims per lane and plane
 #pragma unroll
-                        for (int i = 0; i < VI; ++i) {
-                            *reinterpret_cast<float4*>(dst + 64 * i) =
-                                make_float4(acc[nt][i][0][h], acc[nt][i][0][2 + h], acc[nt][i][1][h], acc[nt][i][1][2 + h]);
-                            *reinterpret_cast<float4*>(dst + 64 * i + 4) =
-                                make_float4(acc[nt][i][2][h], acc[nt][i][2][2 + h], acc[nt][i][3][h], acc[nt][i][3][2 + h]);
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int row = 8 * nt + 2 * c + h;
+                            if (cu.r0 + row >= p.group) continue;
+                            const float mm = m[nt][h] * sc, sum = l[nt][h];      // sum 0: no key, mm is not used
+                            if (whole) {
+                                const int64_t out_row = static_cast<int64_t>(cu.b) * p.H + cu.kvh * p.group + cu.r0 + row;
+                                const float inv = sum != 0.f ? 1.f / sum : 0.f;
+                                uint8_t* dst = static_cast<uint8_t*>(p.o) + (out_row * D + 8 * g) * 2;
+#pragma unroll
+                                for (int i = 0; i < VI; ++i) {
+                                    uint32_t w[4];
+#pragma unroll
+                                    for (int x = 0; x < 4; ++x) w[x] = sm100::pack2<DTYPE>(acc[nt][i][x][h] * inv, acc[nt][i][x][2 + h] * inv);
+                                    *reinterpret_cast<uint4*>(dst + 128 * i) = make_uint4(w[0], w[1], w[2], w[3]);
+                                }
+                                if (g == 0) p.lse[out_row] = sum != 0.f ? (mm - P_OFF) * 0.6931471805599453f + logf(sum) : -INFINITY;
+                            } else {
+                                float* dst = part + warp * C::PART_FLOATS;
+#pragma unroll
+                                for (int i = 0; i < VI; ++i)
+#pragma unroll
+                                    for (int x = 0; x < 4; x += 2)
+                                        *reinterpret_cast<float4*>(dst + row * D + 64 * i + 8 * g + 2 * x) =
+                                            make_float4(acc[nt][i][x][h], acc[nt][i][x][2 + h], acc[nt][i][x + 1][h], acc[nt][i][x + 1][2 + h]);
+                                if (g == 0) *reinterpret_cast<float2*>(dst + GH * D + 2 * row) = make_float2(mm, sum);
+                            }
+                        }
+                } else {
+                    // several warps share a head: through shared memory
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int row = 8 * nt + 2 * c + h;
+                            if (g == 0) merge_ml[warp * GH + row] = make_float2(m[nt][h] * sc, l[nt][h]);
+                            float* dst = merge + (warp * GH + row) * C::ROW + 8 * g;
+#pragma unroll
+                            for (int i = 0; i < VI; ++i)
+#pragma unroll
+                                for (int x = 0; x < 4; x += 2)
+                                    *reinterpret_cast<float4*>(dst + 64 * i + 2 * x) =
+                                        make_float4(acc[nt][i][x][h], acc[nt][i][x][2 + h], acc[nt][i][x + 1][h], acc[nt][i][x + 1][2 + h]);
+                        }
+                    __syncthreads();
+                    const int rows = p.group < GH ? p.group : GH;         // of a head; the last part of a group may have fewer
+                    for (int e = tid; e < hpt * rows * (D / 4); e += C::THREADS) {
+                        const int d4 = e % (D / 4), x = e / (D / 4), row = x % rows, hh = x / rows;
+                        const int head = (cu.h << hs) + hh, kvh = head / p.sub, r0 = (head - kvh * p.sub) * 16;
+                        if (r0 + row >= p.group) continue;
+                        float mm = -INFINITY;
+                        for (int w = hh; w < NW; w += hpt) {
+                            const float2 ml = merge_ml[w * GH + row];
+                            if (ml.y != 0.f) mm = fmaxf(mm, ml.x);
+                        }
+                        float sum = 0.f;
+                        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+                        for (int w = hh; w < NW; w += hpt) {
+                            const float2 ml = merge_ml[w * GH + row];
+                            if (ml.y == 0.f) continue;       // this warp saw no key of the pair
+                            const float f = sm100::ex2_approx(ml.x - mm);
+                            const float4 v = *reinterpret_cast<const float4*>(merge + (w * GH + row) * C::ROW + 4 * d4);
+                            sum = fmaf(f, ml.y, sum);
+                            o.x = fmaf(f, v.x, o.x);
+                            o.y = fmaf(f, v.y, o.y);
+                            o.z = fmaf(f, v.z, o.z);
+                            o.w = fmaf(f, v.w, o.w);
+                        }
+                        if (whole) {
+                            const int64_t out_row = static_cast<int64_t>(cu.b) * p.H + kvh * p.group + r0 + row;
+                            const float inv = sum != 0.f ? 1.f / sum : 0.f;
+                            uint2 w;
+                            w.x = sm100::pack2<DTYPE>(o.x * inv, o.y * inv);
+                            w.y = sm100::pack2<DTYPE>(o.z * inv, o.w * inv);
+                            reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.o) + out_row * D * 2)[d4] = w;
+                            if (d4 == 0) p.lse[out_row] = sum != 0.f ? (mm - P_OFF) * 0.6931471805599453f + logf(sum) : -INFINITY;
+                        } else {
+                            float* dst = part + hh * C::PART_FLOATS;
+                            *reinterpret_cast<float4*>(dst + row * D + 4 * d4) = o;
+                            if (d4 == 0) *reinterpret_cast<float2*>(dst + GH * D + 2 * row) = make_float2(mm, sum);
                         }
                     }
+                    __syncthreads();     // the merge buffer may be written again
                 }
-                __syncthreads();
-                const int rows = p.group - cu.r0 < GH ? p.group - cu.r0 : GH;
-                const bool whole = end_pair && from_start;
-                float* part = p.parts + (2 * static_cast<int64_t>(blockIdx.x) + (n_pairs > 0 ? 1 : 0)) * C::PART_FLOATS;
-                for (int e = tid; e < rows * (D / 4); e += C::THREADS) {
-                    const int row = e / (D / 4), d4 = e % (D / 4);
-                    float mm = -INFINITY;
-#pragma unroll
-                    for (int w = 0; w < NW; ++w) {
-                        const float2 ml = merge_ml[w * GH + row];
-                        if (ml.y != 0.f) mm = fmaxf(mm, ml.x);
-                    }
-                    float sum = 0.f;
-                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                    for (int w = 0; w < NW; ++w) {
-                        const float2 ml = merge_ml[w * GH + row];
-                        if (ml.y == 0.f) continue;       // this warp saw no key of the pair
-                        const float f = sm100::ex2_approx(ml.x - mm);
-                        const float4 v = *reinterpret_cast<const float4*>(merge + (w * GH + row) * C::ROW + 4 * d4);
-                        sum = fmaf(f, ml.y, sum);
-                        o.x = fmaf(f, v.x, o.x);
-                        o.y = fmaf(f, v.y, o.y);
-                        o.z = fmaf(f, v.z, o.z);
-                        o.w = fmaf(f, v.w, o.w);
-                    }
-                    if (whole) {
-                        const int64_t out_row = static_cast<int64_t>(cu.b) * p.H + cu.kvh * p.group + cu.r0 + row;
-                        const float inv = sum != 0.f ? 1.f / sum : 0.f;
-                        uint2 w;
-                        w.x = sm100::pack2<DTYPE>(o.x * inv, o.y * inv);
-                        w.y = sm100::pack2<DTYPE>(o.z * inv, o.w * inv);
-                        reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.o) + out_row * D * 2)[d4] = w;
-                        if (d4 == 0) p.lse[out_row] = sum != 0.f ? (mm - P_OFF) * 0.6931471805599453f + logf(sum) : -INFINITY;
-                    } else {
-                        *reinterpret_cast<float4*>(part + row * D + 4 * d4) = o;
-                        if (d4 == 0) *reinterpret_cast<float2*>(part + GH * D + 2 * row) = make_float2(mm, sum);
-                    }
-                }
-                __syncthreads();     // the merge buffer may be written again
                 ++n_pairs;
             }
-            if (cu.next(p, heads) && s + 1 < steps) {
+            if (cu.next(p, groups) && s + 1 < steps) {
                 start_pair();
                 from_start = true;
             }
@@ -577,68 +651,79 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
 }
 
 // Joins the partial results of the pairs that more than one CTA of the first kernel worked on, and writes the rows of
-// sequences without a visible key.  One CTA per (sequence, K/V head, head part); the list layout is worked out before
-// the first kernel's results are waited for.
+// sequences without a visible key.  One CTA per (sequence, head); the list layout is worked out before the first kernel's
+// results are waited for.  The threads are 16-byte columns of a row x rows x shares of the parts.
 template <int D, int DTYPE, int GH>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(512)
 attn_paged_join_kernel(const DecodeParams p) {
     using C = DecodeCfg<D, GH>;
-    constexpr int NW = C::NW;
+    constexpr int NW = C::NW, COLS = D / 4, TEAMS = 512 / COLS;
     constexpr float P_OFF = ExpRange<DTYPE>::P_OFF;
-    __shared__ int64_t red[16];
+    __shared__ int64_t red[4][16];
     __shared__ float wgt[GH][2 * kMaxCtas + 2];
-    const int heads = p.Hkv * p.sub;
-    const int b = blockIdx.x / heads, h = blockIdx.x - b * heads;
+    __shared__ float4 sums[TEAMS][COLS];
+    const int b = blockIdx.x / p.heads, head = blockIdx.x - b * p.heads;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    int64_t before = 0, total = 0;
-    for (int x = tid; x < p.B; x += 256) {
-        const int n = seq_tiles<NW>(seq_range<C::CK>(p, x));
-        total += n;
-        if (x < b) before += n;
+    int64_t sum4[4] = {0, 0, 0, 0};                   // tiles of the sequences before b and of all, in either form of the list
+    for (int x = tid; x < p.B; x += 512) {
+        const SeqRange r = seq_range<C::CK>(p, x);
+        const int n0 = seq_tiles<NW>(r, p.hpt_shift), n1 = seq_tiles<NW>(r, 0);
+        sum4[2] += n0;
+        sum4[3] += n1;
+        if (x < b) {
+            sum4[0] += n0;
+            sum4[1] += n1;
+        }
     }
-    before = warp_sum(before);
-    total = warp_sum(total);
-    if (lane == 0) {
-        red[warp] = before;
-        red[8 + warp] = total;
+#pragma unroll
+    for (int f = 0; f < 4; ++f) {
+        sum4[f] = warp_sum(sum4[f]);
+        if (lane == 0) red[f][warp] = sum4[f];
     }
     __syncthreads();
-    before = total = 0;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) {
-        before += red[w];
-        total += red[8 + w];
+    for (int f = 0; f < 4; ++f) {
+        sum4[f] = 0;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) sum4[f] += red[f][w];
     }
-    total *= heads;
-    const int n = seq_tiles<NW>(seq_range<C::CK>(p, b));
+    const ListForm form = list_form(p, sum4[2], sum4[3]);
+    const int64_t total = form.total;
+    const int hs = form.hpt_shift, groups = p.heads >> hs;
+    const int64_t before = hs == p.hpt_shift ? sum4[0] : sum4[1];
+    const int n = seq_tiles<NW>(seq_range<C::CK>(p, b), hs);
     // Every CTA waits for the first kernel, also one without work: in a graph this kernel's end stands for both.
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int kvh = h / p.sub, r0 = (h - kvh * p.sub) * 16;
+    const int kvh = head / p.sub, r0 = (head - kvh * p.sub) * 16;
     const int rows = p.group - r0 < GH ? p.group - r0 : GH;
     const int64_t row0 = static_cast<int64_t>(b) * p.H + kvh * p.group + r0;
     if (n == 0) {
-        for (int e = tid; e < rows * (D / 4); e += 256) {
+        for (int e = tid; e < rows * COLS; e += 512) {
             reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.o) + row0 * D * 2)[e] = make_uint2(0u, 0u);
             if (e < rows) p.lse[row0 + e] = -INFINITY;
         }
         return;
     }
-    const int64_t t0 = before * heads + static_cast<int64_t>(h) * n, t1 = t0 + n;
+    const int hg = head >> hs, hh = head - (hg << hs);
+    const int64_t t0 = before * groups + static_cast<int64_t>(hg) * n, t1 = t0 + n;
     const int ctas = cta_count(total, p.grid);
     const int c0 = cta_of_tile(total, t0, ctas), c1 = cta_of_tile(total, t1 - 1, ctas);
     if (c0 == c1) return;                        // finished by the first kernel
     // the pair is the first of every CTA but, perhaps, of c0
     const int slot0 = 2 * c0 + (cta_begin(total, c0, ctas) < t0 ? 1 : 0);
     const int np = c1 - c0 + 1;
-    auto slot = [&](int i) { return i == 0 ? slot0 : 2 * (c0 + i); };
-    for (int e = tid; e < rows * np; e += 256) {
+    auto part = [&](int i) {
+        const int64_t slot = i == 0 ? slot0 : 2 * (c0 + i);
+        return p.parts + ((slot << hs) + hh) * C::PART_FLOATS;
+    };
+    for (int e = tid; e < rows * np; e += 512) {
         const int row = e / np, i = e - row * np;
-        const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.parts + static_cast<int64_t>(slot(i)) * C::PART_FLOATS + GH * D + 2 * row));
+        const float2 ml = __ldcg(reinterpret_cast<const float2*>(part(i) + GH * D + 2 * row));
         wgt[row][2 * i] = ml.x;
         wgt[row][2 * i + 1] = ml.y;
     }
     __syncthreads();
-    for (int row = warp; row < rows; row += 8) {     // weights exp2(m_i - max), scaled by 1 / sum
+    for (int row = warp; row < rows; row += 16) {    // weights exp2(m_i - max) / sum
         float mm = -INFINITY;
         for (int i = lane; i < np; i += 32)
             if (wgt[row][2 * i + 1] != 0.f) mm = fmaxf(mm, wgt[row][2 * i]);
@@ -658,24 +743,39 @@ attn_paged_join_kernel(const DecodeParams p) {
         if (lane == 0) p.lse[row0 + row] = sum != 0.f ? (mm - P_OFF) * 0.6931471805599453f + logf(sum) : -INFINITY;
     }
     __syncthreads();
-    for (int e = tid; e < rows * (D / 4); e += 256) {
-        const int row = e / (D / 4), d4 = e % (D / 4);
+    const int team = tid / COLS, col = tid % COLS;
+    int lanes_of_rows = 1;                                   // rows side by side: a power of two, the rest of the teams share parts
+    while (lanes_of_rows < rows && lanes_of_rows < TEAMS) lanes_of_rows <<= 1;
+    const int shares = TEAMS / lanes_of_rows, share = team / lanes_of_rows;
+    for (int rr = 0; rr < rows; rr += lanes_of_rows) {
+        const int row = rr + team % lanes_of_rows;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int i = 0; i < np; ++i) {
-            const float f = wgt[row][2 * i];
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(p.parts + static_cast<int64_t>(slot(i)) * C::PART_FLOATS + row * D + 4 * d4));
-            if (f != 0.f) {     // a part without a visible key adds nothing
-                o.x = fmaf(f, v.x, o.x);
-                o.y = fmaf(f, v.y, o.y);
-                o.z = fmaf(f, v.z, o.z);
-                o.w = fmaf(f, v.w, o.w);
+        if (row < rows) {
+#pragma unroll 8
+            for (int i = share; i < np; i += shares) {
+                const float f = wgt[row][2 * i];
+                const float4 v = __ldcg(reinterpret_cast<const float4*>(part(i) + row * D) + col);
+                if (f != 0.f) {     // a part without a visible key adds nothing
+                    o.x = fmaf(f, v.x, o.x);
+                    o.y = fmaf(f, v.y, o.y);
+                    o.z = fmaf(f, v.z, o.z);
+                    o.w = fmaf(f, v.w, o.w);
+                }
             }
         }
-        uint2 w;
-        w.x = sm100::pack2<DTYPE>(o.x, o.y);
-        w.y = sm100::pack2<DTYPE>(o.z, o.w);
-        reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.o) + (row0 + row) * D * 2)[d4] = w;
+        sums[team][col] = o;
+        __syncthreads();
+        if (share == 0 && row < rows) {
+            for (int s = 1; s < shares; ++s) {
+                const float4 v = sums[team + s * lanes_of_rows][col];
+                o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
+            }
+            uint2 w;
+            w.x = sm100::pack2<DTYPE>(o.x, o.y);
+            w.y = sm100::pack2<DTYPE>(o.z, o.w);
+            reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.o) + (row0 + row) * D * 2)[col] = w;
+        }
+        __syncthreads();
     }
 }
 

@@ -112,8 +112,10 @@ def test_append_validation(lib):
 
 def test_decode_validation(lib):
     ws_bytes = lib.attn_paged_decode_workspace_bytes
-    assert ws_bytes(8, 2, 128) == (2 * 148 * 8 * 130 * 4 + 255) // 256 * 256
-    assert ws_bytes(40, 2, 64) == (2 * 148 * 16 * 66 * 4 + 255) // 256 * 256 and ws_bytes(3, 2, 64) == 0 and ws_bytes(2, 2, 96) == 0
+    # two partial results per SM, each of as many heads as a tile covers (a power of two that divides them, at most 8)
+    assert ws_bytes(8, 2, 128) == (2 * 148 * 2 * 8 * 130 * 4 + 255) // 256 * 256
+    assert ws_bytes(40, 2, 64) == (2 * 148 * 4 * 16 * 66 * 4 + 255) // 256 * 256 and ws_bytes(3, 2, 64) == 0 and ws_bytes(2, 2, 96) == 0
+    assert ws_bytes(64, 64, 64) == (2 * 148 * 8 * 8 * 66 * 4 + 255) // 256 * 256
 
     def f(q=0x1000, kc=0x5000, vc=0x6000, cs=None, pages=4, page=16, bt=0x700, ts=4, mp=4, lens=0x800, o=0x2000, lse=0x3000, B=3, H=4, Hkv=2, D=64,
           scale=0.1, window=0, sinks=0, dtype=0, ws=0x10000, ws_n=1 << 24):

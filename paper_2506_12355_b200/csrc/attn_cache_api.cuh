@@ -119,6 +119,11 @@ int log2_of(int x) {
     return s;
 }
 
+// Tokens, and items of a token and a few heads, are counted in 32 bits (more would not fit any GPU's memory).
+bool rope_tokens_ok(int64_t tokens, int H, int Hkv) {
+    return tokens < (1LL << 31) - 64 && H < (1 << 20) && Hkv < (1 << 20) && (tokens / 8 + 1) * ((H > Hkv ? H : Hkv) / 4 + 1) < (1LL << 32);
+}
+
 void rope_units(attn_rope::RopeParams& p, int D) {
     const int per = attn_rope::kDeep * (256 / D);
     int end = 0;
@@ -132,8 +137,7 @@ template <bool PAGED>
 int launch_rope(attn_rope::RopeParams& p, int D, int dtype, cudaStream_t st) {
     rope_units(p, D);
     if (p.tokens == 0 || p.unit_end[2] == 0) return ATTN_OK;
-    const int64_t gx = (p.tokens + attn_rope::kWarps - 1) / attn_rope::kWarps;
-    if (gx > 2147483647LL) return ATTN_ERR_BAD_SHAPE;
+    const int64_t gx = (static_cast<int64_t>(p.tokens) + attn_rope::kWarps - 1) / attn_rope::kWarps;
     // few tokens: their heads are spread over blocks until the GPU has eight blocks per SM
     int64_t gy = (148 * 8 + gx - 1) / gx;
     if (gy > p.unit_end[2]) gy = p.unit_end[2];
@@ -163,7 +167,7 @@ int validate_window(int Sq, int* window, int sinks, int q_offset) {
     return ATTN_OK;
 }
 
-constexpr int kRopeBwdBlocks = 148 * 4;   // blocks of the gradient kernel at most (each leaves 2 D partial sums)
+constexpr int kRopeBwdBlocks = 148 * attn_rope::kBwdBlocks;   // blocks of the gradient kernel at most: one wave (each leaves D partial sums)
 
 }  // namespace
 
@@ -219,6 +223,7 @@ int attn_qk_norm_rope(const void* q, const void* k, const void* v, const long lo
     if (R > 0 && !positions && S > table_len) return ATTN_ERR_BAD_SHAPE;
     const int64_t tokens = static_cast<int64_t>(B) * S;
     if (tokens == 0 || (H == 0 && Hkv == 0)) return ATTN_OK;
+    if (!rope_tokens_ok(tokens, H, Hkv)) return ATTN_ERR_BAD_SHAPE;
     if (!in_strides || (H > 0 && (!q || !q_out)) || (Hkv > 0 && (!k || !k_out || !v != !v_out))) return ATTN_ERR_NULL_POINTER;
     if (misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(q_out, 16) || misaligned(k_out, 16) ||
         misaligned(v_out, 16) || misaligned(positions, 4) || !strides_ok(in_strides, 9))
@@ -245,7 +250,7 @@ int attn_qk_norm_rope(const void* q, const void* k, const void* v, const long lo
     p.interleaved = interleaved;
     p.positions = positions;
     p.eps = eps;
-    p.tokens = tokens;
+    p.tokens = static_cast<int>(tokens);
     p.S = S;
     p.status = cached_status_ptr();
     if (!p.status) return ATTN_ERR_CUDA;
@@ -253,7 +258,7 @@ int attn_qk_norm_rope(const void* q, const void* k, const void* v, const long lo
 }
 
 size_t attn_qk_norm_rope_bwd_workspace_bytes(int D) {
-    return head_dim_ok(D) ? static_cast<size_t>(kRopeBwdBlocks) * 2 * D * sizeof(float) : 0;
+    return head_dim_ok(D) ? static_cast<size_t>(kRopeBwdBlocks) * D * sizeof(float) : 0;
 }
 
 int attn_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const void* q, const void* k,
@@ -267,6 +272,7 @@ int attn_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const 
     if (rc != ATTN_OK) return rc;
     if (R > 0 && !positions && S > table_len) return ATTN_ERR_BAD_SHAPE;
     const int64_t tokens = static_cast<int64_t>(B) * S;
+    if (!rope_tokens_ok(tokens, H, Hkv)) return ATTN_ERR_BAD_SHAPE;
     if ((q_weight && !dq_weight) || (k_weight && !dk_weight)) return ATTN_ERR_NULL_POINTER;
     if (misaligned(dq_weight, 4) || misaligned(dk_weight, 4)) return ATTN_ERR_MISALIGNED;
     if (tokens > 0) {
@@ -315,13 +321,25 @@ int attn_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const 
     p.interleaved = interleaved;
     p.positions = positions;
     p.eps = eps;
-    p.tokens = tokens;
+    p.tokens = static_cast<int>(tokens);
     p.S = S;
     p.partial = static_cast<float*>(workspace);
     p.status = cached_status_ptr();
     if (!p.status) return ATTN_ERR_CUDA;
-    int64_t blocks = (tokens + attn_rope::kWarps - 1) / attn_rope::kWarps;
-    if (blocks > kRopeBwdBlocks) blocks = kRopeBwdBlocks;
+    // blocks of q and of (k, v): by their bytes (a row of q or k is read twice and written, of v read and written), each at
+    // least one where it has heads, and no more than it has items
+    const int per_unit = attn_rope::kDeep * (256 / D);
+    const int64_t steps = (tokens + attn_rope::kWarps - 1) / attn_rope::kWarps;
+    const int64_t q_items = steps * ((H + per_unit - 1) / per_unit), k_items = steps * ((Hkv + per_unit - 1) / per_unit);
+    const double q_cost = 3.0 * H, kv_cost = (dv ? 5.0 : 3.0) * Hkv;
+    int64_t q_blocks = H == 0 ? 0 : static_cast<int64_t>(kRopeBwdBlocks * q_cost / (q_cost + kv_cost) + 0.5);
+    if (H > 0 && q_blocks < 1) q_blocks = 1;
+    if (Hkv > 0 && q_blocks > kRopeBwdBlocks - 1) q_blocks = kRopeBwdBlocks - 1;
+    int64_t kv_blocks = Hkv == 0 ? 0 : kRopeBwdBlocks - q_blocks;
+    if (q_blocks > q_items) q_blocks = q_items;
+    if (kv_blocks > k_items) kv_blocks = k_items;
+    const int64_t blocks = q_blocks + kv_blocks;
+    p.q_blocks = static_cast<int>(q_blocks);
 #define ATTN_ROPE_CASE(DD, TT) \
     if (D == DD && dtype == TT) attn_rope::attn_rope_bwd_kernel<DD, TT><<<static_cast<unsigned>(blocks), attn_rope::kWarps * 32, 0, st>>>(p);
     ATTN_ROPE_CASE(64, 0)
@@ -334,7 +352,7 @@ int attn_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const 
     if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
     if (!dq_weight && !dk_weight) return ATTN_OK;
     return launch_dependent(attn_rope::attn_rope_weight_grad_kernel, dim3(2 * D / 32), dim3(1024), 0, st, p.partial,
-                            static_cast<int>(blocks), D, dq_weight, dk_weight)
+                            p.q_blocks, static_cast<int>(blocks), D, dq_weight, dk_weight)
                ? ATTN_OK
                : ATTN_ERR_CUDA;
 }

@@ -45,7 +45,7 @@ def test_norm_rope_validation(lib):
 
 
 def test_norm_rope_bwd_validation(lib):
-    assert lib.attn_qk_norm_rope_bwd_workspace_bytes(64) == 148 * 4 * 2 * 64 * 4 and lib.attn_qk_norm_rope_bwd_workspace_bytes(96) == 0
+    assert lib.attn_qk_norm_rope_bwd_workspace_bytes(64) == 148 * 2 * 64 * 4 and lib.attn_qk_norm_rope_bwd_workspace_bytes(96) == 0
 
     def f(dq=0x1000, dk=0x2000, dv=0x3000, q=0x7000, k=0x8000, qw=0x100, kw=0x200, tab=0x400, n=128, R=64, eps=1e-6, dqi=0x4000, dki=0x5000,
           dvi=0x6000, out=None, dqw=0x500, dkw=0x600, B=1, S=128, H=4, Hkv=2, D=64, dtype=0, ws=0x10000, ws_n=1 << 22):

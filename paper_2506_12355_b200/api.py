@@ -118,6 +118,42 @@ def load() -> ctypes.CDLL:
     return lib
 
 
+# Entry points that _binding marshals in C++, in the order in which its bind() takes their addresses.
+_BOUND = ["attn_qk_norm_rope", "attn_qk_norm_rope_bwd", "attn_qk_norm_rope_bwd_workspace_bytes", "attn_paged_append", "attn_paged_decode",
+          "attn_paged_decode_workspace_bytes", "attn_fwd_window", "attn_bwd_window", "attn_bwd_window_workspace_bytes"]
+
+
+def _bind():
+    """The _binding extension, or None where it is not built (the calls then take their Python path)."""
+    try:
+        from . import _binding
+    except ImportError:
+        return None
+    lib = load()
+    _binding.bind([ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _BOUND])
+    return _binding
+
+
+_UNBOUND = object()
+_binding_module = _UNBOUND
+
+
+def _fast(name, stream, *args):
+    """The call through _binding: its result, or NotImplemented where the Python path has to take it (an explicit stream, tensors
+    of another device than the current one, anything that needs a message)."""
+    global _binding_module
+    if stream is not None:
+        return NotImplemented
+    if _binding_module is _UNBOUND:
+        _binding_module = _bind()
+    if _binding_module is None:
+        return NotImplemented
+    result = getattr(_binding_module, name)(*args)
+    if type(result) is int:
+        raise AttnError(result, name)
+    return result
+
+
 def _dtype_code(t: torch.Tensor) -> int:
     if t.dtype == torch.float16:
         return DTYPE_FP16
@@ -385,6 +421,9 @@ def attn_bwd(q, k, v, o, lse, dout, scale: float, causal: bool = False, dq=None,
 def attn_fwd_window(q, k, v, scale: float, window: int, sinks: int = 0, q_offset: int = 0, out=None, lse=None, stream=None):
     """Attention under a sliding window: q [B,H,Sq,D] at positions q_offset, q_offset + 1, .., k, v [B,Hkv,Sk,D] (D in {64, 128});
     key j is visible at position p iff j <= p and (j > p - window or j < sinks); window 0: no lower end."""
+    result = _fast("attn_fwd_window", stream, q, k, v, scale, window, sinks, q_offset, out, lse)
+    if result is not NotImplemented:
+        return result
     B, H, Hkv, Sq, Sk, D, _ = _check_grouped(q, k, v)
     dt, dtype, device = _dtype_code(q), q.dtype, q.device
     if out is None:
@@ -408,6 +447,9 @@ def attn_bwd_window(q, k, v, o, lse, dout, scale: float, window: int, sinks: int
                     workspace=None, stream=None):
     """Gradients (dq, dk, dv) of attn_fwd_window's output for the upstream gradient dout; o and lse from the forward call.
     `workspace`: CUDA uint8 tensor of at least attn_bwd_window_workspace_bytes(...) bytes (allocated here when None)."""
+    result = _fast("attn_bwd_window", stream, q, k, v, o, lse, dout, scale, window, sinks, q_offset, dq, dk, dv, workspace)
+    if result is not NotImplemented:
+        return result
     B, H, Hkv, Sq, Sk, D, _ = _check_grouped(q, k, v)
     dt, dtype, device = _dtype_code(q), q.dtype, q.device
     q_shape, k_shape = (B, H, Sq, D), (B, Hkv, Sk, D)
@@ -433,14 +475,31 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-_Strides = {n: ctypes.c_longlong * n for n in (6, 9)}
+_stride_arrays = {}
+
+
+def _strides(*values):
+    """A host array of element strides.  A caller's tensors come with the same strides call after call, so the arrays are
+    kept (they are only read)."""
+    a = _stride_arrays.get(values)
+    if a is None:
+        if len(_stride_arrays) >= 1024:
+            _stride_arrays.clear()
+        a = _stride_arrays[values] = (ctypes.c_longlong * len(values))(*values)
+    return a
 
 
 def _rows3(a, b, c=None):
-    """Element strides of axes 0, 1, 2 of two or three tensors (zeros for None) as a host array."""
+    """Element strides of axes 0, 1, 2 of two or three tensors (zeros for None)."""
     if c is None:
-        return _Strides[9](*a.stride()[:3], *b.stride()[:3], 0, 0, 0)
-    return _Strides[9](*a.stride()[:3], *b.stride()[:3], *c.stride()[:3])
+        return _strides(*a.stride()[:3], *b.stride()[:3], 0, 0, 0)
+    return _strides(*a.stride()[:3], *b.stride()[:3], *c.stride()[:3])
+
+
+def _is(t, shape, dtype, index):
+    """Cheap form of _require for the checks that every call makes (whose cost is a good part of a small call): contiguous in the
+    last axis, this shape, type and GPU."""
+    return t.shape == shape and t.dtype is dtype and t.get_device() == index and (t.stride(-1) == 1 or shape[-1] <= 1)
 
 
 def _require(t, name, shape, dtype, device, dense=True):
@@ -458,23 +517,23 @@ def _require(t, name, shape, dtype, device, dense=True):
         raise ValueError("the values of a head of %s must be contiguous" % name)
 
 
-def _check_rope(x, D, q_weight, k_weight, cos_sin):
-    """Weights [D] of one type (x's or fp32) and the table fp32 [positions, R]: (weights are fp32, table length, R)."""
-    f32 = None
-    for w in (q_weight, k_weight):
-        if w is None:
-            continue
-        _require(w, "q_weight, k_weight", (D,), x.dtype if w.dtype != torch.float32 else torch.float32, x.device)
-        if f32 is not None and f32 != (w.dtype == torch.float32):
-            raise TypeError("q_weight and k_weight must share one dtype")
-        f32 = w.dtype == torch.float32
+def _check_rope(dtype, device, D, q_weight, k_weight, cos_sin):
+    """Weights [D] of one type (`dtype` or fp32) and the table fp32 [positions, R]: (weights are fp32, table length, R)."""
+    index = device.index
+    any_weight = q_weight if q_weight is not None else k_weight
+    f32 = any_weight is not None and any_weight.dtype is torch.float32
+    wanted = torch.float32 if f32 else dtype
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None and not _is(w, (D,), wanted, index):
+            _require(w, name, (D,), wanted, device)
     if cos_sin is None:
-        return int(bool(f32)), 0, 0
-    if cos_sin.dim() != 2:
-        raise ValueError("cos_sin must be [positions, R]")
+        return f32, 0, 0
     shape = cos_sin.shape
-    _require(cos_sin, "cos_sin", shape, torch.float32, x.device)
-    return int(bool(f32)), shape[0], shape[1]
+    if len(shape) != 2:
+        raise ValueError("cos_sin must be [positions, R]")
+    if not (_is(cos_sin, shape, torch.float32, index) and cos_sin.is_contiguous()):
+        _require(cos_sin, "cos_sin", shape, torch.float32, device)
+    return f32, shape[0], shape[1]
 
 
 def attn_qk_norm_rope(q, k, v, q_weight, k_weight, cos_sin, positions=None, eps: float = 1e-6, interleaved: bool = False,
@@ -484,6 +543,9 @@ def attn_qk_norm_rope(q, k, v, q_weight, k_weight, cos_sin, positions=None, eps:
     copied to v_out [B,Hkv,S,D].  q_weight, k_weight: [D] in q's dtype or float32 (None: not normalised); cos_sin: float32
     [positions, R], R/2 cosines then R/2 sines per position (None: not rotated); positions: int32 [B,S] (None: 0 .. S-1);
     interleaved: pairs (2i, 2i+1) instead of (i, i + R/2)."""
+    result = _fast("attn_qk_norm_rope", stream, q, k, v, q_weight, k_weight, cos_sin, positions, eps, interleaved, q_out, k_out, v_out)
+    if result is not NotImplemented:
+        return result
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q and k must be [B,S,heads,D]")
     B, S, H, D = q.shape
@@ -491,9 +553,12 @@ def attn_qk_norm_rope(q, k, v, q_weight, k_weight, cos_sin, positions=None, eps:
     dt, dtype, device = _dtype_code(q), q.dtype, q.device
     if not q.is_cuda:
         raise ValueError("q must be a CUDA tensor")
-    _require(q, "q", (B, S, H, D), dtype, device, False)
-    _require(k, "k", (B, S, Hkv, D), dtype, device, False)
-    f32, n_pos, R = _check_rope(q, D, q_weight, k_weight, cos_sin)
+    index = device.index
+    if not _is(q, q.shape, dtype, index):
+        _require(q, "q", (B, S, H, D), dtype, device, False)
+    if not _is(k, (B, S, Hkv, D), dtype, index):
+        _require(k, "k", (B, S, Hkv, D), dtype, device, False)
+    f32, n_pos, R = _check_rope(dtype, device, D, q_weight, k_weight, cos_sin)
     if positions is not None:
         _require(positions, "positions", (B, S), torch.int32, device)
     if q_out is None:
@@ -508,7 +573,8 @@ def attn_qk_norm_rope(q, k, v, q_weight, k_weight, cos_sin, positions=None, eps:
     if v is None:
         v_out = None
     else:
-        _require(v, "v", (B, S, Hkv, D), dtype, device, False)
+        if not _is(v, (B, S, Hkv, D), dtype, index):
+            _require(v, "v", (B, S, Hkv, D), dtype, device, False)
         if v_out is None:
             v_out = torch.empty(kv_shape, dtype=dtype, device=device)
         else:
@@ -529,6 +595,10 @@ def attn_qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positio
     outputs, q [B,S,H,D], k [B,S,Hkv,D] its inputs.  Returns (dq_in [B,S,H,D], dk_in, dv_in [B,S,Hkv,D], dq_weight, dk_weight
     (float32 [D], None without a weight)).  dq_in, dk_in, dv_in may be given as strided views of one buffer.
     `workspace`: CUDA uint8 tensor of at least attn_qk_norm_rope_bwd_workspace_bytes(D) bytes (allocated here when None)."""
+    result = _fast("attn_qk_norm_rope_bwd", stream, dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positions, eps, interleaved, dq_in, dk_in, dv_in,
+                   workspace)
+    if result is not NotImplemented:
+        return result
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q and k must be [B,S,heads,D]")
     B, S, H, D = q.shape
@@ -541,7 +611,7 @@ def attn_qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positio
     _require(k, "k", k_shape, dtype, device, False)
     _require(dq, "dq", (B, H, S, D), dtype, device)
     _require(dk, "dk", (B, Hkv, S, D), dtype, device)
-    f32, n_pos, R = _check_rope(q, D, q_weight, k_weight, cos_sin)
+    f32, n_pos, R = _check_rope(dtype, device, D, q_weight, k_weight, cos_sin)
     if positions is not None:
         _require(positions, "positions", (B, S), torch.int32, device)
     if dq_in is None:
@@ -577,19 +647,20 @@ def _bytes(workspace):
 
 def _check_cache(D, dtype, device, k_cache, v_cache, block_table, seq_lens):
     """Caches [pages, Hkv, page_size, D] (any strides, rows contiguous), block_table int32 [sequences, max_pages], seq_lens
-    int32 [sequences].  Returns (pages, Hkv, page_size, the caches' strides)."""
-    shape = k_cache.shape
+    int32 [sequences].  Returns (pages, Hkv, page_size, the caches' strides, sequences, max_pages)."""
+    shape, index = k_cache.shape, device.index
     if len(shape) != 4 or shape[3] != D:
         raise ValueError("k_cache and v_cache must be [pages, Hkv, page_size, %d], got %s" % (D, list(shape)))
-    _require(k_cache, "k_cache", shape, dtype, device, False)
-    _require(v_cache, "v_cache", shape, dtype, device, False)
+    if not (_is(k_cache, shape, dtype, index) and _is(v_cache, shape, dtype, index)):
+        _require(k_cache, "k_cache", shape, dtype, device, False)
+        _require(v_cache, "v_cache", shape, dtype, device, False)
     if seq_lens.dim() != 1 or block_table.dim() != 2:
         raise ValueError("block_table must be [sequences, max_pages] and seq_lens [sequences]")
-    n = seq_lens.shape[0]
-    _require(seq_lens, "seq_lens", (n,), torch.int32, device)
-    _require(block_table, "block_table", (n, block_table.shape[1]), torch.int32, device, False)
-    k, v = k_cache.stride(), v_cache.stride()
-    return shape[0], shape[1], shape[2], _Strides[6](k[0], k[1], k[2], v[0], v[1], v[2])
+    n, width = block_table.shape
+    if not (_is(seq_lens, (n,), torch.int32, index) and _is(block_table, (n, width), torch.int32, index)):
+        _require(seq_lens, "seq_lens", (n,), torch.int32, device)
+        _require(block_table, "block_table", (n, width), torch.int32, device, False)
+    return shape[0], shape[1], shape[2], _strides(*k_cache.stride()[:3], *v_cache.stride()[:3]), n, width
 
 
 def attn_paged_append(q, k, v, k_cache, v_cache, block_table, seq_lens, q_weight=None, k_weight=None, cos_sin=None, cu_seqlens=None,
@@ -599,38 +670,46 @@ def attn_paged_append(q, k, v, k_cache, v_cache, block_table, seq_lens, q_weight
     ([pages, Hkv, page_size, D], any strides).  seq_lens int32 [B]: lengths with the new tokens; block_table int32 [B, max_pages];
     cu_seqlens int32 [B+1]: first new token of each sequence and the end (None: one token per sequence, T == B).  Tokens
     behind the end, and of sequences of length 0, are padding: nothing is written for them.  Returns q_out [T,H,D]."""
+    result = _fast("attn_paged_append", stream, q, k, v, k_cache, v_cache, block_table, seq_lens, q_weight, k_weight, cos_sin, cu_seqlens, eps,
+                   interleaved, q_out)
+    if result is not NotImplemented:
+        return result
     if k.dim() != 3 or (q is not None and q.dim() != 3):
         raise ValueError("q must be [tokens,H,D]; k and v [tokens,Hkv,D]")
     T, Hkv, D = kv_shape = k.shape
     dt, dtype, device = _dtype_code(k), k.dtype, k.device
     if not k.is_cuda:
         raise ValueError("k must be a CUDA tensor")
-    _require(k, "k", kv_shape, dtype, device, False)
-    _require(v, "v", kv_shape, dtype, device, False)
+    index = device.index
+    if not (_is(k, kv_shape, dtype, index) and _is(v, kv_shape, dtype, index)):
+        _require(k, "k", kv_shape, dtype, device, False)
+        _require(v, "v", kv_shape, dtype, device, False)
     H, qs = 0, (0, 0)
     if q is not None:
         H = q.shape[1]
-        _require(q, "q", (T, H, D), dtype, device, False)
+        q_shape = (T, H, D)
+        if not _is(q, q_shape, dtype, index):
+            _require(q, "q", q_shape, dtype, device, False)
         qs = q.stride()
         if q_out is None:
-            q_out = torch.empty((T, H, D), dtype=dtype, device=device)
-        else:
-            _require(q_out, "q_out", (T, H, D), dtype, device)
+            q_out = torch.empty(q_shape, dtype=dtype, device=device)
+        elif not (_is(q_out, q_shape, dtype, index) and q_out.is_contiguous()):
+            _require(q_out, "q_out", q_shape, dtype, device)
     elif q_out is not None:
         raise ValueError("q_out without q")
-    f32, n_pos, R = _check_rope(k, D, q_weight, k_weight, cos_sin)
-    pages, heads, page_size, cache_strides = _check_cache(D, dtype, device, k_cache, v_cache, block_table, seq_lens)
+    f32, n_pos, R = _check_rope(dtype, device, D, q_weight, k_weight, cos_sin)
+    pages, heads, page_size, cache_strides, n_seqs, width = _check_cache(D, dtype, device, k_cache, v_cache, block_table, seq_lens)
     if heads != Hkv:
         raise ValueError("the caches hold %d heads, k has %d" % (heads, Hkv))
-    n_seqs = seq_lens.shape[0]
     if cu_seqlens is not None:
-        _require(cu_seqlens, "cu_seqlens", (n_seqs + 1,), torch.int32, device)
+        if not _is(cu_seqlens, (n_seqs + 1,), torch.int32, index):
+            _require(cu_seqlens, "cu_seqlens", (n_seqs + 1,), torch.int32, device)
     elif T != n_seqs:
         raise ValueError("without cu_seqlens there is one token per sequence: %d tokens, %d sequences" % (T, n_seqs))
     ks, vs = k.stride(), v.stride()
-    _call("attn_paged_append", device, stream, _ptr(q), k.data_ptr(), v.data_ptr(), _Strides[6](qs[0], qs[1], ks[0], ks[1], vs[0], vs[1]),
+    _call("attn_paged_append", device, stream, _ptr(q), k.data_ptr(), v.data_ptr(), _strides(qs[0], qs[1], ks[0], ks[1], vs[0], vs[1]),
           _ptr(q_weight), _ptr(k_weight), f32, _ptr(cos_sin), n_pos, R, bool(interleaved), float(eps), _ptr(q_out), k_cache.data_ptr(),
-          v_cache.data_ptr(), cache_strides, pages, page_size, block_table.data_ptr(), block_table.stride(0), block_table.shape[1],
+          v_cache.data_ptr(), cache_strides, pages, page_size, block_table.data_ptr(), block_table.stride(0), width,
           seq_lens.data_ptr(), _ptr(cu_seqlens), n_seqs, T, H, Hkv, D, dt)
     return q_out
 
@@ -644,16 +723,20 @@ def attn_paged_decode(q, k_cache, v_cache, block_table, seq_lens, scale: float, 
     """Attention of one new token per sequence, q [B,H,D], over a paged cache (see attn_paged_append): keys below seq_lens[b],
     and with window > 0 only the last `window` of them and the first `sinks`.  Returns o [B,H,D] and lse [B,H] (float32).
     `workspace`: CUDA uint8 tensor of at least attn_paged_decode_workspace_bytes(H, Hkv, D) bytes (allocated here when None)."""
+    result = _fast("attn_paged_decode", stream, q, k_cache, v_cache, block_table, seq_lens, scale, window, sinks, out, lse, workspace)
+    if result is not NotImplemented:
+        return result
     if q.dim() != 3:
         raise ValueError("q must be [B,H,D]")
     B, H, D = q_shape = q.shape
     dt, dtype, device = _dtype_code(q), q.dtype, q.device
     if not q.is_cuda:
         raise ValueError("q must be a CUDA tensor")
-    _require(q, "q", q_shape, dtype, device)
-    pages, Hkv, page_size, cache_strides = _check_cache(D, dtype, device, k_cache, v_cache, block_table, seq_lens)
-    if seq_lens.shape[0] != B:
-        raise ValueError("q has %d rows, seq_lens %d" % (B, seq_lens.shape[0]))
+    if not q.is_contiguous():
+        raise ValueError("q must be contiguous")
+    pages, Hkv, page_size, cache_strides, n_seqs, width = _check_cache(D, dtype, device, k_cache, v_cache, block_table, seq_lens)
+    if n_seqs != B:
+        raise ValueError("q has %d rows, seq_lens %d" % (B, n_seqs))
     if out is None:
         out = torch.empty(q_shape, dtype=dtype, device=device)
     else:
@@ -665,7 +748,7 @@ def attn_paged_decode(q, k_cache, v_cache, block_table, seq_lens, scale: float, 
     if workspace is None:
         workspace = torch.empty(max(attn_paged_decode_workspace_bytes(H, Hkv, D), 256), dtype=torch.uint8, device=device)
     _call("attn_paged_decode", device, stream, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), cache_strides, pages, page_size,
-          block_table.data_ptr(), block_table.stride(0), block_table.shape[1], seq_lens.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H,
+          block_table.data_ptr(), block_table.stride(0), width, seq_lens.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H,
           Hkv, D, float(scale), int(window), int(sinks), dt, workspace.data_ptr(), _bytes(workspace))
     return out, lse
 

@@ -12,6 +12,8 @@ LIB_PATH = os.path.join(_HERE, "libattn_fwd.so")
 # entry that makes the producer leave out one K/V load): used by one GPU test to make a wait run out
 # and check the time-out status.  Never loaded by the package.
 WAIT_TEST_LIB_PATH = os.path.join(_HERE, "libattn_fwd_waittest.so")
+# Optional Python extension (see csrc/binding.cpp); without it api.py marshals every call itself.
+BINDING_PATH = os.path.join(_HERE, "_binding.so")
 WAIT_TEST_FLAGS = ["-DATTN_TEST_HOOKS", "-DATTN_TEST_WAIT_LIMIT_NS=1000000ull"]
 
 NVCC_FLAGS = [
@@ -42,8 +44,32 @@ def _compile(path: str, extra, verbose: bool) -> str:
     return path
 
 
+def build_binding(force: bool = False) -> str:
+    """Compile csrc/binding.cpp, the C++ argument marshalling of the latency-bound entry points, against the installed torch."""
+    src = os.path.join(CSRC, "binding.cpp")
+    header = os.path.join(_HERE, "..", "include", "attn_fwd.h")
+    if not force and os.path.exists(BINDING_PATH) and os.path.getmtime(BINDING_PATH) >= max(os.path.getmtime(src), os.path.getmtime(header)):
+        return BINDING_PATH
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    torch_lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cuda = os.environ.get("CUDA_HOME") or cpp_extension.CUDA_HOME or "/usr/local/cuda"
+    tmp = BINDING_PATH + ".tmp.%d" % os.getpid()
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), "-I", sysconfig.get_paths()["include"]]
+    for inc in cpp_extension.include_paths() + [os.path.join(cuda, "include")]:
+        cmd += ["-isystem", inc]
+    cmd += ["-o", tmp, src, "-L", torch_lib, "-Wl,-rpath," + torch_lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    subprocess.check_call(cmd)
+    os.replace(tmp, BINDING_PATH)
+    return BINDING_PATH
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile csrc/attn_api.cu (which includes every kernel header) into libattn_fwd.so."""
+    """Compile csrc/attn_api.cu (which includes every kernel header) into libattn_fwd.so, and the Python extension."""
+    build_binding(force)
     if not force and not is_stale():
         return LIB_PATH
     return _compile(LIB_PATH, [], verbose)

@@ -150,3 +150,16 @@ def test_binding_refuses_wrong_tensors():
         api.attn_paged_decode(torch.zeros(3, 4, 64, dtype=torch.float16), c, c, bt, lens, 0.1)
     with pytest.raises(ValueError):
         api.attn_paged_append(None, torch.zeros(3, 2, 64, dtype=torch.float16), torch.zeros(3, 2, 64, dtype=torch.float16), c, c, bt, lens)
+
+
+def test_extension_is_built_and_refuses_what_is_not_plain():
+    build.build()
+    b = api._bind()
+    assert b is not None
+    x = torch.zeros(1, 8, 4, 64, dtype=torch.float16)
+    # CPU tensors, wrong argument counts and wrong types go back to the Python path, which reports them
+    assert b.attn_fwd_window(x, x, x, 0.1, 4, 0, 0, None, None) is NotImplemented
+    assert b.attn_fwd_window(x, x, x) is NotImplemented
+    assert b.attn_paged_decode(1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11) is NotImplemented
+    with pytest.raises(ValueError):
+        b.bind([1, 2])

@@ -305,3 +305,32 @@ def test_serving_steps_match_attention_over_the_same_tokens():
             assert (want[0, :, -1].float() - o[b].float()).abs().max() <= 2 * 2.0 ** -8 * 5
             assert (wl[0, :, -1] - lse[b]).abs().max() <= 1e-3
     assert api.attn_last_device_status() == 0
+
+
+def test_both_ways_of_marshalling_agree():
+    """Without an explicit stream a plain call is marshalled by the extension, with one by Python: same results, same refusals."""
+    D, dt = 64, torch.bfloat16
+    kc, vc, tab, ks, vs = make_cache([70, 33], 2, D, 16, dt, "slot", 40, dead=0.0)
+    tab, lens = tab.cuda(), torch.tensor([70, 33], dtype=torch.int32).cuda()
+    q = torch.randn(2, 8, D, generator=torch.Generator().manual_seed(1)).to(dt).cuda()
+    here = torch.cuda.current_stream()
+    for extra in ({}, dict(window=20, sinks=3)):
+        a = api.attn_paged_decode(q, kc, vc, tab, lens, 0.125, **extra)
+        b = api.attn_paged_decode(q, kc, vc, tab, lens, 0.125, stream=here, **extra)
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+    for s in (None, here):
+        with pytest.raises(api.AttnError) as err:
+            api.attn_paged_decode(q, kc, vc, tab, lens, float("nan"), stream=s)
+        assert err.value.status == 6
+        with pytest.raises(ValueError):
+            api.attn_paged_decode(q, kc, vc, tab[:1], lens, 0.125, stream=s)
+        with pytest.raises(TypeError):
+            api.attn_paged_decode(q, kc, vc, tab, lens.long(), 0.125, stream=s)
+        with pytest.raises(ValueError):
+            api.attn_paged_decode(q, kc.cpu(), vc, tab, lens, 0.125, stream=s)
+    # outputs given by the caller, one of the wrong shape
+    o, lse = torch.empty_like(q), torch.empty(2, 8, device="cuda")
+    r = api.attn_paged_decode(q, kc, vc, tab, lens, 0.125, out=o, lse=lse)
+    assert r[0].data_ptr() == o.data_ptr() and r[1].data_ptr() == lse.data_ptr()
+    with pytest.raises(ValueError):
+        api.attn_paged_decode(q, kc, vc, tab, lens, 0.125, out=o[:, :4])

@@ -19,6 +19,7 @@
 #include "attn_combine.cuh"
 #include "attn_paged.cuh"
 #include "attn_rope.cuh"
+#include "attn_rope_tma.cuh"
 #include "attn_simt.cuh"
 #include "attn_tc_qtmem.cuh"
 #include "attn_tc_pipe.cuh"

@@ -25,6 +25,8 @@ bool strides_ok(const long long* s, int n) {
 bool head_dim_ok(int D) { return D == 64 || D == 128 || D == 256; }
 bool dtype_ok(int dtype) { return dtype == ATTN_DTYPE_FP16 || dtype == ATTN_DTYPE_BF16; }
 
+constexpr int kRopeBwdBlocks = 148 * attn_rope::kBwdBlocks;   // blocks of the gradient kernel at most: one wave (each leaves D partial sums)
+
 // What the three entry points of the rotation share.
 int validate_rope(const void* q_weight, const void* k_weight, const float* cos_sin, int table_len, int R, float eps, int D, int dtype) {
     if (!head_dim_ok(D)) return ATTN_ERR_UNSUPPORTED_HEAD_DIM;
@@ -55,62 +57,82 @@ int tile_heads_shift(int64_t heads, int D) {
     return s;
 }
 
-// Tensor map over one cache: columns, then the slot, head and page axes by ascending stride; box = 64 columns x `rows` slots,
-// 128-byte swizzle.  `axes` receives the coordinate number of the slot, head and page axis (2 bits each).  A map is a pure
-// function of these arguments; the last ones are kept per thread, as a serving loop passes the same caches in every step.
-struct CacheMapKey {
+// Rank-4 tensor map of 16-bit elements: D contiguous columns, then three axes of n[i] elements at stride[i] (in elements, any
+// order); box[0] columns, box[1 + i] of axis i.  A map is a pure function of these arguments; encoded maps are kept in a small
+// per-thread cache, as a training or serving loop passes the same tensors again (see make_map).
+struct Map4Key {
     const void* base;
-    long long stride[3];
-    int dtype, D, n[3], rows;
-    bool operator==(const CacheMapKey& o) const {
-        return base == o.base && stride[0] == o.stride[0] && stride[1] == o.stride[1] && stride[2] == o.stride[2] && dtype == o.dtype &&
-               D == o.D && n[0] == o.n[0] && n[1] == o.n[1] && n[2] == o.n[2] && rows == o.rows;
+    int64_t stride[3];
+    int dtype, D, n[3], box[4], swizzle;
+    bool operator==(const Map4Key& o) const {
+        bool same = base == o.base && dtype == o.dtype && D == o.D && box[0] == o.box[0] && swizzle == o.swizzle;
+        for (int i = 0; i < 3; ++i) same = same && stride[i] == o.stride[i] && n[i] == o.n[i] && box[1 + i] == o.box[1 + i];
+        return same;
     }
 };
 
-bool make_cache_map(CUtensorMap* map, int* axes, const void* base, const long long* cache_strides, int dtype, int D, int num_pages, int Hkv,
-                    int page_size, int rows) {
+// Strides that a map can have: above 0 (an axis of one element may have any) and, in bytes, below 2^40.
+bool mappable(const int64_t* stride, const int* n) {
+    for (int i = 0; i < 3; ++i)
+        if (n[i] > 1 && (stride[i] <= 0 || stride[i] >= (1LL << 39))) return false;
+    return true;
+}
+
+bool make_map4(CUtensorMap* map, const Map4Key& key) {
     struct Entry {
         bool valid = false;
-        CacheMapKey key;
+        Map4Key key;
         CUtensorMap map;
-        int axes;
     };
-    constexpr int kEntries = 128;     // the caches of 64 layers
+    constexpr int kEntries = 256;
     thread_local Entry cache[kEntries];
-    const CacheMapKey key{base, {cache_strides[2], cache_strides[1], cache_strides[0]}, dtype, D, {page_size, Hkv, num_pages}, rows};
-    Entry& e = cache[((reinterpret_cast<uintptr_t>(base) >> 9) * 0x9E3779B97F4A7C15ull >> 40) % kEntries];
+    const uint64_t h = ((reinterpret_cast<uintptr_t>(key.base) >> 7) + static_cast<uint64_t>(key.stride[0] + 3 * key.stride[1]) * 31 + key.n[0]) *
+                       0x9E3779B97F4A7C15ull;
+    Entry& e = cache[(h >> 40) % kEntries];
     if (!e.valid || !(e.key == key)) {
         EncodeTiledFn enc = get_encode_fn();
         if (!enc) return false;
-        int order[3] = {0, 1, 2};     // slot, head, page
-        for (int i = 0; i < 2; ++i)
-            for (int j = 0; j < 2 - i; ++j)
-                if (key.stride[order[j]] > key.stride[order[j + 1]]) {
-                    const int x = order[j];
-                    order[j] = order[j + 1];
-                    order[j + 1] = x;
-                }
-        cuuint64_t dims[4] = {static_cast<cuuint64_t>(D)}, strides[3];
-        cuuint32_t box[4] = {64}, estr[4] = {1, 1, 1, 1};
-        e.axes = 0;
+        cuuint64_t dims[4] = {static_cast<cuuint64_t>(key.D)}, strides[3];
+        cuuint32_t box[4] = {static_cast<cuuint32_t>(key.box[0])}, estr[4] = {1, 1, 1, 1};
         for (int i = 0; i < 3; ++i) {
-            const int a = order[i];
-            dims[1 + i] = static_cast<cuuint64_t>(key.n[a]);
-            // (an axis of one element may come with any stride, 0 among them: give it one that the encoder accepts)
-            strides[i] = static_cast<cuuint64_t>(key.n[a] > 1 ? key.stride[a] : D) * 2;
-            box[1 + i] = a == 0 ? static_cast<cuuint32_t>(rows) : 1;
-            e.axes |= (i + 1) << (2 * a);
+            dims[1 + i] = static_cast<cuuint64_t>(key.n[i]);
+            strides[i] = static_cast<cuuint64_t>(key.n[i] > 1 ? key.stride[i] : key.D) * 2;
+            box[1 + i] = static_cast<cuuint32_t>(key.box[1 + i]);
         }
-        const CUtensorMapDataType type = dtype == ATTN_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-        e.valid = enc(&e.map, type, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+        const CUtensorMapDataType type = key.dtype == ATTN_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+        e.valid = enc(&e.map, type, 4, const_cast<void*>(key.base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                      key.swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
         if (!e.valid) return false;
         e.key = key;
     }
     *map = e.map;
-    *axes = e.axes;
     return true;
+}
+
+// Map over one cache for the decode kernel: the slot, head and page axes by ascending stride; box = 64 columns x `rows` slots,
+// 128-byte swizzle.  `axes` receives the coordinate number of the slot, head and page axis (2 bits each).
+bool make_cache_map(CUtensorMap* map, int* axes, const void* base, const long long* cache_strides, int dtype, int D, int num_pages, int Hkv,
+                    int page_size, int rows) {
+    const int64_t stride[3] = {cache_strides[2], cache_strides[1], cache_strides[0]};     // slot, head, page
+    const int n[3] = {page_size, Hkv, num_pages};
+    int order[3] = {0, 1, 2};
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2 - i; ++j)
+            if (stride[order[j]] > stride[order[j + 1]]) {
+                const int x = order[j];
+                order[j] = order[j + 1];
+                order[j + 1] = x;
+            }
+    Map4Key key{base, {}, dtype, D, {}, {64, 1, 1, 1}, 1};
+    *axes = 0;
+    for (int i = 0; i < 3; ++i) {
+        key.stride[i] = stride[order[i]];
+        key.n[i] = n[order[i]];
+        if (order[i] == 0) key.box[1 + i] = rows;
+        *axes |= (i + 1) << (2 * order[i]);
+    }
+    return make_map4(map, key);
 }
 
 int log2_of(int x) {
@@ -155,6 +177,52 @@ int launch_rope(attn_rope::RopeParams& p, int D, int dtype, cudaStream_t st) {
     return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;
 }
 
+// The TMA form of the gradient.  *launched false: a stride that a tensor map cannot have (0, for a broadcast input), the caller
+// takes the register form.  p: as for that form.
+int launch_rope_bwd_tma(const attn_rope::RopeParams& p, int B, int D, int dtype, cudaStream_t st, bool* launched, int* ctas) {
+    *launched = false;
+    const int hb = 1024 / D;
+    attn_rope::TmaMaps maps;
+    attn_rope::TmaParams tp = {};
+    tp.r = p;
+    tp.partial = p.partial;
+    tp.token_blocks = (p.S + 7) / 8;
+    for (int i = 0; i < 3; ++i) {
+        tp.units[i] = (p.heads[i] + hb - 1) / hb;
+        if (p.heads[i] == 0) continue;
+        const int n[3] = {p.S, p.heads[i], B};
+        auto make = [&](CUtensorMap* map, const void* base, const attn_rope::Strides& s) {
+            const Map4Key key{base, {s.token, s.head, s.batch}, dtype, D, {n[0], n[1], n[2]}, {D, 8, hb, 1}, 0};
+            return mappable(key.stride, n) && make_map4(map, key);
+        };
+        if (!make(&maps.dy[i], p.dy[i], p.ds[i]) || !make(&maps.out[i], p.out[i], p.os[i])) return ATTN_OK;
+        if (i < 2 && p.weight[i] && !make(&maps.x[i], p.in[i], p.is[i])) return ATTN_OK;
+    }
+    DeviceInfo di;
+    if (device_info(&di) != ATTN_OK) return ATTN_ERR_CUDA;
+    tp.tiles = static_cast<int64_t>(B) * tp.token_blocks * (tp.units[0] + tp.units[1] + tp.units[2]);
+    if (tp.tiles / di.sm_count >= 2147483647LL) return ATTN_OK;
+    int grid = di.sm_count < kRopeBwdBlocks / 2 ? di.sm_count : kRopeBwdBlocks / 2;      // (a CTA leaves 2 D partial sums)
+    if (tp.tiles < grid) grid = static_cast<int>(tp.tiles);
+    *ctas = grid;
+#define ATTN_ROPE_CASE(DD, TT)                                                                                       \
+    if (D == DD && dtype == TT) {                                                                                     \
+        using C = attn_rope::TmaCfg<DD>;                                                                              \
+        auto kern = attn_rope::attn_rope_bwd_tma_kernel<DD, TT>;                                                      \
+        if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), C::SMEM)) return ATTN_ERR_CUDA;                  \
+        kern<<<grid, C::THREADS, C::SMEM, st>>>(maps, tp);                                                            \
+    }
+    ATTN_ROPE_CASE(64, 0)
+    ATTN_ROPE_CASE(64, 1)
+    ATTN_ROPE_CASE(128, 0)
+    ATTN_ROPE_CASE(128, 1)
+    ATTN_ROPE_CASE(256, 0)
+    ATTN_ROPE_CASE(256, 1)
+#undef ATTN_ROPE_CASE
+    *launched = true;
+    return cudaGetLastError() == cudaSuccess ? ATTN_OK : ATTN_ERR_CUDA;
+}
+
 // The row strides of [B, heads, S, D], contiguous.
 attn_rope::Strides head_major(int heads, int S, int D) {
     return attn_rope::Strides{static_cast<int64_t>(heads) * S * D, D, static_cast<int64_t>(S) * D};
@@ -167,7 +235,6 @@ int validate_window(int Sq, int* window, int sinks, int q_offset) {
     return ATTN_OK;
 }
 
-constexpr int kRopeBwdBlocks = 148 * attn_rope::kBwdBlocks;   // blocks of the gradient kernel at most: one wave (each leaves D partial sums)
 
 }  // namespace
 
@@ -326,6 +393,16 @@ int attn_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const 
     p.partial = static_cast<float*>(workspace);
     p.status = cached_status_ptr();
     if (!p.status) return ATTN_ERR_CUDA;
+    bool launched;
+    int ctas;
+    rc = launch_rope_bwd_tma(p, B, D, dtype, st, &launched, &ctas);
+    if (rc != ATTN_OK) return rc;
+    const bool sums = dq_weight || dk_weight;
+    if (launched)
+        return !sums || launch_dependent(attn_rope::attn_rope_weight_grad_kernel, dim3(2 * D / 32), dim3(1024), 0, st, p.partial, ctas,
+                                         p.partial + D, ctas, 2 * D, D, dq_weight, dk_weight)
+                   ? ATTN_OK
+                   : ATTN_ERR_CUDA;
     // blocks of q and of (k, v): by their bytes (a row of q or k is read twice and written, of v read and written), each at
     // least one where it has heads, and no more than it has items
     const int per_unit = attn_rope::kDeep * (256 / D);
@@ -350,9 +427,9 @@ int attn_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const 
     ATTN_ROPE_CASE(256, 1)
 #undef ATTN_ROPE_CASE
     if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
-    if (!dq_weight && !dk_weight) return ATTN_OK;
-    return launch_dependent(attn_rope::attn_rope_weight_grad_kernel, dim3(2 * D / 32), dim3(1024), 0, st, p.partial,
-                            p.q_blocks, static_cast<int>(blocks), D, dq_weight, dk_weight)
+    return !sums || launch_dependent(attn_rope::attn_rope_weight_grad_kernel, dim3(2 * D / 32), dim3(1024), 0, st, p.partial, p.q_blocks,
+                                     p.partial + static_cast<int64_t>(p.q_blocks) * D, static_cast<int>(kv_blocks), D, D, dq_weight,
+                                     dk_weight)
                ? ATTN_OK
                : ATTN_ERR_CUDA;
 }

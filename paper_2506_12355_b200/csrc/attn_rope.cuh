@@ -19,6 +19,8 @@
 #include <cuda_fp16.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "attn_paged.cuh"
 #include "sm100_ptx.cuh"
 
@@ -138,11 +140,37 @@ __device__ __forceinline__ void load_weight(const void* w, int f32, const Place&
 }
 
 // The other value of each pair.
-__device__ __forceinline__ F2 partner(const F2* x, int e, int interleaved) {
-    if (!interleaved) return x[e ^ 2];
-    float lo, hi;
-    x[e].get(lo, hi);
-    return F2(hi, lo);
+template <bool INTER>
+__device__ __forceinline__ F2 partner(const F2* x, int e) {
+    if constexpr (INTER) {
+        float lo, hi;
+        x[e].get(lo, hi);
+        return F2(hi, lo);
+    } else {
+        return x[e ^ 2];
+    }
+}
+
+// The kernels' arithmetic in four forms, chosen once per row group by branches that all threads take alike: neighbouring pairs
+// or not, the whole head rotated or not (then a lane's values may be unrotated, and an unrotated value must not meet a
+// "partner": 0 times infinity is no number).  As run-time selects inside the arithmetic these cost a third of its instructions.
+template <class Work>
+__device__ __forceinline__ void by_form(const RopeParams& p, int D, Work&& work) {
+    if (p.interleaved) {
+        if (p.R == D) work(std::true_type{}, std::true_type{}); else work(std::true_type{}, std::false_type{});
+    } else {
+        if (p.R == D) work(std::false_type{}, std::true_type{}); else work(std::false_type{}, std::false_type{});
+    }
+}
+
+// x turned by (cs, sn)
+template <bool INTER, bool WHOLE>
+__device__ __forceinline__ void turn_values(F2* y, const F2* x, const F2* cs, const F2* sn, bool turns) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        y[e] = x[e] * cs[e];
+        if (WHOLE || turns) y[e] = fma2(partner<INTER>(x, e), sn[e], y[e]);
+    }
 }
 
 // One token's rotation, for the values of a lane: y_e = n_e cs_e + partner_e sn_e.
@@ -258,7 +286,7 @@ attn_rope_kernel(const RopeParams p) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     f.cs[e] = f.cs[e] * w[e];
-                    f.sn[e] = f.sn[e] * partner(w, e, p.interleaved);
+                    f.sn[e] = f.sn[e] * (p.interleaved ? partner<true>(w, e) : partner<false>(w, e));
                 }
             }
         }
@@ -274,29 +302,29 @@ attn_rope_kernel(const RopeParams p) {
                 if (i * RPW < left) raw[i] = load_row(src, at);
                 src += RPW * src_head;
             }
+            if (kind < 2)
+                by_form(p, D, [&](auto inter, auto whole_head) {
+#pragma unroll
+                    for (int i = 0; i < kDeep; ++i) {
+                        if (i * RPW >= left + sub) break;      // uniform over the warp
+                        F2 x[4], y[4];
+                        unpack_row<DTYPE>(raw[i], x);
+                        float r = bad;
+                        if (norm) {
+                            F2 ss = x[0] * x[0];
+#pragma unroll
+                            for (int e = 1; e < 4; ++e) ss = fma2(x[e], x[e], ss);
+                            r *= rsqrtf(row_sum<LPR>(ss.sum()) * (1.f / D) + p.eps);
+                        }
+                        turn_values<decltype(inter)::value, decltype(whole_head)::value>(y, x, f.cs, f.sn, at.turns);
+                        const F2 rr(r, r);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[e] = y[e] * rr;
+                        raw[i] = pack_row<DTYPE>(y);
+                    }
+                });
 #pragma unroll
             for (int i = 0; i < kDeep; ++i) {
-                if (i * RPW >= left + sub) break;      // uniform over the warp
-                if (kind < 2) {
-                    F2 x[4], y[4];
-                    unpack_row<DTYPE>(raw[i], x);
-                    float r = bad;
-                    if (norm) {
-                        F2 ss = x[0] * x[0];
-#pragma unroll
-                        for (int e = 1; e < 4; ++e) ss = fma2(x[e], x[e], ss);
-                        r *= rsqrtf(row_sum<LPR>(ss.sum()) * (1.f / D) + p.eps);
-                    }
-                    const F2 rr(r, r);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        y[e] = x[e] * f.cs[e];
-                        // (an unrotated value must not meet a "partner": 0 times infinity is no number)
-                        if (at.turns) y[e] = fma2(partner(x, e, p.interleaved), f.sn[e], y[e]);
-                        y[e] = y[e] * rr;
-                    }
-                    raw[i] = pack_row<DTYPE>(y);
-                }
                 if (i * RPW < left) store_row(dst, at, raw[i]);
                 dst += RPW * dst_head;
             }
@@ -365,39 +393,39 @@ attn_rope_bwd_kernel(const RopeParams p) {
                     for (int e = 0; e < 4; ++e) turn.cs[e] = F2(__int_as_float(0x7fffffff), __int_as_float(0x7fffffff));
                 }
             }
+            if (kind < 2)
+                by_form(p, D, [&](auto inter, auto whole_head) {
+#pragma unroll
+                    for (int i = 0; i < kDeep; ++i) {
+                        if (i * RPW >= left + sub) break;      // uniform over the warp
+                        F2 g[4], h[4];       // h: g, turned back
+                        unpack_row<DTYPE>(gr[i], g);
+                        turn_values<decltype(inter)::value, decltype(whole_head)::value>(h, g, turn.cs, turn.sn, at.turns);
+                        if (norm) {
+                            F2 x[4], hx[4], ss(0.f, 0.f), gx(0.f, 0.f);
+                            unpack_row<DTYPE>(xr[i], x);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                ss = fma2(x[e], x[e], ss);
+                                hx[e] = h[e] * x[e];
+                                gx = fma2(hx[e], w[e], gx);
+                            }
+                            const float r = rsqrtf(row_sum<LPR>(ss.sum()) * (1.f / D) + p.eps);
+                            const float k = -row_sum<LPR>(gx.sum()) * (1.f / D) * r * r * r;
+                            // (lanes past the last head hold zeros in x and g: at eps 0 their r is infinite)
+                            const float rd = i * RPW < left ? r : 0.f;
+                            const F2 rr(r, r), kk(k, k), rrd(rd, rd);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                dw[e] = fma2(hx[e], rrd, dw[e]);
+                                h[e] = fma2(h[e], w[e] * rr, kk * x[e]);
+                            }
+                        }
+                        gr[i] = pack_row<DTYPE>(h);
+                    }
+                });
 #pragma unroll
             for (int i = 0; i < kDeep; ++i) {
-                if (i * RPW >= left + sub) break;      // uniform over the warp
-                if (kind < 2) {
-                    F2 g[4], h[4];       // h: g, turned back
-                    unpack_row<DTYPE>(gr[i], g);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        h[e] = g[e] * turn.cs[e];
-                        if (at.turns) h[e] = fma2(partner(g, e, p.interleaved), turn.sn[e], h[e]);
-                    }
-                    if (norm) {
-                        F2 x[4], hx[4], ss(0.f, 0.f), gx(0.f, 0.f);
-                        unpack_row<DTYPE>(xr[i], x);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            ss = fma2(x[e], x[e], ss);
-                            hx[e] = h[e] * x[e];
-                            gx = fma2(hx[e], w[e], gx);
-                        }
-                        const float r = rsqrtf(row_sum<LPR>(ss.sum()) * (1.f / D) + p.eps);
-                        const float k = -row_sum<LPR>(gx.sum()) * (1.f / D) * r * r * r;
-                        // (lanes past the last head hold zeros in x and g: at eps 0 their r is infinite)
-                        const float rd = i * RPW < left ? r : 0.f;
-                        const F2 rr(r, r), kk(k, k), rrd(rd, rd);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            dw[e] = fma2(hx[e], rrd, dw[e]);
-                            h[e] = fma2(h[e], w[e] * rr, kk * x[e]);
-                        }
-                    }
-                    gr[i] = pack_row<DTYPE>(h);
-                }
                 if (i * RPW < left) store_row(dst, at, gr[i]);
                 dst += RPW * o_head;
             }
@@ -421,16 +449,20 @@ attn_rope_bwd_kernel(const RopeParams p) {
     }
 }
 
-// dq_weight, dk_weight [D] fp32 from the blocks' sums; 32 columns of one of them per block, 32 warps.
+// dq_weight, dk_weight [D] fp32 from the blocks' sums: q's are nq rows from q_sums, k's nk rows from k_sums, `stride` floats
+// apart.  32 columns of one of them per block, 32 warps.
 __global__ void __launch_bounds__(1024)
-attn_rope_weight_grad_kernel(const float* partial, int q_blocks, int blocks, int D, float* dqw, float* dkw) {
+attn_rope_weight_grad_kernel(const float* q_sums, int nq, const float* k_sums, int nk, int stride, int D, float* dqw, float* dkw) {
     __shared__ float sums[32][33];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const bool is_q = static_cast<int>(blockIdx.x) * 32 < D;
     const int col = blockIdx.x * 32 + lane - (is_q ? 0 : D);
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    const float* from = (is_q ? q_sums : k_sums) + col;
+    const int n = is_q ? nq : nk;
     float x = 0.f;
-    for (int r = (is_q ? 0 : q_blocks) + warp; r < (is_q ? q_blocks : blocks); r += 32) x += __ldcg(partial + static_cast<int64_t>(r) * D + col);
+#pragma unroll 4
+    for (int r = warp; r < n; r += 32) x += __ldcg(from + static_cast<int64_t>(r) * stride);
     sums[warp][lane] = x;
     __syncthreads();
     if (warp == 0) {

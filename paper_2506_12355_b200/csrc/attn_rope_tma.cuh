@@ -1,0 +1,265 @@
+// The gradient of attn_rope.cuh's forward pass with all rows moved by TMA, for dense [B, S, heads, D] tensors.
+//
+// A tile is 8 tokens x 1024 / D heads of one of the three tensors (16 KB, and as much of the forward pass's input beside it), laid
+// out [head][token][D] in shared memory whatever the strides of its source are (the tensor maps order the axes), so that the
+// result is written over it and leaves through another map: the change of layout costs nothing.  One CTA per SM walks a
+// contiguous run of tiles; a ring of 192 KB keeps loads and stores in flight while 16 warps work.  The register form in
+// attn_rope.cuh (a load, arithmetic and a store per warp: 64 KB in flight at most, and only while nobody computes) takes
+// 71 us for 4 x 2048 tokens x 48 heads of 128, this one 58 (4.9 TB/s).  What bounds it now is the issue rate of the arithmetic;
+// two groups of warps on alternate tiles (61 us), two or four rows at a time (78 us and more: fewer warps for their registers)
+// are slower.  For the forward pass, with half the arithmetic and no second operand, this form gains nothing over the registers
+// (71 us either way for 16384 tokens x 48 heads of 128).
+//
+//   warps 0-15  arithmetic: warp w has token w % 8 and every other group of heads; the rotation's factors stay in registers
+//               while the tiles of one token block (all heads of q, then k, then v) pass
+//   warp  16    loads (one lane)
+//   warp  17    stores (one lane); frees a stage once its store has read it
+//
+// Every wait is bounded (see sm100_ptx.cuh).
+#pragma once
+#include <type_traits>
+
+#include "attn_rope.cuh"
+#include "attn_tc_common.cuh"
+
+namespace attn_rope {
+template <int D>
+struct TmaCfg {
+    static constexpr int TB = 8, HB = 1024 / D;
+    static constexpr int TILE = TB * HB * D * 2;
+    static constexpr int STAGE = 2 * TILE;                    // the output's gradient, and the forward pass's input
+    static constexpr int NSTAGE = 196608 / STAGE;
+    static constexpr int WARPS = 16, THREADS = (WARPS + 2) * 32;
+    static constexpr int RPW = 256 / D;                       // rows of a warp at a time
+    static constexpr int SMEM = 128 + NSTAGE * STAGE + 3 * NSTAGE * 8 + 16;
+    static_assert(2 * WARPS * RPW * D * 4 <= NSTAGE * STAGE && SMEM <= 232448, "shared memory (the ring later holds the warps' sums)");
+};
+
+struct TmaParams {
+    RopeParams r;             // heads, weights, table, positions, eps, S, status
+    int units[3];             // groups of 1024 / D heads of q, k, v
+    int token_blocks;         // of 8 tokens, per sequence
+    int64_t tiles;            // (sequence, token block, unit)
+    float* partial;           // [CTA][2][D]: sums of q's and k's weight gradients
+};
+
+struct TmaMaps {
+    CUtensorMap dy[3];        // dq, dk, dv (head-major)
+    CUtensorMap x[2];         // q, k
+    CUtensorMap out[3];
+};
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+        : "memory");
+}
+__device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2, int c3) {
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+                 : "memory");
+}
+
+__device__ __forceinline__ uint4 lds_row(uint32_t row, const Place& at) {
+    uint4 x;
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(row + 2 * at.a) : "memory");
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x.z), "=r"(x.w) : "r"(row + 2 * at.b) : "memory");
+    return x;
+}
+__device__ __forceinline__ void sts_row(uint32_t row, const Place& at, const uint4& x) {
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(row + 2 * at.a), "r"(x.x), "r"(x.y) : "memory");
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(row + 2 * at.b), "r"(x.z), "r"(x.w) : "memory");
+}
+
+// A CTA's walk over its run of tiles.
+struct TileAt {
+    int b, tb, u;             // sequence, token block, unit among those of q, k, v
+    __device__ __forceinline__ void start(const TmaParams& p, int64_t tile, int per_block) {
+        const int64_t block = tile / per_block;
+        u = static_cast<int>(tile - block * per_block);
+        b = static_cast<int>(block / p.token_blocks);
+        tb = static_cast<int>(block - static_cast<int64_t>(b) * p.token_blocks);
+    }
+    // true: the next tile belongs to other tokens
+    __device__ __forceinline__ bool next(const TmaParams& p, int per_block) {
+        if (++u < per_block) return false;
+        u = 0;
+        if (++tb == p.token_blocks) {
+            tb = 0;
+            ++b;
+        }
+        return true;
+    }
+    __device__ __forceinline__ int kind(const TmaParams& p) const { return u < p.units[0] ? 0 : (u < p.units[0] + p.units[1] ? 1 : 2); }
+    __device__ __forceinline__ int head0(const TmaParams& p, int kind, int HB) const {
+        return (u - (kind > 0 ? p.units[0] : 0) - (kind > 1 ? p.units[1] : 0)) * HB;
+    }
+};
+
+template <int D, int DTYPE>
+__global__ void __launch_bounds__(TmaCfg<D>::THREADS, 1)
+attn_rope_bwd_tma_kernel(const __grid_constant__ TmaMaps maps, const __grid_constant__ TmaParams p) {
+    using C = TmaCfg<D>;
+    constexpr int NST = C::NSTAGE, LPR = D / 8, RPW = C::RPW;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (sm100::smem_u32(smem_raw) + 127u) & ~127u;
+    const uint32_t bars = base + NST * C::STAGE;              // full[NST], done[NST], empty[NST]
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_raw + (bars - sm100::smem_u32(smem_raw)) + 3 * NST * 8);
+    auto full = [&](int s) { return bars + 8 * s; };
+    auto done = [&](int s) { return bars + 8 * (NST + s); };
+    auto empty = [&](int s) { return bars + 8 * (2 * NST + s); };
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        *abort_flag = 0;
+        for (int s = 0; s < NST; ++s) {
+            sm100::mbar_init(full(s), 1);
+            sm100::mbar_init(done(s), C::WARPS);
+            sm100::mbar_init(empty(s), 1);
+        }
+        sm100::fence_barrier_init();
+        sm100::fence_proxy_async_smem();
+    }
+    __syncthreads();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int per_block = p.units[0] + p.units[1] + p.units[2];
+    const int64_t first = p.tiles * blockIdx.x / gridDim.x;
+    const int n = static_cast<int>(p.tiles * (blockIdx.x + 1) / gridDim.x - first);
+    TileAt at_tile;
+    at_tile.start(p, first, per_block);
+    F2 dw[2][4];                                              // this lane's part of the weights' gradients
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dw[k][e] = F2(0.f, 0.f);
+
+    if (warp == C::WARPS) {
+        // =========================== loads ===========================
+        if (lane == 0) {
+            for (int i = 0; i < n; ++i) {
+                const int s = i % NST;
+                if (!sm100::mbar_wait(empty(s), ((i / NST) & 1) ^ 1, abort_flag)) break;
+                const int kind = at_tile.kind(p), h0 = at_tile.head0(p, kind, C::HB), t0 = at_tile.tb * C::TB;
+                const bool with_x = kind < 2 && p.r.weight[kind] != nullptr;
+                sm100::mbar_arrive_expect_tx(full(s), with_x ? 2 * C::TILE : C::TILE);
+                tma_load_4d(base + s * C::STAGE, &maps.dy[kind], full(s), 0, t0, h0, at_tile.b);
+                if (with_x) tma_load_4d(base + s * C::STAGE + C::TILE, &maps.x[kind & 1], full(s), 0, t0, h0, at_tile.b);
+                at_tile.next(p, per_block);
+            }
+        }
+    } else if (warp == C::WARPS + 1) {
+        // =========================== stores ===========================
+        if (lane == 0) {
+            constexpr int PENDING = 2;                        // stores that may still be reading their stage
+            bool ok = true;
+            for (int i = 0; i < n; ++i) {
+                const int s = i % NST;
+                if (!(ok = sm100::mbar_wait(done(s), (i / NST) & 1, abort_flag))) break;
+                const int kind = at_tile.kind(p);
+                tma_store_4d(&maps.out[kind], base + s * C::STAGE, 0, at_tile.tb * C::TB, at_tile.head0(p, kind, C::HB), at_tile.b);
+                sm100::tma_store_commit();
+                if (i >= PENDING) {
+                    sm100::tma_store_wait_read<PENDING>();
+                    sm100::mbar_arrive(empty((i - PENDING) % NST));
+                }
+                at_tile.next(p, per_block);
+            }
+            sm100::tma_store_wait_all<0>();                   // shared memory must outlive its readers
+        }
+    } else {
+        // =========================== arithmetic ===========================
+        const int sub = lane / LPR, l = lane % LPR, t_in = warp & 7, half = warp >> 3;
+        const Place at(p.r, l);
+        Turn turn;                                            // of this warp's token
+        F2 w[4];
+        bool new_tokens = true;
+        int my_kind = -1;                                     // tensor whose weights are loaded
+        for (int i = 0; i < n; ++i) {
+            const int s = i % NST, kind = at_tile.kind(p), h0 = at_tile.head0(p, kind, C::HB), token = at_tile.tb * C::TB + t_in;
+            const bool norm = kind < 2 && p.r.weight[kind] != nullptr, live = token < p.r.S;
+            if (kind < 2 && new_tokens && live) {
+                int pos = p.r.positions ? __ldg(p.r.positions + static_cast<int64_t>(at_tile.b) * p.r.S + token) : token;
+                const bool bad = p.r.R > 0 && static_cast<unsigned>(pos) >= static_cast<unsigned>(p.r.table_len);
+                if (bad) {
+                    report_bad_index(p.r.status);
+                    pos = 0;
+                }
+                turn.load(p.r, pos, l, at, true);
+                if (bad) {                                    // the token's gradients, and with them the weights', become NaN
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) turn.cs[e] = F2(__int_as_float(0x7fffffff), __int_as_float(0x7fffffff));
+                }
+                new_tokens = false;
+            }
+            if (norm && kind != my_kind) load_weight<DTYPE>(p.r.weight[kind], p.r.weight_f32, at, w);
+            my_kind = kind;
+            if (!sm100::mbar_wait(full(s), (i / NST) & 1, abort_flag)) break;
+            if (kind < 2 && live) {
+                const int left = p.r.heads[kind] - h0;        // heads of this tile that exist
+                by_form(p.r, D, [&](auto inter, auto whole_head) {
+                    uint32_t row = base + s * C::STAGE + ((half * RPW + sub) * C::TB + t_in) * D * 2;
+#pragma unroll
+                    for (int k = 0; k < C::HB / (2 * RPW); ++k, row += 2 * RPW * C::TB * D * 2) {
+                        const int h = (2 * k + half) * RPW;
+                        if (h >= left) break;                 // uniform over the warp
+                        F2 g[4], y[4];
+                        unpack_row<DTYPE>(lds_row(row, at), g);
+                        turn_values<decltype(inter)::value, decltype(whole_head)::value>(y, g, turn.cs, turn.sn, at.turns);
+                        if (norm) {
+                            F2 x[4], hx[4], ss(0.f, 0.f), gx(0.f, 0.f);
+                            unpack_row<DTYPE>(lds_row(row + C::TILE, at), x);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                ss = fma2(x[e], x[e], ss);
+                                hx[e] = y[e] * x[e];
+                                gx = fma2(hx[e], w[e], gx);
+                            }
+                            const float r = rsqrtf(row_sum<LPR>(ss.sum()) * (1.f / D) + p.r.eps);
+                            const float k3 = -row_sum<LPR>(gx.sum()) * (1.f / D) * r * r * r;
+                            // (rows past the last head hold zeros in x and g: at eps 0 their r is infinite)
+                            const float rd = h + sub < left ? r : 0.f;
+                            const F2 rr(r, r), kk(k3, k3), rrd(rd, rd);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                if (kind == 0) dw[0][e] = fma2(hx[e], rrd, dw[0][e]); else dw[1][e] = fma2(hx[e], rrd, dw[1][e]);
+                                y[e] = fma2(y[e], w[e] * rr, kk * x[e]);
+                            }
+                        }
+                        sts_row(row, at, pack_row<DTYPE>(y));
+                    }
+                });
+                sm100::fence_proxy_async_smem();              // the store reads what was just written
+            }
+            __syncwarp();
+            if (lane == 0) sm100::mbar_arrive(done(s));
+            if (at_tile.next(p, per_block)) new_tokens = true;
+        }
+    }
+    __syncthreads();                                          // loads and stores are over: the ring is free
+    // this CTA's sums of the weight gradients: the warps' side by side, then column by column, always in the same order
+    float* sums = reinterpret_cast<float*>(smem_raw + (base - sm100::smem_u32(smem_raw)));
+    constexpr int ROWS = C::WARPS * RPW;
+    if (warp < C::WARPS) {
+        const int l = lane % LPR;
+        const Place at(p.r, l);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float* mine = sums + (k * ROWS + warp * RPW + lane / LPR) * D;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                dw[k][e].get(mine[at.a + 2 * e], mine[at.a + 2 * e + 1]);
+                dw[k][2 + e].get(mine[at.b + 2 * e], mine[at.b + 2 * e + 1]);
+            }
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * D; i += C::THREADS) {
+        float x = 0.f;
+#pragma unroll 8
+        for (int r = 0; r < ROWS; ++r) x += sums[((i / D) * ROWS + r) * D + i % D];
+        p.partial[static_cast<int64_t>(blockIdx.x) * 2 * D + i] = x;
+    }
+    if (threadIdx.x == 0 && *abort_flag != 0) atomicExch(p.r.status, attn_tc::kStatusTimeout);
+}
+
+}  // namespace attn_rope

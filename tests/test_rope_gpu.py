@@ -226,6 +226,35 @@ def test_gradient_without_weights_and_empty():
     assert (r[3] == 0).all() and (r[4] == 0).all()
 
 
+def test_gradient_of_broadcast_inputs_and_bad_positions():
+    # inputs that stand for every sequence (stride 0), as a tensor map cannot describe them
+    D, B, S, R = 128, 3, 21, 64
+    q, k, _, qw, kw = make(1, S, 4, 2, D, torch.bfloat16, 12)
+    q, k = q.expand(B, -1, -1, -1), k.expand(B, -1, -1, -1)
+    g = torch.Generator().manual_seed(13)
+    dq, dk = (torch.randn(B, h, S, D, generator=g).bfloat16().cuda() for h in (4, 2))
+    tab = table(S, R)
+    res = api.attn_qk_norm_rope_bwd(dq, dk, None, q, k, qw, kw, tab.cuda(), eps=EPS)
+    for got, gw, dy, x, w in ((res[0], res[3], dq, q, qw), (res[1], res[4], dk, k, kw)):
+        want, size, dw, dwsize = grad64(dy.cpu().transpose(1, 2), x.cpu(), w.cpu(), tab[None, :, None], R, False)
+        assert ((got.cpu().double() - want).abs() <= half_step(torch.bfloat16) * want.abs() + 2.0 ** -18 * size).all()
+        assert ((gw.cpu().double() - dw.sum((0, 1, 2))).abs() <= 2.0 ** -16 * dwsize.sum((0, 1, 2))).all()
+    # contiguous ones give the same rows on the other path
+    same = api.attn_qk_norm_rope_bwd(dq, dk, None, q.contiguous(), k.contiguous(), qw, kw, tab.cuda(), eps=EPS)
+    assert (same[0].float() - res[0].float()).abs().max() <= 2 * half_step(torch.bfloat16) * res[0].float().abs().max()
+    for x, y in ((q, k), (q.contiguous(), k.contiguous())):
+        pos = torch.arange(S, dtype=torch.int32).repeat(B, 1)
+        pos[1, 5], pos[2, 0] = S, -3
+        r = api.attn_qk_norm_rope_bwd(dq, dk, None, x, y, qw, kw, tab.cuda(), pos.cuda(), eps=EPS)
+        assert api.attn_last_device_status() == 13 and api.attn_last_device_status() == 0
+        bad = torch.zeros(B, S, dtype=torch.bool)
+        bad[1, 5] = bad[2, 0] = True
+        for t in r[:2]:
+            nan = torch.isnan(t).flatten(2).cpu()
+            assert nan[bad][:, :].any(-1).all() and not nan[~bad].any()
+        assert torch.isnan(r[3]).any() and torch.isnan(r[4]).any()
+
+
 def test_graph_replay_and_second_stream():
     D = 128
     q, k, v, qw, kw = make(1, 70, 4, 2, D, torch.bfloat16, 11)

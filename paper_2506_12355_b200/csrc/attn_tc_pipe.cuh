@@ -107,6 +107,9 @@ struct PipeItem {
     // WINDOW: steps below n_sink are the tiles 0, 1, ..; step i >= n_sink is tile i + shift.  The first of those may lie
     // below Q tile 1's window, which then leaves that step (the hole) out: hole is its number, or -1.
     int n_sink, shift, hole;
+    // One tile of first keys of which at most 32 are visible: its step is a fraction of a usual one (32 score columns, two
+    // products of 16 keys).  16384 queries x 32 heads, window 1024, 4 first keys: 24 us of 292 went to whole steps for them.
+    __device__ __forceinline__ bool short_first(const PipeParams& prm) const { return n_sink == 1 && prm.sinks <= 32; }
     __device__ __forceinline__ int tile_of(int i) const { return i < n_sink ? i : i + shift; }
     __device__ __forceinline__ bool takes(int t, int i) const { return i < nkv(t) && !(t == 1 && i == hole); }
     // steps that Q tile t takes before step i
@@ -406,21 +409,22 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             // =========================== MMA issuer ===========================
             const bool leader = elect_one();
             constexpr uint32_t IDESC_S = make_idesc_f16(BM, BN, FP8 ? 0 : DTYPE, 0, 0);   // format 0 of kind::f8f6f4 is E4M3
+            constexpr uint32_t IDESC_S32 = make_idesc_f16(BM, 32, FP8 ? 0 : DTYPE, 0, 0);          // WINDOW: 32 keys (short_first)
             constexpr uint32_t IDESC_O = make_idesc_f16(BM, D, FP8 ? 0 : DTYPE, 0, 1);
             constexpr uint32_t DESC_HI = smem_desc_hi_sw128(1024);
             const uint32_t q_lo[2] = {smem_desc_lo(sQ(0), 16), smem_desc_lo(sQ(1), 16)};
             const uint32_t k_lo0 = smem_desc_lo(sKV(0), 16);          // K tile in slot 0 (K-major)
             const uint32_t v_lo0 = smem_desc_lo(sKV(0), BN * 128);    // V tile in slot 0 (MN-major)
-            auto issue_s = [&](int t, int s) {   // S_t = Q_t K^T : one instruction per 32 bytes of the head dim
+            auto issue_s = [&](int t, int s, uint32_t idesc) {   // S_t = Q_t K^T : one instruction per 32 bytes of the head dim
                 if (leader) {
                     const uint32_t a0 = q_lo[t], b0 = k_lo0 + s * (C::KV_BYTES >> 4);
 #pragma unroll
                     for (int kk = 0; kk < D / KSTEP; ++kk) {
                         const uint32_t off = ((kk >> 2) * 128 * 128 + (kk & 3) * 32) >> 4;
                         if constexpr (FP8)
-                            mma_f8_ss_lohi(tmem + C::s_col(t), a0 + off, b0 + off, DESC_HI, IDESC_S, kk > 0);
+                            mma_f8_ss_lohi(tmem + C::s_col(t), a0 + off, b0 + off, DESC_HI, idesc, kk > 0);
                         else
-                            mma_f16_ss_lohi(tmem + C::s_col(t), a0 + off, b0 + off, DESC_HI, IDESC_S, kk > 0);
+                            mma_f16_ss_lohi(tmem + C::s_col(t), a0 + off, b0 + off, DESC_HI, idesc, kk > 0);
                     }
                 }
             };
@@ -461,7 +465,7 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                         ok = mbar_wait(bar(B_QFULL + t), uses[t] & 1, abort_flag);
                         if (ok) {
                             tc_fence_after_sync();
-                            issue_s(t, 2 * (kv_base % NGRP) + 1);
+                            issue_s(t, 2 * (kv_base % NGRP) + 1, WINDOW && it.short_first(prm) ? IDESC_S32 : IDESC_S);
                             commit(B_SFULL + t);
                             if (it.nkv(t) == 1) commit(B_QEMPTY + t);
                         }
@@ -482,16 +486,18 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                             // the epilogue of the previous item must have read O_t before it is overwritten
                             if (jt == 0 && uses[t] > 0 && !(ok = mbar_wait(bar(B_OFREE + t), (uses[t] - 1) & 1, abort_flag))) break;
                             tc_fence_after_sync();
-                            issue_pv(t, vslot, jt > 0, 0, 3 * (BN / KSTEP) / 4);
+                            const bool short_step = WINDOW && j == 0 && it.short_first(prm);
+                            if (short_step) issue_pv(t, vslot, false, 0, 32 / KSTEP);
+                            else issue_pv(t, vslot, jt > 0, 0, 3 * (BN / KSTEP) / 4);
                             if (!(ok = mbar_wait(bar(B_PFULL2 + t), par, abort_flag))) break;
                             tc_fence_after_sync();
-                            issue_pv(t, vslot, true, 3 * (BN / KSTEP) / 4, BN / KSTEP);
+                            if (!short_step) issue_pv(t, vslot, true, 3 * (BN / KSTEP) / 4, BN / KSTEP);
                             if (j + 1 == it.nkv(t)) commit(B_OFINAL + t);
                         }
                         if (WINDOW ? it.takes(t, j + 1) : j + 1 < it.nkv(t)) {
                             if (WINDOW && it.before(t, j + 1) == 0 && !(ok = mbar_wait(bar(B_QFULL + t), uses[t] & 1, abort_flag))) break;
                             tc_fence_after_sync();
-                            issue_s(t, kslot);
+                            issue_s(t, kslot, IDESC_S);
                             commit(B_SFULL + t);
                             if (j + 2 == it.nkv(t)) commit(B_QEMPTY + t);   // that was the last S of this item
                         }
@@ -552,6 +558,36 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             for (int j = 0; j < n; ++j) {
                 if (!(ok = mbar_wait(bar(B_SFULL + t), (it_base + j) & 1, abort_flag))) break;
                 tc_fence_after_sync();
+                if constexpr (WINDOW) {
+                    if (j == 0 && it.short_first(prm)) {
+                        // the 32 columns of the first keys, with their exact maximum as the row's first reference
+                        uint32_t s32[32], pk[16];
+                        tmem_ld_32x32b_x32(tS, s32);
+                        tmem_ld_wait();
+                        const uint32_t seen = window_keys(0, row - prm.k_offset, prm.Sk, prm.window, prm.sinks);
+                        float mx = -INFINITY;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (seen & (1u << e)) mx = fmaxf(mx, __uint_as_float(s32[e]));
+                        unset = mx == -INFINITY;
+                        m = unset ? 0.f : mx;
+                        any_unset = __any_sync(0xffffffffu, unset);
+                        const float nmc = -m * c;
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            const float p0 = (seen & (1u << e)) ? ex2_approx(fmaf(__uint_as_float(s32[e]), c, nmc)) : 0.f;
+                            const float p1 = (seen & (2u << e)) ? ex2_approx(fmaf(__uint_as_float(s32[e + 1]), c, nmc)) : 0.f;
+                            l += p0 + p1;
+                            pk[e / 2] = pack2<DTYPE>(p0, p1);
+                        }
+                        store_p(0, pk);
+                        tmem_st_wait();
+                        tc_fence_before_sync();
+                        mbar_arrive(bar(B_PFULL + t));
+                        mbar_arrive(bar(B_PFULL2 + t));
+                        continue;
+                    }
+                }
                 // Visibility of this K/V tile, per warp (rows 32 w .. 32 w + 31 of the Q tile): a chunk of
                 // 32 keys is FULL (every row sees all of it), EMPTY (no row sees any of it) or PARTIAL.
                 const int step = WINDOW && t == 1 && it.hole >= 0 && j >= it.hole ? j + 1 : j;

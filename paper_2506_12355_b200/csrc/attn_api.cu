@@ -732,7 +732,7 @@ int bwd(const void* q, const void* k, const void* v, const void* o, const float*
             !allow_dynamic_smem(reinterpret_cast<const void*>(kkv), CKV::SMEM_BYTES))                                      \
             return ATTN_ERR_CUDA;                                                                                          \
         const int64_t rows = BH * sq_pad;                                                                                  \
-        int64_t blocks = (rows + 7) / 8;                                                                                   \
+        int64_t blocks = (rows + 31) / 32;                                                                                   \
         if (blocks > 148 * 16) blocks = 148 * 16;                                                                          \
         attn_grad::attn_bwd_rows_kernel<DD, TT><<<static_cast<unsigned>(blocks), 256, 0, st>>>(o, dout, lse, nl2, ndelta, Sq, \
                                                                                               prm.Sq_pad, rows);          \

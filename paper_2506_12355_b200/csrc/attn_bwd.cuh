@@ -131,63 +131,70 @@ __device__ __forceinline__ void zero_rows(void* base, int64_t first_row, int row
     for (int i = tid; i < n; i += nthreads) p[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// Per query row, one warp per row: ndelta = -sum_d dO_id * O_id and nl2 = -LSE * log2(e), written with the row
-// stride Sq_pad (padding rows: 0).  `rows` counts padded rows: B * H * Sq_pad.
+// Per query row: ndelta = -sum_d dO_id * O_id and nl2 = -LSE * log2(e), written with the row stride Sq_pad (padding rows: 0).
+// `rows` counts padded rows: B * H * Sq_pad (a multiple of 64).  A warp takes four rows at a time, all of their loads in flight
+// together (one row after the other took 42 us for 32 heads x 8192 rows of 128, four together 24; 134 MB).
 template <int D, int DTYPE>
 __global__ void attn_bwd_rows_kernel(const void* __restrict__ o, const void* __restrict__ dout, const float* __restrict__ lse,
                                      float* __restrict__ nl2, float* __restrict__ ndelta, int Sq, int Sq_pad, int64_t rows) {
+    constexpr int R = 4, W = D / 64;          // rows at a time; 32-bit words of a row per lane
     const int lane = threadIdx.x & 31;
     const int64_t warps = static_cast<int64_t>(gridDim.x) * (blockDim.x >> 5);
-    for (int64_t prow = static_cast<int64_t>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5); prow < rows; prow += warps) {
-        const int64_t bh = prow / Sq_pad;
+    for (int64_t prow = R * (static_cast<int64_t>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5)); prow < rows; prow += R * warps) {
+        const int64_t bh = prow / Sq_pad;      // four rows from a multiple of four lie in one head
         const int i = static_cast<int>(prow - bh * Sq_pad);
-        if (i >= Sq) {
-            if (lane == 0) {
-                nl2[prow] = 0.f;
-                ndelta[prow] = 0.f;
-            }
-            continue;
-        }
         const int64_t row = bh * Sq + i;
-        float acc = 0.f;
-        if constexpr (D == 128) {
-            const uint2 a = reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(o) + row * D * 2)[lane];
-            const uint2 b = reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(dout) + row * D * 2)[lane];
-            const uint32_t aw[2] = {a.x, a.y}, bw[2] = {b.x, b.y};
+        uint32_t a[R][W], b[R][W];
+        float l = 0.f;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float a0, a1, b0, b1;
-                if constexpr (DTYPE == 0) {
-                    const float2 fa = __half22float2(*reinterpret_cast<const __half2*>(&aw[i]));
-                    const float2 fb = __half22float2(*reinterpret_cast<const __half2*>(&bw[i]));
-                    a0 = fa.x; a1 = fa.y; b0 = fb.x; b1 = fb.y;
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+            for (int w = 0; w < W; ++w) a[r][w] = b[r][w] = 0u;
+            if (i + r < Sq) {
+                const uint8_t* pa = static_cast<const uint8_t*>(o) + (row + r) * D * 2;
+                const uint8_t* pb = static_cast<const uint8_t*>(dout) + (row + r) * D * 2;
+                if constexpr (W == 2) {
+                    const uint2 x = reinterpret_cast<const uint2*>(pa)[lane], y = reinterpret_cast<const uint2*>(pb)[lane];
+                    a[r][0] = x.x; a[r][1] = x.y;
+                    b[r][0] = y.x; b[r][1] = y.y;
                 } else {
-                    const float2 fa = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&aw[i]));
-                    const float2 fb = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&bw[i]));
-                    a0 = fa.x; a1 = fa.y; b0 = fb.x; b1 = fb.y;
+                    a[r][0] = reinterpret_cast<const uint32_t*>(pa)[lane];
+                    b[r][0] = reinterpret_cast<const uint32_t*>(pb)[lane];
                 }
-                acc = fmaf(a0, b0, acc);
-                acc = fmaf(a1, b1, acc);
             }
-        } else {
-            const uint32_t a = reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(o) + row * D * 2)[lane];
-            const uint32_t b = reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(dout) + row * D * 2)[lane];
-            float2 fa, fb;
-            if constexpr (DTYPE == 0) {
-                fa = __half22float2(*reinterpret_cast<const __half2*>(&a));
-                fb = __half22float2(*reinterpret_cast<const __half2*>(&b));
-            } else {
-                fa = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&a));
-                fb = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&b));
+        }
+        if (lane < R && i + lane < Sq) l = lse[row + lane];
+        float acc[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            acc[r] = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                float2 fa, fb;
+                if constexpr (DTYPE == 0) {
+                    fa = __half22float2(*reinterpret_cast<const __half2*>(&a[r][w]));
+                    fb = __half22float2(*reinterpret_cast<const __half2*>(&b[r][w]));
+                } else {
+                    fa = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&a[r][w]));
+                    fb = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&b[r][w]));
+                }
+                if constexpr (W == 2) {
+                    acc[r] = fmaf(fa.x, fb.x, acc[r]);
+                    acc[r] = fmaf(fa.y, fb.y, acc[r]);
+                } else {
+                    acc[r] = fmaf(fa.x, fb.x, fa.y * fb.y);
+                }
             }
-            acc = fmaf(fa.x, fb.x, fa.y * fb.y);
         }
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, off);
-        if (lane == 0) {
-            const float l = lse[row];
-            nl2[prow] = (l == -INFINITY) ? -INFINITY : -l * 1.4426950408889634f;
-            ndelta[prow] = -acc;
+        for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+            for (int r = 0; r < R; ++r) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], off);
+        if (lane < R) {
+            const float mine = lane == 0 ? acc[0] : (lane == 1 ? acc[1] : (lane == 2 ? acc[2] : acc[3]));
+            const bool real = i + lane < Sq;
+            nl2[prow + lane] = !real ? 0.f : (l == -INFINITY ? -INFINITY : -l * 1.4426950408889634f);
+            ndelta[prow + lane] = real ? -mine : 0.f;
         }
     }
 }

@@ -545,7 +545,8 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
     p.status = cached_status_ptr();
     if (!p.status) return ATTN_ERR_CUDA;
     const int64_t pairs = static_cast<int64_t>(B) * p.heads;
-    if (pairs > 2147483647LL) return ATTN_ERR_BAD_SHAPE;
+    const int64_t join_blocks = (H + attn_paged::kJoinWarps - 1) / attn_paged::kJoinWarps;
+    if (pairs > 2147483647LL || B * join_blocks > 2147483647LL) return ATTN_ERR_BAD_SHAPE;
     // one CTA per SM, and no more than there can be tiles (16 keys are the smallest tile)
     const int64_t most = pairs * ((static_cast<int64_t>(p.max_len) + 15) / 16 + 2);
     int grid = di.sm_count < attn_paged::kMaxCtas ? di.sm_count : attn_paged::kMaxCtas;
@@ -564,7 +565,8 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
             return ATTN_ERR_CUDA;                                                                                        \
         kern<<<grid, C::THREADS, C::SMEM_BYTES, st>>>(mk, mv, p);                                                        \
         if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;                                                     \
-        return launch_dependent(attn_paged::attn_paged_join_kernel<DD, TT, GG>, dim3(static_cast<unsigned>(pairs)), dim3(512), 0, st, p) \
+        return launch_dependent(attn_paged::attn_paged_join_kernel<DD, TT, GG>, dim3(static_cast<unsigned>(B * join_blocks)), \
+                                dim3(attn_paged::kJoinWarps * 32), 0, st, p, static_cast<int>(join_blocks)) \
                    ? ATTN_OK                                                                                             \
                    : ATTN_ERR_CUDA;                                                                                      \
     }

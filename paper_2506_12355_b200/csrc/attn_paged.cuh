@@ -651,21 +651,23 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
 }
 
 // Joins the partial results of the pairs that more than one CTA of the first kernel worked on, and writes the rows of
-// sequences without a visible key.  One CTA per (sequence, head); the list layout is worked out before the first kernel's
-// results are waited for.  The threads are 16-byte columns of a row x rows x shares of the parts.
+// sequences without a visible key.  A warp per row (sequence and query head), eight rows of one sequence to a block; the
+// list layout is worked out before the first kernel's results are waited for, and after that a row takes two dependent rounds
+// of loads: the parts' exponents and sums, one per lane, then their rows.
+constexpr int kJoinWarps = 8;
 template <int D, int DTYPE, int GH>
-__global__ void __launch_bounds__(512)
-attn_paged_join_kernel(const DecodeParams p) {
+__global__ void __launch_bounds__(kJoinWarps * 32)
+attn_paged_join_kernel(const DecodeParams p, int blocks_per_seq) {
     using C = DecodeCfg<D, GH>;
-    constexpr int NW = C::NW, COLS = D / 4, TEAMS = 512 / COLS;
+    constexpr int NW = C::NW, COLS = D / 4;                // 16-byte columns of a partial row
+    constexpr int TEAMS = COLS >= 32 ? 1 : 32 / COLS, PER = COLS >= 32 ? COLS / 32 : 1;
     constexpr float P_OFF = ExpRange<DTYPE>::P_OFF;
-    __shared__ int64_t red[4][16];
-    __shared__ float wgt[GH][2 * kMaxCtas + 2];
-    __shared__ float4 sums[TEAMS][COLS];
-    const int b = blockIdx.x / p.heads, head = blockIdx.x - b * p.heads;
+    __shared__ int64_t red[4][kJoinWarps];
+    const int b = blockIdx.x / blocks_per_seq;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    int64_t sum4[4] = {0, 0, 0, 0};                   // tiles of the sequences before b and of all, in either form of the list
-    for (int x = tid; x < p.B; x += 512) {
+    const int q_head = (blockIdx.x - b * blocks_per_seq) * kJoinWarps + warp;
+    int64_t sum4[4] = {0, 0, 0, 0};                        // tiles of the sequences before b and of all, in either form of the list
+    for (int x = tid; x < p.B; x += kJoinWarps * 32) {
         const SeqRange r = seq_range<C::CK>(p, x);
         const int n0 = seq_tiles<NW>(r, p.hpt_shift), n1 = seq_tiles<NW>(r, 0);
         sum4[2] += n0;
@@ -685,23 +687,23 @@ attn_paged_join_kernel(const DecodeParams p) {
     for (int f = 0; f < 4; ++f) {
         sum4[f] = 0;
 #pragma unroll
-        for (int w = 0; w < 16; ++w) sum4[f] += red[f][w];
+        for (int w = 0; w < kJoinWarps; ++w) sum4[f] += red[f][w];
     }
     const ListForm form = list_form(p, sum4[2], sum4[3]);
     const int64_t total = form.total;
     const int hs = form.hpt_shift, groups = p.heads >> hs;
     const int64_t before = hs == p.hpt_shift ? sum4[0] : sum4[1];
     const int n = seq_tiles<NW>(seq_range<C::CK>(p, b), hs);
-    // Every CTA waits for the first kernel, also one without work: in a graph this kernel's end stands for both.
+    // Every block waits for the first kernel, also one without work: in a graph this kernel's end stands for both.
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int kvh = head / p.sub, r0 = (head - kvh * p.sub) * 16;
-    const int rows = p.group - r0 < GH ? p.group - r0 : GH;
-    const int64_t row0 = static_cast<int64_t>(b) * p.H + kvh * p.group + r0;
+    if (q_head >= p.H) return;
+    const int kvh = q_head / p.group, in_group = q_head - kvh * p.group, row = in_group & 15;
+    const int head = kvh * p.sub + (in_group >> 4);
+    const int64_t out_row = static_cast<int64_t>(b) * p.H + q_head;
+    uint2* out = reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.o) + out_row * D * 2);
     if (n == 0) {
-        for (int e = tid; e < rows * COLS; e += 512) {
-            reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.o) + row0 * D * 2)[e] = make_uint2(0u, 0u);
-            if (e < rows) p.lse[row0 + e] = -INFINITY;
-        }
+        for (int e = lane; e < COLS; e += 32) out[e] = make_uint2(0u, 0u);
+        if (lane == 0) p.lse[out_row] = -INFINITY;
         return;
     }
     const int hg = head >> hs, hh = head - (hg << hs);
@@ -716,67 +718,67 @@ attn_paged_join_kernel(const DecodeParams p) {
         const int64_t slot = i == 0 ? slot0 : 2 * (c0 + i);
         return p.parts + ((slot << hs) + hh) * C::PART_FLOATS;
     };
-    for (int e = tid; e < rows * np; e += 512) {
-        const int row = e / np, i = e - row * np;
-        const float2 ml = __ldcg(reinterpret_cast<const float2*>(part(i) + GH * D + 2 * row));
-        wgt[row][2 * i] = ml.x;
-        wgt[row][2 * i + 1] = ml.y;
-    }
-    __syncthreads();
-    for (int row = warp; row < rows; row += 16) {    // weights exp2(m_i - max) / sum
-        float mm = -INFINITY;
-        for (int i = lane; i < np; i += 32)
-            if (wgt[row][2 * i + 1] != 0.f) mm = fmaxf(mm, wgt[row][2 * i]);
+    // up to 32 parts at a time: a row of more is joined in rounds, like the rounds of an online softmax
+    float mm = -INFINITY, sum = 0.f;
+    float4 o[PER];
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, off));
-        float sum = 0.f;
-        for (int i = lane; i < np; i += 32) {
-            const float l = wgt[row][2 * i + 1];
-            const float f = l != 0.f ? sm100::ex2_approx(wgt[row][2 * i] - mm) : 0.f;
-            sum = fmaf(f, l, sum);
-            wgt[row][2 * i] = f;
-        }
+    for (int k = 0; k < PER; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int team = TEAMS > 1 ? lane / COLS : 0, col = TEAMS > 1 ? lane % COLS : lane;
+    for (int i0 = 0; i0 < np; i0 += 32) {
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (i0 + lane < np) ml = __ldcg(reinterpret_cast<const float2*>(part(i0 + lane) + GH * D + 2 * row));
+        float mx = ml.y != 0.f ? ml.x : -INFINITY;
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-        const float inv = sum != 0.f ? 1.f / sum : 0.f;
-        for (int i = lane; i < np; i += 32) wgt[row][2 * i] *= inv;
-        if (lane == 0) p.lse[row0 + row] = sum != 0.f ? (mm - P_OFF) * 0.6931471805599453f + logf(sum) : -INFINITY;
-    }
-    __syncthreads();
-    const int team = tid / COLS, col = tid % COLS;
-    int lanes_of_rows = 1;                                   // rows side by side: a power of two, the rest of the teams share parts
-    while (lanes_of_rows < rows && lanes_of_rows < TEAMS) lanes_of_rows <<= 1;
-    const int shares = TEAMS / lanes_of_rows, share = team / lanes_of_rows;
-    for (int rr = 0; rr < rows; rr += lanes_of_rows) {
-        const int row = rr + team % lanes_of_rows;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (row < rows) {
-#pragma unroll 8
-            for (int i = share; i < np; i += shares) {
-                const float f = wgt[row][2 * i];
-                const float4 v = __ldcg(reinterpret_cast<const float4*>(part(i) + row * D) + col);
-                if (f != 0.f) {     // a part without a visible key adds nothing
-                    o.x = fmaf(f, v.x, o.x);
-                    o.y = fmaf(f, v.y, o.y);
-                    o.z = fmaf(f, v.z, o.z);
-                    o.w = fmaf(f, v.w, o.w);
+        for (int off = 16; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+        const float mn = fmaxf(mm, mx);
+        const float keep = mm == -INFINITY ? 0.f : sm100::ex2_approx(mm - mn);
+        const float f = ml.y != 0.f ? sm100::ex2_approx(ml.x - mn) : 0.f;
+        float part_sum = f * ml.y;
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) part_sum += __shfl_xor_sync(0xffffffffu, part_sum, off);
+        sum = fmaf(sum, keep, part_sum);
+        mm = mn;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) { o[k].x *= keep; o[k].y *= keep; o[k].z *= keep; o[k].w *= keep; }
+        const int m = np - i0 < 32 ? np - i0 : 32;
+#pragma unroll 4
+        for (int i = 0; i < m; i += TEAMS) {
+            const int mine = i + team < m ? i + team : m - 1;                // (a weight of 0 below for the repeated one)
+            float w = __shfl_sync(0xffffffffu, f, mine);
+            if (i + team >= m) w = 0.f;
+            const float4* src = reinterpret_cast<const float4*>(part(i0 + mine) + row * D);
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                const float4 v = __ldcg(src + col + 32 * k);
+                if (w != 0.f) {     // a part without a visible key adds nothing
+                    o[k].x = fmaf(w, v.x, o[k].x);
+                    o[k].y = fmaf(w, v.y, o[k].y);
+                    o[k].z = fmaf(w, v.z, o[k].z);
+                    o[k].w = fmaf(w, v.w, o[k].w);
                 }
             }
         }
-        sums[team][col] = o;
-        __syncthreads();
-        if (share == 0 && row < rows) {
-            for (int s = 1; s < shares; ++s) {
-                const float4 v = sums[team + s * lanes_of_rows][col];
-                o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
-            }
-            uint2 w;
-            w.x = sm100::pack2<DTYPE>(o.x, o.y);
-            w.y = sm100::pack2<DTYPE>(o.z, o.w);
-            reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.o) + (row0 + row) * D * 2)[col] = w;
-        }
-        __syncthreads();
     }
+    if constexpr (TEAMS > 1) {
+#pragma unroll
+        for (int off = COLS; off < 32; off <<= 1) {
+            o[0].x += __shfl_xor_sync(0xffffffffu, o[0].x, off);
+            o[0].y += __shfl_xor_sync(0xffffffffu, o[0].y, off);
+            o[0].z += __shfl_xor_sync(0xffffffffu, o[0].z, off);
+            o[0].w += __shfl_xor_sync(0xffffffffu, o[0].w, off);
+        }
+    }
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    if (team == 0) {
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            uint2 w;
+            w.x = sm100::pack2<DTYPE>(o[k].x * inv, o[k].y * inv);
+            w.y = sm100::pack2<DTYPE>(o[k].z * inv, o[k].w * inv);
+            out[col + 32 * k] = w;
+        }
+    }
+    if (lane == 0) p.lse[out_row] = sum != 0.f ? (mm - P_OFF) * 0.6931471805599453f + logf(sum) : -INFINITY;
 }
 
 }  // namespace attn_paged

@@ -358,7 +358,8 @@ int attn_paged_append(const void* q, const void* k, const void* v, const long lo
  *            does not matter (it may be NaN).  num_pages == 0: every key is hidden.
  * workspace: device, 256-byte aligned, at least attn_paged_decode_workspace_bytes(H, Hkv, D) bytes (whatever the lengths are), or
  *            ATTN_ERR_WORKSPACE.  Two calls that may run at the same time need one each.
- * The lengths and the table are read on the device, so a captured call may be replayed with new ones.  The result does
+ * One or two kernels are enqueued.  The lengths and the table are read on the device, so a captured call may be replayed with
+ * new ones.  The result does
  * not depend on timing (no atomics).  The key axis is cut evenly over the GPU whatever the lengths are; the cut depends on
  * all lengths of the batch, so a sequence's result may differ in its last bits when other sequences' lengths change.
  */

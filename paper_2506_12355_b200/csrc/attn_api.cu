@@ -611,6 +611,24 @@ bool launch_dependent(void (*kern)(Params...), dim3 grid, dim3 block, size_t sme
     return cudaLaunchKernelEx(&cfg, kern, Params(args)...) == cudaSuccess;
 }
 
+// A launch in clusters of `size` blocks.
+template <class... Params, class... Args>
+bool launch_cluster(void (*kern)(Params...), dim3 grid, dim3 block, size_t smem, unsigned size, cudaStream_t st, const Args&... args) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = size;
+    attr.val.clusterDim.y = 1;
+    attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, args...) == cudaSuccess;
+}
+
 // How attn_bwd_window cuts the work on the first keys' tiles (BwdParams::n_chunks; a function of the shape alone, because
 // the workspace size follows from it).  Such a tile has the steps of its own window and, for every query behind that, one per
 // 64 rows and query head.  Those are cut so that an item is no longer than a usual tile or than a third of an SM's share

@@ -552,6 +552,10 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
     int grid = di.sm_count < attn_paged::kMaxCtas ? di.sm_count : attn_paged::kMaxCtas;
     if (most < grid) grid = static_cast<int>(most);
     p.grid = grid;
+    // Few pairs whose sequences cannot be long: clusters (see attn_paged.cuh).  At most 16 of 8 CTAs are resident at once, and a
+    // CTA should not have more than 8 tiles while other SMs have none.
+    const int64_t tile_keys = D == 256 ? 4 * 16 : (D == 128 ? 8 * 16 : 8 * 32);
+    p.cluster = pairs <= 16 && p.max_len <= attn_paged::kCluster * 8 * tile_keys ? 1 : 0;
 #define ATTN_DECODE_CASE(DD, TT, GG)                                                                                     \
     if (D == DD && dtype == TT && (p.group <= 8) == (GG == 8)) {                                                         \
         using C = attn_paged::DecodeCfg<DD, GG>;                                                                         \
@@ -563,6 +567,11 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
         if (!make_cache_map(&mk, &p.k_axes, k_cache, cache_strides, TT, DD, num_pages, Hkv, page_size, rows) ||          \
             !make_cache_map(&mv, &p.v_axes, v_cache, cache_strides + 3, TT, DD, num_pages, Hkv, page_size, rows))        \
             return ATTN_ERR_CUDA;                                                                                        \
+        if (p.cluster)                                                                                                   \
+            return launch_cluster(kern, dim3(static_cast<unsigned>(pairs) * attn_paged::kCluster), dim3(C::THREADS), C::SMEM_BYTES, \
+                                  attn_paged::kCluster, st, mk, mv, p)                                                   \
+                       ? ATTN_OK                                                                                         \
+                       : ATTN_ERR_CUDA;                                                                                  \
         kern<<<grid, C::THREADS, C::SMEM_BYTES, st>>>(mk, mv, p);                                                        \
         if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;                                                     \
         return launch_dependent(attn_paged::attn_paged_join_kernel<DD, TT, GG>, dim3(static_cast<unsigned>(B * join_blocks)), \

@@ -14,6 +14,8 @@
 //     contiguous part, whatever the lengths are.  Each CTA lays the list out for itself from the device-side lengths (no
 //     host copy of them, no plan to keep).  A pair inside one CTA's part is finished there; one that is cut by a border
 //     leaves one fp32 partial result per CTA (at most two per CTA), and a second small kernel joins those.
+//   * A few pairs of short sequences (one conversation) are a matter of latency: there a cluster of 8 CTAs takes one pair,
+//     each an eighth of its tiles, and joins the parts through distributed shared memory: one launch, no list to lay out.
 //   * Each warp keeps a ring of its own in shared memory, filled by TMA boxes of up to CK rows x 128 bytes (a box lies in one
 //     page), one mbarrier per stage, and no other synchronisation: 128 to 192 KB per SM are in flight.  Measured at
 //     4 x 65536 keys of 8 heads x 128: per-thread 16-byte copies (cp.async) stop at 4.9 TB/s however deep the ring is, the TMA
@@ -77,7 +79,29 @@ struct DecodeParams {
     int window, sinks;
     float scale_log2;
     int grid;                   // CTAs of the first kernel
+    int cluster;                // 1: a cluster of kCluster CTAs per (sequence, head), no second kernel
 };
+constexpr int kCluster = 8;
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// the same shared-memory address in CTA `rank` of the cluster
+__device__ __forceinline__ uint32_t map_rank(uint32_t addr, int rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+    return v;
+}
 
 // Visible chunks of CK keys of one sequence: n_sink of them from key 0, then those from chunk `lo`.
 struct SeqRange {
@@ -251,6 +275,16 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
+    TileWalk<NW, CK> ld, cu;      // the copies run NSTAGE - 1 tiles ahead of the arithmetic
+    int steps, hs = 0, groups = p.heads;
+    const int rank = static_cast<int>(blockIdx.x) % kCluster;
+    if (p.cluster) {
+        const int pair = static_cast<int>(blockIdx.x) / kCluster, b = pair / p.heads;
+        ld.at(p, 0, b, pair - b * p.heads, 0);
+        ld.t = ld.t_end * rank / kCluster;
+        steps = ld.t_end * (rank + 1) / kCluster - ld.t;
+        if (pair == b * p.heads && rank == 0 && tid == 0 && p.seq_lens[b] > p.max_len) report_bad_index(p.status);
+    } else {
     // ---- lay out the tile list: total tiles, and the pair and tile at which this CTA's part begins ----
     const int per = (p.B + C::THREADS - 1) / C::THREADS;     // consecutive sequences of a thread
     const int b0 = tid * per, b1 = b0 + per < p.B ? b0 + per : p.B;
@@ -284,13 +318,14 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         }
     const ListForm form = list_form(p, total2[0], total2[1]);
     const int64_t total = form.total;
-    const int hs = form.hpt_shift, groups = p.heads >> hs;
+    hs = form.hpt_shift;
+    groups = p.heads >> hs;
     const bool side = hs == p.hpt_shift;
     const int64_t before = side ? before2[0] : before2[1], my_tiles = side ? mine[0] : mine[1];
     const int ctas = cta_count(total, p.grid);
     if (static_cast<int>(blockIdx.x) >= ctas) return;
     const int64_t first = cta_begin(total, blockIdx.x, ctas);
-    const int steps = static_cast<int>(cta_begin(total, blockIdx.x + 1, ctas) - first);
+    steps = static_cast<int>(cta_begin(total, blockIdx.x + 1, ctas) - first);
     // the thread whose sequences hold tile `first` finds it
     if (first >= before * groups && first < (before + my_tiles) * groups) {
         int64_t rem = first - before * groups;
@@ -306,9 +341,10 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         }
     }
     __syncthreads();
-    TileWalk<NW, CK> ld, cu;      // the copies run NSTAGE - 1 tiles ahead of the arithmetic
     ld.at(p, hs, static_cast<int>(scan[32]), static_cast<int>(scan[33]), static_cast<int>(scan[34]));
+    }
     cu = ld;
+    const int own_b = cu.b, own_kvh = cu.kvh, own_r0 = cu.r0;     // of a cluster's pair
     __syncthreads();          // the merge buffer takes over the scan's shared memory
 
     const uint32_t ring = sm100::smem_u32(smem) + warp * C::CHUNK_BYTES, my_bars = bars + 8 * warp * NSTAGE;
@@ -541,7 +577,7 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
             // ---- end of the pair, or of this CTA's part ----
             const bool end_pair = cu.t + 1 == cu.t_end;
             if (end_pair || s + 1 == steps) {
-                const bool whole = end_pair && from_start;
+                const bool whole = end_pair && from_start && !p.cluster;
                 const int hpt = 1 << hs;
                 float* part = p.parts + (2 * static_cast<int64_t>(blockIdx.x) + (n_pairs > 0 ? 1 : 0)) * hpt * C::PART_FLOATS;
 #pragma unroll
@@ -631,7 +667,8 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                             reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.o) + out_row * D * 2)[d4] = w;
                             if (d4 == 0) p.lse[out_row] = sum != 0.f ? (mm - P_OFF) * 0.6931471805599453f + logf(sum) : -INFINITY;
                         } else {
-                            float* dst = part + hh * C::PART_FLOATS;
+                            // (a cluster's parts stay in shared memory, in the ring: every copy into it has been waited for)
+                            float* dst = p.cluster ? reinterpret_cast<float*>(smem) : part + hh * C::PART_FLOATS;
                             *reinterpret_cast<float4*>(dst + row * D + 4 * d4) = o;
                             if (d4 == 0) *reinterpret_cast<float2*>(dst + GH * D + 2 * row) = make_float2(mm, sum);
                         }
@@ -648,6 +685,50 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     }
     __syncthreads();
     if (tid == 0 && *abort_flag != 0) atomicExch(p.status, attn_tc::kStatusTimeout);
+    if (p.cluster) {
+        float* mine = reinterpret_cast<float*>(smem);
+        if (steps == 0)
+            for (int row = tid; row < GH; row += C::THREADS) *reinterpret_cast<float2*>(mine + GH * D + 2 * row) = make_float2(-INFINITY, 0.f);
+        cluster_sync();
+        // row `rank` (and rank + 8) of the pair: this CTA joins it, a thread per 16-byte column
+        const int rows = p.group - own_r0 < GH ? p.group - own_r0 : GH;
+        const uint32_t base = sm100::smem_u32(smem);
+        for (int row = rank; row < rows; row += kCluster) {
+            for (int d4 = tid; d4 < D / 4; d4 += C::THREADS) {
+                float2 ml[kCluster];
+                float4 v[kCluster];
+#pragma unroll
+                for (int k = 0; k < kCluster; ++k) {
+                    const uint32_t from = map_rank(base, k);
+                    ml[k] = ld_cluster2(from + (GH * D + 2 * row) * 4);
+                    v[k] = ld_cluster4(from + (row * D + 4 * d4) * 4);
+                }
+                float mm = -INFINITY, sum = 0.f;
+                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int k = 0; k < kCluster; ++k)
+                    if (ml[k].y != 0.f) mm = fmaxf(mm, ml[k].x);
+#pragma unroll
+                for (int k = 0; k < kCluster; ++k) {
+                    if (ml[k].y == 0.f) continue;        // no key of the pair (its O is not set)
+                    const float f = sm100::ex2_approx(ml[k].x - mm);
+                    sum = fmaf(f, ml[k].y, sum);
+                    o.x = fmaf(f, v[k].x, o.x);
+                    o.y = fmaf(f, v[k].y, o.y);
+                    o.z = fmaf(f, v[k].z, o.z);
+                    o.w = fmaf(f, v[k].w, o.w);
+                }
+                const int64_t out_row = static_cast<int64_t>(own_b) * p.H + own_kvh * p.group + own_r0 + row;
+                const float inv = sum != 0.f ? 1.f / sum : 0.f;
+                uint2 w;
+                w.x = sm100::pack2<DTYPE>(o.x * inv, o.y * inv);
+                w.y = sm100::pack2<DTYPE>(o.z * inv, o.w * inv);
+                reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.o) + out_row * D * 2)[d4] = w;
+                if (d4 == 0) p.lse[out_row] = sum != 0.f ? (mm - P_OFF) * 0.6931471805599453f + logf(sum) : -INFINITY;
+            }
+        }
+        cluster_sync();      // a peer may still read this CTA's part
+    }
 }
 
 // Joins the partial results of the pairs that more than one CTA of the first kernel worked on, and writes the rows of

@@ -132,6 +132,14 @@ def test_decode_window(window, sinks, H, Hkv):
     run_decode(EDGES + [2000], H, Hkv, 64, 16, "bf16", "head", window, sinks, seed=5)
 
 
+@pytest.mark.parametrize("lens", [[1], [0], [16], [129], [1000], [4096], [0, 5], [300, 2000]])
+@pytest.mark.parametrize("H,Hkv,D", [(2, 1, 64), (8, 8, 128), (20, 1, 64), (24, 2, 256), (12, 4, 128)])
+def test_decode_few_pairs(lens, H, Hkv, D):
+    """One or two sequences: few pairs of a sequence and a head, which clusters of CTAs take."""
+    run_decode(lens, H, Hkv, D, 16, "bf16", "slot", seed=6)
+    run_decode(lens, H, Hkv, D, 64, "fp16", "head", window=70, sinks=5, seed=7)
+
+
 def test_decode_zero_scale_and_large_scores():
     run_decode([1, 50, 400], 4, 2, 128, 16, "bf16", "head", scale=0.0, seed=6)
     run_decode([1, 50, 3000], 4, 2, 128, 16, "fp16", "head", scale=3.0, seed=7)    # scores of a hundred and more: the maximum moves

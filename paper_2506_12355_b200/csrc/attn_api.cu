@@ -288,8 +288,10 @@ int launch_tc_pipe(const void* q, const void* k, const void* v, void* o, float* 
     constexpr int PD = DTYPE == ATTN_DTYPE_FP8_E4M3 ? ATTN_FP8_POLY_DEN : (D == 64 ? ATTN_POLY64_DEN : ATTN_POLY_DEN);
     auto kern = n_splits > 1 ? attn_tc::attn_fwd_tc_pipe_kernel<D, DTYPE, PN, PD, !WINDOW> : attn_tc::attn_fwd_tc_pipe_kernel<D, DTYPE, PN, PD, false, WINDOW>;
     if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), C::SMEM_BYTES)) return ATTN_ERR_CUDA;
-    const int64_t BH = static_cast<int64_t>(B) * H;
-    const int64_t n_pairs = (static_cast<int64_t>(Sq) + 2 * C::BM - 1) / (2 * C::BM);
+    int64_t BH = static_cast<int64_t>(B) * H;
+    const bool head_pairs = WINDOW && (H / Hkv) % 2 == 0;
+    const int pair_rows = head_pairs ? C::BM : 2 * C::BM;
+    const int64_t n_pairs = (static_cast<int64_t>(Sq) + pair_rows - 1) / pair_rows;
     if (n_pairs * BH * n_splits > 2147483647LL) return ATTN_ERR_BAD_SHAPE;
     CUtensorMap mq, mk, mv, mo;
     if (!make_map(&mq, q, DTYPE, BH, Sq, D, C::BM) ||
@@ -311,13 +313,15 @@ int launch_tc_pipe(const void* q, const void* k, const void* v, void* o, float* 
     prm.H = H;
     prm.Hkv = Hkv;
     prm.k_offset = k_offset;
+    prm.head_pairs = head_pairs ? 1 : 0;
+    if (head_pairs) BH /= 2;     // from here on: what the items count as heads
     prm.n_pairs = static_cast<int>(n_pairs);
     prm.BH = static_cast<int>(BH);
     // walk together as many heads as keep their K and V (2 * Sk * D * 2 bytes each) inside ~24 MB of L2 (the L2 is split over two dies)
     const int64_t kv_bytes_per_head = 2LL * ES * Sk * D;
     int64_t hpg = (static_cast<int64_t>(ATTN_L2_MB) << 20) / (kv_bytes_per_head > 0 ? kv_bytes_per_head : 1);
     if (hpg < 1) hpg = 1;
-    hpg *= H / Hkv;  // the query heads of one K/V head share its footprint
+    hpg *= H / Hkv / (head_pairs ? 2 : 1);  // the query heads of one K/V head share its footprint
     if (hpg > BH) hpg = BH;
     prm.heads_per_group = static_cast<int>(hpg);
     // under the causal mask the last three groups are merged into one: its items, ordered longest-first, then

@@ -75,6 +75,8 @@ struct PipeParams {
     int k_offset;           // global index of key 0 of this K/V shard (0 for whole problems); enters the causal mask.
                             // Negative: minus the position of query 0
     int window, sinks;      // WINDOW: keys that a query sees up to its own, and first keys that stay visible
+    int head_pairs;         // WINDOW: 1: an item is 128 rows of two neighbouring heads (n_pairs: 128-row tiles; BH and
+                            // heads_per_group count pairs of heads), 0: a pair of Q tiles of one head
     int n_items;            // work items: n_pairs * BH * n_splits, plus one for every item at or beyond halves_from
     int halves_from;        // items from this index on are cut into their two Q tiles (each half a work item of its own,
                             // consecutive indices); INT_MAX: none.  Used when the last wave of a launch of equally long
@@ -124,7 +126,7 @@ __device__ __forceinline__ void pipe_window_steps(const PipeParams& prm, PipeIte
     int lo[2], hi[2];     // window tiles of each Q tile; hi < lo: none
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const int r0 = it.q0 + t * BM, r1 = r0 + BM - 1 < prm.Sq ? r0 + BM - 1 : prm.Sq - 1;
+        const int r0 = it.q0 + (prm.head_pairs ? 0 : t * BM), r1 = r0 + BM - 1 < prm.Sq ? r0 + BM - 1 : prm.Sq - 1;
         const int k0 = r0 + off - prm.window + 1, k1 = r1 + off;
         lo[t] = (k0 > 0 ? k0 : 0) / BN;
         hi[t] = (r0 < prm.Sq && k0 < prm.Sk) ? (k1 < prm.Sk ? k1 : prm.Sk - 1) / BN : -1;
@@ -137,7 +139,7 @@ __device__ __forceinline__ void pipe_window_steps(const PipeParams& prm, PipeIte
     // Q tile 1 without window tiles of its own (it stands behind all keys) still takes those first tiles that the pair walks
     // as Q tile 0's window
     const int own = hi[1] >= lo[1] ? hi[1] - lo[0] + 1 : (any && sink_tiles > lo[0] ? sink_tiles - lo[0] : 0);
-    it.n_kv1 = it.q0 + BM >= prm.Sq ? 0 : it.n_sink + own;
+    it.n_kv1 = !prm.head_pairs && it.q0 + BM >= prm.Sq ? 0 : it.n_sink + own;
     it.hole = (hi[1] >= lo[1] && lo[1] > lo[0] && lo[0] >= sink_tiles) ? it.n_sink : -1;
     if (only_tile == 1) it.n_kv0 = -1;
     if (only_tile == 0) it.n_kv1 = -1;
@@ -165,6 +167,12 @@ __device__ __forceinline__ PipeItem pipe_decode_item(const PipeParams& prm, int 
     it.bh = g * prm.heads_per_group + (r - pr * hg);
     const int pair = prm.causal ? prm.n_pairs - 1 - pr : pr;   // causal: longest rows first
     it.q0 = pair * 2 * BM;
+    if constexpr (WINDOW) {
+        if (prm.head_pairs) {
+            it.bh *= 2;
+            it.q0 = pair * BM;
+        }
+    }
     // grouped-query attention: H / Hkv consecutive query heads read the same K/V head
     it.kv_bh = (it.bh / prm.H) * prm.Hkv + (it.bh % prm.H) / (prm.H / prm.Hkv);
     if constexpr (WINDOW) {
@@ -313,6 +321,9 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         if (hand_back) mbar_arrive(bar(B_SCHEDEMPTY + slot));
         return item;
     };
+    // first row of Q tile t of an item, and its head's distance from the item's
+    auto tile_row = [&](int q0, int t) { return WINDOW && prm.head_pairs ? q0 : q0 + t * BM; };
+    auto tile_head = [&](int t) { return WINDOW && prm.head_pairs ? t : 0; };
 
     if (warp >= 8) {
         reg_dec_service();
@@ -363,7 +374,7 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                         mbar_arrive_expect_tx(bar(B_QFULL + t), C::Q_BYTES);
 #pragma unroll
                         for (int bx = 0; bx < NBOX; ++bx)
-                            tma_load_3d(sQ(t) + bx * BM * 128, &tmQ, bar(B_QFULL + t), bx * C::BOX_COLS, it.q0 + t * BM, it.bh);
+                            tma_load_3d(sQ(t) + bx * BM * 128, &tmQ, bar(B_QFULL + t), bx * C::BOX_COLS, tile_row(it.q0, t), it.bh + tile_head(t));
                     }
                     ++q_uses[t];
                     return true;
@@ -536,12 +547,12 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             if (item < 0) break;
             const int n = WINDOW && it.nkv(t) > 0 ? it.before(t, it.nkv(t)) : it.nkv(t);
             const int q0 = it.q0;
-            const int row = q0 + t * BM + r;
+            const int row = tile_row(q0, t) + r;
             if (n <= 0) {
                 // beyond Sq, or (K/V shards under the causal mask) rows that see no key: O = 0, LSE = -inf;
                 // n < 0: the tile is another work item's
                 if (n == 0 && row < prm.Sq) {
-                    const int64_t grow0 = static_cast<int64_t>(it.o_bh) * prm.Sq + row;
+                    const int64_t grow0 = static_cast<int64_t>(it.o_bh + tile_head(t)) * prm.Sq + row;
                     uint4* orow0 = reinterpret_cast<uint4*>(static_cast<uint8_t*>(prm.o) + grow0 * D * 2);
 #pragma unroll
                     for (int g = 0; g < D / 8; ++g) orow0[g] = make_uint4(0u, 0u, 0u, 0u);
@@ -549,7 +560,7 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                 }
                 continue;
             }
-            const int row_w0 = q0 + t * BM + (warp & 3) * 32;   // first row of this warp
+            const int row_w0 = tile_row(q0, t) + (warp & 3) * 32;   // first row of this warp
             float m = -INFINITY, l = 0.f;
             // WINDOW: a row's first tiles may be hidden from it altogether, so its reference maximum is taken from the first
             // tile that shows it a key (without a window that is always the first tile).
@@ -847,7 +858,7 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             // the 2^-126 floor of the polynomial exponential: they give O = 0, LSE = -inf.
             const bool seen = l > 1e-30f;
             const float inv = seen ? prm.o_scale / l : 0.f;
-            const int64_t grow = static_cast<int64_t>(it.o_bh) * prm.Sq + row;
+            const int64_t grow = static_cast<int64_t>(it.o_bh + tile_head(t)) * prm.Sq + row;
             // O leaves through a swizzled staging tile in shared memory and a TMA store (full-line writes;
             // rows beyond Sq are clipped by the tensor map), 64 columns at a time.
             const uint32_t ost = sOst(t);
@@ -875,7 +886,7 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                 fence_proxy_async_smem();
                 asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory");
                 if (r == 0) {
-                    tma_store_3d(&tmO, ost, h * 64, q0 + t * BM, it.o_bh);
+                    tma_store_3d(&tmO, ost, h * 64, tile_row(q0, t), it.o_bh + tile_head(t));
                     tma_store_commit();
                 }
             }

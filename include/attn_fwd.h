@@ -291,6 +291,7 @@ size_t attn_bwd_window_workspace_bytes(int B, int H, int Hkv, int Sq, int Sk, in
  * positions: device int32 [B][S], or NULL: the token's index s (then S <= table_len).  A position outside
  *            [0, table_len) gives NaN in that token's q and k rows and ATTN_ERR_DEVICE_INDEX in the device status.
  * q_out [B,H,S,D]; k_out, v_out [B,Hkv,S,D]: device, contiguous, 16-byte aligned.
+ * The outputs must not overlap the inputs.
  * D in {64, 128, 256}; H and Hkv are independent.  B * S == 0 is a successful no-op.  Arithmetic in fp32, rounded once.
  */
 int attn_qk_norm_rope(const void* q, const void* k, const void* v, const long long* in_strides, const void* q_weight,
@@ -323,7 +324,8 @@ size_t attn_qk_norm_rope_bwd_workspace_bytes(int D);
 /*
  * Paged key/value cache.  k_cache and v_cache hold num_pages pages of page_size key (value) rows for each of Hkv heads:
  * the row of slot s, head h in page p begins at element p * page + h * head + s * slot of its cache, cache_strides =
- * HOST array {page, head, slot} of k_cache, then of v_cache (elements, multiples of 8; any order of the axes).  Key j of
+ * HOST array {page, head, slot} of k_cache, then of v_cache (elements, multiples of 8, below 2^39 and above 0 wherever the
+ * axis has more than one element; any order of the axes).  Key j of
  * sequence b lies in page block_table[b * table_stride + j / page_size], slot j % page_size.  page_size is a power of
  * two; max_pages * page_size <= 2^31 - 1, max_pages being the entries of a row of block_table (device int32).
  * Entries that no key of a sequence needs are not read; pages may be shared by sequences.

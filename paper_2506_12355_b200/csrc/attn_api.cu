@@ -636,7 +636,8 @@ bool launch_cluster(void (*kern)(Params...), dim3 grid, dim3 block, size_t smem,
 // How attn_bwd_window cuts the work on the first keys' tiles (BwdParams::n_chunks; a function of the shape alone, because
 // the workspace size follows from it).  Such a tile has the steps of its own window and, for every query behind that, one per
 // 64 rows and query head.  Those are cut so that an item is no longer than a usual tile or than a third of an SM's share
-// of the whole pass, whichever is more; where they are fewer than a usual tile's steps they stay with the tile.
+// of the whole pass, whichever is more; where they are no more than that they stay with the tile (as they do when there
+// are hundreds of such tiles: the partial results then never take more than ~180 MB at head dim 128).
 struct SinkPlan {
     int n_tiles = 0, n_chunks = 0;
     size_t part_floats = 0;
@@ -652,9 +653,9 @@ SinkPlan sink_plan(int B, int H, int Hkv, int Sq, int Sk, int D, int window, int
     const int64_t usual = group * ((window_rows + 63) / 64 + 1);
     int64_t last = (Sk < 128 ? Sk : 128) - 1 + static_cast<int64_t>(window) - 1 - q_offset;   // last query of tile 0's window
     int64_t behind = last < 0 ? subs : subs - (last / 64 + 1);
-    if (behind * group <= usual) return s;
     const int64_t all = static_cast<int64_t>(B) * Hkv * (tiles * usual + n_tiles * behind * group);
     const int64_t share = all / (148 * 3), steps = usual > share ? usual : share;
+    if (behind * group <= steps) return s;
     int64_t n = (behind * group + steps - 1) / steps;
     if (n > 64) n = 64;
     s.n_tiles = static_cast<int>(n_tiles);

@@ -512,6 +512,11 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
     int rc = validate_cache(k_cache, v_cache, cache_strides, num_pages, page_size, block_table, max_pages, seq_lens);
     if (rc != ATTN_OK) return rc;
     if (misaligned(q, 16) || misaligned(o, 16) || misaligned(lse, 4)) return ATTN_ERR_MISALIGNED;
+    for (int i = 0; i < 2; ++i) {
+        const int64_t stride[3] = {cache_strides[3 * i], cache_strides[3 * i + 1], cache_strides[3 * i + 2]};
+        const int n[3] = {num_pages, Hkv, page_size};
+        if (!mappable(stride, n)) return ATTN_ERR_BAD_SHAPE;
+    }
     if (!workspace || misaligned(workspace, 256) || workspace_bytes < attn_paged_decode_workspace_bytes(H, Hkv, D)) return ATTN_ERR_WORKSPACE;
     rc = check_arch();
     if (rc != ATTN_OK) return rc;
@@ -519,8 +524,6 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
     if (device_info(&di) != ATTN_OK) return ATTN_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (num_pages == 0) return fill_empty(o, lse, static_cast<int64_t>(B) * H * D, static_cast<int64_t>(B) * H, st);
-    for (int i = 0; i < 6; ++i)
-        if (cache_strides[i] < 0 || cache_strides[i] >= (1LL << 39)) return ATTN_ERR_BAD_SHAPE;
     attn_paged::DecodeParams p = {};
     p.q = q;
     p.o = o;

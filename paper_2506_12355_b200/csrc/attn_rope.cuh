@@ -251,14 +251,35 @@ attn_rope_kernel(const RopeParams p) {
     const int token = blockIdx.x * kWarps + warp;
     if (token >= p.tokens) return;
     int b = 0, s = token;
+    if constexpr (!PAGED) {
+        b = static_cast<unsigned>(token) / static_cast<unsigned>(p.S);
+        s = token - b * p.S;
+    }
+    const Place at(p, l);
+    int u = blockIdx.y;
+    // The rows of unit u: asked for before the position, the page and the rotation's factors, whose loads depend on one another.
+    uint4 raw[kDeep];
+    int left;                    // this lane's rows are those i with i * RPW < left
+    auto load_unit = [&](int kind) {
+        const int h0 = (u - (kind == 0 ? 0 : p.unit_end[kind - 1])) * (kDeep * RPW);
+        left = p.heads[kind] - h0 - sub;
+        const int64_t head = p.is[kind].head * 2;
+        const uint8_t* src = static_cast<const uint8_t*>(p.in[kind]) + (b * p.is[kind].batch + s * p.is[kind].token) * 2 + (h0 + sub) * head;
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) {
+            raw[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (i * RPW < left) raw[i] = load_row(src, at);
+            src += RPW * head;
+        }
+    };
+    load_unit(u < p.unit_end[0] ? 0 : (u < p.unit_end[1] ? 1 : 2));
+    bool loaded = true;
     int pos, page = 0, slot = 0;
     float bad = 1.f;             // NaN: the token's q and k rows become NaN
     if constexpr (PAGED) {
         pos = place_token(p, token, page, slot);
         if (pos < 0) return;
     } else {
-        b = static_cast<unsigned>(token) / static_cast<unsigned>(p.S);
-        s = token - b * p.S;
         pos = p.positions ? __ldg(p.positions + token) : s;
         if (p.R > 0 && static_cast<unsigned>(pos) >= static_cast<unsigned>(p.table_len)) {
             report_bad_index(p.status);
@@ -266,15 +287,12 @@ attn_rope_kernel(const RopeParams p) {
             pos = 0;
         }
     }
-    const Place at(p, l);
-    int u = blockIdx.y;
 #pragma unroll
     for (int kind = 0; kind < 3; ++kind) {
         if (u >= p.unit_end[kind]) continue;
-        const int heads = p.heads[kind], first_unit = kind == 0 ? 0 : p.unit_end[kind - 1];
+        if (!loaded) load_unit(kind);
         const bool cache = PAGED && kind > 0, norm = kind < 2 && p.weight[kind] != nullptr;
-        const int64_t src_head = p.is[kind].head * 2, dst_head = p.os[kind].head * 2;
-        const uint8_t* src0 = static_cast<const uint8_t*>(p.in[kind]) + (b * p.is[kind].batch + s * p.is[kind].token) * 2 + sub * src_head;
+        const int64_t dst_head = p.os[kind].head * 2;
         uint8_t* dst0 = static_cast<uint8_t*>(p.out[kind]) + sub * dst_head +
                         (cache ? page * p.os[kind].batch + slot * p.os[kind].token : b * p.os[kind].batch + s * p.os[kind].token) * 2;
         Turn f;                  // the rotation with the weights folded in
@@ -290,18 +308,7 @@ attn_rope_kernel(const RopeParams p) {
                 }
             }
         }
-        for (; u < p.unit_end[kind]; u += gridDim.y) {
-            const int h0 = (u - first_unit) * (kDeep * RPW);
-            const int left = heads - h0 - sub;          // this lane's rows are those i with i * RPW < left
-            const uint8_t* src = src0 + h0 * src_head;
-            uint8_t* dst = dst0 + h0 * dst_head;
-            uint4 raw[kDeep];
-#pragma unroll
-            for (int i = 0; i < kDeep; ++i) {
-                raw[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (i * RPW < left) raw[i] = load_row(src, at);
-                src += RPW * src_head;
-            }
+        for (;;) {
             if (kind < 2)
                 by_form(p, D, [&](auto inter, auto whole_head) {
 #pragma unroll
@@ -323,12 +330,17 @@ attn_rope_kernel(const RopeParams p) {
                         raw[i] = pack_row<DTYPE>(y);
                     }
                 });
+            uint8_t* dst = dst0 + (u - (kind == 0 ? 0 : p.unit_end[kind - 1])) * (kDeep * RPW) * dst_head;
 #pragma unroll
             for (int i = 0; i < kDeep; ++i) {
                 if (i * RPW < left) store_row(dst, at, raw[i]);
                 dst += RPW * dst_head;
             }
+            u += gridDim.y;
+            if (u >= p.unit_end[kind]) break;
+            load_unit(kind);
         }
+        loaded = false;
     }
 }
 

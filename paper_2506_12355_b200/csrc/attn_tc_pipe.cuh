@@ -29,7 +29,10 @@
 //
 // Sliding window (WINDOW = true): query i at position p = i + q_offset sees key j iff j <= p and (j > p - window or
 // j < sinks).  The steps of an item are then the tiles of the first tokens and a run of tiles from the window's lower
-// edge; the rest of the loop is the same.  What changes inside it is noted at the places.
+// edge; the rest of the loop is the same.  What changes inside it is noted at the places.  Where each K/V head has an even number
+// of query heads, the two Q tiles of an item are the same rows of two neighbouring heads: they see the same keys, so every
+// step works for both (two tiles of one head each leave out a step at one end, and a step for one tile takes 83 % of the
+// time of one for two; 16384 queries x 32 heads over 8, window 1024 + 4 first keys: 282 -> 273 us).
 //
 // 8-bit inputs (the FP8 case study of Section 4.4): the same kernel with E4M3 tiles of half the size,
 // kind::f8f6f4 MMAs and P written back as E4M3, four values per tensor-memory column; see the

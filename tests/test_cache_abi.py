@@ -83,6 +83,12 @@ def test_window_validation(lib):
     for name in ("dout", "dq", "dk", "dv"):
         assert b(**{name: None}) == 1
     assert b(ws=None) == 10 and b(ws_n=64) == 10
+    # partial sums of the first keys' gradients: none without such keys, and bounded when all keys are first keys
+    plain = lib.attn_bwd_workspace_bytes(1, 32, 16384)
+    assert lib.attn_bwd_window_workspace_bytes(1, 32, 8, 16384, 16384, 128, 1024, 0, 0) == plain
+    assert 0 < lib.attn_bwd_window_workspace_bytes(1, 32, 8, 16384, 16384, 128, 1024, 4, 0) - plain < 200 << 20
+    for s in (128, 500, 2000, 5000, 16384, 2 ** 31 - 1):
+        assert lib.attn_bwd_window_workspace_bytes(1, 32, 8, 16384, 16384, 128, 64, s, 0) - plain < 200 << 20
     assert lib.attn_bwd_window_workspace_bytes(1, 2, 2, 100, 100, 64, 10, 0, 0) >= lib.attn_bwd_workspace_bytes(1, 2, 100)
     assert lib.attn_bwd_window_workspace_bytes(-1, 2, 2, 100, 100, 64, 10, 0, 0) == 0
 
@@ -125,6 +131,8 @@ def test_decode_validation(lib):
         assert f(**{name: None}) == 1, name
     assert f(B=-1) == 2 and f(Hkv=3) == 2 and f(window=-1) == 2 and f(sinks=-1) == 2 and f(page=12) == 2 and f(mp=-1) == 2
     assert f(D=96) == 3 and f(dtype=2) == 4 and f(q=0x1008) == 5 and f(lse=0x3002) == 5
+    for cs in (ll(0, 1024, 64, 2048, 1024, 64), ll(2048, 1024, 64, 2048, 0, 64), ll(2048, -1024, 64, 2048, 1024, 64), ll(1 << 39, 1024, 64, 2048, 1024, 64)):
+        assert f(cs=cs) == 2                                              # strides that the copies cannot take
     assert f(scale=float("nan")) == 6 and f(scale=-1.0) == 6
     assert f(ws=None) == 10 and f(ws=0x10010) == 10 and f(ws_n=100) == 10
     assert f(B=0) == 0 and f(H=0, Hkv=0) == 0

@@ -126,6 +126,33 @@ def test_decode_length_mixes(lens):
     run_decode(lens, 4, 2, 128 if sum(lens) < 20000 else 64, 16, "fp16", "slot", seed=4)
 
 
+@pytest.mark.parametrize("H,Hkv,D,kind", [(8, 8, 64, "fp16"), (32, 8, 128, "bf16"), (48, 16, 64, "bf16"), (64, 4, 128, "fp16"),
+                                          (160, 8, 128, "bf16"), (8, 4, 256, "fp16"), (24, 24, 128, "fp16"), (6, 6, 64, "bf16")])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (700, 5)])
+def test_decode_long_lists(H, Hkv, D, kind, window, sinks):
+    """Enough tiles that the warps of a CTA take different heads: all of them where 8 (D = 256: 4) divide the heads, some or none."""
+    g = torch.Generator().manual_seed(3)
+    lens = torch.randint(0, 2000, (24,), generator=g).tolist() + [1, 16, 0, 2500]
+    run_decode(lens, H, Hkv, D, 16, kind, "slot", window, sinks, seed=13)
+
+
+def test_decode_padded_and_interleaved_caches():
+    """Views of larger buffers: padded pages, K and V side by side in one row, a head axis outside the pages."""
+    dt, D, Hkv, page, lens = torch.float16, 64, 3, 8, [77, 5, 300]
+    kc, vc, tab, ks, vs = make_cache(lens, Hkv, D, page, dt, "head", 14)
+    q = torch.randn(3, 6, D, generator=torch.Generator().manual_seed(4)).to(dt).cuda()
+    tab, len_t, n = tab.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), kc.shape[0]
+    nan = lambda *s: torch.full(s, float("nan"), dtype=dt, device="cuda")
+    padded = nan(n, Hkv, page + 3, D + 8)[:, :, :page, :D], nan(n, Hkv + 1, page, D)[:, :Hkv]
+    side = nan(n, page, Hkv, 2 * D).transpose(1, 2)
+    heads_first = nan(Hkv, n, page, D).transpose(0, 1), nan(Hkv, page, n, D).permute(2, 0, 1, 3)
+    for k, v in (padded, (side[..., :D], side[..., D:]), heads_first):
+        k.copy_(kc)
+        v.copy_(vc)
+        o, lse = api.attn_paged_decode(q, k, v, tab, len_t, 0.125)
+        check_decode(o, lse, q, ks, vs, 0.125, 0, 0, dt)
+
+
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (16, 4), (100, 0), (100, 33), (130, 200), (999, 1), (100000, 4)])
 @pytest.mark.parametrize("H,Hkv", [(4, 2), (12, 1)])
 def test_decode_window(window, sinks, H, Hkv):
@@ -194,10 +221,11 @@ def test_decode_offsets_beyond_32_bits():
     assert torch.equal(kc[pages - 1, :, 6].cpu(), k[0]) and torch.equal(vc[pages - 1, :, 6].cpu(), v[0])
 
 
-def test_decode_graph_with_new_lengths_and_two_streams():
-    D, page, dt, lens = 128, 16, torch.bfloat16, [300, 5, 0, 900]
-    kc, vc, tab, ks, vs = make_cache([900] * 4, 2, D, page, dt, "head", 11)
-    q = torch.randn(4, 8, D, generator=torch.Generator().manual_seed(2)).to(dt).cuda()
+@pytest.mark.parametrize("times", [1, 9])      # few pairs (clusters), many (a list of tiles, two kernels)
+def test_decode_graph_with_new_lengths_and_two_streams(times):
+    D, page, dt, lens = 128, 16, torch.bfloat16, [300, 5, 0, 900] * times
+    kc, vc, tab, ks, vs = make_cache([900] * len(lens), 2, D, page, dt, "head", 11)
+    q = torch.randn(len(lens), 8, D, generator=torch.Generator().manual_seed(2)).to(dt).cuda()
     tab, len_t = tab.cuda(), torch.tensor(lens, dtype=torch.int32).cuda()
     ws = [torch.empty(api.attn_paged_decode_workspace_bytes(8, 2, D), dtype=torch.uint8, device="cuda") for _ in range(2)]
     api.attn_paged_decode(q, kc, vc, tab, len_t, 0.1, workspace=ws[0])
@@ -206,6 +234,7 @@ def test_decode_graph_with_new_lengths_and_two_streams():
         o, lse = api.attn_paged_decode(q, kc, vc, tab, len_t, 0.1, workspace=ws[0])
     side = torch.cuda.Stream()
     for new in ([300, 5, 0, 900], [1, 900, 899, 17], [0, 0, 0, 0], [900, 900, 900, 900]):
+        new = new * times
         len_t.copy_(torch.tensor(new, dtype=torch.int32))
         torch.cuda.synchronize()
         graph.replay()

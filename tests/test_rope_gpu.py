@@ -186,6 +186,25 @@ def test_gradient(B, S, H, Hkv, D, R, inter, kind):
     assert all(torch.equal(a, b) for a, b in zip(res, again))     # the sums' order is fixed
 
 
+def test_other_input_layouts():
+    """Head-major inputs, and rows with room between them."""
+    D, R, dt = 128, 64, torch.float16
+    g = torch.Generator().manual_seed(15)
+    q = torch.randn(2, 5, 40, D, generator=g).to(dt).cuda().transpose(1, 2)                  # [B,S,H,D] over [B,H,S,D]
+    k = torch.randn(2, 40, 3, D + 24, generator=g).to(dt).cuda()[..., 8:8 + D]
+    qw, kw = (1 + 0.2 * torch.randn(2, D, generator=g)).to(dt).cuda()
+    tab = table(40, R)
+    qo, ko, _ = api.attn_qk_norm_rope(q, k, None, qw, kw, tab.cuda(), eps=EPS)
+    dq, dk = torch.randn(2, 5, 40, D, generator=g).to(dt).cuda(), torch.randn(2, 3, 40, D, generator=g).to(dt).cuda()
+    di = torch.empty(2, 5, 40, D, dtype=dt, device="cuda").transpose(1, 2)
+    res = api.attn_qk_norm_rope_bwd(dq, dk, None, q, k, qw, kw, tab.cuda(), eps=EPS, dq_in=di)
+    for out, x, w, got, dy in ((qo, q, qw, di, dq), (ko, k, kw, res[1], dk)):
+        want, size = rows64(x.cpu(), w.cpu(), tab[None, :, None], R, False)
+        check_rows(out.cpu().transpose(1, 2), want, size, dt, "rows")
+        want, size, _, _ = grad64(dy.cpu().transpose(1, 2), x.cpu(), w.cpu(), tab[None, :, None], R, False)
+        assert ((got.cpu().double() - want).abs() <= half_step(dt) * want.abs() + 2.0 ** -18 * size + 2.0 ** -25).all()
+
+
 def test_gradient_against_differences():
     # central differences of sum(y * g) in 64 bits, at points of the 16-bit grid, against the kernel's gradient
     D, R = 64, 32

@@ -284,8 +284,9 @@ int launch_tc_pipe(const void* q, const void* k, const void* v, void* o, float* 
     using C = attn_tc::PipeCfg<D, ES>;
     // share of the exponentials evaluated by the polynomial (measured best): 1 pair in 8 at head dim 128, 1 in 4 at
     // head dim 64, where the tensor core leaves more issue slots to the softmax warps
-    constexpr int PN = DTYPE == ATTN_DTYPE_FP8_E4M3 ? ATTN_FP8_POLY_NUM : (D == 64 ? ATTN_POLY64_NUM : ATTN_POLY_NUM);
-    constexpr int PD = DTYPE == ATTN_DTYPE_FP8_E4M3 ? ATTN_FP8_POLY_DEN : (D == 64 ? ATTN_POLY64_DEN : ATTN_POLY_DEN);
+    // (none under a window: with a handful of keys per row the polynomial's 7.5e-5 would stand in the LSE as it is)
+    constexpr int PN = WINDOW ? 0 : DTYPE == ATTN_DTYPE_FP8_E4M3 ? ATTN_FP8_POLY_NUM : (D == 64 ? ATTN_POLY64_NUM : ATTN_POLY_NUM);
+    constexpr int PD = WINDOW ? 1 : DTYPE == ATTN_DTYPE_FP8_E4M3 ? ATTN_FP8_POLY_DEN : (D == 64 ? ATTN_POLY64_DEN : ATTN_POLY_DEN);
     auto kern = n_splits > 1 ? attn_tc::attn_fwd_tc_pipe_kernel<D, DTYPE, PN, PD, !WINDOW> : attn_tc::attn_fwd_tc_pipe_kernel<D, DTYPE, PN, PD, false, WINDOW>;
     if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), C::SMEM_BYTES)) return ATTN_ERR_CUDA;
     int64_t BH = static_cast<int64_t>(B) * H;
@@ -757,8 +758,8 @@ int bwd(const void* q, const void* k, const void* v, const void* o, const float*
         const int64_t rows = BH * sq_pad;                                                                                  \
         int64_t blocks = (rows + 31) / 32;                                                                                   \
         if (blocks > 148 * 16) blocks = 148 * 16;                                                                          \
-        attn_grad::attn_bwd_rows_kernel<DD, TT><<<static_cast<unsigned>(blocks), 256, 0, st>>>(o, dout, lse, nl2, ndelta, Sq, \
-                                                                                              prm.Sq_pad, rows);          \
+        attn_grad::attn_bwd_rows_kernel<DD, TT, WINDOW><<<static_cast<unsigned>(blocks), 256, 0, st>>>(o, dout, lse, nl2, ndelta, Sq, \
+                                                                                              prm.Sq_pad, rows, q, k, v, prm); \
         prm.out0 = dq;                                                                                                     \
         prm.out1 = nullptr;                                                                                                \
         prm.n_tiles_total = static_cast<int>(n_qtiles * BH);                                                               \

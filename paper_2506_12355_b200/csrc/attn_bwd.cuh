@@ -134,9 +134,36 @@ __device__ __forceinline__ void zero_rows(void* base, int64_t first_row, int row
 // Per query row: ndelta = -sum_d dO_id * O_id and nl2 = -LSE * log2(e), written with the row stride Sq_pad (padding rows: 0).
 // `rows` counts padded rows: B * H * Sq_pad (a multiple of 64).  A warp takes four rows at a time, all of their loads in flight
 // together (one row after the other took 42 us for 32 heads x 8192 rows of 128, four together 24; 134 MB).
-template <int D, int DTYPE>
+//
+// WINDOW: rows that see few keys take delta = sum_j P_ij dP_ij from the keys themselves.  With O rounded to 16 bits
+// delta is off by about u / sqrt(n - 1) of dQ's and dK's size (u: one rounding, n keys), beside the roundings of dS and of the
+// result: 1.73 instead of 1.41 u for two keys.  From n = 9 on it is below 1.46.
+constexpr int kFewKeys = 8;
+
+template <int DTYPE>
+__device__ __forceinline__ float2 widen2(uint32_t x) {
+    if constexpr (DTYPE == 0) return __half22float2(*reinterpret_cast<const __half2*>(&x));
+    else return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x));
+}
+
+// a lane's share of a row of D 16-bit values
+template <int W>
+__device__ __forceinline__ void load_words(const void* base, int64_t row, int lane, uint32_t* x) {
+    const uint8_t* p = static_cast<const uint8_t*>(base) + row * W * 128;
+    if constexpr (W == 2) {
+        const uint2 u = reinterpret_cast<const uint2*>(p)[lane];
+        x[0] = u.x;
+        x[1] = u.y;
+    } else {
+        x[0] = reinterpret_cast<const uint32_t*>(p)[lane];
+    }
+}
+
+template <int D, int DTYPE, bool WINDOW>
 __global__ void attn_bwd_rows_kernel(const void* __restrict__ o, const void* __restrict__ dout, const float* __restrict__ lse,
-                                     float* __restrict__ nl2, float* __restrict__ ndelta, int Sq, int Sq_pad, int64_t rows) {
+                                     float* __restrict__ nl2, float* __restrict__ ndelta, int Sq, int Sq_pad, int64_t rows,
+                                     const void* __restrict__ q, const void* __restrict__ k, const void* __restrict__ v,
+                                     const BwdParams prm) {
     constexpr int R = 4, W = D / 64;          // rows at a time; 32-bit words of a row per lane
     const int lane = threadIdx.x & 31;
     const int64_t warps = static_cast<int64_t>(gridDim.x) * (blockDim.x >> 5);
@@ -151,16 +178,8 @@ __global__ void attn_bwd_rows_kernel(const void* __restrict__ o, const void* __r
 #pragma unroll
             for (int w = 0; w < W; ++w) a[r][w] = b[r][w] = 0u;
             if (i + r < Sq) {
-                const uint8_t* pa = static_cast<const uint8_t*>(o) + (row + r) * D * 2;
-                const uint8_t* pb = static_cast<const uint8_t*>(dout) + (row + r) * D * 2;
-                if constexpr (W == 2) {
-                    const uint2 x = reinterpret_cast<const uint2*>(pa)[lane], y = reinterpret_cast<const uint2*>(pb)[lane];
-                    a[r][0] = x.x; a[r][1] = x.y;
-                    b[r][0] = y.x; b[r][1] = y.y;
-                } else {
-                    a[r][0] = reinterpret_cast<const uint32_t*>(pa)[lane];
-                    b[r][0] = reinterpret_cast<const uint32_t*>(pb)[lane];
-                }
+                load_words<W>(o, row + r, lane, a[r]);
+                load_words<W>(dout, row + r, lane, b[r]);
             }
         }
         if (lane < R && i + lane < Sq) l = lse[row + lane];
@@ -170,14 +189,7 @@ __global__ void attn_bwd_rows_kernel(const void* __restrict__ o, const void* __r
             acc[r] = 0.f;
 #pragma unroll
             for (int w = 0; w < W; ++w) {
-                float2 fa, fb;
-                if constexpr (DTYPE == 0) {
-                    fa = __half22float2(*reinterpret_cast<const __half2*>(&a[r][w]));
-                    fb = __half22float2(*reinterpret_cast<const __half2*>(&b[r][w]));
-                } else {
-                    fa = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&a[r][w]));
-                    fb = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&b[r][w]));
-                }
+                const float2 fa = widen2<DTYPE>(a[r][w]), fb = widen2<DTYPE>(b[r][w]);
                 if constexpr (W == 2) {
                     acc[r] = fmaf(fa.x, fb.x, acc[r]);
                     acc[r] = fmaf(fa.y, fb.y, acc[r]);
@@ -190,6 +202,64 @@ __global__ void attn_bwd_rows_kernel(const void* __restrict__ o, const void* __r
         for (int off = 16; off > 0; off >>= 1)
 #pragma unroll
             for (int r = 0; r < R; ++r) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], off);
+        if constexpr (WINDOW) {
+#pragma unroll 1
+            for (int r = 0; r < R; ++r) {
+                const int p = i + r + prm.q_offset, last = p < prm.Sk - 1 ? p : prm.Sk - 1;
+                int low = p - prm.window + 1;
+                low = low > 0 ? low : 0;
+                const int near = last >= low ? last - low + 1 : 0;                       // keys of the window, and first keys before it
+                int first = prm.sinks < prm.Sk ? prm.sinks : prm.Sk;
+                first = first < low ? first : low;
+                if (i + r >= Sq || near + static_cast<int64_t>(first) > kFewKeys) continue;   // uniform over the warp
+                const int64_t kv_row = ((bh / prm.H) * prm.Hkv + (bh % prm.H) / (prm.H / prm.Hkv)) * prm.Sk;
+                const float nl = -__shfl_sync(0xffffffffu, l, r) * 1.4426950408889634f;
+                uint32_t qw[W], gw[W];
+                load_words<W>(q, row + r, lane, qw);
+                load_words<W>(dout, row + r, lane, gw);
+                float sum = 0.f, weighted = 0.f;
+                constexpr int N = 4;                   // keys whose loads are in flight together
+                for (int x0 = 0; x0 < near + first; x0 += N) {
+                    uint32_t kw[N][W], vw[N][W];
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        const int x = x0 + j < near + first ? x0 + j : x0;      // (past the end: a repeated key of weight 0)
+                        const int64_t key = kv_row + (x < first ? x : low + x - first);
+                        load_words<W>(k, key, lane, kw[j]);
+                        load_words<W>(v, key, lane, vw[j]);
+                    }
+                    float s[N], dp[N];
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        s[j] = dp[j] = 0.f;
+#pragma unroll
+                        for (int w = 0; w < W; ++w) {
+                            const float2 fq = widen2<DTYPE>(qw[w]), fk = widen2<DTYPE>(kw[j][w]), fg = widen2<DTYPE>(gw[w]), fv = widen2<DTYPE>(vw[j][w]);
+                            s[j] = fmaf(fq.y, fk.y, fmaf(fq.x, fk.x, s[j]));
+                            dp[j] = fmaf(fg.y, fv.y, fmaf(fg.x, fv.x, dp[j]));
+                        }
+                    }
+#pragma unroll
+                    for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+                        for (int j = 0; j < N; ++j) {
+                            s[j] += __shfl_xor_sync(0xffffffffu, s[j], off);
+                            dp[j] += __shfl_xor_sync(0xffffffffu, dp[j], off);
+                        }
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        const float pr = x0 + j < near + first ? ex2_approx(fmaf(s[j], prm.scale_log2, nl)) : 0.f;
+                        sum += pr;
+                        weighted = fmaf(pr, dp[j], weighted);
+                    }
+                }
+                const float exact = sum > 0.f ? weighted / sum : 0.f;
+                acc[0] = r == 0 ? exact : acc[0];
+                acc[1] = r == 1 ? exact : acc[1];
+                acc[2] = r == 2 ? exact : acc[2];
+                acc[3] = r == 3 ? exact : acc[3];
+            }
+        }
         if (lane < R) {
             const float mine = lane == 0 ? acc[0] : (lane == 1 ? acc[1] : (lane == 2 ? acc[2] : acc[3]));
             const bool real = i + lane < Sq;

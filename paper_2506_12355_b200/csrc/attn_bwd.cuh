@@ -137,8 +137,10 @@ __device__ __forceinline__ void zero_rows(void* base, int64_t first_row, int row
 //
 // WINDOW: rows that see few keys take delta = sum_j P_ij dP_ij from the keys themselves.  With O rounded to 16 bits
 // delta is off by about u / sqrt(n - 1) of dQ's and dK's size (u: one rounding, n keys), beside the roundings of dS and of the
-// result: 1.73 instead of 1.41 u for two keys.  From n = 9 on it is below 1.46.
-constexpr int kFewKeys = 8;
+// result: 1.73 instead of 1.41 u for two keys, 1.46 for nine.  Rows of up to kFewKeys keys are always done so, by the warp
+// that has them; the first rows of a sequence (everything before them visible) up to kFewFirst keys, a warp each in extra
+// blocks: short sequences consist of them, and there are no more than kFewFirst - kFewKeys per head.
+constexpr int kFewKeys = 8, kFewFirst = 32;
 
 template <int DTYPE>
 __device__ __forceinline__ float2 widen2(uint32_t x) {
@@ -159,14 +161,94 @@ __device__ __forceinline__ void load_words(const void* base, int64_t row, int la
     }
 }
 
+// The keys that query row i sees: `first` first ones, then `near` from `low`.
+struct SeenKeys {
+    int low, near, first;
+    __device__ __forceinline__ SeenKeys(const BwdParams& prm, int i) {
+        const int p = i + prm.q_offset, last = p < prm.Sk - 1 ? p : prm.Sk - 1;
+        low = p - prm.window + 1;
+        low = low > 0 ? low : 0;
+        near = last >= low ? last - low + 1 : 0;
+        first = prm.sinks < prm.Sk ? prm.sinks : prm.Sk;
+        first = first < low ? first : low;
+    }
+    __device__ __forceinline__ int64_t count() const { return static_cast<int64_t>(near) + first; }
+    // one of the rows that the extra blocks take
+    __device__ __forceinline__ bool first_rows() const { return low == 0 && near > kFewKeys && near <= kFewFirst; }
+};
+
+// sum_j P_ij dP_ij of one row from its keys, executed by a warp; l: the row's LSE.
+template <int D, int DTYPE>
+__device__ __forceinline__ float delta_from_keys(const BwdParams& prm, const SeenKeys& seen, const void* q, const void* k, const void* v,
+                                                 const void* dout, int64_t bh, int64_t row, float l, int lane) {
+    constexpr int W = D / 64, N = 4;              // N: keys whose loads are in flight together
+    const int64_t kv_row = ((bh / prm.H) * prm.Hkv + (bh % prm.H) / (prm.H / prm.Hkv)) * prm.Sk;
+    const float nl = -l * 1.4426950408889634f;
+    const int n = seen.near + seen.first;
+    uint32_t qw[W], gw[W];
+    load_words<W>(q, row, lane, qw);
+    load_words<W>(dout, row, lane, gw);
+    float sum = 0.f, weighted = 0.f;
+    for (int x0 = 0; x0 < n; x0 += N) {
+        uint32_t kw[N][W], vw[N][W];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int x = x0 + j < n ? x0 + j : x0;          // (past the end: a repeated key of weight 0)
+            const int64_t key = kv_row + (x < seen.first ? x : seen.low + x - seen.first);
+            load_words<W>(k, key, lane, kw[j]);
+            load_words<W>(v, key, lane, vw[j]);
+        }
+        float s[N], dp[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            s[j] = dp[j] = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float2 fq = widen2<DTYPE>(qw[w]), fk = widen2<DTYPE>(kw[j][w]), fg = widen2<DTYPE>(gw[w]), fv = widen2<DTYPE>(vw[j][w]);
+                s[j] = fmaf(fq.y, fk.y, fmaf(fq.x, fk.x, s[j]));
+                dp[j] = fmaf(fg.y, fv.y, fmaf(fg.x, fv.x, dp[j]));
+            }
+        }
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                s[j] += __shfl_xor_sync(0xffffffffu, s[j], off);
+                dp[j] += __shfl_xor_sync(0xffffffffu, dp[j], off);
+            }
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float pr = x0 + j < n ? ex2_approx(fmaf(s[j], prm.scale_log2, nl)) : 0.f;
+            sum += pr;
+            weighted = fmaf(pr, dp[j], weighted);
+        }
+    }
+    return sum > 0.f ? weighted / sum : 0.f;
+}
+
+// plain_blocks: blocks that walk all rows; those behind them (WINDOW) take the first rows, a warp each.
 template <int D, int DTYPE, bool WINDOW>
 __global__ void attn_bwd_rows_kernel(const void* __restrict__ o, const void* __restrict__ dout, const float* __restrict__ lse,
                                      float* __restrict__ nl2, float* __restrict__ ndelta, int Sq, int Sq_pad, int64_t rows,
                                      const void* __restrict__ q, const void* __restrict__ k, const void* __restrict__ v,
-                                     const BwdParams prm) {
+                                     const BwdParams prm, int plain_blocks) {
     constexpr int R = 4, W = D / 64;          // rows at a time; 32-bit words of a row per lane
     const int lane = threadIdx.x & 31;
-    const int64_t warps = static_cast<int64_t>(gridDim.x) * (blockDim.x >> 5);
+    if constexpr (WINDOW) {
+        if (static_cast<int>(blockIdx.x) >= plain_blocks) {
+            const int64_t x = static_cast<int64_t>(blockIdx.x - plain_blocks) * (blockDim.x >> 5) + (threadIdx.x >> 5);
+            const int64_t bh = x / kFewFirst;
+            const int i = static_cast<int>(x - bh * kFewFirst);
+            if (bh * Sq_pad >= rows || i >= Sq) return;
+            const SeenKeys seen(prm, i);
+            if (!seen.first_rows()) return;
+            const int64_t row = bh * Sq + i;
+            const float exact = delta_from_keys<D, DTYPE>(prm, seen, q, k, v, dout, bh, row, lse[row], lane);
+            if (lane == 0) ndelta[bh * Sq_pad + i] = -exact;
+            return;
+        }
+    }
+    const int64_t warps = static_cast<int64_t>(plain_blocks) * (blockDim.x >> 5);
     for (int64_t prow = R * (static_cast<int64_t>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5)); prow < rows; prow += R * warps) {
         const int64_t bh = prow / Sq_pad;      // four rows from a multiple of four lie in one head
         const int i = static_cast<int>(prow - bh * Sq_pad);
@@ -202,58 +284,15 @@ __global__ void attn_bwd_rows_kernel(const void* __restrict__ o, const void* __r
         for (int off = 16; off > 0; off >>= 1)
 #pragma unroll
             for (int r = 0; r < R; ++r) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], off);
+        bool others = false;                  // this lane's row is written by an extra block
         if constexpr (WINDOW) {
 #pragma unroll 1
             for (int r = 0; r < R; ++r) {
-                const int p = i + r + prm.q_offset, last = p < prm.Sk - 1 ? p : prm.Sk - 1;
-                int low = p - prm.window + 1;
-                low = low > 0 ? low : 0;
-                const int near = last >= low ? last - low + 1 : 0;                       // keys of the window, and first keys before it
-                int first = prm.sinks < prm.Sk ? prm.sinks : prm.Sk;
-                first = first < low ? first : low;
-                if (i + r >= Sq || near + static_cast<int64_t>(first) > kFewKeys) continue;   // uniform over the warp
-                const int64_t kv_row = ((bh / prm.H) * prm.Hkv + (bh % prm.H) / (prm.H / prm.Hkv)) * prm.Sk;
-                const float nl = -__shfl_sync(0xffffffffu, l, r) * 1.4426950408889634f;
-                uint32_t qw[W], gw[W];
-                load_words<W>(q, row + r, lane, qw);
-                load_words<W>(dout, row + r, lane, gw);
-                float sum = 0.f, weighted = 0.f;
-                constexpr int N = 4;                   // keys whose loads are in flight together
-                for (int x0 = 0; x0 < near + first; x0 += N) {
-                    uint32_t kw[N][W], vw[N][W];
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const int x = x0 + j < near + first ? x0 + j : x0;      // (past the end: a repeated key of weight 0)
-                        const int64_t key = kv_row + (x < first ? x : low + x - first);
-                        load_words<W>(k, key, lane, kw[j]);
-                        load_words<W>(v, key, lane, vw[j]);
-                    }
-                    float s[N], dp[N];
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        s[j] = dp[j] = 0.f;
-#pragma unroll
-                        for (int w = 0; w < W; ++w) {
-                            const float2 fq = widen2<DTYPE>(qw[w]), fk = widen2<DTYPE>(kw[j][w]), fg = widen2<DTYPE>(gw[w]), fv = widen2<DTYPE>(vw[j][w]);
-                            s[j] = fmaf(fq.y, fk.y, fmaf(fq.x, fk.x, s[j]));
-                            dp[j] = fmaf(fg.y, fv.y, fmaf(fg.x, fv.x, dp[j]));
-                        }
-                    }
-#pragma unroll
-                    for (int off = 16; off > 0; off >>= 1)
-#pragma unroll
-                        for (int j = 0; j < N; ++j) {
-                            s[j] += __shfl_xor_sync(0xffffffffu, s[j], off);
-                            dp[j] += __shfl_xor_sync(0xffffffffu, dp[j], off);
-                        }
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const float pr = x0 + j < near + first ? ex2_approx(fmaf(s[j], prm.scale_log2, nl)) : 0.f;
-                        sum += pr;
-                        weighted = fmaf(pr, dp[j], weighted);
-                    }
-                }
-                const float exact = sum > 0.f ? weighted / sum : 0.f;
+                if (i + r >= Sq) break;
+                const SeenKeys seen(prm, i + r);
+                if (lane == r) others = seen.first_rows();
+                if (seen.count() > kFewKeys) continue;   // uniform over the warp
+                const float exact = delta_from_keys<D, DTYPE>(prm, seen, q, k, v, dout, bh, row + r, __shfl_sync(0xffffffffu, l, r), lane);
                 acc[0] = r == 0 ? exact : acc[0];
                 acc[1] = r == 1 ? exact : acc[1];
                 acc[2] = r == 2 ? exact : acc[2];
@@ -264,7 +303,7 @@ __global__ void attn_bwd_rows_kernel(const void* __restrict__ o, const void* __r
             const float mine = lane == 0 ? acc[0] : (lane == 1 ? acc[1] : (lane == 2 ? acc[2] : acc[3]));
             const bool real = i + lane < Sq;
             nl2[prow + lane] = !real ? 0.f : (l == -INFINITY ? -INFINITY : -l * 1.4426950408889634f);
-            ndelta[prow + lane] = real ? -mine : 0.f;
+            if (!others) ndelta[prow + lane] = real ? -mine : 0.f;
         }
     }
 }

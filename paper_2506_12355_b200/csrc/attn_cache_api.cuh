@@ -3,6 +3,12 @@
 
 namespace {
 
+int log2_of(int x) {
+    int s = 0;
+    while ((1 << s) < x) ++s;
+    return s;
+}
+
 bool misaligned(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
 
 // The status word's address, looked up once per device.
@@ -135,12 +141,6 @@ bool make_cache_map(CUtensorMap* map, int* axes, const void* base, const long lo
     return make_map4(map, key);
 }
 
-int log2_of(int x) {
-    int s = 0;
-    while ((1 << s) < x) ++s;
-    return s;
-}
-
 // Tokens, and items of a token and a few heads, are counted in 32 bits (more would not fit any GPU's memory).
 bool rope_tokens_ok(int64_t tokens, int H, int Hkv) {
     return tokens < (1LL << 31) - 64 && H < (1 << 20) && Hkv < (1 << 20) && (tokens / 8 + 1) * ((H > Hkv ? H : Hkv) / 4 + 1) < (1LL << 32);
@@ -181,26 +181,35 @@ int launch_rope(attn_rope::RopeParams& p, int D, int dtype, cudaStream_t st) {
 // takes the register form.  p: as for that form.
 int launch_rope_bwd_tma(const attn_rope::RopeParams& p, int B, int D, int dtype, cudaStream_t st, bool* launched, int* ctas) {
     *launched = false;
-    const int hb = 1024 / D;
+    const int most = log2_of(1024 / D);      // log2 of the heads of a tile of 8 tokens
     attn_rope::TmaMaps maps;
     attn_rope::TmaParams tp = {};
     tp.r = p;
     tp.partial = p.partial;
-    tp.token_blocks = (p.S + 7) / 8;
+    tp.block_shift = 3;
     for (int i = 0; i < 3; ++i) {
-        tp.units[i] = (p.heads[i] + hb - 1) / hb;
+        int hb = 0;
+        while (hb < most && (1 << hb) < p.heads[i]) ++hb;
+        tp.hb_shift[i] = hb;
+        tp.tb_shift[i] = 3 + most - hb;
+        tp.units[i] = (p.heads[i] + (1 << hb) - 1) >> hb;
         if (p.heads[i] == 0) continue;
-        const int n[3] = {p.S, p.heads[i], B};
+        if (tp.tb_shift[i] > tp.block_shift) tp.block_shift = tp.tb_shift[i];
+        const int n[3] = {p.S, p.heads[i], B}, box_t = 1 << tp.tb_shift[i], box_h = 1 << hb;
         auto make = [&](CUtensorMap* map, const void* base, const attn_rope::Strides& s) {
-            const Map4Key key{base, {s.token, s.head, s.batch}, dtype, D, {n[0], n[1], n[2]}, {D, 8, hb, 1}, 0};
+            const Map4Key key{base, {s.token, s.head, s.batch}, dtype, D, {n[0], n[1], n[2]}, {D, box_t, box_h, 1}, 0};
             return mappable(key.stride, n) && make_map4(map, key);
         };
         if (!make(&maps.dy[i], p.dy[i], p.ds[i]) || !make(&maps.out[i], p.out[i], p.os[i])) return ATTN_OK;
         if (i < 2 && p.weight[i] && !make(&maps.x[i], p.in[i], p.is[i])) return ATTN_OK;
     }
+    const bool packed = (p.heads[0] > 0 && tp.tb_shift[0] != 3) || (p.heads[1] > 0 && tp.tb_shift[1] != 3);
+    tp.token_blocks = static_cast<int>((static_cast<int64_t>(p.S) + (1 << tp.block_shift) - 1) >> tp.block_shift);
+    for (int i = 0; i < 3; ++i)
+        if (p.heads[i] > 0) tp.per_block += tp.units[i] << (tp.block_shift - tp.tb_shift[i]);
     DeviceInfo di;
     if (device_info(&di) != ATTN_OK) return ATTN_ERR_CUDA;
-    tp.tiles = static_cast<int64_t>(B) * tp.token_blocks * (tp.units[0] + tp.units[1] + tp.units[2]);
+    tp.tiles = static_cast<int64_t>(B) * tp.token_blocks * tp.per_block;
     if (tp.tiles / di.sm_count >= 2147483647LL) return ATTN_OK;
     int grid = di.sm_count < kRopeBwdBlocks / 2 ? di.sm_count : kRopeBwdBlocks / 2;      // (a CTA leaves 2 D partial sums)
     if (tp.tiles < grid) grid = static_cast<int>(tp.tiles);
@@ -208,7 +217,7 @@ int launch_rope_bwd_tma(const attn_rope::RopeParams& p, int B, int D, int dtype,
 #define ATTN_ROPE_CASE(DD, TT)                                                                                       \
     if (D == DD && dtype == TT) {                                                                                     \
         using C = attn_rope::TmaCfg<DD>;                                                                              \
-        auto kern = attn_rope::attn_rope_bwd_tma_kernel<DD, TT>;                                                      \
+        auto kern = packed ? attn_rope::attn_rope_bwd_tma_kernel<DD, TT, true> : attn_rope::attn_rope_bwd_tma_kernel<DD, TT, false>; \
         if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), C::SMEM)) return ATTN_ERR_CUDA;                  \
         kern<<<grid, C::THREADS, C::SMEM, st>>>(maps, tp);                                                            \
     }

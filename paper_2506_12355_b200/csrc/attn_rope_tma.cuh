@@ -1,17 +1,19 @@
 // The gradient of attn_rope.cuh's forward pass with all rows moved by TMA, for dense [B, S, heads, D] tensors.
 //
-// A tile is 8 tokens x 1024 / D heads of one of the three tensors (16 KB, and as much of the forward pass's input beside it), laid
-// out [head][token][D] in shared memory whatever the strides of its source are (the tensor maps order the axes), so that the
+// A tile is 8 tokens x 1024 / D heads of one of the three tensors (16 KB, and as much of the forward pass's input beside it), or,
+// of a tensor with fewer heads, as many more tokens (8 tokens of 2 heads of 64 would fill an eighth of it: 24578 tokens of
+// 2 + 2 x 2 such heads took 51 us, now 22), laid out [head][token][D] in shared memory whatever the strides of its source are (the tensor maps order the axes), so that the
 // result is written over it and leaves through another map: the change of layout costs nothing.  One CTA per SM walks a
 // contiguous run of tiles; a ring of 192 KB keeps loads and stores in flight while 16 warps work.  The register form in
 // attn_rope.cuh (a load, arithmetic and a store per warp: 64 KB in flight at most, and only while nobody computes) takes
-// 71 us for 4 x 2048 tokens x 48 heads of 128, this one 58 (4.9 TB/s).  What bounds it now is the issue rate of the arithmetic;
+// 71 us for 4 x 2048 tokens x 48 heads of 128, this one 60 (4.8 TB/s; 50 with the arithmetic left out).  What bounds it now is the
+// arithmetic, 16 warps of which do not hide the shuffles' latency;
 // two groups of warps on alternate tiles (61 us), two or four rows at a time (78 us and more: fewer warps for their registers)
 // are slower.  For the forward pass, with half the arithmetic and no second operand, this form gains nothing over the registers
 // (71 us either way for 16384 tokens x 48 heads of 128).
 //
-//   warps 0-15  arithmetic: warp w has token w % 8 and every other group of heads; the rotation's factors stay in registers
-//               while the tiles of one token block (all heads of q, then k, then v) pass
+//   warps 0-15  arithmetic: warp w has token w % 8 and every other group of heads, and the rotation's factors stay in registers
+//               while tiles of the same tokens pass; in a tile of more tokens each row brings its own
 //   warp  16    loads (one lane)
 //   warp  17    stores (one lane); frees a stage once its store has read it
 //
@@ -25,8 +27,8 @@
 namespace attn_rope {
 template <int D>
 struct TmaCfg {
-    static constexpr int TB = 8, HB = 1024 / D;
-    static constexpr int TILE = TB * HB * D * 2;
+    static constexpr int ROWS = 8192 / D;                     // tokens x heads of a tile
+    static constexpr int TILE = ROWS * D * 2;
     static constexpr int STAGE = 2 * TILE;                    // the output's gradient, and the forward pass's input
     static constexpr int NSTAGE = 196608 / STAGE;
     static constexpr int WARPS = 16, THREADS = (WARPS + 2) * 32;
@@ -37,9 +39,12 @@ struct TmaCfg {
 
 struct TmaParams {
     RopeParams r;             // heads, weights, table, positions, eps, S, status
-    int units[3];             // groups of 1024 / D heads of q, k, v
-    int token_blocks;         // of 8 tokens, per sequence
-    int64_t tiles;            // (sequence, token block, unit)
+    int units[3];             // groups of heads of q, k, v, 1 << hb_shift of them to a tile
+    int hb_shift[3], tb_shift[3];   // log2 of a tile's heads and tokens
+    int block_shift;          // log2 of the tokens of a block: the largest tile's
+    int token_blocks;         // per sequence
+    int per_block;            // tiles of a block: those of q, k, v
+    int64_t tiles;
     float* partial;           // [CTA][2][D]: sums of q's and k's weight gradients
 };
 
@@ -72,32 +77,53 @@ __device__ __forceinline__ void sts_row(uint32_t row, const Place& at, const uin
     asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(row + 2 * at.b), "r"(x.z), "r"(x.w) : "memory");
 }
 
-// A CTA's walk over its run of tiles.
+// A CTA's walk over its run of tiles: by sequence, token block, tensor, (PACKED) tokens inside the block, heads.
+template <bool PACKED>
 struct TileAt {
-    int b, tb, u;             // sequence, token block, unit among those of q, k, v
-    __device__ __forceinline__ void start(const TmaParams& p, int64_t tile, int per_block) {
-        const int64_t block = tile / per_block;
-        u = static_cast<int>(tile - block * per_block);
+    int b, tb, kind, unit, sub;
+    __device__ __forceinline__ int subs(const TmaParams& p) const { return PACKED ? 1 << (p.block_shift - p.tb_shift[kind]) : 1; }
+    __device__ __forceinline__ void start(const TmaParams& p, int64_t tile) {
+        const int64_t block = tile / p.per_block;
+        int u = static_cast<int>(tile - block * p.per_block);
         b = static_cast<int>(block / p.token_blocks);
         tb = static_cast<int>(block - static_cast<int64_t>(b) * p.token_blocks);
-    }
-    // true: the next tile belongs to other tokens
-    __device__ __forceinline__ bool next(const TmaParams& p, int per_block) {
-        if (++u < per_block) return false;
-        u = 0;
-        if (++tb == p.token_blocks) {
-            tb = 0;
-            ++b;
+        for (kind = 0; kind < 2; ++kind) {
+            const int n = p.units[kind] * subs(p);
+            if (u < n) break;
+            u -= n;
         }
-        return true;
+        sub = PACKED ? u / (p.units[kind] > 0 ? p.units[kind] : 1) : 0;
+        unit = u - sub * p.units[kind];
     }
-    __device__ __forceinline__ int kind(const TmaParams& p) const { return u < p.units[0] ? 0 : (u < p.units[0] + p.units[1] ? 1 : 2); }
-    __device__ __forceinline__ int head0(const TmaParams& p, int kind, int HB) const {
-        return (u - (kind > 0 ? p.units[0] : 0) - (kind > 1 ? p.units[1] : 0)) * HB;
+    // true: the next tile belongs to other tokens, or (PACKED) another tensor
+    __device__ __forceinline__ bool next(const TmaParams& p) {
+        if (++unit < p.units[kind]) return false;
+        unit = 0;
+        if (PACKED) {
+            if (++sub < subs(p)) return true;
+            sub = 0;
+        }
+        bool other = PACKED;
+        do {
+            if (++kind == 3) {
+                kind = 0;
+                other = true;
+                if (++tb == p.token_blocks) {
+                    tb = 0;
+                    ++b;
+                }
+            }
+        } while (p.units[kind] == 0);
+        return other;
     }
+    __device__ __forceinline__ int token0(const TmaParams& p) const {
+        return PACKED ? (tb << p.block_shift) + (sub << p.tb_shift[kind]) : tb * 8;
+    }
+    __device__ __forceinline__ int head0(const TmaParams& p) const { return unit << p.hb_shift[kind]; }
 };
 
-template <int D, int DTYPE>
+// PACKED: q or k has tiles of more than 8 tokens (a form of its own: what their rows need costs the others registers).
+template <int D, int DTYPE, bool PACKED>
 __global__ void __launch_bounds__(TmaCfg<D>::THREADS, 1)
 attn_rope_bwd_tma_kernel(const __grid_constant__ TmaMaps maps, const __grid_constant__ TmaParams p) {
     using C = TmaCfg<D>;
@@ -122,11 +148,10 @@ attn_rope_bwd_tma_kernel(const __grid_constant__ TmaMaps maps, const __grid_cons
     }
     __syncthreads();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int per_block = p.units[0] + p.units[1] + p.units[2];
     const int64_t first = p.tiles * blockIdx.x / gridDim.x;
     const int n = static_cast<int>(p.tiles * (blockIdx.x + 1) / gridDim.x - first);
-    TileAt at_tile;
-    at_tile.start(p, first, per_block);
+    TileAt<PACKED> at_tile;
+    if (n > 0) at_tile.start(p, first);
     F2 dw[2][4];                                              // this lane's part of the weights' gradients
 #pragma unroll
     for (int k = 0; k < 2; ++k)
@@ -139,12 +164,12 @@ attn_rope_bwd_tma_kernel(const __grid_constant__ TmaMaps maps, const __grid_cons
             for (int i = 0; i < n; ++i) {
                 const int s = i % NST;
                 if (!sm100::mbar_wait(empty(s), ((i / NST) & 1) ^ 1, abort_flag)) break;
-                const int kind = at_tile.kind(p), h0 = at_tile.head0(p, kind, C::HB), t0 = at_tile.tb * C::TB;
+                const int kind = at_tile.kind, h0 = at_tile.head0(p), t0 = at_tile.token0(p);
                 const bool with_x = kind < 2 && p.r.weight[kind] != nullptr;
                 sm100::mbar_arrive_expect_tx(full(s), with_x ? 2 * C::TILE : C::TILE);
                 tma_load_4d(base + s * C::STAGE, &maps.dy[kind], full(s), 0, t0, h0, at_tile.b);
                 if (with_x) tma_load_4d(base + s * C::STAGE + C::TILE, &maps.x[kind & 1], full(s), 0, t0, h0, at_tile.b);
-                at_tile.next(p, per_block);
+                at_tile.next(p);
             }
         }
     } else if (warp == C::WARPS + 1) {
@@ -155,53 +180,70 @@ attn_rope_bwd_tma_kernel(const __grid_constant__ TmaMaps maps, const __grid_cons
             for (int i = 0; i < n; ++i) {
                 const int s = i % NST;
                 if (!(ok = sm100::mbar_wait(done(s), (i / NST) & 1, abort_flag))) break;
-                const int kind = at_tile.kind(p);
-                tma_store_4d(&maps.out[kind], base + s * C::STAGE, 0, at_tile.tb * C::TB, at_tile.head0(p, kind, C::HB), at_tile.b);
+                // (the last block of a sequence may end before all of its tiles begin)
+                if (at_tile.token0(p) < p.r.S)
+                    tma_store_4d(&maps.out[at_tile.kind], base + s * C::STAGE, 0, at_tile.token0(p), at_tile.head0(p), at_tile.b);
                 sm100::tma_store_commit();
                 if (i >= PENDING) {
                     sm100::tma_store_wait_read<PENDING>();
                     sm100::mbar_arrive(empty((i - PENDING) % NST));
                 }
-                at_tile.next(p, per_block);
+                at_tile.next(p);
             }
             sm100::tma_store_wait_all<0>();                   // shared memory must outlive its readers
         }
     } else {
         // =========================== arithmetic ===========================
-        const int sub = lane / LPR, l = lane % LPR, t_in = warp & 7, half = warp >> 3;
+        const int sub = lane / LPR, l = lane % LPR;
         const Place at(p.r, l);
-        Turn turn;                                            // of this warp's token
+        Turn turn;                                            // of the token whose rows this lane works on
         F2 w[4];
+        int my_kind = -1;                                     // tensor that w belongs to
         bool new_tokens = true;
-        int my_kind = -1;                                     // tensor whose weights are loaded
-        for (int i = 0; i < n; ++i) {
-            const int s = i % NST, kind = at_tile.kind(p), h0 = at_tile.head0(p, kind, C::HB), token = at_tile.tb * C::TB + t_in;
-            const bool norm = kind < 2 && p.r.weight[kind] != nullptr, live = token < p.r.S;
-            if (kind < 2 && new_tokens && live) {
-                int pos = p.r.positions ? __ldg(p.r.positions + static_cast<int64_t>(at_tile.b) * p.r.S + token) : token;
-                const bool bad = p.r.R > 0 && static_cast<unsigned>(pos) >= static_cast<unsigned>(p.r.table_len);
-                if (bad) {
-                    report_bad_index(p.r.status);
-                    pos = 0;
-                }
-                turn.load(p.r, pos, l, at, true);
-                if (bad) {                                    // the token's gradients, and with them the weights', become NaN
+        auto load_turn = [&](int b, int token) {
+            int pos = p.r.positions ? __ldg(p.r.positions + static_cast<int64_t>(b) * p.r.S + token) : token;
+            const bool bad = p.r.R > 0 && static_cast<unsigned>(pos) >= static_cast<unsigned>(p.r.table_len);
+            if (bad) {
+                report_bad_index(p.r.status);
+                pos = 0;
+            }
+            turn.load(p.r, pos, l, at, true);
+            if (bad) {                                        // the token's gradients, and with them the weights', become NaN
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) turn.cs[e] = F2(__int_as_float(0x7fffffff), __int_as_float(0x7fffffff));
-                }
+                for (int e = 0; e < 4; ++e) turn.cs[e] = F2(__int_as_float(0x7fffffff), __int_as_float(0x7fffffff));
+            }
+        };
+        for (int i = 0; i < n; ++i) {
+            const int s = i % NST, kind = at_tile.kind, h0 = at_tile.head0(p), t0 = at_tile.token0(p);
+            const bool norm = kind < 2 && p.r.weight[kind] != nullptr;
+            const int hb = kind < 2 ? p.hb_shift[kind] : 0;
+            const bool wide = kind < 2 && (!PACKED || p.tb_shift[kind] == 3);  // 8 tokens: a warp has one of them
+            if (wide && new_tokens) {
+                if (t0 + (warp & 7) < p.r.S) load_turn(at_tile.b, t0 + (warp & 7));
                 new_tokens = false;
             }
             if (norm && kind != my_kind) load_weight<DTYPE>(p.r.weight[kind], p.r.weight_f32, at, w);
             my_kind = kind;
             if (!sm100::mbar_wait(full(s), (i / NST) & 1, abort_flag)) break;
-            if (kind < 2 && live) {
-                const int left = p.r.heads[kind] - h0;        // heads of this tile that exist
+            if (kind < 2) {
+                const int tb = p.tb_shift[kind], left = p.r.heads[kind] - h0;        // heads of this tile that exist
                 by_form(p.r, D, [&](auto inter, auto whole_head) {
-                    uint32_t row = base + s * C::STAGE + ((half * RPW + sub) * C::TB + t_in) * D * 2;
 #pragma unroll
-                    for (int k = 0; k < C::HB / (2 * RPW); ++k, row += 2 * RPW * C::TB * D * 2) {
-                        const int h = (2 * k + half) * RPW;
-                        if (h >= left) break;                 // uniform over the warp
+                    for (int k = 0; k < C::ROWS / (C::WARPS * RPW); ++k) {
+                        int h, tok;                           // this lane's row
+                        if (!PACKED || wide) {
+                            h = (k * (C::WARPS / 8) + (warp >> 3)) * RPW;
+                            tok = warp & 7;
+                            if (h >= left || t0 + tok >= p.r.S) break;        // uniform over the warp
+                            h += sub;
+                        } else {
+                            const int r = (k * C::WARPS + warp) * RPW + sub;
+                            h = r & ((1 << hb) - 1);
+                            tok = r >> hb;
+                            if (t0 + tok < p.r.S) load_turn(at_tile.b, t0 + tok);
+                        }
+                        const bool live = h < left && t0 + tok < p.r.S;
+                        const uint32_t row = base + s * C::STAGE + ((h << tb) + tok) * D * 2;
                         F2 g[4], y[4];
                         unpack_row<DTYPE>(lds_row(row, at), g);
                         turn_values<decltype(inter)::value, decltype(whole_head)::value>(y, g, turn.cs, turn.sn, at.turns);
@@ -216,14 +258,19 @@ attn_rope_bwd_tma_kernel(const __grid_constant__ TmaMaps maps, const __grid_cons
                             }
                             const float r = rsqrtf(row_sum<LPR>(ss.sum()) * (1.f / D) + p.r.eps);
                             const float k3 = -row_sum<LPR>(gx.sum()) * (1.f / D) * r * r * r;
-                            // (rows past the last head hold zeros in x and g: at eps 0 their r is infinite)
-                            const float rd = h + sub < left ? r : 0.f;
-                            const F2 rr(r, r), kk(k3, k3), rrd(rd, rd);
+                            const F2 rr(r, r), kk(k3, k3);
+                            // (rows that do not exist are zero in x and g: at eps 0 their r is infinite)
+                            if (live) {
+                                if (kind == 0) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                if (kind == 0) dw[0][e] = fma2(hx[e], rrd, dw[0][e]); else dw[1][e] = fma2(hx[e], rrd, dw[1][e]);
-                                y[e] = fma2(y[e], w[e] * rr, kk * x[e]);
+                                    for (int e = 0; e < 4; ++e) dw[0][e] = fma2(hx[e], rr, dw[0][e]);
+                                } else {
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) dw[1][e] = fma2(hx[e], rr, dw[1][e]);
+                                }
                             }
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) y[e] = fma2(y[e], w[e] * rr, kk * x[e]);
                         }
                         sts_row(row, at, pack_row<DTYPE>(y));
                     }
@@ -232,7 +279,7 @@ attn_rope_bwd_tma_kernel(const __grid_constant__ TmaMaps maps, const __grid_cons
             }
             __syncwarp();
             if (lane == 0) sm100::mbar_arrive(done(s));
-            if (at_tile.next(p, per_block)) new_tokens = true;
+            if (at_tile.next(p)) new_tokens = true;
         }
     }
     __syncthreads();                                          // loads and stores are over: the ring is free

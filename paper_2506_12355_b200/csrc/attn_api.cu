@@ -756,8 +756,8 @@ int bwd(const void* q, const void* k, const void* v, const void* o, const float*
             !allow_dynamic_smem(reinterpret_cast<const void*>(kkv), CKV::SMEM_BYTES))                                      \
             return ATTN_ERR_CUDA;                                                                                          \
         const int64_t rows = BH * sq_pad;                                                                                  \
-        int64_t blocks = (rows + 31) / 32;                                                                                   \
-        if (blocks > 148 * 16) blocks = 148 * 16;                                                                          \
+        int64_t blocks = (rows + 63) / 64;                                                                                 \
+        if (blocks > 1 << 20) blocks = 1 << 20;                                                                            \
         const int64_t first_blocks = WINDOW ? (BH * attn_grad::kFewFirst + 7) / 8 : 0;                                     \
         attn_grad::attn_bwd_rows_kernel<DD, TT, WINDOW><<<static_cast<unsigned>(blocks + first_blocks), 256, 0, st>>>(       \
             o, dout, lse, nl2, ndelta, Sq, prm.Sq_pad, rows, q, k, v, prm, static_cast<int>(blocks));                       \

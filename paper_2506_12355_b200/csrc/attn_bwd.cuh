@@ -132,14 +132,15 @@ __device__ __forceinline__ void zero_rows(void* base, int64_t first_row, int row
 }
 
 // Per query row: ndelta = -sum_d dO_id * O_id and nl2 = -LSE * log2(e), written with the row stride Sq_pad (padding rows: 0).
-// `rows` counts padded rows: B * H * Sq_pad (a multiple of 64).  A warp takes four rows at a time, all of their loads in flight
-// together (one row after the other took 42 us for 32 heads x 8192 rows of 128, four together 24; 134 MB).
+// `rows` counts padded rows: B * H * Sq_pad (a multiple of 64).  Bound by HBM (D = 128: 134 MB for 32 heads x 8192 rows).  A
+// warp takes eight rows at a time in 16-byte loads and adds their partial sums up with 10 shuffles (a row's lanes would
+// take five each).
 //
 // WINDOW: rows that see few keys take delta = sum_j P_ij dP_ij from the keys themselves.  With O rounded to 16 bits
 // delta is off by about u / sqrt(n - 1) of dQ's and dK's size (u: one rounding, n keys), beside the roundings of dS and of the
 // result: 1.73 instead of 1.41 u for two keys, 1.46 for nine.  Rows of up to kFewKeys keys are always done so, by the warp
-// that has them; the first rows of a sequence (everything before them visible) up to kFewFirst keys, a warp each in extra
-// blocks: short sequences consist of them, and there are no more than kFewFirst - kFewKeys per head.
+// that has them; of the first kFewFirst rows of a sequence those with everything before them visible up to kFewFirst keys, a
+// warp each in extra blocks: short sequences consist of them, and eight one after the other in a warp are a tail of 20 us.
 constexpr int kFewKeys = 8, kFewFirst = 32;
 
 template <int DTYPE>
@@ -173,8 +174,8 @@ struct SeenKeys {
         first = first < low ? first : low;
     }
     __device__ __forceinline__ int64_t count() const { return static_cast<int64_t>(near) + first; }
-    // one of the rows that the extra blocks take
-    __device__ __forceinline__ bool first_rows() const { return low == 0 && near > kFewKeys && near <= kFewFirst; }
+    // Row i is one that the extra blocks take.
+    __device__ __forceinline__ bool first_rows(int i) const { return i < kFewFirst && low == 0 && near <= kFewFirst; }
 };
 
 // sum_j P_ij dP_ij of one row from its keys, executed by a warp; l: the row's LSE.
@@ -232,7 +233,8 @@ __global__ void attn_bwd_rows_kernel(const void* __restrict__ o, const void* __r
                                      float* __restrict__ nl2, float* __restrict__ ndelta, int Sq, int Sq_pad, int64_t rows,
                                      const void* __restrict__ q, const void* __restrict__ k, const void* __restrict__ v,
                                      const BwdParams prm, int plain_blocks) {
-    constexpr int R = 4, W = D / 64;          // rows at a time; 32-bit words of a row per lane
+    constexpr int R = 8;                      // rows at a time
+    constexpr int G = D / 8, SETS = G / 4;    // lanes of a row (16 bytes each); loads of a tensor: 32 / G rows each
     const int lane = threadIdx.x & 31;
     if constexpr (WINDOW) {
         if (static_cast<int>(blockIdx.x) >= plain_blocks) {
@@ -241,7 +243,7 @@ __global__ void attn_bwd_rows_kernel(const void* __restrict__ o, const void* __r
             const int i = static_cast<int>(x - bh * kFewFirst);
             if (bh * Sq_pad >= rows || i >= Sq) return;
             const SeenKeys seen(prm, i);
-            if (!seen.first_rows()) return;
+            if (!seen.first_rows(i)) return;
             const int64_t row = bh * Sq + i;
             const float exact = delta_from_keys<D, DTYPE>(prm, seen, q, k, v, dout, bh, row, lse[row], lane);
             if (lane == 0) ndelta[bh * Sq_pad + i] = -exact;
@@ -250,60 +252,79 @@ __global__ void attn_bwd_rows_kernel(const void* __restrict__ o, const void* __r
     }
     const int64_t warps = static_cast<int64_t>(plain_blocks) * (blockDim.x >> 5);
     for (int64_t prow = R * (static_cast<int64_t>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5)); prow < rows; prow += R * warps) {
-        const int64_t bh = prow / Sq_pad;      // four rows from a multiple of four lie in one head
+        // eight rows from a multiple of eight lie in one head
+        const int64_t bh = rows <= INT32_MAX ? static_cast<uint32_t>(prow) / static_cast<uint32_t>(Sq_pad) : prow / Sq_pad;
         const int i = static_cast<int>(prow - bh * Sq_pad);
         const int64_t row = bh * Sq + i;
-        uint32_t a[R][W], b[R][W];
-        float l = 0.f;
+        uint4 a[SETS], b[SETS];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-#pragma unroll
-            for (int w = 0; w < W; ++w) a[r][w] = b[r][w] = 0u;
+        for (int x = 0; x < SETS; ++x) {
+            const int r = x * (32 / G) + lane / G;
+            a[x] = b[x] = make_uint4(0u, 0u, 0u, 0u);
             if (i + r < Sq) {
-                load_words<W>(o, row + r, lane, a[r]);
-                load_words<W>(dout, row + r, lane, b[r]);
+                a[x] = reinterpret_cast<const uint4*>(o)[(row + r) * G + lane % G];
+                b[x] = reinterpret_cast<const uint4*>(dout)[(row + r) * G + lane % G];
             }
         }
-        if (lane < R && i + lane < Sq) l = lse[row + lane];
-        float acc[R];
+        const bool real = lane < R && i + lane < Sq;
+        const float l = real ? lse[row + lane] : 0.f;
+        // Eight partial sums a lane: 8 / SETS per row, of neighbouring elements.  They are added over the lanes of a row while
+        // every step leaves a lane half as many of them to add.
+        float acc[8];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            acc[r] = 0.f;
+        for (int x = 0; x < SETS; ++x) {
+            constexpr int P = 8 / SETS, N = 4 / P;   // sums of a row in a lane; words of each
+            const uint32_t aw[4] = {a[x].x, a[x].y, a[x].z, a[x].w}, bw[4] = {b[x].x, b[x].y, b[x].z, b[x].w};
 #pragma unroll
-            for (int w = 0; w < W; ++w) {
-                const float2 fa = widen2<DTYPE>(a[r][w]), fb = widen2<DTYPE>(b[r][w]);
-                if constexpr (W == 2) {
-                    acc[r] = fmaf(fa.x, fb.x, acc[r]);
-                    acc[r] = fmaf(fa.y, fb.y, acc[r]);
+            for (int y = 0; y < P; ++y) {
+                const float2 fa = widen2<DTYPE>(aw[y * N]), fb = widen2<DTYPE>(bw[y * N]);
+                float s;
+                if constexpr (N == 2) {
+                    const float2 ga = widen2<DTYPE>(aw[y * N + N - 1]), gb = widen2<DTYPE>(bw[y * N + N - 1]);
+                    s = fmaf(ga.y, gb.y, fmaf(ga.x, gb.x, fmaf(fa.y, fb.y, fa.x * fb.x)));
                 } else {
-                    acc[r] = fmaf(fa.x, fb.x, fa.y * fb.y);
+                    s = fmaf(fa.x, fb.x, fa.y * fb.y);
                 }
+                acc[x * P + y] = s;
             }
         }
+        int off = G / 2;
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1)
+        for (int n = 4; n > 0; n >>= 1, off >>= 1) {
+            const bool upper = lane & off;
 #pragma unroll
-            for (int r = 0; r < R; ++r) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], off);
+            for (int x = 0; x < n; ++x) {
+                const float mine = upper ? acc[n + x] : acc[x], other = upper ? acc[x] : acc[n + x];
+                acc[x] = mine + __shfl_xor_sync(0xffffffffu, other, off);
+            }
+        }
+        float sum = acc[0];
+        int from;                                  // the lane that has row `lane`
+        if constexpr (D == 128) {                  // lane bits 4, 3, 2: row bits 0, 2, 1; bit 1: which of the row's two sums
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            from = (lane & 1) << 4 | (lane & 4) << 1 | (lane & 2) << 1;
+        } else {                                   // lane bits 4, 3, 2: row bits 1, 0, 2; bits 1, 0: which of its four sums
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            from = (lane & 3) << 3 | (lane & 4);
+        }
+        sum = __shfl_sync(0xffffffffu, sum, from);
         bool others = false;                  // this lane's row is written by an extra block
         if constexpr (WINDOW) {
-#pragma unroll 1
-            for (int r = 0; r < R; ++r) {
-                if (i + r >= Sq) break;
-                const SeenKeys seen(prm, i + r);
-                if (lane == r) others = seen.first_rows();
-                if (seen.count() > kFewKeys) continue;   // uniform over the warp
-                const float exact = delta_from_keys<D, DTYPE>(prm, seen, q, k, v, dout, bh, row + r, __shfl_sync(0xffffffffu, l, r), lane);
-                acc[0] = r == 0 ? exact : acc[0];
-                acc[1] = r == 1 ? exact : acc[1];
-                acc[2] = r == 2 ? exact : acc[2];
-                acc[3] = r == 3 ? exact : acc[3];
+            const SeenKeys seen(prm, i + (lane & (R - 1)));
+            others = real && seen.first_rows(i + lane);
+            uint32_t few = __ballot_sync(0xffffffffu, real && !others && seen.count() <= kFewKeys);
+            while (few) {
+                const int r = __ffs(few) - 1;
+                few &= few - 1;
+                const float exact = delta_from_keys<D, DTYPE>(prm, SeenKeys(prm, i + r), q, k, v, dout, bh, row + r, __shfl_sync(0xffffffffu, l, r), lane);
+                if (lane == r) sum = exact;
             }
         }
         if (lane < R) {
-            const float mine = lane == 0 ? acc[0] : (lane == 1 ? acc[1] : (lane == 2 ? acc[2] : acc[3]));
-            const bool real = i + lane < Sq;
             nl2[prow + lane] = !real ? 0.f : (l == -INFINITY ? -INFINITY : -l * 1.4426950408889634f);
-            if (!others) ndelta[prow + lane] = real ? -mine : 0.f;
+            if (!others) ndelta[prow + lane] = real ? -sum : 0.f;
         }
     }
 }

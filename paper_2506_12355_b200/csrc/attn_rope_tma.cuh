@@ -1,16 +1,17 @@
 // The gradient of attn_rope.cuh's forward pass with all rows moved by TMA, for dense [B, S, heads, D] tensors.
 //
-// A tile is 8 tokens x 1024 / D heads of one of the three tensors (16 KB, and as much of the forward pass's input beside it), or,
-// of a tensor with fewer heads, as many more tokens (8 tokens of 2 heads of 64 would fill an eighth of it: 24578 tokens of
-// 2 + 2 x 2 such heads took 51 us, now 22), laid out [head][token][D] in shared memory whatever the strides of its source are (the tensor maps order the axes), so that the
-// result is written over it and leaves through another map: the change of layout costs nothing.  One CTA per SM walks a
-// contiguous run of tiles; a ring of 192 KB keeps loads and stores in flight while 16 warps work.  The register form in
+// A tile is 8 tokens x 1024 / D heads of one of the three tensors (16 KB, and as much of the forward pass's input beside it),
+// or, of a tensor with fewer heads, as many more tokens (8 tokens of 2 heads of 64 would fill an eighth of it: 24578 tokens of
+// 2 + 2 x 2 such heads took 51 us, now 22), laid out [head][token][D] in shared memory whatever the strides of its source
+// are (the tensor maps order the axes), so that the result is written over it and leaves through another map: the change of
+// layout costs nothing.  One CTA per SM walks a contiguous run of tiles; a ring of 192 KB keeps loads and stores in flight
+// while 16 warps work.  The register form in
 // attn_rope.cuh (a load, arithmetic and a store per warp: 64 KB in flight at most, and only while nobody computes) takes
-// 71 us for 4 x 2048 tokens x 48 heads of 128, this one 60 (4.8 TB/s; 50 with the arithmetic left out).  What bounds it now is the
-// arithmetic, 16 warps of which do not hide the shuffles' latency;
-// two groups of warps on alternate tiles (61 us), two or four rows at a time (78 us and more: fewer warps for their registers)
-// are slower.  For the forward pass, with half the arithmetic and no second operand, this form gains nothing over the registers
-// (71 us either way for 16384 tokens x 48 heads of 128).
+// 71 us for 4 x 2048 tokens x 48 heads of 128, this one 60 (4.8 TB/s; 50 with the arithmetic left out).  What bounds it now
+// is the arithmetic: its shuffles' latency, which 16 warps of 96 registers do not hide, and half of all issue slots.  Two
+// groups of warps on alternate tiles (61 us), two or four rows at a time (78 us and more: fewer warps for their registers)
+// are slower.  For the forward pass, with half the arithmetic and no second operand, this form gains nothing over the
+// registers (71 us either way for 16384 tokens x 48 heads of 128).
 //
 //   warps 0-15  arithmetic: warp w has token w % 8 and every other group of heads, and the rotation's factors stay in registers
 //               while tiles of the same tokens pass; in a tile of more tokens each row brings its own

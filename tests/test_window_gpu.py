@@ -142,6 +142,19 @@ def test_keys_that_end_before_the_queries(W, sinks, off):
     run(1, 2, 2, 300, 280, 64, "bf16", W, sinks, off, seed=4)
 
 
+@pytest.mark.parametrize("Sq,Sk,W,off", [(100, 20, 1000, 0), (200, 32, 300, 40), (70, 9, 100, 0), (100, 8, 1000, 3), (90, 33, 64, 0), (10, 10, 50, 0), (3, 25, 100, 12)])
+def test_few_keys_for_many_queries(Sq, Sk, W, off):
+    # all rows see the same few keys, also those behind the sequence's first rows; nothing is taken from the workspace's old content
+    q, k, v, g = inputs(2, 2, 1, Sq, Sk, 128, torch.bfloat16, 6)
+    scale = float(torch.tensor(1 / math.sqrt(128), dtype=torch.float32))
+    ref = reference(q, k, v, g, scale, W, 0, off)
+    o, lse = api.attn_fwd_window(q, k, v, scale, W, 0, off)
+    workspace = torch.full((api.attn_bwd_window_workspace_bytes(2, 2, 1, Sq, Sk, 128, W, 0, off),), 255, dtype=torch.uint8, device="cuda")
+    grads = api.attn_bwd_window(q, k, v, o, lse, g, scale, W, 0, off, workspace=workspace)
+    for name, t in zip(("dq", "dk", "dv"), grads):
+        check(name, t, *ref[name])
+
+
 def test_more_keys_than_positions():
     run(1, 2, 1, 200, 900, 64, "fp16", 64, 3, 100, seed=5)       # keys behind every query: zero gradients
 

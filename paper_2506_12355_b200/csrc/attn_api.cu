@@ -760,7 +760,7 @@ int bwd(const void* q, const void* k, const void* v, const void* o, const float*
         if (blocks > 1 << 20) blocks = 1 << 20;                                                                            \
         const int64_t first_blocks = WINDOW ? (BH * attn_grad::kFewFirst + 7) / 8 : 0;                                     \
         attn_grad::attn_bwd_rows_kernel<DD, TT, WINDOW><<<static_cast<unsigned>(blocks + first_blocks), 256, 0, st>>>(       \
-            o, dout, lse, nl2, ndelta, Sq, prm.Sq_pad, rows, q, k, v, prm, static_cast<int>(blocks));                       \
+            o, dout, lse, nl2, ndelta, Sq, prm.Sq_pad, rows, q, k, v, prm, static_cast<int>(first_blocks));                 \
         prm.out0 = dq;                                                                                                     \
         prm.out1 = nullptr;                                                                                                \
         prm.n_tiles_total = static_cast<int>(n_qtiles * BH);                                                               \

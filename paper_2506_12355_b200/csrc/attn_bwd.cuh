@@ -227,18 +227,19 @@ __device__ __forceinline__ float delta_from_keys(const BwdParams& prm, const See
     return sum > 0.f ? weighted / sum : 0.f;
 }
 
-// plain_blocks: blocks that walk all rows; those behind them (WINDOW) take the first rows, a warp each.
+// first_blocks (WINDOW): blocks that take the first rows, a warp each; they start before those that walk all rows, because a
+// warp's keys come one round trip after the other.
 template <int D, int DTYPE, bool WINDOW>
 __global__ void attn_bwd_rows_kernel(const void* __restrict__ o, const void* __restrict__ dout, const float* __restrict__ lse,
                                      float* __restrict__ nl2, float* __restrict__ ndelta, int Sq, int Sq_pad, int64_t rows,
                                      const void* __restrict__ q, const void* __restrict__ k, const void* __restrict__ v,
-                                     const BwdParams prm, int plain_blocks) {
+                                     const BwdParams prm, int first_blocks) {
     constexpr int R = 8;                      // rows at a time
     constexpr int G = D / 8, SETS = G / 4;    // lanes of a row (16 bytes each); loads of a tensor: 32 / G rows each
     const int lane = threadIdx.x & 31;
     if constexpr (WINDOW) {
-        if (static_cast<int>(blockIdx.x) >= plain_blocks) {
-            const int64_t x = static_cast<int64_t>(blockIdx.x - plain_blocks) * (blockDim.x >> 5) + (threadIdx.x >> 5);
+        if (static_cast<int>(blockIdx.x) < first_blocks) {
+            const int64_t x = static_cast<int64_t>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5);
             const int64_t bh = x / kFewFirst;
             const int i = static_cast<int>(x - bh * kFewFirst);
             if (bh * Sq_pad >= rows || i >= Sq) return;
@@ -250,8 +251,9 @@ __global__ void attn_bwd_rows_kernel(const void* __restrict__ o, const void* __r
             return;
         }
     }
-    const int64_t warps = static_cast<int64_t>(plain_blocks) * (blockDim.x >> 5);
-    for (int64_t prow = R * (static_cast<int64_t>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5)); prow < rows; prow += R * warps) {
+    const int block = static_cast<int>(blockIdx.x) - (WINDOW ? first_blocks : 0), blocks = static_cast<int>(gridDim.x) - (WINDOW ? first_blocks : 0);
+    const int64_t warps = static_cast<int64_t>(blocks) * (blockDim.x >> 5);
+    for (int64_t prow = R * (static_cast<int64_t>(block) * (blockDim.x >> 5) + (threadIdx.x >> 5)); prow < rows; prow += R * warps) {
         // eight rows from a multiple of eight lie in one head
         const int64_t bh = rows <= INT32_MAX ? static_cast<uint32_t>(prow) / static_cast<uint32_t>(Sq_pad) : prow / Sq_pad;
         const int i = static_cast<int>(prow - bh * Sq_pad);

@@ -14,8 +14,9 @@
 //     contiguous part, whatever the lengths are.  Each CTA lays the list out for itself from the device-side lengths (no
 //     host copy of them, no plan to keep).  A pair inside one CTA's part is finished there; one that is cut by a border
 //     leaves one fp32 partial result per CTA (at most two per CTA), and a second small kernel joins those.
-//   * A few pairs of short sequences (one conversation) are a matter of latency: there a cluster of 8 CTAs takes one pair,
-//     each an eighth of its tiles, and joins the parts through distributed shared memory: one launch, no list to lay out.
+//   * A few pairs of short sequences (one conversation) are a matter of latency: there a cluster of 8, 4, 2 or 1 CTAs
+//     takes one pair, each an equal share of its tiles, and joins the parts through distributed shared memory: one launch, no
+//     list to lay out.
 //   * Each warp keeps a ring of its own in shared memory, filled by TMA boxes of up to CK rows x 128 bytes (a box lies in one
 //     page), one mbarrier per stage, and no other synchronisation: 128 to 192 KB per SM are in flight.  Measured at
 //     4 x 65536 keys of 8 heads x 128: per-thread 16-byte copies (cp.async) stop at 4.9 TB/s however deep the ring is, the TMA
@@ -79,7 +80,7 @@ struct DecodeParams {
     int window, sinks;
     float scale_log2;
     int grid;                   // CTAs of the first kernel
-    int cluster;                // 1: a cluster of kCluster CTAs per (sequence, head), no second kernel
+    int cluster;                // > 0: a cluster of so many CTAs (up to kCluster) per (sequence, head), no second kernel
 };
 constexpr int kCluster = 8;
 
@@ -147,15 +148,19 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, u
 // that a cut pair has a partial result from every CTA between its first and its last one.
 __device__ __forceinline__ int cta_count(int64_t total, int grid) { return total < grid ? static_cast<int>(total) : grid; }
 
-// The list's form follows from its length.  Heads side by side read whole pages and leave nothing to merge inside a CTA
-// (64 sequences of up to 8192 keys, 8 heads of 128: 180 us against 199), but cut each pair into as many parts as there are
-// CTAs on it, and joining those is what a short list waits for (one sequence of 1000 keys: 12.5 us against 9.3 with all
-// warps on one head).  So tiles side by side are taken when every CTA gets at least kLongList of them.
-constexpr int kLongList = 4;
+// The list's form follows from its length and from the parts that it cuts a pair into.  Heads side by side read whole pages
+// and leave nothing to merge inside a CTA (64 sequences of up to 8192 keys, 8 heads of 128: 171 us against 205), but cut each
+// pair into as many parts as there are CTAs on it, and joining those is what a short list or one of few sequences waits for
+// (4 sequences of 2000 keys: 24 us against 17 with all warps on one head; 2 of 16000: 55 against 35; 16 of 2000: 34 either
+// way).  So tiles side by side are taken when every CTA gets at least kLongList of them and a pair has about kFewParts parts
+// at most.
+constexpr int kLongList = 4, kFewParts = 10;
 struct ListForm { int64_t total; int hpt_shift; };
 __device__ __forceinline__ ListForm list_form(const DecodeParams& p, int64_t total_side, int64_t total_one) {
-    total_side *= p.heads >> p.hpt_shift;
-    if (p.hpt_shift == 0 || total_side >= static_cast<int64_t>(kLongList) * p.grid) return {total_side, p.hpt_shift};
+    const int groups = p.heads >> p.hpt_shift;
+    total_side *= groups;
+    const bool side = total_side >= static_cast<int64_t>(kLongList) * p.grid && static_cast<int64_t>(p.B) * groups * kFewParts >= p.grid;
+    if (p.hpt_shift == 0 || side) return {total_side, p.hpt_shift};
     return {total_one * p.heads, 0};
 }
 __device__ __forceinline__ int64_t cta_begin(int64_t total, int c, int ctas) { return total * c / ctas; }
@@ -277,12 +282,12 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
 
     TileWalk<NW, CK> ld, cu;      // the copies run NSTAGE - 1 tiles ahead of the arithmetic
     int steps, hs = 0, groups = p.heads;
-    const int rank = static_cast<int>(blockIdx.x) % kCluster;
+    const int rank = p.cluster ? static_cast<int>(blockIdx.x) % p.cluster : 0;
     if (p.cluster) {
-        const int pair = static_cast<int>(blockIdx.x) / kCluster, b = pair / p.heads;
+        const int pair = static_cast<int>(blockIdx.x) / p.cluster, b = pair / p.heads;
         ld.at(p, 0, b, pair - b * p.heads, 0);
-        ld.t = ld.t_end * rank / kCluster;
-        steps = ld.t_end * (rank + 1) / kCluster - ld.t;
+        ld.t = ld.t_end * rank / p.cluster;
+        steps = ld.t_end * (rank + 1) / p.cluster - ld.t;
         if (pair == b * p.heads && rank == 0 && tid == 0 && p.seq_lens[b] > p.max_len) report_bad_index(p.status);
     } else {
     // ---- lay out the tile list: total tiles, and the pair and tile at which this CTA's part begins ----
@@ -690,15 +695,18 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         if (steps == 0)
             for (int row = tid; row < GH; row += C::THREADS) *reinterpret_cast<float2*>(mine + GH * D + 2 * row) = make_float2(-INFINITY, 0.f);
         cluster_sync();
-        // row `rank` (and rank + 8) of the pair: this CTA joins it, a thread per 16-byte column
+        // every p.cluster-th row of the pair from `rank`: this CTA joins it, a thread per 16-byte column
         const int rows = p.group - own_r0 < GH ? p.group - own_r0 : GH;
         const uint32_t base = sm100::smem_u32(smem);
-        for (int row = rank; row < rows; row += kCluster) {
+        for (int row = rank; row < rows; row += p.cluster) {
             for (int d4 = tid; d4 < D / 4; d4 += C::THREADS) {
                 float2 ml[kCluster];
                 float4 v[kCluster];
 #pragma unroll
                 for (int k = 0; k < kCluster; ++k) {
+                    ml[k] = make_float2(-INFINITY, 0.f);
+                    v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (k >= p.cluster) continue;
                     const uint32_t from = map_rank(base, k);
                     ml[k] = ld_cluster2(from + (GH * D + 2 * row) * 4);
                     v[k] = ld_cluster4(from + (row * D + 4 * d4) * 4);

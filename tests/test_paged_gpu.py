@@ -167,6 +167,19 @@ def test_decode_few_pairs(lens, H, Hkv, D):
     run_decode(lens, H, Hkv, D, 64, "fp16", "head", window=70, sinks=5, seed=7)
 
 
+@pytest.mark.parametrize("n", [3, 4, 7, 8, 15, 18, 19])
+@pytest.mark.parametrize("Hkv,group,D", [(8, 4, 128), (8, 2, 64), (4, 12, 128), (2, 20, 256)])
+def test_decode_some_pairs(n, Hkv, group, D):
+    """Every size of cluster, and the shapes on both sides of the last one."""
+    lens = [(0, 1, 500, 129, 16, 333, 512)[i % 7] for i in range(n)]
+    run_decode(lens, Hkv * group, Hkv, D, 16, "bf16", "head", seed=8)
+    run_decode(lens, Hkv * group, Hkv, D, 32, "fp16", "slot", window=200, sinks=3, seed=9)
+
+
+def test_decode_few_long_sequences():
+    run_decode([14000, 9000], 8, 8, 128, 64, "bf16", "head", seed=10)
+
+
 def test_decode_zero_scale_and_large_scores():
     run_decode([1, 50, 400], 4, 2, 128, 16, "bf16", "head", scale=0.0, seed=6)
     run_decode([1, 50, 3000], 4, 2, 128, 16, "fp16", "head", scale=3.0, seed=7)    # scores of a hundred and more: the maximum moves

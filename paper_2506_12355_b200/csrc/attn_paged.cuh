@@ -80,7 +80,7 @@ struct DecodeParams {
     int window, sinks;
     float scale_log2;
     int grid;                   // CTAs of the first kernel
-    int cluster;                // > 0: a cluster of so many CTAs (up to kCluster) per (sequence, head), no second kernel
+    int cluster;                // > 0: a cluster of so many CTAs (a power of two up to kCluster) per (sequence, head), no second kernel
 };
 constexpr int kCluster = 8;
 
@@ -282,12 +282,12 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
 
     TileWalk<NW, CK> ld, cu;      // the copies run NSTAGE - 1 tiles ahead of the arithmetic
     int steps, hs = 0, groups = p.heads;
-    const int rank = p.cluster ? static_cast<int>(blockIdx.x) % p.cluster : 0;
+    const int shift = 31 - __clz(p.cluster | 1), rank = static_cast<int>(blockIdx.x) & ((1 << shift) - 1);
     if (p.cluster) {
-        const int pair = static_cast<int>(blockIdx.x) / p.cluster, b = pair / p.heads;
+        const int pair = static_cast<int>(blockIdx.x) >> shift, b = pair / p.heads;
         ld.at(p, 0, b, pair - b * p.heads, 0);
-        ld.t = ld.t_end * rank / p.cluster;
-        steps = ld.t_end * (rank + 1) / p.cluster - ld.t;
+        ld.t = ld.t_end * rank >> shift;
+        steps = (ld.t_end * (rank + 1) >> shift) - ld.t;
         if (pair == b * p.heads && rank == 0 && tid == 0 && p.seq_lens[b] > p.max_len) report_bad_index(p.status);
     } else {
     // ---- lay out the tile list: total tiles, and the pair and tile at which this CTA's part begins ----

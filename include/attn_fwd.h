@@ -336,7 +336,8 @@ size_t attn_qk_norm_rope_bwd_workspace_bytes(int D);
  *            both be NULL (keys and values only).
  * seq_lens : device int32 [n_seqs], the sequences' lengths WITH the new tokens.
  * cu_seqlens: device int32 [n_seqs + 1], first token of each sequence's new ones and their end; NULL: one new token per
- *            sequence, tokens == n_seqs.  Tokens behind cu_seqlens[n_seqs] and tokens of sequences of length 0 are padding: their
+ *            sequence, tokens == n_seqs.  The entries do not decrease; the first may be above 0 (a slice of a larger batch's list).
+ *            Tokens before cu_seqlens[0], tokens from cu_seqlens[n_seqs] on and tokens of sequences of length 0 are padding: their
  *            rows of q_out and the cache stay as they were.
  * q_out    : device, contiguous [tokens, H, D].
  * A token whose position falls below 0, beyond the block table or the rotation table, or whose page is not in

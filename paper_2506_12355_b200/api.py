@@ -669,7 +669,8 @@ def attn_paged_append(q, k, v, k_cache, v_cache, block_table, seq_lens, q_weight
     attn_qk_norm_rope at each token's position in its sequence, k and v [T,Hkv,D] written into the pages of k_cache, v_cache
     ([pages, Hkv, page_size, D], any strides).  seq_lens int32 [B]: lengths with the new tokens; block_table int32 [B, max_pages];
     cu_seqlens int32 [B+1]: first new token of each sequence and the end (None: one token per sequence, T == B).  Tokens
-    behind the end, and of sequences of length 0, are padding: nothing is written for them.  Returns q_out [T,H,D]."""
+    before the first and behind the end, and of sequences of length 0, are padding: nothing is written for them.  Returns
+    q_out [T,H,D]."""
     result = _fast("attn_paged_append", stream, q, k, v, k_cache, v_cache, block_table, seq_lens, q_weight, k_weight, cos_sin, cu_seqlens, eps,
                    interleaved, q_out)
     if result is not NotImplemented:

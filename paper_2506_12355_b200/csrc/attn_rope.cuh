@@ -207,13 +207,13 @@ __device__ __forceinline__ float row_sum(float x) {
     return x;
 }
 
-// Where one token's rows go in the paged form.  Returns the position, or -1 when the token is not written (padding behind
-// the last sequence, or an entry that is out of range).
+// Where one token's rows go in the paged form.  Returns the position, or -1 when the token is not written (padding before the
+// first sequence's new tokens or behind the last one's, or an entry that is out of range).
 __device__ __forceinline__ int place_token(const RopeParams& p, int t, int& page, int& slot) {
     int seq, pos;
     if (p.cu_seqlens) {
         // last sequence that begins at or before t (empty sequences share a begin; the last of them is not empty or is the end)
-        if (t >= __ldg(p.cu_seqlens + p.n_seqs)) return -1;
+        if (t < __ldg(p.cu_seqlens) || t >= __ldg(p.cu_seqlens + p.n_seqs)) return -1;
         int lo = 0, hi = p.n_seqs;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;

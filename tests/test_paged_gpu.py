@@ -308,6 +308,29 @@ def test_append_ragged(D, R, inter, kind, page, layout):
     assert torch.equal(got_k, kc0) and torch.equal(got_v, vc0)        # and so does every other slot
 
 
+@pytest.mark.parametrize("first", [1, 5, 13])
+def test_append_tokens_before_the_first_sequence_are_padding(first):
+    """A slice of a larger batch's cu_seqlens beside the whole projection: the tokens in front of it belong to no sequence here."""
+    D, dt, page, H, Hkv = 64, torch.float16, 16, 4, 2
+    lens, new = [100, 3, 20], [10, 3, 4]
+    kc, vc, tab, ks, vs = make_cache(lens, Hkv, D, page, dt, "head", 23, dead=0.5)
+    kc0, vc0 = kc.cpu().clone(), vc.cpu().clone()
+    cu = torch.tensor([first, first + 10, first + 13, first + 17], dtype=torch.int32)
+    T = int(cu[-1]) + 6
+    qkv = torch.randn(T, H + 2 * Hkv, D, generator=torch.Generator().manual_seed(24)).to(dt).cuda()
+    q_out = torch.full((T, H, D), 0.25, dtype=dt, device="cuda")
+    api.attn_paged_append(qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:], kc, vc, tab.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(),
+                          cu_seqlens=cu.cuda(), q_out=q_out)
+    assert api.attn_last_device_status() == 0
+    want_k, want_v, x = kc0.clone(), vc0.clone(), qkv.cpu()
+    want_q = torch.full((T, H, D), 0.25, dtype=dt)
+    for b, (n, m) in enumerate(zip(lens, new)):
+        pos, t = torch.arange(n - m, n), slice(int(cu[b]), int(cu[b + 1]))
+        p = tab[b].long()[pos // page]
+        want_q[t], want_k[p, :, pos % page], want_v[p, :, pos % page] = x[t, :H], x[t, H:H + Hkv], x[t, H + Hkv:]
+    assert torch.equal(q_out.cpu(), want_q) and torch.equal(kc.cpu(), want_k) and torch.equal(vc.cpu(), want_v)
+
+
 def test_append_reports_and_skips_bad_entries():
     D, dt, page = 64, torch.float16, 16
     kc, vc, tab, ks, vs = make_cache([20, 20, 20, 20], 1, D, page, dt, "head", 22, dead=0.0)

@@ -254,7 +254,9 @@ size_t attn_bwd_workspace_bytes(int B, int H, int Sq);
  * 2^31 - 1 - 256.  K/V tiles that no row of a Q tile sees are neither read nor computed, so the time goes with
  * Sq * min(window + sinks, Sk).  A query without a visible key gives O = 0, LSE = -inf.
  * K and V must be finite also where they are hidden (tiles are computed whole: a NaN or infinity in a hidden V row
- * would reach rows of the same tile).  Everything else -- layouts, scale, errors, asynchrony -- as for attn_fwd_gqa.
+ * would reach rows of the same tile).  The sums of P V are kept in fp32, with P relative to a reference that may lag the row's
+ * largest score by a factor of 2^14: largest |V| times visible keys times 2^14 must stay below 2^127.
+ * Everything else -- layouts, scale, errors, asynchrony -- as for attn_fwd_gqa.
  */
 int attn_fwd_window(const void* q, const void* k, const void* v, void* o, float* lse, int B, int H, int Hkv, int Sq, int Sk,
                     int D, float scale, int window, int sinks, int q_offset, int dtype, void* stream);

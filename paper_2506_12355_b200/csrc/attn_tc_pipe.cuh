@@ -222,10 +222,10 @@ attn_fwd_tc_pipe_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
     constexpr int PCOLS = 32 * ES / 4;           // tensor-memory columns of 32 P values
     constexpr float P_OFF = FP8 ? 5.f : 0.f;
     // WINDOW: rows often take their first reference from a tile that shows them one key or a few (the first tokens, the
-    // window's lower edge), and the true maximum then runs further ahead.  P may grow as far as its type goes: up to 2^14 in
-    // fp16; bf16 and the fp32 sums have the exponents for 2^64.  (With 2^8 nearly every item took the rescaling path once:
-    // 45 instead of ~25 us at 32 heads x 1000 queries, window 255, one first token.)
-    constexpr float LAG = FP8 ? 3.f : (WINDOW ? (DTYPE == 0 ? 14.f : 64.f) : 8.f);
+    // window's lower edge), and the true maximum then runs further ahead.  P may grow to 2^14, as far as fp16 goes (with 2^8
+    // nearly every item took the rescaling path once: 45 instead of ~25 us at 32 heads x 1000 queries, window 255, one first
+    // token).  In bf16 as well: every further power of two in P is one less for V before the fp32 sums of P V overflow.
+    constexpr float LAG = FP8 ? 3.f : (WINDOW ? 14.f : 8.f);
     using C = PipeCfg<D, ES>;
     constexpr int BM = C::BM, BN = C::BN, NBOX = C::NBOX, NSLOT = C::NSLOT;
     constexpr int NGRP = NSLOT / 2;   // ring groups in flight (two tile slots each)

@@ -179,6 +179,17 @@ def test_scores_far_below_zero_behind_hidden_tiles():
     run(1, 2, 1, 600, 600, 64, "bf16", 129, 1, 0, scale=1.0, data=(q, k, v, g))
 
 
+@pytest.mark.parametrize("sinks", [0, 2, 40])
+def test_large_values_behind_a_low_first_reference(sinks):
+    """The first keys that a row meets score far below the later ones (by 40, 2^57 in the probabilities), and the values are near
+    2^100: neither the probabilities nor their sums may carry the whole distance, or the products leave fp32 (2^127)."""
+    q, k, v, g = inputs(1, 4, 2, 600, 600, 128, torch.bfloat16, 21)
+    q, k = (1 + 0.01 * q.float()).bfloat16(), (1 + 0.01 * k.float()).bfloat16()
+    k[:, :, :200] = 0                              # scores 0; all later ones about 128 * 0.3125
+    v = (v.float() * 2.0 ** 100).bfloat16()
+    run(1, 4, 2, 600, 600, 128, "bf16", 300, sinks, 0, scale=0.3125, backward=False, data=(q, k, v, g))
+
+
 def test_full_window_is_causal_attention():
     """No lower end: the same operator as the causal calls.  Those evaluate part of the exponentials by a polynomial (2^-13), the
     window kernels do not, so the two are compared within the tolerance that allows for it, on either side of the exact value."""

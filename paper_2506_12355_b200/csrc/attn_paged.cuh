@@ -271,12 +271,15 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     int64_t* scan = reinterpret_cast<int64_t*>(merge);       // at the beginning: [0..31] warp sums, [32..34] the start
     const uint32_t bars = sm100::smem_u32(smem) + NSTAGE * C::STAGE_BYTES + C::MERGE_BYTES;     // [warp][stage]: a chunk has arrived
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + NSTAGE * C::STAGE_BYTES + C::MERGE_BYTES + 8 * NW * NSTAGE);
-    if (tid < NW * NSTAGE) sm100::mbar_init(bars + 8 * tid, 1);
+    if (tid < NW * NSTAGE) {     // a thread per barrier: each fences its own
+        sm100::mbar_init(bars + 8 * tid, 1);
+        sm100::fence_barrier_init();
+        sm100::fence_proxy_async_smem();
+    }
     if (tid == 0) {
         *abort_flag = 0;
         sm100::prefetch_tensormap(&tmK);
         sm100::prefetch_tensormap(&tmV);
-        sm100::fence_barrier_init();
     }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 

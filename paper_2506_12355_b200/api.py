@@ -138,12 +138,10 @@ _UNBOUND = object()
 _binding_module = _UNBOUND
 
 
-def _fast(name, stream, *args):
-    """The call through _binding: its result, or NotImplemented where the Python path has to take it (an explicit stream, tensors
-    of another device than the current one, anything that needs a message)."""
+def _fast(name, *args):
+    """The call through _binding: its result, or NotImplemented where the Python path has to take it (tensors of another device
+    than the current one, anything that needs a message)."""
     global _binding_module
-    if stream is not None:
-        return NotImplemented
     if _binding_module is _UNBOUND:
         _binding_module = _bind()
     if _binding_module is None:
@@ -174,14 +172,31 @@ def _stream_ptr(stream) -> int:
     return int(stream.cuda_stream)
 
 
-def _call(name, device, stream, *args):
-    """The C entry point `name` with `args` and the stream, on `device`; raises AttnError for a status other than ATTN_OK."""
+def _on_stream(stream, tensor, fn, *args, **kwargs):
+    """fn(*args, **kwargs) with `stream` as torch's current stream, on `tensor`'s device.  The outputs and workspaces that the call
+    allocates then come from `stream`'s pool: out of another stream's they might still be in use by that stream's earlier work, and a
+    workspace, dropped when the call returns, would be handed out there again while the kernels on `stream` use it."""
+    if tensor.is_cuda:
+        device, handle = tensor.device, int(stream.cuda_stream)
+        if handle == 0:
+            stream = torch.cuda.default_stream(device)
+        elif not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(handle, device=device)
+        if stream.device != device:
+            raise ValueError("the stream belongs to %s, the tensors to %s" % (stream.device, device))
+        with torch.cuda.stream(stream):
+            return fn(*args, **kwargs)
+    return fn(*args, **kwargs)      # which says what is wrong
+
+
+def _call(name, device, *args):
+    """The C entry point `name` with `args` and torch's current stream of `device`; raises AttnError for a status other than ATTN_OK."""
     fn = getattr(_lib or load(), name)
     if device.index == torch.cuda.current_device():
-        rc = fn(*args, _stream_ptr(stream))
+        rc = fn(*args, _stream_ptr(None))
     else:
         with torch.cuda.device(device):
-            rc = fn(*args, _stream_ptr(stream))
+            rc = fn(*args, _stream_ptr(None))
     if rc != 0:
         raise AttnError(rc, name)
 
@@ -227,6 +242,8 @@ def _outputs(q, B, H, Sq, Dv, out, lse, dtype=None):
 
 
 def _call_device(fn_name, q, k, v, scale, causal, out, lse, stream):
+    if stream is not None and (out is None or lse is None):
+        return _on_stream(stream, q, _call_device, fn_name, q, k, v, scale, causal, out, lse, None)
     B, H, Sq, Sk, D = _check_qkv(q, k, v)
     if not (q.is_cuda and k.is_cuda and v.is_cuda):
         raise ValueError("q, k, v must be CUDA tensors")
@@ -244,13 +261,16 @@ def _call_device(fn_name, q, k, v, scale, causal, out, lse, stream):
 def attn_fwd(q, k, v, scale: float, causal: bool = False, out=None, lse=None, stream=None):
     """O [B,H,Sq,D] (dtype of q) and LSE [B,H,Sq] (fp32) on the tensor-core kernel.
 
-    Enqueues on `stream` (default: torch's current stream) and returns without synchronising.
+    Enqueues on `stream` (default: torch's current stream) and returns without synchronising.  As under torch.cuda.stream(stream),
+    what a call allocates belongs to its stream; inputs and given outputs are the caller's to order against it.
     """
     return _call_device("attn_fwd", q, k, v, scale, causal, out, lse, stream)
 
 
 def attn_fwd_gqa(q, k, v, scale: float, causal: bool = False, out=None, lse=None, stream=None):
     """Grouped-query / multi-query attention: q [B,H,Sq,D], k, v [B,Hkv,Sk,D] with H % Hkv == 0."""
+    if stream is not None and (out is None or lse is None):
+        return _on_stream(stream, q, attn_fwd_gqa, q, k, v, scale, causal, out, lse)
     B, H, Hkv, Sq, Sk, D, _ = _check_grouped(q, k, v)
     dt = _dtype_code(q)
     out, lse = _outputs(q, B, H, Sq, D, out, lse)
@@ -265,6 +285,8 @@ def attn_fwd_gqa(q, k, v, scale: float, causal: bool = False, out=None, lse=None
 def attn_fwd_partial(q, k, v, scale: float, causal: bool, k_offset: int, out=None, lse=None, stream=None):
     """Attention over one K/V shard whose first key has global index k_offset: q [B,H,Sq,D],
     k, v [B,Hkv,Sk_shard,D].  Returns the shard's normalised O_r and LSE_r (merge with attn_combine)."""
+    if stream is not None and (out is None or lse is None):
+        return _on_stream(stream, q, attn_fwd_partial, q, k, v, scale, causal, k_offset, out, lse)
     B, H, Hkv, Sq, Sk, D, _ = _check_grouped(q, k, v)
     dt = _dtype_code(q)
     out, lse = _outputs(q, B, H, Sq, D, out, lse)
@@ -279,6 +301,8 @@ def attn_fwd_partial(q, k, v, scale: float, causal: bool, k_offset: int, out=Non
 
 def attn_combine(o_parts, lse_parts, out=None, lse=None, stream=None):
     """Merges partial results: o_parts [n,B,H,Sq,D] (16-bit), lse_parts [n,B,H,Sq] (fp32)."""
+    if stream is not None and (out is None or lse is None):
+        return _on_stream(stream, o_parts, attn_combine, o_parts, lse_parts, out, lse)
     n, B, H, Sq, D = o_parts.shape
     if tuple(lse_parts.shape) != (n, B, H, Sq) or lse_parts.dtype != torch.float32:
         raise ValueError("lse_parts must be fp32 [n,B,H,Sq]")
@@ -323,6 +347,8 @@ def attn_combine_gather(o_part_ptrs, lse_part_ptrs, shape, dtype, out, lse, row_
 def attn_fwd_qkv_dims(q, k, v, scale: float, causal: bool = False, out=None, lse=None, stream=None):
     """Attention with separate Q/K and V head dims (the 192/128 MLA head shape): q [B,H,Sq,Dqk],
     k [B,Hkv,Sk,Dqk], v [B,Hkv,Sk,Dv]; returns o [B,H,Sq,Dv] and lse [B,H,Sq]."""
+    if stream is not None and (out is None or lse is None):
+        return _on_stream(stream, q, attn_fwd_qkv_dims, q, k, v, scale, causal, out, lse)
     B, H, Hkv, Sq, Sk, Dqk, Dv = _check_grouped(q, k, v, same_v_dim=False)
     dt = _dtype_code(q)
     out, lse = _outputs(q, B, H, Sq, Dv, out, lse)
@@ -343,6 +369,8 @@ def attn_fwd_splitkv(q, k, v, scale: float, causal: bool, n_splits: int, workspa
     """attn_fwd_gqa with the keys split into n_splits ranges that run concurrently, then merged (split-KV
     decoding).  `workspace`: CUDA uint8 tensor of at least attn_fwd_splitkv_workspace_bytes(...) bytes
     (allocated here when None)."""
+    if stream is not None and (out is None or lse is None or workspace is None):
+        return _on_stream(stream, q, attn_fwd_splitkv, q, k, v, scale, causal, n_splits, workspace, out, lse)
     B, H, Hkv, Sq, Sk, D, _ = _check_grouped(q, k, v)
     dt = _dtype_code(q)
     if workspace is None:
@@ -362,6 +390,8 @@ def attn_fwd_fp8(q, k, v, scale: float, q_factor: float = 1.0, k_factor: float =
     """Attention on E4M3 inputs with one dequantisation factor per tensor: q [B,H,Sq,128],
     k, v [B,Hkv,Sk,128] as CUDA uint8 (or torch.float8_e4m3fn) tensors; returns o (bf16) and lse (fp32).
     impl 0: tensor-core kernel; impl 1: CUDA-core cross-check kernel."""
+    if stream is not None and (out is None or lse is None):
+        return _on_stream(stream, q, attn_fwd_fp8, q, k, v, scale, q_factor, k_factor, v_factor, causal, out, lse, impl=impl)
     if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
         raise ValueError("q, k, v must be [B,H,S,D]")
     for t in (q, k, v):
@@ -393,6 +423,8 @@ def attn_bwd(q, k, v, o, lse, dout, scale: float, causal: bool = False, dq=None,
     """Gradients (dq, dk, dv) of the attention output for the upstream gradient dout: q, o, dout [B,H,Sq,D];
     k, v [B,Hkv,Sk,D]; lse [B,H,Sq] fp32; o and lse from the forward call on the same inputs.  D in {64, 128}.
     `workspace`: CUDA uint8 tensor of at least attn_bwd_workspace_bytes(B, H, Sq) bytes (allocated here when None)."""
+    if stream is not None and (dq is None or dk is None or dv is None or workspace is None):
+        return _on_stream(stream, q, attn_bwd, q, k, v, o, lse, dout, scale, causal, dq, dk, dv, workspace)
     B, H, Hkv, Sq, Sk, D, _ = _check_grouped(q, k, v)
     if tuple(o.shape) != tuple(q.shape) or tuple(dout.shape) != tuple(q.shape):
         raise ValueError("o and dout must have q's shape")
@@ -421,7 +453,9 @@ def attn_bwd(q, k, v, o, lse, dout, scale: float, causal: bool = False, dq=None,
 def attn_fwd_window(q, k, v, scale: float, window: int, sinks: int = 0, q_offset: int = 0, out=None, lse=None, stream=None):
     """Attention under a sliding window: q [B,H,Sq,D] at positions q_offset, q_offset + 1, .., k, v [B,Hkv,Sk,D] (D in {64, 128});
     key j is visible at position p iff j <= p and (j > p - window or j < sinks); window 0: no lower end."""
-    result = _fast("attn_fwd_window", stream, q, k, v, scale, window, sinks, q_offset, out, lse)
+    if stream is not None:
+        return _on_stream(stream, q, attn_fwd_window, q, k, v, scale, window, sinks, q_offset, out, lse)
+    result = _fast("attn_fwd_window", q, k, v, scale, window, sinks, q_offset, out, lse)
     if result is not NotImplemented:
         return result
     B, H, Hkv, Sq, Sk, D, _ = _check_grouped(q, k, v)
@@ -434,7 +468,7 @@ def attn_fwd_window(q, k, v, scale: float, window: int, sinks: int = 0, q_offset
         lse = torch.empty((B, H, Sq), dtype=torch.float32, device=device)
     else:
         _require(lse, "lse", (B, H, Sq), torch.float32, device)
-    _call("attn_fwd_window", device, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H, Hkv, Sq, Sk, D,
+    _call("attn_fwd_window", device, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H, Hkv, Sq, Sk, D,
           float(scale), int(window), int(sinks), int(q_offset), dt)
     return out, lse
 
@@ -447,7 +481,9 @@ def attn_bwd_window(q, k, v, o, lse, dout, scale: float, window: int, sinks: int
                     workspace=None, stream=None):
     """Gradients (dq, dk, dv) of attn_fwd_window's output for the upstream gradient dout; o and lse from the forward call.
     `workspace`: CUDA uint8 tensor of at least attn_bwd_window_workspace_bytes(...) bytes (allocated here when None)."""
-    result = _fast("attn_bwd_window", stream, q, k, v, o, lse, dout, scale, window, sinks, q_offset, dq, dk, dv, workspace)
+    if stream is not None:
+        return _on_stream(stream, q, attn_bwd_window, q, k, v, o, lse, dout, scale, window, sinks, q_offset, dq, dk, dv, workspace)
+    result = _fast("attn_bwd_window", q, k, v, o, lse, dout, scale, window, sinks, q_offset, dq, dk, dv, workspace)
     if result is not NotImplemented:
         return result
     B, H, Hkv, Sq, Sk, D, _ = _check_grouped(q, k, v)
@@ -465,7 +501,7 @@ def attn_bwd_window(q, k, v, o, lse, dout, scale: float, window: int, sinks: int
     if workspace is None:
         n = attn_bwd_window_workspace_bytes(B, H, Hkv, Sq, Sk, D, window, sinks, q_offset)
         workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=device)
-    _call("attn_bwd_window", device, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), dout.data_ptr(),
+    _call("attn_bwd_window", device, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), dout.data_ptr(),
           dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, H, Hkv, Sq, Sk, D, float(scale), int(window), int(sinks), int(q_offset), dt, workspace.data_ptr(),
           _bytes(workspace))
     return dq, dk, dv
@@ -543,7 +579,9 @@ def attn_qk_norm_rope(q, k, v, q_weight, k_weight, cos_sin, positions=None, eps:
     copied to v_out [B,Hkv,S,D].  q_weight, k_weight: [D] in q's dtype or float32 (None: not normalised); cos_sin: float32
     [positions, R], R/2 cosines then R/2 sines per position (None: not rotated); positions: int32 [B,S] (None: 0 .. S-1);
     interleaved: pairs (2i, 2i+1) instead of (i, i + R/2)."""
-    result = _fast("attn_qk_norm_rope", stream, q, k, v, q_weight, k_weight, cos_sin, positions, eps, interleaved, q_out, k_out, v_out)
+    if stream is not None:
+        return _on_stream(stream, q, attn_qk_norm_rope, q, k, v, q_weight, k_weight, cos_sin, positions, eps, interleaved, q_out, k_out, v_out)
+    result = _fast("attn_qk_norm_rope", q, k, v, q_weight, k_weight, cos_sin, positions, eps, interleaved, q_out, k_out, v_out)
     if result is not NotImplemented:
         return result
     if q.dim() != 4 or k.dim() != 4:
@@ -579,7 +617,7 @@ def attn_qk_norm_rope(q, k, v, q_weight, k_weight, cos_sin, positions=None, eps:
             v_out = torch.empty(kv_shape, dtype=dtype, device=device)
         else:
             _require(v_out, "v_out", kv_shape, dtype, device)
-    _call("attn_qk_norm_rope", device, stream, q.data_ptr(), k.data_ptr(), _ptr(v), _rows3(q, k, v), _ptr(q_weight), _ptr(k_weight), f32,
+    _call("attn_qk_norm_rope", device, q.data_ptr(), k.data_ptr(), _ptr(v), _rows3(q, k, v), _ptr(q_weight), _ptr(k_weight), f32,
           _ptr(cos_sin), n_pos, R, bool(interleaved), _ptr(positions), float(eps), q_out.data_ptr(), k_out.data_ptr(), _ptr(v_out), B, S, H,
           Hkv, D, dt)
     return q_out, k_out, v_out
@@ -595,7 +633,10 @@ def attn_qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positio
     outputs, q [B,S,H,D], k [B,S,Hkv,D] its inputs.  Returns (dq_in [B,S,H,D], dk_in, dv_in [B,S,Hkv,D], dq_weight, dk_weight
     (float32 [D], None without a weight)).  dq_in, dk_in, dv_in may be given as strided views of one buffer.
     `workspace`: CUDA uint8 tensor of at least attn_qk_norm_rope_bwd_workspace_bytes(D) bytes (allocated here when None)."""
-    result = _fast("attn_qk_norm_rope_bwd", stream, dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positions, eps, interleaved, dq_in, dk_in, dv_in,
+    if stream is not None:
+        return _on_stream(stream, q, attn_qk_norm_rope_bwd, dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positions, eps, interleaved, dq_in, dk_in, dv_in,
+                          workspace)
+    result = _fast("attn_qk_norm_rope_bwd", dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positions, eps, interleaved, dq_in, dk_in, dv_in,
                    workspace)
     if result is not NotImplemented:
         return result
@@ -634,7 +675,7 @@ def attn_qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positio
     dkw = None if k_weight is None else torch.empty(D, dtype=torch.float32, device=device)
     if workspace is None:
         workspace = torch.empty(max(attn_qk_norm_rope_bwd_workspace_bytes(D), 256), dtype=torch.uint8, device=device)
-    _call("attn_qk_norm_rope_bwd", device, stream, dq.data_ptr(), dk.data_ptr(), _ptr(dv), q.data_ptr(), k.data_ptr(), _rows3(q, k),
+    _call("attn_qk_norm_rope_bwd", device, dq.data_ptr(), dk.data_ptr(), _ptr(dv), q.data_ptr(), k.data_ptr(), _rows3(q, k),
           _ptr(q_weight), _ptr(k_weight), f32, _ptr(cos_sin), n_pos, R, bool(interleaved), _ptr(positions), float(eps), dq_in.data_ptr(),
           dk_in.data_ptr(), _ptr(dv_in), _rows3(dq_in, dk_in, dv_in), _ptr(dqw), _ptr(dkw), B, S, H, Hkv, D, dt, workspace.data_ptr(),
           _bytes(workspace))
@@ -671,7 +712,10 @@ def attn_paged_append(q, k, v, k_cache, v_cache, block_table, seq_lens, q_weight
     cu_seqlens int32 [B+1]: first new token of each sequence and the end (None: one token per sequence, T == B).  Tokens
     before the first and behind the end, and of sequences of length 0, are padding: nothing is written for them.  Returns
     q_out [T,H,D]."""
-    result = _fast("attn_paged_append", stream, q, k, v, k_cache, v_cache, block_table, seq_lens, q_weight, k_weight, cos_sin, cu_seqlens, eps,
+    if stream is not None:
+        return _on_stream(stream, k, attn_paged_append, q, k, v, k_cache, v_cache, block_table, seq_lens, q_weight, k_weight, cos_sin, cu_seqlens, eps, interleaved,
+                          q_out)
+    result = _fast("attn_paged_append", q, k, v, k_cache, v_cache, block_table, seq_lens, q_weight, k_weight, cos_sin, cu_seqlens, eps,
                    interleaved, q_out)
     if result is not NotImplemented:
         return result
@@ -708,7 +752,7 @@ def attn_paged_append(q, k, v, k_cache, v_cache, block_table, seq_lens, q_weight
     elif T != n_seqs:
         raise ValueError("without cu_seqlens there is one token per sequence: %d tokens, %d sequences" % (T, n_seqs))
     ks, vs = k.stride(), v.stride()
-    _call("attn_paged_append", device, stream, _ptr(q), k.data_ptr(), v.data_ptr(), _strides(qs[0], qs[1], ks[0], ks[1], vs[0], vs[1]),
+    _call("attn_paged_append", device, _ptr(q), k.data_ptr(), v.data_ptr(), _strides(qs[0], qs[1], ks[0], ks[1], vs[0], vs[1]),
           _ptr(q_weight), _ptr(k_weight), f32, _ptr(cos_sin), n_pos, R, bool(interleaved), float(eps), _ptr(q_out), k_cache.data_ptr(),
           v_cache.data_ptr(), cache_strides, pages, page_size, block_table.data_ptr(), block_table.stride(0), width,
           seq_lens.data_ptr(), _ptr(cu_seqlens), n_seqs, T, H, Hkv, D, dt)
@@ -724,7 +768,9 @@ def attn_paged_decode(q, k_cache, v_cache, block_table, seq_lens, scale: float, 
     """Attention of one new token per sequence, q [B,H,D], over a paged cache (see attn_paged_append): keys below seq_lens[b],
     and with window > 0 only the last `window` of them and the first `sinks`.  Returns o [B,H,D] and lse [B,H] (float32).
     `workspace`: CUDA uint8 tensor of at least attn_paged_decode_workspace_bytes(H, Hkv, D) bytes (allocated here when None)."""
-    result = _fast("attn_paged_decode", stream, q, k_cache, v_cache, block_table, seq_lens, scale, window, sinks, out, lse, workspace)
+    if stream is not None:
+        return _on_stream(stream, q, attn_paged_decode, q, k_cache, v_cache, block_table, seq_lens, scale, window, sinks, out, lse, workspace)
+    result = _fast("attn_paged_decode", q, k_cache, v_cache, block_table, seq_lens, scale, window, sinks, out, lse, workspace)
     if result is not NotImplemented:
         return result
     if q.dim() != 3:
@@ -748,7 +794,7 @@ def attn_paged_decode(q, k_cache, v_cache, block_table, seq_lens, scale: float, 
         _require(lse, "lse", (B, H), torch.float32, device)
     if workspace is None:
         workspace = torch.empty(max(attn_paged_decode_workspace_bytes(H, Hkv, D), 256), dtype=torch.uint8, device=device)
-    _call("attn_paged_decode", device, stream, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), cache_strides, pages, page_size,
+    _call("attn_paged_decode", device, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), cache_strides, pages, page_size,
           block_table.data_ptr(), block_table.stride(0), width, seq_lens.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H,
           Hkv, D, float(scale), int(window), int(sinks), dt, workspace.data_ptr(), _bytes(workspace))
     return out, lse

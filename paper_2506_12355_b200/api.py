@@ -241,6 +241,19 @@ def _outputs(q, B, H, Sq, Dv, out, lse, dtype=None):
     return out, lse
 
 
+def _workspace(workspace, bytes, device):
+    """The caller's workspace, whose size the entry point checks (its address goes to the kernels as it is), or a new one."""
+    if workspace is None:
+        return torch.empty(max(bytes, 256), dtype=torch.uint8, device=device)
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on %s" % (device,))
+    return workspace
+
+
+def _bytes(workspace):
+    return workspace.numel() * workspace.element_size()
+
+
 def _call_device(fn_name, q, k, v, scale, causal, out, lse, stream):
     if stream is not None and (out is None or lse is None):
         return _on_stream(stream, q, _call_device, fn_name, q, k, v, scale, causal, out, lse, None)
@@ -373,13 +386,12 @@ def attn_fwd_splitkv(q, k, v, scale: float, causal: bool, n_splits: int, workspa
         return _on_stream(stream, q, attn_fwd_splitkv, q, k, v, scale, causal, n_splits, workspace, out, lse)
     B, H, Hkv, Sq, Sk, D, _ = _check_grouped(q, k, v)
     dt = _dtype_code(q)
-    if workspace is None:
-        workspace = torch.empty(attn_fwd_splitkv_workspace_bytes(B, H, Sq, D, n_splits), dtype=torch.uint8, device=q.device)
+    workspace = _workspace(workspace, attn_fwd_splitkv_workspace_bytes(B, H, Sq, D, n_splits), q.device)
     out, lse = _outputs(q, B, H, Sq, D, out, lse)
     with torch.cuda.device(q.device):
         rc = load().attn_fwd_splitkv(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
                                      B, H, Hkv, Sq, Sk, D, float(scale), int(bool(causal)), dt, int(n_splits),
-                                     workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
+                                     workspace.data_ptr(), _bytes(workspace), _stream_ptr(stream))
     if rc != 0:
         raise AttnError(rc, "attn_fwd_splitkv")
     return out, lse
@@ -439,12 +451,11 @@ def attn_bwd(q, k, v, o, lse, dout, scale: float, causal: bool = False, dq=None,
     dq = torch.empty_like(q) if dq is None else dq
     dk = torch.empty_like(k) if dk is None else dk
     dv = torch.empty_like(v) if dv is None else dv
-    if workspace is None:
-        workspace = torch.empty(max(attn_bwd_workspace_bytes(B, H, Sq), 256), dtype=torch.uint8, device=q.device)
+    workspace = _workspace(workspace, attn_bwd_workspace_bytes(B, H, Sq), q.device)
     with torch.cuda.device(q.device):
         rc = load().attn_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), dout.data_ptr(),
                              dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, H, Hkv, Sq, Sk, D, float(scale),
-                             int(bool(causal)), dt, workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
+                             int(bool(causal)), dt, workspace.data_ptr(), _bytes(workspace), _stream_ptr(stream))
     if rc != 0:
         raise AttnError(rc, "attn_bwd")
     return dq, dk, dv
@@ -498,9 +509,7 @@ def attn_bwd_window(q, k, v, o, lse, dout, scale: float, window: int, sinks: int
     _require(dq, "dq", q_shape, dtype, device)
     _require(dk, "dk", k_shape, dtype, device)
     _require(dv, "dv", k_shape, dtype, device)
-    if workspace is None:
-        n = attn_bwd_window_workspace_bytes(B, H, Hkv, Sq, Sk, D, window, sinks, q_offset)
-        workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+    workspace = _workspace(workspace, attn_bwd_window_workspace_bytes(B, H, Hkv, Sq, Sk, D, window, sinks, q_offset), device)
     _call("attn_bwd_window", device, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), dout.data_ptr(),
           dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, H, Hkv, Sq, Sk, D, float(scale), int(window), int(sinks), int(q_offset), dt, workspace.data_ptr(),
           _bytes(workspace))
@@ -673,17 +682,12 @@ def attn_qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positio
             _require(dv_in, "dv_in", k_shape, dtype, device, False)
     dqw = None if q_weight is None else torch.empty(D, dtype=torch.float32, device=device)
     dkw = None if k_weight is None else torch.empty(D, dtype=torch.float32, device=device)
-    if workspace is None:
-        workspace = torch.empty(max(attn_qk_norm_rope_bwd_workspace_bytes(D), 256), dtype=torch.uint8, device=device)
+    workspace = _workspace(workspace, attn_qk_norm_rope_bwd_workspace_bytes(D), device)
     _call("attn_qk_norm_rope_bwd", device, dq.data_ptr(), dk.data_ptr(), _ptr(dv), q.data_ptr(), k.data_ptr(), _rows3(q, k),
           _ptr(q_weight), _ptr(k_weight), f32, _ptr(cos_sin), n_pos, R, bool(interleaved), _ptr(positions), float(eps), dq_in.data_ptr(),
           dk_in.data_ptr(), _ptr(dv_in), _rows3(dq_in, dk_in, dv_in), _ptr(dqw), _ptr(dkw), B, S, H, Hkv, D, dt, workspace.data_ptr(),
           _bytes(workspace))
     return dq_in, dk_in, dv_in, dqw, dkw
-
-
-def _bytes(workspace):
-    return workspace.numel() * workspace.element_size()
 
 
 def _check_cache(D, dtype, device, k_cache, v_cache, block_table, seq_lens):
@@ -792,8 +796,7 @@ def attn_paged_decode(q, k_cache, v_cache, block_table, seq_lens, scale: float, 
         lse = torch.empty((B, H), dtype=torch.float32, device=device)
     else:
         _require(lse, "lse", (B, H), torch.float32, device)
-    if workspace is None:
-        workspace = torch.empty(max(attn_paged_decode_workspace_bytes(H, Hkv, D), 256), dtype=torch.uint8, device=device)
+    workspace = _workspace(workspace, attn_paged_decode_workspace_bytes(H, Hkv, D), device)
     _call("attn_paged_decode", device, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), cache_strides, pages, page_size,
           block_table.data_ptr(), block_table.stride(0), width, seq_lens.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H,
           Hkv, D, float(scale), int(window), int(sinks), dt, workspace.data_ptr(), _bytes(workspace))

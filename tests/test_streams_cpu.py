@@ -11,11 +11,11 @@ from paper_2506_12355_b200 import api
 
 
 class Tensor:
-    """What the binding asks of a tensor; contiguous unless given strides."""
+    """What the binding asks of a tensor."""
     next_address = 1 << 20
 
-    def __init__(self, shape, dtype, device=0, stream=None):
-        self.shape, self.dtype, self.stream = torch.Size(shape), dtype, stream
+    def __init__(self, shape, dtype, device=0, stream=None, dense=True):
+        self.shape, self.dtype, self.stream, self.dense = torch.Size(shape), dtype, stream, dense
         self.device = torch.device("cuda", device) if isinstance(device, int) else device
         self.address = Tensor.next_address
         Tensor.next_address += 1 << 20
@@ -36,7 +36,7 @@ class Tensor:
         return tuple(s) if axis is None else s[axis]
 
     def is_contiguous(self):
-        return True
+        return self.dense
 
     def numel(self):
         return self.shape.numel()
@@ -179,3 +179,40 @@ def test_a_handle_of_another_library_is_wrapped(world, handle):
         calls(device)["attn_paged_decode"](types.SimpleNamespace(cuda_stream=handle))
         assert world.launches.pop() == ("attn_paged_decode", handle)
         assert all(t.stream.cuda_stream == handle and t.stream.device.index == t.device.index for t in world.made)
+
+
+def workspace_calls():
+    """name -> a call of every entry point that takes a workspace, taking that."""
+    def t(*shape, dtype=F16):
+        return Tensor(shape, dtype)
+    q, k, v = t(B, H, S, D), t(B, HKV, S, D), t(B, HKV, S, D)
+    lse, w, tab = t(B, H, S, dtype=F32), t(D), t(S, D, dtype=F32)
+    qt, kt = t(B, S, H, D), t(B, S, HKV, D)
+    kc, table, lens = t(PAGES, HKV, PAGE, D), t(B, 3, dtype=I32), t(B, dtype=I32)
+    return dict(
+        attn_fwd_splitkv=lambda x, **s: api.attn_fwd_splitkv(q, k, v, 0.1, False, 2, workspace=x, **s),
+        attn_bwd=lambda x, **s: api.attn_bwd(q, k, v, q, lse, q, 0.1, workspace=x, **s),
+        attn_bwd_window=lambda x, **s: api.attn_bwd_window(q, k, v, q, lse, q, 0.1, 8, 1, workspace=x, **s),
+        attn_qk_norm_rope_bwd=lambda x, **s: api.attn_qk_norm_rope_bwd(q, k, v, qt, kt, w, w, tab, workspace=x, **s),
+        attn_paged_decode=lambda x, **s: api.attn_paged_decode(t(B, H, D), kc, kc, table, lens, 0.1, workspace=x, **s),
+    )
+
+
+@pytest.mark.parametrize("name", sorted(workspace_calls()))
+def test_a_workspace_lies_on_the_calls_device(world, name):
+    """Its address goes to the kernels as it is: host memory, another GPU's, or a view with gaps is refused before a launch."""
+    call = workspace_calls()[name]
+    for bad in (Tensor((8192,), torch.uint8, torch.device("cpu")), Tensor((8192,), torch.uint8, 1), Tensor((8192,), torch.uint8, 0, dense=False)):
+        for stream in (None, Stream(81)):
+            with pytest.raises(ValueError):
+                call(bad, stream=stream)
+    assert not world.launches
+    call(Tensor((8192,), torch.uint8))
+    assert [n for n, _ in world.launches] == [name]
+
+
+def test_a_workspace_of_another_type_counts_in_bytes(world, monkeypatch):
+    seen = []
+    world.attn_bwd = lambda *args: seen.append(args[-2]) or 0
+    workspace_calls()["attn_bwd"](Tensor((2048,), F32))
+    assert seen == [8192]

@@ -227,8 +227,8 @@ def _check_grouped(q, k, v, same_v_dim=True):
         raise ValueError("k must be [B,Hkv,Sk,D] and v [B,Hkv,Sk,%s] matching q's B and D" % ("D" if same_v_dim else "Dv"))
     if not (q.is_contiguous() and k.is_contiguous() and v.is_contiguous()):
         raise ValueError("q, k, v must be contiguous")
-    if not (q.is_cuda and k.is_cuda and v.is_cuda) or not (q.dtype == k.dtype == v.dtype):
-        raise ValueError("q, k, v must be CUDA tensors of one dtype")
+    if not q.is_cuda or not (q.device == k.device == v.device) or not (q.dtype == k.dtype == v.dtype):
+        raise ValueError("q, k, v must be CUDA tensors of one device and dtype")
     return B, H, Hkv, Sq, Sk, D, Dv
 
 
@@ -258,8 +258,8 @@ def _call_device(fn_name, q, k, v, scale, causal, out, lse, stream):
     if stream is not None and (out is None or lse is None):
         return _on_stream(stream, q, _call_device, fn_name, q, k, v, scale, causal, out, lse, None)
     B, H, Sq, Sk, D = _check_qkv(q, k, v)
-    if not (q.is_cuda and k.is_cuda and v.is_cuda):
-        raise ValueError("q, k, v must be CUDA tensors")
+    if not q.is_cuda or not (q.device == k.device == v.device):
+        raise ValueError("q, k, v must be CUDA tensors of one device")
     dt = _dtype_code(q)
     out, lse = _outputs(q, B, H, Sq, D, out, lse)
     with torch.cuda.device(q.device):
@@ -319,8 +319,8 @@ def attn_combine(o_parts, lse_parts, out=None, lse=None, stream=None):
     n, B, H, Sq, D = o_parts.shape
     if tuple(lse_parts.shape) != (n, B, H, Sq) or lse_parts.dtype != torch.float32:
         raise ValueError("lse_parts must be fp32 [n,B,H,Sq]")
-    if not (o_parts.is_contiguous() and lse_parts.is_contiguous() and o_parts.is_cuda and lse_parts.is_cuda):
-        raise ValueError("o_parts, lse_parts must be contiguous CUDA tensors")
+    if not (o_parts.is_contiguous() and lse_parts.is_contiguous() and o_parts.is_cuda and lse_parts.device == o_parts.device):
+        raise ValueError("o_parts, lse_parts must be contiguous CUDA tensors of one device")
     dt = _dtype_code(o_parts)
     if out is None:
         out = torch.empty((B, H, Sq, D), dtype=o_parts.dtype, device=o_parts.device)
@@ -407,8 +407,8 @@ def attn_fwd_fp8(q, k, v, scale: float, q_factor: float = 1.0, k_factor: float =
     if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
         raise ValueError("q, k, v must be [B,H,S,D]")
     for t in (q, k, v):
-        if t.dtype not in (torch.uint8, torch.float8_e4m3fn) or not t.is_cuda or not t.is_contiguous():
-            raise ValueError("q, k, v must be contiguous CUDA tensors of E4M3 bytes")
+        if t.dtype not in (torch.uint8, torch.float8_e4m3fn) or not t.is_cuda or t.device != q.device or not t.is_contiguous():
+            raise ValueError("q, k, v must be contiguous CUDA tensors of E4M3 bytes on one device")
     B, H, Sq, D = q.shape
     Hkv, Sk = k.shape[1], k.shape[2]
     if tuple(k.shape) != (B, Hkv, Sk, D) or tuple(v.shape) != (B, Hkv, Sk, D):
@@ -443,8 +443,8 @@ def attn_bwd(q, k, v, o, lse, dout, scale: float, causal: bool = False, dq=None,
     if tuple(lse.shape) != (B, H, Sq) or lse.dtype != torch.float32:
         raise ValueError("lse must be fp32 [B,H,Sq]")
     for t in (o, dout, lse):
-        if not (t.is_cuda and t.is_contiguous()):
-            raise ValueError("o, dout, lse must be contiguous CUDA tensors")
+        if t.device != q.device or not t.is_contiguous():
+            raise ValueError("o, dout, lse must be contiguous CUDA tensors on q's device")
     if not (q.dtype == o.dtype == dout.dtype):
         raise TypeError("q, k, v, o, dout must share one dtype")
     dt = _dtype_code(q)

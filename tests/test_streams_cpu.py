@@ -216,3 +216,23 @@ def test_a_workspace_of_another_type_counts_in_bytes(world, monkeypatch):
     world.attn_bwd = lambda *args: seen.append(args[-2]) or 0
     workspace_calls()["attn_bwd"](Tensor((2048,), F32))
     assert seen == [8192]
+
+
+def test_inputs_of_two_devices_are_refused(world):
+    """One call reads memory of one GPU: a tensor of another would reach the kernels as an address that they may not read."""
+    def t(*shape, dtype=F16, device=0):
+        return Tensor(shape, dtype, device)
+    q, k = t(B, H, S, D), t(B, HKV, S, D)
+    lse, far_q, far_k, far_lse = t(B, H, S, dtype=F32), t(B, H, S, D, device=1), t(B, HKV, S, D, device=1), t(B, H, S, dtype=F32, device=1)
+    b8, far_b8 = t(B, H, S, 128, dtype=torch.uint8), t(B, H, S, 128, dtype=torch.uint8, device=1)
+    for call in (lambda: api.attn_fwd(q, far_q, q, 0.1), lambda: api.attn_fwd(q, q, far_q, 0.1), lambda: api.attn_fwd_simt(far_q, q, q, 0.1),
+                 lambda: api.attn_fwd_gqa(q, far_k, k, 0.1), lambda: api.attn_fwd_partial(q, k, far_k, 0.1, False, 0),
+                 lambda: api.attn_fwd_qkv_dims(q, k, far_k, 0.1), lambda: api.attn_fwd_splitkv(q, far_k, far_k, 0.1, False, 2),
+                 lambda: api.attn_fwd_fp8(b8, far_b8, b8, 0.1), lambda: api.attn_combine(t(3, B, H, S, D), t(3, B, H, S, dtype=F32, device=1)),
+                 lambda: api.attn_fwd_window(q, far_k, k, 0.1, 8), lambda: api.attn_fwd_window(q, k, far_k, 0.1, 8),
+                 lambda: api.attn_bwd_window(q, k, far_k, q, lse, q, 0.1, 8), lambda: api.attn_bwd_window(q, k, k, far_q, lse, q, 0.1, 8),
+                 lambda: api.attn_bwd(q, far_k, k, q, lse, q, 0.1), lambda: api.attn_bwd(q, k, k, far_q, lse, q, 0.1),
+                 lambda: api.attn_bwd(q, k, k, q, far_lse, q, 0.1), lambda: api.attn_bwd(q, k, k, q, lse, far_q, 0.1)):
+        with pytest.raises(ValueError):
+            call()
+    assert not world.launches

@@ -287,7 +287,9 @@ int launch_tc_pipe(const void* q, const void* k, const void* v, void* o, float* 
     // (none under a window: with a handful of keys per row the polynomial's 7.5e-5 would stand in the LSE as it is)
     constexpr int PN = WINDOW ? 0 : DTYPE == ATTN_DTYPE_FP8_E4M3 ? ATTN_FP8_POLY_NUM : (D == 64 ? ATTN_POLY64_NUM : ATTN_POLY_NUM);
     constexpr int PD = WINDOW ? 1 : DTYPE == ATTN_DTYPE_FP8_E4M3 ? ATTN_FP8_POLY_DEN : (D == 64 ? ATTN_POLY64_DEN : ATTN_POLY_DEN);
-    auto kern = n_splits > 1 ? attn_tc::attn_fwd_tc_pipe_kernel<D, DTYPE, PN, PD, !WINDOW> : attn_tc::attn_fwd_tc_pipe_kernel<D, DTYPE, PN, PD, false, WINDOW>;
+    auto kern = attn_tc::attn_fwd_tc_pipe_kernel<D, DTYPE, PN, PD, false, WINDOW>;
+    if constexpr (!WINDOW && DTYPE != ATTN_DTYPE_FP8_E4M3)       // the calls that cut the keys into ranges have neither
+        if (n_splits > 1) kern = attn_tc::attn_fwd_tc_pipe_kernel<D, DTYPE, PN, PD, true>;
     if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), C::SMEM_BYTES)) return ATTN_ERR_CUDA;
     int64_t BH = static_cast<int64_t>(B) * H;
     const bool head_pairs = WINDOW && (H / Hkv) % 2 == 0;

@@ -186,6 +186,56 @@ def test_gradient(B, S, H, Hkv, D, R, inter, kind):
     assert all(torch.equal(a, b) for a, b in zip(res, again))     # the sums' order is fixed
 
 
+LONG_CASES = [
+    # more than two laps of the gradient kernel's ring of 6 stages per CTA (148 of them), with a last block that is not full
+    (2, 2050, 32, 8, 128, 128, False, "bf16", False),      # 8 x 8 tiles of all tensors: 20 per CTA
+    (1, 4099, 12, 3, 256, 128, True, "fp16", True),        # heads that do not fill a tile: 17
+    (3, 16395, 2, 2, 64, 64, False, "fp16", False),        # tiles of 64 tokens: 15
+    (3, 3001, 32, 1, 64, 32, True, "bf16", True),          # q in tiles of 8 tokens, k and v of 128, by turns: 16
+    (2, 5003, 1, 9, 128, 64, False, "fp16", True),         # the other way round
+]
+
+
+@pytest.mark.parametrize("B,S,H,Hkv,D,R,inter,kind,given", LONG_CASES)
+def test_gradient_of_many_tiles(B, S, H, Hkv, D, R, inter, kind, given):
+    """Every stage of the ring is filled, worked on, stored and handed back several times; the walk crosses blocks, tensors and
+    sequences.  Tolerances as for the small cases: a lane adds fewer than 256 terms of a weight's sum here as well."""
+    dt = DT[kind]
+    q, k, v, qw, kw = make(B, S, H, Hkv, D, dt, 16)
+    g = torch.Generator().manual_seed(17)
+    dq, dk, dv = (torch.randn(B, h, S, D, generator=g).to(dt).cuda() for h in (H, Hkv, Hkv))
+    tab = table(S, R).cuda()
+    pos = torch.randint(0, S, (B, S), generator=g, dtype=torch.int32).cuda() if given else None
+    buf = torch.full((B, S, H + 2 * Hkv, D), float("nan"), dtype=dt, device="cuda")
+    outs = buf[:, :, :H], buf[:, :, H:H + Hkv], buf[:, :, H + Hkv:]
+    ws = torch.full((api.attn_qk_norm_rope_bwd_workspace_bytes(D),), 255, dtype=torch.uint8, device="cuda")
+    res = api.attn_qk_norm_rope_bwd(dq, dk, dv, q, k, qw, kw, tab, pos, eps=EPS, interleaved=inter, dq_in=outs[0], dk_in=outs[1], dv_in=outs[2],
+                                    workspace=ws)
+    assert api.attn_last_device_status() == 0
+    row = tab[pos.long()][:, :, None] if given else tab[None, :, None]
+    for got, gw, dy, x, w in ((outs[0], res[3], dq, q, qw), (outs[1], res[4], dk, k, kw)):
+        want, size, dw, dwsize = grad64(dy.transpose(1, 2), x, w, row, R, inter)
+        err = (got.double() - want).abs()
+        tol = half_step(dt) * want.abs() + 2.0 ** -18 * size + (2.0 ** -25 if dt == torch.float16 else 0.0)
+        assert (err <= tol).all(), "over by %g" % (err - tol).max()
+        werr = (gw.double() - dw.sum((0, 1, 2))).abs()
+        assert (werr <= 2.0 ** -16 * dwsize.sum((0, 1, 2))).all()
+    assert torch.equal(outs[2], dv.transpose(1, 2))
+    again = api.attn_qk_norm_rope_bwd(dq, dk, dv, q, k, qw, kw, tab, pos, eps=EPS, interleaved=inter)
+    assert all(torch.equal(a, b) for a, b in zip(res, again))
+
+
+def test_forward_of_many_tokens():
+    dt, B, S, H, Hkv, D = torch.bfloat16, 2, 3001, 16, 4, 128
+    q, k, v, qw, kw = make(B, S, H, Hkv, D, dt, 18)
+    tab = table(S, D).cuda()
+    qo, ko, vo = api.attn_qk_norm_rope(q, k, v, qw, kw, tab, eps=EPS)
+    for got, x, w in ((qo, q, qw), (ko, k, kw)):
+        want, size = rows64(x, w, tab[None, :, None], D, False)
+        check_rows(got.transpose(1, 2), want, size, dt, "rows")
+    assert torch.equal(vo.transpose(1, 2), v)
+
+
 def test_other_input_layouts():
     """Head-major inputs, and rows with room between them."""
     D, R, dt = 128, 64, torch.float16

@@ -190,6 +190,35 @@ def test_large_values_behind_a_low_first_reference(sinks):
     run(1, 4, 2, 600, 600, 128, "bf16", 300, sinks, 0, scale=0.3125, backward=False, data=(q, k, v, g))
 
 
+@pytest.mark.parametrize("W,sinks,off", [(2, 0, 0), (3, 0, 5), (5, 3, 0), (9, 1, 0), (40, 0, 0), (129, 4, 0), (300, 130, 0), (0, 0, 0)])
+@pytest.mark.parametrize("D,kind", [(64, "bf16"), (64, "fp16"), (128, "bf16"), (128, "fp16")])
+def test_precision_of_the_exponentials(W, sinks, off, D, kind):
+    """The window kernels take every exponential from the hardware's exp2 (2^-22), none from the polynomial of the causal kernels
+    (2^-13), which would stand in the LSE of rows with few keys as it is.  In units of 2^-24:
+      LSE  ex2 4; the reference's product with the scale, once in the exponent and once at the end, 2.4 |m|; the log of the sum 2 |log l|,
+           at most 2 (14 ln 2 + ln n); the last addition |LSE|; n additions, in eight chains, n / 8 + 4: below 8 x size for
+           size = 10 + |LSE| + largest |score| + ln n, and n / 4.
+      O    one rounding of P (e) and one of the result, and the same for the exponentials: dp = e + 2^-21 size + n 2^-26.
+    The scores add nothing: q and k are multiples of 1/4 up to 3, so every sum of products is a multiple of 1/16 below 2^11."""
+    S = 520
+    q, k, v, g = inputs(1, 4, 2, S, S + off, D, DT[kind], 22)
+    q, k = ((4 * t.float()).round().clamp(-12, 12).div(4).to(DT[kind]) for t in (q, k))
+    scale = float(torch.tensor(1 / math.sqrt(D), dtype=torch.float32))
+    o, lse = api.attn_fwd_window(q, k, v, scale, W, sinks, off)
+    assert api.attn_last_device_status() == 0
+    dt = q.dtype
+    e, tiny = torch.finfo(dt).eps / 2, 2.0 ** -25 if dt == torch.float16 else 0.0
+    qq, kk, vv = q.double(), k.double().repeat_interleave(2, 1), v.double().repeat_interleave(2, 1)
+    vis = visible(S, S + off, W, sinks, off)
+    x = (qq @ kk.transpose(-1, -2) * scale).masked_fill(~vis, -math.inf)
+    want, n = torch.logsumexp(x, -1, keepdim=True), vis.sum(-1)[None, None, :, None]
+    size = 10 + want.abs() + x.masked_fill(~vis, 0.0).abs().amax(-1, keepdim=True) + torch.log(n.double())
+    check("lse", lse, want[..., 0], (2.0 ** -21 * size + n * 2.0 ** -26)[..., 0])
+    p = torch.softmax(x, -1)
+    dp = e + 2.0 ** -21 * size + n * 2.0 ** -26
+    check("o", o, p @ vv, e * (p @ vv).abs() + dp * (p @ vv.abs()) + n * tiny * vv.abs().max() + tiny)
+
+
 def test_full_window_is_causal_attention():
     """No lower end: the same operator as the causal calls.  Those evaluate part of the exponentials by a polynomial (2^-13), the
     window kernels do not, so the two are compared within the tolerance that allows for it, on either side of the exact value."""

@@ -172,21 +172,32 @@ def _stream_ptr(stream) -> int:
     return int(stream.cuda_stream)
 
 
+# torch's current stream read and set without the Stream objects of torch.cuda.stream (9 us of a call's host time)
+_get_stream, _set_stream = (getattr(torch._C, name, None) for name in ("_cuda_getCurrentStream", "_cuda_setStream"))
+
+
 def _on_stream(stream, tensor, fn, *args, **kwargs):
     """fn(*args, **kwargs) with `stream` as torch's current stream, on `tensor`'s device.  The outputs and workspaces that the call
     allocates then come from `stream`'s pool: out of another stream's they might still be in use by that stream's earlier work, and a
     workspace, dropped when the call returns, would be handed out there again while the kernels on `stream` use it."""
-    if tensor.is_cuda:
-        device, handle = tensor.device, int(stream.cuda_stream)
-        if handle == 0:
-            stream = torch.cuda.default_stream(device)
-        elif not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(handle, device=device)
-        if stream.device != device:
-            raise ValueError("the stream belongs to %s, the tensors to %s" % (stream.device, device))
+    if not tensor.is_cuda:
+        return fn(*args, **kwargs)      # which says what is wrong
+    device, handle = tensor.device, int(stream.cuda_stream)
+    if handle == 0:
+        stream = torch.cuda.default_stream(device)
+    elif not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(handle, device=device)
+    if stream.device != device:
+        raise ValueError("the stream belongs to %s, the tensors to %s" % (stream.device, device))
+    if _get_stream is None or _set_stream is None or device.index != torch.cuda.current_device():
         with torch.cuda.stream(stream):
             return fn(*args, **kwargs)
-    return fn(*args, **kwargs)      # which says what is wrong
+    before = _get_stream(device.index)
+    _set_stream(stream_id=stream.stream_id, device_index=stream.device_index, device_type=stream.device_type)
+    try:
+        return fn(*args, **kwargs)
+    finally:
+        _set_stream(stream_id=before[0], device_index=before[1], device_type=before[2])
 
 
 def _call(name, device, *args):

@@ -106,6 +106,7 @@ def world(monkeypatch):
     monkeypatch.setattr(api, "_lib", w)
     monkeypatch.setattr(api, "_binding_module", None)
     monkeypatch.setattr(api, "_raw_stream", None)
+    monkeypatch.setattr(api, "_set_stream", None)
     return w
 
 

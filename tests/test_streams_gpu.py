@@ -98,3 +98,24 @@ def test_the_python_marshalling_gives_the_same(monkeypatch):
                 got = call(stream)
                 torch.cuda.synchronize()
                 assert all(torch.equal(x, y) for x, y in zip(got, result))
+
+
+def test_the_current_stream_stays(monkeypatch):
+    """... after a call on another one, after a refused one, and where torch's short cuts to it are missing."""
+    q = torch.randn(1, 2, 64, 64, device="cuda").half()
+    want = api.attn_fwd_window(q, q, q, 0.125, 8)
+    torch.cuda.synchronize()
+    outer, inner = torch.cuda.Stream(), torch.cuda.Stream()
+    for short_cut in (True, False):
+        if not short_cut:
+            monkeypatch.setattr(api, "_set_stream", None)
+        for current in (torch.cuda.default_stream(), outer):
+            with torch.cuda.stream(current):
+                for stream in (inner, torch.cuda.default_stream(), torch.cuda.ExternalStream(inner.cuda_stream), current):
+                    got = api.attn_fwd_window(q, q, q, 0.125, 8, stream=stream)
+                    assert torch.cuda.current_stream() == current
+                    stream.synchronize()
+                    assert all(torch.equal(a, b) for a, b in zip(got, want))
+                    with pytest.raises(ValueError):
+                        api.attn_fwd_gqa(q, q[:, :, :, :32], q, 0.125, stream=stream)
+                    assert torch.cuda.current_stream() == current

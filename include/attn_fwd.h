@@ -255,7 +255,9 @@ size_t attn_bwd_workspace_bytes(int B, int H, int Sq);
  * Sq * min(window + sinks, Sk).  A query without a visible key gives O = 0, LSE = -inf.
  * K and V must be finite also where they are hidden (tiles are computed whole: a NaN or infinity in a hidden V row
  * would reach rows of the same tile).  The sums of P V are kept in fp32, with P relative to a reference that may lag the row's
- * largest score by a factor of 2^14: largest |V| times visible keys times 2^14 must stay below 2^127.
+ * largest score by a factor of 2^14: largest |V| times visible keys times 2^14 must stay below 2^127.  As in attn_fwd, P is rounded
+ * to the 16-bit type before that product (LSE comes from the unrounded sum): O carries about 1.35 roundings of its type in the
+ * 2-norm, where a single rounding at the end would be 1.
  * Everything else -- layouts, scale, errors, asynchrony -- as for attn_fwd_gqa.
  */
 int attn_fwd_window(const void* q, const void* k, const void* v, void* o, float* lse, int B, int H, int Hkv, int Sq, int Sk,
@@ -264,7 +266,8 @@ int attn_fwd_window(const void* q, const void* k, const void* v, void* o, float*
 /*
  * attn_bwd_window -- backward pass of attn_fwd_window: arguments as attn_bwd, with the window of the forward call.
  * workspace: at least attn_bwd_window_workspace_bytes(...) bytes (with sinks it also holds
- * partial sums for the first keys, whose gradients collect from every later query).  Deterministic (no atomics).
+ * partial sums for the first keys, whose gradients collect from every later query).  Deterministic (no atomics).  As in attn_bwd, P
+ * and dS are rounded to the 16-bit type before their products: the gradients carry about 1.43 roundings.
  */
 int attn_bwd_window(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* dout, void* dq,
                     void* dk, void* dv, int B, int H, int Hkv, int Sq, int Sk, int D, float scale, int window, int sinks,
@@ -311,6 +314,7 @@ int attn_qk_norm_rope(const void* q, const void* k, const void* v, const long lo
  *            repeat); NULL allowed where the weight is NULL, otherwise required.
  * workspace: device, 256-byte aligned, at least attn_qk_norm_rope_bwd_workspace_bytes(D) bytes, or ATTN_ERR_WORKSPACE.
  *            Two calls that may run at the same time need one each.
+ * The outputs must not overlap the inputs.
  * B * S == 0 writes zero weight gradients.  A position out of range gives NaN in its rows and in the weight gradients.
  */
 int attn_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const void* q, const void* k,
@@ -363,9 +367,13 @@ int attn_paged_append(const void* q, const void* k, const void* v, const long lo
  *            does not matter (it may be NaN).  num_pages == 0: every key is hidden.
  * workspace: device, 256-byte aligned, at least attn_paged_decode_workspace_bytes(H, Hkv, D) bytes (whatever the lengths are), or
  *            ATTN_ERR_WORKSPACE.  Two calls that may run at the same time need one each.
- * One or two kernels are enqueued.  The lengths and the table are read on the device, so a captured call may be replayed with
- * new ones.  The result does
- * not depend on timing (no atomics).  The key axis is cut evenly over the GPU whatever the lengths are; the cut depends on
+ * The lengths and the table are read on the device, so a captured call may be replayed with new ones; what is enqueued follows
+ * from the host's arguments alone.  It is one kernel, the faster form for a few short sequences, where B times the K/V heads (a
+ * group of more than 16 query heads counts once per 16) is at most 148 and max_pages * page_size at most c * (16384 at D = 64,
+ * 8192 at D = 128, 4096 at D = 256) / 8, with c = 8, 4, 2, 1 for up to 16, 32, 64, 148 of them; else two.  max_pages counts here,
+ * not the lengths: with a block table that is much wider than the sequences, a view of its first columns (max_pages smaller,
+ * table_stride as it is) lets short sequences have that form.
+ * The result does not depend on timing (no atomics).  The key axis is cut evenly over the GPU whatever the lengths are; the cut depends on
  * all lengths of the batch, so a sequence's result may differ in its last bits when other sequences' lengths change.
  */
 int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, const long long* cache_strides, int num_pages,

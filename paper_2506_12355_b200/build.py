@@ -12,7 +12,8 @@ LIB_PATH = os.path.join(_HERE, "libattn_fwd.so")
 # entry that makes the producer leave out one K/V load): used by one GPU test to make a wait run out
 # and check the time-out status.  Never loaded by the package.
 WAIT_TEST_LIB_PATH = os.path.join(_HERE, "libattn_fwd_waittest.so")
-# Optional Python extension (see csrc/binding.cpp); without it api.py marshals every call itself.
+# Python extension (see csrc/binding.cpp) that build() makes beside the library.  Where it is missing, as beside a library that was
+# built by hand, api.py marshals every call itself.
 BINDING_PATH = os.path.join(_HERE, "_binding.so")
 WAIT_TEST_FLAGS = ["-DATTN_TEST_HOOKS", "-DATTN_TEST_WAIT_LIMIT_NS=1000000ull"]
 

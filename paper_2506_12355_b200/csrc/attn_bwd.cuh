@@ -19,6 +19,10 @@
 //                     the A operand that dV += P^T dO_i and dK += dS^T Q_i need; one thread per key row, the
 //                     per-query -L log2(e) and -delta arrive in shared memory with the streamed tiles.
 //
+// P and dS are rounded to the 16-bit type of the inputs before their products (an MMA takes both operands in one such type), the
+// accumulators are fp32.  Against 64 bits the gradients are off by 1.43 roundings of their type in the 2-norm, where a single
+// rounding at the end is 1 (bf16, 8192 rows under a window of 1024: 2.37e-3 and 1.66e-3).
+//
 // Recomputing S and dP in both passes costs 7 tile products instead of 5 but needs no atomics and no
 // cross-CTA reduction, so the results are deterministic.  A small kernel first prepares the two row vectors
 // (-L log2(e) and -delta) in the caller's workspace.  Where the 512 tensor-memory columns allow it (everywhere but

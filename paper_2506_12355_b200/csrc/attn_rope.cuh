@@ -347,7 +347,7 @@ attn_rope_kernel(const RopeParams p) {
 // Gradient.  dy: head-major gradients of the outputs; in: q, k as the forward pass read them; out: gradients laid out like
 // the inputs.  One wave of blocks, shared out between q and (k, v) by their bytes; an item is a token and kDeep x
 // rows-per-warp of its heads, eight neighbouring tokens to a block, so that even a few thousand tokens are many items per
-// warp (with whole tokens as items the last round was mostly empty: 67 us for 4 x 2048 tokens x 48 heads of 128).  A warp
+// warp (with whole tokens as items the last round is mostly empty); 70 us for 4 x 2048 tokens x 48 heads of 128.  A warp
 // keeps the weight gradients of its rows in registers; each block leaves its sum in `partial`, and
 // attn_rope_weight_grad_kernel adds those in a fixed order.
 template <int D, int DTYPE>

@@ -7,7 +7,7 @@
 // layout costs nothing.  One CTA per SM walks a contiguous run of tiles; a ring of 192 KB keeps loads and stores in flight
 // while 16 warps work.  The register form in
 // attn_rope.cuh (a load, arithmetic and a store per warp: 64 KB in flight at most, and only while nobody computes) takes
-// 71 us for 4 x 2048 tokens x 48 heads of 128, this one 60 (4.8 TB/s; 50 with the arithmetic left out).  What bounds it now
+// 70 us for 4 x 2048 tokens x 48 heads of 128, this one 59 (4.8 TB/s; 50 with the arithmetic left out).  What bounds it now
 // is the arithmetic: its shuffles' latency, which 16 warps of 96 registers do not hide, and half of all issue slots.  Two
 // groups of warps on alternate tiles (61 us), two or four rows at a time (78 us and more: fewer warps for their registers)
 // are slower.  For the forward pass, with half the arithmetic and no second operand, this form gains nothing over the

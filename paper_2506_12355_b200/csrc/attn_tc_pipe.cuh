@@ -24,8 +24,14 @@
 // items, which the host announces through PipeParams::halves_from.
 //
 // Running maximum: the reference maximum m of a row is only advanced when the true maximum has
-// grown by more than 2^8; otherwise the stale m is kept (P values up to 256, exact after the final
+// grown by more than 2^8 (under a window 2^14); otherwise the stale m is kept (P values up to 256, exact after the final
 // division by l), so the O accumulator rarely needs rescaling.
+//
+// P is rounded to the type of Q, K and V before the product with V (an MMA takes both operands in one 16-bit type), while the
+// row sum l, and with it LSE, adds the unrounded values.  Against 64 bits O is off by 1.3 roundings of its type in the 2-norm in
+// fp16 and 1.36 in bf16, where a single rounding at the end is 1 (2.6e-4 and 2.0e-4 for 1000 rows under a window of 255; 2.26e-3
+// and 1.64e-3 for 16384 rows under 1024).  P in two 16-bit parts, as in attn_paged.cuh, would take that away and cost half as many
+// products again (there they are a few percent of the time).
 //
 // Sliding window (WINDOW = true): query i at position p = i + q_offset sees key j iff j <= p and (j > p - window or
 // j < sinks).  The steps of an item are then the tiles of the first tokens and a run of tiles from the window's lower

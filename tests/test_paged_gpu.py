@@ -176,6 +176,22 @@ def test_decode_some_pairs(n, Hkv, group, D):
     run_decode(lens, Hkv * group, Hkv, D, 32, "fp16", "slot", window=200, sinks=3, seed=9)
 
 
+@pytest.mark.parametrize("lens", [[1000], [700, 3, 0]])
+def test_decode_through_a_view_of_a_wide_table(lens):
+    """The form of the call follows from the table's width: the whole table (a list of tiles) and a view of its first columns
+    (clusters), on which the rows stand further apart than they are wide."""
+    D, dt, page = 128, torch.bfloat16, 16
+    kc, vc, tab, ks, vs = make_cache(lens, 4, D, page, dt, "head", 15)
+    wide = torch.full((len(lens), 2048), -1, dtype=torch.int32)
+    wide[:, :tab.shape[1]] = tab
+    wide, len_t = wide.cuda(), torch.tensor(lens, dtype=torch.int32).cuda()
+    q = torch.randn(len(lens), 8, D, generator=torch.Generator().manual_seed(5)).to(dt).cuda()
+    for t in (wide, wide[:, :tab.shape[1]]):
+        o, lse = api.attn_paged_decode(q, kc, vc, t, len_t, 0.09)
+        assert api.attn_last_device_status() == 0
+        check_decode(o, lse, q, ks, vs, 0.09, 0, 0, dt)
+
+
 def test_decode_few_long_sequences():
     run_decode([14000, 9000], 8, 8, 128, 64, "bf16", "head", seed=10)
 

@@ -423,3 +423,47 @@ def test_both_ways_of_marshalling_agree():
     assert r[0].data_ptr() == o.data_ptr() and r[1].data_ptr() == lse.data_ptr()
     with pytest.raises(ValueError):
         api.attn_paged_decode(q, kc, vc, tab, lens, 0.125, out=o[:, :4])
+
+
+def test_serving_step_as_one_graph():
+    """Lengths advanced, tokens appended and attended in one captured graph, replayed step after step, against eager calls."""
+    D, H, Hkv, page, dt, steps = 64, 8, 2, 16, torch.float16, 40
+    lens0, g = [1, 15, 200, 63], torch.Generator().manual_seed(50)
+    B, per = len(lens0), 16
+    tab = torch.randperm(B * per, generator=g).to(torch.int32).view(B, per).cuda()
+    rt = table(per * page, D).cuda()
+    qw, kw = (1 + 0.2 * torch.randn(2, D, generator=g)).to(dt).cuda()
+    start = torch.randn(B * per, Hkv, page, D, generator=g).to(dt).cuda()
+    tokens = torch.randn(steps, B, H + 2 * Hkv, D, generator=g).to(dt).cuda()
+    ws = torch.empty(api.attn_paged_decode_workspace_bytes(H, Hkv, D), dtype=torch.uint8, device="cuda")
+
+    def step(x, kc, vc, lens):
+        lens += 1
+        q = api.attn_paged_append(x[:, :H], x[:, H:H + Hkv], x[:, H + Hkv:], kc, vc, tab, lens, qw, kw, rt)
+        return api.attn_paged_decode(q, kc, vc, tab, lens, 0.125, window=100, sinks=3, workspace=ws)
+    kc, vc, lens = start.clone(), start.clone(), torch.tensor(lens0, dtype=torch.int32).cuda()
+    want = [step(x, kc, vc, lens) for x in tokens]
+    kc2, vc2, lens2, x2 = start.clone(), start.clone(), torch.tensor(lens0, dtype=torch.int32).cuda(), torch.empty_like(tokens[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o, lse = step(x2, kc2, vc2, lens2)
+    for x, (wo, wl) in zip(tokens, want):
+        x2.copy_(x)
+        graph.replay()
+        assert torch.equal(o, wo) and torch.equal(lse, wl)
+    assert torch.equal(kc, kc2) and torch.equal(vc, vc2) and lens2.tolist() == [n + steps for n in lens0]
+    assert api.attn_last_device_status() == 0
+
+
+@pytest.mark.parametrize("times", [1, 12])      # clusters, a list of tiles
+def test_decode_of_sequences_that_share_pages(times):
+    """A common beginning is held once: several sequences name the same pages, some the same ones altogether."""
+    D, dt, page, n = 64, torch.bfloat16, 16, 150
+    kc, vc, tab, ks, vs = make_cache([n], 2, D, page, dt, "head", 51)
+    lens = [150, 33, 150, 96] * times
+    q = torch.randn(len(lens), 6, D, generator=torch.Generator().manual_seed(6)).to(dt).cuda()
+    o, lse = api.attn_paged_decode(q, kc, vc, tab.expand(len(lens), -1).contiguous().cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), 0.125)
+    check_decode(o, lse, q, [ks[0][:m] for m in lens], [vs[0][:m] for m in lens], 0.125, 0, 0, dt)
+    # the rows of the block table may be one and the same (stride 0)
+    o2, lse2 = api.attn_paged_decode(q, kc, vc, tab.cuda().expand(len(lens), -1), torch.tensor(lens, dtype=torch.int32).cuda(), 0.125)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2) and api.attn_last_device_status() == 0

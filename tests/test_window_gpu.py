@@ -219,6 +219,13 @@ def test_precision_of_the_exponentials(W, sinks, off, D, kind):
     check("o", o, p @ vv, e * (p @ vv).abs() + dp * (p @ vv.abs()) + n * tiny * vv.abs().max() + tiny)
 
 
+@pytest.mark.parametrize("W,sinks", [(2 ** 31 - 1, 0), (2 ** 31 - 1, 5), (1, 7), (0, 0), (2 ** 31 - 500, 2 ** 31 - 1), (2 ** 31 - 400, 33)])
+def test_the_last_positions(W, sinks):
+    """Queries at the end of the range of positions (2^31 - 1 - 256): nothing in the step lists and masks passes 32 bits."""
+    Sq = 300
+    run(1, 2, 1, Sq, 200, 64, "bf16", W, sinks, 2 ** 31 - 1 - 256 - Sq, seed=23)
+
+
 def test_full_window_is_causal_attention():
     """No lower end: the same operator as the causal calls.  Those evaluate part of the exponentials by a polynomial (2^-13), the
     window kernels do not, so the two are compared within the tolerance that allows for it, on either side of the exact value."""

@@ -69,6 +69,16 @@ float number(PyObject* o) {
     return static_cast<float>(v);
 }
 
+// An argument's truth value; one that has none (an array of several) goes to the Python path, which raises what Python raises.
+int truth(PyObject* o) {
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) {
+        PyErr_Clear();
+        throw NotPlain();
+    }
+    return v;
+}
+
 // What the tensors of one call have in common.
 struct Call {
     c10::DeviceIndex device;
@@ -199,7 +209,7 @@ PyObject* norm_rope(PyObject* const* a) {
     strides3(st + 3, &k);
     strides3(st + 6, v);
     const int rc = fn.norm_rope(q.data_ptr(), k.data_ptr(), ptr(v), st, ptr(r.qw), ptr(r.kw), r.f32, static_cast<const float*>(ptr(r.table)), r.len,
-                                r.R, PyObject_IsTrue(a[8]), static_cast<const int*>(ptr(pos)), number(a[7]), qo.data_ptr(), ko.data_ptr(),
+                                r.R, truth(a[8]), static_cast<const int*>(ptr(pos)), number(a[7]), qo.data_ptr(), ko.data_ptr(),
                                 v ? vo.data_ptr() : nullptr, small(B), small(S), small(H), small(Hkv), small(D), c.dtype, c.stream);
     return rc ? status(rc) : tuple({&qo, &ko, v ? &vo : nullptr});
 }
@@ -231,7 +241,7 @@ PyObject* norm_rope_bwd(PyObject* const* a) {
     strides3(out + 3, &ki);
     strides3(out + 6, dv ? &vi : nullptr);
     const int rc = fn.norm_rope_bwd(dq.data_ptr(), dk.data_ptr(), ptr(dv), q.data_ptr(), k.data_ptr(), in, ptr(r.qw), ptr(r.kw), r.f32,
-                                    static_cast<const float*>(ptr(r.table)), r.len, r.R, PyObject_IsTrue(a[10]),
+                                    static_cast<const float*>(ptr(r.table)), r.len, r.R, truth(a[10]),
                                     static_cast<const int*>(ptr(pos)), number(a[9]), qi.data_ptr(), ki.data_ptr(),
                                     dv ? vi.data_ptr() : nullptr, out, r.qw ? qw.data_ptr<float>() : nullptr,
                                     r.kw ? kw.data_ptr<float>() : nullptr, small(B), small(S), small(H), small(Hkv), small(D), c.dtype,
@@ -256,7 +266,7 @@ PyObject* append(PyObject* const* a) {
     const Tensor qo = c.output(tensor(a[13]), {T, H, D});
     const long long st[6] = {q->stride(0), q->stride(1), k.stride(0), k.stride(1), v.stride(0), v.stride(1)};
     const int rc = fn.append(q->data_ptr(), k.data_ptr(), v.data_ptr(), st, ptr(r.qw), ptr(r.kw), r.f32, static_cast<const float*>(ptr(r.table)),
-                             r.len, r.R, PyObject_IsTrue(a[12]), number(a[11]), qo.data_ptr(), m.k.data_ptr(), m.v.data_ptr(), m.strides,
+                             r.len, r.R, truth(a[12]), number(a[11]), qo.data_ptr(), m.k.data_ptr(), m.v.data_ptr(), m.strides,
                              m.pages, m.page_size, m.table.data_ptr<int>(), m.table.stride(0), m.width, m.lens.data_ptr<int>(),
                              static_cast<const int*>(ptr(cu)), m.n, small(T), small(H), small(Hkv), small(D), c.dtype, c.stream);
     return rc ? status(rc) : wrap(qo);

@@ -347,3 +347,11 @@ def test_graph_replay_and_second_stream():
     got = api.attn_qk_norm_rope(q, k, v, qw, kw, tab, stream=side)
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_flag_without_a_truth_value_is_refused():
+    q, k, v, qw, kw = make(1, 8, 2, 1, 64, torch.float16, 25)
+    tab = table(8, 64).cuda()
+    for bad in (torch.tensor([True, False]), torch.zeros(0, 2, dtype=torch.bool)):
+        with pytest.raises(RuntimeError):
+            api.attn_qk_norm_rope(q, k, v, qw, kw, tab, interleaved=bad)

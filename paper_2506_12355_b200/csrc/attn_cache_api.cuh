@@ -3,6 +3,10 @@
 
 namespace {
 
+#ifdef ATTN_TEST_HOOKS
+int g_test_skip_step = -1;
+#endif
+
 int log2_of(int x) {
     int s = 0;
     while ((1 << s) < x) ++s;
@@ -186,6 +190,10 @@ int launch_rope_bwd_tma(const attn_rope::RopeParams& p, int B, int D, int dtype,
     attn_rope::TmaParams tp = {};
     tp.r = p;
     tp.partial = p.partial;
+#ifdef ATTN_TEST_HOOKS
+    tp.test_skip_tile = g_test_skip_step;
+    g_test_skip_step = -1;
+#endif
     tp.block_shift = 3;
     for (int i = 0; i < 3; ++i) {
         int hb = 0;
@@ -248,6 +256,12 @@ int validate_window(int Sq, int* window, int sinks, int q_offset) {
 }  // namespace
 
 extern "C" {
+
+#ifdef ATTN_TEST_HOOKS
+// Test build only (never part of libattn_fwd.so): the next launch of the decode kernel (of the rotation's gradient) leaves out the
+// copies of this step of every warp (tile of every CTA), so that the wait for them runs out.
+void attn_test_skip_step(int step) { g_test_skip_step = step; }
+#endif
 
 int attn_fwd_window(const void* q, const void* k, const void* v, void* o, float* lse, int B, int H, int Hkv, int Sq, int Sk,
                     int D, float scale, int window, int sinks, int q_offset, int dtype, void* stream) {
@@ -571,6 +585,10 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
     const int64_t tile_keys = D == 256 ? 4 * 16 : (D == 128 ? 8 * 16 : 8 * 32);
     int cluster = attn_paged::kCluster;
     while (cluster > 1 && pairs * cluster > 128) cluster >>= 1;
+#ifdef ATTN_TEST_HOOKS
+    p.test_skip_step = g_test_skip_step;
+    g_test_skip_step = -1;
+#endif
     p.cluster = pairs * cluster <= di.sm_count && p.max_len <= cluster * 8 * tile_keys ? cluster : 0;
 #define ATTN_DECODE_CASE(DD, TT, GG)                                                                                     \
     if (D == DD && dtype == TT && (p.group <= 8) == (GG == 8)) {                                                         \

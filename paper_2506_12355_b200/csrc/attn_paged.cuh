@@ -80,6 +80,9 @@ struct DecodeParams {
     int window, sinks;
     float scale_log2;
     int grid;                   // CTAs of the first kernel
+#ifdef ATTN_TEST_HOOKS
+    int test_skip_step;         // test build only: the step of every warp whose copies are left out (-1: none)
+#endif
     int cluster;                // > 0: a cluster of so many CTAs (a power of two up to kCluster) per (sequence, head), no second kernel
 };
 constexpr int kCluster = 8;
@@ -382,7 +385,8 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     auto issue = [&](int stage, uint32_t& live_out) {
         live_out = 0;
         if (loaded < steps) {
-            const int k0 = key_next, page = page_next, key = k0 + (lane & (CK - 1));
+            const int k0 = key_next, key = k0 + (lane & (CK - 1));
+            int page = page_next;
             const bool seen = page >= 0 && key < ld.r.len && (key >= ld.r.win_lo || key < p.sinks);
             const uint32_t live = __ballot_sync(0xffffffffu, seen) & (CK == 32 ? 0xffffffffu : 0xffffu);
             live_out = live;
@@ -391,6 +395,9 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                 // pages that are loaded: the first lane of each box counts
                 const uint32_t boxes = __ballot_sync(0xffffffffu, lane < CK && (lane & (box - 1)) == 0 && page >= 0);
                 if (lane == 0) sm100::mbar_arrive_expect_tx(bar, __popc(boxes) * 2 * NPL * box * 128);
+#ifdef ATTN_TEST_HOOKS
+                if (loaded == p.test_skip_step) page = -1;      // this step's copies are left out
+#endif
                 __syncwarp();     // armed before the first copy; and every lane has read what this stage held
                 for (int o0 = 0; o0 < 2 * NPL * (CK >> p.box_shift); o0 += 32) {
                     const int o = o0 + lane, row = (o / (2 * NPL)) << p.box_shift, pl = o % (2 * NPL);
@@ -463,11 +470,16 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
             issue((st + NSTAGE - 1) % NSTAGE, live_q[(st + NSTAGE - 1) % NSTAGE]);
             uint32_t live = live_q[st];
             if (live) {
-                // (a copy that never arrives ends in an error status: the rest of the loop goes on without its keys)
-                if (!sm100::mbar_wait(my_bars + 8 * st, (phases >> st) & 1, abort_flag)) live = 0;
-                phases ^= 1u << st;
+                // A copy that does not arrive ends in an error status: the rest of the loop goes on without its keys, and asks for
+                // nothing more (its stage is not free).
+                if (__all_sync(0xffffffffu, sm100::mbar_wait(my_bars + 8 * st, (phases >> st) & 1, abort_flag))) {
+                    phases ^= 1u << st;
+                } else {
+                    live = 0;
+                    loaded = steps;
+                }
             }
-            if (__any_sync(0xffffffffu, live != 0)) {
+            if (live) {
                 const uint32_t src = ring + st * C::STAGE_BYTES;
                 const bool full = live == (CK == 32 ? 0xffffffffu : 0xffffu);
                 float sf[NSUB][NT][4];               // S^T: keys krow (0, 1) and krow + 8 (2, 3) of each group, heads 2 c, 2 c + 1
@@ -692,7 +704,7 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         }
     }
     __syncthreads();
-    if (tid == 0 && *abort_flag != 0) atomicExch(p.status, attn_tc::kStatusTimeout);
+    if (tid == 0 && *abort_flag != 0) attn_tc::report_timeout(p.status);
     if (p.cluster) {
         float* mine = reinterpret_cast<float*>(smem);
         if (steps == 0)

@@ -47,6 +47,9 @@ struct TmaParams {
     int per_block;            // tiles of a block: those of q, k, v
     int64_t tiles;
     float* partial;           // [CTA][2][D]: sums of q's and k's weight gradients
+#ifdef ATTN_TEST_HOOKS
+    int test_skip_tile;       // test build only: the tile of every CTA whose copies are left out (-1: none)
+#endif
 };
 
 struct TmaMaps {
@@ -168,6 +171,12 @@ attn_rope_bwd_tma_kernel(const __grid_constant__ TmaMaps maps, const __grid_cons
                 const int kind = at_tile.kind, h0 = at_tile.head0(p), t0 = at_tile.token0(p);
                 const bool with_x = kind < 2 && p.r.weight[kind] != nullptr;
                 sm100::mbar_arrive_expect_tx(full(s), with_x ? 2 * C::TILE : C::TILE);
+#ifdef ATTN_TEST_HOOKS
+                if (i == p.test_skip_tile) {                  // this tile's copies are left out
+                    at_tile.next(p);
+                    continue;
+                }
+#endif
                 tma_load_4d(base + s * C::STAGE, &maps.dy[kind], full(s), 0, t0, h0, at_tile.b);
                 if (with_x) tma_load_4d(base + s * C::STAGE + C::TILE, &maps.x[kind & 1], full(s), 0, t0, h0, at_tile.b);
                 at_tile.next(p);
@@ -225,7 +234,8 @@ attn_rope_bwd_tma_kernel(const __grid_constant__ TmaMaps maps, const __grid_cons
             }
             if (norm && kind != my_kind) load_weight<DTYPE>(p.r.weight[kind], p.r.weight_f32, at, w);
             my_kind = kind;
-            if (!sm100::mbar_wait(full(s), (i / NST) & 1, abort_flag)) break;
+            // (the vote keeps a warp together where a wait runs out: its lanes shuffle)
+            if (!__all_sync(0xffffffffu, sm100::mbar_wait(full(s), (i / NST) & 1, abort_flag))) break;
             if (kind < 2) {
                 const int tb = p.tb_shift[kind], left = p.r.heads[kind] - h0;        // heads of this tile that exist
                 by_form(p.r, D, [&](auto inter, auto whole_head) {
@@ -307,7 +317,7 @@ attn_rope_bwd_tma_kernel(const __grid_constant__ TmaMaps maps, const __grid_cons
         for (int r = 0; r < ROWS; ++r) x += sums[((i / D) * ROWS + r) * D + i % D];
         p.partial[static_cast<int64_t>(blockIdx.x) * 2 * D + i] = x;
     }
-    if (threadIdx.x == 0 && *abort_flag != 0) atomicExch(p.r.status, attn_tc::kStatusTimeout);
+    if (threadIdx.x == 0 && *abort_flag != 0) attn_tc::report_timeout(p.r.status);
 }
 
 }  // namespace attn_rope

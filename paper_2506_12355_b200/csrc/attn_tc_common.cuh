@@ -38,13 +38,23 @@ __device__ __forceinline__ uint32_t window_queries(int p0, int key, int Sk, int 
     return ~low_bits(key - p0) & until;
 }
 
+// End of a CTA in which a wait ran out, executed by one thread once no role asks for anything more.  Copies and products that the
+// CTA did ask for may still be on their way into its shared and tensor memory, which therefore has to stay its own for a while:
+// those that arrive at all take microseconds.
+constexpr uint64_t kSettleNs = 200000;
+__device__ __forceinline__ void report_timeout(int* status) {
+    const uint64_t t0 = sm100::globaltimer_ns();
+    while (sm100::globaltimer_ns() - t0 < kSettleNs) __nanosleep(1000);
+    atomicExch(status, kStatusTimeout);
+}
+
 // End of a persistent kernel, executed by one thread per CTA after the CTA's last draw from the work
 // counter: reports a timed-out wait, and hands the counter back zeroed.  counter[0] is the next work
 // item, counter[1] the number of CTAs that have finished; the CTA that finishes last resets both, so
 // the next launch that uses this counter (launches that share one are ordered on one stream) starts
 // from zero without a memset.  Every CTA reaches this point, also after a timed-out wait.
 __device__ __forceinline__ void finish_cta(int* status, bool timed_out, unsigned int* counter) {
-    if (timed_out) atomicExch(status, kStatusTimeout);
+    if (timed_out) report_timeout(status);
     if (counter) {
         __threadfence();
         if (atomicAdd(counter + 1, 1u) == gridDim.x - 1) {

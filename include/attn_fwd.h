@@ -328,6 +328,29 @@ int attn_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const 
 size_t attn_qk_norm_rope_bwd_workspace_bytes(int D);
 
 /*
+ * attn_qk_norm_rope_axes, attn_qk_norm_rope_axes_bwd -- the same with several position axes, as tokens of images and videos have
+ * them (time, height, width): pair i belongs to axis pair_axes[i] and turns by the angle of cos_sin[positions[axis][b][s]][i].
+ *
+ * n_axes   : 1 to 4.
+ * pair_axes: HOST array of R/2 axis numbers below n_axes, in any order: runs of pairs per axis, or axes that take turns.
+ * positions: device int32 [n_axes][B][S], required.  A position outside [0, table_len) on any of the axes (whether a pair belongs
+ *            to it or not) gives NaN in that token's q and k rows (in the gradients: as in attn_qk_norm_rope_bwd) and
+ *            ATTN_ERR_DEVICE_INDEX in the device status; with R == 0 positions are not looked at.
+ * All other arguments, layouts, the workspace (attn_qk_norm_rope_bwd_workspace_bytes) and limits: as in the calls with one axis.
+ */
+int attn_qk_norm_rope_axes(const void* q, const void* k, const void* v, const long long* in_strides, const void* q_weight,
+                           const void* k_weight, int weight_f32, const float* cos_sin, int table_len, int R, int interleaved,
+                           const int* positions, int n_axes, const unsigned char* pair_axes, float eps, void* q_out, void* k_out,
+                           void* v_out, int B, int S, int H, int Hkv, int D, int dtype, void* stream);
+
+int attn_qk_norm_rope_axes_bwd(const void* dq, const void* dk, const void* dv, const void* q, const void* k,
+                               const long long* in_strides, const void* q_weight, const void* k_weight, int weight_f32,
+                               const float* cos_sin, int table_len, int R, int interleaved, const int* positions, int n_axes,
+                               const unsigned char* pair_axes, float eps, void* dq_in, void* dk_in, void* dv_in,
+                               const long long* out_strides, float* dq_weight, float* dk_weight, int B, int S, int H, int Hkv,
+                               int D, int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Paged key/value cache.  k_cache and v_cache hold num_pages pages of page_size key (value) rows for each of Hkv heads:
  * the row of slot s, head h in page p begins at element p * page + h * head + s * slot of its cache, cache_strides =
  * HOST array {page, head, slot} of k_cache, then of v_cache (elements, multiples of 8, below 2^39 and above 0 wherever the
@@ -355,6 +378,18 @@ int attn_paged_append(const void* q, const void* k, const void* v, const long lo
                       float eps, void* q_out, void* k_cache, void* v_cache, const long long* cache_strides, int num_pages,
                       int page_size, const int* block_table, long long table_stride, int max_pages, const int* seq_lens,
                       const int* cu_seqlens, int n_seqs, int tokens, int H, int Hkv, int D, int dtype, void* stream);
+
+/*
+ * attn_paged_append_axes -- attn_paged_append with the rotation of attn_qk_norm_rope_axes: where a token goes in the cache follows
+ * from seq_lens and cu_seqlens as before, what it turns by from positions, device int32 [n_axes][tokens] (padding tokens' entries
+ * are not looked at).  A token with a position outside [0, table_len) is skipped and reported like one whose place is out of range.
+ */
+int attn_paged_append_axes(const void* q, const void* k, const void* v, const long long* in_strides, const void* q_weight,
+                           const void* k_weight, int weight_f32, const float* cos_sin, int table_len, int R, int interleaved,
+                           const int* positions, int n_axes, const unsigned char* pair_axes, float eps, void* q_out,
+                           void* k_cache, void* v_cache, const long long* cache_strides, int num_pages, int page_size,
+                           const int* block_table, long long table_stride, int max_pages, const int* seq_lens,
+                           const int* cu_seqlens, int n_seqs, int tokens, int H, int Hkv, int D, int dtype, void* stream);
 
 /*
  * attn_paged_decode -- attention of one new token per sequence over a paged cache: row b of q sees the keys

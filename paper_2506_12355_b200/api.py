@@ -29,6 +29,7 @@ EXPORTS = ["attn_bwd", "attn_bwd_workspace_bytes", "attn_fwd", "attn_fwd_gqa", "
            "attn_fwd_host_static", "attn_fwd_host_static_capacity",
            "attn_fwd_window", "attn_bwd_window", "attn_bwd_window_workspace_bytes",
            "attn_qk_norm_rope", "attn_qk_norm_rope_bwd", "attn_qk_norm_rope_bwd_workspace_bytes", "attn_paged_append", "attn_paged_decode",
+           "attn_qk_norm_rope_axes", "attn_qk_norm_rope_axes_bwd", "attn_paged_append_axes",
            "attn_paged_decode_workspace_bytes",
            "attn_query_support", "attn_last_device_status", "attn_status_string"]
 
@@ -104,6 +105,14 @@ def load() -> ctypes.CDLL:
     lib.attn_qk_norm_rope_bwd_workspace_bytes.argtypes = [i]
     lib.attn_paged_append.restype = i
     lib.attn_paged_append.argtypes = [vp] * 6 + [i, vp, i, i, i, f] + [vp] * 4 + [i, i, vp, ll, i, vp, vp] + [i] * 6 + [vp]
+    # with several axes: their number and the pairs' axes behind the positions (of the append: behind `interleaved`)
+    lib.attn_qk_norm_rope_axes.restype = i
+    lib.attn_qk_norm_rope_axes.argtypes = [vp] * 6 + [i, vp, i, i, i, vp, i, ctypes.c_char_p, f, vp, vp, vp] + [i] * 6 + [vp]
+    lib.attn_qk_norm_rope_axes_bwd.restype = i
+    lib.attn_qk_norm_rope_axes_bwd.argtypes = [vp] * 8 + [i, vp, i, i, i, vp, i, ctypes.c_char_p, f] + [vp] * 6 + [i] * 6 + [vp, sz, vp]
+    lib.attn_paged_append_axes.restype = i
+    lib.attn_paged_append_axes.argtypes = ([vp] * 6 + [i, vp, i, i, i, vp, i, ctypes.c_char_p, f] + [vp] * 4 + [i, i, vp, ll, i, vp, vp]
+                                           + [i] * 6 + [vp])
     lib.attn_paged_decode.restype = i
     lib.attn_paged_decode.argtypes = [vp] * 4 + [i, i, vp, ll, i] + [vp] * 3 + [i] * 4 + [f, i, i, i, vp, sz, vp]
     lib.attn_paged_decode_workspace_bytes.restype = sz
@@ -120,7 +129,8 @@ def load() -> ctypes.CDLL:
 
 # Entry points that _binding marshals in C++, in the order in which its bind() takes their addresses.
 _BOUND = ["attn_qk_norm_rope", "attn_qk_norm_rope_bwd", "attn_qk_norm_rope_bwd_workspace_bytes", "attn_paged_append", "attn_paged_decode",
-          "attn_paged_decode_workspace_bytes", "attn_fwd_window", "attn_bwd_window", "attn_bwd_window_workspace_bytes"]
+          "attn_paged_decode_workspace_bytes", "attn_fwd_window", "attn_bwd_window", "attn_bwd_window_workspace_bytes", "attn_qk_norm_rope_axes",
+          "attn_qk_norm_rope_axes_bwd", "attn_paged_append_axes"]
 
 
 def _bind():
@@ -604,6 +614,64 @@ def attn_qk_norm_rope(q, k, v, q_weight, k_weight, cos_sin, positions=None, eps:
     result = _fast("attn_qk_norm_rope", q, k, v, q_weight, k_weight, cos_sin, positions, eps, interleaved, q_out, k_out, v_out)
     if result is not NotImplemented:
         return result
+    return _qk_norm_rope(q, k, v, q_weight, k_weight, cos_sin, positions, None, eps, interleaved, q_out, k_out, v_out)
+
+
+def rope_pair_axes(sections, order: str = "blocks") -> bytes:
+    """The axis of each pair for the calls with several axes, axis a having sections[a] pairs: order "blocks" gives runs of pairs
+    (0 0 .. 1 1 .. 2 2 ..), "cyclic" lets the axes take turns until their pairs are used up (0 1 2 0 1 2 .. 0 0)."""
+    left = [int(n) for n in sections]
+    if not 1 <= len(left) <= 4 or min(left) < 0:
+        raise ValueError("sections are the pairs of 1 to 4 axes")
+    if order == "blocks":
+        return bytes(a for a, n in enumerate(left) for _ in range(n))
+    if order != "cyclic":
+        raise ValueError("order must be 'blocks' or 'cyclic'")
+    of = bytearray()
+    while any(left):
+        for a, n in enumerate(left):
+            if n:
+                left[a] -= 1
+                of.append(a)
+    return bytes(of)
+
+
+def _not_none(pair_axes):
+    if pair_axes is None:
+        raise ValueError("pair_axes must say which axis each pair belongs to")
+    return pair_axes
+
+
+def _where(positions, pair_axes, R, tokens, device):
+    """What the C calls take for the positions: of one axis [..] (or None), or of several, [axes, ..] with the axis of each pair."""
+    if pair_axes is None:
+        if positions is not None:
+            _require(positions, "positions", tokens, torch.int32, device)
+        return (_ptr(positions),)
+    axes = pair_axes if isinstance(pair_axes, bytes) else bytes(int(a) for a in pair_axes)
+    if positions is None or positions.dim() != len(tokens) + 1 or not 1 <= positions.shape[0] <= 4:
+        raise ValueError("positions must be [axes, %s] with 1 to 4 axes" % ", ".join(str(n) for n in tokens))
+    _require(positions, "positions", (positions.shape[0],) + tuple(tokens), torch.int32, device)
+    if 2 * len(axes) != R or any(a >= positions.shape[0] for a in axes):
+        raise ValueError("pair_axes must be %d axis numbers below %d" % (R // 2, positions.shape[0]))
+    return positions.data_ptr(), positions.shape[0], axes
+
+
+def attn_qk_norm_rope_axes(q, k, v, q_weight, k_weight, cos_sin, positions, pair_axes, eps: float = 1e-6, interleaved: bool = False,
+                           q_out=None, k_out=None, v_out=None, stream=None):
+    """attn_qk_norm_rope with several position axes (time, height, width of images and videos): positions int32 [axes,B,S], and
+    pair_axes the axis of each of the R/2 pairs (bytes or a sequence of whole numbers; see rope_pair_axes).  Pair i of token s turns
+    by cos_sin[positions[pair_axes[i], b, s], i]."""
+    if stream is not None:
+        return _on_stream(stream, q, attn_qk_norm_rope_axes, q, k, v, q_weight, k_weight, cos_sin, positions, pair_axes, eps, interleaved, q_out,
+                          k_out, v_out)
+    result = _fast("attn_qk_norm_rope_axes", q, k, v, q_weight, k_weight, cos_sin, positions, pair_axes, eps, interleaved, q_out, k_out, v_out)
+    if result is not NotImplemented:
+        return result
+    return _qk_norm_rope(q, k, v, q_weight, k_weight, cos_sin, positions, _not_none(pair_axes), eps, interleaved, q_out, k_out, v_out)
+
+
+def _qk_norm_rope(q, k, v, q_weight, k_weight, cos_sin, positions, pair_axes, eps, interleaved, q_out, k_out, v_out):
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q and k must be [B,S,heads,D]")
     B, S, H, D = q.shape
@@ -617,8 +685,7 @@ def attn_qk_norm_rope(q, k, v, q_weight, k_weight, cos_sin, positions=None, eps:
     if not _is(k, (B, S, Hkv, D), dtype, index):
         _require(k, "k", (B, S, Hkv, D), dtype, device, False)
     f32, n_pos, R = _check_rope(dtype, device, D, q_weight, k_weight, cos_sin)
-    if positions is not None:
-        _require(positions, "positions", (B, S), torch.int32, device)
+    where = _where(positions, pair_axes, R, (B, S), device)
     if q_out is None:
         q_out = torch.empty((B, H, S, D), dtype=dtype, device=device)
     else:
@@ -637,8 +704,8 @@ def attn_qk_norm_rope(q, k, v, q_weight, k_weight, cos_sin, positions=None, eps:
             v_out = torch.empty(kv_shape, dtype=dtype, device=device)
         else:
             _require(v_out, "v_out", kv_shape, dtype, device)
-    _call("attn_qk_norm_rope", device, q.data_ptr(), k.data_ptr(), _ptr(v), _rows3(q, k, v), _ptr(q_weight), _ptr(k_weight), f32,
-          _ptr(cos_sin), n_pos, R, bool(interleaved), _ptr(positions), float(eps), q_out.data_ptr(), k_out.data_ptr(), _ptr(v_out), B, S, H,
+    _call("attn_qk_norm_rope" if pair_axes is None else "attn_qk_norm_rope_axes", device, q.data_ptr(), k.data_ptr(), _ptr(v), _rows3(q, k, v), _ptr(q_weight), _ptr(k_weight), f32,
+          _ptr(cos_sin), n_pos, R, bool(interleaved), *where, float(eps), q_out.data_ptr(), k_out.data_ptr(), _ptr(v_out), B, S, H,
           Hkv, D, dt)
     return q_out, k_out, v_out
 
@@ -660,6 +727,24 @@ def attn_qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positio
                    workspace)
     if result is not NotImplemented:
         return result
+    return _qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positions, None, eps, interleaved, dq_in, dk_in, dv_in, workspace)
+
+
+def attn_qk_norm_rope_axes_bwd(dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positions, pair_axes, eps: float = 1e-6,
+                               interleaved: bool = False, dq_in=None, dk_in=None, dv_in=None, workspace=None, stream=None):
+    """Gradients of attn_qk_norm_rope_axes; arguments and results as of attn_qk_norm_rope_bwd."""
+    if stream is not None:
+        return _on_stream(stream, q, attn_qk_norm_rope_axes_bwd, dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positions, pair_axes, eps, interleaved,
+                          dq_in, dk_in, dv_in, workspace)
+    result = _fast("attn_qk_norm_rope_axes_bwd", dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positions, pair_axes, eps, interleaved, dq_in,
+                   dk_in, dv_in, workspace)
+    if result is not NotImplemented:
+        return result
+    return _qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positions, _not_none(pair_axes), eps, interleaved, dq_in, dk_in, dv_in,
+                             workspace)
+
+
+def _qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positions, pair_axes, eps, interleaved, dq_in, dk_in, dv_in, workspace):
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q and k must be [B,S,heads,D]")
     B, S, H, D = q.shape
@@ -673,8 +758,7 @@ def attn_qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positio
     _require(dq, "dq", (B, H, S, D), dtype, device)
     _require(dk, "dk", (B, Hkv, S, D), dtype, device)
     f32, n_pos, R = _check_rope(dtype, device, D, q_weight, k_weight, cos_sin)
-    if positions is not None:
-        _require(positions, "positions", (B, S), torch.int32, device)
+    where = _where(positions, pair_axes, R, (B, S), device)
     if dq_in is None:
         dq_in = torch.empty(q_shape, dtype=dtype, device=device)
     else:
@@ -694,8 +778,8 @@ def attn_qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positio
     dqw = None if q_weight is None else torch.empty(D, dtype=torch.float32, device=device)
     dkw = None if k_weight is None else torch.empty(D, dtype=torch.float32, device=device)
     workspace = _workspace(workspace, attn_qk_norm_rope_bwd_workspace_bytes(D), device)
-    _call("attn_qk_norm_rope_bwd", device, dq.data_ptr(), dk.data_ptr(), _ptr(dv), q.data_ptr(), k.data_ptr(), _rows3(q, k),
-          _ptr(q_weight), _ptr(k_weight), f32, _ptr(cos_sin), n_pos, R, bool(interleaved), _ptr(positions), float(eps), dq_in.data_ptr(),
+    _call("attn_qk_norm_rope_bwd" if pair_axes is None else "attn_qk_norm_rope_axes_bwd", device, dq.data_ptr(), dk.data_ptr(), _ptr(dv), q.data_ptr(), k.data_ptr(), _rows3(q, k),
+          _ptr(q_weight), _ptr(k_weight), f32, _ptr(cos_sin), n_pos, R, bool(interleaved), *where, float(eps), dq_in.data_ptr(),
           dk_in.data_ptr(), _ptr(dv_in), _rows3(dq_in, dk_in, dv_in), _ptr(dqw), _ptr(dkw), B, S, H, Hkv, D, dt, workspace.data_ptr(),
           _bytes(workspace))
     return dq_in, dk_in, dv_in, dqw, dkw
@@ -734,6 +818,27 @@ def attn_paged_append(q, k, v, k_cache, v_cache, block_table, seq_lens, q_weight
                    interleaved, q_out)
     if result is not NotImplemented:
         return result
+    return _paged_append(q, k, v, k_cache, v_cache, block_table, seq_lens, None, None, q_weight, k_weight, cos_sin, cu_seqlens, eps, interleaved,
+                         q_out)
+
+
+def attn_paged_append_axes(q, k, v, k_cache, v_cache, block_table, seq_lens, positions, pair_axes, q_weight=None, k_weight=None,
+                           cos_sin=None, cu_seqlens=None, eps: float = 1e-6, interleaved: bool = False, q_out=None, stream=None):
+    """attn_paged_append with the rotation of attn_qk_norm_rope_axes: positions int32 [axes,T] and pair_axes say what each token
+    turns by; its place in the cache follows from seq_lens and cu_seqlens as before."""
+    if stream is not None:
+        return _on_stream(stream, k, attn_paged_append_axes, q, k, v, k_cache, v_cache, block_table, seq_lens, positions, pair_axes, q_weight, k_weight,
+                          cos_sin, cu_seqlens, eps, interleaved, q_out)
+    result = _fast("attn_paged_append_axes", q, k, v, k_cache, v_cache, block_table, seq_lens, positions, pair_axes, q_weight, k_weight, cos_sin,
+                   cu_seqlens, eps, interleaved, q_out)
+    if result is not NotImplemented:
+        return result
+    return _paged_append(q, k, v, k_cache, v_cache, block_table, seq_lens, positions, _not_none(pair_axes), q_weight, k_weight, cos_sin, cu_seqlens,
+                         eps, interleaved, q_out)
+
+
+def _paged_append(q, k, v, k_cache, v_cache, block_table, seq_lens, positions, pair_axes, q_weight, k_weight, cos_sin, cu_seqlens, eps,
+                  interleaved, q_out):
     if k.dim() != 3 or (q is not None and q.dim() != 3):
         raise ValueError("q must be [tokens,H,D]; k and v [tokens,Hkv,D]")
     T, Hkv, D = kv_shape = k.shape
@@ -766,9 +871,10 @@ def attn_paged_append(q, k, v, k_cache, v_cache, block_table, seq_lens, q_weight
             _require(cu_seqlens, "cu_seqlens", (n_seqs + 1,), torch.int32, device)
     elif T != n_seqs:
         raise ValueError("without cu_seqlens there is one token per sequence: %d tokens, %d sequences" % (T, n_seqs))
+    where = () if pair_axes is None else _where(positions, pair_axes, R, (T,), device)
     ks, vs = k.stride(), v.stride()
-    _call("attn_paged_append", device, _ptr(q), k.data_ptr(), v.data_ptr(), _strides(qs[0], qs[1], ks[0], ks[1], vs[0], vs[1]),
-          _ptr(q_weight), _ptr(k_weight), f32, _ptr(cos_sin), n_pos, R, bool(interleaved), float(eps), _ptr(q_out), k_cache.data_ptr(),
+    _call("attn_paged_append" if pair_axes is None else "attn_paged_append_axes", device, _ptr(q), k.data_ptr(), v.data_ptr(), _strides(qs[0], qs[1], ks[0], ks[1], vs[0], vs[1]),
+          _ptr(q_weight), _ptr(k_weight), f32, _ptr(cos_sin), n_pos, R, bool(interleaved), *where, float(eps), _ptr(q_out), k_cache.data_ptr(),
           v_cache.data_ptr(), cache_strides, pages, page_size, block_table.data_ptr(), block_table.stride(0), width,
           seq_lens.data_ptr(), _ptr(cu_seqlens), n_seqs, T, H, Hkv, D, dt)
     return q_out

@@ -159,6 +159,19 @@ void rope_units(attn_rope::RopeParams& p, int D) {
     }
 }
 
+// Several position axes: their number, at most 4, and the axis of each of the R / 2 pairs; positions are required.
+int set_axes(attn_rope::RopeParams& p, int R, const int* positions, int64_t tokens, int n_axes, const unsigned char* pair_axes) {
+    if (n_axes < 1 || n_axes > 4) return ATTN_ERR_BAD_SHAPE;
+    if ((tokens > 0 && !positions) || (R > 0 && !pair_axes)) return ATTN_ERR_NULL_POINTER;
+    if (misaligned(positions, 4)) return ATTN_ERR_MISALIGNED;
+    for (int i = 0; i < R / 2; ++i) {
+        if (pair_axes[i] >= n_axes) return ATTN_ERR_BAD_SHAPE;
+        p.pair_axes[i / 4] |= static_cast<uint8_t>(pair_axes[i] << (2 * (i % 4)));
+    }
+    p.n_axes = n_axes;
+    return ATTN_OK;
+}
+
 template <bool PAGED>
 int launch_rope(attn_rope::RopeParams& p, int D, int dtype, cudaStream_t st) {
     rope_units(p, D);
@@ -170,7 +183,9 @@ int launch_rope(attn_rope::RopeParams& p, int D, int dtype, cudaStream_t st) {
     if (gy > 65535) gy = 65535;
     const dim3 grid(static_cast<unsigned>(gx), static_cast<unsigned>(gy));
 #define ATTN_ROPE_CASE(DD, TT) \
-    if (D == DD && dtype == TT) attn_rope::attn_rope_kernel<DD, TT, PAGED><<<grid, attn_rope::kWarps * 32, 0, st>>>(p);
+    if (D == DD && dtype == TT)                                                                          \
+        (p.n_axes ? attn_rope::attn_rope_kernel<DD, TT, PAGED, true> : attn_rope::attn_rope_kernel<DD, TT, PAGED, false>) \
+            <<<grid, attn_rope::kWarps * 32, 0, st>>>(p);
     ATTN_ROPE_CASE(64, 0)
     ATTN_ROPE_CASE(64, 1)
     ATTN_ROPE_CASE(128, 0)
@@ -225,7 +240,8 @@ int launch_rope_bwd_tma(const attn_rope::RopeParams& p, int B, int D, int dtype,
 #define ATTN_ROPE_CASE(DD, TT)                                                                                       \
     if (D == DD && dtype == TT) {                                                                                     \
         using C = attn_rope::TmaCfg<DD>;                                                                              \
-        auto kern = packed ? attn_rope::attn_rope_bwd_tma_kernel<DD, TT, true> : attn_rope::attn_rope_bwd_tma_kernel<DD, TT, false>; \
+        auto kern = p.n_axes ? (packed ? attn_rope::attn_rope_bwd_tma_kernel<DD, TT, true, true> : attn_rope::attn_rope_bwd_tma_kernel<DD, TT, false, true>) \
+                             : (packed ? attn_rope::attn_rope_bwd_tma_kernel<DD, TT, true, false> : attn_rope::attn_rope_bwd_tma_kernel<DD, TT, false, false>); \
         if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), C::SMEM)) return ATTN_ERR_CUDA;                  \
         kern<<<grid, C::THREADS, C::SMEM, st>>>(maps, tp);                                                            \
     }
@@ -252,6 +268,225 @@ int validate_window(int Sq, int* window, int sinks, int q_offset) {
     return ATTN_OK;
 }
 
+// Bytes of the gradient's partial sums.
+size_t rope_bwd_bytes(int D) { return head_dim_ok(D) ? static_cast<size_t>(kRopeBwdBlocks) * D * sizeof(float) : 0; }
+
+// The three calls of the rotation.  several: positions [n_axes][tokens], the axis of each pair in pair_axes.
+int norm_rope(const void* q, const void* k, const void* v, const long long* in_strides, const void* q_weight,
+                      const void* k_weight, int weight_f32, const float* cos_sin, int table_len, int R, int interleaved,
+                      const int* positions, float eps, void* q_out, void* k_out, void* v_out, int B, int S, int H, int Hkv,
+                      int D, int dtype, void* stream, bool several, int n_axes, const unsigned char* pair_axes) {
+    if (B < 0 || S < 0 || H < 0 || Hkv < 0 || S > kMaxSeq) return ATTN_ERR_BAD_SHAPE;
+    int rc = validate_rope(q_weight, k_weight, cos_sin, table_len, R, eps, D, dtype);
+    if (rc != ATTN_OK) return rc;
+    const int64_t tokens = static_cast<int64_t>(B) * S;
+    attn_rope::RopeParams p = {};
+    if (several) rc = set_axes(p, R, positions, tokens, n_axes, pair_axes);
+    if (rc != ATTN_OK) return rc;
+    if (!several && R > 0 && !positions && S > table_len) return ATTN_ERR_BAD_SHAPE;
+    if (tokens == 0 || (H == 0 && Hkv == 0)) return ATTN_OK;
+    if (!rope_tokens_ok(tokens, H, Hkv)) return ATTN_ERR_BAD_SHAPE;
+    if (!in_strides || (H > 0 && (!q || !q_out)) || (Hkv > 0 && (!k || !k_out || !v != !v_out))) return ATTN_ERR_NULL_POINTER;
+    if (misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(q_out, 16) || misaligned(k_out, 16) ||
+        misaligned(v_out, 16) || misaligned(positions, 4) || !strides_ok(in_strides, 9))
+        return ATTN_ERR_MISALIGNED;
+    rc = check_arch();
+    if (rc != ATTN_OK) return rc;
+    const void* in[3] = {q, k, v};
+    void* out[3] = {q_out, k_out, v_out};
+    const int heads[3] = {H, Hkv, v ? Hkv : 0};
+    for (int i = 0; i < 3; ++i) {
+        p.in[i] = in[i];
+        p.out[i] = out[i];
+        p.heads[i] = heads[i];
+        p.is[i] = attn_rope::Strides{in_strides[3 * i], in_strides[3 * i + 1], in_strides[3 * i + 2]};
+        p.os[i] = head_major(heads[i], S, D);
+    }
+    p.weight[0] = q_weight;
+    p.weight[1] = k_weight;
+    p.weight_f32 = weight_f32;
+    p.table = cos_sin;
+    p.table_len = table_len;
+    p.R = R;
+    p.interleaved = interleaved;
+    p.positions = positions;
+    p.eps = eps;
+    p.tokens = static_cast<int>(tokens);
+    p.S = S;
+    p.status = cached_status_ptr();
+    if (!p.status) return ATTN_ERR_CUDA;
+    return launch_rope<false>(p, D, dtype, static_cast<cudaStream_t>(stream));
+}
+
+int norm_rope_bwd(const void* dq, const void* dk, const void* dv, const void* q, const void* k,
+                          const long long* in_strides, const void* q_weight, const void* k_weight, int weight_f32,
+                          const float* cos_sin, int table_len, int R, int interleaved, const int* positions, float eps,
+                          void* dq_in, void* dk_in, void* dv_in, const long long* out_strides, float* dq_weight,
+                          float* dk_weight, int B, int S, int H, int Hkv, int D, int dtype, void* workspace,
+                          size_t workspace_bytes, void* stream, bool several, int n_axes, const unsigned char* pair_axes) {
+    if (B < 0 || S < 0 || H < 0 || Hkv < 0 || S > kMaxSeq) return ATTN_ERR_BAD_SHAPE;
+    int rc = validate_rope(q_weight, k_weight, cos_sin, table_len, R, eps, D, dtype);
+    if (rc != ATTN_OK) return rc;
+    const int64_t tokens = static_cast<int64_t>(B) * S;
+    attn_rope::RopeParams p = {};
+    if (several) rc = set_axes(p, R, positions, tokens, n_axes, pair_axes);
+    if (rc != ATTN_OK) return rc;
+    if (!several && R > 0 && !positions && S > table_len) return ATTN_ERR_BAD_SHAPE;
+    if (!rope_tokens_ok(tokens, H, Hkv)) return ATTN_ERR_BAD_SHAPE;
+    if ((q_weight && !dq_weight) || (k_weight && !dk_weight)) return ATTN_ERR_NULL_POINTER;
+    if (misaligned(dq_weight, 4) || misaligned(dk_weight, 4)) return ATTN_ERR_MISALIGNED;
+    if (tokens > 0) {
+        if (!in_strides || !out_strides) return ATTN_ERR_NULL_POINTER;
+        if (H > 0 && (!dq || !dq_in || (q_weight && !q))) return ATTN_ERR_NULL_POINTER;
+        if (Hkv > 0 && (!dk || !dk_in || (k_weight && !k) || !dv != !dv_in)) return ATTN_ERR_NULL_POINTER;
+        if (misaligned(dq, 16) || misaligned(dk, 16) || misaligned(dv, 16) || misaligned(q, 16) || misaligned(k, 16) ||
+            misaligned(dq_in, 16) || misaligned(dk_in, 16) || misaligned(dv_in, 16) || misaligned(positions, 4) ||
+            !strides_ok(in_strides, 6) || !strides_ok(out_strides, 9))
+            return ATTN_ERR_MISALIGNED;
+        const int heads[3] = {H, Hkv, dv ? Hkv : 0};
+        for (int i = 0; i < 3; ++i) {   // an output whose rows lie on top of each other
+            const long long* s = out_strides + 3 * i;
+            if (heads[i] > 0 && ((B > 1 && s[0] == 0) || (S > 1 && s[1] == 0) || (heads[i] > 1 && s[2] == 0))) return ATTN_ERR_BAD_SHAPE;
+        }
+    }
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < rope_bwd_bytes(D)) return ATTN_ERR_WORKSPACE;
+    rc = check_arch();
+    if (rc != ATTN_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (tokens == 0 || (H == 0 && Hkv == 0)) {
+        if (dq_weight && cudaMemsetAsync(dq_weight, 0, D * sizeof(float), st) != cudaSuccess) return ATTN_ERR_CUDA;
+        if (dk_weight && cudaMemsetAsync(dk_weight, 0, D * sizeof(float), st) != cudaSuccess) return ATTN_ERR_CUDA;
+        return ATTN_OK;
+    }
+    const void* in[3] = {q, k, nullptr};
+    const void* dy[3] = {dq, dk, dv};
+    void* out[3] = {dq_in, dk_in, dv_in};
+    const int heads[3] = {H, Hkv, dv ? Hkv : 0};
+    for (int i = 0; i < 3; ++i) {
+        p.in[i] = in[i];
+        p.dy[i] = dy[i];
+        p.out[i] = out[i];
+        p.heads[i] = heads[i];
+        if (i < 2) p.is[i] = attn_rope::Strides{in_strides[3 * i], in_strides[3 * i + 1], in_strides[3 * i + 2]};
+        p.os[i] = attn_rope::Strides{out_strides[3 * i], out_strides[3 * i + 1], out_strides[3 * i + 2]};
+        p.ds[i] = head_major(heads[i], S, D);
+    }
+    p.weight[0] = q_weight;
+    p.weight[1] = k_weight;
+    p.weight_f32 = weight_f32;
+    p.table = cos_sin;
+    p.table_len = table_len;
+    p.R = R;
+    p.interleaved = interleaved;
+    p.positions = positions;
+    p.eps = eps;
+    p.tokens = static_cast<int>(tokens);
+    p.S = S;
+    p.partial = static_cast<float*>(workspace);
+    p.status = cached_status_ptr();
+    if (!p.status) return ATTN_ERR_CUDA;
+    bool launched;
+    int ctas;
+    rc = launch_rope_bwd_tma(p, B, D, dtype, st, &launched, &ctas);
+    if (rc != ATTN_OK) return rc;
+    const bool sums = dq_weight || dk_weight;
+    if (launched)
+        return !sums || launch_dependent(attn_rope::attn_rope_weight_grad_kernel, dim3(2 * D / 32), dim3(1024), 0, st, p.partial, ctas,
+                                         p.partial + D, ctas, 2 * D, D, dq_weight, dk_weight)
+                   ? ATTN_OK
+                   : ATTN_ERR_CUDA;
+    // blocks of q and of (k, v): by their bytes (a row of q or k is read twice and written, of v read and written), each at
+    // least one where it has heads, and no more than it has items
+    const int per_unit = attn_rope::kDeep * (256 / D);
+    const int64_t steps = (tokens + attn_rope::kWarps - 1) / attn_rope::kWarps;
+    const int64_t q_items = steps * ((H + per_unit - 1) / per_unit), k_items = steps * ((Hkv + per_unit - 1) / per_unit);
+    const double q_cost = 3.0 * H, kv_cost = (dv ? 5.0 : 3.0) * Hkv;
+    int64_t q_blocks = H == 0 ? 0 : static_cast<int64_t>(kRopeBwdBlocks * q_cost / (q_cost + kv_cost) + 0.5);
+    if (H > 0 && q_blocks < 1) q_blocks = 1;
+    if (Hkv > 0 && q_blocks > kRopeBwdBlocks - 1) q_blocks = kRopeBwdBlocks - 1;
+    int64_t kv_blocks = Hkv == 0 ? 0 : kRopeBwdBlocks - q_blocks;
+    if (q_blocks > q_items) q_blocks = q_items;
+    if (kv_blocks > k_items) kv_blocks = k_items;
+    const int64_t blocks = q_blocks + kv_blocks;
+    p.q_blocks = static_cast<int>(q_blocks);
+#define ATTN_ROPE_CASE(DD, TT) \
+    if (D == DD && dtype == TT)                                                                                    \
+        (p.n_axes ? attn_rope::attn_rope_bwd_kernel<DD, TT, true> : attn_rope::attn_rope_bwd_kernel<DD, TT, false>) \
+            <<<static_cast<unsigned>(blocks), attn_rope::kWarps * 32, 0, st>>>(p);
+    ATTN_ROPE_CASE(64, 0)
+    ATTN_ROPE_CASE(64, 1)
+    ATTN_ROPE_CASE(128, 0)
+    ATTN_ROPE_CASE(128, 1)
+    ATTN_ROPE_CASE(256, 0)
+    ATTN_ROPE_CASE(256, 1)
+#undef ATTN_ROPE_CASE
+    if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
+    return !sums || launch_dependent(attn_rope::attn_rope_weight_grad_kernel, dim3(2 * D / 32), dim3(1024), 0, st, p.partial, p.q_blocks,
+                                     p.partial + static_cast<int64_t>(p.q_blocks) * D, static_cast<int>(kv_blocks), D, D, dq_weight,
+                                     dk_weight)
+               ? ATTN_OK
+               : ATTN_ERR_CUDA;
+}
+
+int paged_append(const void* q, const void* k, const void* v, const long long* in_strides, const void* q_weight,
+                      const void* k_weight, int weight_f32, const float* cos_sin, int table_len, int R, int interleaved,
+                      float eps, void* q_out, void* k_cache, void* v_cache, const long long* cache_strides, int num_pages,
+                      int page_size, const int* block_table, long long table_stride, int max_pages, const int* seq_lens,
+                      const int* cu_seqlens, int n_seqs, int tokens, int H, int Hkv, int D, int dtype, void* stream, bool several,
+                      const int* positions, int n_axes, const unsigned char* pair_axes) {
+    if (n_seqs < 0 || tokens < 0 || H < 0 || Hkv < 0 || (!cu_seqlens && tokens != n_seqs)) return ATTN_ERR_BAD_SHAPE;
+    int rc = validate_rope(q_weight, k_weight, cos_sin, table_len, R, eps, D, dtype);
+    if (rc != ATTN_OK) return rc;
+    attn_rope::RopeParams p = {};
+    if (several) rc = set_axes(p, R, positions, tokens, n_axes, pair_axes);
+    if (rc != ATTN_OK) return rc;
+    if (tokens == 0 || n_seqs == 0 || (H == 0 && Hkv == 0)) return ATTN_OK;
+    if (!in_strides || !q != !q_out || (Hkv > 0 && (!k || !v)) || (H > 0 && !q && Hkv == 0)) return ATTN_ERR_NULL_POINTER;
+    rc = validate_cache(k_cache, v_cache, cache_strides, num_pages, page_size, block_table, max_pages, seq_lens);
+    if (rc != ATTN_OK) return rc;
+    if (misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(q_out, 16) || misaligned(cu_seqlens, 4) ||
+        !strides_ok(in_strides, 6))
+        return ATTN_ERR_MISALIGNED;
+    for (int i = 0; i < 2; ++i) {   // cache rows that lie on top of each other
+        const long long* s = cache_strides + 3 * i;
+        if (Hkv > 0 && ((num_pages > 1 && s[0] == 0) || (Hkv > 1 && s[1] == 0) || (page_size > 1 && s[2] == 0))) return ATTN_ERR_BAD_SHAPE;
+    }
+    rc = check_arch();
+    if (rc != ATTN_OK) return rc;
+    const void* in[3] = {q, k, v};
+    void* out[3] = {q_out, k_cache, v_cache};
+    const int heads[3] = {q ? H : 0, Hkv, Hkv};
+    for (int i = 0; i < 3; ++i) {
+        p.in[i] = in[i];
+        p.out[i] = out[i];
+        p.heads[i] = heads[i];
+        p.is[i] = attn_rope::Strides{0, in_strides[2 * i], in_strides[2 * i + 1]};
+    }
+    p.os[0] = attn_rope::Strides{0, static_cast<int64_t>(H) * D, D};
+    for (int i = 0; i < 2; ++i) p.os[1 + i] = attn_rope::Strides{cache_strides[3 * i], cache_strides[3 * i + 2], cache_strides[3 * i + 1]};
+    p.weight[0] = q_weight;
+    p.weight[1] = k_weight;
+    p.weight_f32 = weight_f32;
+    p.table = cos_sin;
+    p.table_len = table_len;
+    p.R = R;
+    p.interleaved = interleaved;
+    p.eps = eps;
+    p.tokens = tokens;
+    p.S = tokens;
+    p.positions = positions;
+    p.cu_seqlens = cu_seqlens;
+    p.seq_lens = seq_lens;
+    p.block_table = block_table;
+    p.table_stride = table_stride;
+    p.n_seqs = n_seqs;
+    p.max_len = max_pages * page_size;
+    p.num_pages = num_pages;
+    p.page_shift = log2_of(page_size);
+    p.status = cached_status_ptr();
+    if (!p.status) return ATTN_ERR_CUDA;
+    return launch_rope<true>(p, D, dtype, static_cast<cudaStream_t>(stream));
+}
 
 }  // namespace
 
@@ -307,49 +542,19 @@ int attn_qk_norm_rope(const void* q, const void* k, const void* v, const long lo
                       const void* k_weight, int weight_f32, const float* cos_sin, int table_len, int R, int interleaved,
                       const int* positions, float eps, void* q_out, void* k_out, void* v_out, int B, int S, int H, int Hkv,
                       int D, int dtype, void* stream) {
-    if (B < 0 || S < 0 || H < 0 || Hkv < 0 || S > kMaxSeq) return ATTN_ERR_BAD_SHAPE;
-    int rc = validate_rope(q_weight, k_weight, cos_sin, table_len, R, eps, D, dtype);
-    if (rc != ATTN_OK) return rc;
-    if (R > 0 && !positions && S > table_len) return ATTN_ERR_BAD_SHAPE;
-    const int64_t tokens = static_cast<int64_t>(B) * S;
-    if (tokens == 0 || (H == 0 && Hkv == 0)) return ATTN_OK;
-    if (!rope_tokens_ok(tokens, H, Hkv)) return ATTN_ERR_BAD_SHAPE;
-    if (!in_strides || (H > 0 && (!q || !q_out)) || (Hkv > 0 && (!k || !k_out || !v != !v_out))) return ATTN_ERR_NULL_POINTER;
-    if (misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(q_out, 16) || misaligned(k_out, 16) ||
-        misaligned(v_out, 16) || misaligned(positions, 4) || !strides_ok(in_strides, 9))
-        return ATTN_ERR_MISALIGNED;
-    rc = check_arch();
-    if (rc != ATTN_OK) return rc;
-    attn_rope::RopeParams p = {};
-    const void* in[3] = {q, k, v};
-    void* out[3] = {q_out, k_out, v_out};
-    const int heads[3] = {H, Hkv, v ? Hkv : 0};
-    for (int i = 0; i < 3; ++i) {
-        p.in[i] = in[i];
-        p.out[i] = out[i];
-        p.heads[i] = heads[i];
-        p.is[i] = attn_rope::Strides{in_strides[3 * i], in_strides[3 * i + 1], in_strides[3 * i + 2]};
-        p.os[i] = head_major(heads[i], S, D);
-    }
-    p.weight[0] = q_weight;
-    p.weight[1] = k_weight;
-    p.weight_f32 = weight_f32;
-    p.table = cos_sin;
-    p.table_len = table_len;
-    p.R = R;
-    p.interleaved = interleaved;
-    p.positions = positions;
-    p.eps = eps;
-    p.tokens = static_cast<int>(tokens);
-    p.S = S;
-    p.status = cached_status_ptr();
-    if (!p.status) return ATTN_ERR_CUDA;
-    return launch_rope<false>(p, D, dtype, static_cast<cudaStream_t>(stream));
+    return norm_rope(q, k, v, in_strides, q_weight, k_weight, weight_f32, cos_sin, table_len, R, interleaved, positions, eps, q_out, k_out,
+                     v_out, B, S, H, Hkv, D, dtype, stream, false, 0, nullptr);
 }
 
-size_t attn_qk_norm_rope_bwd_workspace_bytes(int D) {
-    return head_dim_ok(D) ? static_cast<size_t>(kRopeBwdBlocks) * D * sizeof(float) : 0;
+int attn_qk_norm_rope_axes(const void* q, const void* k, const void* v, const long long* in_strides, const void* q_weight,
+                           const void* k_weight, int weight_f32, const float* cos_sin, int table_len, int R, int interleaved,
+                           const int* positions, int n_axes, const unsigned char* pair_axes, float eps, void* q_out, void* k_out,
+                           void* v_out, int B, int S, int H, int Hkv, int D, int dtype, void* stream) {
+    return norm_rope(q, k, v, in_strides, q_weight, k_weight, weight_f32, cos_sin, table_len, R, interleaved, positions, eps, q_out, k_out,
+                     v_out, B, S, H, Hkv, D, dtype, stream, true, n_axes, pair_axes);
 }
+
+size_t attn_qk_norm_rope_bwd_workspace_bytes(int D) { return rope_bwd_bytes(D); }
 
 int attn_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const void* q, const void* k,
                           const long long* in_strides, const void* q_weight, const void* k_weight, int weight_f32,
@@ -357,104 +562,20 @@ int attn_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const 
                           void* dq_in, void* dk_in, void* dv_in, const long long* out_strides, float* dq_weight,
                           float* dk_weight, int B, int S, int H, int Hkv, int D, int dtype, void* workspace,
                           size_t workspace_bytes, void* stream) {
-    if (B < 0 || S < 0 || H < 0 || Hkv < 0 || S > kMaxSeq) return ATTN_ERR_BAD_SHAPE;
-    int rc = validate_rope(q_weight, k_weight, cos_sin, table_len, R, eps, D, dtype);
-    if (rc != ATTN_OK) return rc;
-    if (R > 0 && !positions && S > table_len) return ATTN_ERR_BAD_SHAPE;
-    const int64_t tokens = static_cast<int64_t>(B) * S;
-    if (!rope_tokens_ok(tokens, H, Hkv)) return ATTN_ERR_BAD_SHAPE;
-    if ((q_weight && !dq_weight) || (k_weight && !dk_weight)) return ATTN_ERR_NULL_POINTER;
-    if (misaligned(dq_weight, 4) || misaligned(dk_weight, 4)) return ATTN_ERR_MISALIGNED;
-    if (tokens > 0) {
-        if (!in_strides || !out_strides) return ATTN_ERR_NULL_POINTER;
-        if (H > 0 && (!dq || !dq_in || (q_weight && !q))) return ATTN_ERR_NULL_POINTER;
-        if (Hkv > 0 && (!dk || !dk_in || (k_weight && !k) || !dv != !dv_in)) return ATTN_ERR_NULL_POINTER;
-        if (misaligned(dq, 16) || misaligned(dk, 16) || misaligned(dv, 16) || misaligned(q, 16) || misaligned(k, 16) ||
-            misaligned(dq_in, 16) || misaligned(dk_in, 16) || misaligned(dv_in, 16) || misaligned(positions, 4) ||
-            !strides_ok(in_strides, 6) || !strides_ok(out_strides, 9))
-            return ATTN_ERR_MISALIGNED;
-        const int heads[3] = {H, Hkv, dv ? Hkv : 0};
-        for (int i = 0; i < 3; ++i) {   // an output whose rows lie on top of each other
-            const long long* s = out_strides + 3 * i;
-            if (heads[i] > 0 && ((B > 1 && s[0] == 0) || (S > 1 && s[1] == 0) || (heads[i] > 1 && s[2] == 0))) return ATTN_ERR_BAD_SHAPE;
-        }
-    }
-    if (!workspace || misaligned(workspace, 256) || workspace_bytes < attn_qk_norm_rope_bwd_workspace_bytes(D)) return ATTN_ERR_WORKSPACE;
-    rc = check_arch();
-    if (rc != ATTN_OK) return rc;
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (tokens == 0 || (H == 0 && Hkv == 0)) {
-        if (dq_weight && cudaMemsetAsync(dq_weight, 0, D * sizeof(float), st) != cudaSuccess) return ATTN_ERR_CUDA;
-        if (dk_weight && cudaMemsetAsync(dk_weight, 0, D * sizeof(float), st) != cudaSuccess) return ATTN_ERR_CUDA;
-        return ATTN_OK;
-    }
-    attn_rope::RopeParams p = {};
-    const void* in[3] = {q, k, nullptr};
-    const void* dy[3] = {dq, dk, dv};
-    void* out[3] = {dq_in, dk_in, dv_in};
-    const int heads[3] = {H, Hkv, dv ? Hkv : 0};
-    for (int i = 0; i < 3; ++i) {
-        p.in[i] = in[i];
-        p.dy[i] = dy[i];
-        p.out[i] = out[i];
-        p.heads[i] = heads[i];
-        if (i < 2) p.is[i] = attn_rope::Strides{in_strides[3 * i], in_strides[3 * i + 1], in_strides[3 * i + 2]};
-        p.os[i] = attn_rope::Strides{out_strides[3 * i], out_strides[3 * i + 1], out_strides[3 * i + 2]};
-        p.ds[i] = head_major(heads[i], S, D);
-    }
-    p.weight[0] = q_weight;
-    p.weight[1] = k_weight;
-    p.weight_f32 = weight_f32;
-    p.table = cos_sin;
-    p.table_len = table_len;
-    p.R = R;
-    p.interleaved = interleaved;
-    p.positions = positions;
-    p.eps = eps;
-    p.tokens = static_cast<int>(tokens);
-    p.S = S;
-    p.partial = static_cast<float*>(workspace);
-    p.status = cached_status_ptr();
-    if (!p.status) return ATTN_ERR_CUDA;
-    bool launched;
-    int ctas;
-    rc = launch_rope_bwd_tma(p, B, D, dtype, st, &launched, &ctas);
-    if (rc != ATTN_OK) return rc;
-    const bool sums = dq_weight || dk_weight;
-    if (launched)
-        return !sums || launch_dependent(attn_rope::attn_rope_weight_grad_kernel, dim3(2 * D / 32), dim3(1024), 0, st, p.partial, ctas,
-                                         p.partial + D, ctas, 2 * D, D, dq_weight, dk_weight)
-                   ? ATTN_OK
-                   : ATTN_ERR_CUDA;
-    // blocks of q and of (k, v): by their bytes (a row of q or k is read twice and written, of v read and written), each at
-    // least one where it has heads, and no more than it has items
-    const int per_unit = attn_rope::kDeep * (256 / D);
-    const int64_t steps = (tokens + attn_rope::kWarps - 1) / attn_rope::kWarps;
-    const int64_t q_items = steps * ((H + per_unit - 1) / per_unit), k_items = steps * ((Hkv + per_unit - 1) / per_unit);
-    const double q_cost = 3.0 * H, kv_cost = (dv ? 5.0 : 3.0) * Hkv;
-    int64_t q_blocks = H == 0 ? 0 : static_cast<int64_t>(kRopeBwdBlocks * q_cost / (q_cost + kv_cost) + 0.5);
-    if (H > 0 && q_blocks < 1) q_blocks = 1;
-    if (Hkv > 0 && q_blocks > kRopeBwdBlocks - 1) q_blocks = kRopeBwdBlocks - 1;
-    int64_t kv_blocks = Hkv == 0 ? 0 : kRopeBwdBlocks - q_blocks;
-    if (q_blocks > q_items) q_blocks = q_items;
-    if (kv_blocks > k_items) kv_blocks = k_items;
-    const int64_t blocks = q_blocks + kv_blocks;
-    p.q_blocks = static_cast<int>(q_blocks);
-#define ATTN_ROPE_CASE(DD, TT) \
-    if (D == DD && dtype == TT) attn_rope::attn_rope_bwd_kernel<DD, TT><<<static_cast<unsigned>(blocks), attn_rope::kWarps * 32, 0, st>>>(p);
-    ATTN_ROPE_CASE(64, 0)
-    ATTN_ROPE_CASE(64, 1)
-    ATTN_ROPE_CASE(128, 0)
-    ATTN_ROPE_CASE(128, 1)
-    ATTN_ROPE_CASE(256, 0)
-    ATTN_ROPE_CASE(256, 1)
-#undef ATTN_ROPE_CASE
-    if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;
-    return !sums || launch_dependent(attn_rope::attn_rope_weight_grad_kernel, dim3(2 * D / 32), dim3(1024), 0, st, p.partial, p.q_blocks,
-                                     p.partial + static_cast<int64_t>(p.q_blocks) * D, static_cast<int>(kv_blocks), D, D, dq_weight,
-                                     dk_weight)
-               ? ATTN_OK
-               : ATTN_ERR_CUDA;
+    return norm_rope_bwd(dq, dk, dv, q, k, in_strides, q_weight, k_weight, weight_f32, cos_sin, table_len, R, interleaved, positions, eps,
+                         dq_in, dk_in, dv_in, out_strides, dq_weight, dk_weight, B, S, H, Hkv, D, dtype, workspace, workspace_bytes, stream,
+                         false, 0, nullptr);
+}
+
+int attn_qk_norm_rope_axes_bwd(const void* dq, const void* dk, const void* dv, const void* q, const void* k,
+                               const long long* in_strides, const void* q_weight, const void* k_weight, int weight_f32,
+                               const float* cos_sin, int table_len, int R, int interleaved, const int* positions, int n_axes,
+                               const unsigned char* pair_axes, float eps, void* dq_in, void* dk_in, void* dv_in,
+                               const long long* out_strides, float* dq_weight, float* dk_weight, int B, int S, int H, int Hkv,
+                               int D, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    return norm_rope_bwd(dq, dk, dv, q, k, in_strides, q_weight, k_weight, weight_f32, cos_sin, table_len, R, interleaved, positions, eps,
+                         dq_in, dk_in, dv_in, out_strides, dq_weight, dk_weight, B, S, H, Hkv, D, dtype, workspace, workspace_bytes, stream,
+                         true, n_axes, pair_axes);
 }
 
 int attn_paged_append(const void* q, const void* k, const void* v, const long long* in_strides, const void* q_weight,
@@ -462,55 +583,20 @@ int attn_paged_append(const void* q, const void* k, const void* v, const long lo
                       float eps, void* q_out, void* k_cache, void* v_cache, const long long* cache_strides, int num_pages,
                       int page_size, const int* block_table, long long table_stride, int max_pages, const int* seq_lens,
                       const int* cu_seqlens, int n_seqs, int tokens, int H, int Hkv, int D, int dtype, void* stream) {
-    if (n_seqs < 0 || tokens < 0 || H < 0 || Hkv < 0 || (!cu_seqlens && tokens != n_seqs)) return ATTN_ERR_BAD_SHAPE;
-    int rc = validate_rope(q_weight, k_weight, cos_sin, table_len, R, eps, D, dtype);
-    if (rc != ATTN_OK) return rc;
-    if (tokens == 0 || n_seqs == 0 || (H == 0 && Hkv == 0)) return ATTN_OK;
-    if (!in_strides || !q != !q_out || (Hkv > 0 && (!k || !v)) || (H > 0 && !q && Hkv == 0)) return ATTN_ERR_NULL_POINTER;
-    rc = validate_cache(k_cache, v_cache, cache_strides, num_pages, page_size, block_table, max_pages, seq_lens);
-    if (rc != ATTN_OK) return rc;
-    if (misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(q_out, 16) || misaligned(cu_seqlens, 4) ||
-        !strides_ok(in_strides, 6))
-        return ATTN_ERR_MISALIGNED;
-    for (int i = 0; i < 2; ++i) {   // cache rows that lie on top of each other
-        const long long* s = cache_strides + 3 * i;
-        if (Hkv > 0 && ((num_pages > 1 && s[0] == 0) || (Hkv > 1 && s[1] == 0) || (page_size > 1 && s[2] == 0))) return ATTN_ERR_BAD_SHAPE;
-    }
-    rc = check_arch();
-    if (rc != ATTN_OK) return rc;
-    attn_rope::RopeParams p = {};
-    const void* in[3] = {q, k, v};
-    void* out[3] = {q_out, k_cache, v_cache};
-    const int heads[3] = {q ? H : 0, Hkv, Hkv};
-    for (int i = 0; i < 3; ++i) {
-        p.in[i] = in[i];
-        p.out[i] = out[i];
-        p.heads[i] = heads[i];
-        p.is[i] = attn_rope::Strides{0, in_strides[2 * i], in_strides[2 * i + 1]};
-    }
-    p.os[0] = attn_rope::Strides{0, static_cast<int64_t>(H) * D, D};
-    for (int i = 0; i < 2; ++i) p.os[1 + i] = attn_rope::Strides{cache_strides[3 * i], cache_strides[3 * i + 2], cache_strides[3 * i + 1]};
-    p.weight[0] = q_weight;
-    p.weight[1] = k_weight;
-    p.weight_f32 = weight_f32;
-    p.table = cos_sin;
-    p.table_len = table_len;
-    p.R = R;
-    p.interleaved = interleaved;
-    p.eps = eps;
-    p.tokens = tokens;
-    p.S = tokens;
-    p.cu_seqlens = cu_seqlens;
-    p.seq_lens = seq_lens;
-    p.block_table = block_table;
-    p.table_stride = table_stride;
-    p.n_seqs = n_seqs;
-    p.max_len = max_pages * page_size;
-    p.num_pages = num_pages;
-    p.page_shift = log2_of(page_size);
-    p.status = cached_status_ptr();
-    if (!p.status) return ATTN_ERR_CUDA;
-    return launch_rope<true>(p, D, dtype, static_cast<cudaStream_t>(stream));
+    return paged_append(q, k, v, in_strides, q_weight, k_weight, weight_f32, cos_sin, table_len, R, interleaved, eps, q_out, k_cache, v_cache,
+                        cache_strides, num_pages, page_size, block_table, table_stride, max_pages, seq_lens, cu_seqlens, n_seqs, tokens, H,
+                        Hkv, D, dtype, stream, false, nullptr, 0, nullptr);
+}
+
+int attn_paged_append_axes(const void* q, const void* k, const void* v, const long long* in_strides, const void* q_weight,
+                           const void* k_weight, int weight_f32, const float* cos_sin, int table_len, int R, int interleaved,
+                           const int* positions, int n_axes, const unsigned char* pair_axes, float eps, void* q_out,
+                           void* k_cache, void* v_cache, const long long* cache_strides, int num_pages, int page_size,
+                           const int* block_table, long long table_stride, int max_pages, const int* seq_lens,
+                           const int* cu_seqlens, int n_seqs, int tokens, int H, int Hkv, int D, int dtype, void* stream) {
+    return paged_append(q, k, v, in_strides, q_weight, k_weight, weight_f32, cos_sin, table_len, R, interleaved, eps, q_out, k_cache, v_cache,
+                        cache_strides, num_pages, page_size, block_table, table_stride, max_pages, seq_lens, cu_seqlens, n_seqs, tokens, H,
+                        Hkv, D, dtype, stream, true, positions, n_axes, pair_axes);
 }
 
 size_t attn_paged_decode_workspace_bytes(int H, int Hkv, int D) {

@@ -3,6 +3,8 @@
 //
 //     n = x rsqrt(mean(x^2) + eps) w   (over one head's D values),     y = R_pos n :
 //     pair i < R/2 of the first R values turns by the angle whose cosine and sine are row pos of the table.
+//     With several position axes (time, height, width, ..) each pair belongs to one of them, and turns by the row of that axis'
+//     position.
 //     Gradient, with g = R_pos^T dy, r = rsqrt(mean(x^2) + eps):  dx = r (g w) - x r^3 mean(g w x),   dw = sum g x r.
 //
 // Memory-bound: each value is read and written once.  The limit on the way there is the issue rate, so the arithmetic per
@@ -43,7 +45,9 @@ struct RopeParams {
     int weight_f32;
     const float* table;         // [table_len][R]: R/2 cosines, R/2 sines
     int table_len, R, interleaved;
-    const int* positions;       // [B, S]; NULL: the token's index in its sequence
+    const int* positions;       // [B, S]; NULL: the token's index in its sequence.  With several axes [axes][B, S] (paged: [axes][tokens])
+    int n_axes;                 // several axes: their number, and the axis of each pair: four pairs to a byte, 2 bits each
+    uint8_t pair_axes[32];
     float eps;
     int tokens;                 // B * S, or tokens of the batch
     int S;
@@ -173,20 +177,91 @@ __device__ __forceinline__ void turn_values(F2* y, const F2* x, const F2* cs, co
     }
 }
 
+// The axes of a lane's four pairs, 2 bits each.  `same`: in every lane of the warp the four pairs belong to one axis (runs of pairs
+// per axis whose lengths are multiples of 4): two 16-byte loads of the table per lane and token, as with one axis.  Axes that
+// take turns need eight single loads.
+struct PairAxes {
+    unsigned of;
+    bool same;
+    __device__ __forceinline__ PairAxes(const RopeParams& p, int l) {
+        of = 8 * l < p.R ? p.pair_axes[l] : 0u;
+        same = __all_sync(0xffffffffu, of == (of & 3u) * 0x55u);
+    }
+};
+
+// One token's positions on all axes.
+struct AxisPositions {
+    int at[4];
+    // false: one of them is out of range (all are 0 then)
+    __device__ __forceinline__ bool load(const RopeParams& p, int64_t token) {
+        bool ok = true;
+#pragma unroll
+        for (int a = 0; a < 4; ++a) at[a] = a < p.n_axes ? __ldg(p.positions + a * static_cast<int64_t>(p.tokens) + token) : 0;
+#pragma unroll
+        for (int a = 0; a < 4; ++a) ok = ok && (p.R == 0 || static_cast<unsigned>(at[a]) < static_cast<unsigned>(p.table_len));
+        if (!ok) at[0] = at[1] = at[2] = at[3] = 0;
+        return ok;
+    }
+    // the position of pair i of a lane's four
+    __device__ __forceinline__ int of_pair(const PairAxes& axes, int i) const {
+        const unsigned a = axes.of >> (2 * i);
+        return a & 2u ? (a & 1u ? at[3] : at[2]) : (a & 1u ? at[1] : at[0]);
+    }
+};
+
 // One token's rotation, for the values of a lane: y_e = n_e cs_e + partner_e sn_e.
 struct Turn {
     F2 cs[4], sn[4];
     // back: the transposed rotation
     __device__ __forceinline__ void load(const RopeParams& p, int pos, int l, const Place& at, bool back) {
         if (!at.turns) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { cs[e] = F2(1.f, 1.f); sn[e] = F2(0.f, 0.f); }
+            none();
             return;
         }
-        const float flip = back ? -1.f : 1.f;
         const float* row = p.table + static_cast<int64_t>(pos) * p.R;     // either way pairs 4 l .. 4 l + 3
-        const float4 c = __ldg(reinterpret_cast<const float4*>(row + 4 * l));
-        float4 s = __ldg(reinterpret_cast<const float4*>(row + (p.R >> 1) + 4 * l));
+        set(p, __ldg(reinterpret_cast<const float4*>(row + 4 * l)), __ldg(reinterpret_cast<const float4*>(row + (p.R >> 1) + 4 * l)), back);
+    }
+    __device__ __forceinline__ void load_axes(const RopeParams& p, const AxisPositions& pos, const PairAxes& axes, int l, const Place& at, bool back) {
+        if (!at.turns) {
+            none();
+            return;
+        }
+        const int half = p.R >> 1;
+        auto row = [&](int i) { return p.table + static_cast<int64_t>(pos.of_pair(axes, i)) * p.R + 4 * l; };
+        if (axes.same) {
+            set(p, __ldg(reinterpret_cast<const float4*>(row(0))), __ldg(reinterpret_cast<const float4*>(row(0) + half)), back);
+        } else {
+            const float *r0 = row(0), *r1 = row(1), *r2 = row(2), *r3 = row(3);
+            const float4 c = make_float4(__ldg(r0), __ldg(r1 + 1), __ldg(r2 + 2), __ldg(r3 + 3));
+            const float4 s = make_float4(__ldg(r0 + half), __ldg(r1 + half + 1), __ldg(r2 + half + 2), __ldg(r3 + half + 3));
+            set(p, c, s, back);
+        }
+    }
+    // The transposed rotation of token `token` of all, the s-th of its sequence.  False: a position is out of range (and reported).
+    template <bool AXES>
+    __device__ __forceinline__ bool load_token(const RopeParams& p, int64_t token, int s, const PairAxes& axes, int l, const Place& at) {
+        bool ok = true;
+        if constexpr (AXES) {
+            AxisPositions pos;
+            ok = pos.load(p, token);
+            load_axes(p, pos, axes, l, at, true);
+        } else {
+            int pos = p.positions ? __ldg(p.positions + token) : s;
+            if (p.R > 0 && static_cast<unsigned>(pos) >= static_cast<unsigned>(p.table_len)) {
+                ok = false;
+                pos = 0;
+            }
+            load(p, pos, l, at, true);
+        }
+        if (!ok) report_bad_index(p.status);
+        return ok;
+    }
+    __device__ __forceinline__ void none() {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { cs[e] = F2(1.f, 1.f); sn[e] = F2(0.f, 0.f); }
+    }
+    __device__ __forceinline__ void set(const RopeParams& p, const float4& c, float4 s, bool back) {
+        const float flip = back ? -1.f : 1.f;
         s.x *= flip; s.y *= flip; s.z *= flip; s.w *= flip;
         if (p.interleaved) {
             cs[0] = F2(c.x, c.x); cs[1] = F2(c.y, c.y); cs[2] = F2(c.z, c.z); cs[3] = F2(c.w, c.w);
@@ -209,6 +284,8 @@ __device__ __forceinline__ float row_sum(float x) {
 
 // Where one token's rows go in the paged form.  Returns the position, or -1 when the token is not written (padding before the
 // first sequence's new tokens or behind the last one's, or an entry that is out of range).
+// AXES: the rotation has positions of its own.
+template <bool AXES>
 __device__ __forceinline__ int place_token(const RopeParams& p, int t, int& page, int& slot) {
     int seq, pos;
     if (p.cu_seqlens) {
@@ -229,7 +306,7 @@ __device__ __forceinline__ int place_token(const RopeParams& p, int t, int& page
         if (len <= 0) return -1;      // a padded row of a batch
         pos = len - 1;
     }
-    if (pos < 0 || pos >= p.max_len || (p.R > 0 && pos >= p.table_len)) {
+    if (pos < 0 || pos >= p.max_len || (!AXES && p.R > 0 && pos >= p.table_len)) {
         report_bad_index(p.status);
         return -1;
     }
@@ -243,7 +320,7 @@ __device__ __forceinline__ int place_token(const RopeParams& p, int t, int& page
 }
 
 // grid: (blocks of 8 tokens, parts of the unit list)
-template <int D, int DTYPE, bool PAGED>
+template <int D, int DTYPE, bool PAGED, bool AXES>
 __global__ void __launch_bounds__(kWarps * 32, 4)
 attn_rope_kernel(const RopeParams p) {
     constexpr int LPR = D / 8, RPW = 32 / LPR;
@@ -277,14 +354,23 @@ attn_rope_kernel(const RopeParams p) {
     int pos, page = 0, slot = 0;
     float bad = 1.f;             // NaN: the token's q and k rows become NaN
     if constexpr (PAGED) {
-        pos = place_token(p, token, page, slot);
+        pos = place_token<AXES>(p, token, page, slot);
         if (pos < 0) return;
-    } else {
+    } else if constexpr (!AXES) {
         pos = p.positions ? __ldg(p.positions + token) : s;
         if (p.R > 0 && static_cast<unsigned>(pos) >= static_cast<unsigned>(p.table_len)) {
             report_bad_index(p.status);
             bad = __int_as_float(0x7fffffff);
             pos = 0;
+        }
+    }
+    AxisPositions axis_pos;
+    const PairAxes axes(p, l);   // (dead code without AXES)
+    if constexpr (AXES) {
+        if (!axis_pos.load(p, token)) {
+            report_bad_index(p.status);
+            if (PAGED) return;   // skipped, like a token whose place in the cache is out of range
+            bad = __int_as_float(0x7fffffff);
         }
     }
 #pragma unroll
@@ -297,7 +383,7 @@ attn_rope_kernel(const RopeParams p) {
                         (cache ? page * p.os[kind].batch + slot * p.os[kind].token : b * p.os[kind].batch + s * p.os[kind].token) * 2;
         Turn f;                  // the rotation with the weights folded in
         if (kind < 2) {
-            f.load(p, pos, l, at, false);
+            if constexpr (AXES) f.load_axes(p, axis_pos, axes, l, at, false); else f.load(p, pos, l, at, false);
             if (norm) {
                 F2 w[4];
                 load_weight<DTYPE>(p.weight[kind], p.weight_f32, at, w);
@@ -350,13 +436,14 @@ attn_rope_kernel(const RopeParams p) {
 // warp (with whole tokens as items the last round is mostly empty); 70 us for 4 x 2048 tokens x 48 heads of 128.  A warp
 // keeps the weight gradients of its rows in registers; each block leaves its sum in `partial`, and
 // attn_rope_weight_grad_kernel adds those in a fixed order.
-template <int D, int DTYPE>
+template <int D, int DTYPE, bool AXES>
 __global__ void __launch_bounds__(kWarps * 32, kBwdBlocks)
 attn_rope_bwd_kernel(const RopeParams p) {
     constexpr int LPR = D / 8, RPW = 32 / LPR;
     __shared__ float sums[kWarps * RPW][D];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane / LPR, l = lane % LPR;
     const Place at(p, l);
+    const PairAxes axes(p, l);      // (dead code without AXES)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const bool is_q = static_cast<int>(blockIdx.x) < p.q_blocks;
     const unsigned block = is_q ? blockIdx.x : blockIdx.x - p.q_blocks, blocks = is_q ? p.q_blocks : gridDim.x - p.q_blocks;
@@ -392,14 +479,7 @@ attn_rope_bwd_kernel(const RopeParams p) {
             }
             Turn turn;
             if (kind < 2) {
-                int pos = p.positions ? __ldg(p.positions + token) : s;
-                bool bad = false;
-                if (p.R > 0 && static_cast<unsigned>(pos) >= static_cast<unsigned>(p.table_len)) {
-                    report_bad_index(p.status);
-                    bad = true;
-                    pos = 0;
-                }
-                turn.load(p, pos, l, at, true);
+                const bool bad = !turn.load_token<AXES>(p, token, s, axes, l, at);
                 if (bad) {       // the token's gradients, and with them the weights', become NaN
 #pragma unroll
                     for (int e = 0; e < 4; ++e) turn.cs[e] = F2(__int_as_float(0x7fffffff), __int_as_float(0x7fffffff));

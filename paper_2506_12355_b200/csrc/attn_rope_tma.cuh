@@ -127,7 +127,7 @@ struct TileAt {
 };
 
 // PACKED: q or k has tiles of more than 8 tokens (a form of its own: what their rows need costs the others registers).
-template <int D, int DTYPE, bool PACKED>
+template <int D, int DTYPE, bool PACKED, bool AXES>
 __global__ void __launch_bounds__(TmaCfg<D>::THREADS, 1)
 attn_rope_bwd_tma_kernel(const __grid_constant__ TmaMaps maps, const __grid_constant__ TmaParams p) {
     using C = TmaCfg<D>;
@@ -206,18 +206,13 @@ attn_rope_bwd_tma_kernel(const __grid_constant__ TmaMaps maps, const __grid_cons
         // =========================== arithmetic ===========================
         const int sub = lane / LPR, l = lane % LPR;
         const Place at(p.r, l);
+        const PairAxes axes(p.r, l);                          // (dead code without AXES)
         Turn turn;                                            // of the token whose rows this lane works on
         F2 w[4];
         int my_kind = -1;                                     // tensor that w belongs to
         bool new_tokens = true;
         auto load_turn = [&](int b, int token) {
-            int pos = p.r.positions ? __ldg(p.r.positions + static_cast<int64_t>(b) * p.r.S + token) : token;
-            const bool bad = p.r.R > 0 && static_cast<unsigned>(pos) >= static_cast<unsigned>(p.r.table_len);
-            if (bad) {
-                report_bad_index(p.r.status);
-                pos = 0;
-            }
-            turn.load(p.r, pos, l, at, true);
+            const bool bad = !turn.load_token<AXES>(p.r, static_cast<int64_t>(b) * p.r.S + token, token, axes, l, at);
             if (bad) {                                        // the token's gradients, and with them the weights', become NaN
 #pragma unroll
                 for (int e = 0; e < 4; ++e) turn.cs[e] = F2(__int_as_float(0x7fffffff), __int_as_float(0x7fffffff));

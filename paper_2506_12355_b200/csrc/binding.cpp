@@ -27,6 +27,9 @@ struct Entries {
     decltype(&attn_fwd_window) fwd_window;
     decltype(&attn_bwd_window) bwd_window;
     decltype(&attn_bwd_window_workspace_bytes) bwd_window_bytes;
+    decltype(&attn_qk_norm_rope_axes) norm_rope_axes;
+    decltype(&attn_qk_norm_rope_axes_bwd) norm_rope_axes_bwd;
+    decltype(&attn_paged_append_axes) append_axes;
 } fn = {};
 
 using at::Tensor;
@@ -144,6 +147,22 @@ struct Rope {
     }
 };
 
+// Positions [axes, ..] and the axis of each pair (bytes, as rope_pair_axes makes them).
+struct Axes {
+    const int* positions;
+    const unsigned char* of;
+    int n;
+    Axes(const Call& c, const Rope& r, PyObject* pos, PyObject* pair_axes, at::IntArrayRef tokens) {
+        const Tensor& t = required(pos);
+        need(PyBytes_Check(pair_axes) && 2 * PyBytes_GET_SIZE(pair_axes) == r.R);
+        need(t.dim() == static_cast<int64_t>(tokens.size()) + 1 && t.sizes().slice(1) == tokens);
+        c.check(t, t.sizes(), at::kInt, true);
+        positions = static_cast<const int*>(t.data_ptr());
+        of = reinterpret_cast<const unsigned char*>(PyBytes_AS_STRING(pair_axes));
+        n = small(t.size(0));
+    }
+};
+
 void strides3(long long* to, const Tensor* t) {
     for (int i = 0; i < 3; ++i) to[i] = t ? t->stride(i) : 0;
 }
@@ -189,10 +208,20 @@ PyObject* tuple(std::initializer_list<const Tensor*> ts) {
     return r;
 }
 
-// attn_qk_norm_rope(q, k, v, q_weight, k_weight, cos_sin, positions, eps, interleaved, q_out, k_out, v_out)
+// Positions of one axis [..], or None.
+const int* positions(const Call& c, PyObject* pos, at::IntArrayRef tokens) {
+    const Tensor* t = tensor(pos);
+    if (t) c.check(*t, tokens, at::kInt, true);
+    return static_cast<const int*>(ptr(t));
+}
+
+// attn_qk_norm_rope(q, k, v, q_weight, k_weight, cos_sin, positions, eps, interleaved, q_out, k_out, v_out), and with several axes
+// attn_qk_norm_rope_axes(.., positions, pair_axes, eps, ..)
+template <bool AXES>
 PyObject* norm_rope(PyObject* const* a) {
     const Tensor &q = required(a[0]), &k = required(a[1]);
-    const Tensor *v = tensor(a[2]), *pos = tensor(a[6]);
+    const Tensor* v = tensor(a[2]);
+    constexpr int N = 7 + AXES;      // the first argument behind those that tell the positions
     need(q.dim() == 4 && k.dim() == 4);
     const int64_t B = q.size(0), S = q.size(1), H = q.size(2), D = q.size(3), Hkv = k.size(2);
     const Call c(q);
@@ -200,24 +229,35 @@ PyObject* norm_rope(PyObject* const* a) {
     c.check(k, {B, S, Hkv, D}, false);
     if (v) c.check(*v, {B, S, Hkv, D}, false);
     const Rope r(c, D, a[3], a[4], a[5]);
-    if (pos) c.check(*pos, {B, S}, at::kInt, true);
-    const Tensor qo = c.output(tensor(a[9]), {B, H, S, D}), ko = c.output(tensor(a[10]), {B, Hkv, S, D});
+    const Tensor qo = c.output(tensor(a[N + 2]), {B, H, S, D}), ko = c.output(tensor(a[N + 3]), {B, Hkv, S, D});
     Tensor vo;
-    if (v) vo = c.output(tensor(a[11]), {B, Hkv, S, D});
+    if (v) vo = c.output(tensor(a[N + 4]), {B, Hkv, S, D});
     long long st[9];
     strides3(st, &q);
     strides3(st + 3, &k);
     strides3(st + 6, v);
-    const int rc = fn.norm_rope(q.data_ptr(), k.data_ptr(), ptr(v), st, ptr(r.qw), ptr(r.kw), r.f32, static_cast<const float*>(ptr(r.table)), r.len,
-                                r.R, truth(a[8]), static_cast<const int*>(ptr(pos)), number(a[7]), qo.data_ptr(), ko.data_ptr(),
-                                v ? vo.data_ptr() : nullptr, small(B), small(S), small(H), small(Hkv), small(D), c.dtype, c.stream);
+    auto call = [&](auto entry, auto... where) {
+        return entry(q.data_ptr(), k.data_ptr(), ptr(v), st, ptr(r.qw), ptr(r.kw), r.f32, static_cast<const float*>(ptr(r.table)), r.len, r.R,
+                     truth(a[N + 1]), where..., number(a[N]), qo.data_ptr(), ko.data_ptr(), v ? vo.data_ptr() : nullptr, small(B), small(S),
+                     small(H), small(Hkv), small(D), c.dtype, c.stream);
+    };
+    int rc;
+    if constexpr (AXES) {
+        const Axes x(c, r, a[6], a[7], {B, S});
+        rc = call(fn.norm_rope_axes, x.positions, x.n, x.of);
+    } else {
+        rc = call(fn.norm_rope, positions(c, a[6], {B, S}));
+    }
     return rc ? status(rc) : tuple({&qo, &ko, v ? &vo : nullptr});
 }
 
-// attn_qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positions, eps, interleaved, dq_in, dk_in, dv_in, workspace)
+// attn_qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, cos_sin, positions, eps, interleaved, dq_in, dk_in, dv_in,
+// workspace), and with several axes attn_qk_norm_rope_axes_bwd(.., positions, pair_axes, eps, ..)
+template <bool AXES>
 PyObject* norm_rope_bwd(PyObject* const* a) {
     const Tensor &dq = required(a[0]), &dk = required(a[1]), &q = required(a[3]), &k = required(a[4]);
-    const Tensor *dv = tensor(a[2]), *pos = tensor(a[8]);
+    const Tensor* dv = tensor(a[2]);
+    constexpr int N = 9 + AXES;
     need(q.dim() == 4 && k.dim() == 4);
     const int64_t B = q.size(0), S = q.size(1), H = q.size(2), D = q.size(3), Hkv = k.size(2);
     const Call c(q);
@@ -227,48 +267,66 @@ PyObject* norm_rope_bwd(PyObject* const* a) {
     c.check(dk, {B, Hkv, S, D}, true);
     if (dv) c.check(*dv, {B, Hkv, S, D}, true);
     const Rope r(c, D, a[5], a[6], a[7]);
-    if (pos) c.check(*pos, {B, S}, at::kInt, true);
-    const Tensor qi = c.output(tensor(a[11]), {B, S, H, D}, false), ki = c.output(tensor(a[12]), {B, S, Hkv, D}, false);
+    const Tensor qi = c.output(tensor(a[N + 2]), {B, S, H, D}, false), ki = c.output(tensor(a[N + 3]), {B, S, Hkv, D}, false);
     Tensor vi, qw, kw;
-    if (dv) vi = c.output(tensor(a[13]), {B, S, Hkv, D}, false);
+    if (dv) vi = c.output(tensor(a[N + 4]), {B, S, Hkv, D}, false);
     if (r.qw) qw = c.make({D}, at::kFloat);
     if (r.kw) kw = c.make({D}, at::kFloat);
-    const Tensor ws = c.workspace(tensor(a[14]), fn.norm_rope_bwd_bytes(small(D)));
+    const Tensor ws = c.workspace(tensor(a[N + 5]), fn.norm_rope_bwd_bytes(small(D)));
     long long in[6], out[9];
     strides3(in, &q);
     strides3(in + 3, &k);
     strides3(out, &qi);
     strides3(out + 3, &ki);
     strides3(out + 6, dv ? &vi : nullptr);
-    const int rc = fn.norm_rope_bwd(dq.data_ptr(), dk.data_ptr(), ptr(dv), q.data_ptr(), k.data_ptr(), in, ptr(r.qw), ptr(r.kw), r.f32,
-                                    static_cast<const float*>(ptr(r.table)), r.len, r.R, truth(a[10]),
-                                    static_cast<const int*>(ptr(pos)), number(a[9]), qi.data_ptr(), ki.data_ptr(),
-                                    dv ? vi.data_ptr() : nullptr, out, r.qw ? qw.data_ptr<float>() : nullptr,
-                                    r.kw ? kw.data_ptr<float>() : nullptr, small(B), small(S), small(H), small(Hkv), small(D), c.dtype,
-                                    ws.data_ptr(), ws.nbytes(), c.stream);
+    auto call = [&](auto entry, auto... where) {
+        return entry(dq.data_ptr(), dk.data_ptr(), ptr(dv), q.data_ptr(), k.data_ptr(), in, ptr(r.qw), ptr(r.kw), r.f32,
+                     static_cast<const float*>(ptr(r.table)), r.len, r.R, truth(a[N + 1]), where..., number(a[N]), qi.data_ptr(), ki.data_ptr(),
+                     dv ? vi.data_ptr() : nullptr, out, r.qw ? qw.data_ptr<float>() : nullptr, r.kw ? kw.data_ptr<float>() : nullptr,
+                     small(B), small(S), small(H), small(Hkv), small(D), c.dtype, ws.data_ptr(), ws.nbytes(), c.stream);
+    };
+    int rc;
+    if constexpr (AXES) {
+        const Axes x(c, r, a[8], a[9], {B, S});
+        rc = call(fn.norm_rope_axes_bwd, x.positions, x.n, x.of);
+    } else {
+        rc = call(fn.norm_rope_bwd, positions(c, a[8], {B, S}));
+    }
     return rc ? status(rc) : tuple({&qi, &ki, dv ? &vi : nullptr, r.qw ? &qw : nullptr, r.kw ? &kw : nullptr});
 }
 
-// attn_paged_append(q, k, v, k_cache, v_cache, block_table, seq_lens, q_weight, k_weight, cos_sin, cu_seqlens, eps, interleaved, q_out)
+// attn_paged_append(q, k, v, k_cache, v_cache, block_table, seq_lens, q_weight, k_weight, cos_sin, cu_seqlens, eps, interleaved, q_out),
+// and with several axes attn_paged_append_axes(.., seq_lens, positions, pair_axes, q_weight, ..)
+template <bool AXES>
 PyObject* append(PyObject* const* a) {
     const Tensor &k = required(a[1]), &v = required(a[2]);
-    const Tensor *q = tensor(a[0]), *cu = tensor(a[10]);
+    constexpr int N = 7 + 2 * AXES;
+    const Tensor *q = tensor(a[0]), *cu = tensor(a[N + 3]);
     need(q && k.dim() == 3 && q->dim() == 3);
     const int64_t T = k.size(0), Hkv = k.size(1), D = k.size(2), H = q->size(1);
     const Call c(k);
     c.check(k, k.sizes(), false);
     c.check(v, k.sizes(), false);
     c.check(*q, {T, H, D}, false);
-    const Rope r(c, D, a[7], a[8], a[9]);
+    const Rope r(c, D, a[N], a[N + 1], a[N + 2]);
     const Cache m(c, D, a[3], a[4], a[5], a[6]);
     need(m.heads == Hkv && (cu || T == m.n));
     if (cu) c.check(*cu, {m.n + 1}, at::kInt, true);
-    const Tensor qo = c.output(tensor(a[13]), {T, H, D});
+    const Tensor qo = c.output(tensor(a[N + 6]), {T, H, D});
     const long long st[6] = {q->stride(0), q->stride(1), k.stride(0), k.stride(1), v.stride(0), v.stride(1)};
-    const int rc = fn.append(q->data_ptr(), k.data_ptr(), v.data_ptr(), st, ptr(r.qw), ptr(r.kw), r.f32, static_cast<const float*>(ptr(r.table)),
-                             r.len, r.R, truth(a[12]), number(a[11]), qo.data_ptr(), m.k.data_ptr(), m.v.data_ptr(), m.strides,
-                             m.pages, m.page_size, m.table.data_ptr<int>(), m.table.stride(0), m.width, m.lens.data_ptr<int>(),
-                             static_cast<const int*>(ptr(cu)), m.n, small(T), small(H), small(Hkv), small(D), c.dtype, c.stream);
+    auto call = [&](auto entry, auto... where) {
+        return entry(q->data_ptr(), k.data_ptr(), v.data_ptr(), st, ptr(r.qw), ptr(r.kw), r.f32, static_cast<const float*>(ptr(r.table)), r.len,
+                     r.R, truth(a[N + 5]), where..., number(a[N + 4]), qo.data_ptr(), m.k.data_ptr(), m.v.data_ptr(), m.strides, m.pages,
+                     m.page_size, m.table.template data_ptr<int>(), m.table.stride(0), m.width, m.lens.template data_ptr<int>(),
+                     static_cast<const int*>(ptr(cu)), m.n, small(T), small(H), small(Hkv), small(D), c.dtype, c.stream);
+    };
+    int rc;
+    if constexpr (AXES) {
+        const Axes x(c, r, a[7], a[8], {T});
+        rc = call(fn.append_axes, x.positions, x.n, x.of);
+    } else {
+        rc = call(fn.append);
+    }
     return rc ? status(rc) : wrap(qo);
 }
 
@@ -368,9 +426,12 @@ PyCFunction fast() {
 
 PyMethodDef methods[] = {
     {"bind", bind, METH_O, nullptr},
-    {"attn_qk_norm_rope", fast<norm_rope, 12>(), METH_FASTCALL, nullptr},
-    {"attn_qk_norm_rope_bwd", fast<norm_rope_bwd, 15>(), METH_FASTCALL, nullptr},
-    {"attn_paged_append", fast<append, 14>(), METH_FASTCALL, nullptr},
+    {"attn_qk_norm_rope", fast<norm_rope<false>, 12>(), METH_FASTCALL, nullptr},
+    {"attn_qk_norm_rope_bwd", fast<norm_rope_bwd<false>, 15>(), METH_FASTCALL, nullptr},
+    {"attn_paged_append", fast<append<false>, 14>(), METH_FASTCALL, nullptr},
+    {"attn_qk_norm_rope_axes", fast<norm_rope<true>, 13>(), METH_FASTCALL, nullptr},
+    {"attn_qk_norm_rope_axes_bwd", fast<norm_rope_bwd<true>, 16>(), METH_FASTCALL, nullptr},
+    {"attn_paged_append_axes", fast<append<true>, 16>(), METH_FASTCALL, nullptr},
     {"attn_paged_decode", fast<decode, 11>(), METH_FASTCALL, nullptr},
     {"attn_fwd_window", fast<fwd_window, 9>(), METH_FASTCALL, nullptr},
     {"attn_bwd_window", fast<bwd_window, 14>(), METH_FASTCALL, nullptr},

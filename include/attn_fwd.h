@@ -420,6 +420,52 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
 size_t attn_paged_decode_workspace_bytes(int H, int Hkv, int D);
 
 /*
+ * attn_paged_prefill -- attention of prompts over the paged cache, causal: token i of the n = cu_seqlens[b+1] - cu_seqlens[b] new
+ * ones of sequence b sees the keys j <= seq_lens[b] - n + i of its sequence.  The keys of the new tokens are in the cache already
+ * (attn_paged_append with the same lists); tokens of earlier calls, and pages that sequences share, are seen through the table.
+ * q, o [tokens, H, D], lse [tokens, H]: device, contiguous; H % Hkv == 0, H / Hkv <= 128; D in {64, 128}.
+ * seq_lens, cu_seqlens: device int32 [n_seqs], [n_seqs + 1], as in attn_paged_append.  Tokens before cu_seqlens[0], tokens from
+ *            cu_seqlens[n_seqs] on and tokens of sequences of length 0 are padding: their rows of o and lse stay as they were.
+ *            A length beyond max_pages * page_size is cut to that, a token in front of its sequence's first key gets O = 0,
+ *            LSE = -inf, a visible key whose page is not in [0, num_pages) counts as hidden, and each is reported as
+ *            ATTN_ERR_DEVICE_INDEX in the device status.  What lies in slots without a key does not matter (it may be NaN).
+ * num_pages and max_pages are at least 1 (unless there is nothing to do).
+ * workspace: device, 256-byte aligned, at least attn_paged_prefill_workspace_bytes(D) bytes (whatever the lengths are), or
+ *            ATTN_ERR_WORKSPACE.  Two calls that may run at the same time need one each.
+ * P is rounded to the 16-bit type before its product, as in attn_fwd.  Two kernels; lengths and tables are read on the device, so
+ * a captured call may be replayed with new ones.  The result does not depend on timing (no atomics); the key axis is cut over
+ * the GPU as in attn_paged_decode, so a sequence's result may differ in its last bits with the lengths of the others.
+ */
+int attn_paged_prefill(const void* q, const void* k_cache, const void* v_cache, const long long* cache_strides, int num_pages,
+                       int page_size, const int* block_table, long long table_stride, int max_pages, const int* seq_lens,
+                       const int* cu_seqlens, void* o, float* lse, int n_seqs, int tokens, int H, int Hkv, int D, float scale,
+                       int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace attn_paged_prefill needs (0 for an unsupported head dim). */
+size_t attn_paged_prefill_workspace_bytes(int D);
+
+/*
+ * attn_paged_prefix_decode -- attn_paged_decode (without a window) for sequences that have long first parts in common, whose keys and
+ * values are then read once for all of them.  Group g is the sequences group_starts[g] .. group_starts[g+1] - 1; their first
+ * prefix_lens[g] keys are the same, whether in the same pages or in copies (a page that a prefix fills in part can only be a copy):
+ * they are read through the block table's row of the group's first sequence.  The result is that of attn_paged_decode.
+ * group_starts, prefix_lens: device int32 [n_groups + 1], [n_groups].  The starts do not decrease; sequences in front of the first
+ *            and behind the last group have no common part.  A prefix may be any length: no more of it is taken as common than the
+ *            group's first sequence has keys, and a sequence that is shorter sees the keys that it has.  n_groups == 0: attn_paged_decode.
+ * H / Hkv <= 128; D in {64, 128}.  The other arguments as in attn_paged_decode.  P is rounded to the 16-bit type before its
+ * product for the common keys.
+ * workspace: device, 256-byte aligned, at least attn_paged_prefix_decode_workspace_bytes(B, H, Hkv, D) bytes, or ATTN_ERR_WORKSPACE.
+ *            Two calls that may run at the same time need one each.
+ */
+int attn_paged_prefix_decode(const void* q, const void* k_cache, const void* v_cache, const long long* cache_strides, int num_pages,
+                             int page_size, const int* block_table, long long table_stride, int max_pages, const int* seq_lens,
+                             const int* group_starts, const int* prefix_lens, int n_groups, void* o, float* lse, int B, int H,
+                             int Hkv, int D, float scale, int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace attn_paged_prefix_decode needs (0 for an invalid shape). */
+size_t attn_paged_prefix_decode_workspace_bytes(int B, int H, int Hkv, int D);
+
+/*
  * attn_fwd_simt -- same operator, same arguments, same conventions, computed by a plain
  * CUDA-core kernel (one warp per query row, fp32 arithmetic, online softmax).  It is one to
  * two orders of magnitude slower than attn_fwd and exists as an on-device cross-check that

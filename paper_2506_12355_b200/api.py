@@ -29,7 +29,8 @@ EXPORTS = ["attn_bwd", "attn_bwd_workspace_bytes", "attn_fwd", "attn_fwd_gqa", "
            "attn_fwd_host_static", "attn_fwd_host_static_capacity",
            "attn_fwd_window", "attn_bwd_window", "attn_bwd_window_workspace_bytes",
            "attn_qk_norm_rope", "attn_qk_norm_rope_bwd", "attn_qk_norm_rope_bwd_workspace_bytes", "attn_paged_append", "attn_paged_decode",
-           "attn_qk_norm_rope_axes", "attn_qk_norm_rope_axes_bwd", "attn_paged_append_axes",
+           "attn_qk_norm_rope_axes", "attn_qk_norm_rope_axes_bwd", "attn_paged_append_axes", "attn_paged_prefill",
+           "attn_paged_prefill_workspace_bytes", "attn_paged_prefix_decode", "attn_paged_prefix_decode_workspace_bytes",
            "attn_paged_decode_workspace_bytes",
            "attn_query_support", "attn_last_device_status", "attn_status_string"]
 
@@ -117,6 +118,14 @@ def load() -> ctypes.CDLL:
     lib.attn_paged_decode.argtypes = [vp] * 4 + [i, i, vp, ll, i] + [vp] * 3 + [i] * 4 + [f, i, i, i, vp, sz, vp]
     lib.attn_paged_decode_workspace_bytes.restype = sz
     lib.attn_paged_decode_workspace_bytes.argtypes = [i] * 3
+    lib.attn_paged_prefill.restype = i
+    lib.attn_paged_prefill.argtypes = [vp] * 4 + [i, i, vp, ll, i] + [vp] * 4 + [i] * 5 + [f, i, vp, sz, vp]
+    lib.attn_paged_prefill_workspace_bytes.restype = sz
+    lib.attn_paged_prefill_workspace_bytes.argtypes = [i]
+    lib.attn_paged_prefix_decode.restype = i
+    lib.attn_paged_prefix_decode.argtypes = [vp] * 4 + [i, i, vp, ll, i] + [vp] * 3 + [i] + [vp] * 2 + [i] * 4 + [f, i, vp, sz, vp]
+    lib.attn_paged_prefix_decode_workspace_bytes.restype = sz
+    lib.attn_paged_prefix_decode_workspace_bytes.argtypes = [i] * 4
     lib.attn_query_support.restype = i
     lib.attn_query_support.argtypes = [i, i, i]
     lib.attn_last_device_status.restype = i
@@ -130,7 +139,8 @@ def load() -> ctypes.CDLL:
 # Entry points that _binding marshals in C++, in the order in which its bind() takes their addresses.
 _BOUND = ["attn_qk_norm_rope", "attn_qk_norm_rope_bwd", "attn_qk_norm_rope_bwd_workspace_bytes", "attn_paged_append", "attn_paged_decode",
           "attn_paged_decode_workspace_bytes", "attn_fwd_window", "attn_bwd_window", "attn_bwd_window_workspace_bytes", "attn_qk_norm_rope_axes",
-          "attn_qk_norm_rope_axes_bwd", "attn_paged_append_axes"]
+          "attn_qk_norm_rope_axes_bwd", "attn_paged_append_axes", "attn_paged_prefill", "attn_paged_prefill_workspace_bytes",
+          "attn_paged_prefix_decode", "attn_paged_prefix_decode_workspace_bytes"]
 
 
 def _bind():
@@ -894,29 +904,95 @@ def attn_paged_decode(q, k_cache, v_cache, block_table, seq_lens, scale: float, 
     result = _fast("attn_paged_decode", q, k_cache, v_cache, block_table, seq_lens, scale, window, sinks, out, lse, workspace)
     if result is not NotImplemented:
         return result
+    B, H, D, dt, device, cache, out, lse = _check_paged_attention(q, k_cache, v_cache, block_table, seq_lens, out, lse)
+    pages, Hkv, page_size, cache_strides, n_seqs, width = cache
+    if n_seqs != B:
+        raise ValueError("q has %d rows, seq_lens %d" % (B, n_seqs))
+    workspace = _workspace(workspace, attn_paged_decode_workspace_bytes(H, Hkv, D), device)
+    _call("attn_paged_decode", device, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), cache_strides, pages, page_size,
+          block_table.data_ptr(), block_table.stride(0), width, seq_lens.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H,
+          Hkv, D, float(scale), int(window), int(sinks), dt, workspace.data_ptr(), _bytes(workspace))
+    return out, lse
+
+
+def _check_paged_attention(q, k_cache, v_cache, block_table, seq_lens, out, lse):
+    """q [rows,H,D] with its outputs, allocated when not given, and the cache: (rows, H, D, type, device, what _check_cache returns,
+    out, lse)."""
     if q.dim() != 3:
-        raise ValueError("q must be [B,H,D]")
-    B, H, D = q_shape = q.shape
+        raise ValueError("q must be [rows,H,D]")
+    rows, H, D = q_shape = q.shape
     dt, dtype, device = _dtype_code(q), q.dtype, q.device
     if not q.is_cuda:
         raise ValueError("q must be a CUDA tensor")
     if not q.is_contiguous():
         raise ValueError("q must be contiguous")
-    pages, Hkv, page_size, cache_strides, n_seqs, width = _check_cache(D, dtype, device, k_cache, v_cache, block_table, seq_lens)
-    if n_seqs != B:
-        raise ValueError("q has %d rows, seq_lens %d" % (B, n_seqs))
+    cache = _check_cache(D, dtype, device, k_cache, v_cache, block_table, seq_lens)
     if out is None:
         out = torch.empty(q_shape, dtype=dtype, device=device)
     else:
         _require(out, "out", q_shape, dtype, device)
     if lse is None:
-        lse = torch.empty((B, H), dtype=torch.float32, device=device)
+        lse = torch.empty((rows, H), dtype=torch.float32, device=device)
     else:
-        _require(lse, "lse", (B, H), torch.float32, device)
-    workspace = _workspace(workspace, attn_paged_decode_workspace_bytes(H, Hkv, D), device)
-    _call("attn_paged_decode", device, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), cache_strides, pages, page_size,
-          block_table.data_ptr(), block_table.stride(0), width, seq_lens.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H,
-          Hkv, D, float(scale), int(window), int(sinks), dt, workspace.data_ptr(), _bytes(workspace))
+        _require(lse, "lse", (rows, H), torch.float32, device)
+    return rows, H, D, dt, device, cache, out, lse
+
+
+def attn_paged_prefill_workspace_bytes(D) -> int:
+    return int((_lib or load()).attn_paged_prefill_workspace_bytes(D))
+
+
+def attn_paged_prefill(q, k_cache, v_cache, block_table, seq_lens, cu_seqlens, scale: float, out=None, lse=None, workspace=None, stream=None):
+    """Causal attention of new tokens, q [T,H,D], over a paged cache that holds their keys already (see attn_paged_append, with the
+    same seq_lens and cu_seqlens): token i of a sequence's n new ones sees the keys j <= seq_lens[b] - n + i.  Returns o [T,H,D] and
+    lse [T,H] (float32); rows of padding tokens (outside cu_seqlens, or of sequences of length 0) are not written.  D 64 or 128.
+    `workspace`: CUDA uint8 tensor of at least attn_paged_prefill_workspace_bytes(D) bytes (allocated here when None)."""
+    if stream is not None:
+        return _on_stream(stream, q, attn_paged_prefill, q, k_cache, v_cache, block_table, seq_lens, cu_seqlens, scale, out, lse, workspace)
+    result = _fast("attn_paged_prefill", q, k_cache, v_cache, block_table, seq_lens, cu_seqlens, scale, out, lse, workspace)
+    if result is not NotImplemented:
+        return result
+    T, H, D, dt, device, cache, out, lse = _check_paged_attention(q, k_cache, v_cache, block_table, seq_lens, out, lse)
+    pages, Hkv, page_size, cache_strides, n_seqs, width = cache
+    if cu_seqlens is None:
+        raise ValueError("cu_seqlens must say where each sequence's new tokens begin")
+    _require(cu_seqlens, "cu_seqlens", (n_seqs + 1,), torch.int32, device)
+    workspace = _workspace(workspace, attn_paged_prefill_workspace_bytes(D), device)
+    _call("attn_paged_prefill", device, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), cache_strides, pages, page_size,
+          block_table.data_ptr(), block_table.stride(0), width, seq_lens.data_ptr(), cu_seqlens.data_ptr(), out.data_ptr(), lse.data_ptr(),
+          n_seqs, T, H, Hkv, D, float(scale), dt, workspace.data_ptr(), _bytes(workspace))
+    return out, lse
+
+
+def attn_paged_prefix_decode_workspace_bytes(B, H, Hkv, D) -> int:
+    return int((_lib or load()).attn_paged_prefix_decode_workspace_bytes(B, H, Hkv, D))
+
+
+def attn_paged_prefix_decode(q, k_cache, v_cache, block_table, seq_lens, group_starts, prefix_lens, scale: float, out=None, lse=None,
+                             workspace=None, stream=None):
+    """attn_paged_decode for sequences with common first parts, which are read once for all: group g is the sequences
+    group_starts[g] .. group_starts[g+1] - 1 (int32 [groups+1]), whose first prefix_lens[g] (int32 [groups]) keys are the same, in shared
+    pages or in copies.  Same result as attn_paged_decode without a window; D 64 or 128.
+    `workspace`: CUDA uint8 tensor of at least attn_paged_prefix_decode_workspace_bytes(B, H, Hkv, D) bytes (allocated here when None)."""
+    if stream is not None:
+        return _on_stream(stream, q, attn_paged_prefix_decode, q, k_cache, v_cache, block_table, seq_lens, group_starts, prefix_lens, scale, out, lse,
+                          workspace)
+    result = _fast("attn_paged_prefix_decode", q, k_cache, v_cache, block_table, seq_lens, group_starts, prefix_lens, scale, out, lse, workspace)
+    if result is not NotImplemented:
+        return result
+    B, H, D, dt, device, cache, out, lse = _check_paged_attention(q, k_cache, v_cache, block_table, seq_lens, out, lse)
+    pages, Hkv, page_size, cache_strides, n_seqs, width = cache
+    if n_seqs != B:
+        raise ValueError("q has %d rows, seq_lens %d" % (B, n_seqs))
+    if prefix_lens.dim() != 1:
+        raise ValueError("prefix_lens must be [groups] and group_starts [groups + 1]")
+    groups = prefix_lens.shape[0]
+    _require(prefix_lens, "prefix_lens", (groups,), torch.int32, device)
+    _require(group_starts, "group_starts", (groups + 1,), torch.int32, device)
+    workspace = _workspace(workspace, attn_paged_prefix_decode_workspace_bytes(B, H, Hkv, D), device)
+    _call("attn_paged_prefix_decode", device, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), cache_strides, pages, page_size,
+          block_table.data_ptr(), block_table.stride(0), width, seq_lens.data_ptr(), group_starts.data_ptr(), prefix_lens.data_ptr(), groups,
+          out.data_ptr(), lse.data_ptr(), B, H, Hkv, D, float(scale), dt, workspace.data_ptr(), _bytes(workspace))
     return out, lse
 
 

@@ -18,6 +18,7 @@
 #include "attn_bwd.cuh"
 #include "attn_combine.cuh"
 #include "attn_paged.cuh"
+#include "attn_paged_tc.cuh"
 #include "attn_rope.cuh"
 #include "attn_rope_tma.cuh"
 #include "attn_simt.cuh"

@@ -488,6 +488,122 @@ int paged_append(const void* q, const void* k, const void* v, const long long* i
     return launch_rope<true>(p, D, dtype, static_cast<cudaStream_t>(stream));
 }
 
+// Blocks per sequence of the joining kernels.
+int64_t join_blocks(int H) { return (H + attn_paged::kJoinWarps - 1) / attn_paged::kJoinWarps; }
+
+// Bytes of the partial results of attn_paged_decode.
+size_t decode_bytes(int H, int Hkv, int D) {
+    if (H < 0 || Hkv < 1 || H % Hkv != 0 || !head_dim_ok(D)) return 0;
+    const int group = H / Hkv, rows = group <= 8 ? 8 : 16;
+    const size_t parts = static_cast<size_t>(2) * attn_paged::kMaxCtas << tile_heads_shift(Hkv * ((group + 15) / 16), D);
+    return align256(parts * rows * (D + 2) * sizeof(float));
+}
+
+// What the calls that attend over the paged cache refuse alike.
+int validate_paged_attention(const void* q, const void* k_cache, const void* v_cache, const long long* cache_strides, int num_pages,
+                             int page_size, const int* block_table, int max_pages, const int* seq_lens, const void* o, const float* lse, int Hkv) {
+    if (!q || !o || !lse) return ATTN_ERR_NULL_POINTER;
+    const int rc = validate_cache(k_cache, v_cache, cache_strides, num_pages, page_size, block_table, max_pages, seq_lens);
+    if (rc != ATTN_OK) return rc;
+    if (misaligned(q, 16) || misaligned(o, 16) || misaligned(lse, 4)) return ATTN_ERR_MISALIGNED;
+    for (int i = 0; i < 2; ++i) {
+        const int64_t stride[3] = {cache_strides[3 * i], cache_strides[3 * i + 1], cache_strides[3 * i + 2]};
+        const int n[3] = {num_pages, Hkv, page_size};
+        if (!mappable(stride, n)) return ATTN_ERR_BAD_SHAPE;
+    }
+    return ATTN_OK;
+}
+
+// The decode kernel's parameters that follow from the call's arguments (valid ones).  False: too many rows.
+bool decode_params(attn_paged::DecodeParams& p, const void* q, int num_pages, int page_size, const int* block_table, long long table_stride,
+                   int max_pages, const int* seq_lens, void* o, float* lse, int B, int H, int Hkv, int D, float scale, void* workspace, int sm_count) {
+    p.q = q;
+    p.o = o;
+    p.lse = lse;
+    p.block_table = block_table;
+    p.seq_lens = seq_lens;
+    p.parts = static_cast<float*>(workspace);
+    p.table_stride = table_stride;
+    p.B = B;
+    p.H = H;
+    p.Hkv = Hkv;
+    p.group = H / Hkv;
+    p.sub = (p.group + 15) / 16;
+    p.heads = Hkv * p.sub;
+    p.hpt_shift = tile_heads_shift(p.heads, D);
+    p.max_len = max_pages * page_size;
+    p.num_pages = num_pages;
+    p.page_shift = log2_of(page_size);
+    p.scale_log2 = scale * 1.4426950408889634f;
+    p.status = cached_status_ptr();
+    const int64_t pairs = static_cast<int64_t>(B) * p.heads;
+    if (pairs > 2147483647LL || B * join_blocks(H) > 2147483647LL) return false;
+    // one CTA per SM, and no more than there can be tiles (16 keys are the smallest tile)
+    const int64_t most = pairs * ((static_cast<int64_t>(p.max_len) + 15) / 16 + 2);
+    const int grid = sm_count < attn_paged::kMaxCtas ? sm_count : attn_paged::kMaxCtas;
+    p.grid = most < grid ? static_cast<int>(most) : grid;
+    return true;
+}
+
+// The two cache maps of the decode kernel, with boxes of up to CK rows.
+template <int CK>
+bool decode_maps(CUtensorMap* mk, CUtensorMap* mv, attn_paged::DecodeParams& p, const void* k_cache, const void* v_cache,
+                 const long long* cache_strides, int dtype, int D, int page_size) {
+    const int rows = page_size < CK ? page_size : CK;
+    p.box_shift = log2_of(rows);
+    return make_cache_map(mk, &p.k_axes, k_cache, cache_strides, dtype, D, p.num_pages, p.Hkv, page_size, rows) &&
+           make_cache_map(mv, &p.v_axes, v_cache, cache_strides + 3, dtype, D, p.num_pages, p.Hkv, page_size, rows);
+}
+
+// Partial results of attn_paged_tc.cuh: two per CTA.
+size_t tc_part_bytes(int D) { return static_cast<size_t>(2) * attn_paged::kMaxCtas * attn_paged_tc::part_floats(D) * sizeof(float); }
+
+#ifdef ATTN_TEST_HOOKS
+int g_test_skip_group = -1;
+#endif
+
+// attn_paged_tc_kernel over `units` sequences (PREFIX: groups) and `tokens` rows of queries.  p: o, lse, parts and rows are set.
+template <int D, int DTYPE, bool PREFIX>
+bool launch_paged_tc(attn_paged_tc::Params& p, const void* q, const void* k_cache, const void* v_cache, const long long* cache_strides, int num_pages,
+                     int page_size, const int* block_table, long long table_stride, int max_pages, const int* seq_lens, const int* starts, int units,
+                     int tokens, int H, int Hkv, float scale, int sm_count, cudaStream_t st) {
+    using C = attn_paged_tc::Cfg<D>;
+    auto kern = attn_paged_tc::attn_paged_tc_kernel<D, DTYPE, PREFIX>;
+    if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), C::SMEM_BYTES)) return false;
+    p.block_table = block_table;
+    p.seq_lens = seq_lens;
+    p.starts = starts;
+    p.table_stride = table_stride;
+    p.units = units;
+    p.tokens = tokens;
+    p.H = H;
+    p.Hkv = Hkv;
+    p.group = H / Hkv;
+    p.tile_tokens = 128 / p.group;
+    p.max_len = max_pages * page_size;
+    p.num_pages = num_pages;
+    p.page_shift = log2_of(page_size);
+    p.scale = scale;
+    // (with a scale of 0 hidden scores, -inf, must still stay -inf)
+    p.scale_log2 = scale > 0.f ? scale * 1.4426950408889634f : 1.17549435e-38f;
+    p.grid = sm_count < attn_paged::kMaxCtas ? sm_count : attn_paged::kMaxCtas;
+    p.status = cached_status_ptr();
+    if (!p.status) return false;
+#ifdef ATTN_TEST_HOOKS
+    p.test_skip_group = g_test_skip_group;
+    g_test_skip_group = -1;
+#endif
+    const int rows = page_size < 128 ? page_size : 128;
+    p.box_shift = log2_of(rows);
+    CUtensorMap mq, mk, mv;
+    const Map4Key qk{q, {D, static_cast<int64_t>(H) * D, 0}, DTYPE, D, {H, tokens, 1}, {64, p.group, p.tile_tokens, 1}, 1};
+    if (!make_map4(&mq, qk) || !make_cache_map(&mk, &p.k_axes, k_cache, cache_strides, DTYPE, D, num_pages, Hkv, page_size, rows) ||
+        !make_cache_map(&mv, &p.v_axes, v_cache, cache_strides + 3, DTYPE, D, num_pages, Hkv, page_size, rows))
+        return false;
+    kern<<<p.grid, C::THREADS, C::SMEM_BYTES, st>>>(mq, mk, mv, p);
+    return cudaGetLastError() == cudaSuccess;
+}
+
 }  // namespace
 
 extern "C" {
@@ -496,6 +612,8 @@ extern "C" {
 // Test build only (never part of libattn_fwd.so): the next launch of the decode kernel (of the rotation's gradient) leaves out the
 // copies of this step of every warp (tile of every CTA), so that the wait for them runs out.
 void attn_test_skip_step(int step) { g_test_skip_step = step; }
+// The next launch of attn_paged_tc_kernel leaves out the copies of this ring group of every CTA.
+void attn_test_skip_group(int group) { g_test_skip_group = group; }
 #endif
 
 int attn_fwd_window(const void* q, const void* k, const void* v, void* o, float* lse, int B, int H, int Hkv, int Sq, int Sk,
@@ -599,12 +717,7 @@ int attn_paged_append_axes(const void* q, const void* k, const void* v, const lo
                         Hkv, D, dtype, stream, true, positions, n_axes, pair_axes);
 }
 
-size_t attn_paged_decode_workspace_bytes(int H, int Hkv, int D) {
-    if (H < 0 || Hkv < 1 || H % Hkv != 0 || !head_dim_ok(D)) return 0;
-    const int group = H / Hkv, rows = group <= 8 ? 8 : 16;
-    const size_t parts = static_cast<size_t>(2) * attn_paged::kMaxCtas << tile_heads_shift(Hkv * ((group + 15) / 16), D);
-    return align256(parts * rows * (D + 2) * sizeof(float));
-}
+size_t attn_paged_decode_workspace_bytes(int H, int Hkv, int D) { return decode_bytes(H, Hkv, D); }
 
 int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, const long long* cache_strides, int num_pages,
                       int page_size, const int* block_table, long long table_stride, int max_pages, const int* seq_lens,
@@ -617,16 +730,9 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
     if (static_cast<int64_t>(B) * H > 2147483647LL) return ATTN_ERR_BAD_SHAPE;
     if (!isfinite(scale) || scale < 0.f) return ATTN_ERR_BAD_SCALE;
     if (B == 0 || H == 0) return ATTN_OK;
-    if (!q || !o || !lse) return ATTN_ERR_NULL_POINTER;
-    int rc = validate_cache(k_cache, v_cache, cache_strides, num_pages, page_size, block_table, max_pages, seq_lens);
+    int rc = validate_paged_attention(q, k_cache, v_cache, cache_strides, num_pages, page_size, block_table, max_pages, seq_lens, o, lse, Hkv);
     if (rc != ATTN_OK) return rc;
-    if (misaligned(q, 16) || misaligned(o, 16) || misaligned(lse, 4)) return ATTN_ERR_MISALIGNED;
-    for (int i = 0; i < 2; ++i) {
-        const int64_t stride[3] = {cache_strides[3 * i], cache_strides[3 * i + 1], cache_strides[3 * i + 2]};
-        const int n[3] = {num_pages, Hkv, page_size};
-        if (!mappable(stride, n)) return ATTN_ERR_BAD_SHAPE;
-    }
-    if (!workspace || misaligned(workspace, 256) || workspace_bytes < attn_paged_decode_workspace_bytes(H, Hkv, D)) return ATTN_ERR_WORKSPACE;
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < decode_bytes(H, Hkv, D)) return ATTN_ERR_WORKSPACE;
     rc = check_arch();
     if (rc != ATTN_OK) return rc;
     DeviceInfo di;
@@ -634,36 +740,13 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (num_pages == 0) return fill_empty(o, lse, static_cast<int64_t>(B) * H * D, static_cast<int64_t>(B) * H, st);
     attn_paged::DecodeParams p = {};
-    p.q = q;
-    p.o = o;
-    p.lse = lse;
-    p.block_table = block_table;
-    p.seq_lens = seq_lens;
-    p.parts = static_cast<float*>(workspace);
-    p.table_stride = table_stride;
-    p.B = B;
-    p.H = H;
-    p.Hkv = Hkv;
-    p.group = H / Hkv;
-    p.sub = (p.group + 15) / 16;
-    p.heads = Hkv * p.sub;
-    p.hpt_shift = tile_heads_shift(p.heads, D);
-    p.max_len = max_pages * page_size;
-    p.num_pages = num_pages;
-    p.page_shift = log2_of(page_size);
+    if (!decode_params(p, q, num_pages, page_size, block_table, table_stride, max_pages, seq_lens, o, lse, B, H, Hkv, D, scale, workspace,
+                       di.sm_count))
+        return ATTN_ERR_BAD_SHAPE;
+    if (!p.status) return ATTN_ERR_CUDA;
     p.window = window;
     p.sinks = sinks;
-    p.scale_log2 = scale * 1.4426950408889634f;
-    p.status = cached_status_ptr();
-    if (!p.status) return ATTN_ERR_CUDA;
     const int64_t pairs = static_cast<int64_t>(B) * p.heads;
-    const int64_t join_blocks = (H + attn_paged::kJoinWarps - 1) / attn_paged::kJoinWarps;
-    if (pairs > 2147483647LL || B * join_blocks > 2147483647LL) return ATTN_ERR_BAD_SHAPE;
-    // one CTA per SM, and no more than there can be tiles (16 keys are the smallest tile)
-    const int64_t most = pairs * ((static_cast<int64_t>(p.max_len) + 15) / 16 + 2);
-    int grid = di.sm_count < attn_paged::kMaxCtas ? di.sm_count : attn_paged::kMaxCtas;
-    if (most < grid) grid = static_cast<int>(most);
-    p.grid = grid;
     // Few pairs whose sequences cannot be long: clusters (see attn_paged.cuh), of as many CTAs as let all of them be resident at
     // once (16 clusters of 8); and a CTA should not have more than 8 tiles while other SMs have none.  8 heads of 128, against
     // the list and its second kernel: 4 sequences of 1000 keys (clusters of 4) 9 us instead of 14, 8 of 1000 (2) 12 instead of
@@ -679,23 +762,19 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
 #define ATTN_DECODE_CASE(DD, TT, GG)                                                                                     \
     if (D == DD && dtype == TT && (p.group <= 8) == (GG == 8)) {                                                         \
         using C = attn_paged::DecodeCfg<DD, GG>;                                                                         \
-        auto kern = attn_paged::attn_paged_decode_kernel<DD, TT, GG>;                                                    \
+        auto kern = attn_paged::attn_paged_decode_kernel<DD, TT, GG, false>;                                             \
         if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), C::SMEM_BYTES)) return ATTN_ERR_CUDA;               \
-        const int rows = page_size < C::CK ? page_size : C::CK;                                                          \
-        p.box_shift = log2_of(rows);                                                                                     \
         CUtensorMap mk, mv;                                                                                              \
-        if (!make_cache_map(&mk, &p.k_axes, k_cache, cache_strides, TT, DD, num_pages, Hkv, page_size, rows) ||          \
-            !make_cache_map(&mv, &p.v_axes, v_cache, cache_strides + 3, TT, DD, num_pages, Hkv, page_size, rows))        \
-            return ATTN_ERR_CUDA;                                                                                        \
+        if (!decode_maps<C::CK>(&mk, &mv, p, k_cache, v_cache, cache_strides, TT, DD, page_size)) return ATTN_ERR_CUDA;  \
         if (p.cluster)                                                                                                   \
-            return launch_cluster(kern, dim3(static_cast<unsigned>(pairs * cluster)), dim3(C::THREADS), C::SMEM_BYTES, \
-                                  static_cast<unsigned>(cluster), st, mk, mv, p)                                                   \
+            return launch_cluster(kern, dim3(static_cast<unsigned>(pairs * cluster)), dim3(C::THREADS), C::SMEM_BYTES,   \
+                                  static_cast<unsigned>(cluster), st, mk, mv, p)                                         \
                        ? ATTN_OK                                                                                         \
                        : ATTN_ERR_CUDA;                                                                                  \
-        kern<<<grid, C::THREADS, C::SMEM_BYTES, st>>>(mk, mv, p);                                                        \
+        kern<<<p.grid, C::THREADS, C::SMEM_BYTES, st>>>(mk, mv, p);                                                      \
         if (cudaGetLastError() != cudaSuccess) return ATTN_ERR_CUDA;                                                     \
-        return launch_dependent(attn_paged::attn_paged_join_kernel<DD, TT, GG>, dim3(static_cast<unsigned>(B * join_blocks)), \
-                                dim3(attn_paged::kJoinWarps * 32), 0, st, p, static_cast<int>(join_blocks)) \
+        return launch_dependent(attn_paged::attn_paged_join_kernel<DD, TT, GG>, dim3(static_cast<unsigned>(B * join_blocks(H))), \
+                                dim3(attn_paged::kJoinWarps * 32), 0, st, p, static_cast<int>(join_blocks(H)))           \
                    ? ATTN_OK                                                                                             \
                    : ATTN_ERR_CUDA;                                                                                      \
     }
@@ -712,6 +791,129 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
     ATTN_DECODE_CASE(256, 0, 16)
     ATTN_DECODE_CASE(256, 1, 16)
 #undef ATTN_DECODE_CASE
+    return ATTN_ERR_UNSUPPORTED_DTYPE;
+}
+
+size_t attn_paged_prefill_workspace_bytes(int D) { return D == 64 || D == 128 ? align256(tc_part_bytes(D)) : 0; }
+
+int attn_paged_prefill(const void* q, const void* k_cache, const void* v_cache, const long long* cache_strides, int num_pages,
+                       int page_size, const int* block_table, long long table_stride, int max_pages, const int* seq_lens,
+                       const int* cu_seqlens, void* o, float* lse, int n_seqs, int tokens, int H, int Hkv, int D, float scale,
+                       int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    if (n_seqs < 0 || tokens < 0 || H < 0 || Hkv < 0) return ATTN_ERR_BAD_SHAPE;
+    if (H > 0 && (Hkv == 0 || H % Hkv != 0 || H / Hkv > 128)) return ATTN_ERR_BAD_SHAPE;
+    if (D != 64 && D != 128) return ATTN_ERR_UNSUPPORTED_HEAD_DIM;
+    if (!dtype_ok(dtype)) return ATTN_ERR_UNSUPPORTED_DTYPE;
+    if (static_cast<int64_t>(tokens) * H > 2147483647LL) return ATTN_ERR_BAD_SHAPE;
+    if (!isfinite(scale) || scale < 0.f) return ATTN_ERR_BAD_SCALE;
+    if (tokens == 0 || n_seqs == 0 || H == 0) return ATTN_OK;
+    if (!cu_seqlens) return ATTN_ERR_NULL_POINTER;
+    int rc = validate_paged_attention(q, k_cache, v_cache, cache_strides, num_pages, page_size, block_table, max_pages, seq_lens, o, lse, Hkv);
+    if (rc != ATTN_OK) return rc;
+    if (num_pages == 0 || max_pages == 0) return ATTN_ERR_BAD_SHAPE;
+    if (misaligned(cu_seqlens, 4)) return ATTN_ERR_MISALIGNED;
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < attn_paged_prefill_workspace_bytes(D)) return ATTN_ERR_WORKSPACE;
+    rc = check_arch();
+    if (rc != ATTN_OK) return rc;
+    DeviceInfo di;
+    if (device_info(&di) != ATTN_OK) return ATTN_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    attn_paged_tc::Params p = {};
+    p.o = o;
+    p.lse = lse;
+    p.parts = static_cast<float*>(workspace);
+#define ATTN_PREFILL_CASE(DD, TT)                                                                                              \
+    if (D == DD && dtype == TT) {                                                                                              \
+        if (!launch_paged_tc<DD, TT, false>(p, q, k_cache, v_cache, cache_strides, num_pages, page_size, block_table, table_stride, max_pages, \
+                                            seq_lens, cu_seqlens, n_seqs, tokens, H, Hkv, scale, di.sm_count, st))              \
+            return ATTN_ERR_CUDA;                                                                                              \
+        return launch_dependent(attn_paged_tc::attn_paged_prefill_join_kernel<DD, TT>, dim3(static_cast<unsigned>(p.grid - 1), 8), \
+                                dim3(attn_paged::kJoinWarps * 32), 0, st, p)                                                   \
+                   ? ATTN_OK                                                                                                   \
+                   : ATTN_ERR_CUDA;                                                                                            \
+    }
+    ATTN_PREFILL_CASE(64, 0)
+    ATTN_PREFILL_CASE(64, 1)
+    ATTN_PREFILL_CASE(128, 0)
+    ATTN_PREFILL_CASE(128, 1)
+#undef ATTN_PREFILL_CASE
+    return ATTN_ERR_UNSUPPORTED_DTYPE;
+}
+
+size_t attn_paged_prefix_decode_workspace_bytes(int B, int H, int Hkv, int D) {
+    if (B < 0 || (D != 64 && D != 128) || decode_bytes(H, Hkv, D) == 0) return 0;
+    // the decode kernel's partial results, both kernels' rows, and the other kernel's partial results
+    return decode_bytes(H, Hkv, D) + 2 * align256(static_cast<size_t>(B) * H * (D + 2) * sizeof(float)) + align256(tc_part_bytes(D));
+}
+
+int attn_paged_prefix_decode(const void* q, const void* k_cache, const void* v_cache, const long long* cache_strides, int num_pages,
+                             int page_size, const int* block_table, long long table_stride, int max_pages, const int* seq_lens,
+                             const int* group_starts, const int* prefix_lens, int n_groups, void* o, float* lse, int B, int H,
+                             int Hkv, int D, float scale, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    if (B < 0 || H < 0 || Hkv < 0 || n_groups < 0) return ATTN_ERR_BAD_SHAPE;
+    if (H > 0 && (Hkv == 0 || H % Hkv != 0 || H / Hkv > 128)) return ATTN_ERR_BAD_SHAPE;
+    if (D != 64 && D != 128) return ATTN_ERR_UNSUPPORTED_HEAD_DIM;
+    if (!dtype_ok(dtype)) return ATTN_ERR_UNSUPPORTED_DTYPE;
+    if (static_cast<int64_t>(B) * H > 2147483647LL) return ATTN_ERR_BAD_SHAPE;
+    if (!isfinite(scale) || scale < 0.f) return ATTN_ERR_BAD_SCALE;
+    if (B == 0 || H == 0) return ATTN_OK;
+    if (n_groups > 0 && (!group_starts || !prefix_lens)) return ATTN_ERR_NULL_POINTER;
+    int rc = validate_paged_attention(q, k_cache, v_cache, cache_strides, num_pages, page_size, block_table, max_pages, seq_lens, o, lse, Hkv);
+    if (rc != ATTN_OK) return rc;
+    if (misaligned(group_starts, 4) || misaligned(prefix_lens, 4)) return ATTN_ERR_MISALIGNED;
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < attn_paged_prefix_decode_workspace_bytes(B, H, Hkv, D)) return ATTN_ERR_WORKSPACE;
+    if (n_groups == 0 || num_pages == 0 || max_pages == 0)
+        return attn_paged_decode(q, k_cache, v_cache, cache_strides, num_pages, page_size, block_table, table_stride, max_pages, seq_lens, o, lse, B,
+                                 H, Hkv, D, scale, 0, 0, dtype, workspace, workspace_bytes, stream);
+    rc = check_arch();
+    if (rc != ATTN_OK) return rc;
+    DeviceInfo di;
+    if (device_info(&di) != ATTN_OK) return ATTN_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    const size_t row_bytes = align256(static_cast<size_t>(B) * H * (D + 2) * sizeof(float));
+    attn_paged::DecodeParams p = {};
+    if (!decode_params(p, q, num_pages, page_size, block_table, table_stride, max_pages, seq_lens, o, lse, B, H, Hkv, D, scale, ws, di.sm_count))
+        return ATTN_ERR_BAD_SHAPE;
+    if (!p.status) return ATTN_ERR_CUDA;
+    ws += decode_bytes(H, Hkv, D);
+    p.rows = reinterpret_cast<float*>(ws);
+    p.group_starts = group_starts;
+    p.prefix_lens = prefix_lens;
+    p.n_groups = n_groups;
+#ifdef ATTN_TEST_HOOKS
+    p.test_skip_step = g_test_skip_step;
+    g_test_skip_step = -1;
+#endif
+    attn_paged_tc::Params pre = {};
+    pre.rows = reinterpret_cast<float*>(ws + row_bytes);
+    pre.parts = reinterpret_cast<float*>(ws + 2 * row_bytes);
+    pre.prefix_lens = prefix_lens;
+#define ATTN_PREFIX_CASE(DD, TT, GG)                                                                                           \
+    if (D == DD && dtype == TT && (p.group <= 8) == (GG == 8)) {                                                               \
+        using C = attn_paged::DecodeCfg<DD, GG>;                                                                               \
+        auto kern = attn_paged::attn_paged_decode_kernel<DD, TT, GG, true>;                                                    \
+        if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), C::SMEM_BYTES)) return ATTN_ERR_CUDA;                     \
+        CUtensorMap mk, mv;                                                                                                    \
+        if (!decode_maps<C::CK>(&mk, &mv, p, k_cache, v_cache, cache_strides, TT, DD, page_size)) return ATTN_ERR_CUDA;        \
+        if (!launch_paged_tc<DD, TT, true>(pre, q, k_cache, v_cache, cache_strides, num_pages, page_size, block_table, table_stride, max_pages, \
+                                           seq_lens, group_starts, n_groups, B, H, Hkv, scale, di.sm_count, st))               \
+            return ATTN_ERR_CUDA;                                                                                              \
+        if (!launch_dependent(kern, dim3(static_cast<unsigned>(p.grid)), dim3(C::THREADS), C::SMEM_BYTES, st, mk, mv, p)) return ATTN_ERR_CUDA; \
+        return launch_dependent(attn_paged_tc::attn_paged_prefix_join_kernel<DD, TT, GG>, dim3(static_cast<unsigned>(B * join_blocks(H))), \
+                                dim3(attn_paged::kJoinWarps * 32), 0, st, p, pre, static_cast<int>(join_blocks(H)))            \
+                   ? ATTN_OK                                                                                                   \
+                   : ATTN_ERR_CUDA;                                                                                            \
+    }
+    ATTN_PREFIX_CASE(64, 0, 8)
+    ATTN_PREFIX_CASE(64, 1, 8)
+    ATTN_PREFIX_CASE(128, 0, 8)
+    ATTN_PREFIX_CASE(128, 1, 8)
+    ATTN_PREFIX_CASE(64, 0, 16)
+    ATTN_PREFIX_CASE(64, 1, 16)
+    ATTN_PREFIX_CASE(128, 0, 16)
+    ATTN_PREFIX_CASE(128, 1, 16)
+#undef ATTN_PREFIX_CASE
     return ATTN_ERR_UNSUPPORTED_DTYPE;
 }
 

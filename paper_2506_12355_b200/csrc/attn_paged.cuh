@@ -83,6 +83,12 @@ struct DecodeParams {
 #ifdef ATTN_TEST_HOOKS
     int test_skip_step;         // test build only: the step of every warp whose copies are left out (-1: none)
 #endif
+    // PREFIX: the first keys of each group of neighbouring sequences are not worked on (attn_paged_tc.cuh), and every row leaves a
+    // partial result
+    const int* group_starts;    // [n_groups + 1]
+    const int* prefix_lens;     // [n_groups]
+    int n_groups;
+    float* rows;                // O [B * H][D], then reference exponent and sum [B * H][2], of pairs that one CTA has to itself
     int cluster;                // > 0: a cluster of so many CTAs (a power of two up to kCluster) per (sequence, head), no second kernel
 };
 constexpr int kCluster = 8;
@@ -113,12 +119,46 @@ struct SeqRange {
     int n_sink, lo, n_chunks;
 };
 
-template <int CK>
+// The common keys of a group: no more than its first sequence has, whose pages are read.
+__device__ __forceinline__ int group_prefix(const int* seq_lens, int first, int prefix, int max_len) {
+    const int len = __ldg(seq_lens + first);
+    const int n = prefix < len ? prefix : len;
+    return n < 0 ? 0 : (n > max_len ? max_len : n);
+}
+
+// PREFIX: the group that sequence b belongs to (-1: none): the last one that begins at or before it.
+__device__ __forceinline__ int group_of(const int* starts, int n_groups, int b) {
+    if (b < __ldg(starts) || b >= __ldg(starts + n_groups)) return -1;
+    int lo = 0, hi = n_groups;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (__ldg(starts + mid) <= b) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// PREFIX: how many first keys of sequence b the other kernel takes.
+__device__ __forceinline__ int prefix_of(const DecodeParams& p, int b) {
+    const int g = group_of(p.group_starts, p.n_groups, b);
+    if (g < 0) return 0;
+    const int first = __ldg(p.group_starts + g);
+    return group_prefix(p.seq_lens, first < 0 ? 0 : first, __ldg(p.prefix_lens + g), p.max_len);
+}
+
+template <int CK, bool PREFIX>
 __device__ __forceinline__ SeqRange seq_range(const DecodeParams& p, int b) {
     SeqRange r;
     int len = p.seq_lens[b];
     len = len < 0 ? 0 : (len > p.max_len ? p.max_len : len);
     r.len = len;
+    if constexpr (PREFIX) {
+        const int prefix = prefix_of(p, b);
+        r.win_lo = prefix < len ? prefix : len;
+        r.lo = r.win_lo / CK;
+        r.n_sink = 0;
+        r.n_chunks = r.win_lo < len ? len / CK + (len % CK != 0) - r.lo : 0;
+        return r;
+    }
     r.win_lo = (p.window > 0 && p.window < len) ? len - p.window : 0;
     r.lo = r.win_lo / CK;
     const int sink_chunks = p.sinks / CK + (p.sinks % CK != 0);
@@ -210,7 +250,7 @@ __device__ __forceinline__ void split2(float x0, float x1, uint32_t& hi, uint32_
 }
 
 // Position in the tile list, advanced tile by tile.  Every warp of a CTA walks the same tiles; kvh and r0 are its own.
-template <int NW, int CK>
+template <int NW, int CK, bool PREFIX>
 struct TileWalk {
     int b, h, t, t_end;   // sequence, group of heads, tile inside the pair, tiles of the pair
     int kvh, r0;          // K/V head, first query head of the part inside its group
@@ -221,7 +261,7 @@ struct TileWalk {
         b = b_;
         h = h_;
         t = t_;
-        r = seq_range<CK>(p, b);
+        r = seq_range<CK, PREFIX>(p, b);
         t_end = seq_tiles<NW>(r, hs);
         split_head(p);
     }
@@ -238,7 +278,7 @@ struct TileWalk {
             h = 0;
             do {
                 if (++b >= p.B) return true;      // the end of the list: not used again
-                r = seq_range<CK>(p, b);
+                r = seq_range<CK, PREFIX>(p, b);
                 t_end = seq_tiles<NW>(r, hs);
             } while (t_end == 0);
         }
@@ -257,8 +297,8 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 // P carries a factor 2^P_OFF where 16-bit floats run out of small numbers (fp16); the reference maximum may lag by 2^LAG.
 template <int DTYPE> struct ExpRange { static constexpr float P_OFF = DTYPE == 0 ? 6.f : 0.f, LAG = 8.f; };
 
-// GH: query heads of an item, 8 (up to 8 query heads per K/V head) or 16.
-template <int D, int DTYPE, int GH>
+// GH: query heads of an item, 8 (up to 8 query heads per K/V head) or 16.  PREFIX: see DecodeParams; not with clusters or a window.
+template <int D, int DTYPE, int GH, bool PREFIX>
 __global__ void __launch_bounds__(DecodeCfg<D, GH>::THREADS, 1)
 attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const DecodeParams p) {
     using C = DecodeCfg<D, GH>;
@@ -286,7 +326,7 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    TileWalk<NW, CK> ld, cu;      // the copies run NSTAGE - 1 tiles ahead of the arithmetic
+    TileWalk<NW, CK, PREFIX> ld, cu;      // the copies run NSTAGE - 1 tiles ahead of the arithmetic
     int steps, hs = 0, groups = p.heads;
     const int shift = 31 - __clz(p.cluster | 1), rank = static_cast<int>(blockIdx.x) & ((1 << shift) - 1);
     if (p.cluster) {
@@ -301,7 +341,7 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     const int b0 = tid * per, b1 = b0 + per < p.B ? b0 + per : p.B;
     int64_t mine[2] = {0, 0};                                // tiles in either form of the list
     for (int b = b0; b < b1; ++b) {
-        const SeqRange r = seq_range<CK>(p, b);
+        const SeqRange r = seq_range<CK, PREFIX>(p, b);
         mine[0] += seq_tiles<NW>(r, p.hpt_shift);
         mine[1] += seq_tiles<NW>(r, 0);
         if (p.seq_lens[b] > p.max_len && blockIdx.x == 0) report_bad_index(p.status);
@@ -334,14 +374,17 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     const bool side = hs == p.hpt_shift;
     const int64_t before = side ? before2[0] : before2[1], my_tiles = side ? mine[0] : mine[1];
     const int ctas = cta_count(total, p.grid);
-    if (static_cast<int>(blockIdx.x) >= ctas) return;
+    if (static_cast<int>(blockIdx.x) >= ctas) {
+        if (PREFIX) asm volatile("griddepcontrol.wait;" ::: "memory");
+        return;
+    }
     const int64_t first = cta_begin(total, blockIdx.x, ctas);
     steps = static_cast<int>(cta_begin(total, blockIdx.x + 1, ctas) - first);
     // the thread whose sequences hold tile `first` finds it
     if (first >= before * groups && first < (before + my_tiles) * groups) {
         int64_t rem = first - before * groups;
         for (int b = b0; b < b1; ++b) {
-            const int n = seq_tiles<NW>(seq_range<CK>(p, b), hs);
+            const int n = seq_tiles<NW>(seq_range<CK, PREFIX>(p, b), hs);
             if (rem < static_cast<int64_t>(n) * groups) {
                 scan[32] = b;
                 scan[33] = rem / n;
@@ -360,7 +403,7 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
 
     const uint32_t ring = sm100::smem_u32(smem) + warp * C::CHUNK_BYTES, my_bars = bars + 8 * warp * NSTAGE;
     // first key of this warp's chunk in the walk's tile; negative: no chunk
-    auto chunk_key = [&](const TileWalk<NW, CK>& w) {
+    auto chunk_key = [&](const TileWalk<NW, CK, PREFIX>& w) {
         const int ch = (w.t * NW + warp) >> hs;
         if (ch >= w.r.n_chunks) return -1;
         return (ch < w.r.n_sink ? ch : w.r.lo + ch - w.r.n_sink) * CK;
@@ -615,8 +658,8 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                             const int row = 8 * nt + 2 * c + h;
                             if (cu.r0 + row >= p.group) continue;
                             const float mm = m[nt][h] * sc, sum = l[nt][h];      // sum 0: no key, mm is not used
-                            if (whole) {
-                                const int64_t out_row = static_cast<int64_t>(cu.b) * p.H + cu.kvh * p.group + cu.r0 + row;
+                            const int64_t out_row = static_cast<int64_t>(cu.b) * p.H + cu.kvh * p.group + cu.r0 + row;
+                            if (whole && !PREFIX) {
                                 const float inv = sum != 0.f ? 1.f / sum : 0.f;
                                 uint8_t* dst = static_cast<uint8_t*>(p.o) + (out_row * D + 8 * g) * 2;
 #pragma unroll
@@ -628,14 +671,19 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                                 }
                                 if (g == 0) p.lse[out_row] = sum != 0.f ? (mm - P_OFF) * 0.6931471805599453f + logf(sum) : -INFINITY;
                             } else {
-                                float* dst = part + warp * C::PART_FLOATS;
+                                float* dst = part + warp * C::PART_FLOATS + row * D;
+                                float* ml = part + warp * C::PART_FLOATS + GH * D + 2 * row;
+                                if (PREFIX && whole) {
+                                    dst = p.rows + out_row * D;
+                                    ml = p.rows + static_cast<int64_t>(p.B) * p.H * D + 2 * out_row;
+                                }
 #pragma unroll
                                 for (int i = 0; i < VI; ++i)
 #pragma unroll
                                     for (int x = 0; x < 4; x += 2)
-                                        *reinterpret_cast<float4*>(dst + row * D + 64 * i + 8 * g + 2 * x) =
+                                        *reinterpret_cast<float4*>(dst + 64 * i + 8 * g + 2 * x) =
                                             make_float4(acc[nt][i][x][h], acc[nt][i][x][2 + h], acc[nt][i][x + 1][h], acc[nt][i][x + 1][2 + h]);
-                                if (g == 0) *reinterpret_cast<float2*>(dst + GH * D + 2 * row) = make_float2(mm, sum);
+                                if (g == 0) *reinterpret_cast<float2*>(ml) = make_float2(mm, sum);
                             }
                         }
                 } else {
@@ -678,8 +726,8 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                             o.z = fmaf(f, v.z, o.z);
                             o.w = fmaf(f, v.w, o.w);
                         }
-                        if (whole) {
-                            const int64_t out_row = static_cast<int64_t>(cu.b) * p.H + kvh * p.group + r0 + row;
+                        const int64_t out_row = static_cast<int64_t>(cu.b) * p.H + kvh * p.group + r0 + row;
+                        if (whole && !PREFIX) {
                             const float inv = sum != 0.f ? 1.f / sum : 0.f;
                             uint2 w;
                             w.x = sm100::pack2<DTYPE>(o.x * inv, o.y * inv);
@@ -689,8 +737,14 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                         } else {
                             // (a cluster's parts stay in shared memory, in the ring: every copy into it has been waited for)
                             float* dst = p.cluster ? reinterpret_cast<float*>(smem) : part + hh * C::PART_FLOATS;
-                            *reinterpret_cast<float4*>(dst + row * D + 4 * d4) = o;
-                            if (d4 == 0) *reinterpret_cast<float2*>(dst + GH * D + 2 * row) = make_float2(mm, sum);
+                            float* ml = dst + GH * D + 2 * row;
+                            dst += row * D;
+                            if (PREFIX && whole) {
+                                dst = p.rows + out_row * D;
+                                ml = p.rows + static_cast<int64_t>(p.B) * p.H * D + 2 * out_row;
+                            }
+                            *reinterpret_cast<float4*>(dst + 4 * d4) = o;
+                            if (d4 == 0) *reinterpret_cast<float2*>(ml) = make_float2(mm, sum);
                         }
                     }
                     __syncthreads();     // the merge buffer may be written again
@@ -705,6 +759,8 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     }
     __syncthreads();
     if (tid == 0 && *abort_flag != 0) attn_tc::report_timeout(p.status);
+    // the end of this kernel stands for the end of the one on the common keys, too
+    if (PREFIX) asm volatile("griddepcontrol.wait;" ::: "memory");
     if (p.cluster) {
         float* mine = reinterpret_cast<float*>(smem);
         if (steps == 0)
@@ -754,74 +810,12 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     }
 }
 
-// Joins the partial results of the pairs that more than one CTA of the first kernel worked on, and writes the rows of
-// sequences without a visible key.  A warp per row (sequence and query head), eight rows of one sequence to a block; the
-// list layout is worked out before the first kernel's results are waited for, and after that a row takes two dependent rounds
-// of loads: the parts' exponents and sums, one per lane, then their rows.
-constexpr int kJoinWarps = 8;
-template <int D, int DTYPE, int GH>
-__global__ void __launch_bounds__(kJoinWarps * 32)
-attn_paged_join_kernel(const DecodeParams p, int blocks_per_seq) {
-    using C = DecodeCfg<D, GH>;
-    constexpr int NW = C::NW, COLS = D / 4;                // 16-byte columns of a partial row
+// One row (sequence and query head) out of np partial results, by one warp: ml_of(i) gives part i's reference exponent, which stands
+// p_off too high, and its sum; row_of(i) its O.  The order of the parts is fixed.
+template <int D, int DTYPE, class MlOf, class RowOf>
+__device__ __forceinline__ void join_row(int np, int lane, float p_off, MlOf ml_of, RowOf row_of, void* out, float* lse) {
+    constexpr int COLS = D / 4;                            // 16-byte columns of a partial row
     constexpr int TEAMS = COLS >= 32 ? 1 : 32 / COLS, PER = COLS >= 32 ? COLS / 32 : 1;
-    constexpr float P_OFF = ExpRange<DTYPE>::P_OFF;
-    __shared__ int64_t red[4][kJoinWarps];
-    const int b = blockIdx.x / blocks_per_seq;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int q_head = (blockIdx.x - b * blocks_per_seq) * kJoinWarps + warp;
-    int64_t sum4[4] = {0, 0, 0, 0};                        // tiles of the sequences before b and of all, in either form of the list
-    for (int x = tid; x < p.B; x += kJoinWarps * 32) {
-        const SeqRange r = seq_range<C::CK>(p, x);
-        const int n0 = seq_tiles<NW>(r, p.hpt_shift), n1 = seq_tiles<NW>(r, 0);
-        sum4[2] += n0;
-        sum4[3] += n1;
-        if (x < b) {
-            sum4[0] += n0;
-            sum4[1] += n1;
-        }
-    }
-#pragma unroll
-    for (int f = 0; f < 4; ++f) {
-        sum4[f] = warp_sum(sum4[f]);
-        if (lane == 0) red[f][warp] = sum4[f];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int f = 0; f < 4; ++f) {
-        sum4[f] = 0;
-#pragma unroll
-        for (int w = 0; w < kJoinWarps; ++w) sum4[f] += red[f][w];
-    }
-    const ListForm form = list_form(p, sum4[2], sum4[3]);
-    const int64_t total = form.total;
-    const int hs = form.hpt_shift, groups = p.heads >> hs;
-    const int64_t before = hs == p.hpt_shift ? sum4[0] : sum4[1];
-    const int n = seq_tiles<NW>(seq_range<C::CK>(p, b), hs);
-    // Every block waits for the first kernel, also one without work: in a graph this kernel's end stands for both.
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (q_head >= p.H) return;
-    const int kvh = q_head / p.group, in_group = q_head - kvh * p.group, row = in_group & 15;
-    const int head = kvh * p.sub + (in_group >> 4);
-    const int64_t out_row = static_cast<int64_t>(b) * p.H + q_head;
-    uint2* out = reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.o) + out_row * D * 2);
-    if (n == 0) {
-        for (int e = lane; e < COLS; e += 32) out[e] = make_uint2(0u, 0u);
-        if (lane == 0) p.lse[out_row] = -INFINITY;
-        return;
-    }
-    const int hg = head >> hs, hh = head - (hg << hs);
-    const int64_t t0 = before * groups + static_cast<int64_t>(hg) * n, t1 = t0 + n;
-    const int ctas = cta_count(total, p.grid);
-    const int c0 = cta_of_tile(total, t0, ctas), c1 = cta_of_tile(total, t1 - 1, ctas);
-    if (c0 == c1) return;                        // finished by the first kernel
-    // the pair is the first of every CTA but, perhaps, of c0
-    const int slot0 = 2 * c0 + (cta_begin(total, c0, ctas) < t0 ? 1 : 0);
-    const int np = c1 - c0 + 1;
-    auto part = [&](int i) {
-        const int64_t slot = i == 0 ? slot0 : 2 * (c0 + i);
-        return p.parts + ((slot << hs) + hh) * C::PART_FLOATS;
-    };
     // up to 32 parts at a time: a row of more is joined in rounds, like the rounds of an online softmax
     float mm = -INFINITY, sum = 0.f;
     float4 o[PER];
@@ -830,7 +824,7 @@ attn_paged_join_kernel(const DecodeParams p, int blocks_per_seq) {
     const int team = TEAMS > 1 ? lane / COLS : 0, col = TEAMS > 1 ? lane % COLS : lane;
     for (int i0 = 0; i0 < np; i0 += 32) {
         float2 ml = make_float2(-INFINITY, 0.f);
-        if (i0 + lane < np) ml = __ldcg(reinterpret_cast<const float2*>(part(i0 + lane) + GH * D + 2 * row));
+        if (i0 + lane < np) ml = __ldcg(ml_of(i0 + lane));
         float mx = ml.y != 0.f ? ml.x : -INFINITY;
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
@@ -850,7 +844,7 @@ attn_paged_join_kernel(const DecodeParams p, int blocks_per_seq) {
             const int mine = i + team < m ? i + team : m - 1;                // (a weight of 0 below for the repeated one)
             float w = __shfl_sync(0xffffffffu, f, mine);
             if (i + team >= m) w = 0.f;
-            const float4* src = reinterpret_cast<const float4*>(part(i0 + mine) + row * D);
+            const float4* src = reinterpret_cast<const float4*>(row_of(i0 + mine));
 #pragma unroll
             for (int k = 0; k < PER; ++k) {
                 const float4 v = __ldcg(src + col + 32 * k);
@@ -879,10 +873,115 @@ attn_paged_join_kernel(const DecodeParams p, int blocks_per_seq) {
             uint2 w;
             w.x = sm100::pack2<DTYPE>(o[k].x * inv, o[k].y * inv);
             w.y = sm100::pack2<DTYPE>(o[k].z * inv, o[k].w * inv);
-            out[col + 32 * k] = w;
+            reinterpret_cast<uint2*>(out)[col + 32 * k] = w;
         }
     }
-    if (lane == 0) p.lse[out_row] = sum != 0.f ? (mm - P_OFF) * 0.6931471805599453f + logf(sum) : -INFINITY;
+    if (lane == 0) *lse = sum != 0.f ? (mm - p_off) * 0.6931471805599453f + logf(sum) : -INFINITY;
+}
+
+constexpr int kJoinWarps = 8;
+// A row without a visible key.
+template <int D>
+__device__ __forceinline__ void empty_row(void* out, float* lse, int lane) {
+    for (int e = lane; e < D / 4; e += 32) static_cast<uint2*>(out)[e] = make_uint2(0u, 0u);
+    if (lane == 0) *lse = -INFINITY;
+}
+
+// Where the partial results of one sequence's heads lie: worked out by a whole block of kJoinWarps warps from the lengths.
+template <int D, int GH, bool PREFIX>
+struct JoinList {
+    using C = DecodeCfg<D, GH>;
+    int64_t total, before;     // tiles of the list, and of the sequences in front
+    int hs, groups, n, ctas;   // log2 of a tile's heads, groups of heads, tiles of a pair of this sequence
+    __device__ __forceinline__ JoinList(const DecodeParams& p, int b, int64_t (*red)[kJoinWarps]) {
+        constexpr int NW = C::NW;
+        const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+        int64_t sum4[4] = {0, 0, 0, 0};                    // tiles of the sequences before b and of all, in either form of the list
+        for (int x = tid; x < p.B; x += kJoinWarps * 32) {
+            const SeqRange r = seq_range<C::CK, PREFIX>(p, x);
+            const int n0 = seq_tiles<NW>(r, p.hpt_shift), n1 = seq_tiles<NW>(r, 0);
+            sum4[2] += n0;
+            sum4[3] += n1;
+            if (x < b) {
+                sum4[0] += n0;
+                sum4[1] += n1;
+            }
+        }
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+            sum4[f] = warp_sum(sum4[f]);
+            if (lane == 0) red[f][warp] = sum4[f];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+            sum4[f] = 0;
+#pragma unroll
+            for (int w = 0; w < kJoinWarps; ++w) sum4[f] += red[f][w];
+        }
+        const ListForm form = list_form(p, sum4[2], sum4[3]);
+        total = form.total;
+        hs = form.hpt_shift;
+        groups = p.heads >> hs;
+        before = hs == p.hpt_shift ? sum4[0] : sum4[1];
+        n = seq_tiles<NW>(seq_range<C::CK, PREFIX>(p, b), hs);
+        ctas = cta_count(total, p.grid);
+    }
+};
+
+// The parts of one row: head (of the K/V heads' parts of at most 16 query heads) and row of the pair.
+struct RowParts {
+    int count = 0;             // 1: one CTA has the pair to itself
+    int c0, hs, hh, head, row;
+    bool odd;                  // the pair is not c0's first (it is that of every CTA behind c0)
+    template <class List>
+    __device__ __forceinline__ void find(const DecodeParams& p, const List& l, int q_head) {       // (l.n > 0)
+        const int kvh = q_head / p.group, in_group = q_head - kvh * p.group;
+        row = in_group & 15;
+        head = kvh * p.sub + (in_group >> 4);
+        hs = l.hs;
+        const int hg = head >> hs;
+        hh = head - (hg << hs);
+        const int64_t t0 = l.before * l.groups + static_cast<int64_t>(hg) * l.n, t1 = t0 + l.n;
+        c0 = cta_of_tile(l.total, t0, l.ctas);
+        count = cta_of_tile(l.total, t1 - 1, l.ctas) - c0 + 1;
+        odd = cta_begin(l.total, c0, l.ctas) < t0;
+    }
+    template <int PART_FLOATS>
+    __device__ __forceinline__ const float* at(const DecodeParams& p, int i) const {
+        const int64_t slot = i == 0 ? 2 * c0 + (odd ? 1 : 0) : 2 * (c0 + i);
+        return p.parts + ((slot << hs) + hh) * PART_FLOATS;
+    }
+};
+
+// Joins the partial results of the pairs that more than one CTA of the first kernel worked on, and writes the rows of
+// sequences without a visible key.  A warp per row (sequence and query head), eight rows of one sequence to a block; the
+// list layout is worked out before the first kernel's results are waited for, and after that a row takes two dependent rounds
+// of loads: the parts' exponents and sums, one per lane, then their rows.
+template <int D, int DTYPE, int GH>
+__global__ void __launch_bounds__(kJoinWarps * 32)
+attn_paged_join_kernel(const DecodeParams p, int blocks_per_seq) {
+    using C = DecodeCfg<D, GH>;
+    constexpr float P_OFF = ExpRange<DTYPE>::P_OFF;
+    __shared__ int64_t red[4][kJoinWarps];
+    const int b = blockIdx.x / blocks_per_seq, lane = threadIdx.x & 31;
+    const int q_head = (blockIdx.x - b * blocks_per_seq) * kJoinWarps + (threadIdx.x >> 5);
+    const JoinList<D, GH, false> list(p, b, red);
+    // Every block waits for the first kernel, also one without work: in a graph this kernel's end stands for both.
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (q_head >= p.H) return;
+    const int64_t out_row = static_cast<int64_t>(b) * p.H + q_head;
+    uint8_t* out = static_cast<uint8_t*>(p.o) + out_row * D * 2;
+    if (list.n == 0) {
+        empty_row<D>(out, p.lse + out_row, lane);
+        return;
+    }
+    RowParts parts;
+    parts.find(p, list, q_head);
+    if (parts.count == 1) return;                // finished by the first kernel
+    auto part = [&](int i) { return parts.at<C::PART_FLOATS>(p, i); };
+    join_row<D, DTYPE>(parts.count, lane, P_OFF, [&](int i) { return reinterpret_cast<const float2*>(part(i) + GH * D) + parts.row; },
+                       [&](int i) { return part(i) + parts.row * D; }, out, p.lse + out_row);
 }
 
 }  // namespace attn_paged

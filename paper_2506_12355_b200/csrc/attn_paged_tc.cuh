@@ -1,0 +1,946 @@
+// Attention of many query rows over the paged cache on the tensor cores (tcgen05), in two forms:
+//
+//   prefill (PREFIX = false): the n new tokens of each sequence of length len; token i sees the keys j <= len - n + i.
+//   prefix  (PREFIX = true):  one new token per sequence, and only the first P keys, which the sequences of a group have in common:
+//                             a token sees the keys j < min(P, its sequence's length).  K and V of the prefix are read once for
+//                             all rows of the group; attn_paged.cuh adds each sequence's other keys.
+//
+//     O = sum_j p_j V_j / sum_j p_j,   p_j = exp(scale <q, K_j>),   LSE = ln sum_j p_j
+//
+// A list is one K/V head and a pair of 128-row tiles of queries; row r of a tile is query head r % G of the K/V head's G, of token
+// r / G (128 / G tokens to a tile, rounded down), which a TMA box brings in that order from [token][head][D].  Its steps are the
+// 128-key tiles that its last token sees.  The steps of all lists, one after the other, are cut evenly over one CTA per SM,
+// whatever the lengths are (each CTA works out its own part from the device-side lengths: no host copy, no plan to keep); a list
+// that a border cuts leaves a partial result per CTA (at most two per CTA, fp32), which a second kernel joins in a fixed order.
+//
+// Inside a CTA it is the pipeline of attn_tc_pipe.cuh: TMA ring of K/V tiles, one MMA-issuing warp, two softmax groups in
+// ping-pong, P back into tensor memory as the second product's operand, a lagging reference maximum.  What paging adds:
+//   * A tile is 128 / page_size boxes per 64 columns, issued by as many lanes of the producer warp; its page numbers are read a
+//     step ahead.
+//   * Slots that hold no key of the sequence (behind its end, or in a page whose number is out of range) may hold anything: their
+//     scores are overwritten with -inf before the softmax, and their V rows with zeros before the product (0 * NaN is no number).
+//   * All exponentials on the special-function unit, as under a window: rows may see only a few keys.
+// P is rounded to the type of Q, K and V before its product and the row sums add the unrounded values (see attn_tc_pipe.cuh).
+#pragma once
+#include "attn_paged.cuh"
+#include "attn_tc_common.cuh"
+
+namespace attn_paged_tc {
+
+using namespace sm100;
+using attn_paged::cta_begin;
+using attn_paged::cta_count;
+using attn_paged::cta_of_tile;
+using attn_paged::group_prefix;
+using attn_paged::report_bad_index;
+using attn_tc::low_bits;
+
+constexpr int kRows = 256;                        // rows of a list: two tiles
+
+template <int D>
+struct Cfg {
+    static constexpr int NBOX = D / 64;           // 64-column boxes (128 bytes a row)
+    static constexpr int Q_BYTES = 128 * D * 2, KV_BYTES = 128 * D * 2;
+    static constexpr int NSLOT = D == 128 ? 4 : 8, NGRP = NSLOT / 2;      // ring slots; a group is V_j and K_{j+1}
+    static constexpr int OST_BYTES = 128 * 128;   // staging of a tile's output, 128 bytes a row
+    static constexpr int TILE_BYTES = 2 * Q_BYTES + NSLOT * KV_BYTES + 2 * OST_BYTES;
+    static constexpr int MISC_BYTES = 1024;
+    static constexpr int SMEM_BYTES = 1024 + TILE_BYTES + MISC_BYTES;
+    static constexpr int THREADS = 384, TMEM_COLS = 512;
+    __host__ __device__ static constexpr int s_col(int t) { return t * 128; }
+    __host__ __device__ static constexpr int o_col(int t) { return 256 + t * D; }
+    static_assert(SMEM_BYTES <= 232448, "shared memory budget");
+};
+
+// floats of one partial result: O [256][D] (not normalised), then reference exponent and sum [256][2]
+__host__ __device__ constexpr int64_t part_floats(int D) { return static_cast<int64_t>(kRows) * (D + 2); }
+
+struct Params {
+    void* o;                    // prefill: [tokens, H, D] and lse [tokens, H]
+    float* lse;
+    float* parts;               // [2 per CTA] partial results of lists that a border cuts
+    float* rows;                // prefix: O [tokens * H][D], then [tokens * H][2], of lists that one CTA has to itself
+    const int* block_table;
+    const int* seq_lens;
+    const int* starts;          // [units + 1]: first token of each sequence (prefill), first sequence of each group (prefix)
+    const int* prefix_lens;     // prefix: [units]
+    int64_t table_stride;
+    int units, tokens;          // sequences and their new tokens; groups and sequences
+    int H, Hkv, group, tile_tokens;
+    int max_len, num_pages, page_shift, box_shift, k_axes, v_axes;
+    float scale, scale_log2;
+    int grid;
+    int* status;
+#ifdef ATTN_TEST_HOOKS
+    int test_skip_group;        // test build only: the ring group of every CTA whose copies are left out (-1: none)
+#endif
+};
+
+// sum over i < n of floor((a i + b) / 128)
+__device__ __forceinline__ int64_t floor_sum(uint32_t n, uint32_t a, uint32_t b) {
+    uint32_t m = 128;
+    int64_t sum = 0;
+    while (n > 0) {
+        sum += static_cast<int64_t>(n) * (n - 1) / 2 * (a / m) + static_cast<int64_t>(n) * (b / m);
+        a %= m;
+        b %= m;
+        const uint64_t y = static_cast<uint64_t>(a) * n + b;
+        if (y < m) break;
+        n = static_cast<uint32_t>(y / m);
+        b = static_cast<uint32_t>(y % m);
+        const uint32_t x = m;
+        m = a;
+        a = x;
+    }
+    return sum;
+}
+
+// One sequence (prefill) or group (prefix).
+template <bool PREFIX>
+struct Unit {
+    int tok0, n;       // its query tokens
+    int base;          // prefill: the last key that token 0 sees
+    int len;           // keys
+    int pairs;
+    __device__ __forceinline__ void load(const Params& p, int u) {
+        tok0 = __ldg(p.starts + u);
+        int end = __ldg(p.starts + u + 1);
+        tok0 = tok0 < 0 ? 0 : (tok0 > p.tokens ? p.tokens : tok0);
+        end = end < tok0 ? tok0 : (end > p.tokens ? p.tokens : end);
+        n = end - tok0;
+        if constexpr (PREFIX) {
+            len = n > 0 ? group_prefix(p.seq_lens, tok0, __ldg(p.prefix_lens + u), p.max_len) : 0;
+            base = 0;
+        } else {
+            len = __ldg(p.seq_lens + u);
+            len = len > p.max_len ? p.max_len : len;
+            base = len - n;
+        }
+        if (len <= 0) n = 0;
+        const int t2 = 2 * p.tile_tokens;
+        pairs = (n + t2 - 1) / t2;
+    }
+    // steps of the first `tokens` query tokens (at least one, also where none of them sees a key)
+    __device__ __forceinline__ int steps_of(int tokens) const {
+        if (PREFIX) return (len + 127) >> 7;
+        return ((base > 0 ? base : 0) + (tokens < n ? tokens : n) - 1) / 128 + 1;
+    }
+    __device__ __forceinline__ int pair_steps(const Params& p, int i) const { return steps_of((i + 1) * 2 * p.tile_tokens); }
+    // steps of the pairs before i
+    __device__ __forceinline__ int64_t steps_before(const Params& p, int i) const {
+        if (PREFIX) return static_cast<int64_t>(i) * ((len + 127) >> 7);
+        const int t2 = 2 * p.tile_tokens, full = i < pairs ? i : pairs - 1;
+        if (i == 0) return 0;
+        return floor_sum(full, t2, (base > 0 ? base : 0) + t2 - 1) + full + (i == pairs ? steps_of(n) : 0);
+    }
+    __device__ __forceinline__ int64_t head_steps(const Params& p) const { return steps_before(p, pairs); }
+};
+
+// Position in the lists: unit, K/V head, pair, step of the pair's list.  All lanes of a warp hold the same one.
+template <bool PREFIX>
+struct Walk {
+    Unit<PREFIX> unit;
+    int u, h, i, step, steps;
+    // Total steps of all lists; all 32 lanes.  mine, before: the steps of this lane's units and of those in front of them.
+    static __device__ __forceinline__ int64_t total(const Params& p, int lane, int64_t& mine, int64_t& before) {
+        const int per = (p.units + 31) / 32, u0 = lane * per, u1 = u0 + per < p.units ? u0 + per : p.units;
+        mine = 0;
+        for (int x = u0; x < u1; ++x) {
+            Unit<PREFIX> unit;
+            unit.load(p, x);
+            mine += p.Hkv * unit.head_steps(p);
+        }
+        before = mine;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int64_t up = __shfl_up_sync(0xffffffffu, before, off);
+            if (lane >= off) before += up;
+        }
+        const int64_t all = __shfl_sync(0xffffffffu, before, 31);
+        before -= mine;
+        return all;
+    }
+    // Step `at` of all (below the total).
+    __device__ __forceinline__ void find(const Params& p, int lane, int64_t at, int64_t mine, int64_t before) {
+        const int per = (p.units + 31) / 32;
+        const bool here = at >= before && at < before + mine;
+        const int owner = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+        int64_t rem = at - before;
+        int x = lane * per;
+        if (here)
+            for (;; ++x) {
+                unit.load(p, x);
+                const int64_t n = p.Hkv * unit.head_steps(p);
+                if (rem < n) break;
+                rem -= n;
+            }
+        u = __shfl_sync(0xffffffffu, x, owner);
+        rem = __shfl_sync(0xffffffffu, rem, owner);
+        unit.load(p, u);
+        const int64_t per_head = unit.head_steps(p);
+        h = static_cast<int>(rem / per_head);
+        rem -= h * per_head;
+        // the last pair with steps_before <= rem, 32 candidates at a time
+        int lo = 0, hi = unit.pairs;
+        while (hi - lo > 1) {
+            const int stride = (hi - lo + 31) / 32, mid = lo + lane * stride;
+            const unsigned ok = __ballot_sync(0xffffffffu, mid < hi && unit.steps_before(p, mid) <= rem);
+            lo += (31 - __clz(ok)) * stride;
+            hi = lo + stride < hi ? lo + stride : hi;
+        }
+        i = lo;
+        step = static_cast<int>(rem - unit.steps_before(p, i));
+        steps = unit.pair_steps(p, i);
+    }
+    // The next list (not called behind the last one).
+    __device__ __forceinline__ void next(const Params& p) {
+        step = 0;
+        if (++i == unit.pairs) {
+            i = 0;
+            if (++h == p.Hkv) {
+                h = 0;
+                do unit.load(p, ++u);
+                while (unit.pairs == 0 && u + 1 < p.units);
+            }
+        }
+        steps = unit.pair_steps(p, i);
+    }
+};
+
+// A CTA's share of one list, as the roles of the CTA get it.
+struct Item {
+    int kvh, tok, n_tok;       // K/V head; first token and the tokens from there to the end of the unit
+    int n0, n1, n_max;         // steps of each tile in this share (-1: a tile without tokens)
+    int tile0;                 // first key tile
+    int base, len;             // last key that the first token sees (prefill); keys
+    int slot;                  // partial result (-1: the whole list)
+    int first_row;             // row of the block table
+    __device__ __forceinline__ int n(int t) const { return t ? n1 : n0; }
+};
+
+__device__ __forceinline__ void reg_inc_softmax() { asm volatile("setmaxnreg.inc.sync.aligned.u32 216;"); }
+__device__ __forceinline__ void reg_dec_service() { asm volatile("setmaxnreg.dec.sync.aligned.u32 64;"); }
+
+template <int D, int DTYPE, bool PREFIX>
+__global__ void __launch_bounds__(Cfg<D>::THREADS, 1)
+attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                     const __grid_constant__ Params p) {
+    using C = Cfg<D>;
+    constexpr int NBOX = C::NBOX, NGRP = C::NGRP;
+    constexpr float LAG = 8.f;                     // the reference maximum may lag by 2^LAG
+    constexpr float P_OFF = attn_paged::ExpRange<DTYPE>::P_OFF;      // what the partial results of attn_paged.cuh carry
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
+    auto sQ = [&](int t) { return smem_base + t * C::Q_BYTES; };
+    auto sKV = [&](int slot) { return smem_base + 2 * C::Q_BYTES + slot * C::KV_BYTES; };
+    auto sOst = [&](int t) { return smem_base + 2 * C::Q_BYTES + C::NSLOT * C::KV_BYTES + t * C::OST_BYTES; };
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem_gen + C::TILE_BYTES);
+    enum {
+        B_QFULL = 0,       // [2] Q tile t loaded
+        B_QEMPTY = 2,      // [2] every S product of tile t of the item has finished
+        B_SFULL = 4,       // [2] S_t ready
+        B_PFULL = 6,       // [2] first three quarters of P_t written (128 threads)
+        B_PFULL2 = 8,      // [2] the rest
+        B_OFINAL = 10,     // [2] the item's last O_t += P_t V has finished
+        B_OFREE = 12,      // [2] O_t is in registers (128 threads)
+        B_SCHEDFULL = 14,  // [4] slot holds an item
+        B_SCHEDEMPTY = 18, // [4] slot read by the MMA warp and the eight softmax warps
+        B_KVFULL = 22,
+        B_KVEMPTY = 22 + NGRP,
+        B_COUNT = 22 + 2 * NGRP
+    };
+    auto bar = [&](int i) { return smem_base + C::TILE_BYTES + i * 8; };
+    volatile int* sched = reinterpret_cast<volatile int*>(bars + B_COUNT);             // [4][16]
+    // [8][8]: of the key tile in ring group g % 8: whether any of its keys' pages is out of range, and which keys as bits.  (The
+    // producer is at most NGRP groups ahead of the tile that the softmax groups are working on.)
+    volatile uint32_t* bad_ring = reinterpret_cast<volatile uint32_t*>(sched + 64);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(const_cast<uint32_t*>(bad_ring) + 64);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    static_assert(8 * B_COUNT + 4 * (64 + 64 + 2) <= C::MISC_BYTES, "barriers and slots");
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tile_rows = p.tile_tokens * p.group;
+
+    if (tid == 0) {
+        *abort_flag = 0;
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(bar(B_QFULL + t), 1);
+            mbar_init(bar(B_QEMPTY + t), 1);
+            mbar_init(bar(B_SFULL + t), 1);
+            mbar_init(bar(B_PFULL + t), 128);
+            mbar_init(bar(B_PFULL2 + t), 128);
+            mbar_init(bar(B_OFINAL + t), 1);
+            mbar_init(bar(B_OFREE + t), 128);
+        }
+        for (int s = 0; s < 4; ++s) {
+            mbar_init(bar(B_SCHEDFULL + s), 1);
+            mbar_init(bar(B_SCHEDEMPTY + s), 9);
+        }
+        for (int s = 0; s < NGRP; ++s) {
+            mbar_init(bar(B_KVFULL + s), 1);
+            mbar_init(bar(B_KVEMPTY + s), 1);
+        }
+        fence_barrier_init();
+        fence_proxy_async_smem();
+    }
+    // rows that no box writes (128 is not a multiple of the group) must be numbers
+    for (int e = tid; tile_rows < 128 && e < 2 * NBOX * (128 - tile_rows) * 8; e += C::THREADS) {
+        const int plane = e / ((128 - tile_rows) * 8);
+        *reinterpret_cast<uint4*>(smem_gen + (plane * 128 + tile_rows) * 128 + (e - plane * (128 - tile_rows) * 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
+    }
+    if (tile_rows < 128) fence_proxy_async_smem();
+    if (warp == 8) {
+        tmem_alloc(smem_u32(tmem_slot), C::TMEM_COLS);
+        tmem_relinquish();
+    }
+    if (warp == 9 && lane == 0) {
+        prefetch_tensormap(&tmQ);
+        prefetch_tensormap(&tmK);
+        prefetch_tensormap(&tmV);
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const uint32_t tmem = *tmem_slot;
+
+    // every wait of a warp ends for all of its lanes alike
+    auto wait = [&](int b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar(b), parity, abort_flag)) != 0; };
+    // The k-th item of this CTA; false: there is none.
+    auto next_item = [&](int k, bool hand_back, Item& it) -> bool {
+        const int slot = k & 3;
+        if (!wait(B_SCHEDFULL + slot, (k >> 2) & 1)) return false;
+        volatile int* e = sched + slot * 16;
+        const bool valid = e[0] != 0;
+        it.kvh = e[1];
+        it.tok = e[2];
+        it.n_tok = e[3];
+        it.n0 = e[4];
+        it.n1 = e[5];
+        it.tile0 = e[6];
+        it.base = e[7];
+        it.len = e[8];
+        it.slot = e[9];
+        it.first_row = e[10];
+        it.n_max = it.n0 > it.n1 ? it.n0 : it.n1;
+        __syncwarp();
+        if (hand_back) mbar_arrive(bar(B_SCHEDEMPTY + slot));
+        return valid;
+    };
+
+    if (warp >= 8) {
+        reg_dec_service();
+        if (warp == 9) {
+            // =========================== lists, TMA ===========================
+            const bool leader = elect_one();
+            Walk<PREFIX> walk;
+            int64_t mine, before, left = 0;
+            const int64_t total = Walk<PREFIX>::total(p, lane, mine, before);
+            const int ctas = cta_count(total, p.grid);
+            if (static_cast<int>(blockIdx.x) < ctas) {
+                const int64_t first = cta_begin(total, blockIdx.x, ctas);
+                left = cta_begin(total, blockIdx.x + 1, ctas) - first;
+                walk.find(p, lane, first, mine, before);
+            }
+            int kv_base = 0, q_uses[2] = {0, 0};
+            const int boxes = 128 >> p.box_shift, slot_mask = (1 << p.page_shift) - 1;
+            for (int k = 0;; ++k) {
+                const int slot = k & 3;
+                if (!wait(B_SCHEDEMPTY + slot, ((k >> 2) & 1) ^ 1)) break;
+                Item it;
+                if (left > 0) {
+                    const int s0 = walk.step, s1 = walk.steps - s0 < left ? walk.steps : s0 + static_cast<int>(left);
+                    const int pair_tok = walk.i * 2 * p.tile_tokens;
+                    it.kvh = walk.h;
+                    it.tok = walk.unit.tok0 + pair_tok;
+                    it.n_tok = walk.unit.n - pair_tok;
+                    it.tile0 = s0;
+                    it.base = walk.unit.base + pair_tok;
+                    it.len = walk.unit.len;
+                    it.first_row = PREFIX ? walk.unit.tok0 : walk.u;
+                    const int all0 = walk.unit.steps_of(pair_tok + p.tile_tokens);
+                    it.n0 = (all0 < s1 ? all0 : s1) - s0;
+                    it.n0 = it.n0 < 0 ? 0 : it.n0;
+                    it.n1 = it.n_tok > p.tile_tokens ? s1 - s0 : -1;
+                    it.n_max = it.n0 > it.n1 ? it.n0 : it.n1;
+                    it.slot = s0 == 0 && s1 == walk.steps ? -1 : 2 * static_cast<int>(blockIdx.x) + (s0 == 0 ? 1 : 0);
+                    left -= s1 - s0;
+                    if (left > 0) walk.next(p);
+                    if (leader) {
+                        volatile int* e = sched + slot * 16;
+                        e[1] = it.kvh;
+                        e[2] = it.tok;
+                        e[3] = it.n_tok;
+                        e[4] = it.n0;
+                        e[5] = it.n1;
+                        e[6] = it.tile0;
+                        e[7] = it.base;
+                        e[8] = it.len;
+                        e[9] = it.slot;
+                        e[10] = it.first_row;
+                        e[0] = 1;
+                        mbar_arrive(bar(B_SCHEDFULL + slot));
+                    }
+                } else {
+                    if (leader) {
+                        sched[slot * 16] = 0;
+                        mbar_arrive(bar(B_SCHEDFULL + slot));
+                    }
+                    break;
+                }
+                const int* table = p.block_table + static_cast<int64_t>(it.first_row) * p.table_stride;
+                // pages of a tile's boxes, box 32 r + lane: -1: no key there, -2: not a page
+                auto fetch = [&](int tile, int* pg) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int box = 32 * r + lane, key = tile * 128 + (box << p.box_shift);
+                        pg[r] = -1;
+                        if (box < boxes && key < it.len) {
+                            pg[r] = __ldg(table + (key >> p.page_shift));
+                            if (static_cast<unsigned>(pg[r]) >= static_cast<unsigned>(p.num_pages)) pg[r] = -2;
+                        }
+                    }
+                };
+                auto count = [&](const int* pg) {
+                    int n = 0;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) n += __popc(__ballot_sync(0xffffffffu, pg[r] >= 0));
+                    return n;
+                };
+                auto load_tile = [&](uint32_t dst, const CUtensorMap* map, int axes, uint32_t full, int tile, const int* pg) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        if (32 * r >= boxes) break;
+                        const int row = (32 * r + lane) << p.box_shift;
+                        if (pg[r] >= 0) {
+#pragma unroll
+                            for (int pl = 0; pl < NBOX; ++pl)
+                                attn_paged::load_box(dst + pl * 16384 + row * 128, map, full, axes, pl, (tile * 128 + row) & slot_mask, it.kvh, pg[r]);
+                        }
+                    }
+                };
+                auto load_q = [&](int t) -> bool {
+                    if (!wait(B_QEMPTY + t, (q_uses[t] & 1) ^ 1)) return false;
+                    if (leader) {
+                        mbar_arrive_expect_tx(bar(B_QFULL + t), NBOX * tile_rows * 128);
+#pragma unroll
+                        for (int bx = 0; bx < NBOX; ++bx)
+                            asm volatile(
+                                "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                                ::"r"(sQ(t) + bx * 16384), "l"(reinterpret_cast<uint64_t>(&tmQ)), "r"(bar(B_QFULL + t)), "r"(64 * bx), "r"(it.kvh * p.group),
+                                "r"(it.tok + t * p.tile_tokens), "r"(0)
+                                : "memory");
+                    }
+                    ++q_uses[t];
+                    return true;
+                };
+                // Ring group i of an item: {V_{i-1}, K_i}, what the MMA warp needs together (see attn_tc_pipe.cuh).
+                int pg_v[4] = {-1, -1, -1, -1}, pg_k[4], pg_next[4];
+                fetch(it.tile0, pg_next);
+                bool ok = it.n0 > 0 ? load_q(0) : true;
+                for (int i = 0; i <= it.n_max && ok; ++i) {
+                    const int group = kv_base + i, g = group % NGRP;
+                    const bool has_v = i > 0, has_k = i < it.n_max;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) pg_k[r] = pg_next[r];
+                    if (i + 1 < it.n_max) fetch(it.tile0 + i + 1, pg_next);
+                    if (!(ok = wait(B_KVEMPTY + g, ((group / NGRP) & 1) ^ 1))) break;
+                    if (has_k) {
+                        volatile uint32_t* bad = bad_ring + (group & 7) * 8;
+                        bool any = false;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) any = any || pg_k[r] == -2;
+                        any = __any_sync(0xffffffffu, any);
+                        if (any) {       // rare: the tile's bits are put together word by word
+                            if (lane == 0) report_bad_index(p.status);
+                            for (int w = 0; w < 4; ++w) {
+                                // key 32 w + lane lies in box (32 w + lane) >> box_shift, whose page number lane box % 32 has
+                                const int box = (32 * w + lane) >> p.box_shift;
+                                int pg = -1;
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) {
+                                    const int x = __shfl_sync(0xffffffffu, pg_k[r], box & 31);
+                                    if (box >> 5 == r) pg = x;
+                                }
+                                const uint32_t word = __ballot_sync(0xffffffffu, pg == -2);
+                                if (lane == 0) bad[1 + w] = word;
+                            }
+                        }
+                        if (lane == 0) bad[0] = any ? 1u : 0u;
+                    }
+                    const int n_boxes = (has_v ? count(pg_v) : 0) + (has_k ? count(pg_k) : 0);
+                    __syncwarp();
+#ifdef ATTN_TEST_HOOKS
+                    if (group != p.test_skip_group)      // (this group's barrier never completes)
+#endif
+                    {
+                        if (lane == 0) mbar_arrive_expect_tx(bar(B_KVFULL + g), (n_boxes * NBOX << p.box_shift) * 128);
+                        __syncwarp();                    // armed before the first copy
+                        if (has_v) load_tile(sKV(2 * g), &tmV, p.v_axes, bar(B_KVFULL + g), it.tile0 + i - 1, pg_v);
+                        if (has_k) load_tile(sKV(2 * g + 1), &tmK, p.k_axes, bar(B_KVFULL + g), it.tile0 + i, pg_k);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) pg_v[r] = pg_k[r];
+                    if (i == 0 && it.n1 > 0) ok = load_q(1);
+                }
+                if (!ok) break;
+                kv_base += it.n_max + 1;
+            }
+        } else if (warp == 8) {
+            // =========================== MMA issuer ===========================
+            const bool leader = elect_one();
+            constexpr uint32_t IDESC_S = make_idesc_f16(128, 128, DTYPE, 0, 0);
+            constexpr uint32_t IDESC_O = make_idesc_f16(128, D, DTYPE, 0, 1);
+            constexpr uint32_t DESC_HI = smem_desc_hi_sw128(1024);
+            const uint32_t q_lo[2] = {smem_desc_lo(sQ(0), 16), smem_desc_lo(sQ(1), 16)};
+            const uint32_t k_lo0 = smem_desc_lo(sKV(0), 16);          // K-major
+            const uint32_t v_lo0 = smem_desc_lo(sKV(0), 16384);       // MN-major
+            auto issue_s = [&](int t, int s) {
+                if (leader) {
+                    const uint32_t a0 = q_lo[t], b0 = k_lo0 + s * (C::KV_BYTES >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint32_t off = ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
+                        mma_f16_ss_lohi(tmem + C::s_col(t), a0 + off, b0 + off, DESC_HI, IDESC_S, kk > 0);
+                    }
+                }
+            };
+            auto issue_pv = [&](int t, int s, bool accumulate, int kk_begin, int kk_end) {
+                if (leader) {
+                    const uint32_t b0 = v_lo0 + s * (C::KV_BYTES >> 4);
+#pragma unroll
+                    for (int kk = kk_begin; kk < kk_end; ++kk)
+                        mma_f16_ts_lohi(tmem + C::o_col(t), tmem + C::s_col(t) + kk * 8, b0 + ((kk * 16 * 128) >> 4), DESC_HI, IDESC_O,
+                                        (accumulate || kk > 0) ? 1u : 0u);
+                }
+            };
+            auto commit = [&](int b) {
+                if (leader) mma_commit(bar(b));
+            };
+            int kv_base = 0, it_base[2] = {0, 0}, uses[2] = {0, 0};
+            bool ok = true;
+            for (int k = 0; ok; ++k) {
+                Item it;
+                if (!next_item(k, leader, it)) break;
+                // V rows that hold no key become zeros (the ring's slot is this warp's until it commits the products that read it)
+                auto clear_v = [&](int j, int slot) {
+                    const int valid = it.len - (it.tile0 + j) * 128;
+                    const volatile uint32_t* bad = bad_ring + ((kv_base + j) & 7) * 8;
+                    const bool some_bad = bad[0] != 0;
+                    if (valid >= 128 && !some_bad) return;
+                    uint8_t* v = smem_gen + 2 * C::Q_BYTES + slot * C::KV_BYTES;
+                    const int from = some_bad ? 0 : (valid < 0 ? 0 : valid);
+                    for (int e = lane; e < (128 - from) * 8; e += 32) {
+                        const int row = from + (e >> 3);
+                        if (row >= valid || ((bad[1 + (row >> 5)] >> (row & 31)) & 1)) {
+#pragma unroll
+                            for (int pl = 0; pl < NBOX; ++pl)
+                                *reinterpret_cast<uint4*>(v + pl * 16384 + row * 128 + (e & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        }
+                    }
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                };
+                ok = wait(B_KVFULL + kv_base % NGRP, (kv_base / NGRP) & 1);
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (ok && it.n(t) > 0) {
+                        ok = wait(B_QFULL + t, uses[t] & 1);
+                        if (ok) {
+                            tc_fence_after_sync();
+                            issue_s(t, 2 * (kv_base % NGRP) + 1);
+                            commit(B_SFULL + t);
+                            if (it.n(t) == 1) commit(B_QEMPTY + t);
+                        }
+                    }
+                }
+                if (ok) commit(B_KVEMPTY + kv_base % NGRP);
+                for (int j = 0; j < it.n_max && ok; ++j) {
+                    const int grp = kv_base + j + 1, gslot = grp % NGRP;
+                    if (!(ok = wait(B_KVFULL + gslot, (grp / NGRP) & 1))) break;
+                    clear_v(j, 2 * gslot);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        if (j < it.n(t)) {
+                            const uint32_t par = (it_base[t] + j) & 1;
+                            if (!(ok = wait(B_PFULL + t, par))) break;
+                            // the previous item's O_t must be in registers before it is overwritten
+                            if (j == 0 && uses[t] > 0 && !(ok = wait(B_OFREE + t, (uses[t] - 1) & 1))) break;
+                            tc_fence_after_sync();
+                            issue_pv(t, 2 * gslot, j > 0, 0, 6);
+                            if (!(ok = wait(B_PFULL2 + t, par))) break;
+                            tc_fence_after_sync();
+                            issue_pv(t, 2 * gslot, true, 6, 8);
+                            if (j + 1 == it.n(t)) commit(B_OFINAL + t);
+                        }
+                        if (j + 1 < it.n(t)) {
+                            issue_s(t, 2 * gslot + 1);
+                            commit(B_SFULL + t);
+                            if (j + 2 == it.n(t)) commit(B_QEMPTY + t);
+                        }
+                    }
+                    if (ok) commit(B_KVEMPTY + gslot);
+                }
+                kv_base += it.n_max + 1;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    it_base[t] += it.n(t) > 0 ? it.n(t) : 0;
+                    uses[t] += it.n(t) > 0 ? 1 : 0;
+                }
+            }
+        } else if (!PREFIX && warp == 10 && blockIdx.x == 0) {
+            // lengths that are out of range (of a prefix call the second kernel reports them)
+            for (int u = lane; u < p.units; u += 32) {
+                const int len = __ldg(p.seq_lens + u), new_tokens = __ldg(p.starts + u + 1) - __ldg(p.starts + u);
+                if (len > p.max_len || (len > 0 && new_tokens > len)) report_bad_index(p.status);
+            }
+        }
+    } else {
+        // =========================== softmax groups ===========================
+        reg_inc_softmax();
+        const int t = warp >> 2, r = tid & 127, w4 = warp & 3;
+        const uint32_t lane_off = static_cast<uint32_t>(w4 * 32) << 16;
+        const uint32_t tS = tmem + C::s_col(t) + lane_off, tO = tmem + C::o_col(t) + lane_off;
+        const float c = p.scale_log2;
+        const int my_token = t * p.tile_tokens + r / p.group, my_head = r % p.group;     // of the pair; of the K/V head
+        const uint32_t ost = sOst(t) + w4 * 4096;                                        // this warp's staging: 32 rows x 128 bytes
+        int it_base = 0, uses = 0, kv_base = 0;
+        bool ok = true;
+        for (int k = 0; ok; ++k) {
+            Item it;
+            if (!next_item(k, lane == 0, it)) break;
+            const int n = it.n(t), group0 = kv_base;
+            kv_base += it.n_max + 1;
+            if (n <= 0) continue;
+            const bool live = r < tile_rows && my_token < it.n_tok;
+            // last key that this row sees; rows without a token ask for no mask
+            int lim = 0;
+            if (live) {
+                if constexpr (PREFIX) {
+                    const int len = __ldg(p.seq_lens + it.tok + my_token);
+                    lim = (len < it.len ? len : it.len) - 1;
+                } else {
+                    lim = it.base + my_token;
+                }
+            }
+            const int lim_lo = __reduce_min_sync(0xffffffffu, live ? lim : 2147483647);
+            const int lim_hi = __reduce_max_sync(0xffffffffu, live ? lim : -2147483647);
+            if (!live) lim = 2147483647;
+            const bool any_live = lim_hi > -2147483647;
+            float m = 0.f, l = 0.f;
+            bool unset = live, any_unset = any_live;       // the reference maximum is taken from the first tile that shows the row a key
+
+            for (int j = 0; j < n; ++j) {
+                if (!(ok = wait(B_SFULL + t, (it_base + j) & 1))) break;
+                tc_fence_after_sync();
+                if (!any_live) {                           // no row of this warp is a query's: whatever S holds may stand in as P
+                    mbar_arrive(bar(B_PFULL + t));
+                    mbar_arrive(bar(B_PFULL2 + t));
+                    continue;
+                }
+                const int kv0 = (it.tile0 + j) * 128;
+                const volatile uint32_t* bad = bad_ring + ((group0 + j) & 7) * 8;
+                const bool some_bad = bad[0] != 0;
+                if (kv0 + 127 > lim_lo || some_bad) {
+                    // hidden scores become -inf in tensor memory, so that masked tiles run the code of all others
+#pragma unroll 1
+                    for (int ch = 0; ch < 4; ++ch) {
+                        const int a = kv0 + 32 * ch;
+                        const uint32_t ok_keys = some_bad ? ~bad[1 + ch] : 0xffffffffu;
+                        if (a + 31 <= lim_lo && ok_keys == 0xffffffffu) continue;
+                        uint32_t tmp[32];
+                        if (a > lim_hi || ok_keys == 0u) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) tmp[e] = 0xff800000u;
+                        } else {
+                            tmem_ld_32x32b_x32(tS + ch * 32, tmp);
+                            tmem_ld_wait();
+                            const uint32_t seen = low_bits(lim > a + 31 ? 32 : lim - a + 1) & ok_keys;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!(seen & (1u << e))) tmp[e] = 0xff800000u;
+                        }
+                        tmem_st_32x32b_x32(tS + ch * 32, tmp);
+                    }
+                    tmem_st_wait();
+                }
+                uint32_t sr[128];
+#pragma unroll
+                for (int ch = 0; ch < 4; ++ch) tmem_ld_32x32b_x32(tS + ch * 32, sr + ch * 32);
+                tmem_ld_wait();
+                auto max_of = [&](float* mx, int e0, int e1) {
+#pragma unroll
+                    for (int e = e0; e < e1; e += 16)
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) mx[x] = max3(mx[x], __uint_as_float(sr[e + 2 * x]), __uint_as_float(sr[e + 2 * x + 1]));
+                };
+                auto max8 = [&](const float* mx) {
+                    return fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7])));
+                };
+                if (any_unset) {
+                    float mx[8];
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) mx[x] = -INFINITY;
+                    max_of(mx, 0, 128);
+                    const float top = max8(mx);
+                    if (unset && top != -INFINITY) {
+                        m = top;
+                        unset = false;
+                    }
+                    any_unset = __any_sync(0xffffffffu, unset);
+                }
+                // Exponentials against the reference maximum of the tiles before, this tile's maximum on the side; once more with a
+                // new reference where a row has grown by more than 2^LAG.
+                float alpha = 1.f;
+#pragma unroll 1
+                for (bool again = false;; again = true) {
+                    const float nmc = -m * c;
+                    const uint64_t c2 = pack_f32x2(c, c), nmc2 = pack_f32x2(nmc, nmc);
+                    uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
+                    float mx[8];
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) mx[x] = -INFINITY;
+                    auto exp_chunk = [&](int ch) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            float x0, x1;
+                            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(sr[ch * 32 + e]), __uint_as_float(sr[ch * 32 + e + 1])), c2, nmc2), x0, x1);
+                            const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+                            acc[(e / 2) & 3] = add_f32x2(acc[(e / 2) & 3], pack_f32x2(p0, p1));
+                            pk[e / 2] = pack2<DTYPE>(p0, p1);
+                        }
+                        tmem_st_32x32b_x16(tS + ch * 16, pk);
+                    };
+#pragma unroll
+                    for (int ch = 0; ch < 3; ++ch) {
+                        exp_chunk(ch);
+                        max_of(mx, ch == 0 ? 0 : (ch == 1 ? 48 : 96), ch == 0 ? 48 : (ch == 1 ? 96 : 128));
+                    }
+                    if (!again) {
+                        const float top = max8(mx);
+                        const bool ahead = live && (top - m) * c > LAG;
+                        if (__any_sync(0xffffffffu, ahead)) {
+                            if (ahead) {
+                                alpha = ex2_approx((m - top) * c);
+                                m = top;
+                            }
+                            // (the last update of O finished before S was produced)
+                            if (j > 0) {
+#pragma unroll 1
+                                for (int ch = 0; ch < D / 32; ++ch) {
+                                    uint32_t orr[32];
+                                    tmem_ld_32x32b_x32(tO + ch * 32, orr);
+                                    tmem_ld_wait();
+#pragma unroll
+                                    for (int e = 0; e < 32; ++e) orr[e] = __float_as_uint(__uint_as_float(orr[e]) * alpha);
+                                    tmem_st_32x32b_x32(tO + ch * 32, orr);
+                                }
+                            }
+                            continue;
+                        }
+                    }
+                    tmem_st_wait();
+                    tc_fence_before_sync();
+                    mbar_arrive(bar(B_PFULL + t));         // first three quarters of P are in place
+                    exp_chunk(3);
+                    float a0, a1, a2, a3;
+                    unpack_f32x2(add_f32x2(acc[0], acc[1]), a0, a1);
+                    unpack_f32x2(add_f32x2(acc[2], acc[3]), a2, a3);
+                    l = l * alpha + ((a0 + a1) + (a2 + a3));
+                    break;
+                }
+                tmem_st_wait();
+                tc_fence_before_sync();
+                mbar_arrive(bar(B_PFULL2 + t));
+            }
+            if (!ok) break;
+            it_base += n;
+
+            // ---- epilogue: through this warp's part of the staging tile, so that rows leave in whole lines ----
+            if (!(ok = wait(B_OFINAL + t, uses & 1))) break;
+            ++uses;
+            tc_fence_after_sync();
+            const bool final_rows = !PREFIX && it.slot < 0;
+            const bool seen = l > 0.f;                     // false: no visible key in this share
+            const float inv = final_rows ? (seen ? 1.f / l : 0.f) : 1.f;
+            // row of [tokens][H] that each of this warp's rows is, from the lane that has the row
+            const int64_t out_row = static_cast<int64_t>(it.tok + my_token) * p.H + it.kvh * p.group + my_head;
+            float* part = p.parts + it.slot * part_floats(D) + (t * 128 + w4 * 32) * D;
+            if (live) {
+                if (final_rows) {
+                    p.lse[out_row] = seen ? fmaf(m, p.scale, logf(l)) : -INFINITY;
+                } else {
+                    float2* ml = reinterpret_cast<float2*>(it.slot < 0 ? p.rows + static_cast<int64_t>(p.tokens) * p.H * D + 2 * out_row
+                                                                       : p.parts + it.slot * part_floats(D) + kRows * D + 2 * (t * 128 + r));
+                    *ml = make_float2(fmaf(m, c, P_OFF), l);
+                }
+            }
+            // 32 rows of 128 bytes: a quarter of a warp per row
+            auto leave = [&](int round, const uint32_t (&v)[32]) {
+                __syncwarp();
+#pragma unroll
+                for (int g = 0; g < 8; ++g)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ost + lane * 128 + ((g ^ (lane & 7)) << 4)), "r"(v[4 * g]), "r"(v[4 * g + 1]),
+                                 "r"(v[4 * g + 2]), "r"(v[4 * g + 3])
+                                 : "memory");
+                __syncwarp();
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    const int row = 4 * x + (lane >> 3), g = lane & 7;
+                    const int64_t to = __shfl_sync(0xffffffffu, out_row, row);
+                    const bool write = __shfl_sync(0xffffffffu, live ? 1 : 0, row) != 0;
+                    const uint4 w = attn_paged::lds128(ost + row * 128 + ((g ^ (row & 7)) << 4));
+                    if (write) {
+                        uint8_t* dst;
+                        if (final_rows)
+                            dst = static_cast<uint8_t*>(p.o) + to * (2 * D);
+                        else if (it.slot < 0)
+                            dst = reinterpret_cast<uint8_t*>(p.rows + to * D);
+                        else
+                            dst = reinterpret_cast<uint8_t*>(part + row * D);
+                        *reinterpret_cast<uint4*>(dst + round * 128 + g * 16) = w;
+                    }
+                }
+            };
+            if (final_rows) {
+#pragma unroll 1
+                for (int h = 0; h < D / 64; ++h) {
+                    uint32_t orr[64], v[32];
+                    tmem_ld_32x32b_x32(tO + h * 64, orr);
+                    tmem_ld_32x32b_x32(tO + h * 64 + 32, orr + 32);
+                    tmem_ld_wait();
+                    if (h == D / 64 - 1) {
+                        tc_fence_before_sync();
+                        mbar_arrive(bar(B_OFREE + t));
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] = pack2<DTYPE>(__uint_as_float(orr[2 * e]) * inv, __uint_as_float(orr[2 * e + 1]) * inv);
+                    leave(h, v);
+                }
+            } else {
+#pragma unroll 1
+                for (int h = 0; h < D / 32; ++h) {
+                    uint32_t v[32];
+                    tmem_ld_32x32b_x32(tO + h * 32, v);
+                    tmem_ld_wait();
+                    if (h == D / 32 - 1) {
+                        tc_fence_before_sync();
+                        mbar_arrive(bar(B_OFREE + t));
+                    }
+                    leave(h, v);
+                }
+            }
+        }
+    }
+
+    // ---- teardown (also reached after a timed-out wait) ----
+    tc_fence_before_sync();
+    __syncthreads();
+    if (tid == 0 && *abort_flag != 0) attn_tc::report_timeout(p.status);
+    __syncthreads();
+    if (warp == 8) tmem_dealloc(tmem, C::TMEM_COLS);
+}
+
+// Joins the partial results of prefill lists that were cut: block (c, y) takes rows of the list whose first border is the one
+// between CTAs c and c + 1.  A warp per row.
+template <int D, int DTYPE>
+__global__ void __launch_bounds__(attn_paged::kJoinWarps * 32)
+attn_paged_prefill_join_kernel(const __grid_constant__ Params p) {
+    constexpr float P_OFF = attn_paged::ExpRange<DTYPE>::P_OFF;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c0 = blockIdx.x;
+    int64_t mine, before;
+    const int64_t total = Walk<false>::total(p, lane, mine, before);
+    const int ctas = cta_count(total, p.grid);
+    Walk<false> walk;
+    const int64_t border = cta_begin(total, c0 + 1, ctas);
+    bool work = c0 + 1 < ctas;
+    if (work) {
+        walk.find(p, lane, border, mine, before);
+        // a border between two lists cuts none; of several borders in one list the first one's block joins it
+        work = walk.step > 0 && border - walk.step >= cta_begin(total, c0, ctas);
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (!work) return;
+    const int64_t start = border - walk.step;
+    const int pair_tok = walk.i * 2 * p.tile_tokens;
+    for (int row = blockIdx.y * attn_paged::kJoinWarps + warp; row < kRows; row += gridDim.y * attn_paged::kJoinWarps) {
+        const int t = row >> 7, r = row & 127, token = t * p.tile_tokens + r / p.group;
+        if (r >= p.tile_tokens * p.group || pair_tok + token >= walk.unit.n) continue;
+        const int64_t end = start + walk.unit.steps_of(pair_tok + (t + 1) * p.tile_tokens);        // of this tile
+        const int n = cta_of_tile(total, end - 1, ctas) - c0 + 1;
+        const int64_t out_row = static_cast<int64_t>(walk.unit.tok0 + pair_tok + token) * p.H + walk.h * p.group + r % p.group;
+        // the list is the last of c0's part, and the first of the others'
+        auto part = [&](int i) { return p.parts + (2 * (c0 + i) + (i == 0 ? 1 : 0)) * part_floats(D); };
+        attn_paged::join_row<D, DTYPE>(n, lane, P_OFF, [&](int i) { return reinterpret_cast<const float2*>(part(i) + kRows * D) + row; },
+                                       [&](int i) { return part(i) + row * D; }, static_cast<uint8_t*>(p.o) + out_row * (2 * D), p.lse + out_row);
+    }
+}
+
+// Joins what the two kernels of a call with shared prefixes have left for each row: the parts of its sequence's own keys
+// (attn_paged.cuh) and those of the prefix.  A warp per row, eight rows of one sequence to a block, as in attn_paged_join_kernel.
+template <int D, int DTYPE, int GH>
+__global__ void __launch_bounds__(attn_paged::kJoinWarps * 32)
+attn_paged_prefix_join_kernel(const __grid_constant__ attn_paged::DecodeParams p, const __grid_constant__ Params pre, int blocks_per_seq) {
+    using C = attn_paged::DecodeCfg<D, GH>;
+    constexpr float P_OFF = attn_paged::ExpRange<DTYPE>::P_OFF;
+    __shared__ int64_t red[4][attn_paged::kJoinWarps];
+    const int b = blockIdx.x / blocks_per_seq, lane = threadIdx.x & 31;
+    const int q_head = (blockIdx.x - b * blocks_per_seq) * attn_paged::kJoinWarps + (threadIdx.x >> 5);
+    const attn_paged::JoinList<D, GH, true> list(p, b, red);
+    // where the prefix's parts lie: the steps in front of the group's, then those of the row's list
+    int64_t mine, before;
+    const int64_t total = Walk<true>::total(pre, lane, mine, before);
+    const int ctas = cta_count(total, pre.grid), g = attn_paged::group_of(pre.starts, pre.units, b);
+    const int64_t out_row = static_cast<int64_t>(b) * p.H + q_head;
+    int n_pre = 0, c0 = 0, c1 = 0, row = 0;
+    if (g >= 0 && q_head < p.H) {
+        const int per = (pre.units + 31) / 32;
+        int64_t start = __shfl_sync(0xffffffffu, before, g / per);
+        Unit<true> unit;
+        for (int x = g / per * per; x < g; ++x) {
+            unit.load(pre, x);
+            start += pre.Hkv * unit.head_steps(pre);
+        }
+        unit.load(pre, g);
+        const int token = b - unit.tok0, pair = token / (2 * pre.tile_tokens), in_pair = token - pair * 2 * pre.tile_tokens;
+        if (token >= 0 && token < unit.n) {
+            const int kvh = q_head / pre.group, t = in_pair >= pre.tile_tokens ? 1 : 0;
+            row = t * 128 + (in_pair - t * pre.tile_tokens) * pre.group + q_head - kvh * pre.group;
+            start += kvh * unit.head_steps(pre) + unit.steps_before(pre, pair);
+            const int64_t end = start + unit.pair_steps(pre, pair);
+            if (end <= total) {
+                c0 = cta_of_tile(total, start, ctas);
+                c1 = cta_of_tile(total, end - 1, ctas);
+                n_pre = c1 - c0 + 1;
+            }
+        }
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (q_head >= p.H) return;
+    uint8_t* out = static_cast<uint8_t*>(p.o) + out_row * D * 2;
+    const int64_t n_rows = static_cast<int64_t>(p.B) * p.H;
+    attn_paged::RowParts own;
+    if (list.n > 0) own.find(p, list, q_head);
+    const int n_own = own.count;
+    if (n_own + n_pre == 0) {
+        attn_paged::empty_row<D>(out, p.lse + out_row, lane);
+        return;
+    }
+    auto own_part = [&](int i) { return own.at<C::PART_FLOATS>(p, i); };
+    auto pre_part = [&](int i) { return pre.parts + (2 * (c0 + i) + (i == 0 ? 1 : 0)) * part_floats(D); };
+    attn_paged::join_row<D, DTYPE>(
+        n_own + n_pre, lane, P_OFF,
+        [&](int i) {
+            const float* at = i < n_own ? (n_own == 1 ? p.rows + n_rows * D + 2 * out_row : own_part(i) + GH * D + 2 * own.row)
+                                        : (n_pre == 1 ? pre.rows + n_rows * D + 2 * out_row : pre_part(i - n_own) + kRows * D + 2 * row);
+            return reinterpret_cast<const float2*>(at);
+        },
+        [&](int i) {
+            return i < n_own ? (n_own == 1 ? p.rows + out_row * D : own_part(i) + own.row * D)
+                             : (n_pre == 1 ? pre.rows + out_row * D : pre_part(i - n_own) + row * D);
+        },
+        out, p.lse + out_row);
+}
+
+}  // namespace attn_paged_tc

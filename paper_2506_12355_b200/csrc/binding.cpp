@@ -30,6 +30,10 @@ struct Entries {
     decltype(&attn_qk_norm_rope_axes) norm_rope_axes;
     decltype(&attn_qk_norm_rope_axes_bwd) norm_rope_axes_bwd;
     decltype(&attn_paged_append_axes) append_axes;
+    decltype(&attn_paged_prefill) prefill;
+    decltype(&attn_paged_prefill_workspace_bytes) prefill_bytes;
+    decltype(&attn_paged_prefix_decode) prefix_decode;
+    decltype(&attn_paged_prefix_decode_workspace_bytes) prefix_decode_bytes;
 } fn = {};
 
 using at::Tensor;
@@ -347,6 +351,43 @@ PyObject* decode(PyObject* const* a) {
     return rc ? status(rc) : tuple({&o, &lse});
 }
 
+// attn_paged_prefill(q, k_cache, v_cache, block_table, seq_lens, cu_seqlens, scale, out, lse, workspace)
+PyObject* prefill(PyObject* const* a) {
+    const Tensor &q = required(a[0]), &cu = required(a[5]);
+    need(q.dim() == 3);
+    const int64_t T = q.size(0), H = q.size(1), D = q.size(2);
+    const Call c(q);
+    c.check(q, q.sizes(), true);
+    const Cache m(c, D, a[1], a[2], a[3], a[4]);
+    c.check(cu, {m.n + 1}, at::kInt, true);
+    const Tensor o = c.output(tensor(a[7]), {T, H, D}), lse = c.output(tensor(a[8]), {T, H}, at::kFloat);
+    const Tensor ws = c.workspace(tensor(a[9]), fn.prefill_bytes(small(D)));
+    const int rc = fn.prefill(q.data_ptr(), m.k.data_ptr(), m.v.data_ptr(), m.strides, m.pages, m.page_size, m.table.data_ptr<int>(),
+                              m.table.stride(0), m.width, m.lens.data_ptr<int>(), cu.data_ptr<int>(), o.data_ptr(), lse.data_ptr<float>(), m.n,
+                              small(T), small(H), m.heads, small(D), number(a[6]), c.dtype, ws.data_ptr(), ws.nbytes(), c.stream);
+    return rc ? status(rc) : tuple({&o, &lse});
+}
+
+// attn_paged_prefix_decode(q, k_cache, v_cache, block_table, seq_lens, group_starts, prefix_lens, scale, out, lse, workspace)
+PyObject* prefix_decode(PyObject* const* a) {
+    const Tensor &q = required(a[0]), &starts = required(a[5]), &lens = required(a[6]);
+    need(q.dim() == 3 && lens.dim() == 1);
+    const int64_t B = q.size(0), H = q.size(1), D = q.size(2), groups = lens.size(0);
+    const Call c(q);
+    c.check(q, q.sizes(), true);
+    const Cache m(c, D, a[1], a[2], a[3], a[4]);
+    need(m.n == B);
+    c.check(lens, lens.sizes(), at::kInt, true);
+    c.check(starts, {groups + 1}, at::kInt, true);
+    const Tensor o = c.output(tensor(a[8]), {B, H, D}), lse = c.output(tensor(a[9]), {B, H}, at::kFloat);
+    const Tensor ws = c.workspace(tensor(a[10]), fn.prefix_decode_bytes(small(B), small(H), m.heads, small(D)));
+    const int rc = fn.prefix_decode(q.data_ptr(), m.k.data_ptr(), m.v.data_ptr(), m.strides, m.pages, m.page_size, m.table.data_ptr<int>(),
+                                    m.table.stride(0), m.width, m.lens.data_ptr<int>(), starts.data_ptr<int>(), lens.data_ptr<int>(),
+                                    small(groups), o.data_ptr(), lse.data_ptr<float>(), small(B), small(H), m.heads, small(D), number(a[7]),
+                                    c.dtype, ws.data_ptr(), ws.nbytes(), c.stream);
+    return rc ? status(rc) : tuple({&o, &lse});
+}
+
 struct Heads {
     int64_t B, H, Hkv, Sq, Sk, D;
     Heads(const Call& c, const Tensor& q, const Tensor& k, const Tensor& v) {
@@ -432,6 +473,8 @@ PyMethodDef methods[] = {
     {"attn_qk_norm_rope_axes", fast<norm_rope<true>, 13>(), METH_FASTCALL, nullptr},
     {"attn_qk_norm_rope_axes_bwd", fast<norm_rope_bwd<true>, 16>(), METH_FASTCALL, nullptr},
     {"attn_paged_append_axes", fast<append<true>, 16>(), METH_FASTCALL, nullptr},
+    {"attn_paged_prefill", fast<prefill, 10>(), METH_FASTCALL, nullptr},
+    {"attn_paged_prefix_decode", fast<prefix_decode, 11>(), METH_FASTCALL, nullptr},
     {"attn_paged_decode", fast<decode, 11>(), METH_FASTCALL, nullptr},
     {"attn_fwd_window", fast<fwd_window, 9>(), METH_FASTCALL, nullptr},
     {"attn_bwd_window", fast<bwd_window, 14>(), METH_FASTCALL, nullptr},

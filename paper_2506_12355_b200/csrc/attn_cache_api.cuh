@@ -556,7 +556,21 @@ bool decode_maps(CUtensorMap* mk, CUtensorMap* mv, attn_paged::DecodeParams& p, 
 }
 
 // Partial results of attn_paged_tc.cuh: two per CTA.
-size_t tc_part_bytes(int D) { return static_cast<size_t>(2) * attn_paged::kMaxCtas * attn_paged_tc::part_floats(D) * sizeof(float); }
+size_t tc_part_bytes(int D) { return align256(static_cast<size_t>(2) * attn_paged::kMaxCtas * attn_paged_tc::part_floats(D) * sizeof(float)); }
+
+// What lies where in the workspace of a call with shared prefixes; the decode kernel's partial results come first.
+struct PrefixWorkspace { size_t rows, plan, prefix_rows, prefix_plan, prefix_parts, bytes; };
+PrefixWorkspace prefix_workspace(int B, int H, int Hkv, int D) {
+    const size_t rows = align256(static_cast<size_t>(B) * H * (D + 2) * sizeof(float));
+    PrefixWorkspace w;
+    w.rows = decode_bytes(H, Hkv, D);
+    w.plan = w.rows + rows;
+    w.prefix_rows = w.plan + align256((static_cast<size_t>(B) + 1) * 2 * sizeof(int64_t));
+    w.prefix_plan = w.prefix_rows + rows;
+    w.prefix_parts = w.prefix_plan + align256((static_cast<size_t>(B) + 1) * sizeof(attn_paged_tc::PrefixPlan));
+    w.bytes = w.prefix_parts + tc_part_bytes(D);
+    return w;
+}
 
 #ifdef ATTN_TEST_HOOKS
 int g_test_skip_group = -1;
@@ -794,7 +808,7 @@ int attn_paged_decode(const void* q, const void* k_cache, const void* v_cache, c
     return ATTN_ERR_UNSUPPORTED_DTYPE;
 }
 
-size_t attn_paged_prefill_workspace_bytes(int D) { return D == 64 || D == 128 ? align256(tc_part_bytes(D)) : 0; }
+size_t attn_paged_prefill_workspace_bytes(int D) { return D == 64 || D == 128 ? tc_part_bytes(D) + align256(attn_paged::kMaxCtas * sizeof(attn_paged_tc::Cut)) : 0; }
 
 int attn_paged_prefill(const void* q, const void* k_cache, const void* v_cache, const long long* cache_strides, int num_pages,
                        int page_size, const int* block_table, long long table_stride, int max_pages, const int* seq_lens,
@@ -822,12 +836,13 @@ int attn_paged_prefill(const void* q, const void* k_cache, const void* v_cache, 
     p.o = o;
     p.lse = lse;
     p.parts = static_cast<float*>(workspace);
+    p.cuts = reinterpret_cast<attn_paged_tc::Cut*>(static_cast<uint8_t*>(workspace) + tc_part_bytes(D));
 #define ATTN_PREFILL_CASE(DD, TT)                                                                                              \
     if (D == DD && dtype == TT) {                                                                                              \
         if (!launch_paged_tc<DD, TT, false>(p, q, k_cache, v_cache, cache_strides, num_pages, page_size, block_table, table_stride, max_pages, \
                                             seq_lens, cu_seqlens, n_seqs, tokens, H, Hkv, scale, di.sm_count, st))              \
             return ATTN_ERR_CUDA;                                                                                              \
-        return launch_dependent(attn_paged_tc::attn_paged_prefill_join_kernel<DD, TT>, dim3(static_cast<unsigned>(p.grid - 1), 8), \
+        return launch_dependent(attn_paged_tc::attn_paged_prefill_join_kernel<DD, TT>, dim3(static_cast<unsigned>(p.grid - 1), attn_paged_tc::kRows / attn_paged::kJoinWarps), \
                                 dim3(attn_paged::kJoinWarps * 32), 0, st, p)                                                   \
                    ? ATTN_OK                                                                                                   \
                    : ATTN_ERR_CUDA;                                                                                            \
@@ -842,8 +857,7 @@ int attn_paged_prefill(const void* q, const void* k_cache, const void* v_cache, 
 
 size_t attn_paged_prefix_decode_workspace_bytes(int B, int H, int Hkv, int D) {
     if (B < 0 || (D != 64 && D != 128) || decode_bytes(H, Hkv, D) == 0) return 0;
-    // the decode kernel's partial results, both kernels' rows, and the other kernel's partial results
-    return decode_bytes(H, Hkv, D) + 2 * align256(static_cast<size_t>(B) * H * (D + 2) * sizeof(float)) + align256(tc_part_bytes(D));
+    return prefix_workspace(B, H, Hkv, D).bytes;
 }
 
 int attn_paged_prefix_decode(const void* q, const void* k_cache, const void* v_cache, const long long* cache_strides, int num_pages,
@@ -862,7 +876,11 @@ int attn_paged_prefix_decode(const void* q, const void* k_cache, const void* v_c
     if (rc != ATTN_OK) return rc;
     if (misaligned(group_starts, 4) || misaligned(prefix_lens, 4)) return ATTN_ERR_MISALIGNED;
     if (!workspace || misaligned(workspace, 256) || workspace_bytes < attn_paged_prefix_decode_workspace_bytes(B, H, Hkv, D)) return ATTN_ERR_WORKSPACE;
-    if (n_groups == 0 || num_pages == 0 || max_pages == 0)
+    // Few keys in all: attn_paged_decode reads the common ones for every sequence (out of L2) and is done before three kernels are.
+    // What the host knows is the width of the table.  8 heads of 128, device times: 4 sequences of 1100 keys 12 us against 26, 16 of
+    // 1200 (79 MB) 25 against 27, 8 of 4200 (138 MB) 35 against 31, 32 of 1200 (157 MB) 36 against 35.
+    const bool few = static_cast<int64_t>(B) * max_pages * page_size < (1LL << 27) / (static_cast<int64_t>(Hkv) * D * 4);
+    if (n_groups == 0 || num_pages == 0 || max_pages == 0 || few)
         return attn_paged_decode(q, k_cache, v_cache, cache_strides, num_pages, page_size, block_table, table_stride, max_pages, seq_lens, o, lse, B,
                                  H, Hkv, D, scale, 0, 0, dtype, workspace, workspace_bytes, stream);
     rc = check_arch();
@@ -871,24 +889,28 @@ int attn_paged_prefix_decode(const void* q, const void* k_cache, const void* v_c
     if (device_info(&di) != ATTN_OK) return ATTN_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    const size_t row_bytes = align256(static_cast<size_t>(B) * H * (D + 2) * sizeof(float));
+    const PrefixWorkspace at = prefix_workspace(B, H, Hkv, D);
     attn_paged::DecodeParams p = {};
     if (!decode_params(p, q, num_pages, page_size, block_table, table_stride, max_pages, seq_lens, o, lse, B, H, Hkv, D, scale, ws, di.sm_count))
         return ATTN_ERR_BAD_SHAPE;
     if (!p.status) return ATTN_ERR_CUDA;
-    ws += decode_bytes(H, Hkv, D);
-    p.rows = reinterpret_cast<float*>(ws);
+    p.rows = reinterpret_cast<float*>(ws + at.rows);
+    p.plan = reinterpret_cast<int64_t*>(ws + at.plan);
     p.group_starts = group_starts;
     p.prefix_lens = prefix_lens;
     p.n_groups = n_groups;
+    p.all_ctas = di.sm_count < attn_paged::kMaxCtas ? di.sm_count : attn_paged::kMaxCtas;
 #ifdef ATTN_TEST_HOOKS
     p.test_skip_step = g_test_skip_step;
     g_test_skip_step = -1;
 #endif
     attn_paged_tc::Params pre = {};
-    pre.rows = reinterpret_cast<float*>(ws + row_bytes);
-    pre.parts = reinterpret_cast<float*>(ws + 2 * row_bytes);
+    pre.rows = reinterpret_cast<float*>(ws + at.prefix_rows);
+    pre.parts = reinterpret_cast<float*>(ws + at.prefix_parts);
+    pre.plan = reinterpret_cast<attn_paged_tc::PrefixPlan*>(ws + at.prefix_plan);
     pre.prefix_lens = prefix_lens;
+    pre.row_bytes = Hkv * D * 4;
+    pre.head_groups = p.heads >> p.hpt_shift;
 #define ATTN_PREFIX_CASE(DD, TT, GG)                                                                                           \
     if (D == DD && dtype == TT && (p.group <= 8) == (GG == 8)) {                                                               \
         using C = attn_paged::DecodeCfg<DD, GG>;                                                                               \

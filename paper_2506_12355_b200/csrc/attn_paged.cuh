@@ -87,7 +87,8 @@ struct DecodeParams {
     // partial result
     const int* group_starts;    // [n_groups + 1]
     const int* prefix_lens;     // [n_groups]
-    int n_groups;
+    int n_groups, all_ctas;     // groups; CTAs that the two kernels share
+    int64_t* plan;              // [2 (B + 1)], for the joining kernel (SeqPlan)
     float* rows;                // O [B * H][D], then reference exponent and sum [B * H][2], of pairs that one CTA has to itself
     int cluster;                // > 0: a cluster of so many CTAs (a power of two up to kCluster) per (sequence, head), no second kernel
 };
@@ -111,6 +112,12 @@ __device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
     float2 v;
     asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
     return v;
+}
+
+__device__ __forceinline__ int64_t warp_sum(int64_t x) {
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+    return x;
 }
 
 // Visible chunks of CK keys of one sequence: n_sink of them from key 0, then those from chunk `lo`.
@@ -138,11 +145,38 @@ __device__ __forceinline__ int group_of(const int* starts, int n_groups, int b) 
 }
 
 // PREFIX: how many first keys of sequence b the other kernel takes.
-__device__ __forceinline__ int prefix_of(const DecodeParams& p, int b) {
-    const int g = group_of(p.group_starts, p.n_groups, b);
+__device__ __forceinline__ int prefix_of(const int* starts, const int* prefix_lens, const int* seq_lens, int n_groups, int max_len, int b) {
+    const int g = group_of(starts, n_groups, b);
     if (g < 0) return 0;
-    const int first = __ldg(p.group_starts + g);
-    return group_prefix(p.seq_lens, first < 0 ? 0 : first, __ldg(p.prefix_lens + g), p.max_len);
+    const int first = __ldg(starts + g);
+    return group_prefix(seq_lens, first < 0 ? 0 : first, __ldg(prefix_lens + g), max_len);
+}
+
+// The two kernels of a call with common prefixes run side by side, each on a part of the SMs (the second one's CTAs take the SMs that
+// the first one's surplus CTAs leave at once): the first is bound by its tensor-core pipeline's latencies, the second by memory.
+// Each works the parts out for itself from the lengths, in whole numbers, so both find the same.
+//
+// What a list of attn_paged_tc.cuh costs beside its steps (Q, first scores, the way out), in steps.  Its even cut counts it too.
+constexpr int kListCost = 3;
+// What a group's lists take of one CTA, in ns: a step of one tile, and by itself each list (its fill and way out, beside a busy memory).
+constexpr int kTileStepNs = 1100, kListNs = 8000;
+__device__ __forceinline__ int64_t group_cost(const int* starts, const int* prefix_lens, const int* seq_lens, int g, int B, int max_len, int Hkv,
+                                              int tile_tokens) {
+    int first = __ldg(starts + g), end = __ldg(starts + g + 1);
+    first = first < 0 ? 0 : (first > B ? B : first);
+    end = end < first ? first : (end > B ? B : end);
+    const int n = end - first, prefix = n > 0 ? group_prefix(seq_lens, first, __ldg(prefix_lens + g), max_len) : 0;
+    if (prefix <= 0) return 0;
+    const int pairs = (n + 2 * tile_tokens - 1) / (2 * tile_tokens);
+    return static_cast<int64_t>(Hkv) * pairs * (static_cast<int64_t>((prefix + 127) / 128) * (n > tile_tokens ? 2 * kTileStepNs : kTileStepNs) + kListNs);
+}
+// CTAs of the first kernel out of `grid`, for lists that take `cost` ns, and own_bytes of keys and values of `pairs` pairs of a sequence and
+// a group of heads for the second one.
+constexpr int kBytesPerNs = 40, kPairNs = 2500;      // a CTA's memory rate, and what a pair costs by itself
+__device__ __forceinline__ int prefix_ctas(int64_t cost, int64_t own_bytes, int64_t pairs, int grid) {
+    if (own_bytes <= 0) return grid;
+    const int64_t own = own_bytes / kBytesPerNs + pairs * kPairNs, n = (cost * grid + (cost + own) / 2) / (cost + own);
+    return cost <= 0 ? 0 : (n < 1 ? 1 : (n > grid - 1 ? grid - 1 : static_cast<int>(n)));
 }
 
 template <int CK, bool PREFIX>
@@ -152,7 +186,7 @@ __device__ __forceinline__ SeqRange seq_range(const DecodeParams& p, int b) {
     len = len < 0 ? 0 : (len > p.max_len ? p.max_len : len);
     r.len = len;
     if constexpr (PREFIX) {
-        const int prefix = prefix_of(p, b);
+        const int prefix = prefix_of(p.group_starts, p.prefix_lens, p.seq_lens, p.n_groups, p.max_len, b);
         r.win_lo = prefix < len ? prefix : len;
         r.lo = r.win_lo / CK;
         r.n_sink = 0;
@@ -187,6 +221,12 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, u
         : "memory");
 }
 
+// a / b for a >= 0, b > 0: the 64-bit division takes several times as long as the 32-bit one
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+    if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+    return a / b;
+}
+
 // CTA c of `ctas` takes the tiles [total * c / ctas, total * (c + 1) / ctas).  No more CTAs than tiles: none is empty, so
 // that a cut pair has a partial result from every CTA between its first and its last one.
 __device__ __forceinline__ int cta_count(int64_t total, int grid) { return total < grid ? static_cast<int>(total) : grid; }
@@ -198,24 +238,24 @@ __device__ __forceinline__ int cta_count(int64_t total, int grid) { return total
 // way).  So tiles side by side are taken when every CTA gets at least kLongList of them and a pair has about kFewParts parts
 // at most.
 constexpr int kLongList = 4, kFewParts = 10;
+// With common prefixes only what the prefix leaves of each sequence is in the list, often a few keys: every pair then costs more by
+// itself (2.7 us) than by its tiles, and heads side by side are an eighth as many (64 sequences of one key behind 8192 common ones:
+// 104 us with one head per pair, 36 side by side).
 struct ListForm { int64_t total; int hpt_shift; };
-__device__ __forceinline__ ListForm list_form(const DecodeParams& p, int64_t total_side, int64_t total_one) {
+template <bool PREFIX>
+__device__ __forceinline__ ListForm list_form(const DecodeParams& p, int64_t total_side, int64_t total_one, int grid) {
     const int groups = p.heads >> p.hpt_shift;
     total_side *= groups;
-    const bool side = total_side >= static_cast<int64_t>(kLongList) * p.grid && static_cast<int64_t>(p.B) * groups * kFewParts >= p.grid;
+    const bool few_parts = static_cast<int64_t>(p.B) * groups * kFewParts >= grid;
+    const bool side = (PREFIX || total_side >= static_cast<int64_t>(kLongList) * grid) && few_parts;
     if (p.hpt_shift == 0 || side) return {total_side, p.hpt_shift};
     return {total_one * p.heads, 0};
 }
-__device__ __forceinline__ int64_t cta_begin(int64_t total, int c, int ctas) { return total * c / ctas; }
+__device__ __forceinline__ int64_t cta_begin(int64_t total, int c, int ctas) { return divide(total * c, ctas); }
 __device__ __forceinline__ int cta_of_tile(int64_t total, int64_t t, int ctas) {
-    return static_cast<int>(((t + 1) * ctas - 1) / total);
+    return static_cast<int>(divide((t + 1) * ctas - 1, total));
 }
 
-__device__ __forceinline__ int64_t warp_sum(int64_t x) {
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
-    return x;
-}
 
 __device__ __forceinline__ uint4 lds128(uint32_t a) {
     uint4 v;
@@ -248,6 +288,24 @@ __device__ __forceinline__ void split2(float x0, float x1, uint32_t& hi, uint32_
     }
     lo = sm100::pack2<DTYPE>(x0 - h0, x1 - h1);
 }
+
+// PREFIX: what the joining kernel needs to know about a sequence's part of the list: left in the workspace by the decode kernel's first
+// CTA, [b]: {tiles in front of sequence b, tiles of one of its pairs}, behind the last sequence {tiles of the list, log2 of a tile's heads + 256 CTAs}.
+struct SeqPlan {
+    int64_t total, before;
+    int hs, groups, n, ctas;
+    static __device__ __forceinline__ SeqPlan read(const DecodeParams& p, int b) {
+        const longlong2 mine = __ldcg(reinterpret_cast<const longlong2*>(p.plan) + b), all = __ldcg(reinterpret_cast<const longlong2*>(p.plan) + p.B);
+        SeqPlan s;
+        s.total = all.x;
+        s.hs = static_cast<int>(all.y & 255);
+        s.groups = p.heads >> s.hs;
+        s.before = mine.x;
+        s.n = static_cast<int>(mine.y);
+        s.ctas = static_cast<int>(all.y >> 8);
+        return s;
+    }
+};
 
 // Position in the tile list, advanced tile by tile.  Every warp of a CTA walks the same tiles; kvh and r0 are its own.
 template <int NW, int CK, bool PREFIX>
@@ -340,8 +398,11 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     const int per = (p.B + C::THREADS - 1) / C::THREADS;     // consecutive sequences of a thread
     const int b0 = tid * per, b1 = b0 + per < p.B ? b0 + per : p.B;
     int64_t mine[2] = {0, 0};                                // tiles in either form of the list
+    int64_t own = 0, cost = 0, seqs = 0;                     // PREFIX: keys of this kernel and the sequences that have any; the other one's cost
     for (int b = b0; b < b1; ++b) {
         const SeqRange r = seq_range<CK, PREFIX>(p, b);
+        own += r.len - r.win_lo;
+        seqs += r.len > r.win_lo ? 1 : 0;
         mine[0] += seq_tiles<NW>(r, p.hpt_shift);
         mine[1] += seq_tiles<NW>(r, 0);
         if (p.seq_lens[b] > p.max_len && blockIdx.x == 0) report_bad_index(p.status);
@@ -358,7 +419,31 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         scan[warp] = incl[0];
         scan[16 + warp] = incl[1];
     }
+    int grid = p.grid;
+    if constexpr (PREFIX) {
+        for (int g = tid; g < p.n_groups; g += C::THREADS)
+            cost += group_cost(p.group_starts, p.prefix_lens, p.seq_lens, g, p.B, p.max_len, p.Hkv, 128 / p.group);
+        own = warp_sum(own);
+        cost = warp_sum(cost);
+        seqs = warp_sum(seqs);
+        if (lane == 0) {
+            scan[40 + warp] = own;
+            scan[48 + warp] = cost;
+            scan[56 + warp] = seqs;
+        }
+    }
     __syncthreads();
+    if constexpr (PREFIX) {
+        own = cost = seqs = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            own += scan[40 + w];
+            cost += scan[48 + w];
+            seqs += scan[56 + w];
+        }
+        grid = p.all_ctas - prefix_ctas(cost, own * (p.Hkv * D * 4), seqs * (p.heads >> p.hpt_shift), p.all_ctas);
+        grid = grid < p.grid ? grid : p.grid;
+    }
     int64_t before2[2] = {incl[0] - mine[0], incl[1] - mine[1]}, total2[2] = {0, 0};
 #pragma unroll
     for (int w = 0; w < NW; ++w)
@@ -367,13 +452,23 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
             if (w < warp) before2[f] += scan[16 * f + w];
             total2[f] += scan[16 * f + w];
         }
-    const ListForm form = list_form(p, total2[0], total2[1]);
+    const ListForm form = list_form<PREFIX>(p, total2[0], total2[1], grid);
     const int64_t total = form.total;
     hs = form.hpt_shift;
     groups = p.heads >> hs;
     const bool side = hs == p.hpt_shift;
     const int64_t before = side ? before2[0] : before2[1], my_tiles = side ? mine[0] : mine[1];
-    const int ctas = cta_count(total, p.grid);
+    const int ctas = cta_count(total, grid);
+    if (PREFIX && blockIdx.x == 0) {
+        longlong2* plan = reinterpret_cast<longlong2*>(p.plan);
+        int64_t at = before;
+        for (int b = b0; b < b1; ++b) {
+            const int n = seq_tiles<NW>(seq_range<CK, PREFIX>(p, b), hs);
+            plan[b] = make_longlong2(at, n);
+            at += n;
+        }
+        if (tid == 0) plan[p.B] = make_longlong2(total, hs | static_cast<int64_t>(ctas) << 8);
+    }
     if (static_cast<int>(blockIdx.x) >= ctas) {
         if (PREFIX) asm volatile("griddepcontrol.wait;" ::: "memory");
         return;
@@ -822,9 +917,24 @@ __device__ __forceinline__ void join_row(int np, int lane, float p_off, MlOf ml_
 #pragma unroll
     for (int k = 0; k < PER; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
     const int team = TEAMS > 1 ? lane / COLS : 0, col = TEAMS > 1 ? lane % COLS : lane;
+    constexpr int BATCH = PER > 1 ? 4 : 8;                 // rows of a lane in flight
     for (int i0 = 0; i0 < np; i0 += 32) {
+        const int m = np - i0 < 32 ? np - i0 : 32;
         float2 ml = make_float2(-INFINITY, 0.f);
-        if (i0 + lane < np) ml = __ldcg(ml_of(i0 + lane));
+        if (lane < m) ml = __ldcg(ml_of(i0 + lane));
+        float4 v[BATCH][PER];
+        auto load = [&](int x0) {
+#pragma unroll
+            for (int x = 0; x < BATCH; ++x) {
+                const int i = x0 + x * TEAMS;
+                if (i >= m) break;
+                const int mine = i + team < m ? i + team : m - 1;            // (a weight of 0 below for the repeated one)
+                const float4* src = reinterpret_cast<const float4*>(row_of(i0 + mine));
+#pragma unroll
+                for (int k = 0; k < PER; ++k) v[x][k] = __ldcg(src + col + 32 * k);
+            }
+        };
+        load(0);                                           // on their way while the weights are worked out
         float mx = ml.y != 0.f ? ml.x : -INFINITY;
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
@@ -838,22 +948,22 @@ __device__ __forceinline__ void join_row(int np, int lane, float p_off, MlOf ml_
         mm = mn;
 #pragma unroll
         for (int k = 0; k < PER; ++k) { o[k].x *= keep; o[k].y *= keep; o[k].z *= keep; o[k].w *= keep; }
-        const int m = np - i0 < 32 ? np - i0 : 32;
-#pragma unroll 4
-        for (int i = 0; i < m; i += TEAMS) {
-            const int mine = i + team < m ? i + team : m - 1;                // (a weight of 0 below for the repeated one)
-            float w = __shfl_sync(0xffffffffu, f, mine);
-            if (i + team >= m) w = 0.f;
-            const float4* src = reinterpret_cast<const float4*>(row_of(i0 + mine));
+        for (int x0 = 0; x0 < m; x0 += BATCH * TEAMS) {
+            if (x0 > 0) load(x0);
 #pragma unroll
-            for (int k = 0; k < PER; ++k) {
-                const float4 v = __ldcg(src + col + 32 * k);
-                if (w != 0.f) {     // a part without a visible key adds nothing
-                    o[k].x = fmaf(w, v.x, o[k].x);
-                    o[k].y = fmaf(w, v.y, o[k].y);
-                    o[k].z = fmaf(w, v.z, o[k].z);
-                    o[k].w = fmaf(w, v.w, o[k].w);
-                }
+            for (int x = 0; x < BATCH; ++x) {
+                const int i = x0 + x * TEAMS;
+                if (i >= m) break;
+                float w = __shfl_sync(0xffffffffu, f, i + team < m ? i + team : m - 1);
+                if (i + team >= m) w = 0.f;
+#pragma unroll
+                for (int k = 0; k < PER; ++k)
+                    if (w != 0.f) {     // a part without a visible key adds nothing
+                        o[k].x = fmaf(w, v[x][k].x, o[k].x);
+                        o[k].y = fmaf(w, v[x][k].y, o[k].y);
+                        o[k].z = fmaf(w, v[x][k].z, o[k].z);
+                        o[k].w = fmaf(w, v[x][k].w, o[k].w);
+                    }
             }
         }
     }
@@ -888,7 +998,7 @@ __device__ __forceinline__ void empty_row(void* out, float* lse, int lane) {
 }
 
 // Where the partial results of one sequence's heads lie: worked out by a whole block of kJoinWarps warps from the lengths.
-template <int D, int GH, bool PREFIX>
+template <int D, int GH>
 struct JoinList {
     using C = DecodeCfg<D, GH>;
     int64_t total, before;     // tiles of the list, and of the sequences in front
@@ -898,7 +1008,7 @@ struct JoinList {
         const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
         int64_t sum4[4] = {0, 0, 0, 0};                    // tiles of the sequences before b and of all, in either form of the list
         for (int x = tid; x < p.B; x += kJoinWarps * 32) {
-            const SeqRange r = seq_range<C::CK, PREFIX>(p, x);
+            const SeqRange r = seq_range<C::CK, false>(p, x);
             const int n0 = seq_tiles<NW>(r, p.hpt_shift), n1 = seq_tiles<NW>(r, 0);
             sum4[2] += n0;
             sum4[3] += n1;
@@ -919,12 +1029,12 @@ struct JoinList {
 #pragma unroll
             for (int w = 0; w < kJoinWarps; ++w) sum4[f] += red[f][w];
         }
-        const ListForm form = list_form(p, sum4[2], sum4[3]);
+        const ListForm form = list_form<false>(p, sum4[2], sum4[3], p.grid);
         total = form.total;
         hs = form.hpt_shift;
         groups = p.heads >> hs;
         before = hs == p.hpt_shift ? sum4[0] : sum4[1];
-        n = seq_tiles<NW>(seq_range<C::CK, PREFIX>(p, b), hs);
+        n = seq_tiles<NW>(seq_range<C::CK, false>(p, b), hs);
         ctas = cta_count(total, p.grid);
     }
 };
@@ -966,7 +1076,7 @@ attn_paged_join_kernel(const DecodeParams p, int blocks_per_seq) {
     __shared__ int64_t red[4][kJoinWarps];
     const int b = blockIdx.x / blocks_per_seq, lane = threadIdx.x & 31;
     const int q_head = (blockIdx.x - b * blocks_per_seq) * kJoinWarps + (threadIdx.x >> 5);
-    const JoinList<D, GH, false> list(p, b, red);
+    const JoinList<D, GH> list(p, b, red);
     // Every block waits for the first kernel, also one without work: in a graph this kernel's end stands for both.
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (q_head >= p.H) return;

@@ -9,18 +9,27 @@
 //
 // A list is one K/V head and a pair of 128-row tiles of queries; row r of a tile is query head r % G of the K/V head's G, of token
 // r / G (128 / G tokens to a tile, rounded down), which a TMA box brings in that order from [token][head][D].  Its steps are the
-// 128-key tiles that its last token sees.  The steps of all lists, one after the other, are cut evenly over one CTA per SM,
-// whatever the lengths are (each CTA works out its own part from the device-side lengths: no host copy, no plan to keep); a list
-// that a border cuts leaves a partial result per CTA (at most two per CTA, fp32), which a second kernel joins in a fixed order.
+// 128-key tiles that its last token sees.  The steps of all lists, one after the other and each list with kListCost steps more for its
+// fill and way out, are cut evenly over one CTA per SM, whatever the lengths are (each CTA works out its own part from the device-side
+// lengths: no host copy, no plan to keep); a list that a border cuts leaves a partial result per CTA (at most two per CTA, fp32),
+// which a second kernel joins in a fixed order.  (Without kListCost 8 prompts of 100 - 4000 tokens, 16 heads of 64, take 261 us instead
+// of 241, prompts of up to 2000 tokens with 32 heads over 8 of 128 195 instead of 166.)
 //
 // Inside a CTA it is the pipeline of attn_tc_pipe.cuh: TMA ring of K/V tiles, one MMA-issuing warp, two softmax groups in
 // ping-pong, P back into tensor memory as the second product's operand, a lagging reference maximum.  What paging adds:
-//   * A tile is 128 / page_size boxes per 64 columns, issued by as many lanes of the producer warp; its page numbers are read a
-//     step ahead.
+//   * A tile is 128 / page_size boxes per 64 columns, issued by as many lanes of a warp, K's by one warp and V's by another (a box
+//     costs its warp about 95 cycles; one warp for both: 2048 tokens behind 14336 in pages of 16 507 us, of 8 706, two: 410 either
+//     way); page numbers are read a step ahead.
 //   * Slots that hold no key of the sequence (behind its end, or in a page whose number is out of range) may hold anything: their
 //     scores are overwritten with -inf before the softmax, and their V rows with zeros before the product (0 * NaN is no number).
+//   * A list of one tile (few query rows: a prefix call's usual case) keeps both softmax groups busy: its rows are in both Q tiles,
+//     one takes the even steps and one the odd ones, and the epilogue adds up the two accumulators in tensor memory.
 //   * All exponentials on the special-function unit, as under a window: rows may see only a few keys.
 // P is rounded to the type of Q, K and V before its product and the row sums add the unrounded values (see attn_tc_pipe.cuh).
+//
+// What bounds it: a step of two tiles takes 1.9 us at D = 128 (1024 tensor cycles a tile, 1.25 PFLOP/s of visible pairs for the 2048
+// tokens above) and 1.7 at D = 64 (its exponentials), a step of one tile 1.0; a list costs 5 us beside its steps (the way out 2.3,
+// then the next list's first scores), and the first scores are there 7 us after the start, most of it instructions that come from L2.
 #pragma once
 #include "attn_paged.cuh"
 #include "attn_tc_common.cuh"
@@ -31,7 +40,9 @@ using namespace sm100;
 using attn_paged::cta_begin;
 using attn_paged::cta_count;
 using attn_paged::cta_of_tile;
+using attn_paged::divide;
 using attn_paged::group_prefix;
+using attn_paged::kListCost;
 using attn_paged::report_bad_index;
 using attn_tc::low_bits;
 
@@ -44,7 +55,7 @@ struct Cfg {
     static constexpr int NSLOT = D == 128 ? 4 : 8, NGRP = NSLOT / 2;      // ring slots; a group is V_j and K_{j+1}
     static constexpr int OST_BYTES = 128 * 128;   // staging of a tile's output, 128 bytes a row
     static constexpr int TILE_BYTES = 2 * Q_BYTES + NSLOT * KV_BYTES + 2 * OST_BYTES;
-    static constexpr int MISC_BYTES = 1024;
+    static constexpr int MISC_BYTES = 2048;
     static constexpr int SMEM_BYTES = 1024 + TILE_BYTES + MISC_BYTES;
     static constexpr int THREADS = 384, TMEM_COLS = 512;
     __host__ __device__ static constexpr int s_col(int t) { return t * 128; }
@@ -55,10 +66,20 @@ struct Cfg {
 // floats of one partial result: O [256][D] (not normalised), then reference exponent and sum [256][2]
 __host__ __device__ constexpr int64_t part_floats(int D) { return static_cast<int64_t>(kRows) * (D + 2); }
 
+// What the joining kernels need to know about the lists, left in the workspace by the kernel that has worked it out.
+struct Cut { int parts[2], tok, n_tok, kvh; };     // partial results of each tile (0: none)
+struct PrefixPlan {
+    int64_t start, stride;      // where step 0 of the sequence's list of K/V head 0 lies, and weight per head.  Behind the last sequence: the
+                                // weight of all lists, and the CTAs that share it
+    int steps, row;             // steps of a list (0: no common keys); row of query head 0 of a K/V head
+};
+
 struct Params {
     void* o;                    // prefill: [tokens, H, D] and lse [tokens, H]
     float* lse;
     float* parts;               // [2 per CTA] partial results of lists that a border cuts
+    Cut* cuts;                  // prefill: [CTA], the list whose first border lies behind the CTA
+    PrefixPlan* plan;           // prefix: [tokens + 1]
     float* rows;                // prefix: O [tokens * H][D], then [tokens * H][2], of lists that one CTA has to itself
     const int* block_table;
     const int* seq_lens;
@@ -69,6 +90,7 @@ struct Params {
     int H, Hkv, group, tile_tokens;
     int max_len, num_pages, page_shift, box_shift, k_axes, v_axes;
     float scale, scale_log2;
+    int row_bytes, head_groups; // prefix: of a key, K and V of all heads; groups of heads of a pair of the other kernel
     int grid;
     int* status;
 #ifdef ATTN_TEST_HOOKS
@@ -120,6 +142,14 @@ struct Unit {
         const int t2 = 2 * p.tile_tokens;
         pairs = (n + t2 - 1) / t2;
     }
+    // that of another lane of the warp
+    __device__ __forceinline__ void from_lane(int lane) {
+        tok0 = __shfl_sync(0xffffffffu, tok0, lane);
+        n = __shfl_sync(0xffffffffu, n, lane);
+        base = __shfl_sync(0xffffffffu, base, lane);
+        len = __shfl_sync(0xffffffffu, len, lane);
+        pairs = __shfl_sync(0xffffffffu, pairs, lane);
+    }
     // steps of the first `tokens` query tokens (at least one, also where none of them sees a key)
     __device__ __forceinline__ int steps_of(int tokens) const {
         if (PREFIX) return (len + 127) >> 7;
@@ -131,24 +161,29 @@ struct Unit {
         if (PREFIX) return static_cast<int64_t>(i) * ((len + 127) >> 7);
         const int t2 = 2 * p.tile_tokens, full = i < pairs ? i : pairs - 1;
         if (i == 0) return 0;
-        return floor_sum(full, t2, (base > 0 ? base : 0) + t2 - 1) + full + (i == pairs ? steps_of(n) : 0);
+        return floor_sum(full, t2, static_cast<uint32_t>(base > 0 ? base : 0) + t2 - 1) + full + (i == pairs ? steps_of(n) : 0);
     }
-    __device__ __forceinline__ int64_t head_steps(const Params& p) const { return steps_before(p, pairs); }
+    __device__ __forceinline__ int64_t weight_before(const Params& p, int i) const { return steps_before(p, i) + static_cast<int64_t>(i) * kListCost; }
+    __device__ __forceinline__ int64_t head_weight(const Params& p) const { return weight_before(p, pairs); }
 };
 
-// Position in the lists: unit, K/V head, pair, step of the pair's list.  All lanes of a warp hold the same one.
+// Position in the lists: unit, K/V head, pair, step of the pair's list (below 0: in what the list costs beside its steps).  All lanes of
+// a warp hold the same one.
 template <bool PREFIX>
 struct Walk {
     Unit<PREFIX> unit;
     int u, h, i, step, steps;
-    // Total steps of all lists; all 32 lanes.  mine, before: the steps of this lane's units and of those in front of them.
-    static __device__ __forceinline__ int64_t total(const Params& p, int lane, int64_t& mine, int64_t& before) {
-        const int per = (p.units + 31) / 32, u0 = lane * per, u1 = u0 + per < p.units ? u0 + per : p.units;
+    int64_t mine, before;      // weight of this lane's units (consecutive ones) and of those in front of them
+    int per, first;            // units of a lane, and this lane's first
+    // Total weight of all lists; all 32 lanes.
+    __device__ __forceinline__ int64_t total(const Params& p, int lane) {
+        per = (p.units + 31) / 32;
+        first = lane * per;
+        const int end = first + per < p.units ? first + per : p.units;
         mine = 0;
-        for (int x = u0; x < u1; ++x) {
-            Unit<PREFIX> unit;
+        for (int x = first; x < end; ++x) {
             unit.load(p, x);
-            mine += p.Hkv * unit.head_steps(p);
+            mine += p.Hkv * unit.head_weight(p);
         }
         before = mine;
 #pragma unroll
@@ -160,41 +195,58 @@ struct Walk {
         before -= mine;
         return all;
     }
-    // Step `at` of all (below the total).
-    __device__ __forceinline__ void find(const Params& p, int lane, int64_t at, int64_t mine, int64_t before) {
-        const int per = (p.units + 31) / 32;
+    // The CTAs that share the lists, after total(): of a prefix call those that prefix_ctas() gives it.
+    __device__ __forceinline__ int ctas(const Params& p, int64_t total, int lane) const {
+        int n = p.grid;
+        if constexpr (PREFIX) {
+            int64_t cost = 0, own = 0, seqs = 0;
+            for (int g = lane; g < p.units; g += 32)
+                cost += attn_paged::group_cost(p.starts, p.prefix_lens, p.seq_lens, g, p.tokens, p.max_len, p.Hkv, p.tile_tokens);
+            for (int b = lane; b < p.tokens; b += 32) {
+                int len = __ldg(p.seq_lens + b);
+                len = len < 0 ? 0 : (len > p.max_len ? p.max_len : len);
+                const int prefix = attn_paged::prefix_of(p.starts, p.prefix_lens, p.seq_lens, p.units, p.max_len, b);
+                own += len > prefix ? len - prefix : 0;
+                seqs += len > prefix ? 1 : 0;
+            }
+            n = attn_paged::prefix_ctas(attn_paged::warp_sum(cost), attn_paged::warp_sum(own) * p.row_bytes, attn_paged::warp_sum(seqs) * p.head_groups, p.grid);
+        }
+        return cta_count(total, n);
+    }
+    // Position `at` of all (below the total), after total().
+    __device__ __forceinline__ void find(const Params& p, int lane, int64_t at) {
         const bool here = at >= before && at < before + mine;
         const int owner = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
         int64_t rem = at - before;
-        int x = lane * per;
-        if (here)
+        int x = first;
+        if (here && per > 1)
             for (;; ++x) {
                 unit.load(p, x);
-                const int64_t n = p.Hkv * unit.head_steps(p);
+                const int64_t n = p.Hkv * unit.head_weight(p);
                 if (rem < n) break;
                 rem -= n;
             }
         u = __shfl_sync(0xffffffffu, x, owner);
         rem = __shfl_sync(0xffffffffu, rem, owner);
-        unit.load(p, u);
-        const int64_t per_head = unit.head_steps(p);
-        h = static_cast<int>(rem / per_head);
+        unit.from_lane(owner);
+        const int64_t per_head = unit.head_weight(p);
+        h = static_cast<int>(divide(rem, per_head));
         rem -= h * per_head;
         // the last pair with steps_before <= rem, 32 candidates at a time
         int lo = 0, hi = unit.pairs;
         while (hi - lo > 1) {
             const int stride = (hi - lo + 31) / 32, mid = lo + lane * stride;
-            const unsigned ok = __ballot_sync(0xffffffffu, mid < hi && unit.steps_before(p, mid) <= rem);
+            const unsigned ok = __ballot_sync(0xffffffffu, mid < hi && unit.weight_before(p, mid) <= rem);
             lo += (31 - __clz(ok)) * stride;
             hi = lo + stride < hi ? lo + stride : hi;
         }
         i = lo;
-        step = static_cast<int>(rem - unit.steps_before(p, i));
+        step = static_cast<int>(rem - unit.weight_before(p, i)) - kListCost;
         steps = unit.pair_steps(p, i);
     }
     // The next list (not called behind the last one).
     __device__ __forceinline__ void next(const Params& p) {
-        step = 0;
+        step = -kListCost;
         if (++i == unit.pairs) {
             i = 0;
             if (++h == p.Hkv) {
@@ -210,7 +262,8 @@ struct Walk {
 // A CTA's share of one list, as the roles of the CTA get it.
 struct Item {
     int kvh, tok, n_tok;       // K/V head; first token and the tokens from there to the end of the unit
-    int n0, n1, n_max;         // steps of each tile in this share (-1: a tile without tokens)
+    int n0, n1, n_max;         // steps of each tile in this share, and of the share
+    bool twin;                 // one tile of queries, in both places: tile 0 takes the even steps, tile 1 the odd ones
     int tile0;                 // first key tile
     int base, len;             // last key that the first token sees (prefill); keys
     int slot;                  // partial result (-1: the whole list)
@@ -245,10 +298,11 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         B_OFINAL = 10,     // [2] the item's last O_t += P_t V has finished
         B_OFREE = 12,      // [2] O_t is in registers (128 threads)
         B_SCHEDFULL = 14,  // [4] slot holds an item
-        B_SCHEDEMPTY = 18, // [4] slot read by the MMA warp and the eight softmax warps
-        B_KVFULL = 22,
-        B_KVEMPTY = 22 + NGRP,
-        B_COUNT = 22 + 2 * NGRP
+        B_SCHEDEMPTY = 18, // [4] slot read by warps 8, 10 and the eight softmax warps
+        B_MERGE = 22,      // tile 1's sums are in shared memory (128 threads)
+        B_KVFULL = 23,     // [NGRP] V_{j-1} and K_j loaded (two warps' copies)
+        B_KVEMPTY = 23 + NGRP,
+        B_COUNT = 23 + 2 * NGRP
     };
     auto bar = [&](int i) { return smem_base + C::TILE_BYTES + i * 8; };
     volatile int* sched = reinterpret_cast<volatile int*>(bars + B_COUNT);             // [4][16]
@@ -257,7 +311,8 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     volatile uint32_t* bad_ring = reinterpret_cast<volatile uint32_t*>(sched + 64);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(const_cast<uint32_t*>(bad_ring) + 64);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    static_assert(8 * B_COUNT + 4 * (64 + 64 + 2) <= C::MISC_BYTES, "barriers and slots");
+    float2* merge = reinterpret_cast<float2*>(smem_gen + C::TILE_BYTES + C::MISC_BYTES - 1024);     // [128]: reference and sum of tile 1's rows
+    static_assert(8 * B_COUNT + 4 * (64 + 64 + 2) <= C::MISC_BYTES - 1024, "barriers and slots");
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int tile_rows = p.tile_tokens * p.group;
 
@@ -274,10 +329,11 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         }
         for (int s = 0; s < 4; ++s) {
             mbar_init(bar(B_SCHEDFULL + s), 1);
-            mbar_init(bar(B_SCHEDEMPTY + s), 9);
+            mbar_init(bar(B_SCHEDEMPTY + s), 10);
         }
+        mbar_init(bar(B_MERGE), 128);
         for (int s = 0; s < NGRP; ++s) {
-            mbar_init(bar(B_KVFULL + s), 1);
+            mbar_init(bar(B_KVFULL + s), 2);
             mbar_init(bar(B_KVEMPTY + s), 1);
         }
         fence_barrier_init();
@@ -322,10 +378,43 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         it.len = e[8];
         it.slot = e[9];
         it.first_row = e[10];
-        it.n_max = it.n0 > it.n1 ? it.n0 : it.n1;
+        it.n_max = e[11] >> 1;
+        it.twin = e[11] & 1;
         __syncwarp();
         if (hand_back) mbar_arrive(bar(B_SCHEDEMPTY + slot));
         return valid;
+    };
+
+    // ---- what the two warps that load tiles share: page numbers of a tile's boxes, box 32 r + lane: -1: no key there, -2: not a page ----
+    const int boxes = 128 >> p.box_shift, slot_mask = (1 << p.page_shift) - 1;
+    auto fetch = [&](const Item& it, int tile, int* pg) {
+        const int* table = p.block_table + static_cast<int64_t>(it.first_row) * p.table_stride;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int box = 32 * r + lane, key = tile * 128 + (box << p.box_shift);
+            pg[r] = -1;
+            if (box < boxes && key < it.len) {
+                pg[r] = __ldg(table + (key >> p.page_shift));
+                if (static_cast<unsigned>(pg[r]) >= static_cast<unsigned>(p.num_pages)) pg[r] = -2;
+            }
+        }
+    };
+    auto load_tile = [&](const Item& it, uint32_t dst, const CUtensorMap* map, int axes, uint32_t full, int tile, const int* pg) {
+        int n = 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) n += __popc(__ballot_sync(0xffffffffu, pg[r] >= 0));
+        if (lane == 0) mbar_arrive_expect_tx(full, (n * NBOX << p.box_shift) * 128);
+        __syncwarp();        // armed before the first copy
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if (32 * r >= boxes) break;
+            const int row = (32 * r + lane) << p.box_shift;
+            if (pg[r] >= 0) {
+#pragma unroll
+                for (int pl = 0; pl < NBOX; ++pl)
+                    attn_paged::load_box(dst + pl * 16384 + row * 128, map, full, axes, pl, (tile * 128 + row) & slot_mask, it.kvh, pg[r]);
+            }
+        }
     };
 
     if (warp >= 8) {
@@ -334,22 +423,27 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             // =========================== lists, TMA ===========================
             const bool leader = elect_one();
             Walk<PREFIX> walk;
-            int64_t mine, before, left = 0;
-            const int64_t total = Walk<PREFIX>::total(p, lane, mine, before);
-            const int ctas = cta_count(total, p.grid);
+            int64_t left = 0;
+            walk.step = 0;
+            const int64_t total = walk.total(p, lane);
+            const int ctas = walk.ctas(p, total, lane);
             if (static_cast<int>(blockIdx.x) < ctas) {
                 const int64_t first = cta_begin(total, blockIdx.x, ctas);
                 left = cta_begin(total, blockIdx.x + 1, ctas) - first;
-                walk.find(p, lane, first, mine, before);
+                walk.find(p, lane, first);
             }
+            // prefill: the list of this CTA that goes on in the next one: none as yet (also where a wait runs out later)
+            if (!PREFIX && leader) p.cuts[blockIdx.x] = Cut{{0, 0}, 0, 0, 0};
             int kv_base = 0, q_uses[2] = {0, 0};
-            const int boxes = 128 >> p.box_shift, slot_mask = (1 << p.page_shift) - 1;
             for (int k = 0;; ++k) {
                 const int slot = k & 3;
                 if (!wait(B_SCHEDEMPTY + slot, ((k >> 2) & 1) ^ 1)) break;
                 Item it;
-                if (left > 0) {
-                    const int s0 = walk.step, s1 = walk.steps - s0 < left ? walk.steps : s0 + static_cast<int>(left);
+                // this CTA's steps of the next list (none where its part ends in front of the list's first step)
+                const int s0 = walk.step < 0 ? 0 : walk.step;
+                const int s1 = left <= 0 ? 0 : (walk.steps - walk.step < left ? walk.steps : walk.step + static_cast<int>(left));
+                left -= s1 - walk.step;
+                if (s1 > s0) {
                     const int pair_tok = walk.i * 2 * p.tile_tokens;
                     it.kvh = walk.h;
                     it.tok = walk.unit.tok0 + pair_tok;
@@ -358,13 +452,31 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     it.base = walk.unit.base + pair_tok;
                     it.len = walk.unit.len;
                     it.first_row = PREFIX ? walk.unit.tok0 : walk.u;
-                    const int all0 = walk.unit.steps_of(pair_tok + p.tile_tokens);
-                    it.n0 = (all0 < s1 ? all0 : s1) - s0;
-                    it.n0 = it.n0 < 0 ? 0 : it.n0;
-                    it.n1 = it.n_tok > p.tile_tokens ? s1 - s0 : -1;
-                    it.n_max = it.n0 > it.n1 ? it.n0 : it.n1;
+                    it.twin = it.n_tok <= p.tile_tokens;
+                    it.n_max = s1 - s0;
+                    if (it.twin) {
+                        it.n0 = (it.n_max + 1) >> 1;
+                        it.n1 = it.n_max >> 1;
+                    } else {
+                        const int all0 = walk.unit.steps_of(pair_tok + p.tile_tokens);
+                        it.n0 = (all0 < s1 ? all0 : s1) - s0;
+                        it.n0 = it.n0 < 0 ? 0 : it.n0;
+                        it.n1 = it.n_max;
+                    }
                     it.slot = s0 == 0 && s1 == walk.steps ? -1 : 2 * static_cast<int>(blockIdx.x) + (s0 == 0 ? 1 : 0);
-                    left -= s1 - s0;
+                    if (!PREFIX && s0 == 0 && s1 < walk.steps) {
+                        if (leader) {
+                            const int64_t start = cta_begin(total, blockIdx.x + 1, ctas) - left - s1;        // where step 0 lies
+                            const int me = static_cast<int>(blockIdx.x);
+                            Cut c;
+                            c.parts[0] = cta_of_tile(total, start + walk.unit.steps_of(pair_tok + p.tile_tokens) - 1, ctas) - me + 1;
+                            c.parts[1] = it.twin ? 0 : cta_of_tile(total, start + walk.steps - 1, ctas) - me + 1;
+                            c.tok = it.tok;
+                            c.n_tok = it.n_tok;
+                            c.kvh = it.kvh;
+                            p.cuts[me] = c;
+                        }
+                    }
                     if (left > 0) walk.next(p);
                     if (leader) {
                         volatile int* e = sched + slot * 16;
@@ -378,6 +490,7 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                         e[8] = it.len;
                         e[9] = it.slot;
                         e[10] = it.first_row;
+                        e[11] = 2 * it.n_max + (it.twin ? 1 : 0);
                         e[0] = 1;
                         mbar_arrive(bar(B_SCHEDFULL + slot));
                     }
@@ -388,37 +501,6 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     }
                     break;
                 }
-                const int* table = p.block_table + static_cast<int64_t>(it.first_row) * p.table_stride;
-                // pages of a tile's boxes, box 32 r + lane: -1: no key there, -2: not a page
-                auto fetch = [&](int tile, int* pg) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int box = 32 * r + lane, key = tile * 128 + (box << p.box_shift);
-                        pg[r] = -1;
-                        if (box < boxes && key < it.len) {
-                            pg[r] = __ldg(table + (key >> p.page_shift));
-                            if (static_cast<unsigned>(pg[r]) >= static_cast<unsigned>(p.num_pages)) pg[r] = -2;
-                        }
-                    }
-                };
-                auto count = [&](const int* pg) {
-                    int n = 0;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) n += __popc(__ballot_sync(0xffffffffu, pg[r] >= 0));
-                    return n;
-                };
-                auto load_tile = [&](uint32_t dst, const CUtensorMap* map, int axes, uint32_t full, int tile, const int* pg) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        if (32 * r >= boxes) break;
-                        const int row = (32 * r + lane) << p.box_shift;
-                        if (pg[r] >= 0) {
-#pragma unroll
-                            for (int pl = 0; pl < NBOX; ++pl)
-                                attn_paged::load_box(dst + pl * 16384 + row * 128, map, full, axes, pl, (tile * 128 + row) & slot_mask, it.kvh, pg[r]);
-                        }
-                    }
-                };
                 auto load_q = [&](int t) -> bool {
                     if (!wait(B_QEMPTY + t, (q_uses[t] & 1) ^ 1)) return false;
                     if (leader) {
@@ -428,62 +510,96 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                             asm volatile(
                                 "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
                                 ::"r"(sQ(t) + bx * 16384), "l"(reinterpret_cast<uint64_t>(&tmQ)), "r"(bar(B_QFULL + t)), "r"(64 * bx), "r"(it.kvh * p.group),
-                                "r"(it.tok + t * p.tile_tokens), "r"(0)
+                                "r"(it.tok + (it.twin ? 0 : t * p.tile_tokens)), "r"(0)
                                 : "memory");
                     }
                     ++q_uses[t];
                     return true;
                 };
-                // Ring group i of an item: {V_{i-1}, K_i}, what the MMA warp needs together (see attn_tc_pipe.cuh).
-                int pg_v[4] = {-1, -1, -1, -1}, pg_k[4], pg_next[4];
-                fetch(it.tile0, pg_next);
+                // Ring group i of an item: {V_{i-1}, K_i}, what the MMA warp needs together (see attn_tc_pipe.cuh).  K here, V by
+                // warp 10.
+                int pg[4], pg_next[4];
+                fetch(it, it.tile0, pg_next);
                 bool ok = it.n0 > 0 ? load_q(0) : true;
                 for (int i = 0; i <= it.n_max && ok; ++i) {
                     const int group = kv_base + i, g = group % NGRP;
-                    const bool has_v = i > 0, has_k = i < it.n_max;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) pg_k[r] = pg_next[r];
-                    if (i + 1 < it.n_max) fetch(it.tile0 + i + 1, pg_next);
+                    for (int r = 0; r < 4; ++r) pg[r] = pg_next[r];
+                    if (i + 1 < it.n_max) fetch(it, it.tile0 + i + 1, pg_next);
                     if (!(ok = wait(B_KVEMPTY + g, ((group / NGRP) & 1) ^ 1))) break;
-                    if (has_k) {
-                        volatile uint32_t* bad = bad_ring + (group & 7) * 8;
-                        bool any = false;
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) any = any || pg_k[r] == -2;
-                        any = __any_sync(0xffffffffu, any);
-                        if (any) {       // rare: the tile's bits are put together word by word
-                            if (lane == 0) report_bad_index(p.status);
-                            for (int w = 0; w < 4; ++w) {
-                                // key 32 w + lane lies in box (32 w + lane) >> box_shift, whose page number lane box % 32 has
-                                const int box = (32 * w + lane) >> p.box_shift;
-                                int pg = -1;
-#pragma unroll
-                                for (int r = 0; r < 4; ++r) {
-                                    const int x = __shfl_sync(0xffffffffu, pg_k[r], box & 31);
-                                    if (box >> 5 == r) pg = x;
-                                }
-                                const uint32_t word = __ballot_sync(0xffffffffu, pg == -2);
-                                if (lane == 0) bad[1 + w] = word;
-                            }
-                        }
-                        if (lane == 0) bad[0] = any ? 1u : 0u;
-                    }
-                    const int n_boxes = (has_v ? count(pg_v) : 0) + (has_k ? count(pg_k) : 0);
-                    __syncwarp();
 #ifdef ATTN_TEST_HOOKS
-                    if (group != p.test_skip_group)      // (this group's barrier never completes)
+                    if (group == p.test_skip_group) continue;      // this group's barrier never completes
 #endif
-                    {
-                        if (lane == 0) mbar_arrive_expect_tx(bar(B_KVFULL + g), (n_boxes * NBOX << p.box_shift) * 128);
-                        __syncwarp();                    // armed before the first copy
-                        if (has_v) load_tile(sKV(2 * g), &tmV, p.v_axes, bar(B_KVFULL + g), it.tile0 + i - 1, pg_v);
-                        if (has_k) load_tile(sKV(2 * g + 1), &tmK, p.k_axes, bar(B_KVFULL + g), it.tile0 + i, pg_k);
+                    if (i == it.n_max) {
+                        if (lane == 0) mbar_arrive(bar(B_KVFULL + g));
+                        continue;
                     }
+                    volatile uint32_t* bad = bad_ring + (group & 7) * 8;
+                    bool any = false;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) pg_v[r] = pg_k[r];
+                    for (int r = 0; r < 4; ++r) any = any || pg[r] == -2;
+                    any = __any_sync(0xffffffffu, any);
+                    if (any) {       // rare: the tile's bits are put together word by word
+                        if (lane == 0) report_bad_index(p.status);
+                        for (int w = 0; w < 4; ++w) {
+                            // key 32 w + lane lies in box (32 w + lane) >> box_shift, whose page number lane box % 32 has
+                            const int box = (32 * w + lane) >> p.box_shift;
+                            int page = -1;
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const int x = __shfl_sync(0xffffffffu, pg[r], box & 31);
+                                if (box >> 5 == r) page = x;
+                            }
+                            const uint32_t word = __ballot_sync(0xffffffffu, page == -2);
+                            if (lane == 0) bad[1 + w] = word;
+                        }
+                    }
+                    if (lane == 0) bad[0] = any ? 1u : 0u;
+                    load_tile(it, sKV(2 * g + 1), &tmK, p.k_axes, bar(B_KVFULL + g), it.tile0 + i, pg);
                     if (i == 0 && it.n1 > 0) ok = load_q(1);
                 }
                 if (!ok) break;
+                kv_base += it.n_max + 1;
+            }
+        } else if (warp == 10) {
+            // =========================== V tiles ===========================
+            int kv_base = 0;
+            bool ok = true;
+            for (int k = 0; ok; ++k) {
+                Item it;
+                if (!next_item(k, lane == 0, it)) break;
+                int pg[4], pg_next[4];
+                fetch(it, it.tile0, pg_next);
+                for (int i = 0; i <= it.n_max; ++i) {
+                    const int group = kv_base + i, g = group % NGRP;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) pg[r] = pg_next[r];
+                    if (i > 0 && i < it.n_max) fetch(it, it.tile0 + i, pg_next);
+                    if (!(ok = wait(B_KVEMPTY + g, ((group / NGRP) & 1) ^ 1))) break;
+                    if (i == 0) {
+                        if (lane == 0) mbar_arrive(bar(B_KVFULL + g));
+                        continue;
+                    }
+                    bool any = false;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) any = any || pg[r] == -2;
+                    if (__any_sync(0xffffffffu, any)) {      // rare: V rows of pages that are out of range become zeros
+                        uint8_t* v = smem_gen + 2 * C::Q_BYTES + 2 * g * C::KV_BYTES;
+                        for (int row = 0; row < 128; ++row) {
+                            const int box = row >> p.box_shift;
+                            int page = -1;
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const int x = __shfl_sync(0xffffffffu, pg[r], box & 31);
+                                if (box >> 5 == r) page = x;
+                            }
+                            if (page == -2 && lane < 8 * NBOX) *reinterpret_cast<uint4*>(v + (lane >> 3) * 16384 + row * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        }
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                    }
+                    load_tile(it, sKV(2 * g), &tmV, p.v_axes, bar(B_KVFULL + g), it.tile0 + i - 1, pg);
+                }
                 kv_base += it.n_max + 1;
             }
         } else if (warp == 8) {
@@ -522,77 +638,127 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             for (int k = 0; ok; ++k) {
                 Item it;
                 if (!next_item(k, leader, it)) break;
-                // V rows that hold no key become zeros (the ring's slot is this warp's until it commits the products that read it)
+                // V rows behind the sequence's end, in the last tile, become zeros (the ring's slot is this warp's until it commits the
+                // products that read it).  That is all this warp looks at: reading the tile's flag, too, costs 4 % of 120 steps.
                 auto clear_v = [&](int j, int slot) {
                     const int valid = it.len - (it.tile0 + j) * 128;
-                    const volatile uint32_t* bad = bad_ring + ((kv_base + j) & 7) * 8;
-                    const bool some_bad = bad[0] != 0;
-                    if (valid >= 128 && !some_bad) return;
+                    if (valid >= 128) return;
                     uint8_t* v = smem_gen + 2 * C::Q_BYTES + slot * C::KV_BYTES;
-                    const int from = some_bad ? 0 : (valid < 0 ? 0 : valid);
-                    for (int e = lane; e < (128 - from) * 8; e += 32) {
-                        const int row = from + (e >> 3);
-                        if (row >= valid || ((bad[1 + (row >> 5)] >> (row & 31)) & 1)) {
+                    const int from = valid < 0 ? 0 : valid;
+#pragma unroll 1
+                    for (int e = from * 8 + lane; e < 128 * 8; e += 32)
 #pragma unroll
-                            for (int pl = 0; pl < NBOX; ++pl)
-                                *reinterpret_cast<uint4*>(v + pl * 16384 + row * 128 + (e & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-                        }
-                    }
+                        for (int pl = 0; pl < NBOX; ++pl) *reinterpret_cast<uint4*>(v + pl * 16384 + e * 16) = make_uint4(0u, 0u, 0u, 0u);
                     fence_proxy_async_smem();
                     __syncwarp();
+                };
+                // O_t += P_t V, the i-th step of the tile; false: a wait ran out
+                auto do_pv = [&](int t, int i, int gslot) {
+                    const uint32_t par = (it_base[t] + i) & 1;
+                    if (!wait(B_PFULL + t, par)) return false;
+                    // the previous item's O_t must be in registers before it is overwritten
+                    if (i == 0 && uses[t] > 0 && !wait(B_OFREE + t, (uses[t] - 1) & 1)) return false;
+                    tc_fence_after_sync();
+                    issue_pv(t, 2 * gslot, i > 0, 0, 6);
+                    if (!wait(B_PFULL2 + t, par)) return false;
+                    tc_fence_after_sync();
+                    issue_pv(t, 2 * gslot, true, 6, 8);
+                    if (i + 1 == it.n(t)) commit(B_OFINAL + t);
+                    return true;
+                };
+                auto do_s = [&](int t, int i, int gslot) {
+                    issue_s(t, 2 * gslot + 1);
+                    commit(B_SFULL + t);
+                    if (i + 1 == it.n(t)) commit(B_QEMPTY + t);      // the last S of the item
                 };
                 ok = wait(B_KVFULL + kv_base % NGRP, (kv_base / NGRP) & 1);
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    if (ok && it.n(t) > 0) {
+                    if (ok && it.n(t) > 0 && !(t == 1 && it.twin)) {
                         ok = wait(B_QFULL + t, uses[t] & 1);
-                        if (ok) {
-                            tc_fence_after_sync();
-                            issue_s(t, 2 * (kv_base % NGRP) + 1);
-                            commit(B_SFULL + t);
-                            if (it.n(t) == 1) commit(B_QEMPTY + t);
-                        }
+                        tc_fence_after_sync();
+                        if (ok) do_s(t, 0, kv_base % NGRP);
                     }
                 }
                 if (ok) commit(B_KVEMPTY + kv_base % NGRP);
-                for (int j = 0; j < it.n_max && ok; ++j) {
-                    const int grp = kv_base + j + 1, gslot = grp % NGRP;
-                    if (!(ok = wait(B_KVFULL + gslot, (grp / NGRP) & 1))) break;
-                    clear_v(j, 2 * gslot);
+                if (!it.twin) {
+#pragma unroll 1
+                    for (int j = 0; j < it.n_max && ok; ++j) {
+                        const int grp = kv_base + j + 1, gslot = grp % NGRP;
+                        if (!(ok = wait(B_KVFULL + gslot, (grp / NGRP) & 1))) break;
+                        clear_v(j, 2 * gslot);
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        if (j < it.n(t)) {
-                            const uint32_t par = (it_base[t] + j) & 1;
-                            if (!(ok = wait(B_PFULL + t, par))) break;
-                            // the previous item's O_t must be in registers before it is overwritten
-                            if (j == 0 && uses[t] > 0 && !(ok = wait(B_OFREE + t, (uses[t] - 1) & 1))) break;
-                            tc_fence_after_sync();
-                            issue_pv(t, 2 * gslot, j > 0, 0, 6);
-                            if (!(ok = wait(B_PFULL2 + t, par))) break;
-                            tc_fence_after_sync();
-                            issue_pv(t, 2 * gslot, true, 6, 8);
-                            if (j + 1 == it.n(t)) commit(B_OFINAL + t);
+                        for (int t = 0; t < 2; ++t) {
+                            if (j < it.n(t) && !(ok = do_pv(t, j, gslot))) break;
+                            if (j + 1 < it.n(t)) do_s(t, j + 1, gslot);
                         }
-                        if (j + 1 < it.n(t)) {
-                            issue_s(t, 2 * gslot + 1);
-                            commit(B_SFULL + t);
-                            if (j + 2 == it.n(t)) commit(B_QEMPTY + t);
+                        if (ok) commit(B_KVEMPTY + gslot);
+                    }
+                } else {
+                    // tile 0 takes the even steps, tile 1 the odd ones; the next step's S first: it waits for no softmax
+#pragma unroll 1
+                    for (int j2 = 0; j2 < it.n0 && ok; ++j2) {
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            const int j = 2 * j2 + t;
+                            if (j >= it.n_max) break;
+                            const int grp = kv_base + j + 1, gslot = grp % NGRP;
+                            if (!(ok = wait(B_KVFULL + gslot, (grp / NGRP) & 1))) break;
+                            clear_v(j, 2 * gslot);
+                            if (j + 1 < it.n_max) {
+                                if (j == 0 && !(ok = wait(B_QFULL + 1, uses[1] & 1))) break;
+                                tc_fence_after_sync();
+                                do_s(t ^ 1, j2 + t, gslot);
+                            }
+                            if (!(ok = do_pv(t, j2, gslot))) break;
+                            commit(B_KVEMPTY + gslot);
                         }
                     }
-                    if (ok) commit(B_KVEMPTY + gslot);
                 }
                 kv_base += it.n_max + 1;
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    it_base[t] += it.n(t) > 0 ? it.n(t) : 0;
+                    it_base[t] += it.n(t);
                     uses[t] += it.n(t) > 0 ? 1 : 0;
                 }
             }
-        } else if (!PREFIX && warp == 10 && blockIdx.x == 0) {
-            // lengths that are out of range (of a prefix call the second kernel reports them)
-            for (int u = lane; u < p.units; u += 32) {
-                const int len = __ldg(p.seq_lens + u), new_tokens = __ldg(p.starts + u + 1) - __ldg(p.starts + u);
-                if (len > p.max_len || (len > 0 && new_tokens > len)) report_bad_index(p.status);
+        } else {
+            // =========================== checks, plans ===========================
+            if constexpr (PREFIX) {
+                // where the partial results of each sequence's rows will lie, a lane per sequence: by the CTAs that have no lists
+                Walk<true> walk;
+                const int64_t total = walk.total(p, lane);
+                const int ctas = walk.ctas(p, total, lane), free = ctas < p.grid ? ctas : 0, stride = p.grid - free;
+                const int first = static_cast<int>(blockIdx.x) - free;
+                if (first == 0 && lane == 0) p.plan[p.tokens] = PrefixPlan{total, ctas, 0, 0};
+                for (int b0 = first; first >= 0 && b0 < p.tokens; b0 += 32 * stride) {
+                    const int b = b0 + lane * stride, g = b < p.tokens ? attn_paged::group_of(p.starts, p.units, b) : -1;
+                    int64_t start = __shfl_sync(0xffffffffu, walk.before, g < 0 ? 0 : g / walk.per);
+                    PrefixPlan plan = {0, 0, 0, 0};
+                    if (g >= 0) {
+                        Unit<true> unit;
+                        for (int x = g / walk.per * walk.per; x < g; ++x) {
+                            unit.load(p, x);
+                            start += p.Hkv * unit.head_weight(p);
+                        }
+                        unit.load(p, g);
+                        const int token = b - unit.tok0, pair = token / (2 * p.tile_tokens), in_pair = token - pair * 2 * p.tile_tokens;
+                        if (token >= 0 && token < unit.n) {
+                            const int t = in_pair >= p.tile_tokens ? 1 : 0;
+                            plan.start = start + unit.weight_before(p, pair) + kListCost;
+                            plan.stride = unit.head_weight(p);
+                            plan.steps = unit.pair_steps(p, pair);
+                            plan.row = t * 128 + (in_pair - t * p.tile_tokens) * p.group;
+                        }
+                    }
+                    if (b < p.tokens) p.plan[b] = plan;
+                }
+            } else {
+                // lengths that are out of range (of a prefix call the second kernel reports them)
+                for (int u = static_cast<int>(blockIdx.x) * 32 + lane; u < p.units; u += 32 * gridDim.x) {
+                    const int len = __ldg(p.seq_lens + u), new_tokens = __ldg(p.starts + u + 1) - __ldg(p.starts + u);
+                    if (len > p.max_len || (len > 0 && new_tokens > len)) report_bad_index(p.status);
+                }
             }
         }
     } else {
@@ -602,9 +768,9 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         const uint32_t lane_off = static_cast<uint32_t>(w4 * 32) << 16;
         const uint32_t tS = tmem + C::s_col(t) + lane_off, tO = tmem + C::o_col(t) + lane_off;
         const float c = p.scale_log2;
-        const int my_token = t * p.tile_tokens + r / p.group, my_head = r % p.group;     // of the pair; of the K/V head
+        const int row_token = r / p.group, my_head = r % p.group;                        // of the tile; of the K/V head
         const uint32_t ost = sOst(t) + w4 * 4096;                                        // this warp's staging: 32 rows x 128 bytes
-        int it_base = 0, uses = 0, kv_base = 0;
+        int it_base = 0, uses = 0, kv_base = 0, merges = 0;
         bool ok = true;
         for (int k = 0; ok; ++k) {
             Item it;
@@ -612,6 +778,7 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             const int n = it.n(t), group0 = kv_base;
             kv_base += it.n_max + 1;
             if (n <= 0) continue;
+            const int my_token = it.twin ? row_token : t * p.tile_tokens + row_token;
             const bool live = r < tile_rows && my_token < it.n_tok;
             // last key that this row sees; rows without a token ask for no mask
             int lim = 0;
@@ -638,10 +805,10 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     mbar_arrive(bar(B_PFULL2 + t));
                     continue;
                 }
-                const int kv0 = (it.tile0 + j) * 128;
-                const volatile uint32_t* bad = bad_ring + ((group0 + j) & 7) * 8;
-                const bool some_bad = bad[0] != 0;
-                if (kv0 + 127 > lim_lo || some_bad) {
+                const int step = it.twin ? 2 * j + t : j, kv0 = (it.tile0 + step) * 128;
+                const volatile uint32_t* bad = bad_ring + ((group0 + step) & 7) * 8;
+                const bool some_bad = __any_sync(0xffffffffu, bad[0] != 0);
+                if (__any_sync(0xffffffffu, kv0 + 127 > lim_lo || some_bad)) {
                     // hidden scores become -inf in tensor memory, so that masked tiles run the code of all others
 #pragma unroll 1
                     for (int ch = 0; ch < 4; ++ch) {
@@ -761,75 +928,103 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             if (!(ok = wait(B_OFINAL + t, uses & 1))) break;
             ++uses;
             tc_fence_after_sync();
+            // Twins: tile 1's group hands over its reference and sum, and tile 0's adds up both accumulators.
+            const bool both = it.twin && it.n1 > 0;
+            float f1 = 0.f, f0 = 1.f;
+            if (both) {
+                if (t == 1) {
+                    merge[r] = make_float2(m, l);
+                    tc_fence_before_sync();
+                    mbar_arrive(bar(B_MERGE));
+                    continue;
+                }
+                if (!(ok = wait(B_MERGE, merges & 1))) break;
+                ++merges;
+                tc_fence_after_sync();
+                const float2 other = merge[r];
+                const float top = l > 0.f ? (other.y > 0.f ? fmaxf(m, other.x) : m) : other.x;
+                f0 = l > 0.f ? ex2_approx((m - top) * c) : 0.f;
+                f1 = other.y > 0.f ? ex2_approx((other.x - top) * c) : 0.f;
+                l = fmaf(f0, l, f1 * other.y);
+                m = top;
+            }
             const bool final_rows = !PREFIX && it.slot < 0;
             const bool seen = l > 0.f;                     // false: no visible key in this share
-            const float inv = final_rows ? (seen ? 1.f / l : 0.f) : 1.f;
-            // row of [tokens][H] that each of this warp's rows is, from the lane that has the row
-            const int64_t out_row = static_cast<int64_t>(it.tok + my_token) * p.H + it.kvh * p.group + my_head;
-            float* part = p.parts + it.slot * part_floats(D) + (t * 128 + w4 * 32) * D;
+            // this row of [tokens][H]
+            const int out_row = live ? (it.tok + my_token) * p.H + it.kvh * p.group + my_head : -1;
+            float* part = p.parts + it.slot * part_floats(D);
             if (live) {
                 if (final_rows) {
                     p.lse[out_row] = seen ? fmaf(m, p.scale, logf(l)) : -INFINITY;
                 } else {
-                    float2* ml = reinterpret_cast<float2*>(it.slot < 0 ? p.rows + static_cast<int64_t>(p.tokens) * p.H * D + 2 * out_row
-                                                                       : p.parts + it.slot * part_floats(D) + kRows * D + 2 * (t * 128 + r));
+                    float2* ml = reinterpret_cast<float2*>(it.slot < 0 ? p.rows + static_cast<int64_t>(p.tokens) * p.H * D + 2 * static_cast<int64_t>(out_row)
+                                                                       : part + kRows * D + 2 * (t * 128 + r));
                     *ml = make_float2(fmaf(m, c, P_OFF), l);
                 }
             }
-            // 32 rows of 128 bytes: a quarter of a warp per row
-            auto leave = [&](int round, const uint32_t (&v)[32]) {
-                __syncwarp();
+            if (final_rows) {
+                const float inv = seen ? 1.f / l : 0.f;
+                f0 *= inv;
+                f1 *= inv;
+            }
+            // Rows leave 128 bytes at a time, a quarter of a warp per row: row 4 x + lane / 8 goes to to + at[x] * row_bytes.
+            uint8_t* to = (final_rows ? static_cast<uint8_t*>(p.o) : reinterpret_cast<uint8_t*>(it.slot < 0 ? p.rows : part)) + (lane & 7) * 16;
+            const int row_bytes = final_rows ? 2 * D : 4 * D;
+            int at[8];
 #pragma unroll
-                for (int g = 0; g < 8; ++g)
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ost + lane * 128 + ((g ^ (lane & 7)) << 4)), "r"(v[4 * g]), "r"(v[4 * g + 1]),
-                                 "r"(v[4 * g + 2]), "r"(v[4 * g + 3])
-                                 : "memory");
+            for (int x = 0; x < 8; ++x) {
+                const int row = 4 * x + (lane >> 3), other = __shfl_sync(0xffffffffu, out_row, row);
+                at[x] = it.slot < 0 ? other : t * 128 + w4 * 32 + row;
+            }
+            auto stage = [&](int piece, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ost + lane * 128 + ((piece ^ (lane & 7)) << 4)), "r"(a), "r"(b), "r"(c), "r"(d)
+                             : "memory");
+            };
+#pragma unroll 1
+            for (int col = 0; col < D; col += 32) {
+                float o[32];
+                {
+                    uint32_t a[32];
+                    tmem_ld_32x32b_x32(tO + col, a);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(a[e]) * f0;
+                    if (both) {
+                        tmem_ld_32x32b_x32(tO + D + col, a);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = fmaf(__uint_as_float(a[e]), f1, o[e]);
+                    }
+                }
+                if (col + 32 == D) {                       // O is in registers
+                    tc_fence_before_sync();
+                    mbar_arrive(bar(B_OFREE + t));
+                    if (both) mbar_arrive(bar(B_OFREE + 1));
+                }
+                if (final_rows) {
+                    const int half = (col >> 3) & 4;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+                        stage(half + g, pack2<DTYPE>(o[8 * g], o[8 * g + 1]), pack2<DTYPE>(o[8 * g + 2], o[8 * g + 3]), pack2<DTYPE>(o[8 * g + 4], o[8 * g + 5]),
+                              pack2<DTYPE>(o[8 * g + 6], o[8 * g + 7]));
+                    if (half == 0) continue;
+                } else {
+#pragma unroll
+                    for (int g = 0; g < 8; ++g)
+                        stage(g, __float_as_uint(o[4 * g]), __float_as_uint(o[4 * g + 1]), __float_as_uint(o[4 * g + 2]), __float_as_uint(o[4 * g + 3]));
+                }
                 __syncwarp();
+                uint4 w[8];
 #pragma unroll
                 for (int x = 0; x < 8; ++x) {
-                    const int row = 4 * x + (lane >> 3), g = lane & 7;
-                    const int64_t to = __shfl_sync(0xffffffffu, out_row, row);
-                    const bool write = __shfl_sync(0xffffffffu, live ? 1 : 0, row) != 0;
-                    const uint4 w = attn_paged::lds128(ost + row * 128 + ((g ^ (row & 7)) << 4));
-                    if (write) {
-                        uint8_t* dst;
-                        if (final_rows)
-                            dst = static_cast<uint8_t*>(p.o) + to * (2 * D);
-                        else if (it.slot < 0)
-                            dst = reinterpret_cast<uint8_t*>(p.rows + to * D);
-                        else
-                            dst = reinterpret_cast<uint8_t*>(part + row * D);
-                        *reinterpret_cast<uint4*>(dst + round * 128 + g * 16) = w;
-                    }
+                    const int row = 4 * x + (lane >> 3);
+                    w[x] = attn_paged::lds128(ost + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
                 }
-            };
-            if (final_rows) {
-#pragma unroll 1
-                for (int h = 0; h < D / 64; ++h) {
-                    uint32_t orr[64], v[32];
-                    tmem_ld_32x32b_x32(tO + h * 64, orr);
-                    tmem_ld_32x32b_x32(tO + h * 64 + 32, orr + 32);
-                    tmem_ld_wait();
-                    if (h == D / 64 - 1) {
-                        tc_fence_before_sync();
-                        mbar_arrive(bar(B_OFREE + t));
-                    }
+                __syncwarp();
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) v[e] = pack2<DTYPE>(__uint_as_float(orr[2 * e]) * inv, __uint_as_float(orr[2 * e + 1]) * inv);
-                    leave(h, v);
-                }
-            } else {
-#pragma unroll 1
-                for (int h = 0; h < D / 32; ++h) {
-                    uint32_t v[32];
-                    tmem_ld_32x32b_x32(tO + h * 32, v);
-                    tmem_ld_wait();
-                    if (h == D / 32 - 1) {
-                        tc_fence_before_sync();
-                        mbar_arrive(bar(B_OFREE + t));
-                    }
-                    leave(h, v);
-                }
+                for (int x = 0; x < 8; ++x)
+                    if (at[x] >= 0) *reinterpret_cast<uint4*>(to + static_cast<int64_t>(at[x]) * row_bytes) = w[x];
+                to += 128;
             }
         }
     }
@@ -843,38 +1038,22 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
 }
 
 // Joins the partial results of prefill lists that were cut: block (c, y) takes rows of the list whose first border is the one
-// between CTAs c and c + 1.  A warp per row.
+// between CTAs c and c + 1 (its last list, and the first of the others).  A warp per row.
 template <int D, int DTYPE>
 __global__ void __launch_bounds__(attn_paged::kJoinWarps * 32)
 attn_paged_prefill_join_kernel(const __grid_constant__ Params p) {
     constexpr float P_OFF = attn_paged::ExpRange<DTYPE>::P_OFF;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c0 = blockIdx.x;
-    int64_t mine, before;
-    const int64_t total = Walk<false>::total(p, lane, mine, before);
-    const int ctas = cta_count(total, p.grid);
-    Walk<false> walk;
-    const int64_t border = cta_begin(total, c0 + 1, ctas);
-    bool work = c0 + 1 < ctas;
-    if (work) {
-        walk.find(p, lane, border, mine, before);
-        // a border between two lists cuts none; of several borders in one list the first one's block joins it
-        work = walk.step > 0 && border - walk.step >= cta_begin(total, c0, ctas);
-    }
+    const int lane = threadIdx.x & 31, c0 = blockIdx.x;
+    const int row = blockIdx.y * attn_paged::kJoinWarps + (threadIdx.x >> 5), t = row >> 7, r = row & 127;
+    const int in_tile = r / p.group, token = t * p.tile_tokens + in_tile;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (!work) return;
-    const int64_t start = border - walk.step;
-    const int pair_tok = walk.i * 2 * p.tile_tokens;
-    for (int row = blockIdx.y * attn_paged::kJoinWarps + warp; row < kRows; row += gridDim.y * attn_paged::kJoinWarps) {
-        const int t = row >> 7, r = row & 127, token = t * p.tile_tokens + r / p.group;
-        if (r >= p.tile_tokens * p.group || pair_tok + token >= walk.unit.n) continue;
-        const int64_t end = start + walk.unit.steps_of(pair_tok + (t + 1) * p.tile_tokens);        // of this tile
-        const int n = cta_of_tile(total, end - 1, ctas) - c0 + 1;
-        const int64_t out_row = static_cast<int64_t>(walk.unit.tok0 + pair_tok + token) * p.H + walk.h * p.group + r % p.group;
-        // the list is the last of c0's part, and the first of the others'
-        auto part = [&](int i) { return p.parts + (2 * (c0 + i) + (i == 0 ? 1 : 0)) * part_floats(D); };
-        attn_paged::join_row<D, DTYPE>(n, lane, P_OFF, [&](int i) { return reinterpret_cast<const float2*>(part(i) + kRows * D) + row; },
-                                       [&](int i) { return part(i) + row * D; }, static_cast<uint8_t*>(p.o) + out_row * (2 * D), p.lse + out_row);
-    }
+    const Cut* cut = p.cuts + c0;
+    const int n = __ldcg(cut->parts + t), tok = __ldcg(&cut->tok), n_tok = __ldcg(&cut->n_tok), kvh = __ldcg(&cut->kvh);
+    if (n == 0 || in_tile >= p.tile_tokens || token >= n_tok) return;
+    const int64_t out_row = static_cast<int64_t>(tok + token) * p.H + kvh * p.group + r - in_tile * p.group;
+    auto part = [&](int i) { return p.parts + (2 * (c0 + i) + (i == 0 ? 1 : 0)) * part_floats(D); };
+    attn_paged::join_row<D, DTYPE>(n, lane, P_OFF, [&](int i) { return reinterpret_cast<const float2*>(part(i) + kRows * D) + row; },
+                                   [&](int i) { return part(i) + row * D; }, static_cast<uint8_t*>(p.o) + out_row * (2 * D), p.lse + out_row);
 }
 
 // Joins what the two kernels of a call with shared prefixes have left for each row: the parts of its sequence's own keys
@@ -884,42 +1063,24 @@ __global__ void __launch_bounds__(attn_paged::kJoinWarps * 32)
 attn_paged_prefix_join_kernel(const __grid_constant__ attn_paged::DecodeParams p, const __grid_constant__ Params pre, int blocks_per_seq) {
     using C = attn_paged::DecodeCfg<D, GH>;
     constexpr float P_OFF = attn_paged::ExpRange<DTYPE>::P_OFF;
-    __shared__ int64_t red[4][attn_paged::kJoinWarps];
     const int b = blockIdx.x / blocks_per_seq, lane = threadIdx.x & 31;
     const int q_head = (blockIdx.x - b * blocks_per_seq) * attn_paged::kJoinWarps + (threadIdx.x >> 5);
-    const attn_paged::JoinList<D, GH, true> list(p, b, red);
-    // where the prefix's parts lie: the steps in front of the group's, then those of the row's list
-    int64_t mine, before;
-    const int64_t total = Walk<true>::total(pre, lane, mine, before);
-    const int ctas = cta_count(total, pre.grid), g = attn_paged::group_of(pre.starts, pre.units, b);
-    const int64_t out_row = static_cast<int64_t>(b) * p.H + q_head;
-    int n_pre = 0, c0 = 0, c1 = 0, row = 0;
-    if (g >= 0 && q_head < p.H) {
-        const int per = (pre.units + 31) / 32;
-        int64_t start = __shfl_sync(0xffffffffu, before, g / per);
-        Unit<true> unit;
-        for (int x = g / per * per; x < g; ++x) {
-            unit.load(pre, x);
-            start += pre.Hkv * unit.head_steps(pre);
-        }
-        unit.load(pre, g);
-        const int token = b - unit.tok0, pair = token / (2 * pre.tile_tokens), in_pair = token - pair * 2 * pre.tile_tokens;
-        if (token >= 0 && token < unit.n) {
-            const int kvh = q_head / pre.group, t = in_pair >= pre.tile_tokens ? 1 : 0;
-            row = t * 128 + (in_pair - t * pre.tile_tokens) * pre.group + q_head - kvh * pre.group;
-            start += kvh * unit.head_steps(pre) + unit.steps_before(pre, pair);
-            const int64_t end = start + unit.pair_steps(pre, pair);
-            if (end <= total) {
-                c0 = cta_of_tile(total, start, ctas);
-                c1 = cta_of_tile(total, end - 1, ctas);
-                n_pre = c1 - c0 + 1;
-            }
-        }
-    }
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (q_head >= p.H) return;
+    const int64_t out_row = static_cast<int64_t>(b) * p.H + q_head;
     uint8_t* out = static_cast<uint8_t*>(p.o) + out_row * D * 2;
     const int64_t n_rows = static_cast<int64_t>(p.B) * p.H;
+    const PrefixPlan* plan = pre.plan + b;
+    const int64_t total = __ldcg(&pre.plan[p.B].start), ctas = __ldcg(&pre.plan[p.B].stride);
+    const int64_t first = __ldcg(&plan->start), stride = __ldcg(&plan->stride);
+    const int steps = __ldcg(&plan->steps), kvh = q_head / pre.group, row = __ldcg(&plan->row) + q_head - kvh * pre.group;
+    const attn_paged::SeqPlan list = attn_paged::SeqPlan::read(p, b);
+    int n_pre = 0, c0 = 0;
+    if (steps > 0) {
+        const int64_t start = first + kvh * stride;
+        c0 = cta_of_tile(total, start, static_cast<int>(ctas));
+        n_pre = cta_of_tile(total, start + steps - 1, static_cast<int>(ctas)) - c0 + 1;
+    }
     attn_paged::RowParts own;
     if (list.n > 0) own.find(p, list, q_head);
     const int n_own = own.count;
@@ -927,20 +1088,28 @@ attn_paged_prefix_join_kernel(const __grid_constant__ attn_paged::DecodeParams p
         attn_paged::empty_row<D>(out, p.lse + out_row, lane);
         return;
     }
-    auto own_part = [&](int i) { return own.at<C::PART_FLOATS>(p, i); };
-    auto pre_part = [&](int i) { return pre.parts + (2 * (c0 + i) + (i == 0 ? 1 : 0)) * part_floats(D); };
-    attn_paged::join_row<D, DTYPE>(
-        n_own + n_pre, lane, P_OFF,
-        [&](int i) {
-            const float* at = i < n_own ? (n_own == 1 ? p.rows + n_rows * D + 2 * out_row : own_part(i) + GH * D + 2 * own.row)
-                                        : (n_pre == 1 ? pre.rows + n_rows * D + 2 * out_row : pre_part(i - n_own) + kRows * D + 2 * row);
-            return reinterpret_cast<const float2*>(at);
-        },
-        [&](int i) {
-            return i < n_own ? (n_own == 1 ? p.rows + out_row * D : own_part(i) + own.row * D)
-                             : (n_pre == 1 ? pre.rows + out_row * D : pre_part(i - n_own) + row * D);
-        },
-        out, p.lse + out_row);
+    // Part i of the sequence's own keys and part i of the prefix: the first one's O, and how far the others lie (see RowParts::at and
+    // Item::slot); exponent and sum at a fixed distance.
+    const float *own0 = p.rows + out_row * D, *pre0 = pre.rows + out_row * D;
+    int64_t own_ml = (n_rows - out_row) * D + 2 * out_row, pre_ml = own_ml;
+    const int64_t own_stride = static_cast<int64_t>(C::PART_FLOATS) << own.hs;
+    if (n_own > 1) {
+        own0 = own.at<C::PART_FLOATS>(p, 0) + own.row * D;
+        own_ml = GH * D + 2 * own.row - own.row * D;
+    }
+    if (n_pre > 1) {
+        pre0 = pre.parts + (2 * c0 + 1) * part_floats(D) + row * D;
+        pre_ml = kRows * D + 2 * row - row * D;
+    }
+    auto part = [&](int i) {
+        const int j = i < n_own ? i : i - n_own;
+        const int64_t stride = i < n_own ? own_stride : part_floats(D);
+        const int away = j == 0 ? 0 : 2 * j - (i < n_own ? (own.odd ? 1 : 0) : 1);
+        return (i < n_own ? own0 : pre0) + away * stride;
+    };
+    attn_paged::join_row<D, DTYPE>(n_own + n_pre, lane, P_OFF,
+                                   [&](int i) { return reinterpret_cast<const float2*>(part(i) + (i < n_own ? own_ml : pre_ml)); }, part, out,
+                                   p.lse + out_row);
 }
 
 }  // namespace attn_paged_tc

@@ -45,11 +45,13 @@ def test_validation(lib):
 
 
 def test_workspaces(lib):
-    # two partial results of 256 rows per SM
-    assert lib.attn_paged_prefill_workspace_bytes(128) == 2 * 148 * 256 * 130 * 4 and lib.attn_paged_prefill_workspace_bytes(64) == 2 * 148 * 256 * 66 * 4
+    up = lambda n: (n + 255) // 256 * 256
+    # two partial results of 256 rows per SM, and what the joining kernels read beside them
+    assert lib.attn_paged_prefill_workspace_bytes(128) == 2 * 148 * 256 * 130 * 4 + up(148 * 20) and lib.attn_paged_prefill_workspace_bytes(64) == 2 * 148 * 256 * 66 * 4 + up(148 * 20)
     assert lib.attn_paged_prefill_workspace_bytes(256) == 0
     b = lib.attn_paged_prefix_decode_workspace_bytes
-    assert b(64, 32, 8, 128) == lib.attn_paged_decode_workspace_bytes(32, 8, 128) + 2 * 64 * 32 * 130 * 4 + 2 * 148 * 256 * 130 * 4
+    rows, plan, prefix_plan = up(64 * 32 * 130 * 4), up(65 * 16), up(65 * 24)
+    assert b(64, 32, 8, 128) == lib.attn_paged_decode_workspace_bytes(32, 8, 128) + 2 * rows + plan + prefix_plan + 2 * 148 * 256 * 130 * 4
     assert b(-1, 32, 8, 128) == 0 and b(4, 3, 2, 64) == 0 and b(4, 4, 2, 256) == 0
 
 

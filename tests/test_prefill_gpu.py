@@ -158,12 +158,19 @@ def test_prefill_of_a_cache_above_4_gigaelements():
     cu, lens = torch.tensor([0, 70], dtype=torch.int32).cuda(), torch.tensor([n], dtype=torch.int32).cuda()
     o, lse = api.attn_paged_prefill(q, kc, vc, tab.cuda(), lens, cu, 0.09)
     check_prefill(o, lse, q, k, v, 0.09, dt)
-    o, lse = api.attn_paged_prefix_decode(q[-1:], kc, vc, tab.cuda(), lens, torch.tensor([0, 1], dtype=torch.int32).cuda(),
+    o, lse = api.attn_paged_prefix_decode(q[-1:], kc, vc, wide(tab, page, Hkv, D).cuda(), lens, torch.tensor([0, 1], dtype=torch.int32).cuda(),
                                           torch.tensor([150], dtype=torch.int32).cuda(), 0.09)
     check_prefill(o, lse, q[-1:], k, v, 0.09, dt)
 
 
 # ------------------------------------------------------------------ shared prefixes
+
+def wide(tab, page, Hkv, D):
+    """The table with as many columns of no page as it takes for the call to share prefixes: below 128 MB of keys and values that it
+    could stand for, all is read for every sequence (attn_paged_decode)."""
+    columns = -(-2 ** 27 // (tab.shape[0] * page * Hkv * D * 4))
+    return torch.cat([tab, torch.full((tab.shape[0], columns), -1, dtype=torch.int32)], 1)
+
 
 def make_shared(lens, starts, prefix, Hkv, D, page, dt, layout, seed):
     """make_cache with the first prefix[g] keys of the sequences of group g in common: whole pages shared, the rest copied."""
@@ -195,7 +202,7 @@ def run_prefix(lens, starts, prefix, H, Hkv, D, page, kind, layout="head", seed=
     q = torch.randn(len(lens), H, D, generator=torch.Generator().manual_seed(seed + 100)).to(dt).cuda()
     scale = 1 / math.sqrt(D) if scale is None else scale
     i32 = lambda x: torch.tensor(x, dtype=torch.int32).cuda()
-    args = (q, kc, vc, tab.cuda(), i32(lens), i32(starts), i32(prefix), scale)
+    args = (q, kc, vc, wide(tab, page, Hkv, D).cuda(), i32(lens), i32(starts), i32(prefix), scale)
     o, lse = api.attn_paged_prefix_decode(*args)
     assert api.attn_last_device_status() == 0
     check_prefix(o, lse, q, ks, vs, scale, dt)
@@ -244,6 +251,7 @@ def test_prefix_bad_pages_lengths_and_groups():
     D, page, dt = 64, 16, torch.float16
     lens = [200, 300, 250]
     kc, vc, tab, ks, vs = make_shared(lens, [0, 3], [160], 2, D, page, dt, "head", 9)
+    tab = wide(tab, page, 2, D)
     q = torch.randn(3, 4, D, generator=torch.Generator().manual_seed(1)).to(dt).cuda()
     i32 = lambda x: torch.tensor(x, dtype=torch.int32).cuda()
     bad = tab.clone()
@@ -268,8 +276,12 @@ def test_prefix_without_groups_is_the_decode():
     q = torch.randn(3, 8, 64, generator=torch.Generator().manual_seed(2)).half().cuda()
     lens = torch.tensor([300, 0, 77], dtype=torch.int32).cuda()
     none = torch.zeros(0, dtype=torch.int32).cuda()
-    a = api.attn_paged_prefix_decode(q, kc, vc, tab.cuda(), lens, torch.zeros(1, dtype=torch.int32).cuda(), none, 0.125)
     b = api.attn_paged_decode(q, kc, vc, tab.cuda(), lens, 0.125)
+    a = api.attn_paged_prefix_decode(q, kc, vc, tab.cuda(), lens, torch.zeros(1, dtype=torch.int32).cuda(), none, 0.125)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    # few keys in all: nothing is shared either
+    a = api.attn_paged_prefix_decode(q, kc, vc, tab.cuda(), lens, torch.tensor([0, 1], dtype=torch.int32).cuda(),
+                                     torch.tensor([200], dtype=torch.int32).cuda(), 0.125)
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
@@ -280,7 +292,7 @@ def test_captured_calls_replayed_with_other_lengths_beside_eager_ones():
     lens, starts, prefix = [600, 700, 650, 900], [0, 3, 4], [512, 100]
     kc, vc, tab, ks, vs = make_shared(lens, starts, prefix, Hkv, D, page, dt, "head", 20)
     i32 = lambda x: torch.tensor(x, dtype=torch.int32).cuda()
-    lens_t, starts_t, prefix_t, cu, table_ = i32(lens), i32(starts), i32(prefix), i32([0, 40, 80, 120, 160]), tab.cuda()
+    lens_t, starts_t, prefix_t, cu, table_ = i32(lens), i32(starts), i32(prefix), i32([0, 40, 80, 120, 160]), wide(tab, page, Hkv, D).cuda()
     g = torch.Generator().manual_seed(21)
     q, qp = torch.randn(4, H, D, generator=g).to(dt).cuda(), torch.randn(160, H, D, generator=g).to(dt).cuda()
     ws = torch.empty(api.attn_paged_prefix_decode_workspace_bytes(4, H, Hkv, D), dtype=torch.uint8, device="cuda")
@@ -329,7 +341,7 @@ def test_serving_step_with_images_behind_a_shared_instruction():
     bt[:, :5] = order[:5]                                                   # 80 tokens in 5 shared pages
     for b in range(3):
         bt[b, 5:14] = order[5 + 9 * b:14 + 9 * b]
-    bt = bt.cuda()
+    bt = wide(bt, page, Hkv, D).cuda()
     qw, kw = ((1 + 0.2 * torch.randn(D, generator=g)).to(dt).cuda() for _ in range(2))
     made_k, made_v, made_q = [], [], []
 

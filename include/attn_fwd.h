@@ -454,6 +454,9 @@ size_t attn_paged_prefill_workspace_bytes(int D);
  *            group's first sequence has keys, and a sequence that is shorter sees the keys that it has.  n_groups == 0: attn_paged_decode.
  * H / Hkv <= 128; D in {64, 128}.  The other arguments as in attn_paged_decode.  P is rounded to the 16-bit type before its
  * product for the common keys.
+ * Where the table is small (B * max_pages * page_size * Hkv * D * 4 bytes of keys and values, were every sequence that long, are
+ * less than 128 MiB) the call is attn_paged_decode, which is then faster: pass the table's used columns (table_stride says where the
+ * next row begins), not the width that the longest sequence ever may need.
  * workspace: device, 256-byte aligned, at least attn_paged_prefix_decode_workspace_bytes(B, H, Hkv, D) bytes, or ATTN_ERR_WORKSPACE.
  *            Two calls that may run at the same time need one each.
  */

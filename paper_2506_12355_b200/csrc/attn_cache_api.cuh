@@ -594,6 +594,7 @@ bool launch_paged_tc(attn_paged_tc::Params& p, const void* q, const void* k_cach
     p.Hkv = Hkv;
     p.group = H / Hkv;
     p.tile_tokens = 128 / p.group;
+    p.twin_weight = D == 64 ? 1 : 2;
     p.max_len = max_pages * page_size;
     p.num_pages = num_pages;
     p.page_shift = log2_of(page_size);

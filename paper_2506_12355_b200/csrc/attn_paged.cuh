@@ -156,8 +156,6 @@ __device__ __forceinline__ int prefix_of(const int* starts, const int* prefix_le
 // the first one's surplus CTAs leave at once): the first is bound by its tensor-core pipeline's latencies, the second by memory.
 // Each works the parts out for itself from the lengths, in whole numbers, so both find the same.
 //
-// What a list of attn_paged_tc.cuh costs beside its steps (Q, first scores, the way out), in steps.  Its even cut counts it too.
-constexpr int kListCost = 3;
 // What a group's lists take of one CTA, in ns: a step of one tile, and by itself each list (its fill and way out, beside a busy memory).
 constexpr int kTileStepNs = 1100, kListNs = 8000;
 __device__ __forceinline__ int64_t group_cost(const int* starts, const int* prefix_lens, const int* seq_lens, int g, int B, int max_len, int Hkv,
@@ -167,8 +165,8 @@ __device__ __forceinline__ int64_t group_cost(const int* starts, const int* pref
     end = end < first ? first : (end > B ? B : end);
     const int n = end - first, prefix = n > 0 ? group_prefix(seq_lens, first, __ldg(prefix_lens + g), max_len) : 0;
     if (prefix <= 0) return 0;
-    const int pairs = (n + 2 * tile_tokens - 1) / (2 * tile_tokens);
-    return static_cast<int64_t>(Hkv) * pairs * (static_cast<int64_t>((prefix + 127) / 128) * (n > tile_tokens ? 2 * kTileStepNs : kTileStepNs) + kListNs);
+    const int pairs = (n + 2 * tile_tokens - 1) / (2 * tile_tokens), tiles = 2 * pairs - (n - (pairs - 1) * 2 * tile_tokens <= tile_tokens ? 1 : 0);
+    return Hkv * (static_cast<int64_t>((prefix + 127) / 128) * tiles * kTileStepNs + static_cast<int64_t>(pairs) * kListNs);
 }
 // CTAs of the first kernel out of `grid`, for lists that take `cost` ns, and own_bytes of keys and values of `pairs` pairs of a sequence and
 // a group of heads for the second one.

@@ -9,11 +9,11 @@
 //
 // A list is one K/V head and a pair of 128-row tiles of queries; row r of a tile is query head r % G of the K/V head's G, of token
 // r / G (128 / G tokens to a tile, rounded down), which a TMA box brings in that order from [token][head][D].  Its steps are the
-// 128-key tiles that its last token sees.  The steps of all lists, one after the other and each list with kListCost steps more for its
-// fill and way out, are cut evenly over one CTA per SM, whatever the lengths are (each CTA works out its own part from the device-side
-// lengths: no host copy, no plan to keep); a list that a border cuts leaves a partial result per CTA (at most two per CTA, fp32),
-// which a second kernel joins in a fixed order.  (Without kListCost 8 prompts of 100 - 4000 tokens, 16 heads of 64, take 261 us instead
-// of 241, prompts of up to 2000 tokens with 32 heads over 8 of 128 195 instead of 166.)
+// 128-key tiles that its last token sees.  The steps of all lists, one after the other, each weighted by what it takes and each list
+// with kListCost more for its fill and way out, are cut evenly over one CTA per SM, whatever the lengths are (each CTA works out its own
+// part from the device-side lengths: no host copy, no plan to keep); a list that a border cuts leaves a partial result per CTA (at most
+// two per CTA, fp32), which a second kernel joins in a fixed order.  (8 prompts of 100 - 4000 tokens, 16 heads of 64: 230 us; without
+// kListCost 260, with all steps alike 243.  Prompts of up to 2000 tokens, 32 heads over 8 of 128: 172; without kListCost 197.)
 //
 // Inside a CTA it is the pipeline of attn_tc_pipe.cuh: TMA ring of K/V tiles, one MMA-issuing warp, two softmax groups in
 // ping-pong, P back into tensor memory as the second product's operand, a lagging reference maximum.  What paging adds:
@@ -42,11 +42,11 @@ using attn_paged::cta_count;
 using attn_paged::cta_of_tile;
 using attn_paged::divide;
 using attn_paged::group_prefix;
-using attn_paged::kListCost;
 using attn_paged::report_bad_index;
 using attn_tc::low_bits;
 
 constexpr int kRows = 256;                        // rows of a list: two tiles
+constexpr int kListCost = 4;                      // what a list costs beside its steps (see step_weight), about 4 us
 
 template <int D>
 struct Cfg {
@@ -71,7 +71,8 @@ struct Cut { int parts[2], tok, n_tok, kvh; };     // partial results of each ti
 struct PrefixPlan {
     int64_t start, stride;      // where step 0 of the sequence's list of K/V head 0 lies, and weight per head.  Behind the last sequence: the
                                 // weight of all lists, and the CTAs that share it
-    int steps, row;             // steps of a list (0: no common keys); row of query head 0 of a K/V head
+    int64_t span;               // from step 0 to the last one (-1: no common keys)
+    int row;                    // row of query head 0 of a K/V head
 };
 
 struct Params {
@@ -88,6 +89,7 @@ struct Params {
     int64_t table_stride;
     int units, tokens;          // sequences and their new tokens; groups and sequences
     int H, Hkv, group, tile_tokens;
+    int twin_weight;            // of a step of one tile
     int max_len, num_pages, page_shift, box_shift, k_axes, v_axes;
     float scale, scale_log2;
     int row_bytes, head_groups; // prefix: of a key, K and V of all heads; groups of heads of a pair of the other kernel
@@ -156,23 +158,29 @@ struct Unit {
         return ((base > 0 ? base : 0) + (tokens < n ? tokens : n) - 1) / 128 + 1;
     }
     __device__ __forceinline__ int pair_steps(const Params& p, int i) const { return steps_of((i + 1) * 2 * p.tile_tokens); }
-    // steps of the pairs before i
-    __device__ __forceinline__ int64_t steps_before(const Params& p, int i) const {
-        if (PREFIX) return static_cast<int64_t>(i) * ((len + 127) >> 7);
-        const int t2 = 2 * p.tile_tokens, full = i < pairs ? i : pairs - 1;
-        if (i == 0) return 0;
-        return floor_sum(full, t2, static_cast<uint32_t>(base > 0 ? base : 0) + t2 - 1) + full + (i == pairs ? steps_of(n) : 0);
+    // Weights, in units of about 1 us: a step of two tiles counts 2, one of one tile (the last pair may have no more) as much at D = 128,
+    // where it waits for the same K and V (with weight 1 32 prompts of 10 - 200 tokens behind 4096, 32 heads over 8: 330 us instead of
+    // 277), and 1 at D = 64; each list counts kListCost more.
+    __device__ __forceinline__ int step_weight(const Params& p, int i) const {
+        return i == pairs - 1 && n - i * 2 * p.tile_tokens <= p.tile_tokens ? p.twin_weight : 2;
     }
-    __device__ __forceinline__ int64_t weight_before(const Params& p, int i) const { return steps_before(p, i) + static_cast<int64_t>(i) * kListCost; }
+    __device__ __forceinline__ int64_t weight_before(const Params& p, int i) const {
+        const int t2 = 2 * p.tile_tokens, full = i < pairs ? i : pairs - 1;      // the last pair has a weight of its own
+        if (i == 0) return 0;
+        const int64_t steps = PREFIX ? static_cast<int64_t>(full) * ((len + 127) >> 7)
+                                     : floor_sum(full, t2, static_cast<uint32_t>(base > 0 ? base : 0) + t2 - 1) + full;
+        return 2 * steps + static_cast<int64_t>(i) * kListCost + (i == pairs ? static_cast<int64_t>(step_weight(p, i - 1)) * steps_of(n) : 0);
+    }
     __device__ __forceinline__ int64_t head_weight(const Params& p) const { return weight_before(p, pairs); }
 };
 
-// Position in the lists: unit, K/V head, pair, step of the pair's list (below 0: in what the list costs beside its steps).  All lanes of
-// a warp hold the same one.
+// Position in the lists: unit, K/V head, pair, and how far into the pair's list in weights (what the list costs beside its steps comes
+// first; a step belongs to whom its first weight does).  All lanes of a warp hold the same one.
 template <bool PREFIX>
 struct Walk {
     Unit<PREFIX> unit;
-    int u, h, i, step, steps;
+    int u, h, i, steps, weight;
+    int64_t at;
     int64_t mine, before;      // weight of this lane's units (consecutive ones) and of those in front of them
     int per, first;            // units of a lane, and this lane's first
     // Total weight of all lists; all 32 lanes.
@@ -211,13 +219,14 @@ struct Walk {
             }
             n = attn_paged::prefix_ctas(attn_paged::warp_sum(cost), attn_paged::warp_sum(own) * p.row_bytes, attn_paged::warp_sum(seqs) * p.head_groups, p.grid);
         }
-        return cta_count(total, n);
+        // (a CTA's part holds the beginning of a step: two weights at least)
+        return cta_count(total / 2, n);
     }
-    // Position `at` of all (below the total), after total().
-    __device__ __forceinline__ void find(const Params& p, int lane, int64_t at) {
-        const bool here = at >= before && at < before + mine;
+    // Position `pos` of all (below the total), after total().
+    __device__ __forceinline__ void find(const Params& p, int lane, int64_t pos) {
+        const bool here = pos >= before && pos < before + mine;
         const int owner = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
-        int64_t rem = at - before;
+        int64_t rem = pos - before;
         int x = first;
         if (here && per > 1)
             for (;; ++x) {
@@ -232,7 +241,7 @@ struct Walk {
         const int64_t per_head = unit.head_weight(p);
         h = static_cast<int>(divide(rem, per_head));
         rem -= h * per_head;
-        // the last pair with steps_before <= rem, 32 candidates at a time
+        // the last pair with weight_before <= rem, 32 candidates at a time
         int lo = 0, hi = unit.pairs;
         while (hi - lo > 1) {
             const int stride = (hi - lo + 31) / 32, mid = lo + lane * stride;
@@ -241,12 +250,19 @@ struct Walk {
             hi = lo + stride < hi ? lo + stride : hi;
         }
         i = lo;
-        step = static_cast<int>(rem - unit.weight_before(p, i)) - kListCost;
+        at = rem - unit.weight_before(p, i);
         steps = unit.pair_steps(p, i);
+        weight = unit.step_weight(p, i);
     }
+    // The first step of the list that begins at `pos` or behind it.
+    __device__ __forceinline__ int step_from(int64_t pos) const {
+        const int64_t x = pos - kListCost;
+        return x <= 0 ? 0 : static_cast<int>((x + weight - 1) >> (weight - 1));
+    }
+    __device__ __forceinline__ int64_t list_weight() const { return kListCost + static_cast<int64_t>(weight) * steps; }
     // The next list (not called behind the last one).
     __device__ __forceinline__ void next(const Params& p) {
-        step = -kListCost;
+        at = 0;
         if (++i == unit.pairs) {
             i = 0;
             if (++h == p.Hkv) {
@@ -256,6 +272,7 @@ struct Walk {
             }
         }
         steps = unit.pair_steps(p, i);
+        weight = unit.step_weight(p, i);
     }
 };
 
@@ -424,7 +441,6 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             const bool leader = elect_one();
             Walk<PREFIX> walk;
             int64_t left = 0;
-            walk.step = 0;
             const int64_t total = walk.total(p, lane);
             const int ctas = walk.ctas(p, total, lane);
             if (static_cast<int>(blockIdx.x) < ctas) {
@@ -439,10 +455,18 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 const int slot = k & 3;
                 if (!wait(B_SCHEDEMPTY + slot, ((k >> 2) & 1) ^ 1)) break;
                 Item it;
-                // this CTA's steps of the next list (none where its part ends in front of the list's first step)
-                const int s0 = walk.step < 0 ? 0 : walk.step;
-                const int s1 = left <= 0 ? 0 : (walk.steps - walk.step < left ? walk.steps : walk.step + static_cast<int>(left));
-                left -= s1 - walk.step;
+                // this CTA's steps of the next list that it has any of
+                int s0 = 0, s1 = 0;
+                int64_t origin = 0;      // where the list begins, counted back from the end of this CTA's part
+                while (left > 0) {
+                    const int64_t end = walk.list_weight() < walk.at + left ? walk.list_weight() : walk.at + left;
+                    s0 = walk.step_from(walk.at);
+                    s1 = walk.step_from(end);
+                    origin = left + walk.at;
+                    left -= end - walk.at;
+                    if (s1 > s0) break;
+                    if (left > 0) walk.next(p);
+                }
                 if (s1 > s0) {
                     const int pair_tok = walk.i * 2 * p.tile_tokens;
                     it.kvh = walk.h;
@@ -466,11 +490,11 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     it.slot = s0 == 0 && s1 == walk.steps ? -1 : 2 * static_cast<int>(blockIdx.x) + (s0 == 0 ? 1 : 0);
                     if (!PREFIX && s0 == 0 && s1 < walk.steps) {
                         if (leader) {
-                            const int64_t start = cta_begin(total, blockIdx.x + 1, ctas) - left - s1;        // where step 0 lies
-                            const int me = static_cast<int>(blockIdx.x);
+                            const int64_t start = cta_begin(total, blockIdx.x + 1, ctas) - origin + kListCost;        // where step 0 lies
+                            const int me = static_cast<int>(blockIdx.x), last0 = walk.unit.steps_of(pair_tok + p.tile_tokens) - 1;
                             Cut c;
-                            c.parts[0] = cta_of_tile(total, start + walk.unit.steps_of(pair_tok + p.tile_tokens) - 1, ctas) - me + 1;
-                            c.parts[1] = it.twin ? 0 : cta_of_tile(total, start + walk.steps - 1, ctas) - me + 1;
+                            c.parts[0] = cta_of_tile(total, start + static_cast<int64_t>(walk.weight) * last0, ctas) - me + 1;
+                            c.parts[1] = it.twin ? 0 : cta_of_tile(total, start + static_cast<int64_t>(walk.weight) * (walk.steps - 1), ctas) - me + 1;
                             c.tok = it.tok;
                             c.n_tok = it.n_tok;
                             c.kvh = it.kvh;
@@ -734,7 +758,7 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 for (int b0 = first; first >= 0 && b0 < p.tokens; b0 += 32 * stride) {
                     const int b = b0 + lane * stride, g = b < p.tokens ? attn_paged::group_of(p.starts, p.units, b) : -1;
                     int64_t start = __shfl_sync(0xffffffffu, walk.before, g < 0 ? 0 : g / walk.per);
-                    PrefixPlan plan = {0, 0, 0, 0};
+                    PrefixPlan plan = {0, 0, -1, 0};
                     if (g >= 0) {
                         Unit<true> unit;
                         for (int x = g / walk.per * walk.per; x < g; ++x) {
@@ -747,7 +771,7 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                             const int t = in_pair >= p.tile_tokens ? 1 : 0;
                             plan.start = start + unit.weight_before(p, pair) + kListCost;
                             plan.stride = unit.head_weight(p);
-                            plan.steps = unit.pair_steps(p, pair);
+                            plan.span = static_cast<int64_t>(unit.step_weight(p, pair)) * (unit.pair_steps(p, pair) - 1);
                             plan.row = t * 128 + (in_pair - t * p.tile_tokens) * p.group;
                         }
                     }
@@ -1073,13 +1097,14 @@ attn_paged_prefix_join_kernel(const __grid_constant__ attn_paged::DecodeParams p
     const PrefixPlan* plan = pre.plan + b;
     const int64_t total = __ldcg(&pre.plan[p.B].start), ctas = __ldcg(&pre.plan[p.B].stride);
     const int64_t first = __ldcg(&plan->start), stride = __ldcg(&plan->stride);
-    const int steps = __ldcg(&plan->steps), kvh = q_head / pre.group, row = __ldcg(&plan->row) + q_head - kvh * pre.group;
+    const int64_t span = __ldcg(&plan->span);
+    const int kvh = q_head / pre.group, row = __ldcg(&plan->row) + q_head - kvh * pre.group;
     const attn_paged::SeqPlan list = attn_paged::SeqPlan::read(p, b);
     int n_pre = 0, c0 = 0;
-    if (steps > 0) {
+    if (span >= 0) {
         const int64_t start = first + kvh * stride;
         c0 = cta_of_tile(total, start, static_cast<int>(ctas));
-        n_pre = cta_of_tile(total, start + steps - 1, static_cast<int>(ctas)) - c0 + 1;
+        n_pre = cta_of_tile(total, start + span, static_cast<int>(ctas)) - c0 + 1;
     }
     attn_paged::RowParts own;
     if (list.n > 0) own.find(p, list, q_head);

@@ -50,7 +50,7 @@ def test_workspaces(lib):
     assert lib.attn_paged_prefill_workspace_bytes(128) == 2 * 148 * 256 * 130 * 4 + up(148 * 20) and lib.attn_paged_prefill_workspace_bytes(64) == 2 * 148 * 256 * 66 * 4 + up(148 * 20)
     assert lib.attn_paged_prefill_workspace_bytes(256) == 0
     b = lib.attn_paged_prefix_decode_workspace_bytes
-    rows, plan, prefix_plan = up(64 * 32 * 130 * 4), up(65 * 16), up(65 * 24)
+    rows, plan, prefix_plan = up(64 * 32 * 130 * 4), up(65 * 16), up(65 * 32)
     assert b(64, 32, 8, 128) == lib.attn_paged_decode_workspace_bytes(32, 8, 128) + 2 * rows + plan + prefix_plan + 2 * 148 * 256 * 130 * 4
     assert b(-1, 32, 8, 128) == 0 and b(4, 3, 2, 64) == 0 and b(4, 4, 2, 256) == 0
 

@@ -456,7 +456,8 @@ size_t attn_paged_prefill_workspace_bytes(int D);
  * product for the common keys.
  * Where the table is small (B * max_pages * page_size * Hkv * D * 4 bytes of keys and values, were every sequence that long, are
  * less than 128 MiB) the call is attn_paged_decode, which is then faster: pass the table's used columns (table_stride says where the
- * next row begins), not the width that the longest sequence ever may need.
+ * next row begins), not the width that the longest sequence ever may need.  Where there are more groups x K/V heads than CTAs (148),
+ * a group whose prefix is short for its number of sequences (groups of one or two foremost) is read for each sequence, too.
  * workspace: device, 256-byte aligned, at least attn_paged_prefix_decode_workspace_bytes(B, H, Hkv, D) bytes, or ATTN_ERR_WORKSPACE.
  *            Two calls that may run at the same time need one each.
  */

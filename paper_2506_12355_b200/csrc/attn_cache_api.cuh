@@ -901,6 +901,7 @@ int attn_paged_prefix_decode(const void* q, const void* k_cache, const void* v_c
     p.prefix_lens = prefix_lens;
     p.n_groups = n_groups;
     p.all_ctas = di.sm_count < attn_paged::kMaxCtas ? di.sm_count : attn_paged::kMaxCtas;
+    p.sharing = attn_paged::Sharing{128 / p.group, 4 * D * p.sub, D == 64 ? 1300 : 1550, static_cast<int64_t>(n_groups) * Hkv <= p.all_ctas};
 #ifdef ATTN_TEST_HOOKS
     p.test_skip_step = g_test_skip_step;
     g_test_skip_step = -1;
@@ -910,19 +911,20 @@ int attn_paged_prefix_decode(const void* q, const void* k_cache, const void* v_c
     pre.parts = reinterpret_cast<float*>(ws + at.prefix_parts);
     pre.plan = reinterpret_cast<attn_paged_tc::PrefixPlan*>(ws + at.prefix_plan);
     pre.prefix_lens = prefix_lens;
+    pre.sharing = p.sharing;
     pre.row_bytes = Hkv * D * 4;
     pre.head_groups = p.heads >> p.hpt_shift;
 #define ATTN_PREFIX_CASE(DD, TT, GG)                                                                                           \
     if (D == DD && dtype == TT && (p.group <= 8) == (GG == 8)) {                                                               \
         using C = attn_paged::DecodeCfg<DD, GG>;                                                                               \
         auto kern = attn_paged::attn_paged_decode_kernel<DD, TT, GG, true>;                                                    \
-        if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), C::SMEM_BYTES)) return ATTN_ERR_CUDA;                     \
+        if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), C::SMEM_BYTES + C::TABLE_BYTES)) return ATTN_ERR_CUDA;                     \
         CUtensorMap mk, mv;                                                                                                    \
         if (!decode_maps<C::CK>(&mk, &mv, p, k_cache, v_cache, cache_strides, TT, DD, page_size)) return ATTN_ERR_CUDA;        \
         if (!launch_paged_tc<DD, TT, true>(pre, q, k_cache, v_cache, cache_strides, num_pages, page_size, block_table, table_stride, max_pages, \
                                            seq_lens, group_starts, n_groups, B, H, Hkv, scale, di.sm_count, st))               \
             return ATTN_ERR_CUDA;                                                                                              \
-        if (!launch_dependent(kern, dim3(static_cast<unsigned>(p.grid)), dim3(C::THREADS), C::SMEM_BYTES, st, mk, mv, p)) return ATTN_ERR_CUDA; \
+        if (!launch_dependent(kern, dim3(static_cast<unsigned>(p.grid)), dim3(C::THREADS), C::SMEM_BYTES + C::TABLE_BYTES, st, mk, mv, p)) return ATTN_ERR_CUDA; \
         return launch_dependent(attn_paged_tc::attn_paged_prefix_join_kernel<DD, TT, GG>, dim3(static_cast<unsigned>(B * join_blocks(H))), \
                                 dim3(attn_paged::kJoinWarps * 32), 0, st, p, pre, static_cast<int>(join_blocks(H)))            \
                    ? ATTN_OK                                                                                                   \

@@ -56,9 +56,18 @@ struct DecodeCfg {
     // ring stages: three where they fit beside the merge buffer
     static constexpr int NSTAGE = 3 * STAGE_BYTES + MERGE_BYTES + 1024 + 512 <= 232448 ? 3 : 2;
     static constexpr int SMEM_BYTES = 1024 + NSTAGE * STAGE_BYTES + MERGE_BYTES + 8 * NW * NSTAGE + 16;
-    static_assert(SMEM_BYTES <= 232448, "shared memory budget");
+    static constexpr int TABLE_AT = SMEM_BYTES - 1024, TABLE_BYTES = 32 * 8;       // with common prefixes: SeqTable
+    static_assert(SMEM_BYTES + (D == 256 ? 0 : TABLE_BYTES) <= 232448 && TABLE_AT % 8 == 0, "shared memory budget");
     // a partial result of one head: O [GH][D] (not normalised), then reference exponent and sum [GH][2], fp32
     static constexpr int PART_FLOATS = GH * (D + 2);
+};
+
+// What decides whether a group's common keys are worth a list of their own (see common_keys).
+struct Sharing {
+    int tile_tokens;            // sequences of a 128-row tile of queries
+    int key_bytes;              // that plain decoding reads of a key, for all query heads of a K/V head
+    int step_ns;                // a step of one tile of a list, where there are many lists
+    int always;                 // no more lists than CTAs
 };
 
 struct DecodeParams {
@@ -88,6 +97,7 @@ struct DecodeParams {
     const int* group_starts;    // [n_groups + 1]
     const int* prefix_lens;     // [n_groups]
     int n_groups, all_ctas;     // groups; CTAs that the two kernels share
+    Sharing sharing;
     int64_t* plan;              // [2 (B + 1)], for the joining kernel (SeqPlan)
     float* rows;                // O [B * H][D], then reference exponent and sum [B * H][2], of pairs that one CTA has to itself
     int cluster;                // > 0: a cluster of so many CTAs (a power of two up to kCluster) per (sequence, head), no second kernel
@@ -144,37 +154,67 @@ __device__ __forceinline__ int group_of(const int* starts, int n_groups, int b) 
     return lo;
 }
 
-// PREFIX: how many first keys of sequence b the other kernel takes.
-__device__ __forceinline__ int prefix_of(const int* starts, const int* prefix_lens, const int* seq_lens, int n_groups, int max_len, int b) {
-    const int g = group_of(starts, n_groups, b);
-    if (g < 0) return 0;
-    const int first = __ldg(starts + g);
-    return group_prefix(seq_lens, first < 0 ? 0 : first, __ldg(prefix_lens + g), max_len);
-}
-
 // The two kernels of a call with common prefixes run side by side, each on a part of the SMs (the second one's CTAs take the SMs that
 // the first one's surplus CTAs leave at once): the first is bound by its tensor-core pipeline's latencies, the second by memory.
 // Each works the parts out for itself from the lengths, in whole numbers, so both find the same.
 //
-// What a group's lists take of one CTA, in ns: a step of one tile, and by itself each list (its fill and way out, beside a busy memory).
+// What a K/V head's lists of a group of n sequences take of one CTA, in ns: a step of one tile, and by itself each list (its fill and way out).
 constexpr int kTileStepNs = 1100, kListNs = 8000;
-__device__ __forceinline__ int64_t group_cost(const int* starts, const int* prefix_lens, const int* seq_lens, int g, int B, int max_len, int Hkv,
-                                              int tile_tokens) {
+__device__ __forceinline__ int64_t list_cost(int n, int prefix, const Sharing& s, int step_ns = kTileStepNs, int list_ns = kListNs) {
+    const int pairs = (n + 2 * s.tile_tokens - 1) / (2 * s.tile_tokens), tiles = 2 * pairs - (n - (pairs - 1) * 2 * s.tile_tokens <= s.tile_tokens ? 1 : 0);
+    return static_cast<int64_t>((prefix + 127) / 128) * tiles * step_ns + static_cast<int64_t>(pairs) * list_ns;
+}
+constexpr int kBusyListNs = 12000, kBusyBytesPerNs = 45;
+constexpr int kBytesPerNs = 40, kPairNs = 2500;      // a CTA's memory rate, and what a pair costs by itself
+
+// The keys of group g that are worked on once for its n sequences; 0 where reading them for each sequence takes less: short prefixes of
+// few sequences.  With all SMs at lists, memory sets a step's time, and a list by itself takes 10 to 13 us.  1024 sequences, 8 K/V heads
+// of 128, without and with lists for all groups: groups of 1 behind about 500 keys 462 and 1149 us, of 4 behind 150 199 and 364, of 4
+// behind 500 460 and 370, of 16 445 and 206.  With no more lists than CTAs (host: groups x K/V heads) they cost no time of others.
+__device__ __forceinline__ int common_keys(const int* starts, const int* prefix_lens, const int* seq_lens, int g, int B, int max_len,
+                                           const Sharing& s, int& n) {
     int first = __ldg(starts + g), end = __ldg(starts + g + 1);
     first = first < 0 ? 0 : (first > B ? B : first);
     end = end < first ? first : (end > B ? B : end);
-    const int n = end - first, prefix = n > 0 ? group_prefix(seq_lens, first, __ldg(prefix_lens + g), max_len) : 0;
+    n = end - first;
+    const int prefix = n > 0 ? group_prefix(seq_lens, first, __ldg(prefix_lens + g), max_len) : 0;
     if (prefix <= 0) return 0;
-    const int pairs = (n + 2 * tile_tokens - 1) / (2 * tile_tokens), tiles = 2 * pairs - (n - (pairs - 1) * 2 * tile_tokens <= tile_tokens ? 1 : 0);
-    return Hkv * (static_cast<int64_t>((prefix + 127) / 128) * tiles * kTileStepNs + static_cast<int64_t>(pairs) * kListNs);
+    return s.always || static_cast<int64_t>(n) * s.key_bytes * prefix / kBusyBytesPerNs > list_cost(n, prefix, s, s.step_ns, kBusyListNs) ? prefix : 0;
+}
+
+// PREFIX: how many first keys of sequence b the other kernel takes.
+__device__ __forceinline__ int prefix_of(const int* starts, const int* prefix_lens, const int* seq_lens, int n_groups, int B, int max_len,
+                                         const Sharing& s, int b) {
+    const int g = group_of(starts, n_groups, b);
+    int n = 0;
+    return g < 0 ? 0 : common_keys(starts, prefix_lens, seq_lens, g, B, max_len, s, n);
+}
+
+// What the lists of group g take of one CTA.
+__device__ __forceinline__ int64_t group_cost(const int* starts, const int* prefix_lens, const int* seq_lens, int g, int B, int max_len, int Hkv,
+                                              const Sharing& s) {
+    int n;
+    const int prefix = common_keys(starts, prefix_lens, seq_lens, g, B, max_len, s, n);
+    return prefix > 0 ? Hkv * list_cost(n, prefix, s) : 0;
 }
 // CTAs of the first kernel out of `grid`, for lists that take `cost` ns, and own_bytes of keys and values of `pairs` pairs of a sequence and
 // a group of heads for the second one.
-constexpr int kBytesPerNs = 40, kPairNs = 2500;      // a CTA's memory rate, and what a pair costs by itself
 __device__ __forceinline__ int prefix_ctas(int64_t cost, int64_t own_bytes, int64_t pairs, int grid) {
     if (own_bytes <= 0) return grid;
     const int64_t own = own_bytes / kBytesPerNs + pairs * kPairNs, n = (cost * grid + (cost + own) / 2) / (cost + own);
     return cost <= 0 ? 0 : (n < 1 ? 1 : (n > grid - 1 ? grid - 1 : static_cast<int>(n)));
+}
+
+// PREFIX: keys win_lo .. len - 1.
+template <int CK>
+__device__ __forceinline__ SeqRange visible(int len, int win_lo) {
+    SeqRange r;
+    r.len = len;
+    r.win_lo = win_lo;
+    r.lo = win_lo / CK;
+    r.n_sink = 0;
+    r.n_chunks = win_lo < len ? len / CK + (len % CK != 0) - r.lo : 0;
+    return r;
 }
 
 template <int CK, bool PREFIX>
@@ -184,12 +224,8 @@ __device__ __forceinline__ SeqRange seq_range(const DecodeParams& p, int b) {
     len = len < 0 ? 0 : (len > p.max_len ? p.max_len : len);
     r.len = len;
     if constexpr (PREFIX) {
-        const int prefix = prefix_of(p.group_starts, p.prefix_lens, p.seq_lens, p.n_groups, p.max_len, b);
-        r.win_lo = prefix < len ? prefix : len;
-        r.lo = r.win_lo / CK;
-        r.n_sink = 0;
-        r.n_chunks = r.win_lo < len ? len / CK + (len % CK != 0) - r.lo : 0;
-        return r;
+        const int prefix = prefix_of(p.group_starts, p.prefix_lens, p.seq_lens, p.n_groups, p.B, p.max_len, p.sharing, b);
+        return visible<CK>(len, prefix < len ? prefix : len);
     }
     r.win_lo = (p.window > 0 && p.window < len) ? len - p.window : 0;
     r.lo = r.win_lo / CK;
@@ -305,6 +341,14 @@ struct SeqPlan {
     }
 };
 
+// PREFIX: the visible keys of the first sequences of a CTA's part, worked out once by all of its threads: walking from one sequence to the
+// next every warp would otherwise look for its group, a chain of loads (100 sequences in 3 groups, 16 heads of 64: 134 us instead of 123).
+struct SeqTable {
+    static constexpr int SIZE = 32;
+    const int2* at;       // shared memory: {len, win_lo}
+    int first;
+};
+
 // Position in the tile list, advanced tile by tile.  Every warp of a CTA walks the same tiles; kvh and r0 are its own.
 template <int NW, int CK, bool PREFIX>
 struct TileWalk {
@@ -312,12 +356,22 @@ struct TileWalk {
     int kvh, r0;          // K/V head, first query head of the part inside its group
     int hs;               // log2 of the heads of a tile
     SeqRange r;
-    __device__ __forceinline__ void at(const DecodeParams& p, int hs_, int b_, int h_, int t_) {
+    SeqTable table;
+    __device__ __forceinline__ void look(const DecodeParams& p) {
+        if (PREFIX && b - table.first < SeqTable::SIZE) {
+            const int2 x = table.at[b - table.first];
+            r = visible<CK>(x.x, x.y);
+        } else {
+            r = seq_range<CK, PREFIX>(p, b);
+        }
+    }
+    __device__ __forceinline__ void at(const DecodeParams& p, int hs_, int b_, int h_, int t_, const SeqTable& table_) {
         hs = hs_;
         b = b_;
         h = h_;
         t = t_;
-        r = seq_range<CK, PREFIX>(p, b);
+        table = table_;
+        look(p);
         t_end = seq_tiles<NW>(r, hs);
         split_head(p);
     }
@@ -334,7 +388,7 @@ struct TileWalk {
             h = 0;
             do {
                 if (++b >= p.B) return true;      // the end of the list: not used again
-                r = seq_range<CK, PREFIX>(p, b);
+                look(p);
                 t_end = seq_tiles<NW>(r, hs);
             } while (t_end == 0);
         }
@@ -387,7 +441,7 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     const int shift = 31 - __clz(p.cluster | 1), rank = static_cast<int>(blockIdx.x) & ((1 << shift) - 1);
     if (p.cluster) {
         const int pair = static_cast<int>(blockIdx.x) >> shift, b = pair / p.heads;
-        ld.at(p, 0, b, pair - b * p.heads, 0);
+        ld.at(p, 0, b, pair - b * p.heads, 0, SeqTable{nullptr, 0});
         ld.t = ld.t_end * rank >> shift;
         steps = (ld.t_end * (rank + 1) >> shift) - ld.t;
         if (pair == b * p.heads && rank == 0 && tid == 0 && p.seq_lens[b] > p.max_len) report_bad_index(p.status);
@@ -397,8 +451,10 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     const int b0 = tid * per, b1 = b0 + per < p.B ? b0 + per : p.B;
     int64_t mine[2] = {0, 0};                                // tiles in either form of the list
     int64_t own = 0, cost = 0, seqs = 0;                     // PREFIX: keys of this kernel and the sequences that have any; the other one's cost
+    SeqRange first_range = {};
     for (int b = b0; b < b1; ++b) {
         const SeqRange r = seq_range<CK, PREFIX>(p, b);
+        if (b == b0) first_range = r;
         own += r.len - r.win_lo;
         seqs += r.len > r.win_lo ? 1 : 0;
         mine[0] += seq_tiles<NW>(r, p.hpt_shift);
@@ -420,7 +476,7 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     int grid = p.grid;
     if constexpr (PREFIX) {
         for (int g = tid; g < p.n_groups; g += C::THREADS)
-            cost += group_cost(p.group_starts, p.prefix_lens, p.seq_lens, g, p.B, p.max_len, p.Hkv, 128 / p.group);
+            cost += group_cost(p.group_starts, p.prefix_lens, p.seq_lens, g, p.B, p.max_len, p.Hkv, p.sharing);
         own = warp_sum(own);
         cost = warp_sum(cost);
         seqs = warp_sum(seqs);
@@ -461,7 +517,7 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         longlong2* plan = reinterpret_cast<longlong2*>(p.plan);
         int64_t at = before;
         for (int b = b0; b < b1; ++b) {
-            const int n = seq_tiles<NW>(seq_range<CK, PREFIX>(p, b), hs);
+            const int n = seq_tiles<NW>(b == b0 ? first_range : seq_range<CK, PREFIX>(p, b), hs);
             plan[b] = make_longlong2(at, n);
             at += n;
         }
@@ -477,7 +533,7 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     if (first >= before * groups && first < (before + my_tiles) * groups) {
         int64_t rem = first - before * groups;
         for (int b = b0; b < b1; ++b) {
-            const int n = seq_tiles<NW>(seq_range<CK, PREFIX>(p, b), hs);
+            const int n = seq_tiles<NW>(b == b0 ? first_range : seq_range<CK, PREFIX>(p, b), hs);
             if (rem < static_cast<int64_t>(n) * groups) {
                 scan[32] = b;
                 scan[33] = rem / n;
@@ -488,7 +544,16 @@ attn_paged_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         }
     }
     __syncthreads();
-    ld.at(p, hs, static_cast<int>(scan[32]), static_cast<int>(scan[33]), static_cast<int>(scan[34]));
+    const SeqTable table{reinterpret_cast<const int2*>(smem + C::TABLE_AT), static_cast<int>(scan[32])};
+    if (PREFIX) {
+        for (int b = b0; b < b1; ++b)
+            if (b >= table.first && b - table.first < SeqTable::SIZE) {
+                const SeqRange r = b == b0 ? first_range : seq_range<CK, PREFIX>(p, b);
+                reinterpret_cast<int2*>(smem + C::TABLE_AT)[b - table.first] = make_int2(r.len, r.win_lo);
+            }
+        __syncthreads();
+    }
+    ld.at(p, hs, static_cast<int>(scan[32]), static_cast<int>(scan[33]), static_cast<int>(scan[34]), table);
     }
     cu = ld;
     const int own_b = cu.b, own_kvh = cu.kvh, own_r0 = cu.r0;     // of a cluster's pair

@@ -41,7 +41,6 @@ using attn_paged::cta_begin;
 using attn_paged::cta_count;
 using attn_paged::cta_of_tile;
 using attn_paged::divide;
-using attn_paged::group_prefix;
 using attn_paged::report_bad_index;
 using attn_tc::low_bits;
 
@@ -92,6 +91,7 @@ struct Params {
     int twin_weight;            // of a step of one tile
     int max_len, num_pages, page_shift, box_shift, k_axes, v_axes;
     float scale, scale_log2;
+    attn_paged::Sharing sharing;
     int row_bytes, head_groups; // prefix: of a key, K and V of all heads; groups of heads of a pair of the other kernel
     int grid;
     int* status;
@@ -133,7 +133,7 @@ struct Unit {
         end = end < tok0 ? tok0 : (end > p.tokens ? p.tokens : end);
         n = end - tok0;
         if constexpr (PREFIX) {
-            len = n > 0 ? group_prefix(p.seq_lens, tok0, __ldg(p.prefix_lens + u), p.max_len) : 0;
+            len = attn_paged::common_keys(p.starts, p.prefix_lens, p.seq_lens, u, p.tokens, p.max_len, p.sharing, n);
             base = 0;
         } else {
             len = __ldg(p.seq_lens + u);
@@ -183,15 +183,19 @@ struct Walk {
     int64_t at;
     int64_t mine, before;      // weight of this lane's units (consecutive ones) and of those in front of them
     int per, first;            // units of a lane, and this lane's first
-    // Total weight of all lists; all 32 lanes.
-    __device__ __forceinline__ int64_t total(const Params& p, int lane) {
+    // The total weight of all lists (prefix: after plan_sums()); all 32 lanes.
+    __device__ __forceinline__ int64_t total(const Params& p, int lane, const volatile int64_t* sums) {
         per = (p.units + 31) / 32;
         first = lane * per;
-        const int end = first + per < p.units ? first + per : p.units;
-        mine = 0;
-        for (int x = first; x < end; ++x) {
-            unit.load(p, x);
-            mine += p.Hkv * unit.head_weight(p);
+        if constexpr (PREFIX) {
+            mine = sums[lane];
+        } else {
+            const int end = first + per < p.units ? first + per : p.units;
+            mine = 0;
+            for (int x = first; x < end; ++x) {
+                unit.load(p, x);
+                mine += p.Hkv * unit.head_weight(p);
+            }
         }
         before = mine;
 #pragma unroll
@@ -203,22 +207,9 @@ struct Walk {
         before -= mine;
         return all;
     }
-    // The CTAs that share the lists, after total(): of a prefix call those that prefix_ctas() gives it.
-    __device__ __forceinline__ int ctas(const Params& p, int64_t total, int lane) const {
-        int n = p.grid;
-        if constexpr (PREFIX) {
-            int64_t cost = 0, own = 0, seqs = 0;
-            for (int g = lane; g < p.units; g += 32)
-                cost += attn_paged::group_cost(p.starts, p.prefix_lens, p.seq_lens, g, p.tokens, p.max_len, p.Hkv, p.tile_tokens);
-            for (int b = lane; b < p.tokens; b += 32) {
-                int len = __ldg(p.seq_lens + b);
-                len = len < 0 ? 0 : (len > p.max_len ? p.max_len : len);
-                const int prefix = attn_paged::prefix_of(p.starts, p.prefix_lens, p.seq_lens, p.units, p.max_len, b);
-                own += len > prefix ? len - prefix : 0;
-                seqs += len > prefix ? 1 : 0;
-            }
-            n = attn_paged::prefix_ctas(attn_paged::warp_sum(cost), attn_paged::warp_sum(own) * p.row_bytes, attn_paged::warp_sum(seqs) * p.head_groups, p.grid);
-        }
+    // The CTAs that share the lists: of a prefix call those that prefix_ctas() gives it.
+    static __device__ __forceinline__ int ctas(const Params& p, int64_t total, const volatile int64_t* sums) {
+        const int n = PREFIX ? attn_paged::prefix_ctas(sums[32], sums[33] * p.row_bytes, sums[34] * p.head_groups, p.grid) : p.grid;
         // (a CTA's part holds the beginning of a step: two weights at least)
         return cta_count(total / 2, n);
     }
@@ -227,17 +218,44 @@ struct Walk {
         const bool here = pos >= before && pos < before + mine;
         const int owner = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
         int64_t rem = pos - before;
-        int x = first;
-        if (here && per > 1)
-            for (;; ++x) {
-                unit.load(p, x);
-                const int64_t n = p.Hkv * unit.head_weight(p);
-                if (rem < n) break;
-                rem -= n;
+        if constexpr (PREFIX) {                        // 32 of the owner's units at a time
+            rem = __shfl_sync(0xffffffffu, rem, owner);
+            const int end = (owner + 1) * per < p.units ? (owner + 1) * per : p.units;
+            for (u = owner * per;; u += 32) {
+                int64_t n = 0;
+                if (u + lane < end) {
+                    unit.load(p, u + lane);
+                    n = p.Hkv * unit.head_weight(p);
+                }
+                int64_t incl = n;
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) {
+                    const int64_t up = __shfl_up_sync(0xffffffffu, incl, off);
+                    if (lane >= off) incl += up;
+                }
+                const unsigned hit = __ballot_sync(0xffffffffu, rem < incl);
+                if (hit != 0u) {
+                    const int at = __ffs(hit) - 1;
+                    rem -= __shfl_sync(0xffffffffu, incl - n, at);
+                    unit.from_lane(at);
+                    u += at;
+                    break;
+                }
+                rem -= __shfl_sync(0xffffffffu, incl, 31);
             }
-        u = __shfl_sync(0xffffffffu, x, owner);
-        rem = __shfl_sync(0xffffffffu, rem, owner);
-        unit.from_lane(owner);
+        } else {
+            int x = first;
+            if (here && per > 1)
+                for (;; ++x) {
+                    unit.load(p, x);
+                    const int64_t n = p.Hkv * unit.head_weight(p);
+                    if (rem < n) break;
+                    rem -= n;
+                }
+            u = __shfl_sync(0xffffffffu, x, owner);
+            rem = __shfl_sync(0xffffffffu, rem, owner);
+            unit.from_lane(owner);
+        }
         const int64_t per_head = unit.head_weight(p);
         h = static_cast<int>(divide(rem, per_head));
         rem -= h * per_head;
@@ -275,6 +293,37 @@ struct Walk {
         weight = unit.step_weight(p, i);
     }
 };
+
+// What every CTA of a prefix call works out from the lengths, by all of its threads (by one warp, as in a prefill, 1024 sequences in as many
+// groups take 0.1 ms).  sums, zero before: [0, 32): the weights of the units of each lane of Walk; [32]: the cost of all lists; [33], [34]:
+// the keys that remain for the other kernel, and the sequences that have any.
+__device__ __forceinline__ void plan_sums(const Params& p, int tid, int threads, unsigned long long* sums) {
+    const int per = (p.units + 31) / 32;
+    int64_t cost = 0, own = 0, seqs = 0;
+    for (int u = tid; u < p.units; u += threads) {
+        Unit<true> unit;
+        unit.load(p, u);
+        if (unit.n > 0) {
+            atomicAdd(sums + u / per, static_cast<unsigned long long>(p.Hkv * unit.head_weight(p)));
+            cost += p.Hkv * attn_paged::list_cost(unit.n, unit.len, p.sharing);
+        }
+    }
+    for (int b = tid; b < p.tokens; b += threads) {
+        int len = __ldg(p.seq_lens + b);
+        len = len < 0 ? 0 : (len > p.max_len ? p.max_len : len);
+        const int prefix = attn_paged::prefix_of(p.starts, p.prefix_lens, p.seq_lens, p.units, p.tokens, p.max_len, p.sharing, b);
+        own += len > prefix ? len - prefix : 0;
+        seqs += len > prefix ? 1 : 0;
+    }
+    cost = attn_paged::warp_sum(cost);
+    own = attn_paged::warp_sum(own);
+    seqs = attn_paged::warp_sum(seqs);
+    if ((tid & 31) == 0) {
+        if (cost > 0) atomicAdd(sums + 32, static_cast<unsigned long long>(cost));
+        if (own > 0) atomicAdd(sums + 33, static_cast<unsigned long long>(own));
+        if (seqs > 0) atomicAdd(sums + 34, static_cast<unsigned long long>(seqs));
+    }
+}
 
 // A CTA's share of one list, as the roles of the CTA get it.
 struct Item {
@@ -322,17 +371,24 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         B_COUNT = 23 + 2 * NGRP
     };
     auto bar = [&](int i) { return smem_base + C::TILE_BYTES + i * 8; };
-    volatile int* sched = reinterpret_cast<volatile int*>(bars + B_COUNT);             // [4][16]
+    constexpr int SCHED = PREFIX ? 12 : 16;
+    volatile int* sched = reinterpret_cast<volatile int*>(bars + B_COUNT);             // [4][SCHED]
     // [8][8]: of the key tile in ring group g % 8: whether any of its keys' pages is out of range, and which keys as bits.  (The
     // producer is at most NGRP groups ahead of the tile that the softmax groups are working on.)
-    volatile uint32_t* bad_ring = reinterpret_cast<volatile uint32_t*>(sched + 64);
+    volatile uint32_t* bad_ring = reinterpret_cast<volatile uint32_t*>(sched + 4 * SCHED);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(const_cast<uint32_t*>(bad_ring) + 64);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     float2* merge = reinterpret_cast<float2*>(smem_gen + C::TILE_BYTES + C::MISC_BYTES - 1024);     // [128]: reference and sum of tile 1's rows
-    static_assert(8 * B_COUNT + 4 * (64 + 64 + 2) <= C::MISC_BYTES - 1024, "barriers and slots");
+    constexpr int SUMS_AT = 8 * B_COUNT + 4 * (4 * SCHED + 64 + 2);
+    unsigned long long* sums = reinterpret_cast<unsigned long long*>(reinterpret_cast<uint8_t*>(bars) + SUMS_AT);       // prefix: [35], see plan_sums
+    static_assert(SUMS_AT + (PREFIX ? 8 * 35 : 0) <= C::MISC_BYTES - 1024 && SUMS_AT % 8 == 0, "barriers and slots");
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int tile_rows = p.tile_tokens * p.group;
 
+    if (PREFIX) {
+        if (tid < 35) sums[tid] = 0;
+        __syncthreads();
+    }
     if (tid == 0) {
         *abort_flag = 0;
         for (int t = 0; t < 2; ++t) {
@@ -371,6 +427,7 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         prefetch_tensormap(&tmK);
         prefetch_tensormap(&tmV);
     }
+    if constexpr (PREFIX) plan_sums(p, tid, C::THREADS, sums);
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -383,7 +440,7 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     auto next_item = [&](int k, bool hand_back, Item& it) -> bool {
         const int slot = k & 3;
         if (!wait(B_SCHEDFULL + slot, (k >> 2) & 1)) return false;
-        volatile int* e = sched + slot * 16;
+        volatile int* e = sched + slot * SCHED;
         const bool valid = e[0] != 0;
         it.kvh = e[1];
         it.tok = e[2];
@@ -434,6 +491,7 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         }
     };
 
+    const volatile int64_t* plan = reinterpret_cast<const volatile int64_t*>(sums);
     if (warp >= 8) {
         reg_dec_service();
         if (warp == 9) {
@@ -441,8 +499,8 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             const bool leader = elect_one();
             Walk<PREFIX> walk;
             int64_t left = 0;
-            const int64_t total = walk.total(p, lane);
-            const int ctas = walk.ctas(p, total, lane);
+            const int64_t total = walk.total(p, lane, plan);
+            const int ctas = walk.ctas(p, total, plan);
             if (static_cast<int>(blockIdx.x) < ctas) {
                 const int64_t first = cta_begin(total, blockIdx.x, ctas);
                 left = cta_begin(total, blockIdx.x + 1, ctas) - first;
@@ -503,7 +561,7 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     }
                     if (left > 0) walk.next(p);
                     if (leader) {
-                        volatile int* e = sched + slot * 16;
+                        volatile int* e = sched + slot * SCHED;
                         e[1] = it.kvh;
                         e[2] = it.tok;
                         e[3] = it.n_tok;
@@ -520,7 +578,7 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     }
                 } else {
                     if (leader) {
-                        sched[slot * 16] = 0;
+                        sched[slot * SCHED] = 0;
                         mbar_arrive(bar(B_SCHEDFULL + slot));
                     }
                     break;
@@ -751,14 +809,14 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             if constexpr (PREFIX) {
                 // where the partial results of each sequence's rows will lie, a lane per sequence: by the CTAs that have no lists
                 Walk<true> walk;
-                const int64_t total = walk.total(p, lane);
-                const int ctas = walk.ctas(p, total, lane), free = ctas < p.grid ? ctas : 0, stride = p.grid - free;
+                const int64_t total = walk.total(p, lane, plan);
+                const int ctas = walk.ctas(p, total, plan), free = ctas < p.grid ? ctas : 0, stride = p.grid - free;
                 const int first = static_cast<int>(blockIdx.x) - free;
                 if (first == 0 && lane == 0) p.plan[p.tokens] = PrefixPlan{total, ctas, 0, 0};
                 for (int b0 = first; first >= 0 && b0 < p.tokens; b0 += 32 * stride) {
                     const int b = b0 + lane * stride, g = b < p.tokens ? attn_paged::group_of(p.starts, p.units, b) : -1;
                     int64_t start = __shfl_sync(0xffffffffu, walk.before, g < 0 ? 0 : g / walk.per);
-                    PrefixPlan plan = {0, 0, -1, 0};
+                    PrefixPlan at = {0, 0, -1, 0};
                     if (g >= 0) {
                         Unit<true> unit;
                         for (int x = g / walk.per * walk.per; x < g; ++x) {
@@ -769,13 +827,13 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                         const int token = b - unit.tok0, pair = token / (2 * p.tile_tokens), in_pair = token - pair * 2 * p.tile_tokens;
                         if (token >= 0 && token < unit.n) {
                             const int t = in_pair >= p.tile_tokens ? 1 : 0;
-                            plan.start = start + unit.weight_before(p, pair) + kListCost;
-                            plan.stride = unit.head_weight(p);
-                            plan.span = static_cast<int64_t>(unit.step_weight(p, pair)) * (unit.pair_steps(p, pair) - 1);
-                            plan.row = t * 128 + (in_pair - t * p.tile_tokens) * p.group;
+                            at.start = start + unit.weight_before(p, pair) + kListCost;
+                            at.stride = unit.head_weight(p);
+                            at.span = static_cast<int64_t>(unit.step_weight(p, pair)) * (unit.pair_steps(p, pair) - 1);
+                            at.row = t * 128 + (in_pair - t * p.tile_tokens) * p.group;
                         }
                     }
-                    if (b < p.tokens) p.plan[b] = plan;
+                    if (b < p.tokens) p.plan[b] = at;
                 }
             } else {
                 // lengths that are out of range (of a prefix call the second kernel reports them)

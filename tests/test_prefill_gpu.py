@@ -242,6 +242,23 @@ def test_prefix_groups(lens, starts, prefix):
     run_prefix(lens, starts, prefix, 4, 4, 64, 8, "fp16", "slot", seed=5)
 
 
+@pytest.mark.parametrize("H,Hkv,D,kind", [(8, 2, 128, "bf16"), (4, 2, 64, "fp16")])
+@pytest.mark.parametrize("singles", [70, 1100])
+def test_prefix_of_many_groups(H, Hkv, D, kind, singles):
+    """Groups of one sequence and short prefixes of few, which are read for each sequence, among groups of many that are not; groups
+    whose sequences have no keys of their own."""
+    lens, starts, prefix = [], [0], []
+    for x in range(singles):
+        size, common = (1, 20) if x % 23 else ((3, 33) if x % 2 else (40, 250))
+        lens += [common + (x + 7 * y) % 30 for y in range(size)]
+        starts.append(len(lens))
+        prefix.append(common)
+    lens += [300] * 100 + [290 + y for y in range(20)]
+    starts += [starts[-1] + 100, starts[-1] + 120]
+    prefix += [300, 290]
+    run_prefix(lens, starts, prefix, H, Hkv, D, 16, kind, seed=7)
+
+
 @pytest.mark.parametrize("scale", [0.0, 1.0])
 def test_prefix_scales(scale):
     run_prefix([400, 300, 290], [0, 3], [280], 8, 2, 128, 16, "fp16", scale=scale, seed=6)

@@ -452,8 +452,8 @@ size_t attn_paged_prefill_workspace_bytes(int D);
  * group_starts, prefix_lens: device int32 [n_groups + 1], [n_groups].  The starts do not decrease; sequences in front of the first
  *            and behind the last group have no common part.  A prefix may be any length: no more of it is taken as common than the
  *            group's first sequence has keys, and a sequence that is shorter sees the keys that it has.  n_groups == 0: attn_paged_decode.
- * H / Hkv <= 128; D in {64, 128}.  The other arguments as in attn_paged_decode.  P is rounded to the 16-bit type before its
- * product for the common keys.
+ * H / Hkv <= 128; D in {64, 128}.  The other arguments as in attn_paged_decode, and O is as exact: P goes into its product in two
+ * 16-bit parts for the common keys, too.
  * Where the table is small (B * max_pages * page_size * Hkv * D * 4 bytes of keys and values, were every sequence that long, are
  * less than 128 MiB) the call is attn_paged_decode, which is then faster: pass the table's used columns (table_stride says where the
  * next row begins), not the width that the longest sequence ever may need.  Where there are more groups x K/V heads than CTAs (148),

@@ -946,6 +946,7 @@ def attn_paged_prefill(q, k_cache, v_cache, block_table, seq_lens, cu_seqlens, s
     """Causal attention of new tokens, q [T,H,D], over a paged cache that holds their keys already (see attn_paged_append, with the
     same seq_lens and cu_seqlens): token i of a sequence's n new ones sees the keys j <= seq_lens[b] - n + i.  Returns o [T,H,D] and
     lse [T,H] (float32); rows of padding tokens (outside cu_seqlens, or of sequences of length 0) are not written.  D 64 or 128.
+    As in attn_fwd the probabilities are rounded to q's type before their product with V (about 1.4 roundings of o in the 2-norm).
     `workspace`: CUDA uint8 tensor of at least attn_paged_prefill_workspace_bytes(D) bytes (allocated here when None)."""
     if stream is not None:
         return _on_stream(stream, q, attn_paged_prefill, q, k_cache, v_cache, block_table, seq_lens, cu_seqlens, scale, out, lse, workspace)
@@ -972,8 +973,8 @@ def attn_paged_prefix_decode(q, k_cache, v_cache, block_table, seq_lens, group_s
                              workspace=None, stream=None):
     """attn_paged_decode for sequences with common first parts, which are read once for all: group g is the sequences
     group_starts[g] .. group_starts[g+1] - 1 (int32 [groups+1]), whose first prefix_lens[g] (int32 [groups]) keys are the same, in shared
-    pages or in copies.  Same result as attn_paged_decode without a window; D 64 or 128.  With less than 128 MiB of keys and values, were
-    every sequence as long as block_table is wide, it is attn_paged_decode: pass block_table[:, :used].
+    pages or in copies.  Same result as attn_paged_decode without a window, and as exact; D 64 or 128.  With less than 128 MiB of keys and
+    values, were every sequence as long as block_table is wide, it is attn_paged_decode: pass block_table[:, :used].
     `workspace`: CUDA uint8 tensor of at least attn_paged_prefix_decode_workspace_bytes(B, H, Hkv, D) bytes (allocated here when None)."""
     if stream is not None:
         return _on_stream(stream, q, attn_paged_prefix_decode, q, k_cache, v_cache, block_table, seq_lens, group_starts, prefix_lens, scale, out, lse,

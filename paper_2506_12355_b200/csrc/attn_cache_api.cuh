@@ -901,8 +901,8 @@ int attn_paged_prefix_decode(const void* q, const void* k_cache, const void* v_c
     p.prefix_lens = prefix_lens;
     p.n_groups = n_groups;
     p.all_ctas = di.sm_count < attn_paged::kMaxCtas ? di.sm_count : attn_paged::kMaxCtas;
-    // (a step takes that long where all SMs are at lists: 1024 sequences in groups of one to 16 behind 50 to 2000 keys)
-    p.sharing = attn_paged::Sharing{128 / p.group, 4 * D * p.sub, D == 64 ? 1300 : 1550, static_cast<int64_t>(n_groups) * Hkv <= p.all_ctas};
+    // (what a step takes where all SMs are at lists, memory and latency together: 1024 sequences in groups of one to 32 behind 50 to 2000 keys)
+    p.sharing = attn_paged::Sharing{128 / p.group, 4 * D * p.sub, D == 64 ? 1300 : 2200, static_cast<int64_t>(n_groups) * Hkv <= p.all_ctas};
 #ifdef ATTN_TEST_HOOKS
     p.test_skip_step = g_test_skip_step;
     g_test_skip_step = -1;

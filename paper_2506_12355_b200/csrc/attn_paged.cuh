@@ -159,13 +159,16 @@ __device__ __forceinline__ int group_of(const int* starts, int n_groups, int b) 
 // Each works the parts out for itself from the lengths, in whole numbers, so both find the same.
 //
 // What a K/V head's lists of a group of n sequences take of one CTA, in ns: a step of one tile, and by itself each list (its fill and way out).
-constexpr int kTileStepNs = 1100, kListNs = 8000;
+// (With 1100 for a step 16 to 200 sequences in up to 5 groups behind 2000 to 16000 keys take 7 % longer on average.)
+constexpr int kTileStepNs = 1600, kListNs = 8000;
 __device__ __forceinline__ int64_t list_cost(int n, int prefix, const Sharing& s, int step_ns = kTileStepNs, int list_ns = kListNs) {
     const int pairs = (n + 2 * s.tile_tokens - 1) / (2 * s.tile_tokens), tiles = 2 * pairs - (n - (pairs - 1) * 2 * s.tile_tokens <= s.tile_tokens ? 1 : 0);
     return static_cast<int64_t>((prefix + 127) / 128) * tiles * step_ns + static_cast<int64_t>(pairs) * list_ns;
 }
 constexpr int kBusyListNs = 12000, kBusyBytesPerNs = 45;
-constexpr int kBytesPerNs = 40, kPairNs = 2500;      // a CTA's memory rate, and what a pair costs by itself
+// A CTA's memory rate, and what a pair costs by itself.  (With 2500 for a pair 1024 sequences in groups of 4 behind 2000 keys, 16 heads of 64:
+// 1600 us instead of 1070, the CTAs of the own keys being the last.)
+constexpr int kBytesPerNs = 40, kPairNs = 3600;
 
 // The keys of group g that are worked on once for its n sequences; 0 where reading them for each sequence takes less: short prefixes of
 // few sequences.  With all SMs at lists, memory sets a step's time, and a list by itself takes 10 to 13 us.  1024 sequences, 8 K/V heads

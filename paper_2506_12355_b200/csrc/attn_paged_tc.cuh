@@ -25,7 +25,10 @@
 //   * A list of one tile (few query rows: a prefix call's usual case) keeps both softmax groups busy: its rows are in both Q tiles,
 //     one takes the even steps and one the odd ones, and the epilogue adds up the two accumulators in tensor memory.
 //   * All exponentials on the special-function unit, as under a window: rows may see only a few keys.
-// P is rounded to the type of Q, K and V before its product and the row sums add the unrounded values (see attn_tc_pipe.cuh).
+// Prefill: P is rounded to the type of Q, K and V before its product and the row sums add the unrounded values (see attn_tc_pipe.cuh).
+// Prefix: P goes into its product in two 16-bit parts, as in attn_paged.cuh, so that a key counts the same whether it is read as a common
+// one or not (rounded once, O was off by 2.3e-3 of its 2-norm in bf16 where its own rounding is 1.66e-3); the second parts lie in the
+// other half of S's columns.
 //
 // What bounds it: a step of two tiles takes 1.9 us at D = 128 (1024 tensor cycles a tile, 1.25 PFLOP/s of visible pairs for the 2048
 // tokens above) and 1.7 at D = 64 (its exponentials), a step of one tile 1.0; a list costs 5 us beside its steps (the way out 2.3,
@@ -340,6 +343,29 @@ struct Item {
 __device__ __forceinline__ void reg_inc_softmax() { asm volatile("setmaxnreg.inc.sync.aligned.u32 216;"); }
 __device__ __forceinline__ void reg_dec_service() { asm volatile("setmaxnreg.dec.sync.aligned.u32 64;"); }
 
+// 16-bit parts of a pair of probabilities, as split2 of attn_paged.cuh makes them, in two steps: what the first parts stand for, and the second
+// ones.  fp16's first parts are cut off instead of rounded (one instruction less; the second part is then off by 2^-21 of the whole; bf16: 2^-16).
+template <int DTYPE>
+__device__ __forceinline__ uint32_t first_parts(float p0, float p1, float& h0, float& h1) {
+    if constexpr (DTYPE == 0) {
+        h0 = __uint_as_float(__float_as_uint(p0) & 0xffffe000u);
+        h1 = __uint_as_float(__float_as_uint(p1) & 0xffffe000u);
+        return pack2<DTYPE>(h0, h1);
+    } else {
+        const uint32_t hi = pack2<DTYPE>(p0, p1);
+        h0 = __uint_as_float(hi << 16);
+        h1 = __uint_as_float(hi & 0xffff0000u);
+        return hi;
+    }
+}
+template <int DTYPE>
+__device__ __forceinline__ uint32_t second_parts(float p0, float p1) {
+    float h0, h1, d0, d1;
+    first_parts<DTYPE>(p0, p1, h0, h1);
+    unpack_f32x2(fma_f32x2(pack_f32x2(h0, h1), pack_f32x2(-1.f, -1.f), pack_f32x2(p0, p1)), d0, d1);
+    return pack2<DTYPE>(d0, d1);
+}
+
 template <int D, int DTYPE, bool PREFIX>
 __global__ void __launch_bounds__(Cfg<D>::THREADS, 1)
 attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -368,7 +394,8 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         B_MERGE = 22,      // tile 1's sums are in shared memory (128 threads)
         B_KVFULL = 23,     // [NGRP] V_{j-1} and K_j loaded (two warps' copies)
         B_KVEMPTY = 23 + NGRP,
-        B_COUNT = 23 + 2 * NGRP
+        B_PLOW = 23 + 2 * NGRP,        // [2] prefix: the second parts of P_t written (128 threads)
+        B_COUNT = B_PLOW + (PREFIX ? 2 : 0)
     };
     auto bar = [&](int i) { return smem_base + C::TILE_BYTES + i * 8; };
     constexpr int SCHED = PREFIX ? 12 : 16;
@@ -397,6 +424,7 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             mbar_init(bar(B_SFULL + t), 1);
             mbar_init(bar(B_PFULL + t), 128);
             mbar_init(bar(B_PFULL2 + t), 128);
+            if (PREFIX) mbar_init(bar(B_PLOW + t), 128);
             mbar_init(bar(B_OFINAL + t), 1);
             mbar_init(bar(B_OFREE + t), 128);
         }
@@ -703,12 +731,13 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     }
                 }
             };
+            // 16 keys at a time; from 8 on (prefix) with the second parts of P
             auto issue_pv = [&](int t, int s, bool accumulate, int kk_begin, int kk_end) {
                 if (leader) {
                     const uint32_t b0 = v_lo0 + s * (C::KV_BYTES >> 4);
 #pragma unroll
                     for (int kk = kk_begin; kk < kk_end; ++kk)
-                        mma_f16_ts_lohi(tmem + C::o_col(t), tmem + C::s_col(t) + kk * 8, b0 + ((kk * 16 * 128) >> 4), DESC_HI, IDESC_O,
+                        mma_f16_ts_lohi(tmem + C::o_col(t), tmem + C::s_col(t) + kk * 8, b0 + ((kk & 7) * 16 * 128 >> 4), DESC_HI, IDESC_O,
                                         (accumulate || kk > 0) ? 1u : 0u);
                 }
             };
@@ -745,6 +774,11 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     if (!wait(B_PFULL2 + t, par)) return false;
                     tc_fence_after_sync();
                     issue_pv(t, 2 * gslot, true, 6, 8);
+                    if constexpr (PREFIX) {
+                        if (!wait(B_PLOW + t, par)) return false;
+                        tc_fence_after_sync();
+                        issue_pv(t, 2 * gslot, true, 8, 16);
+                    }
                     if (i + 1 == it.n(t)) commit(B_OFINAL + t);
                     return true;
                 };
@@ -879,12 +913,26 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             float m = 0.f, l = 0.f;
             bool unset = live, any_unset = any_live;       // the reference maximum is taken from the first tile that shows the row a key
 
+            // O_t *= alpha, before step j (the last update of O finished before S was produced)
+            auto rescale = [&](int j, float alpha) {
+                if (j == 0) return;
+#pragma unroll 1
+                for (int ch = 0; ch < D / 32; ++ch) {
+                    uint32_t orr[32];
+                    tmem_ld_32x32b_x32(tO + ch * 32, orr);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) orr[e] = __float_as_uint(__uint_as_float(orr[e]) * alpha);
+                    tmem_st_32x32b_x32(tO + ch * 32, orr);
+                }
+            };
             for (int j = 0; j < n; ++j) {
                 if (!(ok = wait(B_SFULL + t, (it_base + j) & 1))) break;
                 tc_fence_after_sync();
                 if (!any_live) {                           // no row of this warp is a query's: whatever S holds may stand in as P
                     mbar_arrive(bar(B_PFULL + t));
                     mbar_arrive(bar(B_PFULL2 + t));
+                    if constexpr (PREFIX) mbar_arrive(bar(B_PLOW + t));
                     continue;
                 }
                 const int step = it.twin ? 2 * j + t : j, kv0 = (it.tile0 + step) * 128;
@@ -926,6 +974,64 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 auto max8 = [&](const float* mx) {
                     return fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7])));
                 };
+                if constexpr (PREFIX) {
+                    // The tile's maximum first, so that S is not needed again: P takes its place in the registers, and its second parts
+                    // are made while the products with the first ones run.
+                    float mx[8];
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) mx[x] = -INFINITY;
+                    max_of(mx, 0, 128);
+                    const float top = max8(mx);
+                    const bool ahead = live && (unset ? top != -INFINITY : (top - m) * c > LAG);
+                    float alpha = 1.f;
+                    if (__any_sync(0xffffffffu, ahead)) {
+                        if (ahead) {
+                            if (!unset) alpha = ex2_approx((m - top) * c);
+                            m = top;
+                            unset = false;
+                        }
+                        rescale(j, alpha);
+                    }
+                    const float nmc = -m * c;
+                    const uint64_t c2 = pack_f32x2(c, c), nmc2 = pack_f32x2(nmc, nmc);
+                    uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+                    for (int ch = 0; ch < 4; ++ch) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int e = ch * 32; e < ch * 32 + 32; e += 2) {
+                            float x0, x1;
+                            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(sr[e]), __uint_as_float(sr[e + 1])), c2, nmc2), x0, x1);
+                            const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+                            acc[(e / 2) & 3] = add_f32x2(acc[(e / 2) & 3], pack_f32x2(p0, p1));
+                            sr[e] = __float_as_uint(p0);
+                            sr[e + 1] = __float_as_uint(p1);
+                            float h0, h1;
+                            pk[(e / 2) & 15] = first_parts<DTYPE>(p0, p1, h0, h1);
+                        }
+                        tmem_st_32x32b_x16(tS + ch * 16, pk);
+                        if (ch >= 2) {
+                            tmem_st_wait();
+                            tc_fence_before_sync();
+                            mbar_arrive(bar((ch == 2 ? B_PFULL : B_PFULL2) + t));
+                        }
+                    }
+#pragma unroll
+                    for (int ch = 0; ch < 4; ++ch) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int e = ch * 32; e < ch * 32 + 32; e += 2) pk[(e / 2) & 15] = second_parts<DTYPE>(__uint_as_float(sr[e]), __uint_as_float(sr[e + 1]));
+                        tmem_st_32x32b_x16(tS + 64 + ch * 16, pk);
+                    }
+                    float a0, a1, a2, a3;
+                    unpack_f32x2(add_f32x2(acc[0], acc[1]), a0, a1);
+                    unpack_f32x2(add_f32x2(acc[2], acc[3]), a2, a3);
+                    l = l * alpha + ((a0 + a1) + (a2 + a3));
+                    tmem_st_wait();
+                    tc_fence_before_sync();
+                    mbar_arrive(bar(B_PLOW + t));
+                    continue;
+                }
                 if (any_unset) {
                     float mx[8];
 #pragma unroll
@@ -974,18 +1080,7 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                                 alpha = ex2_approx((m - top) * c);
                                 m = top;
                             }
-                            // (the last update of O finished before S was produced)
-                            if (j > 0) {
-#pragma unroll 1
-                                for (int ch = 0; ch < D / 32; ++ch) {
-                                    uint32_t orr[32];
-                                    tmem_ld_32x32b_x32(tO + ch * 32, orr);
-                                    tmem_ld_wait();
-#pragma unroll
-                                    for (int e = 0; e < 32; ++e) orr[e] = __float_as_uint(__uint_as_float(orr[e]) * alpha);
-                                    tmem_st_32x32b_x32(tO + ch * 32, orr);
-                                }
-                            }
+                            rescale(j, alpha);
                             continue;
                         }
                     }

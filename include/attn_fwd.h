@@ -456,8 +456,9 @@ size_t attn_paged_prefill_workspace_bytes(int D);
  * 16-bit parts for the common keys, too.
  * Where the table is small (B * max_pages * page_size * Hkv * D * 4 bytes of keys and values, were every sequence that long, are
  * less than 128 MiB) the call is attn_paged_decode, which is then faster: pass the table's used columns (table_stride says where the
- * next row begins), not the width that the longest sequence ever may need.  Where there are more groups x K/V heads than CTAs (148),
- * a group whose prefix is short for its number of sequences (groups of one or two foremost) is read for each sequence, too.
+ * next row begins), not the width that the longest sequence ever may need.  Where the groups have more blocks of 256 query rows than
+ * there are CTAs (148), common keys that are few for a group's number of blocks and sequences (16 keys of 1024 sequences; most
+ * prefixes of groups of one or two) are read for each sequence, too.
  * workspace: device, 256-byte aligned, at least attn_paged_prefix_decode_workspace_bytes(B, H, Hkv, D) bytes, or ATTN_ERR_WORKSPACE.
  *            Two calls that may run at the same time need one each.
  */

@@ -901,8 +901,12 @@ int attn_paged_prefix_decode(const void* q, const void* k_cache, const void* v_c
     p.prefix_lens = prefix_lens;
     p.n_groups = n_groups;
     p.all_ctas = di.sm_count < attn_paged::kMaxCtas ? di.sm_count : attn_paged::kMaxCtas;
-    // (what a step takes where all SMs are at lists, memory and latency together: 1024 sequences in groups of one to 32 behind 50 to 2000 keys)
-    p.sharing = attn_paged::Sharing{128 / p.group, 4 * D * p.sub, D == 64 ? 1300 : 2200, static_cast<int64_t>(n_groups) * Hkv <= p.all_ctas};
+    // A group has ceil(sequences / two tiles) lists per K/V head: n_groups + B / (two tiles) at most for all groups.
+    const int tile_tokens = 128 / p.group;
+    const int64_t lists = (n_groups + static_cast<int64_t>(B) / (2 * tile_tokens)) * Hkv;
+    // (2200, 1300: what a step takes where all SMs are at lists, memory and latency together: 1024 sequences in groups of one to 32 behind 50
+    // to 2000 keys)
+    p.sharing = attn_paged::Sharing{tile_tokens, 4 * D * p.sub, D == 64 ? 1300 : 2200, lists <= p.all_ctas};
 #ifdef ATTN_TEST_HOOKS
     p.test_skip_step = g_test_skip_step;
     g_test_skip_step = -1;

@@ -67,7 +67,7 @@ struct Sharing {
     int tile_tokens;            // sequences of a 128-row tile of queries
     int key_bytes;              // that plain decoding reads of a key, for all query heads of a K/V head
     int step_ns;                // a step of one tile of a list, where there are many lists
-    int always;                 // no more lists than CTAs
+    int always;                 // no more lists than CTAs: all groups that have common keys
 };
 
 struct DecodeParams {
@@ -173,7 +173,7 @@ constexpr int kBytesPerNs = 40, kPairNs = 3600;
 // The keys of group g that are worked on once for its n sequences; 0 where reading them for each sequence takes less: short prefixes of
 // few sequences.  With all SMs at lists, memory sets a step's time, and a list by itself takes 10 to 13 us.  1024 sequences, 8 K/V heads
 // of 128, without and with lists for all groups: groups of 1 behind about 500 keys 462 and 1149 us, of 4 behind 150 199 and 364, of 4
-// behind 500 460 and 370, of 16 445 and 206.  With no more lists than CTAs (host: groups x K/V heads) they cost no time of others.
+// behind 500 460 and 370, of 16 445 and 206.  With no more lists than CTAs (Sharing::always) a list's CTAs have no other list to get to.
 __device__ __forceinline__ int common_keys(const int* starts, const int* prefix_lens, const int* seq_lens, int g, int B, int max_len,
                                            const Sharing& s, int& n) {
     int first = __ldg(starts + g), end = __ldg(starts + g + 1);

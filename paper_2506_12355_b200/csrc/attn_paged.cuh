@@ -158,12 +158,15 @@ __device__ __forceinline__ int group_of(const int* starts, int n_groups, int b) 
 // the first one's surplus CTAs leave at once): the first is bound by its tensor-core pipeline's latencies, the second by memory.
 // Each works the parts out for itself from the lengths, in whole numbers, so both find the same.
 //
+// 128-key steps over so many keys, which may be 2^31 - 1.
+__host__ __device__ __forceinline__ int key_steps(int keys) { return keys > 0 ? ((keys - 1) >> 7) + 1 : 0; }
+
 // What a K/V head's lists of a group of n sequences take of one CTA, in ns: a step of one tile, and by itself each list (its fill and way out).
 // (With 1100 for a step 16 to 200 sequences in up to 5 groups behind 2000 to 16000 keys take 7 % longer on average.)
 constexpr int kTileStepNs = 1600, kListNs = 8000;
-__device__ __forceinline__ int64_t list_cost(int n, int prefix, const Sharing& s, int step_ns = kTileStepNs, int list_ns = kListNs) {
+__host__ __device__ __forceinline__ int64_t list_cost(int n, int prefix, const Sharing& s, int step_ns = kTileStepNs, int list_ns = kListNs) {
     const int pairs = (n + 2 * s.tile_tokens - 1) / (2 * s.tile_tokens), tiles = 2 * pairs - (n - (pairs - 1) * 2 * s.tile_tokens <= s.tile_tokens ? 1 : 0);
-    return static_cast<int64_t>((prefix + 127) / 128) * tiles * step_ns + static_cast<int64_t>(pairs) * list_ns;
+    return static_cast<int64_t>(key_steps(prefix)) * tiles * step_ns + static_cast<int64_t>(pairs) * list_ns;
 }
 constexpr int kBusyListNs = 12000, kBusyBytesPerNs = 45;
 // A CTA's memory rate, and what a pair costs by itself.  (With 2500 for a pair 1024 sequences in groups of 4 behind 2000 keys, 16 heads of 64:

@@ -44,6 +44,7 @@ using attn_paged::cta_begin;
 using attn_paged::cta_count;
 using attn_paged::cta_of_tile;
 using attn_paged::divide;
+using attn_paged::key_steps;
 using attn_paged::report_bad_index;
 using attn_tc::low_bits;
 
@@ -104,7 +105,7 @@ struct Params {
 };
 
 // sum over i < n of floor((a i + b) / 128)
-__device__ __forceinline__ int64_t floor_sum(uint32_t n, uint32_t a, uint32_t b) {
+__host__ __device__ __forceinline__ int64_t floor_sum(uint32_t n, uint32_t a, uint32_t b) {
     uint32_t m = 128;
     int64_t sum = 0;
     while (n > 0) {
@@ -156,25 +157,25 @@ struct Unit {
         pairs = __shfl_sync(0xffffffffu, pairs, lane);
     }
     // steps of the first `tokens` query tokens (at least one, also where none of them sees a key)
-    __device__ __forceinline__ int steps_of(int tokens) const {
-        if (PREFIX) return (len + 127) >> 7;
+    __host__ __device__ __forceinline__ int steps_of(int tokens) const {
+        if (PREFIX) return key_steps(len);
         return ((base > 0 ? base : 0) + (tokens < n ? tokens : n) - 1) / 128 + 1;
     }
-    __device__ __forceinline__ int pair_steps(const Params& p, int i) const { return steps_of((i + 1) * 2 * p.tile_tokens); }
+    __host__ __device__ __forceinline__ int pair_steps(const Params& p, int i) const { return steps_of((i + 1) * 2 * p.tile_tokens); }
     // Weights, in units of about 1 us: a step of two tiles counts 2, one of one tile (the last pair may have no more) as much at D = 128,
     // where it waits for the same K and V (with weight 1 32 prompts of 10 - 200 tokens behind 4096, 32 heads over 8: 330 us instead of
     // 277), and 1 at D = 64; each list counts kListCost more.
-    __device__ __forceinline__ int step_weight(const Params& p, int i) const {
+    __host__ __device__ __forceinline__ int step_weight(const Params& p, int i) const {
         return i == pairs - 1 && n - i * 2 * p.tile_tokens <= p.tile_tokens ? p.twin_weight : 2;
     }
-    __device__ __forceinline__ int64_t weight_before(const Params& p, int i) const {
+    __host__ __device__ __forceinline__ int64_t weight_before(const Params& p, int i) const {
         const int t2 = 2 * p.tile_tokens, full = i < pairs ? i : pairs - 1;      // the last pair has a weight of its own
         if (i == 0) return 0;
-        const int64_t steps = PREFIX ? static_cast<int64_t>(full) * ((len + 127) >> 7)
+        const int64_t steps = PREFIX ? static_cast<int64_t>(full) * key_steps(len)
                                      : floor_sum(full, t2, static_cast<uint32_t>(base > 0 ? base : 0) + t2 - 1) + full;
         return 2 * steps + static_cast<int64_t>(i) * kListCost + (i == pairs ? static_cast<int64_t>(step_weight(p, i - 1)) * steps_of(n) : 0);
     }
-    __device__ __forceinline__ int64_t head_weight(const Params& p) const { return weight_before(p, pairs); }
+    __host__ __device__ __forceinline__ int64_t head_weight(const Params& p) const { return weight_before(p, pairs); }
 };
 
 // Position in the lists: unit, K/V head, pair, and how far into the pair's list in weights (what the list costs beside its steps comes

@@ -1110,9 +1110,9 @@ struct JoinList {
 
 // The parts of one row: head (of the K/V heads' parts of at most 16 query heads) and row of the pair.
 struct RowParts {
-    int count = 0;             // 1: one CTA has the pair to itself
-    int c0, hs, hh, head, row;
-    bool odd;                  // the pair is not c0's first (it is that of every CTA behind c0)
+    int count = 0;             // 1: one CTA has the pair to itself; 0: no keys
+    int c0 = 0, hs = 0, hh = 0, head = 0, row = 0;
+    bool odd = false;          // the pair is not c0's first (it is that of every CTA behind c0)
     template <class List>
     __device__ __forceinline__ void find(const DecodeParams& p, const List& l, int q_head) {       // (l.n > 0)
         const int kvh = q_head / p.group, in_group = q_head - kvh * p.group;

@@ -1120,14 +1120,14 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 ++merges;
                 tc_fence_after_sync();
                 const float2 other = merge[r];
-                const float top = l > 0.f ? (other.y > 0.f ? fmaxf(m, other.x) : m) : other.x;
-                f0 = l > 0.f ? ex2_approx((m - top) * c) : 0.f;
-                f1 = other.y > 0.f ? ex2_approx((other.x - top) * c) : 0.f;
+                const float top = l != 0.f ? (other.y != 0.f ? fmaxf(m, other.x) : m) : other.x;
+                f0 = l != 0.f ? ex2_approx((m - top) * c) : 0.f;
+                f1 = other.y != 0.f ? ex2_approx((other.x - top) * c) : 0.f;
                 l = fmaf(f0, l, f1 * other.y);
                 m = top;
             }
             const bool final_rows = !PREFIX && it.slot < 0;
-            const bool seen = l > 0.f;                     // false: no visible key in this share
+            const bool seen = l != 0.f;                    // false: no visible key in this share (a sum that is no number stays one)
             // this row of [tokens][H]
             const int out_row = live ? (it.tok + my_token) * p.H + it.kvh * p.group + my_head : -1;
             float* part = p.parts + it.slot * part_floats(D);

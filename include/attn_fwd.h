@@ -426,7 +426,8 @@ size_t attn_paged_decode_workspace_bytes(int H, int Hkv, int D);
  * q, o [tokens, H, D], lse [tokens, H]: device, contiguous; H % Hkv == 0, H / Hkv <= 128; D in {64, 128}.
  * seq_lens, cu_seqlens: device int32 [n_seqs], [n_seqs + 1], as in attn_paged_append.  Tokens before cu_seqlens[0], tokens from
  *            cu_seqlens[n_seqs] on and tokens of sequences of length 0 are padding: their rows of o and lse stay as they were.
- *            A length beyond max_pages * page_size is cut to that, a token in front of its sequence's first key gets O = 0,
+ *            Lists that reach beyond the call's tokens, or begin below 0, are cut to them (n is what is left),
+ *            a length beyond max_pages * page_size is cut to that, a token in front of its sequence's first key gets O = 0,
  *            LSE = -inf, a visible key whose page is not in [0, num_pages) counts as hidden, and each is reported as
  *            ATTN_ERR_DEVICE_INDEX in the device status.  What lies in slots without a key does not matter (it may be NaN).
  * num_pages and max_pages are at least 1 (unless there is nothing to do).

@@ -873,8 +873,8 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             } else {
                 // lengths that are out of range (of a prefix call the second kernel reports them)
                 for (int u = static_cast<int>(blockIdx.x) * 32 + lane; u < p.units; u += 32 * gridDim.x) {
-                    const int len = __ldg(p.seq_lens + u), new_tokens = __ldg(p.starts + u + 1) - __ldg(p.starts + u);
-                    if (len > p.max_len || (len > 0 && new_tokens > len)) report_bad_index(p.status);
+                    const int len = __ldg(p.seq_lens + u), begin = __ldg(p.starts + u), end = __ldg(p.starts + u + 1);
+                    if (len > p.max_len || (len > 0 && (begin < 0 || end > p.tokens || end - begin > len))) report_bad_index(p.status);
                 }
             }
         }

@@ -6,7 +6,7 @@ import torch
 
 from paper_2506_12355_b200 import api
 from test_paged_gpu import make_cache
-from test_prefill_gpu import check_prefill, make_shared, wide
+from test_prefill_gpu import check_prefill, check_prefix, make_shared, wide
 from test_rope_gpu import DT
 
 pytestmark = pytest.mark.gpu
@@ -50,3 +50,54 @@ def test_a_common_key_that_is_no_number_shows_in_o_and_lse(n):
     assert torch.isnan(o[:, 4:]).all() and torch.isnan(lse[:, 4:]).all()
     for b in range(n):
         check_prefill(o[b:b + 1, :4], lse[b:b + 1, :4], q[b:b + 1, :4], ks[b][:, :1], vs[b][:, :1], D ** -0.5, dt)
+
+
+def malformed(lens, tokens, cu, seed=45):
+    """One call over 3 sequences whose lists are not what they should be: (o, lse, q, keys, values, status), rows preset to 7."""
+    D, H, Hkv, page, dt = 64, 4, 2, 16, torch.float16
+    kc, vc, tab, ks, vs = make_cache(lens, Hkv, D, page, dt, "head", seed)
+    q = torch.randn(tokens, H, D, generator=torch.Generator().manual_seed(seed + 1)).to(dt).cuda()
+    o, lse = torch.full_like(q, 7.0), torch.full((tokens, H), 7.0, device="cuda")
+    api.attn_paged_prefill(q, kc, vc, tab.cuda(), i32(lens), i32(cu), 0.125, o, lse)
+    return o, lse, q, ks, vs, api.attn_last_device_status()
+
+
+def check_rows_of(case, first, end, b, last):
+    """Token first sees the keys 0 .. last of sequence b, the next one key more, and so on."""
+    o, lse, q, ks, vs, _ = case
+    n = last + end - first                           # keys behind the last token: none
+    check_prefill(o[first:end], lse[first:end], q[first:end], ks[b][:n], vs[b][:n], 0.125, torch.float16)
+
+
+def test_lists_that_reach_beyond_the_tokens_are_cut_and_reported():
+    lens = [200, 64, 40]
+    case = malformed(lens, 60, [0, 20, 40, 60])
+    assert case[5] == 0
+    check_rows_of(case, 40, 60, 2, 20)
+    case = malformed(lens, 50, [0, 20, 40, 60])               # the last sequence's new tokens are 10 then
+    assert case[5] == 13
+    check_rows_of(case, 0, 20, 0, 180)
+    check_rows_of(case, 20, 40, 1, 44)
+    check_rows_of(case, 40, 50, 2, 30)
+    case = malformed(lens, 60, [-4, 20, 40, 60])
+    assert case[5] == 13
+    check_rows_of(case, 0, 20, 0, 180)
+    check_rows_of(case, 40, 60, 2, 20)
+    case = malformed([200, 64, 0], 50, [0, 20, 40, 60])       # a padded sequence's list does not matter
+    assert case[5] == 0 and (case[0][40:] == 7).all() and (case[1][40:] == 7).all()
+
+
+def test_lists_that_run_backwards():
+    lens = [200, 64, 40]
+    case = malformed(lens, 60, [0, 40, 20, 60])               # tokens 20 .. 39 are in two lists
+    check_rows_of(case, 0, 20, 0, 160)
+    check_rows_of(case, 40, 60, 2, 20)
+    case = malformed(lens, 70, [50, 10, 10, 30])              # the last sequence has tokens 10 .. 29
+    check_rows_of(case, 10, 30, 2, 20)
+    for rows in (slice(0, 10), slice(30, 70)):
+        assert (case[0][rows] == 7).all() and (case[1][rows] == 7).all()
+    case = malformed(lens, 60, [50, 10, 10, 10])
+    assert case[5] == 0 and (case[0] == 7).all() and (case[1] == 7).all()
+    case = malformed(lens, 60, [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1, -2 ** 31])     # sequence 1 has all tokens
+    assert case[5] == 13
+    check_rows_of(case, 0, 60, 1, 4)

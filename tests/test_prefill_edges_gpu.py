@@ -101,3 +101,15 @@ def test_lists_that_run_backwards():
     case = malformed(lens, 60, [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1, -2 ** 31])     # sequence 1 has all tokens
     assert case[5] == 13
     check_rows_of(case, 0, 60, 1, 4)
+
+
+@pytest.mark.parametrize("starts,prefix", [([0, 3, 1], [160, 160]), ([-5, 2, 99], [160, 160]), ([3, 0, 3], [-1, 2 ** 31 - 1]), ([7, 9], [5]), ([0, 3], [-1]),
+                                           ([-2 ** 31, 2 ** 31 - 1], [160])])
+def test_groups_that_run_backwards_or_past_the_batch(starts, prefix):
+    """Each sequence is in a group whose common keys are its own, or in none: the results are those of plain decoding."""
+    D, H, Hkv, page, dt, lens = 64, 4, 2, 16, torch.float16, [200, 300, 250]
+    kc, vc, tab, ks, vs = make_shared(lens, [0, 3], [160], Hkv, D, page, dt, "head", 9)
+    q = torch.randn(3, H, D, generator=torch.Generator().manual_seed(1)).to(dt).cuda()
+    o, lse = api.attn_paged_prefix_decode(q, kc, vc, wide(tab, page, Hkv, D).cuda(), i32(lens), i32(starts), i32(prefix), 0.125)
+    assert api.attn_last_device_status() == 0
+    check_prefix(o, lse, q, ks, vs, 0.125, dt)

@@ -179,13 +179,18 @@ __device__ __forceinline__ void turn_values(F2* y, const F2* x, const F2* cs, co
 
 // The axes of a lane's four pairs, 2 bits each.  `same`: in every lane of the warp the four pairs belong to one axis (runs of pairs
 // per axis whose lengths are multiples of 4): two 16-byte loads of the table per lane and token, as with one axis.  Axes that
-// take turns need eight single loads.
+// take turns need eight single loads.  (With one axis nothing is asked: the vote cost the gradient half a us of 60.)
 struct PairAxes {
     unsigned of;
     bool same;
-    __device__ __forceinline__ PairAxes(const RopeParams& p, int l) {
-        of = 8 * l < p.R ? p.pair_axes[l] : 0u;
-        same = __all_sync(0xffffffffu, of == (of & 3u) * 0x55u);
+    template <bool AXES>
+    static __device__ __forceinline__ PairAxes of_lane(const RopeParams& p, int l) {
+        PairAxes a = {0u, true};
+        if constexpr (AXES) {
+            a.of = 8 * l < p.R ? p.pair_axes[l] : 0u;
+            a.same = __all_sync(0xffffffffu, a.of == (a.of & 3u) * 0x55u);
+        }
+        return a;
     }
 };
 
@@ -365,7 +370,7 @@ attn_rope_kernel(const RopeParams p) {
         }
     }
     AxisPositions axis_pos;
-    const PairAxes axes(p, l);   // (dead code without AXES)
+    const PairAxes axes = PairAxes::of_lane<AXES>(p, l);
     if constexpr (AXES) {
         if (!axis_pos.load(p, token)) {
             report_bad_index(p.status);
@@ -443,7 +448,7 @@ attn_rope_bwd_kernel(const RopeParams p) {
     __shared__ float sums[kWarps * RPW][D];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane / LPR, l = lane % LPR;
     const Place at(p, l);
-    const PairAxes axes(p, l);      // (dead code without AXES)
+    const PairAxes axes = PairAxes::of_lane<AXES>(p, l);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const bool is_q = static_cast<int>(blockIdx.x) < p.q_blocks;
     const unsigned block = is_q ? blockIdx.x : blockIdx.x - p.q_blocks, blocks = is_q ? p.q_blocks : gridDim.x - p.q_blocks;

@@ -206,7 +206,7 @@ attn_rope_bwd_tma_kernel(const __grid_constant__ TmaMaps maps, const __grid_cons
         // =========================== arithmetic ===========================
         const int sub = lane / LPR, l = lane % LPR;
         const Place at(p.r, l);
-        const PairAxes axes(p.r, l);                          // (dead code without AXES)
+        const PairAxes axes = PairAxes::of_lane<AXES>(p.r, l);
         Turn turn;                                            // of the token whose rows this lane works on
         F2 w[4];
         int my_kind = -1;                                     // tensor that w belongs to

@@ -6,7 +6,7 @@ import torch
 
 from paper_2506_12355_b200 import api
 from test_paged_gpu import make_cache
-from test_prefill_gpu import check_prefill, check_prefix, make_shared, wide
+from test_prefill_gpu import check_prefill, check_prefix, make_shared, run_prefill, wide
 from test_rope_gpu import DT
 
 pytestmark = pytest.mark.gpu
@@ -113,3 +113,18 @@ def test_groups_that_run_backwards_or_past_the_batch(starts, prefix):
     o, lse = api.attn_paged_prefix_decode(q, kc, vc, wide(tab, page, Hkv, D).cuda(), i32(lens), i32(starts), i32(prefix), 0.125)
     assert api.attn_last_device_status() == 0
     check_prefix(o, lse, q, ks, vs, 0.125, dt)
+
+
+@pytest.mark.parametrize("D,kind", [(64, "bf16"), (128, "fp16")])
+def test_prefill_of_many_sequences_most_of_which_bring_little(D, kind):
+    """More sequences than one lane's share of the plan fits into a few rounds: most bring no token or one, some are padding, a run of 900
+    brings nothing at all."""
+    lens, news = [], []
+    for b in range(2500):
+        if 800 <= b < 1700:
+            lens.append(3 if b % 2 else 0)
+            news.append(0)
+        else:
+            lens.append(0 if b % 11 == 3 else 1 + (b * 7) % 50)
+            news.append(0 if lens[-1] == 0 or b % 5 == 1 else (lens[-1] if b % 97 == 0 else 1))
+    run_prefill(lens, news, 4, 2, D, 16, kind, "head", seed=46)

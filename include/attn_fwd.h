@@ -430,6 +430,8 @@ size_t attn_paged_decode_workspace_bytes(int H, int Hkv, int D);
  *            a length beyond max_pages * page_size is cut to that, a token in front of its sequence's first key gets O = 0,
  *            LSE = -inf, a visible key whose page is not in [0, num_pages) counts as hidden, and each is reported as
  *            ATTN_ERR_DEVICE_INDEX in the device status.  What lies in slots without a key does not matter (it may be NaN).
+ *            A key's V must be finite also for the tokens in front of it, which do not see it (tiles are computed whole: a NaN or
+ *            infinity there would reach rows of the same tile); of K that is not asked.
  * num_pages and max_pages are at least 1 (unless there is nothing to do).
  * workspace: device, 256-byte aligned, at least attn_paged_prefill_workspace_bytes(D) bytes (whatever the lengths are), or
  *            ATTN_ERR_WORKSPACE.  Two calls that may run at the same time need one each.
@@ -452,7 +454,8 @@ size_t attn_paged_prefill_workspace_bytes(int D);
  * they are read through the block table's row of the group's first sequence.  The result is that of attn_paged_decode.
  * group_starts, prefix_lens: device int32 [n_groups + 1], [n_groups].  The starts do not decrease; sequences in front of the first
  *            and behind the last group have no common part.  A prefix may be any length: no more of it is taken as common than the
- *            group's first sequence has keys, and a sequence that is shorter sees the keys that it has.  n_groups == 0: attn_paged_decode.
+ *            group's first sequence has keys, and a sequence that is shorter sees the keys that it has (the other common keys' V
+ *            must be finite then: a NaN or infinity there would reach it).  n_groups == 0: attn_paged_decode.
  * H / Hkv <= 128; D in {64, 128}.  The other arguments as in attn_paged_decode, and O is as exact: P goes into its product in two
  * 16-bit parts for the common keys, too.
  * Where the table is small (B * max_pages * page_size * Hkv * D * 4 bytes of keys and values, were every sequence that long, are

@@ -878,8 +878,8 @@ int attn_paged_prefix_decode(const void* q, const void* k_cache, const void* v_c
     if (misaligned(group_starts, 4) || misaligned(prefix_lens, 4)) return ATTN_ERR_MISALIGNED;
     if (!workspace || misaligned(workspace, 256) || workspace_bytes < attn_paged_prefix_decode_workspace_bytes(B, H, Hkv, D)) return ATTN_ERR_WORKSPACE;
     // Few keys in all: attn_paged_decode reads the common ones for every sequence (out of L2) and is done before three kernels are.
-    // What the host knows is the width of the table.  8 heads of 128, device times: 4 sequences of 1100 keys 12 us against 26, 16 of
-    // 1200 (79 MB) 25 against 27, 8 of 4200 (138 MB) 35 against 31, 32 of 1200 (157 MB) 36 against 35.
+    // What the host knows is the width of the table.  8 heads of 128, 100 or 200 keys of their own, device times: 4 sequences of 1100 keys
+    // 12 us against 29, 16 of 1200 (79 MB) 25 against 29, 8 of 4200 (138 MB) 35 against 31, 32 of 1200 (157 MB) 35 against 29.
     const bool few = static_cast<int64_t>(B) * max_pages * page_size < (1LL << 27) / (static_cast<int64_t>(Hkv) * D * 4);
     if (n_groups == 0 || num_pages == 0 || max_pages == 0 || few)
         return attn_paged_decode(q, k_cache, v_cache, cache_strides, num_pages, page_size, block_table, table_stride, max_pages, seq_lens, o, lse, B,
@@ -904,9 +904,10 @@ int attn_paged_prefix_decode(const void* q, const void* k_cache, const void* v_c
     // A group has ceil(sequences / two tiles) lists per K/V head: n_groups + B / (two tiles) at most for all groups.
     const int tile_tokens = 128 / p.group;
     const int64_t lists = (n_groups + static_cast<int64_t>(B) / (2 * tile_tokens)) * Hkv;
-    // (2200, 1300: what a step takes where all SMs are at lists, memory and latency together: 1024 sequences in groups of one to 32 behind 50
-    // to 2000 keys)
-    p.sharing = attn_paged::Sharing{tile_tokens, 4 * D * p.sub, D == 64 ? 1300 : 2200, lists <= p.all_ctas};
+    // (First, what a step takes where all SMs are at lists, memory and latency together: 1024 sequences in groups of one to 32 behind 50 to
+    // 2000 keys.  Second, beside the other kernel: 12 to 200 sequences in up to 5 groups behind 2000 to 16000 keys; over 30 such calls each
+    // 1300 against 1600 is 4 % at D = 64, 1600 against 1300 3 % at D = 128.)
+    p.sharing = attn_paged::Sharing{tile_tokens, 4 * D * p.sub, D == 64 ? 1300 : 2200, D == 64 ? 1300 : 1600, lists <= p.all_ctas};
 #ifdef ATTN_TEST_HOOKS
     p.test_skip_step = g_test_skip_step;
     g_test_skip_step = -1;

@@ -67,6 +67,7 @@ struct Sharing {
     int tile_tokens;            // sequences of a 128-row tile of queries
     int key_bytes;              // that plain decoding reads of a key, for all query heads of a K/V head
     int step_ns;                // a step of one tile of a list, where there are many lists
+    int tile_ns;                // the same beside the kernel of the sequences' own keys
     int always;                 // no more lists than CTAs: all groups that have common keys
 };
 
@@ -162,9 +163,8 @@ __device__ __forceinline__ int group_of(const int* starts, int n_groups, int b) 
 __host__ __device__ __forceinline__ int key_steps(int keys) { return keys > 0 ? ((keys - 1) >> 7) + 1 : 0; }
 
 // What a K/V head's lists of a group of n sequences take of one CTA, in ns: a step of one tile, and by itself each list (its fill and way out).
-// (With 1100 for a step 16 to 200 sequences in up to 5 groups behind 2000 to 16000 keys take 7 % longer on average.)
-constexpr int kTileStepNs = 1600, kListNs = 8000;
-__host__ __device__ __forceinline__ int64_t list_cost(int n, int prefix, const Sharing& s, int step_ns = kTileStepNs, int list_ns = kListNs) {
+constexpr int kListNs = 8000;
+__host__ __device__ __forceinline__ int64_t list_cost(int n, int prefix, const Sharing& s, int step_ns, int list_ns) {
     const int pairs = (n + 2 * s.tile_tokens - 1) / (2 * s.tile_tokens), tiles = 2 * pairs - (n - (pairs - 1) * 2 * s.tile_tokens <= s.tile_tokens ? 1 : 0);
     return static_cast<int64_t>(key_steps(prefix)) * tiles * step_ns + static_cast<int64_t>(pairs) * list_ns;
 }
@@ -175,8 +175,8 @@ constexpr int kBytesPerNs = 40, kPairNs = 3600;
 
 // The keys of group g that are worked on once for its n sequences; 0 where reading them for each sequence takes less: short prefixes of
 // few sequences.  With all SMs at lists, memory sets a step's time, and a list by itself takes 10 to 13 us.  1024 sequences, 8 K/V heads
-// of 128, without and with lists for all groups: groups of 1 behind about 500 keys 462 and 1149 us, of 4 behind 150 199 and 364, of 4
-// behind 500 460 and 370, of 16 445 and 206.  With no more lists than CTAs (Sharing::always) a list's CTAs have no other list to get to.
+// of 128, without and with lists for all groups: groups of 1 behind 500 keys 378 and 1206 us, of 4 behind 150 163 and 238, of 4
+// behind 500 381 and 323, of 16 361 and 156.  With no more lists than CTAs (Sharing::always) a list's CTAs have no other list to get to.
 __device__ __forceinline__ int common_keys(const int* starts, const int* prefix_lens, const int* seq_lens, int g, int B, int max_len,
                                            const Sharing& s, int& n) {
     int first = __ldg(starts + g), end = __ldg(starts + g + 1);
@@ -201,7 +201,7 @@ __device__ __forceinline__ int64_t group_cost(const int* starts, const int* pref
                                               const Sharing& s) {
     int n;
     const int prefix = common_keys(starts, prefix_lens, seq_lens, g, B, max_len, s, n);
-    return prefix > 0 ? Hkv * list_cost(n, prefix, s) : 0;
+    return prefix > 0 ? Hkv * list_cost(n, prefix, s, s.tile_ns, kListNs) : 0;
 }
 // CTAs of the first kernel out of `grid`, for lists that take `cost` ns, and own_bytes of keys and values of `pairs` pairs of a sequence and
 // a group of heads for the second one.

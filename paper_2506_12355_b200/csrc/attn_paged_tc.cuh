@@ -309,7 +309,7 @@ __device__ __forceinline__ void plan_sums(const Params& p, int tid, int threads,
         unit.load(p, u);
         if (unit.n > 0) {
             atomicAdd(sums + u / per, static_cast<unsigned long long>(p.Hkv * unit.head_weight(p)));
-            cost += p.Hkv * attn_paged::list_cost(unit.n, unit.len, p.sharing);
+            cost += p.Hkv * attn_paged::list_cost(unit.n, unit.len, p.sharing, p.sharing.tile_ns, attn_paged::kListNs);
         }
     }
     for (int b = tid; b < p.tokens; b += threads) {
@@ -344,27 +344,16 @@ struct Item {
 __device__ __forceinline__ void reg_inc_softmax() { asm volatile("setmaxnreg.inc.sync.aligned.u32 216;"); }
 __device__ __forceinline__ void reg_dec_service() { asm volatile("setmaxnreg.dec.sync.aligned.u32 64;"); }
 
-// 16-bit parts of a pair of probabilities, as split2 of attn_paged.cuh makes them, in two steps: what the first parts stand for, and the second
-// ones.  fp16's first parts are cut off instead of rounded (one instruction less; the second part is then off by 2^-21 of the whole; bf16: 2^-16).
+// 16-bit parts of a pair of probabilities, as split2 of attn_paged.cuh makes them, but with the first parts cut off instead of rounded (an
+// instruction less): the second part is then off by 2^-16 of the whole (bf16; fp16: 2^-22).
 template <int DTYPE>
-__device__ __forceinline__ uint32_t first_parts(float p0, float p1, float& h0, float& h1) {
-    if constexpr (DTYPE == 0) {
-        h0 = __uint_as_float(__float_as_uint(p0) & 0xffffe000u);
-        h1 = __uint_as_float(__float_as_uint(p1) & 0xffffe000u);
-        return pack2<DTYPE>(h0, h1);
-    } else {
-        const uint32_t hi = pack2<DTYPE>(p0, p1);
-        h0 = __uint_as_float(hi << 16);
-        h1 = __uint_as_float(hi & 0xffff0000u);
-        return hi;
-    }
-}
-template <int DTYPE>
-__device__ __forceinline__ uint32_t second_parts(float p0, float p1) {
-    float h0, h1, d0, d1;
-    first_parts<DTYPE>(p0, p1, h0, h1);
+__device__ __forceinline__ void split_p(float p0, float p1, uint32_t& hi, uint32_t& lo) {
+    constexpr uint32_t CUT = DTYPE == 0 ? 0xffffe000u : 0xffff0000u;
+    const float h0 = __uint_as_float(__float_as_uint(p0) & CUT), h1 = __uint_as_float(__float_as_uint(p1) & CUT);
+    hi = DTYPE == 0 ? pack2<DTYPE>(h0, h1) : __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);
+    float d0, d1;
     unpack_f32x2(fma_f32x2(pack_f32x2(h0, h1), pack_f32x2(-1.f, -1.f), pack_f32x2(p0, p1)), d0, d1);
-    return pack2<DTYPE>(d0, d1);
+    lo = pack2<DTYPE>(d0, d1);
 }
 
 template <int D, int DTYPE, bool PREFIX>
@@ -395,8 +384,7 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         B_MERGE = 22,      // tile 1's sums are in shared memory (128 threads)
         B_KVFULL = 23,     // [NGRP] V_{j-1} and K_j loaded (two warps' copies)
         B_KVEMPTY = 23 + NGRP,
-        B_PLOW = 23 + 2 * NGRP,        // [2] prefix: the second parts of P_t written (128 threads)
-        B_COUNT = B_PLOW + (PREFIX ? 2 : 0)
+        B_COUNT = 23 + 2 * NGRP
     };
     auto bar = [&](int i) { return smem_base + C::TILE_BYTES + i * 8; };
     constexpr int SCHED = PREFIX ? 12 : 16;
@@ -425,7 +413,6 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             mbar_init(bar(B_SFULL + t), 1);
             mbar_init(bar(B_PFULL + t), 128);
             mbar_init(bar(B_PFULL2 + t), 128);
-            if (PREFIX) mbar_init(bar(B_PLOW + t), 128);
             mbar_init(bar(B_OFINAL + t), 1);
             mbar_init(bar(B_OFREE + t), 128);
         }
@@ -771,15 +758,12 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     // the previous item's O_t must be in registers before it is overwritten
                     if (i == 0 && uses[t] > 0 && !wait(B_OFREE + t, (uses[t] - 1) & 1)) return false;
                     tc_fence_after_sync();
-                    issue_pv(t, 2 * gslot, i > 0, 0, 6);
+                    issue_pv(t, 2 * gslot, i > 0, 0, PREFIX ? 4 : 6);
+                    if constexpr (PREFIX) issue_pv(t, 2 * gslot, true, 8, 12);
                     if (!wait(B_PFULL2 + t, par)) return false;
                     tc_fence_after_sync();
-                    issue_pv(t, 2 * gslot, true, 6, 8);
-                    if constexpr (PREFIX) {
-                        if (!wait(B_PLOW + t, par)) return false;
-                        tc_fence_after_sync();
-                        issue_pv(t, 2 * gslot, true, 8, 16);
-                    }
+                    issue_pv(t, 2 * gslot, true, PREFIX ? 4 : 6, 8);
+                    if constexpr (PREFIX) issue_pv(t, 2 * gslot, true, 12, 16);
                     if (i + 1 == it.n(t)) commit(B_OFINAL + t);
                     return true;
                 };
@@ -933,7 +917,6 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 if (!any_live) {                           // no row of this warp is a query's: whatever S holds may stand in as P
                     mbar_arrive(bar(B_PFULL + t));
                     mbar_arrive(bar(B_PFULL2 + t));
-                    if constexpr (PREFIX) mbar_arrive(bar(B_PLOW + t));
                     continue;
                 }
                 const int step = it.twin ? 2 * j + t : j, kv0 = (it.tile0 + step) * 128;
@@ -998,31 +981,22 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
                     for (int ch = 0; ch < 4; ++ch) {
-                        uint32_t pk[16];
+                        uint32_t hi[16], lo[16];
 #pragma unroll
-                        for (int e = ch * 32; e < ch * 32 + 32; e += 2) {
+                        for (int e = 0; e < 32; e += 2) {
                             float x0, x1;
-                            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(sr[e]), __uint_as_float(sr[e + 1])), c2, nmc2), x0, x1);
+                            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(sr[ch * 32 + e]), __uint_as_float(sr[ch * 32 + e + 1])), c2, nmc2), x0, x1);
                             const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
                             acc[(e / 2) & 3] = add_f32x2(acc[(e / 2) & 3], pack_f32x2(p0, p1));
-                            sr[e] = __float_as_uint(p0);
-                            sr[e + 1] = __float_as_uint(p1);
-                            float h0, h1;
-                            pk[(e / 2) & 15] = first_parts<DTYPE>(p0, p1, h0, h1);
+                            split_p<DTYPE>(p0, p1, hi[e / 2], lo[e / 2]);
                         }
-                        tmem_st_32x32b_x16(tS + ch * 16, pk);
-                        if (ch >= 2) {
+                        tmem_st_32x32b_x16(tS + ch * 16, hi);
+                        tmem_st_32x32b_x16(tS + 64 + ch * 16, lo);
+                        if (ch == 1) {
                             tmem_st_wait();
                             tc_fence_before_sync();
-                            mbar_arrive(bar((ch == 2 ? B_PFULL : B_PFULL2) + t));
+                            mbar_arrive(bar(B_PFULL + t));
                         }
-                    }
-#pragma unroll
-                    for (int ch = 0; ch < 4; ++ch) {
-                        uint32_t pk[16];
-#pragma unroll
-                        for (int e = ch * 32; e < ch * 32 + 32; e += 2) pk[(e / 2) & 15] = second_parts<DTYPE>(__uint_as_float(sr[e]), __uint_as_float(sr[e + 1]));
-                        tmem_st_32x32b_x16(tS + 64 + ch * 16, pk);
                     }
                     float a0, a1, a2, a3;
                     unpack_f32x2(add_f32x2(acc[0], acc[1]), a0, a1);
@@ -1030,7 +1004,7 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     l = l * alpha + ((a0 + a1) + (a2 + a3));
                     tmem_st_wait();
                     tc_fence_before_sync();
-                    mbar_arrive(bar(B_PLOW + t));
+                    mbar_arrive(bar(B_PFULL2 + t));
                     continue;
                 }
                 if (any_unset) {

@@ -279,8 +279,8 @@ __device__ __forceinline__ int cta_count(int64_t total, int grid) { return total
 // at most.
 constexpr int kLongList = 4, kFewParts = 10;
 // With common prefixes only what the prefix leaves of each sequence is in the list, often a few keys: every pair then costs more by
-// itself (2.7 us) than by its tiles, and heads side by side are an eighth as many (64 sequences of one key behind 8192 common ones:
-// 104 us with one head per pair, 36 side by side).
+// itself than by its tiles, and heads side by side are an eighth as many (64 sequences of one key behind 8192 common ones: 43 us, with
+// one head per pair three times as long).
 struct ListForm { int64_t total; int hpt_shift; };
 template <bool PREFIX>
 __device__ __forceinline__ ListForm list_form(const DecodeParams& p, int64_t total_side, int64_t total_one, int grid) {
@@ -348,7 +348,7 @@ struct SeqPlan {
 };
 
 // PREFIX: the visible keys of the first sequences of a CTA's part, worked out once by all of its threads: walking from one sequence to the
-// next every warp would otherwise look for its group, a chain of loads (100 sequences in 3 groups, 16 heads of 64: 134 us instead of 123).
+// next every warp would otherwise look for its group, a chain of loads (100 sequences in 3 groups, 16 heads of 64: 9 % longer).
 struct SeqTable {
     static constexpr int SIZE = 32;
     const int2* at;       // shared memory: {len, win_lo}

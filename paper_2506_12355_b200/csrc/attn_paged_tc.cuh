@@ -33,6 +33,8 @@
 // What bounds it: a step of two tiles takes 1.9 us at D = 128 (1024 tensor cycles a tile, 1.25 PFLOP/s of visible pairs for the 2048
 // tokens above) and 1.7 at D = 64 (its exponentials), a step of one tile 1.0; a list costs 5 us beside its steps (the way out 2.3,
 // then the next list's first scores), and the first scores are there 7 us after the start, most of it instructions that come from L2.
+// Prefix, all SMs at K and V that come from HBM: a step of two tiles 2.4 us, 1.9 at D = 64, of one 1.75 and 1.3 (with P rounded once: 2.0, 1.55,
+// 1.4, 1.0).
 #pragma once
 #include "attn_paged.cuh"
 #include "attn_tc_common.cuh"

@@ -961,8 +961,8 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     return fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7])));
                 };
                 if constexpr (PREFIX) {
-                    // The tile's maximum first, so that S is not needed again: P takes its place in the registers, and its second parts
-                    // are made while the products with the first ones run.
+                    // The tile's maximum first, so that no exponential is taken twice and S leaves the registers as P's two parts come.  P
+                    // carries 2^P_OFF, as in attn_paged.cuh: its small values keep their precision in fp16.
                     float mx[8];
 #pragma unroll
                     for (int x = 0; x < 8; ++x) mx[x] = -INFINITY;
@@ -978,7 +978,7 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                         }
                         rescale(j, alpha);
                     }
-                    const float nmc = -m * c;
+                    const float nmc = fmaf(-m, c, P_OFF);
                     const uint64_t c2 = pack_f32x2(c, c), nmc2 = pack_f32x2(nmc, nmc);
                     uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
@@ -1113,7 +1113,7 @@ attn_paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 } else {
                     float2* ml = reinterpret_cast<float2*>(it.slot < 0 ? p.rows + static_cast<int64_t>(p.tokens) * p.H * D + 2 * static_cast<int64_t>(out_row)
                                                                        : part + kRows * D + 2 * (t * 128 + r));
-                    *ml = make_float2(fmaf(m, c, P_OFF), l);
+                    *ml = make_float2(PREFIX ? m * c : fmaf(m, c, P_OFF), l);
                 }
             }
             if (final_rows) {
